@@ -15,7 +15,9 @@
  *   gracekv_gather       ragged compressed cache + index map  (App. A.5)
  *
  * Decoding on the result (gracekv_decode_*, App. A.3 Eq. app_decode_logit)
- * follows at the end of this header.
+ * follows after the pass; then the serving calls around it: the prompt's own
+ * attention (gracekv_prompt_*) and a paged cache of many requests
+ * (gracekv_paged_*).
  *
  * Conventions for every call:
  *   - Tensor arguments are DEVICE pointers to contiguous row-major arrays owned
@@ -48,7 +50,7 @@
 extern "C" {
 #endif
 
-#define GRACEKV_ABI_VERSION 4
+#define GRACEKV_ABI_VERSION 5
 
 typedef enum {
     GKV_OK = 0,
@@ -456,6 +458,142 @@ gkv_status gracekv_decode_attention(const gkv_decode_cache *c, int32_t l0, int32
  * gracekv_decode_attention on this workspace gave up, GKV_EINVAL when the
  * offsets of a call pointed past n_entries, else GKV_OK. */
 gkv_status gracekv_decode_status(void *workspace, void *stream);
+
+/*
+ * The prompt's attention (the prefill whose K and V the pass compresses):
+ * causal softmax attention of packed sequences with grouped heads.  No
+ * context, no allocation.  Sequence s holds the query rows
+ * [cu_q[s], cu_q[s + 1]) and the key rows [cu_k[s], cu_k[s + 1]); with nq and
+ * nk their numbers, its query i sees its keys j <= i + nk - nq (the queries
+ * are the last nq of the nk positions: nk = nq for a whole prompt, nk > nq
+ * for a chunk that continues one).  Query head h reads KV head h / (Hq / G):
+ *     x_j = q . k_j / sqrt(d),  out = sum_j softmax(x)_j v_j,
+ *     lse = log sum_j exp(x_j) ;
+ * a query that sees no key gives out 0 and lse -inf.  Rows of q that belong to
+ * no sequence are not written.
+ *
+ * All pointers DEVICE memory, owned by the caller.  q, out: rows of tokens,
+ * element (token, head, channel) at token * ts + head * hs + channel with the
+ * tensor's own strides in elements (so [N][Hq][d], [Hq][N][d] and a slice of a
+ * fused projection all pass); k, v the same with G heads.  out may not overlap
+ * the inputs.  n_q and n_k bound the rows: a sequence whose cu words run
+ * backwards or past them is skipped and reported by gracekv_prompt_status.
+ * d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED); pointers on 16
+ * bytes, strides multiples of 16 bytes and not negative, lse on 4 bytes,
+ * n_seqs >= 0, n_q and n_k below 2^31.  Values: bf16 products are exact, sums
+ * fp32; the softmax weights of bf16 inputs are rounded to bf16 for the value
+ * product and the output once to bf16; fp32 inputs stay fp32 throughout.
+ * Keys and values of rows outside a sequence do not reach it whatever they
+ * hold; a non-finite value inside a sequence may reach any of its queries.
+ */
+typedef struct {
+    int32_t G, Hq, d, dtype;          /* KV heads, query heads, head dim, gkv_dtype of q, k, v, out */
+    int32_t n_seqs;
+    int64_t n_q, n_k;                 /* rows of q, out, lse; rows of k, v */
+    const int32_t *cu_q, *cu_k;       /* [n_seqs + 1] */
+    const void *q, *k, *v;
+    void *out;
+    float *lse;                       /* [n_q][Hq], nullable */
+    int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
+} gkv_prompt;
+
+/* Bytes of the device workspace of gracekv_prompt_attention: a function of
+ * G, Hq, d and dtype alone (the other fields are not read), so one workspace
+ * serves every call of a model.  The caller allocates it 256-byte aligned and
+ * zeroes it once.  One workspace serves one stream at a time. */
+gkv_status gracekv_prompt_workspace_size(const gkv_prompt *p, size_t *bytes);
+
+/* Enqueues the attention on `stream`.  Errors: GKV_EINVAL (shapes, strides,
+ * pointers), GKV_EUNSUPPORTED, GKV_ECUDA. */
+gkv_status gracekv_prompt_attention(const gkv_prompt *p, void *workspace, void *stream);
+
+/* Synchronises `stream` and reports (then clears) the workspace's status word:
+ * GKV_ETIMEOUT when a bounded device-side wait gave up, GKV_EINVAL when cu
+ * words did not fit n_q / n_k or ran backwards, else GKV_OK. */
+gkv_status gracekv_prompt_status(void *workspace, void *stream);
+
+/*
+ * A paged cache of many requests.  One pool of pages holds the entries of
+ * every (layer, request, KV head); a page belongs to one of them.  The
+ * lengths are per (layer, request, KV head), as the global allocation makes
+ * them, and every entry carries log m (App. A.3, Eq. app_decode_logit):
+ * entries of the compressed cache, then the tokens generated since.
+ *
+ * All pointers DEVICE memory, owned by the caller.  Entry i of (l, b, g) is
+ * row i % page_size of page table[l][b][g][i / page_size].  Table words past a
+ * length are not read.  A page number outside [0, n_pages), or a length past
+ * max_pages * page_size, is not followed: the entry is skipped and
+ * gracekv_paged_status reports GKV_EINVAL.  K, V on 16 bytes, the others on 4;
+ * d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED), page_size >= 1,
+ * n_pages * page_size below 2^31.
+ */
+typedef struct {
+    int32_t L, B, G, Hq, d, dtype;    /* layers, request slots, KV heads, query heads, head dim, gkv_dtype */
+    int32_t page_size, max_pages;
+    int64_t n_pages;
+    void *K, *V;                      /* [n_pages][page_size][d] */
+    float *log_m;                     /* [n_pages][page_size]; NULL: every entry has log m = 0 */
+    const int32_t *table;             /* [L][B][G][max_pages] */
+    int32_t *lens;                    /* [L][B][G] entries */
+    double rope_base;                 /* of gracekv_paged_append (0: no rotation) */
+} gkv_paged_cache;
+
+/* Bytes of the device workspace of the calls below for this geometry (L, B,
+ * G, Hq, d, dtype).  The caller allocates it 256-byte aligned and zeroes it
+ * once; every call leaves it zeroed again, the status word aside.  One
+ * workspace serves one stream at a time. */
+gkv_status gracekv_paged_workspace_size(const gkv_paged_cache *c, size_t *bytes);
+
+/* A packed cache (gracekv_gather's K_out, V_out [n_entries][d], log_m
+ * [n_entries], offsets [L G + 1], all device) becomes request b's entries in
+ * every layer: entry e of (l, g) goes to its index e - offsets[l G + g], and
+ * lens[l][b][g] = offsets[l G + g + 1] - offsets[l G + g].  The table must hold
+ * pages for them.  log_m may be NULL (written as 0); it must be NULL when the
+ * cache has none.  Offsets past n_entries or running backwards give that head
+ * length 0 and GKV_EINVAL from gracekv_paged_status; so do entries past
+ * max_pages pages (the length is cut there).  Errors: GKV_EINVAL, GKV_ECUDA. */
+gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K, const void *V,
+                              const float *log_m, const int64_t *offsets, int64_t n_entries, void *workspace,
+                              void *stream);
+
+/* The lengths of every layer grow by the tokens of a step: lens[l][b][g] +=
+ * cu_new[b + 1] - cu_new[b] (device [B + 1]; NULL: one token for every (l, b, g)
+ * of a length above 0, the others stay idle).  Once per step, before the
+ * layers' appends.  Errors: GKV_EINVAL, GKV_ECUDA. */
+gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream);
+
+/* The new tokens of layer l: keys rotated to their positions and stored, values
+ * stored, log m = 0 (App. A.5: appended tokens have multiplicity 1), queries
+ * rotated into q_out.  Token t belongs to request b with cu_new[b] <= t <
+ * cu_new[b + 1] (device [B + 1]; NULL: n_tokens = B, token t is request t's)
+ * and becomes entry lens[l][b][g] - (cu_new[b + 1] - t): the lengths count the
+ * new tokens already (gracekv_paged_advance).  A negative index (an idle
+ * request) stores nothing.  Rotation of a vector x to position p: the pair
+ * (x[i], x[i + d/2]) turns by p * rope_base^(-2 i / d), computed in fp32 from an
+ * angle that is exact to 2^-26 turns at every int32 position, rounded once.
+ *   pos [n_tokens] int32; k, v [n_tokens][G][d], q and q_out [n_tokens][Hq][d],
+ *   token and head strides in elements as in gkv_prompt; q (with q_out) may be
+ *   NULL.  q_out may be q itself.
+ * Errors: GKV_EINVAL (n_tokens < 0, n_tokens != B without cu_new, pointers,
+ * strides), GKV_ECUDA. */
+gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, int32_t n_tokens, const int32_t *cu_new,
+                                const int32_t *pos, const void *k, int64_t k_ts, int64_t k_hs, const void *v,
+                                int64_t v_ts, int64_t v_hs, const void *q, int64_t q_ts, int64_t q_hs, void *q_out,
+                                int64_t qo_ts, int64_t qo_hs, void *workspace, void *stream);
+
+/* Attention of one token per request over layer l: q [B][Hq][d] (rotated; its
+ * own entry appended), out [B][Hq][d] of the cache's dtype:
+ *     x_e = q_h . k_e / sqrt(d) + log m_e,  out_h = sum_e softmax(x)_e v_e
+ * over the lens[l][b][g] entries; a length of 0 gives 0.  page_size must be a
+ * multiple of 16 here (GKV_EUNSUPPORTED).  Errors: GKV_EINVAL,
+ * GKV_EUNSUPPORTED, GKV_ECUDA. */
+gkv_status gracekv_paged_attention(const gkv_paged_cache *c, int32_t l, const void *q, void *out, void *workspace,
+                                   void *stream);
+
+/* Synchronises `stream` and reports (then clears) the workspace's status word:
+ * GKV_ETIMEOUT when a bounded device-side wait gave up, GKV_EINVAL when a
+ * call met a page number, length or offset it did not follow, else GKV_OK. */
+gkv_status gracekv_paged_status(void *workspace, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,236 @@
+// paged.cu -- writing the paged cache (gracekv_paged_load / _advance /
+// _append).
+//
+// load: the packed cache of a compressed request becomes its pages, entry for
+// entry: one read and one write of 2 d elements and log m per entry.
+//
+// append: the pair (a, b) = (x[i], x[i + d/2]) of a key or query turns by the
+// angle phi = p theta_i, theta_i = base^(-2i/d):  (a cos phi - b sin phi,
+// a sin phi + b cos phi).  p can be large while only phi mod 2 pi counts, so
+// the angle is kept in turns as a 64-bit fraction: F_i = 2^64 theta_i / (2 pi)
+// (host, fp64), and p F_i mod 2^64 is the fraction of a turn -- one integer
+// product, exact up to p times F_i's rounding (below 2^-21 of 2^-11 turns for
+// any int32 p) -- whose upper 32 bits go to sincospi.  A thread holds 16 bytes
+// of each half of a row, so the rotation stays in its registers; its sines and
+// cosines serve every head it takes.
+#include "paged.cuh"
+
+#include <math.h>
+
+namespace gkv {
+namespace {
+
+using namespace serve;
+
+struct Turns {
+    unsigned long long f[64];      // 2^64 theta_i / (2 pi)
+};
+
+struct AppendArgs {
+    Paged c;
+    int l, n_tokens;
+    const int32_t *cu_new, *pos;
+    const char *k, *v, *q;
+    char *q_out;
+    int64_t k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, qo_ts, qo_hs;     // bytes
+    int rotate;
+    int *status;
+};
+
+__device__ __forceinline__ uint4 ld16(const char *p) { return __ldg(reinterpret_cast<const uint4 *>(p)); }
+__device__ __forceinline__ void st16(char *p, uint4 x) { *reinterpret_cast<uint4 *>(p) = x; }
+
+template <typename T>
+__device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, const float *sn) {
+    constexpr int N = 16 / sizeof(T);
+    T xa[N], xb[N];
+    *reinterpret_cast<uint4 *>(xa) = a;
+    *reinterpret_cast<uint4 *>(xb) = b;
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        const float u = to_f(xa[j]), w = to_f(xb[j]);
+        put(&xa[j], u * cs[j] - w * sn[j]);
+        put(&xb[j], u * sn[j] + w * cs[j]);
+    }
+    a = *reinterpret_cast<uint4 *>(xa);
+    b = *reinterpret_cast<uint4 *>(xb);
+}
+
+// One thread per (token, row of the token, 16-byte chunk of each half); rows:
+// G keys, G values, Hq queries.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
+    constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
+    const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int ch = (int)(i % CH);
+    const int r = (int)(i / CH % rows);
+    const int64_t t = i / CH / rows;
+    if (t >= a.n_tokens) return;
+    const bool is_q = r >= 2 * a.c.G, is_v = !is_q && r >= a.c.G;
+    const int h = is_q ? r - 2 * a.c.G : is_v ? r - a.c.G : r;
+    float cs[N], sn[N];
+    if (!is_v && a.rotate) {
+        const long long p = a.pos[t];
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const int hi = (int)(((unsigned long long)p * turns.f[ch * N + j]) >> 32);
+            sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
+        }
+    }
+    const char *src = (is_q ? a.q + t * a.q_ts + h * a.q_hs : is_v ? a.v + t * a.v_ts + h * a.v_hs
+                                                                  : a.k + t * a.k_ts + h * a.k_hs) + ch * 16;
+    uint4 x = ld16(src), y = ld16(src + RB / 2);
+    if (!is_v && a.rotate) turn16<T>(x, y, cs, sn);
+    char *dst;
+    if (is_q) {
+        dst = a.q_out + t * a.qo_ts + h * a.qo_hs;
+    } else {
+        int b = (int)t, tail = 1;
+        if (a.cu_new) {
+            b = seq_of(a.cu_new, a.c.B, t);
+            if (t < a.cu_new[b] || t >= a.cu_new[b + 1]) return;        // a token of no request
+            tail = a.cu_new[b + 1] - (int)t;
+        }
+        const int64_t s = ((int64_t)a.l * a.c.B + b) * a.c.G + h;
+        const int idx = a.c.lens[s] - tail;
+        if (idx < 0) return;
+        const int64_t row = entry_row(a.c, s, idx, a.status);
+        if (row < 0) return;
+        dst = (is_v ? a.c.V : a.c.K) + row * RB;
+        if (!is_v && ch == 0 && a.c.log_m) a.c.log_m[row] = 0.f;
+    }
+    st16(dst + ch * 16, x);
+    st16(dst + ch * 16 + RB / 2, y);
+}
+
+__global__ void paged_advance_kernel(int32_t *lens, const int32_t *cu_new, int n, int B, int G) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= n) return;
+    const int b = i / G % B, len = lens[i];
+    lens[i] = len + (cu_new ? max(0, cu_new[b + 1] - cu_new[b]) : (len > 0));
+}
+
+struct LoadArgs {
+    Paged c;
+    int b;
+    const char *K, *V;
+    const float *log_m;
+    const int64_t *off;
+    int64_t n_entries;
+    int *status;
+};
+
+// The heads' lengths (offsets that do not fit give 0), one thread per (l, g).
+__global__ void paged_load_lens_kernel(const LoadArgs a) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= a.c.L * a.c.G) return;
+    const int64_t lo = a.off[i], hi = a.off[i + 1], cap = (int64_t)a.c.page_size * a.c.max_pages;
+    int64_t n = hi - lo;
+    if (lo < 0 || n < 0 || hi > a.n_entries) { atomicOr(a.status, kStRange); n = 0; }
+    if (n > cap) { atomicOr(a.status, kStRange); n = cap; }
+    a.c.lens[((int64_t)(i / a.c.G) * a.c.B + a.b) * a.c.G + i % a.c.G] = (int)n;
+}
+
+// One thread per (entry, 16 bytes of its key and of its value).
+template <int RB>
+__global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
+    constexpr int CH = RB / 16;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, e = i / CH;
+    const int ch = (int)(i % CH);
+    if (e >= a.n_entries) return;
+    int lo = 0, hi = a.c.L * a.c.G;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.off[mid] <= e) lo = mid; else hi = mid;
+    }
+    const int64_t o0 = a.off[lo], o1 = a.off[lo + 1];
+    if (o0 < 0 || e < o0 || e >= o1 || o1 > a.n_entries || e - o0 >= (int64_t)a.c.page_size * a.c.max_pages) return;
+    const int64_t s = ((int64_t)(lo / a.c.G) * a.c.B + a.b) * a.c.G + lo % a.c.G;
+    const int64_t row = entry_row(a.c, s, (int)(e - o0), a.status);
+    if (row < 0) return;
+    st16(a.c.K + row * RB + ch * 16, ld16(a.K + e * RB + ch * 16));
+    st16(a.c.V + row * RB + ch * 16, ld16(a.V + e * RB + ch * 16));
+    if (ch == 0 && a.c.log_m) a.c.log_m[row] = a.log_m ? a.log_m[e] : 0.f;
+}
+
+}  // namespace
+}  // namespace gkv
+
+using namespace gkv;
+
+extern "C" gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K, const void *V,
+                                         const float *log_m, const int64_t *offsets, int64_t n_entries,
+                                         void *workspace, void *stream) {
+    const gkv_status st = check_paged(c);
+    if (st != GKV_OK) return st;
+    if (b < 0 || b >= c->B || !offsets || !al(offsets, 8) || n_entries < 0 || n_entries >= (1LL << 31)) return GKV_EINVAL;
+    if (n_entries > 0 && (!K || !V || !al(K, 16) || !al(V, 16))) return GKV_EINVAL;
+    if (!al(log_m, 4) || (log_m && !c->log_m) || !workspace || !al(workspace, 256)) return GKV_EINVAL;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const LoadArgs a{paged_of(c), b, static_cast<const char *>(K), static_cast<const char *>(V), log_m, offsets,
+                     n_entries, static_cast<int *>(workspace)};
+    paged_load_lens_kernel<<<(c->L * c->G + 255) / 256, 256, 0, s>>>(a);
+    const int rb = c->d * elem_bytes(c->dtype);
+    const unsigned n = (unsigned)((n_entries * (rb / 16) + 255) / 256);
+    if (n > 0) {
+        if (rb == 128) paged_load_kernel<128><<<n, 256, 0, s>>>(a);
+        else if (rb == 256) paged_load_kernel<256><<<n, 256, 0, s>>>(a);
+        else paged_load_kernel<512><<<n, 256, 0, s>>>(a);
+    }
+    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream) {
+    const gkv_status st = check_paged(c);
+    if (st != GKV_OK) return st;
+    if (!al(cu_new, 4)) return GKV_EINVAL;
+    const int n = c->L * c->B * c->G;
+    paged_advance_kernel<<<(n + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream)>>>(c->lens, cu_new, n, c->B, c->G);
+    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, int32_t n_tokens,
+                                           const int32_t *cu_new, const int32_t *pos, const void *k, int64_t k_ts,
+                                           int64_t k_hs, const void *v, int64_t v_ts, int64_t v_hs, const void *q,
+                                           int64_t q_ts, int64_t q_hs, void *q_out, int64_t qo_ts, int64_t qo_hs,
+                                           void *workspace, void *stream) {
+    const gkv_status st = check_paged(c);
+    if (st != GKV_OK) return st;
+    if (l < 0 || l >= c->L || n_tokens < 0 || (!cu_new && n_tokens != c->B) || !al(cu_new, 4)) return GKV_EINVAL;
+    if (!workspace || !al(workspace, 256)) return GKV_EINVAL;
+    if (n_tokens == 0) return GKV_OK;
+    if (!pos || !al(pos, 4) || !rows_ok(k, k_ts, k_hs, c->dtype) || !rows_ok(v, v_ts, v_hs, c->dtype)) return GKV_EINVAL;
+    if ((q != nullptr) != (q_out != nullptr)) return GKV_EINVAL;
+    if (q && (!rows_ok(q, q_ts, q_hs, c->dtype) || !rows_ok(q_out, qo_ts, qo_hs, c->dtype))) return GKV_EINVAL;
+    if (!(c->rope_base >= 0.0) || isinf(c->rope_base)) return GKV_EINVAL;
+    const int es = elem_bytes(c->dtype);
+    AppendArgs a{paged_of(c), l, n_tokens, cu_new, pos, static_cast<const char *>(k), static_cast<const char *>(v),
+                 static_cast<const char *>(q), static_cast<char *>(q_out),
+                 k_ts * es, k_hs * es, v_ts * es, v_hs * es, q_ts * es, q_hs * es, qo_ts * es, qo_hs * es,
+                 c->rope_base > 0.0, static_cast<int *>(workspace)};
+    Turns turns{};
+    if (a.rotate)
+        for (int i = 0; i < c->d / 2; i++) {
+            // theta / (2 pi) of a turn; whole turns (bases below 1) drop out
+            const double f = pow(c->rope_base, -2.0 * i / c->d) / 6.283185307179586476925287;
+            turns.f[i] = (unsigned long long)ldexp(f - floor(f), 64);
+        }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int64_t items = (int64_t)n_tokens * (2 * c->G + (q ? c->Hq : 0)) * (c->d * es / 32);
+    const int64_t blocks = (items + 255) / 256;
+    if (blocks >= (1LL << 31)) return GKV_EUNSUPPORTED;
+    const unsigned n = (unsigned)blocks;
+    if (c->dtype == GKV_BF16) {
+        if (c->d == 128) paged_append_kernel<__nv_bfloat16, 128><<<n, 256, 0, s>>>(a, turns);
+        else paged_append_kernel<__nv_bfloat16, 64><<<n, 256, 0, s>>>(a, turns);
+    } else {
+        if (c->d == 128) paged_append_kernel<float, 128><<<n, 256, 0, s>>>(a, turns);
+        else paged_append_kernel<float, 64><<<n, 256, 0, s>>>(a, turns);
+    }
+    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+extern "C" gkv_status gracekv_paged_status(void *workspace, void *stream) {
+    return serve::read_status(workspace, stream);
+}

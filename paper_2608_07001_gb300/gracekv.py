@@ -54,6 +54,23 @@ class GkvDecodeCache(C.Structure):
     ]
 
 
+class GkvPrompt(C.Structure):
+    _fields_ = [
+        ("G", C.c_int32), ("Hq", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32), ("n_seqs", C.c_int32),
+        ("n_q", C.c_int64), ("n_k", C.c_int64), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p),
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+    ] + [(n, C.c_int64) for n in ("q_ts", "q_hs", "k_ts", "k_hs", "v_ts", "v_hs", "o_ts", "o_hs")]
+
+
+class GkvPagedCache(C.Structure):
+    _fields_ = [
+        ("L", C.c_int32), ("B", C.c_int32), ("G", C.c_int32), ("Hq", C.c_int32), ("d", C.c_int32),
+        ("dtype", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int64),
+        ("K", C.c_void_p), ("V", C.c_void_p), ("log_m", C.c_void_p), ("table", C.c_void_p),
+        ("lens", C.c_void_p), ("rope_base", C.c_double),
+    ]
+
+
 class GraceKVError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"gracekv status {status}: {msg}")
@@ -69,7 +86,10 @@ EXPORTED = ["gracekv_default_params", "gracekv_budget_for_ratio", "gracekv_graph
             "gracekv_export", "gracekv_profile", "gracekv_stats", "gracekv_row_stats_noalloc",
             "gracekv_compress_host", "gracekv_export_floor", "gracekv_head_sensitivity",
             "gracekv_set_graph_queries", "gracekv_decode_workspace_size", "gracekv_decode_append",
-            "gracekv_decode_attention", "gracekv_decode_status"]
+            "gracekv_decode_attention", "gracekv_decode_status",
+            "gracekv_prompt_workspace_size", "gracekv_prompt_attention", "gracekv_prompt_status",
+            "gracekv_paged_workspace_size", "gracekv_paged_load", "gracekv_paged_advance",
+            "gracekv_paged_append", "gracekv_paged_attention", "gracekv_paged_status"]
 
 
 def lib() -> C.CDLL:
@@ -112,6 +132,16 @@ def lib() -> C.CDLL:
     L.gracekv_decode_append.argtypes = [dcp, i32, i32, i32, vp, vp, vp]
     L.gracekv_decode_attention.argtypes = [dcp, i32, i32, i32, vp, vp, vp, vp]
     L.gracekv_decode_status.argtypes = [vp, vp]
+    prp, pcp = C.POINTER(GkvPrompt), C.POINTER(GkvPagedCache)
+    L.gracekv_prompt_workspace_size.argtypes = [prp, C.POINTER(C.c_size_t)]
+    L.gracekv_prompt_attention.argtypes = [prp, vp, vp]
+    L.gracekv_prompt_status.argtypes = [vp, vp]
+    L.gracekv_paged_workspace_size.argtypes = [pcp, C.POINTER(C.c_size_t)]
+    L.gracekv_paged_load.argtypes = [pcp, i32, vp, vp, vp, vp, i64, vp, vp]
+    L.gracekv_paged_advance.argtypes = [pcp, vp, vp]
+    L.gracekv_paged_append.argtypes = [pcp, i32, i32, vp, vp] + [vp, i64, i64] * 4 + [vp, vp]
+    L.gracekv_paged_attention.argtypes = [pcp, i32, vp, vp, vp, vp]
+    L.gracekv_paged_status.argtypes = [vp, vp]
     _lib = L
     return L
 
@@ -482,3 +512,276 @@ class Decoder:
 
     def status(self, stream=None):
         _raise(lib().gracekv_decode_status(_ptr(self.workspace), _stream(stream)))
+
+
+# ---- serving: the prompt's attention and the paged cache --------------------
+_DTYPES = {torch.float32: GKV_F32, torch.bfloat16: GKV_BF16}
+
+
+def _bad(why: str):
+    return GraceKVError(GKV_EINVAL, why)
+
+
+def _rows(name: str, t: torch.Tensor, n: int, heads: int, d: int, dtype, device):
+    """(pointer, token stride, head stride) of [n, heads, d] rows with contiguous channels."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype or t.device != device:
+        raise _bad(f"{name} is {t.dtype} on {t.device}, not {dtype} on {device}")
+    if tuple(t.shape) != (n, heads, d):
+        raise _bad(f"{name} is {tuple(t.shape)}, not {(n, heads, d)}")
+    ts, hs, cs = t.stride()
+    if cs != 1:
+        raise _bad(f"the channels of {name} must be contiguous")
+    # the stride of an axis of one element is arbitrary and never used
+    return t.data_ptr(), ts if n > 1 else 0, hs if heads > 1 else 0
+
+
+def _words(name: str, t: torch.Tensor, shape, dtype, device):
+    """Pointer of a contiguous index or statistics array."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
+        raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _on(stream, *tensors):
+    """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
+    if stream is None:
+        return torch.cuda.current_stream(tensors[0].device).cuda_stream
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _empty_like_on(stream, shape, dtype, device):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class PromptAttention:
+    """Causal attention of packed prompts (gracekv_prompt_* of the C ABI).
+
+    One object holds the workspace of one stream.  q [N, Hq, d], k and v
+    [Nk, G, d] with any token and head strides of whole 16 bytes (a slice of a
+    fused projection, or K[l].transpose(0, 1) of a [L, G, T, d] cache);
+    cu_q, cu_k int32 device row bounds of the sequences (cu_k = cu_q when not
+    given).  A sequence with more keys than queries continues a prompt: its
+    queries are the last ones.
+    """
+
+    def __init__(self, *, G: int, Hq: int, d: int, dtype, device="cuda"):
+        if dtype not in _DTYPES:
+            raise _bad(f"dtype must be bf16 or fp32, not {dtype}")
+        self.G, self.Hq, self.d, self.dtype = G, Hq, d, dtype
+        self.desc = GkvPrompt(G, Hq, d, _DTYPES[dtype])
+        n = C.c_size_t()
+        _raise(lib().gracekv_prompt_workspace_size(C.byref(self.desc), C.byref(n)))
+        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=device)
+
+    def __call__(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, return_lse=False, stream=None):
+        """out [N, Hq, d] of q's dtype (or (out, lse [N, Hq] fp32) with return_lse)."""
+        p, dev = self.desc, self.workspace.device
+        cu_k = cu_q if cu_k is None else cu_k
+        n_q, n_k = q.shape[0], k.shape[0]
+        if out is None:
+            out = _empty_like_on(stream, (n_q, self.Hq, self.d), self.dtype, dev)
+        if lse is None and return_lse:
+            lse = _empty_like_on(stream, (n_q, self.Hq), torch.float32, dev)
+        p.n_seqs, p.n_q, p.n_k = cu_q.numel() - 1, n_q, n_k
+        p.cu_q = _words("cu_q", cu_q, (p.n_seqs + 1,), torch.int32, dev)
+        p.cu_k = _words("cu_k", cu_k, (p.n_seqs + 1,), torch.int32, dev)
+        p.q, p.q_ts, p.q_hs = _rows("q", q, n_q, self.Hq, self.d, self.dtype, dev)
+        p.k, p.k_ts, p.k_hs = _rows("k", k, n_k, self.G, self.d, self.dtype, dev)
+        p.v, p.v_ts, p.v_hs = _rows("v", v, n_k, self.G, self.d, self.dtype, dev)
+        p.out, p.o_ts, p.o_hs = _rows("out", out, n_q, self.Hq, self.d, self.dtype, dev)
+        p.lse = None if lse is None else _words("lse", lse, (n_q, self.Hq), torch.float32, dev)
+        _raise(lib().gracekv_prompt_attention(C.byref(p), self.workspace.data_ptr(),
+                                              _on(stream, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
+        return (out, lse) if return_lse else out
+
+    def status(self, stream=None):
+        _raise(lib().gracekv_prompt_status(self.workspace.data_ptr(), _on(stream, self.workspace)))
+
+
+class PagedCache:
+    """A paged cache of many requests (gracekv_paged_* of the C ABI).
+
+    K, V [n_pages, page_size, d], log_m [n_pages, page_size] fp32 (or None),
+    table [L, B, G, max_pages] int32 and lens [L, B, G] int32 are the caller's
+    device tensors; `PagedCache.allocate` makes them and then also hands out
+    the pages (`load`, `advance`, `release`).  A dense [L, G, T, d] cache is one
+    too: L G pages of T entries.  One object holds the workspace of one stream.
+    """
+
+    def __init__(self, K, V, table, lens, *, Hq: int, log_m=None, rope_base: float = 0.0):
+        if K.dtype not in _DTYPES:
+            raise _bad(f"K must be bf16 or fp32, not {K.dtype}")
+        if K.dim() != 3 or table.dim() != 4:
+            raise _bad("K is [n_pages, page_size, d] and table [L, B, G, max_pages]")
+        dev = K.device
+        n_pages, ps, d = K.shape
+        L, B, G, mp = table.shape
+        self.K, self.V, self.log_m, self.table, self.lens = K, V, log_m, table, lens
+        self.L, self.B, self.G, self.Hq, self.d, self.dtype = L, B, G, Hq, d, K.dtype
+        self.page_size, self.max_pages, self.n_pages = ps, mp, n_pages
+        self.desc = GkvPagedCache(
+            L, B, G, Hq, d, _DTYPES[K.dtype], ps, mp, n_pages, _words("K", K, K.shape, K.dtype, dev),
+            _words("V", V, K.shape, K.dtype, dev),
+            None if log_m is None else _words("log_m", log_m, (n_pages, ps), torch.float32, dev),
+            _words("table", table, table.shape, torch.int32, dev), _words("lens", lens, (L, B, G), torch.int32, dev),
+            float(rope_base))
+        n = C.c_size_t()
+        _raise(lib().gracekv_paged_workspace_size(C.byref(self.desc), C.byref(n)))
+        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)
+        self._free = None
+
+    @staticmethod
+    def allocate(*, L: int, B: int, G: int, Hq: int, d: int, dtype, n_pages: int, max_pages: int,
+                 page_size: int = 64, log_m: bool = True, rope_base: float = 0.0, device="cuda") -> "PagedCache":
+        """An empty cache that hands out its own pages."""
+        import numpy as np
+        c = PagedCache(torch.empty(n_pages, page_size, d, dtype=dtype, device=device),
+                       torch.empty(n_pages, page_size, d, dtype=dtype, device=device),
+                       torch.full((L, B, G, max_pages), -1, dtype=torch.int32, device=device),
+                       torch.zeros(L, B, G, dtype=torch.int32, device=device), Hq=Hq, rope_base=rope_base,
+                       log_m=torch.empty(n_pages, page_size, device=device) if log_m else None)
+        c._free = np.arange(n_pages - 1, -1, -1, dtype=np.int32)     # a stack: the last one goes next
+        c._n_free = n_pages
+        c._host_lens = np.zeros((L, B, G), np.int64)
+        c._host_table = np.full((L, B, G, max_pages), -1, np.int32)
+        return c
+
+    def _own_pages(self):
+        if self._free is None:
+            raise GraceKVError(GKV_ESTATE, "this cache's pages are the caller's (PagedCache.allocate hands them out)")
+
+    def _grow(self, new_lens, stream):
+        """Pages for the host lengths to become new_lens."""
+        import numpy as np
+        ps = self.page_size
+        have, need = -(-self._host_lens // ps), -(-new_lens // ps)
+        if need.max(initial=0) > self.max_pages:
+            raise GraceKVError(GKV_ECAPACITY, "a sequence needs more than max_pages pages")
+        n = int((need - have).sum())
+        if n > self._n_free:
+            raise GraceKVError(GKV_ECAPACITY, f"{n} pages needed, {self._n_free} free")
+        if n:
+            more = (need - have).reshape(-1)
+            seq = np.repeat(np.arange(more.size), more)
+            step = np.arange(n) - np.repeat(np.cumsum(more) - more, more)
+            at = seq * self.max_pages + have.reshape(-1)[seq] + step
+            pages = self._free[self._n_free - n:self._n_free][::-1].copy()
+            self._n_free -= n
+            self._host_table.reshape(-1)[at] = pages
+            with torch.cuda.stream(stream):
+                self.table.view(-1).index_copy_(0, torch.from_numpy(at).to(self.table.device),
+                                                torch.from_numpy(pages).to(self.table.device))
+        self._host_lens = new_lens
+
+    def load_packed(self, b: int, K, V, log_m, offsets, stream=None):
+        """The packed cache K, V [E, d], log_m [E] or None, offsets [L G + 1] int64
+        becomes request b's entries (the table already holds their pages)."""
+        dev, E = self.K.device, K.shape[0]
+        _raise(lib().gracekv_paged_load(
+            C.byref(self.desc), b, _words("K", K, (E, self.d), self.dtype, dev),
+            _words("V", V, (E, self.d), self.dtype, dev),
+            None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
+            _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self.workspace.data_ptr(),
+            _on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens, self.workspace)))
+
+    def load(self, b: int, cache: Cache, n_entries: int, stream=None):
+        """A compressed cache (Compressor's output) as request b, replacing what the
+        slot held.  Reads the offsets back to the host once."""
+        import numpy as np
+        self._own_pages()
+        s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
+        with torch.cuda.stream(s):
+            off = cache.offsets.cpu().numpy()
+        counts = np.diff(off)
+        if off[0] < 0 or counts.min() < 0 or off[-1] > n_entries or n_entries > cache.K.shape[0]:
+            raise _bad("the cache's offsets do not fit its entries")
+        self.release(b, stream)
+        new = self._host_lens.copy()
+        new[:, b] = counts.reshape(self.L, self.G)
+        self._grow(new, s)
+        self.load_packed(b, cache.K[:n_entries], cache.V[:n_entries],
+                         None if self.log_m is None else cache.log_m[:n_entries], cache.offsets, stream)
+
+    def advance(self, counts=None, stream=None):
+        """The next step's tokens: counts[b] of each request (default: one for every
+        request with entries).  Lengths grow, pages are assigned; returns the
+        device cu_new of the appends (None with the default)."""
+        import numpy as np
+        s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
+        cu = None
+        if counts is not None:
+            counts = np.asarray(counts, dtype=np.int64)
+            if counts.shape != (self.B,) or counts.min() < 0:
+                raise _bad("counts is one token count per request")
+            with torch.cuda.stream(s):
+                cu = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(self.K.device)
+        if self._free is not None:
+            add = (self._host_lens > 0) if counts is None else counts[None, :, None]
+            self._grow(self._host_lens + add, s)
+        self.advance_by(cu, stream)
+        return cu
+
+    def advance_by(self, cu_new=None, stream=None):
+        """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
+        p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
+        _raise(lib().gracekv_paged_advance(C.byref(self.desc), p, _on(stream, self.lens, cu_new)))
+
+    def release(self, b: int, stream=None):
+        """Request b's pages return to the pool; the slot is idle."""
+        import numpy as np
+        self._own_pages()
+        if not 0 <= b < self.B:
+            raise _bad(f"request {b} of {self.B}")
+        s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
+        held = self._host_table[:, b]
+        pages = held[held >= 0]
+        self._free[self._n_free:self._n_free + pages.size] = pages
+        self._n_free += pages.size
+        held[...] = -1
+        self._host_lens = np.array(self._host_lens)
+        self._host_lens[:, b] = 0
+        with torch.cuda.stream(s):
+            self.lens[:, b] = 0
+
+    def append(self, l: int, k, v, pos, q=None, cu_new=None, out=None, stream=None):
+        """Layer l's new tokens: k, v [N, G, d] into the pages (k rotated to pos [N]
+        int32); returns q [N, Hq, d] rotated (into `out`, which may be q), or None."""
+        dev, N = self.K.device, k.shape[0]
+        if q is not None and out is None:
+            out = _empty_like_on(stream, (N, self.Hq, self.d), self.dtype, dev)
+        none = (None, 0, 0)
+        _raise(lib().gracekv_paged_append(
+            C.byref(self.desc), l, N,
+            None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
+            _words("pos", pos, (N,), torch.int32, dev), *_rows("k", k, N, self.G, self.d, self.dtype, dev),
+            *_rows("v", v, N, self.G, self.d, self.dtype, dev),
+            *(none if q is None else _rows("q", q, N, self.Hq, self.d, self.dtype, dev)),
+            *(none if q is None else _rows("out", out, N, self.Hq, self.d, self.dtype, dev)),
+            self.workspace.data_ptr(), _on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
+                                           self.lens, self.workspace)))
+        return out
+
+    def attention(self, l: int, q, out=None, stream=None):
+        """q [B, Hq, d], one rotated query per request slot -> out [B, Hq, d] of the
+        cache's dtype over layer l (zeros for an idle slot)."""
+        dev, shape = self.K.device, (self.B, self.Hq, self.d)
+        if out is None:
+            out = _empty_like_on(stream, shape, self.dtype, dev)
+        _raise(lib().gracekv_paged_attention(
+            C.byref(self.desc), l, _words("q", q, shape, self.dtype, dev), _words("out", out, shape, self.dtype, dev),
+            self.workspace.data_ptr(), _on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens,
+                                           self.workspace)))
+        return out
+
+    def status(self, stream=None):
+        _raise(lib().gracekv_paged_status(self.workspace.data_ptr(), _on(stream, self.workspace)))
