@@ -523,9 +523,10 @@ gkv_status gracekv_prompt_status(void *workspace, void *stream);
  * row i % page_size of page table[l][b][g][i / page_size].  Table words past a
  * length are not read.  A page number outside [0, n_pages), or a length past
  * max_pages * page_size, is not followed: the entry is skipped and
- * gracekv_paged_status reports GKV_EINVAL.  K, V on 16 bytes, the others on 4;
- * d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED), page_size >= 1,
- * n_pages * page_size below 2^31.
+ * gracekv_paged_status reports GKV_EINVAL.  K, V, log_m on 16 bytes, the
+ * others on 4; d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED),
+ * page_size >= 1, n_pages * page_size below 2^31, max_pages * page_size at most
+ * 2^31 - 4096.
  */
 typedef struct {
     int32_t L, B, G, Hq, d, dtype;    /* layers, request slots, KV heads, query heads, head dim, gkv_dtype */

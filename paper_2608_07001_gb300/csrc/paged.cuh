@@ -32,9 +32,9 @@ inline gkv_status check_paged(const gkv_paged_cache *c) {
     const gkv_status st = check_paged_geometry(c);
     if (st != GKV_OK) return st;
     if (c->page_size < 1 || c->max_pages < 1 || c->n_pages < 1 || c->n_pages >= (1LL << 31) / c->page_size) return GKV_EINVAL;
-    if ((int64_t)c->page_size * c->max_pages >= (1LL << 31)) return GKV_EINVAL;
+    if ((int64_t)c->page_size * c->max_pages > (1LL << 31) - 4096) return GKV_EINVAL;
     if (!c->K || !c->V || !c->table || !c->lens) return GKV_EINVAL;
-    if (!al(c->K, 16) || !al(c->V, 16) || !al(c->log_m, 4) || !al(c->table, 4) || !al(c->lens, 4)) return GKV_EINVAL;
+    if (!al(c->K, 16) || !al(c->V, 16) || !al(c->log_m, 16) || !al(c->table, 4) || !al(c->lens, 4)) return GKV_EINVAL;
     return GKV_OK;
 }
 
