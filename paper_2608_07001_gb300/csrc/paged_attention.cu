@@ -642,19 +642,18 @@ bool pa_map(CUtensorMap *m, const void *p, int64_t rows, int d, int box) {
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kPaMaxDevices = 64;
 
 template <typename T, int D, int GQ>
 cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
     using C = PaCfg<T, D>;
-    static std::atomic<int> grid_of[kPaMaxDevices];
+    static std::atomic<int> grid_of[kMaxDevices];
     const auto kern = paged_attention_kernel<T, D, GQ>;
     const size_t smem = (size_t)C::NST * 2 * C::TB + 8 * D * sizeof(float) +
                         (C::BF ? 0 : (size_t)(GQ * D + kPaWarps * GQ * 32) * sizeof(float));
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= kPaMaxDevices) return cudaErrorInvalidDevice;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
     int grid = grid_of[dev].load(std::memory_order_relaxed);
     if (grid == 0) {
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

@@ -8,7 +8,7 @@
 // exp(M - M').
 //
 // This version: one warp per (token, query head), lanes over the channels.
-#include "serve.cuh"
+#include "prompt.cuh"
 
 #include <math.h>
 
@@ -17,35 +17,11 @@ namespace {
 
 using namespace serve;
 
-struct PromptArgs {
-    const void *q, *k, *v;
-    void *out;
-    float *lse;
-    const int32_t *cu_q, *cu_k;
-    int n_seqs, G, Hq;
-    int64_t n_q, n_k, q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
-    float scale;                   // 1 / sqrt(d)
-    int *status;
-};
-
-// The rows of sequence s; false when its cu words do not fit.
-__device__ __forceinline__ bool seq_bounds(const PromptArgs &a, int s, int64_t &q0, int64_t &nq, int64_t &k0, int64_t &nk) {
-    q0 = a.cu_q[s];
-    nq = a.cu_q[s + 1] - q0;
-    k0 = a.cu_k[s];
-    nk = a.cu_k[s + 1] - k0;
-    return q0 >= 0 && nq >= 0 && q0 + nq <= a.n_q && k0 >= 0 && nk >= 0 && k0 + nk <= a.n_k;
-}
-
 template <typename T, int D>
 __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
     constexpr int E = D / 32;
     const int lane = threadIdx.x & 31;
-    if (blockIdx.x == 0)
-        for (int s = threadIdx.x; s < a.n_seqs; s += 256) {
-            int64_t q0, nq, k0, nk;
-            if (!seq_bounds(a, s, q0, nq, k0, nk)) atomicOr(a.status, kStRange);
-        }
+    if (blockIdx.x == 0) check_bounds(a);
     const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (w >= a.n_q * a.Hq) return;
     const int64_t row = w / a.Hq;
@@ -120,6 +96,10 @@ extern "C" gkv_status gracekv_prompt_attention(const gkv_prompt *p, void *worksp
                  p->q_ts, p->q_hs, p->k_ts, p->k_hs, p->v_ts, p->v_hs, p->o_ts, p->o_hs,
                  (float)(1.0 / sqrt((double)p->d)), static_cast<int *>(workspace)};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p->dtype == GKV_BF16) {
+        const cudaError_t e = serve::launch_prompt_tc(a, p->d, s);
+        if (e != cudaErrorNotSupported) return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    }
     const int64_t blocks = (p->n_q * p->Hq + 7) / 8;
     if (blocks >= (1LL << 31)) return GKV_EUNSUPPORTED;
     const unsigned n = (unsigned)blocks;

@@ -1,0 +1,56 @@
+// prompt.cuh -- the prompt's attention as its kernels see it.
+#pragma once
+
+#include "serve.cuh"
+
+namespace gkv {
+namespace serve {
+
+struct PromptArgs {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    const int32_t *cu_q, *cu_k;
+    int n_seqs, G, Hq;
+    int64_t n_q, n_k, q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
+    float scale;                   // 1 / sqrt(d)
+    int *status;
+};
+
+// The rows of sequence s; false when its cu words do not fit.
+__device__ __forceinline__ bool seq_bounds(const PromptArgs &a, int s, int64_t &q0, int64_t &nq, int64_t &k0, int64_t &nk) {
+    q0 = a.cu_q[s];
+    nq = a.cu_q[s + 1] - q0;
+    k0 = a.cu_k[s];
+    nk = a.cu_k[s + 1] - k0;
+    return q0 >= 0 && nq >= 0 && q0 + nq <= a.n_q && k0 >= 0 && nk >= 0 && k0 + nk <= a.n_k;
+}
+
+// Work slots of `tok` queries: sequence s owns the slots from cu_q[s] / tok + s
+// on, which is room for its ceil(nq / tok) blocks whatever the lengths (the
+// floors of two bounds nq apart differ by at least floor(nq / tok), and one
+// more slot a sequence is left), so n_q / tok + n_seqs slots cover every
+// packing without a pass over the lengths.
+__host__ __device__ __forceinline__ int64_t prompt_slots(int64_t n_q, int n_seqs, int tok) { return n_q / tok + n_seqs; }
+__device__ __forceinline__ int slot_seq(const int32_t *cu, int n, int64_t slot, int tok) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu[mid] / tok + mid <= slot) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Flags the sequences whose cu words do not fit (one block of a launch calls it).
+__device__ __forceinline__ void check_bounds(const PromptArgs &a) {
+    for (int s = threadIdx.x; s < a.n_seqs; s += blockDim.x) {
+        int64_t q0, nq, k0, nk;
+        if (!seq_bounds(a, s, q0, nq, k0, nk)) atomicOr(a.status, kStRange);
+    }
+}
+
+// bf16 on tcgen05; cudaErrorNotSupported when a tensor's strides have no tensor map.
+cudaError_t launch_prompt_tc(const PromptArgs &a, int d, cudaStream_t s);
+
+}  // namespace serve
+}  // namespace gkv

@@ -1,0 +1,441 @@
+// prompt_tc.cu -- the prompt's attention for bf16 on tcgen05.
+//
+// For the 256 rows of a CTA (two tiles of 128; a row is a query token and one
+// of the gq heads that share a KV head, so a tile holds 128 / gq tokens and
+// every key tile is read once for all gq heads):
+//   S = Q K^T (fp32 in TMEM), P = 2^(S c - M c), c = log2(e) / sqrt(d),
+//   O += P V, Z += sum P, out = O / Z, lse = M / sqrt(d) + ln Z.
+// M is a row's reference, not its exact maximum: it follows the running maximum
+// only when that has grown by more than 2^kLazy, so the accumulator in TMEM is
+// rescaled a few times instead of once a key tile; P stays below 2^kLazy, and O
+// and Z share the reference, so the quotient is the same.
+//
+// What bounds it: at d = 128 a 128 x 128 tile costs 2 x 128^3 MACs in each of
+// the two products against 128^2 exponentials, so the tensor pipe; at d = 64
+// the exponentials weigh twice as much.  The two row tiles alternate: while the
+// tensor core works on one's S and PV, the other's warps take its softmax.
+//
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread a row, its 128 scores
+// in registers), 8 TMA (Q once, then K and V tiles of 128 keys through a ring),
+// 9 MMA issue (10, 11 idle: registers are split by warpgroup).  TMEM: S0, S1 (128 columns each; P overlays the lower half of
+// its S as packed bf16), O0, O1.  P is the A operand of its product from TMEM;
+// V is the B operand as it lies in memory (rows of channels, "MN-major").
+// tcgen05 operations of one thread complete in order, so the commit of S(j + 1)
+// also tells that PV(j) is done: the rescaling needs no barrier of its own.
+//
+// Masks: only the tiles that reach past a row's last key compare columns; the
+// keys past a sequence's end get weight 0 that way, and their V rows, which
+// may hold anything, are zeroed in shared memory before the product.
+#include "prompt.cuh"
+#include "tc.cuh"
+
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+
+namespace gkv {
+namespace serve {
+namespace {
+
+constexpr int kN = 128;                        // keys of a tile
+constexpr int kThreads = 384;                  // three warpgroups: two of softmax, one of TMA and MMA issue
+// Registers a thread after the split; 256 x 208 + 128 x 88 = 384 x 168, the launch's own.
+constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
+static_assert(256 * kRegsSoftmax + 128 * kRegsIssue <= kThreads * kRegs, "register split");
+constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr float kLazy = 8.f;                   // log2 of the growth a reference lets pass
+constexpr uint64_t kWaitNs = 2000000000ull;
+
+template <int D>
+struct Cfg {
+    static constexpr int NB = D / 64;                          // 64-channel blocks of a row
+    static constexpr uint32_t TILE = NB * 128 * 128;           // bytes of a 128-row tile
+    static constexpr int NST = (D == 128 ? 5 : 8);             // ring slots (K and V tiles in turn)
+    static constexpr size_t SMEM = 1024 + (2 + NST) * (size_t)TILE;
+};
+
+struct Bars {
+    uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], odone[2], vfix, fin;
+    uint32_t tbase;
+    int abort;
+};
+
+struct Tc {
+    int gq, tpt;               // heads of a KV head, tokens of a row tile
+    int kh, vh;                // head coordinate step of k, v (0: one head for all)
+};
+
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars &b, int *status) {
+    const uint32_t addr = tc::smem_u32(bar);
+    if (tc::mbar_try_wait(addr, parity)) return true;
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (uint32_t it = 0;; it++) {
+        if (tc::mbar_try_wait(addr, parity)) return true;
+        if ((it & 63u) == 63u) {
+            if (*(volatile int *)&b.abort) return false;
+            if (tc::globaltimer_ns() - t0 > kWaitNs) {
+                atomicOr(status, kStTimeout);
+                atomicExch(&b.abort, 1);
+                return false;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_tc_kernel(const PromptArgs a, const Tc t, const __grid_constant__ CUtensorMap mapQ,
+                     const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) &
+                                                            ~static_cast<uintptr_t>(1023));
+    unsigned char *Qs = base, *ring = base + 2 * C::TILE;
+    __shared__ Bars b;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (blockIdx.x == 0) check_bounds(a);
+    // ---- the CTA's rows: heavy blocks (late tokens) first
+    const int g = blockIdx.x % a.G;
+    const int tok = 2 * t.tpt;
+    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
+    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    int64_t q0, nq64, k0, nk64;
+    if (!seq_bounds(a, s, q0, nq64, k0, nk64)) return;
+    const int64_t t0_64 = (slot - (q0 / tok + s)) * tok;
+    if (t0_64 < 0 || t0_64 >= nq64) return;
+    const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
+    const int off = nk - nq;                             // query i sees keys <= i + off
+    const int ntile = t0 + t.tpt < nq ? 2 : 1;
+    // key tiles of each row tile: up to the last key its last token sees
+    const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
+    const int nkv0 = last0 >= 0 ? last0 / kN + 1 : 0, nkv1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
+    const int n = max(nkv0, nkv1);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::NST; i++) {
+            tc::mbar_init(tc::smem_u32(&b.full[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.empty[i]), 1);
+        }
+        tc::mbar_init(tc::smem_u32(&b.qfull), 1);
+        tc::mbar_init(tc::smem_u32(&b.vfix), 1);
+        tc::mbar_init(tc::smem_u32(&b.fin), 1);
+        for (int i = 0; i < 2; i++) {
+            tc::mbar_init(tc::smem_u32(&b.sfull[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.pfull[i]), 4);
+            tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
+        }
+        b.abort = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == kWarpMma) {
+        tc::tmem_alloc(tc::smem_u32(&b.tbase), 512);
+        tc::tmem_relinquish();
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tb = b.tbase;
+
+    // the sequence's last key tile is partial and other rows follow it: their V rows are zeroed
+    const bool fix = n > 0 && nk - (n - 1) * kN < kN && k0 + nk < a.n_k;
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+        // ---------------- softmax and epilogue: one thread a row ----------------
+        const int i = warp >> 2, q = warp & 3, r = q * 32 + lane;
+        const int tk = r / t.gq, h = r - tk * t.gq;
+        const int token = t0 + i * t.tpt + tk;
+        const bool live = tk < t.tpt && token < nq;
+        const int lim = live ? token + off : -1;         // last key the row sees
+        const float c = a.scale * kLog2e;
+        const uint32_t ts = tb + ((uint32_t)(q * 32) << 16) + (uint32_t)(i * kN), to = tb + ((uint32_t)(q * 32) << 16) + 2 * kN + i * D;
+        // the first token of the tile sees the fewest keys: below its limit no mask is needed
+        const int clear = t0 + i * t.tpt + off;
+        float m = -INFINITY, z = 0.f;                    // m: the reference times c
+        const int nj = i ? nkv1 : nkv0;
+        bool ok = true;
+        for (int j = 0; j < nj; j++) {
+            ok = __all_sync(0xffffffffu, wait(&b.sfull[i], j & 1, b, a.status));
+            if (!ok) break;
+            tc::tc_fence_after();
+            uint32_t x[4][32];
+#pragma unroll
+            for (int k = 0; k < 4; k++) tc::tmem_ld32_async(ts + 32 * k, x[k]);
+            tc::tmem_wait_ld(x[0]);
+#pragma unroll
+            for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
+            if (j * kN + kN - 1 > clear) {
+                const int rel = lim - j * kN;
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int e = 0; e < 32; e++)
+                        if (k * 32 + e > rel) x[k][e] = 0xff800000u;       // -inf
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                    mx[k] = fmaxf(mx[k], fmaxf(__uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1])));
+            const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+            if (m == -INFINITY) m = mn;                  // nothing accumulated yet
+            else if (__builtin_expect(mn > m + kLazy, 0)) z = -z;          // asks for a rescale (z > 0 marks none)
+            if (__any_sync(0xffffffffu, z < 0.f)) {
+                float w = 1.f;
+                if (z < 0.f) {
+                    w = tc::ex2(m - mn);
+                    z = -z * w;
+                    m = mn;
+                }
+#pragma unroll
+                for (int k = 0; k < D / 32; k++) {
+                    uint32_t o[32];
+                    tc::tmem_ld32_async(to + 32 * k, o);
+                    tc::tmem_wait_ld(o);
+#pragma unroll
+                    for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
+                    tc::tmem_st32(to + 32 * k, o);
+                }
+            }
+            const float sh = m == -INFINITY ? 0.f : -m;
+            const float2 c2 = make_float2(c, c), s2 = make_float2(sh, sh);
+            float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; e++) {
+                    const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * k + e / 16][(2 * e) & 31]),
+                                                            __uint_as_float(x[2 * k + e / 16][((2 * e) & 31) + 1])), c2, s2);
+                    const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
+                    acc = __fadd2_rn(acc, w);
+                    p[e] = pack2(w.x, w.y);
+                }
+                tc::tmem_st32(ts + 32 * k, p);
+            }
+            z += acc.x + acc.y;
+            tc::tmem_wait_st();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i]));
+        }
+        if (ok && nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status));
+        tc::tc_fence_after();
+        if (ok) {
+            const float inv = z > 0.f ? 1.f / z : z;     // no key: z = 0; a NaN stays
+            const int64_t row = q0 + token;
+            const int hq = g * t.gq + h;
+            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.out) + row * a.o_ts + hq * a.o_hs;
+            if (i < ntile) {
+#pragma unroll
+                for (int k = 0; k < D / 32; k++) {
+                    uint32_t v[32];
+                    if (nj > 0) {
+                        tc::tmem_ld32_async(to + 32 * k, v);
+                        tc::tmem_wait_ld(v);
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint4 u = make_uint4(0, 0, 0, 0);
+                            if (lim >= 0) {
+                                u.x = pack2(__uint_as_float(v[e]) * inv, __uint_as_float(v[e + 1]) * inv);
+                                u.y = pack2(__uint_as_float(v[e + 2]) * inv, __uint_as_float(v[e + 3]) * inv);
+                                u.z = pack2(__uint_as_float(v[e + 4]) * inv, __uint_as_float(v[e + 5]) * inv);
+                                u.w = pack2(__uint_as_float(v[e + 6]) * inv, __uint_as_float(v[e + 7]) * inv);
+                            }
+                            *reinterpret_cast<uint4 *>(o + k * 32 + e) = u;
+                        }
+                    }
+                }
+                if (live && a.lse)
+                    a.lse[row * a.Hq + hq] = lim >= 0 ? (m + log2f(z)) * 0.6931471805599453f : -INFINITY;
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+        if (warp == kWarpTma) {
+            // ---------------- producer ----------------
+            int issued = 0;
+            bool ok = n > 0;
+            if (lane == 0 && ok) {
+                tc::tma_prefetch_desc(&mapQ);
+                tc::tma_prefetch_desc(&mapK);
+                tc::tma_prefetch_desc(&mapV);
+                const uint32_t qb = tc::smem_u32(&b.qfull);
+                tc::mbar_expect_tx(qb, (uint32_t)(ntile * C::NB * t.tpt * t.gq * 128));
+                for (int i = 0; i < ntile; i++)
+    #pragma unroll
+                    for (int c = 0; c < C::NB; c++)
+                        tc::tma_load_3d(tc::smem_u32(Qs + i * C::TILE + c * 128 * 128), &mapQ, c * 64, g * t.gq,
+                                        (int)(q0 + t0 + i * t.tpt), qb);
+                for (int i = 0; i < 2 * n; i++) {
+                    const int st = i % C::NST;
+                    ok = !*(volatile int *)&b.abort && wait(&b.empty[st], ((i / C::NST) & 1) ^ 1, b, a.status);
+                    if (!ok) break;
+                    const uint32_t fb = tc::smem_u32(&b.full[st]);
+                    tc::mbar_expect_tx(fb, C::TILE);
+    #pragma unroll
+                    for (int c = 0; c < C::NB; c++)
+                        tc::tma_load_3d(tc::smem_u32(ring + st * C::TILE + c * 128 * 128), (i & 1) ? &mapV : &mapK, c * 64,
+                                        g * ((i & 1) ? t.vh : t.kh), (int)(k0 + (i >> 1) * kN), fb);
+                    issued++;
+                }
+            }
+            issued = __shfl_sync(0xffffffffu, issued, 0);
+            ok = issued == 2 * n && n > 0;
+            if (fix && ok) {
+                const int st = (2 * n - 1) % C::NST, keep = nk - (n - 1) * kN;
+                if (wait(&b.full[st], ((2 * n - 1) / C::NST) & 1, b, a.status)) {
+                    for (int i = lane; i < (kN - keep) * C::NB * 8; i += 32) {
+                        const int r = keep + i / (C::NB * 8), c = i % (C::NB * 8);
+                        *reinterpret_cast<uint4 *>(ring + st * C::TILE + (c >> 3) * (128 * 128) + r * 128 + (c & 7) * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.vfix));
+                }
+            }
+            // the copies still in flight land before the block exits
+            if (lane == 0 && n > 0) {
+                for (int i = max(0, issued - C::NST); i < issued; i++)
+                    tc::mbar_wait(tc::smem_u32(&b.full[i % C::NST]), (i / C::NST) & 1, kWaitNs);
+                tc::mbar_wait(tc::smem_u32(&b.qfull), 0, kWaitNs);
+            }
+        } else if (warp == kWarpMma) {
+            // ---------------- MMA issue ----------------
+            if (lane == 0 && n > 0) {
+                constexpr uint32_t idS = tc::idesc_bf16_f32(128, kN), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
+                const uint32_t qa = tc::smem_u32(Qs), ra = tc::smem_u32(ring);
+                int committed = 0;                           // commits to b.odone[0], b.odone[1] are the last ones
+                bool ok = wait(&b.qfull, 0, b, a.status);
+                auto qk = [&](int i, int j) {                // S_i = Q_i K_j^T
+                    const uint32_t ks = ra + (uint32_t)((2 * j) % C::NST) * C::TILE;
+    #pragma unroll
+                    for (int c = 0; c < C::NB; c++)
+    #pragma unroll
+                        for (int x = 0; x < 4; x++)
+                            tc::mma_bf16(tb + i * kN, tc::sdesc_sw128(qa + i * C::TILE + c * 128 * 128 + 32 * x),
+                                         tc::sdesc_sw128(ks + c * 128 * 128 + 32 * x), idS, (c | x) != 0);
+                    tc::mma_commit(tc::smem_u32(&b.sfull[i]));
+                };
+                if (ok) ok = wait(&b.full[0], 0, b, a.status);
+                if (ok) {
+                    tc::tc_fence_after();
+                    for (int i = 0; i < ntile; i++)
+                        if ((i ? nkv1 : nkv0) > 0) qk(i, 0);
+                    tc::mma_commit(tc::smem_u32(&b.empty[0]));
+                    committed = 1;
+                }
+                for (int j = 0; ok && j < n; j++) {
+                    const int vi = 2 * j + 1, ki = 2 * j + 2;
+                    ok = wait(&b.full[vi % C::NST], (vi / C::NST) & 1, b, a.status);
+                    if (ok && fix && j == n - 1) ok = wait(&b.vfix, 0, b, a.status);
+                    if (ok && j + 1 < n) ok = wait(&b.full[ki % C::NST], (ki / C::NST) & 1, b, a.status);
+                    const uint32_t vs = ra + (uint32_t)(vi % C::NST) * C::TILE;
+                    for (int i = 0; ok && i < ntile; i++) {
+                        const int ni = i ? nkv1 : nkv0;
+                        if (j >= ni) continue;
+                        ok = wait(&b.pfull[i], j & 1, b, a.status);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+    #pragma unroll
+                        for (int x = 0; x < kN / 16; x++)
+                            tc::mma_bf16_ts(tb + 2 * kN + i * D, tb + i * kN + x * 8,
+                                            tc::sdesc_sw128_mn(vs + x * 16 * 128, 128 * 128), idO, (j | x) != 0);
+                        if (j == ni - 1) tc::mma_commit(tc::smem_u32(&b.odone[i]));
+                        else qk(i, j + 1);
+                    }
+                    if (!ok) break;
+                    tc::mma_commit(tc::smem_u32(&b.empty[vi % C::NST]));
+                    if (j + 1 < n) tc::mma_commit(tc::smem_u32(&b.empty[ki % C::NST]));
+                }
+                if (!ok) {
+                    atomicOr(a.status, kStTimeout);
+                    atomicExch(&b.abort, 1);
+                }
+                // every operation issued is done before TMEM is freed: one more commit covers them
+                if (committed) {
+                    tc::mma_commit(tc::smem_u32(&b.fin));
+                    tc::mbar_wait(tc::smem_u32(&b.fin), 0, kWaitNs);
+                }
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == kWarpMma) {
+        tc::tc_fence_after();
+        tc::tmem_dealloc(tb, 512);
+    }
+}
+
+// [tokens][heads][d] rows with element strides ts, hs: boxes of 64 channels x
+// box_h heads x box_t tokens, 128-byte swizzle.
+bool make_map(CUtensorMap *m, const void *p, int64_t tokens, int heads, int d, int64_t ts, int64_t hs, int box_h, int box_t) {
+    auto enc = tc::tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t gdim[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
+    cuuint64_t gstr[2] = {(cuuint64_t)(heads > 1 ? hs : d) * 2, (cuuint64_t)(tokens > 1 ? ts : (int64_t)d * heads) * 2};
+    if (gstr[0] == 0 || gstr[1] == 0) return false;
+    cuuint32_t box[3] = {64, (cuuint32_t)box_h, (cuuint32_t)box_t};
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), gdim, gstr, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const PromptArgs &a, cudaStream_t s) {
+    Tc t;
+    t.gq = a.Hq / a.G;
+    t.tpt = 128 / t.gq;
+    // a broadcast head (stride 0) is one head read for every group
+    t.kh = a.k_hs != 0;
+    t.vh = a.v_hs != 0;
+    CUtensorMap mq, mk, mv;
+    if (!make_map(&mq, a.q, a.n_q, a.Hq, D, a.q_ts, a.q_hs, t.gq, t.tpt)) return cudaErrorNotSupported;
+    if (a.n_k == 0) {
+        mk = mv = mq;
+    } else if (!make_map(&mk, a.k, a.n_k, t.kh ? a.G : 1, D, a.k_ts, a.k_hs, 1, kN) ||
+               !make_map(&mv, a.v, a.n_k, t.vh ? a.G : 1, D, a.v_ts, a.v_hs, 1, kN)) {
+        return cudaErrorNotSupported;
+    }
+    const int64_t blocks = prompt_slots(a.n_q, a.n_seqs, 2 * t.tpt) * a.G;
+    if (blocks >= (1LL << 31)) return cudaErrorNotSupported;
+    static std::atomic<int> ready[kMaxDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (!ready[dev].load(std::memory_order_relaxed)) {
+        cudaFuncAttributes at;
+        e = cudaFuncGetAttributes(&at, prompt_tc_kernel<D>);
+        if (e != cudaSuccess) return e;
+        if (at.numRegs != kRegs) return cudaErrorInvalidConfiguration;     // the register split would not add up
+        e = cudaFuncSetAttribute(prompt_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::SMEM);
+        if (e != cudaSuccess) return e;
+        ready[dev].store(1, std::memory_order_relaxed);
+    }
+    prompt_tc_kernel<D><<<(unsigned)blocks, kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_prompt_tc(const PromptArgs &a, int d, cudaStream_t s) {
+    return d == 128 ? launch<128>(a, s) : launch<64>(a, s);
+}
+
+}  // namespace serve
+}  // namespace gkv

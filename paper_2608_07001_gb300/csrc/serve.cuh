@@ -16,6 +16,7 @@ namespace serve {
 constexpr int kStTimeout = 1;      // a bounded device-side wait gave up
 constexpr int kStRange = 2;        // a page number, length, offset or cu word was not followed
 constexpr size_t kWsHead = 256;
+constexpr int kMaxDevices = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
 inline bool al(const void *p, uintptr_t m) { return (reinterpret_cast<uintptr_t>(p) & (m - 1)) == 0; }
