@@ -7,7 +7,9 @@
 // and sum Z of the softmax: a new maximum M' scales the sums so far by
 // exp(M - M').
 //
-// This version: one warp per (token, query head), lanes over the channels.
+// bf16 runs on tcgen05 (prompt_tc.cu), fp32 on CUDA cores (prompt_f32.cu).
+// This file checks the arguments and lays out the workspace: the status word,
+// the counters of split blocks, their parts.
 #include "prompt.cuh"
 
 #include <math.h>
@@ -17,43 +19,7 @@ namespace {
 
 using namespace serve;
 
-template <typename T, int D>
-__global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
-    if (blockIdx.x == 0) check_bounds(a);
-    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (w >= a.n_q * a.Hq) return;
-    const int64_t row = w / a.Hq;
-    const int h = (int)(w % a.Hq), g = h / (a.Hq / a.G);
-    const int s = seq_of(a.cu_q, a.n_seqs, row);
-    int64_t q0, nq, k0, nk;
-    if (!seq_bounds(a, s, q0, nq, k0, nk) || row < q0 || row >= q0 + nq) return;      // a row of no sequence
-    const int64_t n = row - q0 + nk - nq + 1;      // keys it sees
-    const T *q = static_cast<const T *>(a.q) + row * a.q_ts + h * a.q_hs + lane * E;
-    const T *k = static_cast<const T *>(a.k) + k0 * a.k_ts + g * a.k_hs + lane * E;
-    const T *v = static_cast<const T *>(a.v) + k0 * a.v_ts + g * a.v_hs + lane * E;
-    float qf[E], acc[E], m = -INFINITY, z = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; e++) { qf[e] = to_f(q[e]); acc[e] = 0.f; }
-    for (int64_t j = 0; j < n; j++) {
-        float x = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; e++) x += qf[e] * to_f(k[j * a.k_ts + e]);
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        x *= a.scale;
-        const float mn = fmaxf(m, x), c = __expf(m - mn), p = __expf(x - mn);
-        m = mn;
-        z = z * c + p;
-#pragma unroll
-        for (int e = 0; e < E; e++) acc[e] = acc[e] * c + p * to_f(v[j * a.v_ts + e]);
-    }
-    T *o = static_cast<T *>(a.out) + row * a.o_ts + h * a.o_hs + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e++) put(o + e, n > 0 ? acc[e] / z : 0.f);
-    if (a.lse && lane == 0) a.lse[row * a.Hq + h] = n > 0 ? m + logf(z) : -INFINITY;
-}
+constexpr size_t kCntBytes = (serve::kPromptParts * sizeof(int) + 255) / 256 * 256;
 
 gkv_status check_geometry(const gkv_prompt *p) {
     if (!p || p->G <= 0 || p->Hq <= 0 || p->Hq % p->G) return GKV_EINVAL;
@@ -75,6 +41,11 @@ gkv_status check_prompt(const gkv_prompt *p) {
 }
 
 }  // namespace
+
+namespace serve {
+// The tcgen05 kernel's parts hold 256 rows, the fp32 kernel's 64.
+size_t prompt_part_floats(int d, int dtype) { return (size_t)(dtype == GKV_BF16 ? 256 : kPromptF32Rows) * (d + 2); }
+}  // namespace serve
 }  // namespace gkv
 
 using namespace gkv;
@@ -83,7 +54,8 @@ extern "C" gkv_status gracekv_prompt_workspace_size(const gkv_prompt *p, size_t 
     const gkv_status st = check_geometry(p);
     if (st != GKV_OK) return st;
     if (!bytes) return GKV_EINVAL;
-    *bytes = serve::kWsHead;
+    *bytes = serve::kWsHead + kCntBytes +
+             (size_t)serve::kPromptParts * serve::prompt_part_floats(p->d, p->dtype) * sizeof(float);
     return GKV_OK;
 }
 
@@ -92,25 +64,17 @@ extern "C" gkv_status gracekv_prompt_attention(const gkv_prompt *p, void *worksp
     if (st != GKV_OK) return st;
     if (!workspace || !al(workspace, 256)) return GKV_EINVAL;
     if (p->n_seqs == 0 || p->n_q == 0) return GKV_OK;
-    PromptArgs a{p->q, p->k, p->v, p->out, p->lse, p->cu_q, p->cu_k, p->n_seqs, p->G, p->Hq, p->n_q, p->n_k,
-                 p->q_ts, p->q_hs, p->k_ts, p->k_hs, p->v_ts, p->v_hs, p->o_ts, p->o_hs,
-                 (float)(1.0 / sqrt((double)p->d)), static_cast<int *>(workspace)};
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    const serve::PromptArgs a{p->q, p->k, p->v, p->out, p->lse, p->cu_q, p->cu_k, p->n_seqs, p->G, p->Hq, p->n_q, p->n_k,
+                              p->q_ts, p->q_hs, p->k_ts, p->k_hs, p->v_ts, p->v_hs, p->o_ts, p->o_hs,
+                              (float)(1.0 / sqrt((double)p->d)), reinterpret_cast<int *>(ws),
+                              reinterpret_cast<int *>(ws + serve::kWsHead),
+                              reinterpret_cast<float *>(ws + serve::kWsHead + kCntBytes), 1};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (p->dtype == GKV_BF16) {
-        const cudaError_t e = serve::launch_prompt_tc(a, p->d, s);
-        if (e != cudaErrorNotSupported) return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
-    }
-    const int64_t blocks = (p->n_q * p->Hq + 7) / 8;
-    if (blocks >= (1LL << 31)) return GKV_EUNSUPPORTED;
-    const unsigned n = (unsigned)blocks;
-    if (p->dtype == GKV_BF16) {
-        if (p->d == 128) prompt_rows_kernel<__nv_bfloat16, 128><<<n, 256, 0, s>>>(a);
-        else prompt_rows_kernel<__nv_bfloat16, 64><<<n, 256, 0, s>>>(a);
-    } else {
-        if (p->d == 128) prompt_rows_kernel<float, 128><<<n, 256, 0, s>>>(a);
-        else prompt_rows_kernel<float, 64><<<n, 256, 0, s>>>(a);
-    }
-    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    cudaError_t e = cudaErrorNotSupported;
+    if (p->dtype == GKV_BF16) e = serve::launch_prompt_tc(a, p->d, s);
+    if (e == cudaErrorNotSupported) e = serve::launch_prompt_f32(a, p->d, p->dtype, s);
+    return e == cudaSuccess ? GKV_OK : e == cudaErrorInvalidConfiguration ? GKV_EUNSUPPORTED : GKV_ECUDA;
 }
 
 extern "C" gkv_status gracekv_prompt_status(void *workspace, void *stream) {

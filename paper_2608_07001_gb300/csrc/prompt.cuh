@@ -6,6 +6,8 @@
 namespace gkv {
 namespace serve {
 
+constexpr int kPromptParts = 304;  // parts of key ranges kept at once (split blocks; two a SM)
+
 struct PromptArgs {
     const void *q, *k, *v;
     void *out;
@@ -15,6 +17,9 @@ struct PromptArgs {
     int64_t n_q, n_k, q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
     float scale;                   // 1 / sqrt(d)
     int *status;
+    int *cnt;                      // [kPromptParts] parts finished of every split block, 0 between calls
+    float *part;                   // [kPromptParts] partial results
+    int split;                     // most parts of a block's keys (set by the launchers)
 };
 
 // The rows of sequence s; false when its cu words do not fit.
@@ -49,8 +54,20 @@ __device__ __forceinline__ void check_bounds(const PromptArgs &a) {
     }
 }
 
+// Parts of a block of n key tiles when a launch splits blocks `split` ways, at
+// least `least` tiles a part.
+__host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
+    const int most = (n + least - 1) / least;
+    return most < 1 ? 1 : most < split ? most : split;
+}
+
+constexpr int kPromptF32Rows = 64;     // rows of a block of the fp32 kernel
+size_t prompt_part_floats(int d, int dtype);       // of one part in the workspace
+
 // bf16 on tcgen05; cudaErrorNotSupported when a tensor's strides have no tensor map.
 cudaError_t launch_prompt_tc(const PromptArgs &a, int d, cudaStream_t s);
+// fp32, and bf16 tensors that launch_prompt_tc does not take.
+cudaError_t launch_prompt_f32(const PromptArgs &a, int d, int dtype, cudaStream_t s);
 
 }  // namespace serve
 }  // namespace gkv

@@ -23,6 +23,10 @@
 // tcgen05 operations of one thread complete in order, so the commit of S(j + 1)
 // also tells that PV(j) is done: the rescaling needs no barrier of its own.
 //
+// Few blocks (a short chunk over a long cache) leave SMs idle: then a block's
+// keys are split into parts that leave O, M and Z in the workspace, and the
+// last part to finish, found with a counter, joins them in order.
+//
 // Masks: only the tiles that reach past a row's last key compare columns; the
 // keys past a sequence's end get weight 0 that way, and their V rows, which
 // may hold anything, are zeroed in shared memory before the product.
@@ -44,6 +48,8 @@ constexpr int kThreads = 384;                  // three warpgroups: two of softm
 constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
 static_assert(256 * kRegsSoftmax + 128 * kRegsIssue <= kThreads * kRegs, "register split");
 constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr int kLeast = 2;                      // key tiles of a part at least
+constexpr int kPartRows = 256;
 constexpr float kLazy = 8.f;                   // log2 of the growth a reference lets pass
 constexpr uint64_t kWaitNs = 2000000000ull;
 
@@ -58,7 +64,7 @@ struct Cfg {
 struct Bars {
     uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], odone[2], vfix, fin;
     uint32_t tbase;
-    int abort;
+    int abort, last;
 };
 
 struct Tc {
@@ -101,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ Bars b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    if (blockIdx.x == 0) check_bounds(a);
+    if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
     // ---- the CTA's rows: heavy blocks (late tokens) first
     const int g = blockIdx.x % a.G;
     const int tok = 2 * t.tpt;
@@ -114,10 +120,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
     const int off = nk - nq;                             // query i sees keys <= i + off
     const int ntile = t0 + t.tpt < nq ? 2 : 1;
-    // key tiles of each row tile: up to the last key its last token sees
+    // key tiles of each row tile, up to the last key its last token sees; of
+    // them this part's: [j0, j0 + n)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
-    const int nkv0 = last0 >= 0 ? last0 / kN + 1 : 0, nkv1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
-    const int n = max(nkv0, nkv1);
+    const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
+    const int all = max(all0, all1), np = parts_of(all, a.split, kLeast);
+    if ((int)blockIdx.y >= np) return;
+    const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
+    const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::NST; i++) {
@@ -145,7 +155,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tb = b.tbase;
 
     // the sequence's last key tile is partial and other rows follow it: their V rows are zeroed
-    const bool fix = n > 0 && nk - (n - 1) * kN < kN && k0 + nk < a.n_k;
+    const int keep = nk - (j1 - 1) * kN;                  // keys of the sequence in the part's last tile, from it on
+    const bool fix = n > 0 && keep < kN && k0 + nk < a.n_k;
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
@@ -172,8 +183,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tmem_wait_ld(x[0]);
 #pragma unroll
             for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
-            if (j * kN + kN - 1 > clear) {
-                const int rel = lim - j * kN;
+            if ((j0 + j) * kN + kN - 1 > clear) {
+                const int rel = lim - (j0 + j) * kN;
 #pragma unroll
                 for (int k = 0; k < 4; k++)
 #pragma unroll
@@ -230,35 +241,110 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok && nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status));
         tc::tc_fence_after();
-        if (ok) {
-            const float inv = z > 0.f ? 1.f / z : z;     // no key: z = 0; a NaN stays
-            const int64_t row = q0 + token;
-            const int hq = g * t.gq + h;
-            __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.out) + row * a.o_ts + hq * a.o_hs;
-            if (i < ntile) {
+        const int64_t row = q0 + token;
+        const int hq = g * t.gq + h;
+        __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.out) + row * a.o_ts + hq * a.o_hs;
+        auto write8 = [&](int col, const float *v, float inv) {
+            uint4 u;
+            u.x = pack2(v[0] * inv, v[1] * inv);
+            u.y = pack2(v[2] * inv, v[3] * inv);
+            u.z = pack2(v[4] * inv, v[5] * inv);
+            u.w = pack2(v[6] * inv, v[7] * inv);
+            *reinterpret_cast<uint4 *>(o + col) = u;
+        };
+        auto write_lse = [&]() {
+            if (a.lse) a.lse[row * a.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
+        };
+        if (np == 1) {
+            if (ok && i < ntile) {
+                const float inv = z > 0.f ? 1.f / z : z;     // no key: 0; a NaN stays
 #pragma unroll
                 for (int k = 0; k < D / 32; k++) {
-                    uint32_t v[32];
+                    float v[32];
                     if (nj > 0) {
-                        tc::tmem_ld32_async(to + 32 * k, v);
-                        tc::tmem_wait_ld(v);
+                        uint32_t u[32];
+                        tc::tmem_ld32_async(to + 32 * k, u);
+                        tc::tmem_wait_ld(u);
+#pragma unroll
+                        for (int e = 0; e < 32; e++) v[e] = __uint_as_float(u[e]);
+                    }
+                    if (nj == 0 || lim < 0) {
+#pragma unroll
+                        for (int e = 0; e < 32; e++) v[e] = 0.f;
                     }
                     if (live) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint4 u = make_uint4(0, 0, 0, 0);
-                            if (lim >= 0) {
-                                u.x = pack2(__uint_as_float(v[e]) * inv, __uint_as_float(v[e + 1]) * inv);
-                                u.y = pack2(__uint_as_float(v[e + 2]) * inv, __uint_as_float(v[e + 3]) * inv);
-                                u.z = pack2(__uint_as_float(v[e + 4]) * inv, __uint_as_float(v[e + 5]) * inv);
-                                u.w = pack2(__uint_as_float(v[e + 6]) * inv, __uint_as_float(v[e + 7]) * inv);
-                            }
-                            *reinterpret_cast<uint4 *>(o + k * 32 + e) = u;
-                        }
+                        for (int e = 0; e < 32; e += 8) write8(k * 32 + e, v + e, inv);
                     }
                 }
-                if (live && a.lse)
-                    a.lse[row * a.Hq + hq] = lim >= 0 ? (m + log2f(z)) * 0.6931471805599453f : -INFINITY;
+                if (live) write_lse();
+            }
+        } else {
+            // a part: [D / 4][rows] sums of 4 channels, then [rows] references, [rows] sums of weights
+            constexpr size_t PF = (size_t)kPartRows * (D + 2);
+            const size_t first = (size_t)blockIdx.x * a.split;
+            float *pp = a.part + (first + blockIdx.y) * PF;
+            const int pr = i * 128 + r;
+            if (ok && i < ntile) {
+#pragma unroll
+                for (int k = 0; k < D / 32; k++) {
+                    uint32_t u[32];
+                    if (nj > 0) {
+                        tc::tmem_ld32_async(to + 32 * k, u);
+                        tc::tmem_wait_ld(u);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e++) u[e] = 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4 *>(pp + ((size_t)(k * 8 + e / 4) * kPartRows + pr) * 4) =
+                            make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                }
+                pp[(size_t)kPartRows * D + pr] = m;
+                pp[(size_t)kPartRows * (D + 1) + pr] = z;
+            }
+            __threadfence();
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (threadIdx.x == 0) b.last = atomicAdd(a.cnt + blockIdx.x, 1) == np - 1;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (b.last) {
+                __threadfence();
+                if (live) {
+                    const float *p0 = a.part + first * PF;
+                    m = -INFINITY;
+                    for (int p = 0; p < np; p++) m = fmaxf(m, __ldcg(p0 + p * PF + (size_t)kPartRows * D + pr));
+                    const float sh = m == -INFINITY ? 0.f : m;
+                    z = 0.f;
+                    for (int p = 0; p < np; p++)
+                        z += __ldcg(p0 + p * PF + (size_t)kPartRows * (D + 1) + pr) *
+                             tc::ex2(__ldcg(p0 + p * PF + (size_t)kPartRows * D + pr) - sh);
+                    const float inv = z > 0.f ? 1.f / z : z;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        float v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; e++) v[e] = 0.f;
+#pragma unroll 2
+                        for (int p = 0; p < np; p++) {
+                            const float w = tc::ex2(__ldcg(p0 + p * PF + (size_t)kPartRows * D + pr) - sh);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 u = __ldcg(reinterpret_cast<const float4 *>(p0 + p * PF) +
+                                                        (size_t)((c + e) / 4) * kPartRows + pr);
+                                v[e] += w * u.x; v[e + 1] += w * u.y; v[e + 2] += w * u.z; v[e + 3] += w * u.w;
+                            }
+                        }
+                        if (lim < 0) {
+#pragma unroll
+                            for (int e = 0; e < 16; e++) v[e] = 0.f;
+                        }
+                        write8(c, v, inv);
+                        write8(c + 8, v + 8, inv);
+                    }
+                    write_lse();
+                }
+                if (threadIdx.x == 0) a.cnt[blockIdx.x] = 0;
             }
         }
     } else {
@@ -287,14 +373,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     #pragma unroll
                     for (int c = 0; c < C::NB; c++)
                         tc::tma_load_3d(tc::smem_u32(ring + st * C::TILE + c * 128 * 128), (i & 1) ? &mapV : &mapK, c * 64,
-                                        g * ((i & 1) ? t.vh : t.kh), (int)(k0 + (i >> 1) * kN), fb);
+                                        g * ((i & 1) ? t.vh : t.kh), (int)(k0 + (j0 + (i >> 1)) * kN), fb);
                     issued++;
                 }
             }
             issued = __shfl_sync(0xffffffffu, issued, 0);
             ok = issued == 2 * n && n > 0;
             if (fix && ok) {
-                const int st = (2 * n - 1) % C::NST, keep = nk - (n - 1) * kN;
+                const int st = (2 * n - 1) % C::NST;
                 if (wait(&b.full[st], ((2 * n - 1) / C::NST) & 1, b, a.status)) {
                     for (int i = lane; i < (kN - keep) * C::NB * 8; i += 32) {
                         const int r = keep + i / (C::NB * 8), c = i % (C::NB * 8);
@@ -396,7 +482,7 @@ bool make_map(CUtensorMap *m, const void *p, int64_t tokens, int heads, int d, i
 }
 
 template <int D>
-cudaError_t launch(const PromptArgs &a, cudaStream_t s) {
+cudaError_t launch(PromptArgs a, cudaStream_t s) {
     Tc t;
     t.gq = a.Hq / a.G;
     t.tpt = 128 / t.gq;
@@ -427,7 +513,9 @@ cudaError_t launch(const PromptArgs &a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         ready[dev].store(1, std::memory_order_relaxed);
     }
-    prompt_tc_kernel<D><<<(unsigned)blocks, kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
+    // fewer blocks than SMs: their keys are split over the others
+    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPromptParts / 2 / blocks, (a.n_k + kN - 1) / kN / kLeast));
+    prompt_tc_kernel<D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
     return cudaGetLastError();
 }
 
