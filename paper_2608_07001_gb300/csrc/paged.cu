@@ -17,6 +17,8 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace gkv {
 namespace {
 
@@ -25,6 +27,26 @@ using namespace serve;
 struct Turns {
     unsigned long long f[64];      // 2^64 theta_i / (2 pi)
 };
+
+// The table of a base, kept per host thread for the calls of a step (d / 2 fp64
+// powers take longer than a launch).
+const Turns &turns_of(double base, int d) {
+    thread_local double have = 0.0;
+    thread_local int have_d = 0;
+    thread_local Turns t{};
+    if (base > 0.0 && (base != have || d != have_d)) {
+        for (int i = 0; i < d / 2; i++) {
+            // theta / (2 pi) of a turn; whole turns (bases below 1) drop out
+            const double f = pow(base, -2.0 * i / d) / 6.283185307179586476925287;
+            t.f[i] = (unsigned long long)ldexp(f - floor(f), 64);
+        }
+        have = base;
+        have_d = d;
+    }
+    return t;
+}
+
+constexpr int64_t kAppendMany = 1 << 19;      // row chunks from which a thread takes 8 rows
 
 struct AppendArgs {
     Paged c;
@@ -56,21 +78,27 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
     b = *reinterpret_cast<uint4 *>(xb);
 }
 
-// One thread per (token, row of the token, 16-byte chunk of each half); rows:
-// G keys, G values, Hq queries.
-template <typename T, int D>
+// A token has 2 G + Hq rows (keys, values, queries).  One thread: the token,
+// one 16-byte chunk of each half, and R of the rows, `stride` apart, so that
+// its sines and cosines serve R rows.  Neighbouring threads take neighbouring
+// chunks: a row's half is one 64- to 256-byte line.
+template <typename T, int D, int R>
 __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
-    const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
+    const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0), stride = (rows + R - 1) / R;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int ch = (int)(i % CH);
-    const int r = (int)(i / CH % rows);
-    const int64_t t = i / CH / rows;
+    const int r0 = (int)(i / CH % stride);
+    const int64_t t = i / CH / stride;
     if (t >= a.n_tokens) return;
-    const bool is_q = r >= 2 * a.c.G, is_v = !is_q && r >= a.c.G;
-    const int h = is_q ? r - 2 * a.c.G : is_v ? r - a.c.G : r;
+    // the request and the entries from the token to its end: looked up by threads with a key or value row
+    int b = (int)t, tail = r0 < 2 * a.c.G ? 1 : 0;
+    if (tail && a.cu_new) {
+        b = seq_of(a.cu_new, a.c.B, t);
+        tail = t >= a.cu_new[b] && t < a.cu_new[b + 1] ? a.cu_new[b + 1] - (int)t : 0;       // 0: of no request
+    }
     float cs[N], sn[N];
-    if (!is_v && a.rotate) {
+    if (a.rotate) {
         const long long p = a.pos[t];
 #pragma unroll
         for (int j = 0; j < N; j++) {
@@ -78,30 +106,59 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
             sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
         }
     }
-    const char *src = (is_q ? a.q + t * a.q_ts + h * a.q_hs : is_v ? a.v + t * a.v_ts + h * a.v_hs
-                                                                  : a.k + t * a.k_ts + h * a.k_hs) + ch * 16;
-    uint4 x = ld16(src), y = ld16(src + RB / 2);
-    if (!is_v && a.rotate) turn16<T>(x, y, cs, sn);
-    char *dst;
-    if (is_q) {
-        dst = a.q_out + t * a.qo_ts + h * a.qo_hs;
-    } else {
-        int b = (int)t, tail = 1;
-        if (a.cu_new) {
-            b = seq_of(a.cu_new, a.c.B, t);
-            if (t < a.cu_new[b] || t >= a.cu_new[b + 1]) return;        // a token of no request
-            tail = a.cu_new[b + 1] - (int)t;
+    constexpr int U = R < 4 ? R : 4;          // rows in flight
+#pragma unroll 1
+    for (int k0 = 0; k0 < R; k0 += U) {
+        uint4 x[U], y[U];
+        char *dst[U];
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+            const int r = r0 + (k0 + k) * stride;
+            dst[k] = nullptr;
+            if (r >= rows) continue;
+            const char *src;
+            if (r >= 2 * a.c.G) {
+                const int h = r - 2 * a.c.G;
+                src = a.q + t * a.q_ts + h * a.q_hs;
+                dst[k] = a.q_out + t * a.qo_ts + h * a.qo_hs;
+            } else {
+                const bool is_v = r >= a.c.G;
+                const int h = is_v ? r - a.c.G : r;
+                src = is_v ? a.v + t * a.v_ts + h * a.v_hs : a.k + t * a.k_ts + h * a.k_hs;
+                const int64_t s = ((int64_t)a.l * a.c.B + b) * a.c.G + h;
+                const int idx = tail ? a.c.lens[s] - tail : -1;
+                const int64_t row = idx >= 0 ? entry_row(a.c, s, idx, a.status) : -1;
+                if (row >= 0) {
+                    dst[k] = (is_v ? a.c.V : a.c.K) + row * RB;
+                    if (!is_v && ch == 0 && a.c.log_m) a.c.log_m[row] = 0.f;
+                }
+            }
+            x[k] = ld16(src + ch * 16);
+            y[k] = ld16(src + ch * 16 + RB / 2);
         }
-        const int64_t s = ((int64_t)a.l * a.c.B + b) * a.c.G + h;
-        const int idx = a.c.lens[s] - tail;
-        if (idx < 0) return;
-        const int64_t row = entry_row(a.c, s, idx, a.status);
-        if (row < 0) return;
-        dst = (is_v ? a.c.V : a.c.K) + row * RB;
-        if (!is_v && ch == 0 && a.c.log_m) a.c.log_m[row] = 0.f;
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+            if (!dst[k]) continue;
+            const int r = r0 + (k0 + k) * stride;
+            if (a.rotate && (r < a.c.G || r >= 2 * a.c.G)) turn16<T>(x[k], y[k], cs, sn);
+            st16(dst[k] + ch * 16, x[k]);
+            st16(dst[k] + ch * 16 + RB / 2, y[k]);
+        }
     }
-    st16(dst + ch * 16, x);
-    st16(dst + ch * 16 + RB / 2, y);
+}
+
+// R: rows of a thread.  Few tokens want every row on its own thread, the
+// latency of one row; many want a thread's sines to serve several.
+template <typename T, int D>
+void launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
+    constexpr int CH = D * (int)sizeof(T) / 32;
+    const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
+    const int64_t one = (int64_t)a.n_tokens * rows * CH;
+    const bool many = one >= kAppendMany;
+    const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 7) / 8) * CH : one;
+    const unsigned n = (unsigned)((threads + 255) / 256);
+    if (many) paged_append_kernel<T, D, 8><<<n, 256, 0, s>>>(a, turns);
+    else paged_append_kernel<T, D, 1><<<n, 256, 0, s>>>(a, turns);
 }
 
 __global__ void paged_advance_kernel(int32_t *lens, const int32_t *cu_new, int n, int B, int G) {
@@ -121,37 +178,69 @@ struct LoadArgs {
     int *status;
 };
 
-// The heads' lengths (offsets that do not fit give 0), one thread per (l, g).
-__global__ void paged_load_lens_kernel(const LoadArgs a) {
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= a.c.L * a.c.G) return;
-    const int64_t lo = a.off[i], hi = a.off[i + 1], cap = (int64_t)a.c.page_size * a.c.max_pages;
-    int64_t n = hi - lo;
-    if (lo < 0 || n < 0 || hi > a.n_entries) { atomicOr(a.status, kStRange); n = 0; }
-    if (n > cap) { atomicOr(a.status, kStRange); n = cap; }
-    a.c.lens[((int64_t)(i / a.c.G) * a.c.B + a.b) * a.c.G + i % a.c.G] = (int)n;
+// The heads' lengths (offsets that do not fit give 0), one thread per (l, g);
+// then a warp copies a run of entries, 16 bytes of the key and of the value a
+// lane and IT times.  The head is searched for the run's first entry and
+// followed from there.
+template <int RB, int IT>
+__global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
+    constexpr int CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
+    constexpr int U = IT < 4 ? IT : 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, cap = (int64_t)a.c.page_size * a.c.max_pages;
+    const int heads = a.c.L * a.c.G, lane = threadIdx.x & 31;
+    if (i < heads) {
+        const int64_t lo = a.off[i], hi = a.off[i + 1];
+        int64_t n = hi - lo;
+        if (lo < 0 || n < 0 || hi > a.n_entries) { atomicOr(a.status, kStRange); n = 0; }
+        if (n > cap) { atomicOr(a.status, kStRange); n = cap; }
+        a.c.lens[((int64_t)(i / a.c.G) * a.c.B + a.b) * a.c.G + i % a.c.G] = (int)n;
+    }
+    const int64_t e0 = (i >> 5) * (RW * IT) + lane / CH;
+    if (e0 >= a.n_entries) return;
+    int h = 0, hi = heads;
+    while (hi - h > 1) {
+        const int mid = (h + hi) >> 1;
+        if (a.off[mid] <= e0) h = mid; else hi = mid;
+    }
+    int64_t o0 = a.off[h], o1 = a.off[h + 1];
+    const int ch = lane % CH;
+#pragma unroll 1
+    for (int k0 = 0; k0 < IT; k0 += U) {
+        uint4 x[U], y[U];
+        int64_t row[U];
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+            const int64_t e = e0 + (int64_t)(k0 + k) * RW;
+            row[k] = -1;
+            if (e >= a.n_entries) continue;
+            while (e >= o1 && h + 1 < heads) {
+                h++;
+                o0 = a.off[h];
+                o1 = a.off[h + 1];
+            }
+            // an entry of no head, of offsets that do not fit, past the table: not copied
+            if (o0 < 0 || e < o0 || e >= o1 || o1 > a.n_entries || e - o0 >= cap) continue;
+            const int64_t s = ((int64_t)(h / a.c.G) * a.c.B + a.b) * a.c.G + h % a.c.G;
+            row[k] = entry_row(a.c, s, (int)(e - o0), a.status);
+            x[k] = ld16(a.K + e * RB + ch * 16);
+            y[k] = ld16(a.V + e * RB + ch * 16);
+        }
+#pragma unroll
+        for (int k = 0; k < U; k++) {
+            if (row[k] < 0) continue;
+            st16(a.c.K + row[k] * RB + ch * 16, x[k]);
+            st16(a.c.V + row[k] * RB + ch * 16, y[k]);
+            if (ch == 0 && a.c.log_m) a.c.log_m[row[k]] = a.log_m ? a.log_m[e0 + (int64_t)(k0 + k) * RW] : 0.f;
+        }
+    }
 }
 
-// One thread per (entry, 16 bytes of its key and of its value).
 template <int RB>
-__global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
-    constexpr int CH = RB / 16;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, e = i / CH;
-    const int ch = (int)(i % CH);
-    if (e >= a.n_entries) return;
-    int lo = 0, hi = a.c.L * a.c.G;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.off[mid] <= e) lo = mid; else hi = mid;
-    }
-    const int64_t o0 = a.off[lo], o1 = a.off[lo + 1];
-    if (o0 < 0 || e < o0 || e >= o1 || o1 > a.n_entries || e - o0 >= (int64_t)a.c.page_size * a.c.max_pages) return;
-    const int64_t s = ((int64_t)(lo / a.c.G) * a.c.B + a.b) * a.c.G + lo % a.c.G;
-    const int64_t row = entry_row(a.c, s, (int)(e - o0), a.status);
-    if (row < 0) return;
-    st16(a.c.K + row * RB + ch * 16, ld16(a.K + e * RB + ch * 16));
-    st16(a.c.V + row * RB + ch * 16, ld16(a.V + e * RB + ch * 16));
-    if (ch == 0 && a.c.log_m) a.c.log_m[row] = a.log_m ? a.log_m[e] : 0.f;
+void launch_load(const LoadArgs &a, cudaStream_t s) {
+    constexpr int IT = 2;
+    constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
+    const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);
+    paged_load_kernel<RB, IT><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a);
 }
 
 }  // namespace
@@ -170,14 +259,10 @@ extern "C" gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, co
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const LoadArgs a{paged_of(c), b, static_cast<const char *>(K), static_cast<const char *>(V), log_m, offsets,
                      n_entries, static_cast<int *>(workspace)};
-    paged_load_lens_kernel<<<(c->L * c->G + 255) / 256, 256, 0, s>>>(a);
     const int rb = c->d * elem_bytes(c->dtype);
-    const unsigned n = (unsigned)((n_entries * (rb / 16) + 255) / 256);
-    if (n > 0) {
-        if (rb == 128) paged_load_kernel<128><<<n, 256, 0, s>>>(a);
-        else if (rb == 256) paged_load_kernel<256><<<n, 256, 0, s>>>(a);
-        else paged_load_kernel<512><<<n, 256, 0, s>>>(a);
-    }
+    if (rb == 128) launch_load<128>(a, s);
+    else if (rb == 256) launch_load<256>(a, s);
+    else launch_load<512>(a, s);
     return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
@@ -209,24 +294,16 @@ extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, 
                  static_cast<const char *>(q), static_cast<char *>(q_out),
                  k_ts * es, k_hs * es, v_ts * es, v_hs * es, q_ts * es, q_hs * es, qo_ts * es, qo_hs * es,
                  c->rope_base > 0.0, static_cast<int *>(workspace)};
-    Turns turns{};
-    if (a.rotate)
-        for (int i = 0; i < c->d / 2; i++) {
-            // theta / (2 pi) of a turn; whole turns (bases below 1) drop out
-            const double f = pow(c->rope_base, -2.0 * i / c->d) / 6.283185307179586476925287;
-            turns.f[i] = (unsigned long long)ldexp(f - floor(f), 64);
-        }
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t items = (int64_t)n_tokens * (2 * c->G + (q ? c->Hq : 0)) * (c->d * es / 32);
-    const int64_t blocks = (items + 255) / 256;
-    if (blocks >= (1LL << 31)) return GKV_EUNSUPPORTED;
-    const unsigned n = (unsigned)blocks;
+    if ((items + 255) / 256 >= (1LL << 31)) return GKV_EUNSUPPORTED;
+    const Turns &turns = turns_of(c->rope_base, c->d);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (c->dtype == GKV_BF16) {
-        if (c->d == 128) paged_append_kernel<__nv_bfloat16, 128><<<n, 256, 0, s>>>(a, turns);
-        else paged_append_kernel<__nv_bfloat16, 64><<<n, 256, 0, s>>>(a, turns);
+        if (c->d == 128) launch_append<__nv_bfloat16, 128>(a, turns, s);
+        else launch_append<__nv_bfloat16, 64>(a, turns, s);
     } else {
-        if (c->d == 128) paged_append_kernel<float, 128><<<n, 256, 0, s>>>(a, turns);
-        else paged_append_kernel<float, 64><<<n, 256, 0, s>>>(a, turns);
+        if (c->d == 128) launch_append<float, 128>(a, turns, s);
+        else launch_append<float, 64>(a, turns, s);
     }
     return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }

@@ -12,6 +12,9 @@
 //     every head its own).  A CTA finds its run from the lengths alone: its
 //     threads sum them in segments and one thread walks the segment its run
 //     begins in.  A run meets one or more sequences; each meeting is a piece.
+//     Where the longest sequence has few tiles (kPaSnap), a run takes the
+//     sequences that begin in it whole instead: joining pieces costs more than
+//     the tiles that it would spread.
 //   * One producer warp streams a piece's tiles through a ring of shared memory:
 //     TMA boxes of up to 64 rows that do not cross a page (the box height is the
 //     largest of 64, 32, 16 dividing the page), 128-byte swizzle, log m as a
@@ -58,7 +61,7 @@ constexpr int kPaF32Warps = 3;                     // of them take tiles in the 
 constexpr int kPaRing = 96 * 1024;                 // bytes of the ring
 constexpr int kPaPerSm = 2;                        // resident CTAs a SM
 constexpr int kPaMaxGrid = 512;
-constexpr int kPaMinTiles = 4;                     // tiles a CTA takes at least
+constexpr int kPaSnap = 8;                         // tiles of the longest sequence up to which none is split
 constexpr uint64_t kPaWaitNs = 2000000000ull;
 
 template <typename T, int D>
@@ -68,6 +71,7 @@ struct PaCfg {
     static constexpr int NB = D * (int)sizeof(T) / 128;          // 128-byte column boxes of a row
     static constexpr int TB = NB * TE * 128;       // bytes of a tile's keys
     static constexpr int NST = kPaRing / (2 * TB); // stages
+    static constexpr int MIN = BF ? 4 : 3;         // tiles of a run at least
     static_assert(NST >= 3 && NST <= 12 && (BF || NST % kPaF32Warps == 0), "ring");
 };
 
@@ -94,6 +98,7 @@ struct PaSmem {
     int s_first;
     int abort, last;
     long long wsum[kPaThreads / 32];
+    int wmax[kPaThreads / 32];
     float m[kPaWarps][8], z[kPaWarps][8], M[8], Z[8];
 };
 
@@ -411,11 +416,16 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     // ---- the CTA's run: tiles of all sequences, and where its own begin
     const int seg = (S + kPaThreads - 1) / kPaThreads;
     long long mine = 0;
+    int most = 0;
     for (int s = tid * seg; s < min(S, (tid + 1) * seg); s++) {
         const int n = pa_len(a, s);
         if (n < a.lens[s]) atomicOr(a.status, kStRange);
         mine += (n + C::TE - 1) / C::TE;
+        most = max(most, (n + C::TE - 1) / C::TE);
     }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (lane == 0) sm.wmax[warp] = most;
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -437,8 +447,10 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     for (int w = 0; w < kPaThreads / 32; w++) {
         if (w < warp) before += sm.wsum[w];
         total += sm.wsum[w];
+        most = max(most, sm.wmax[w]);
     }
-    const long long nc = min((long long)gridDim.x, (total + kPaMinTiles - 1) / kPaMinTiles);
+    const bool snap = most <= kPaSnap;
+    const long long nc = min((long long)gridDim.x, (total + C::MIN - 1) / C::MIN);
     const long long lo = (long long)blockIdx.x < nc ? blockIdx.x * total / nc : total;
     const long long hi = (long long)blockIdx.x < nc ? (blockIdx.x + 1) * total / nc : total;
     if (lo < hi && lo >= before && lo < before + mine) {
@@ -448,6 +460,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             if (lo < before + n) break;
             before += n;
         }
+        if (snap && lo > before) before += (pa_len(a, s++) + C::TE - 1) / C::TE;
         sm.s_first = s;
         sm.first = before;
     }
@@ -470,7 +483,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         long long vs = sm.first;
         for (int s = sm.s_first; ok && s < S && vs < hi; s++) {
             const int n = pa_len(a, s), nt = (n + C::TE - 1) / C::TE;
-            const int t0 = (int)(max(lo, vs) - vs), t1 = (int)(min(hi, vs + nt) - vs);
+            const int t0 = snap ? 0 : (int)(max(lo, vs) - vs), t1 = snap ? nt : (int)(min(hi, vs + nt) - vs);
             vs += nt;
             int held0 = 0, held = 0;                 // boxes [held0, held0 + held) looked up, one a lane
             int row = -1;
@@ -535,7 +548,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         const int n = pa_len(a, s), nt = (n + C::TE - 1) / C::TE;
         if (nt == 0) continue;
         const long long ve = vs + nt;
-        const int t0 = (int)(max(lo, vs) - vs), t1 = (int)(min(hi, ve) - vs);
+        const int t0 = snap ? 0 : (int)(max(lo, vs) - vs), t1 = snap ? nt : (int)(min(hi, ve) - vs);
         if constexpr (C::BF) {
             w.begin(a, s, gq);
         } else {
@@ -575,7 +588,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         }
         T *out = static_cast<T *>(a.out) + (size_t)s * gq * D;
         const int c_lo = pa_run_of(vs, total, nc), c_hi = pa_run_of(ve - 1, total, nc);
-        if (c_lo == c_hi) {
+        if (snap || c_lo == c_hi) {
             for (int i = tid; i < gq * D; i += kPaCons) {
                 const float Z = sm.Z[i / D];
                 put(out + i, Z > 0.f ? sum[i] / Z : 0.f);
@@ -594,28 +607,33 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                 __threadfence();
                 const int np = c_hi - c_lo + 1;
                 auto piece = [&](int p) { return a.part + (size_t)(2 * (c_lo + p) + (p == 0)) * PF; };
-                for (int h = warp; h < gq; h += kPaWarps) {        // one warp a head: maximum, sum
-                    float M = -INFINITY, Z = 0.f;
-                    for (int p = lane; p < np; p += 32) M = fmaxf(M, __ldcg(piece(p) + 8 * D + h));
-#pragma unroll
-                    for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-                    for (int p = lane; p < np; p += 32)
-                        Z += __ldcg(piece(p) + 8 * D + 8 + h) * tc::ex2(__ldcg(piece(p) + 8 * D + h) - pa_shift(M));
-#pragma unroll
-                    for (int o = 16; o >= 1; o >>= 1) Z += __shfl_xor_sync(0xffffffffu, Z, o);
-                    if (lane == 0) { sm.M[h] = M; sm.Z[h] = Z; }
-                }
-                pa_sync();
+                // four channels a thread, over the pieces in order, eight loads in flight
                 for (int i = tid * 4; i < gq * D; i += kPaCons * 4) {
                     const int h = i / D;
-                    const float sh = pa_shift(sm.M[h]), Z = sm.Z[h];
+                    float M = -INFINITY, Z = 0.f;
                     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int p = 0; p < np; p++) {
-                        const float *q = piece(p);
-                        const float f = tc::ex2(__ldcg(q + 8 * D + h) - sh);
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(q + i));
-                        v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+                    for (int p0 = 0; p0 < np; p0 += 8) {
+                        float m[8], z[8], mx = M;
+                        float4 x[8];
+#pragma unroll
+                        for (int p = 0; p < 8; p++) {
+                            const float *q = piece(p0 + p);
+                            const bool on = p0 + p < np;
+                            m[p] = on ? __ldcg(q + 8 * D + h) : -INFINITY;
+                            z[p] = on ? __ldcg(q + 8 * D + 8 + h) : 0.f;
+                            x[p] = on ? __ldcg(reinterpret_cast<const float4 *>(q + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            mx = fmaxf(mx, m[p]);
+                        }
+                        const float sh = pa_shift(mx), f = tc::ex2(M - sh);
+                        M = mx;
+                        Z *= f;
+                        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll
+                        for (int p = 0; p < 8; p++) {
+                            const float g = tc::ex2(m[p] - sh);
+                            Z += g * z[p];
+                            v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
+                        }
                     }
                     const float r = Z > 0.f ? 1.f / Z : 0.f;
                     put(out + i, v.x * r); put(out + i + 1, v.y * r); put(out + i + 2, v.z * r); put(out + i + 3, v.w * r);

@@ -8,9 +8,10 @@
 // exp(M - M').
 //
 // bf16 runs on tcgen05 (prompt_tc.cu), fp32 on CUDA cores (prompt_f32.cu).
-// This file checks the arguments and lays out the workspace: the status word,
-// the counters of split blocks, their parts.
+// This file checks the arguments, lays out the workspace (the status word, the
+// parts of split blocks) and joins the parts.
 #include "prompt.cuh"
+#include "tc.cuh"
 
 #include <math.h>
 
@@ -19,7 +20,75 @@ namespace {
 
 using namespace serve;
 
-constexpr size_t kCntBytes = (serve::kPromptParts * sizeof(int) + 255) / 256 * 256;
+// One thread: four channels of a row, over the block's parts in order, eight
+// loads in flight.  TC: a warp takes 32 rows of one channel group, as the parts
+// lie; else neighbouring groups of a row.
+template <typename T, int D, bool TC>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
+    constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? kKeysTc : kKeysF32;
+    constexpr size_t PF = part_floats(ROWS, D);
+    const int i = blockIdx.y * 256 + threadIdx.x;
+    const int r = TC ? i % ROWS : i / (D / 4), c = TC ? i / ROWS : i % (D / 4);
+    const int gq = a.Hq / a.G, half = TC ? kRowsTc / 2 : kRowsF32, tpt = half / gq, tok = TC ? 2 * tpt : tpt;
+    const int g = blockIdx.x % a.G;
+    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
+    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    int64_t q0, nq, k0, nk;
+    if (!seq_bounds(a, s, q0, nq, k0, nk)) return;
+    const int64_t t0 = (slot - (q0 / tok + s)) * tok;
+    if (t0 < 0 || t0 >= nq) return;
+    const int last = (int)((nq < t0 + tok ? nq : t0 + tok) - 1 + nk - nq);
+    const int np = parts_of(last >= 0 ? last / KEYS + 1 : 0, a.split);
+    const int tk = r % half / gq;
+    const int64_t t = t0 + r / half * tpt + tk;
+    if (np == 1 || tk >= tpt || t >= nq) return;
+    const float *p0 = a.part + (size_t)blockIdx.x * a.split * PF;
+    const size_t at = TC ? (size_t)c * ROWS + r : (size_t)r * (D / 4) + c;
+    float M = -INFINITY, Z = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int b = 0; b < np; b += 8) {
+        float m[8], z[8], mx = M;
+        float4 x[8];
+#pragma unroll
+        for (int p = 0; p < 8; p++) {
+            const float *q = p0 + (size_t)(b + p) * PF;
+            const bool on = b + p < np;
+            m[p] = on ? q[ROWS * D + r] : -INFINITY;
+            z[p] = on ? q[ROWS * D + ROWS + r] : 0.f;
+            x[p] = on ? reinterpret_cast<const float4 *>(q)[at] : make_float4(0.f, 0.f, 0.f, 0.f);
+            mx = fmaxf(mx, m[p]);
+        }
+        const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
+        M = mx;
+        Z *= w;
+        v.x *= w; v.y *= w; v.z *= w; v.w *= w;
+#pragma unroll
+        for (int p = 0; p < 8; p++) {
+            const float f = tc::ex2(m[p] - sh);
+            Z += f * z[p];
+            v.x += f * x[p].x; v.y += f * x[p].y; v.z += f * x[p].z; v.w += f * x[p].w;
+        }
+    }
+    // a row that sees no key: 0; a NaN stays
+    const float inv = Z > 0.f ? 1.f / Z : Z;
+    const int h = g * gq + r % half % gq;
+    T *o = static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + c * 4;
+    put(o, v.x * inv);
+    put(o + 1, v.y * inv);
+    put(o + 2, v.z * inv);
+    put(o + 3, v.w * inv);
+    if (c == 0 && a.lse) a.lse[(q0 + t) * a.Hq + h] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.6931471805599453f;
+}
+
+template <typename T, bool TC>
+cudaError_t join(const PromptArgs &a, int d, cudaStream_t s) {
+    constexpr int ROWS = TC ? kRowsTc : kRowsF32;
+    const int gq = a.Hq / a.G, tok = TC ? 2 * (kRowsTc / 2 / gq) : kRowsF32 / gq;
+    const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS * (d / 4) / 256);
+    if (d == 128) prompt_join_kernel<T, 128, TC><<<grid, 256, 0, s>>>(a);
+    else prompt_join_kernel<T, 64, TC><<<grid, 256, 0, s>>>(a);
+    return cudaGetLastError();
+}
 
 gkv_status check_geometry(const gkv_prompt *p) {
     if (!p || p->G <= 0 || p->Hq <= 0 || p->Hq % p->G) return GKV_EINVAL;
@@ -43,8 +112,10 @@ gkv_status check_prompt(const gkv_prompt *p) {
 }  // namespace
 
 namespace serve {
-// The tcgen05 kernel's parts hold 256 rows, the fp32 kernel's 64.
-size_t prompt_part_floats(int d, int dtype) { return (size_t)(dtype == GKV_BF16 ? 256 : kPromptF32Rows) * (d + 2); }
+cudaError_t launch_prompt_join(const PromptArgs &a, int d, int dtype, bool tc_parts, cudaStream_t s) {
+    if (dtype == GKV_F32) return join<float, false>(a, d, s);
+    return tc_parts ? join<__nv_bfloat16, true>(a, d, s) : join<__nv_bfloat16, false>(a, d, s);
+}
 }  // namespace serve
 }  // namespace gkv
 
@@ -54,8 +125,9 @@ extern "C" gkv_status gracekv_prompt_workspace_size(const gkv_prompt *p, size_t 
     const gkv_status st = check_geometry(p);
     if (st != GKV_OK) return st;
     if (!bytes) return GKV_EINVAL;
-    *bytes = serve::kWsHead + kCntBytes +
-             (size_t)serve::kPromptParts * serve::prompt_part_floats(p->d, p->dtype) * sizeof(float);
+    const size_t f32 = serve::kPartsF32 * serve::part_floats(serve::kRowsF32, p->d);
+    const size_t tc = p->dtype == GKV_BF16 ? serve::kPartsTc * serve::part_floats(serve::kRowsTc, p->d) : 0;
+    *bytes = serve::kWsHead + (f32 > tc ? f32 : tc) * sizeof(float);
     return GKV_OK;
 }
 
@@ -68,8 +140,7 @@ extern "C" gkv_status gracekv_prompt_attention(const gkv_prompt *p, void *worksp
     const serve::PromptArgs a{p->q, p->k, p->v, p->out, p->lse, p->cu_q, p->cu_k, p->n_seqs, p->G, p->Hq, p->n_q, p->n_k,
                               p->q_ts, p->q_hs, p->k_ts, p->k_hs, p->v_ts, p->v_hs, p->o_ts, p->o_hs,
                               (float)(1.0 / sqrt((double)p->d)), reinterpret_cast<int *>(ws),
-                              reinterpret_cast<int *>(ws + serve::kWsHead),
-                              reinterpret_cast<float *>(ws + serve::kWsHead + kCntBytes), 1};
+                              reinterpret_cast<float *>(ws + serve::kWsHead), 1};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaErrorNotSupported;
     if (p->dtype == GKV_BF16) e = serve::launch_prompt_tc(a, p->d, s);

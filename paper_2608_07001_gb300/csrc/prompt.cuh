@@ -6,7 +6,13 @@
 namespace gkv {
 namespace serve {
 
-constexpr int kPromptParts = 304;  // parts of key ranges kept at once (split blocks; two a SM)
+// A launch with few blocks splits each block's keys into parts that run beside
+// one another and leave O, M and Z in the workspace; a second launch joins them
+// in order.  Most parts kept at once: one CTA a SM (tcgen05), four a SM (fp32,
+// whose parts are a quarter of the rows and two CTAs are resident).
+constexpr int kPartsTc = 152, kPartsF32 = 608;
+constexpr int kRowsTc = 256, kRowsF32 = 64;        // rows of a block
+constexpr int kKeysTc = 128, kKeysF32 = 64;        // keys of a tile
 
 struct PromptArgs {
     const void *q, *k, *v;
@@ -17,8 +23,7 @@ struct PromptArgs {
     int64_t n_q, n_k, q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
     float scale;                   // 1 / sqrt(d)
     int *status;
-    int *cnt;                      // [kPromptParts] parts finished of every split block, 0 between calls
-    float *part;                   // [kPromptParts] partial results
+    float *part;                   // partial results
     int split;                     // most parts of a block's keys (set by the launchers)
 };
 
@@ -54,15 +59,15 @@ __device__ __forceinline__ void check_bounds(const PromptArgs &a) {
     }
 }
 
-// Parts of a block of n key tiles when a launch splits blocks `split` ways, at
-// least `least` tiles a part.
-__host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
-    const int most = (n + least - 1) / least;
-    return most < 1 ? 1 : most < split ? most : split;
-}
+// Parts of a block of n key tiles when a launch splits blocks `split` ways.
+__host__ __device__ __forceinline__ int parts_of(int n, int split) { return n < 1 ? 1 : n < split ? n : split; }
+// Floats of a part: 4-channel groups of the sums (by row or by group), then the
+// rows' maxima (base 2) and weight sums.
+__host__ __device__ constexpr size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
 
-constexpr int kPromptF32Rows = 64;     // rows of a block of the fp32 kernel
-size_t prompt_part_floats(int d, int dtype);       // of one part in the workspace
+// Joins the parts of a split launch of the tcgen05 kernel (sums [d / 4][rows])
+// or of the fp32 kernel ([rows][d / 4]).
+cudaError_t launch_prompt_join(const PromptArgs &a, int d, int dtype, bool tc_parts, cudaStream_t s);
 
 // bf16 on tcgen05; cudaErrorNotSupported when a tensor's strides have no tensor map.
 cudaError_t launch_prompt_tc(const PromptArgs &a, int d, cudaStream_t s);

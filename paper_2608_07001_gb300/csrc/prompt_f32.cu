@@ -12,9 +12,8 @@
 // the issue slots, along the channels for S and across output columns for PV.
 // K of the next tile arrives (cp.async) under PV, V under S.  Two blocks a SM.
 //
-// When a launch has fewer blocks than the GPU holds, a block's keys are split:
-// a part leaves O, M and Z in the workspace and the last one to finish, found
-// with a counter, joins them in order, so results do not depend on timing.
+// When a launch has fewer blocks than the GPU holds, a block's keys are split
+// into parts (prompt.cuh) that prompt.cu joins.
 #include "prompt.cuh"
 #include "tc.cuh"
 
@@ -27,9 +26,8 @@ namespace gkv {
 namespace serve {
 namespace {
 
-constexpr int kR = kPromptF32Rows, kK = 64, kThreads = 128;
+constexpr int kR = kRowsF32, kK = kKeysF32, kThreads = 128;
 constexpr int kPs = kK + 4;                    // floats of a row of P
-constexpr int kLeast = 1;                      // key tiles of a part at least
 
 template <int D>
 struct Cfg {
@@ -59,7 +57,6 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     using C = Cfg<D>;
     extern __shared__ __align__(16) float sm[];
     float *Qs = sm, *Ks = Qs + C::Q, *Vs = Ks + C::K, *Ps = Vs + C::V;
-    __shared__ int last_s;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
 
@@ -74,7 +71,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64, off = nk - nq;
     const int last = min(nq, t0 + tok) - 1 + off;
     const int n = last >= 0 ? last / kK + 1 : 0;
-    const int np = parts_of(n, a.split, kLeast);
+    const int np = parts_of(n, a.split);
     if ((int)blockIdx.y >= np) return;
     const int j0 = (int)((int64_t)blockIdx.y * n / np), j1 = (int)((int64_t)(blockIdx.y + 1) * n / np);
 
@@ -196,67 +193,38 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
 #pragma unroll
         for (int w = 8; w >= 1; w >>= 1) z[i] += __shfl_xor_sync(0xffffffffu, z[i], w);
 
-    auto write = [&](int r, int col, float4 v, float M, float Z) {       // 4 outputs of row r
-        const int tk = r / gq, t = t0 + tk;
-        if (tk >= tok || t >= nq) return;
-        const int h = g * gq + r % gq;
-        const float inv = Z > 0.f ? 1.f / Z : Z;
-        T *p = static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + col;
-        put(p, v.x * inv);
-        put(p + 1, v.y * inv);
-        put(p + 2, v.z * inv);
-        put(p + 3, v.w * inv);
-        if (col == 0 && a.lse) a.lse[(q0 + t) * a.Hq + h] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.6931471805599453f;
-    };
-    if (np == 1) {
+    if (np > 1) {       // a part: [kR][D] sums, then [kR] maxima, [kR] sums of weights
+        float *pp = a.part + ((size_t)blockIdx.x * a.split + blockIdx.y) * part_floats(kR, D);
 #pragma unroll
-        for (int i = 0; i < 8; i++)
+        for (int i = 0; i < 8; i++) {
 #pragma unroll
             for (int c = 0; c < D / 64; c++)
-                write(ty * 8 + i, c * 64 + tx * 4, make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y),
-                      m[i], z[i]);
+                *reinterpret_cast<float4 *>(pp + (ty * 8 + i) * D + c * 64 + tx * 4) =
+                    make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
+            if (tx == 0) { pp[kR * D + ty * 8 + i] = m[i]; pp[kR * (D + 1) + ty * 8 + i] = z[i]; }
+        }
         return;
     }
-    // ---- a part: [kR][D] sums, then [kR] maxima, [kR] sums of weights
-    constexpr int PF = kR * (D + 2);
-    const int64_t first = (int64_t)blockIdx.x * a.split;
-    float *pp = a.part + (first + blockIdx.y) * PF;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
+        const int r = ty * 8 + i, tk = r / gq, t = t0 + tk, h = g * gq + r % gq;
+        if (tk >= tok || t >= nq) continue;
+        const float inv = z[i] > 0.f ? 1.f / z[i] : z[i];        // no key: 0; a NaN stays
+        T *p = static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + tx * 4;
 #pragma unroll
-        for (int c = 0; c < D / 64; c++)
-            *reinterpret_cast<float4 *>(pp + (ty * 8 + i) * D + c * 64 + tx * 4) =
-                make_float4(o[i][2 * c].x, o[i][2 * c].y, o[i][2 * c + 1].x, o[i][2 * c + 1].y);
-        if (tx == 0) { pp[kR * D + ty * 8 + i] = m[i]; pp[kR * (D + 1) + ty * 8 + i] = z[i]; }
-    }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) last_s = atomicAdd(a.cnt + blockIdx.x, 1) == np - 1;
-    __syncthreads();
-    if (!last_s) return;
-    __threadfence();
-    const float *p0 = a.part + first * PF;
-    for (int i = tid; i < kR * (D / 4); i += kThreads) {
-        const int r = i / (D / 4), col = (i % (D / 4)) * 4;
-        float M = -INFINITY, Z = 0.f;
-        for (int p = 0; p < np; p++) M = fmaxf(M, __ldcg(p0 + (size_t)p * PF + kR * D + r));
-        const float sh = M == -INFINITY ? 0.f : M;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int p = 0; p < np; p++) {
-            const float *q = p0 + (size_t)p * PF;
-            const float w = tc::ex2(__ldcg(q + kR * D + r) - sh);
-            const float4 u = __ldcg(reinterpret_cast<const float4 *>(q + r * D + col));
-            Z += w * __ldcg(q + kR * (D + 1) + r);
-            v.x += w * u.x; v.y += w * u.y; v.z += w * u.z; v.w += w * u.w;
+        for (int c = 0; c < D / 64; c++) {
+            put(p + c * 64, o[i][2 * c].x * inv);
+            put(p + c * 64 + 1, o[i][2 * c].y * inv);
+            put(p + c * 64 + 2, o[i][2 * c + 1].x * inv);
+            put(p + c * 64 + 3, o[i][2 * c + 1].y * inv);
         }
-        write(r, col, v, M, Z);
+        if (tx == 0 && a.lse)
+            a.lse[(q0 + t) * a.Hq + h] = z[i] == 0.f ? -INFINITY : (m[i] + log2f(z[i])) * 0.6931471805599453f;
     }
-    if (tid == 0) a.cnt[blockIdx.x] = 0;
 }
 
 template <typename T, int D>
-cudaError_t launch(PromptArgs a, cudaStream_t s) {
+cudaError_t launch(PromptArgs a, int dtype, cudaStream_t s) {
     static std::atomic<int> ready[kMaxDevices];
     const size_t smem = Cfg<D>::SMEM;
     int dev = 0;
@@ -272,16 +240,17 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
     const int64_t blocks = prompt_slots(a.n_q, a.n_seqs, tok) * a.G;
     if (blocks >= (1LL << 31)) return cudaErrorInvalidConfiguration;
     // as many parts as fit beside one another, none smaller than a key tile
-    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPromptParts / blocks, (a.n_k + kK - 1) / kK));
+    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsF32 / blocks, (a.n_k + kK - 1) / kK));
     prompt_f32_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, smem, s>>>(a);
-    return cudaGetLastError();
+    e = cudaGetLastError();
+    return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, dtype, false, s) : e;
 }
 
 }  // namespace
 
 cudaError_t launch_prompt_f32(const PromptArgs &a, int d, int dtype, cudaStream_t s) {
-    if (dtype == GKV_BF16) return d == 128 ? launch<__nv_bfloat16, 128>(a, s) : launch<__nv_bfloat16, 64>(a, s);
-    return d == 128 ? launch<float, 128>(a, s) : launch<float, 64>(a, s);
+    if (dtype == GKV_BF16) return d == 128 ? launch<__nv_bfloat16, 128>(a, dtype, s) : launch<__nv_bfloat16, 64>(a, dtype, s);
+    return d == 128 ? launch<float, 128>(a, dtype, s) : launch<float, 64>(a, dtype, s);
 }
 
 }  // namespace serve

@@ -24,8 +24,7 @@
 // also tells that PV(j) is done: the rescaling needs no barrier of its own.
 //
 // Few blocks (a short chunk over a long cache) leave SMs idle: then a block's
-// keys are split into parts that leave O, M and Z in the workspace, and the
-// last part to finish, found with a counter, joins them in order.
+// keys are split into parts (prompt.cuh) that prompt.cu joins.
 //
 // Masks: only the tiles that reach past a row's last key compare columns; the
 // keys past a sequence's end get weight 0 that way, and their V rows, which
@@ -42,14 +41,12 @@ namespace gkv {
 namespace serve {
 namespace {
 
-constexpr int kN = 128;                        // keys of a tile
+constexpr int kN = kKeysTc;
 constexpr int kThreads = 384;                  // three warpgroups: two of softmax, one of TMA and MMA issue
 // Registers a thread after the split; 256 x 208 + 128 x 88 = 384 x 168, the launch's own.
 constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
 static_assert(256 * kRegsSoftmax + 128 * kRegsIssue <= kThreads * kRegs, "register split");
 constexpr int kWarpTma = 8, kWarpMma = 9;
-constexpr int kLeast = 2;                      // key tiles of a part at least
-constexpr int kPartRows = 256;
 constexpr float kLazy = 8.f;                   // log2 of the growth a reference lets pass
 constexpr uint64_t kWaitNs = 2000000000ull;
 
@@ -64,7 +61,7 @@ struct Cfg {
 struct Bars {
     uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], odone[2], vfix, fin;
     uint32_t tbase;
-    int abort, last;
+    int abort;
 };
 
 struct Tc {
@@ -124,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // them this part's: [j0, j0 + n)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
     const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
-    const int all = max(all0, all1), np = parts_of(all, a.split, kLeast);
+    const int all = max(all0, all1), np = parts_of(all, a.split);
     if ((int)blockIdx.y >= np) return;
     const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
     const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
@@ -281,9 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else {
             // a part: [D / 4][rows] sums of 4 channels, then [rows] references, [rows] sums of weights
-            constexpr size_t PF = (size_t)kPartRows * (D + 2);
-            const size_t first = (size_t)blockIdx.x * a.split;
-            float *pp = a.part + (first + blockIdx.y) * PF;
+            float *pp = a.part + ((size_t)blockIdx.x * a.split + blockIdx.y) * part_floats(kRowsTc, D);
             const int pr = i * 128 + r;
             if (ok && i < ntile) {
 #pragma unroll
@@ -298,53 +293,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4 *>(pp + ((size_t)(k * 8 + e / 4) * kPartRows + pr) * 4) =
+                        *reinterpret_cast<uint4 *>(pp + ((size_t)(k * 8 + e / 4) * kRowsTc + pr) * 4) =
                             make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
                 }
-                pp[(size_t)kPartRows * D + pr] = m;
-                pp[(size_t)kPartRows * (D + 1) + pr] = z;
-            }
-            __threadfence();
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (threadIdx.x == 0) b.last = atomicAdd(a.cnt + blockIdx.x, 1) == np - 1;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (b.last) {
-                __threadfence();
-                if (live) {
-                    const float *p0 = a.part + first * PF;
-                    m = -INFINITY;
-                    for (int p = 0; p < np; p++) m = fmaxf(m, __ldcg(p0 + p * PF + (size_t)kPartRows * D + pr));
-                    const float sh = m == -INFINITY ? 0.f : m;
-                    z = 0.f;
-                    for (int p = 0; p < np; p++)
-                        z += __ldcg(p0 + p * PF + (size_t)kPartRows * (D + 1) + pr) *
-                             tc::ex2(__ldcg(p0 + p * PF + (size_t)kPartRows * D + pr) - sh);
-                    const float inv = z > 0.f ? 1.f / z : z;
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        float v[16];
-#pragma unroll
-                        for (int e = 0; e < 16; e++) v[e] = 0.f;
-#pragma unroll 2
-                        for (int p = 0; p < np; p++) {
-                            const float w = tc::ex2(__ldcg(p0 + p * PF + (size_t)kPartRows * D + pr) - sh);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const float4 u = __ldcg(reinterpret_cast<const float4 *>(p0 + p * PF) +
-                                                        (size_t)((c + e) / 4) * kPartRows + pr);
-                                v[e] += w * u.x; v[e + 1] += w * u.y; v[e + 2] += w * u.z; v[e + 3] += w * u.w;
-                            }
-                        }
-                        if (lim < 0) {
-#pragma unroll
-                            for (int e = 0; e < 16; e++) v[e] = 0.f;
-                        }
-                        write8(c, v, inv);
-                        write8(c + 8, v + 8, inv);
-                    }
-                    write_lse();
-                }
-                if (threadIdx.x == 0) a.cnt[blockIdx.x] = 0;
+                pp[(size_t)kRowsTc * D + pr] = m;
+                pp[(size_t)kRowsTc * (D + 1) + pr] = z;
             }
         }
     } else {
@@ -514,9 +467,10 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
         ready[dev].store(1, std::memory_order_relaxed);
     }
     // fewer blocks than SMs: their keys are split over the others
-    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPromptParts / 2 / blocks, (a.n_k + kN - 1) / kN / kLeast));
+    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + kN - 1) / kN));
     prompt_tc_kernel<D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
-    return cudaGetLastError();
+    e = cudaGetLastError();
+    return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, GKV_BF16, true, s) : e;
 }
 
 }  // namespace

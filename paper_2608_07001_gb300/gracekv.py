@@ -522,14 +522,16 @@ def _bad(why: str):
     return GraceKVError(GKV_EINVAL, why)
 
 
-def _rows(name: str, t: torch.Tensor, n: int, heads: int, d: int, dtype, device):
-    """(pointer, token stride, head stride) of [n, heads, d] rows with contiguous channels."""
+def _refuse(name: str, t: torch.Tensor, shape, dtype, device):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype or t.device != device:
-        raise _bad(f"{name} is {t.dtype} on {t.device}, not {dtype} on {device}")
-    if tuple(t.shape) != (n, heads, d):
-        raise _bad(f"{name} is {tuple(t.shape)}, not {(n, heads, d)}")
+    raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} {tuple(shape)} on {device}")
+
+
+def _rows(name: str, t: torch.Tensor, n: int, heads: int, d: int, dtype, device):
+    """(pointer, token stride, head stride) of [n, heads, d] rows with contiguous channels."""
+    if t.dtype is not dtype or t.shape != (n, heads, d) or t.device != device:
+        _refuse(name, t, (n, heads, d), dtype, device)
     ts, hs, cs = t.stride()
     if cs != 1:
         raise _bad(f"the channels of {name} must be contiguous")
@@ -539,17 +541,17 @@ def _rows(name: str, t: torch.Tensor, n: int, heads: int, d: int, dtype, device)
 
 def _words(name: str, t: torch.Tensor, shape, dtype, device):
     """Pointer of a contiguous index or statistics array."""
-    if not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        _refuse(name, t, shape, dtype, device)
+    if not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
-        raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} {tuple(shape)} on {device}")
     return t.data_ptr()
 
 
-def _on(stream, *tensors):
+def _on(stream, device, *tensors):
     """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
     if stream is None:
-        return torch.cuda.current_stream(tensors[0].device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(device.index)
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -582,10 +584,11 @@ class PromptAttention:
         n = C.c_size_t()
         _raise(lib().gracekv_prompt_workspace_size(C.byref(self.desc), C.byref(n)))
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=device)
+        self._ref, self._device, self._ws = C.byref(self.desc), self.workspace.device, self.workspace.data_ptr()
 
     def __call__(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, return_lse=False, stream=None):
         """out [N, Hq, d] of q's dtype (or (out, lse [N, Hq] fp32) with return_lse)."""
-        p, dev = self.desc, self.workspace.device
+        p, dev = self.desc, self._device
         cu_k = cu_q if cu_k is None else cu_k
         n_q, n_k = q.shape[0], k.shape[0]
         if out is None:
@@ -600,12 +603,12 @@ class PromptAttention:
         p.v, p.v_ts, p.v_hs = _rows("v", v, n_k, self.G, self.d, self.dtype, dev)
         p.out, p.o_ts, p.o_hs = _rows("out", out, n_q, self.Hq, self.d, self.dtype, dev)
         p.lse = None if lse is None else _words("lse", lse, (n_q, self.Hq), torch.float32, dev)
-        _raise(lib().gracekv_prompt_attention(C.byref(p), self.workspace.data_ptr(),
-                                              _on(stream, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
+        _raise(lib().gracekv_prompt_attention(self._ref, self._ws,
+                                              _on(stream, dev, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
         return (out, lse) if return_lse else out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_prompt_status(self.workspace.data_ptr(), _on(stream, self.workspace)))
+        _raise(lib().gracekv_prompt_status(self.workspace.data_ptr(), _on(stream, self.workspace.device, self.workspace)))
 
 
 class PagedCache:
@@ -638,6 +641,7 @@ class PagedCache:
         n = C.c_size_t()
         _raise(lib().gracekv_paged_workspace_size(C.byref(self.desc), C.byref(n)))
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)
+        self._ref, self._device, self._ws = C.byref(self.desc), dev, self.workspace.data_ptr()
         self._free = None
 
     @staticmethod
@@ -686,13 +690,13 @@ class PagedCache:
     def load_packed(self, b: int, K, V, log_m, offsets, stream=None):
         """The packed cache K, V [E, d], log_m [E] or None, offsets [L G + 1] int64
         becomes request b's entries (the table already holds their pages)."""
-        dev, E = self.K.device, K.shape[0]
+        dev, E = self._device, K.shape[0]
         _raise(lib().gracekv_paged_load(
-            C.byref(self.desc), b, _words("K", K, (E, self.d), self.dtype, dev),
+            self._ref, b, _words("K", K, (E, self.d), self.dtype, dev),
             _words("V", V, (E, self.d), self.dtype, dev),
             None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
-            _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self.workspace.data_ptr(),
-            _on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens, self.workspace)))
+            _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self._ws,
+            _on(stream, dev, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens, self.workspace)))
 
     def load(self, b: int, cache: Cache, n_entries: int, stream=None):
         """A compressed cache (Compressor's output) as request b, replacing what the
@@ -734,7 +738,7 @@ class PagedCache:
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
         p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
-        _raise(lib().gracekv_paged_advance(C.byref(self.desc), p, _on(stream, self.lens, cu_new)))
+        _raise(lib().gracekv_paged_advance(self._ref, p, _on(stream, self.K.device, self.lens, cu_new)))
 
     def release(self, b: int, stream=None):
         """Request b's pages return to the pool; the slot is idle."""
@@ -756,32 +760,32 @@ class PagedCache:
     def append(self, l: int, k, v, pos, q=None, cu_new=None, out=None, stream=None):
         """Layer l's new tokens: k, v [N, G, d] into the pages (k rotated to pos [N]
         int32); returns q [N, Hq, d] rotated (into `out`, which may be q), or None."""
-        dev, N = self.K.device, k.shape[0]
+        dev, N = self._device, k.shape[0]
         if q is not None and out is None:
             out = _empty_like_on(stream, (N, self.Hq, self.d), self.dtype, dev)
         none = (None, 0, 0)
         _raise(lib().gracekv_paged_append(
-            C.byref(self.desc), l, N,
+            self._ref, l, N,
             None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
             _words("pos", pos, (N,), torch.int32, dev), *_rows("k", k, N, self.G, self.d, self.dtype, dev),
             *_rows("v", v, N, self.G, self.d, self.dtype, dev),
             *(none if q is None else _rows("q", q, N, self.Hq, self.d, self.dtype, dev)),
             *(none if q is None else _rows("out", out, N, self.Hq, self.d, self.dtype, dev)),
-            self.workspace.data_ptr(), _on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
+            self._ws, _on(stream, dev, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
                                            self.lens, self.workspace)))
         return out
 
     def attention(self, l: int, q, out=None, stream=None):
         """q [B, Hq, d], one rotated query per request slot -> out [B, Hq, d] of the
         cache's dtype over layer l (zeros for an idle slot)."""
-        dev, shape = self.K.device, (self.B, self.Hq, self.d)
+        dev, shape = self._device, (self.B, self.Hq, self.d)
         if out is None:
             out = _empty_like_on(stream, shape, self.dtype, dev)
         _raise(lib().gracekv_paged_attention(
-            C.byref(self.desc), l, _words("q", q, shape, self.dtype, dev), _words("out", out, shape, self.dtype, dev),
-            self.workspace.data_ptr(), _on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens,
+            self._ref, l, _words("q", q, shape, self.dtype, dev), _words("out", out, shape, self.dtype, dev),
+            self._ws, _on(stream, dev, q, out, self.K, self.V, self.log_m, self.table, self.lens,
                                            self.workspace)))
         return out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_paged_status(self.workspace.data_ptr(), _on(stream, self.workspace)))
+        _raise(lib().gracekv_paged_status(self.workspace.data_ptr(), _on(stream, self.workspace.device, self.workspace)))
