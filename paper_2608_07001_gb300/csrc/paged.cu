@@ -46,7 +46,7 @@ const Turns &turns_of(double base, int d) {
     return t;
 }
 
-constexpr int64_t kAppendMany = 1 << 19;      // row chunks from which a thread takes 8 rows
+constexpr int64_t kAppendMany = 1 << 19;      // row chunks from which a thread takes 4 rows
 
 struct AppendArgs {
     Paged c;
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
             sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
         }
     }
-    constexpr int U = R < 4 ? R : 4;          // rows in flight
+    constexpr int U = R < 2 ? R : 2;          // rows in flight
 #pragma unroll 1
     for (int k0 = 0; k0 < R; k0 += U) {
         uint4 x[U], y[U];
@@ -148,16 +148,18 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
 }
 
 // R: rows of a thread.  Few tokens want every row on its own thread, the
-// latency of one row; many want a thread's sines to serve several.
+// latency of one row; many want a thread's sines to serve several (32768 tokens
+// of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread: 201 / 158 /
+// 137 / 144 us with two in flight, 5.9 TB/s at best).
 template <typename T, int D>
 void launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
     constexpr int CH = D * (int)sizeof(T) / 32;
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
     const int64_t one = (int64_t)a.n_tokens * rows * CH;
     const bool many = one >= kAppendMany;
-    const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 7) / 8) * CH : one;
+    const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 3) / 4) * CH : one;
     const unsigned n = (unsigned)((threads + 255) / 256);
-    if (many) paged_append_kernel<T, D, 8><<<n, 256, 0, s>>>(a, turns);
+    if (many) paged_append_kernel<T, D, 4><<<n, 256, 0, s>>>(a, turns);
     else paged_append_kernel<T, D, 1><<<n, 256, 0, s>>>(a, turns);
 }
 
@@ -237,6 +239,7 @@ __global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
 
 template <int RB>
 void launch_load(const LoadArgs &a, cudaStream_t s) {
+    // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes (6.5 TB/s); one 187, four 200
     constexpr int IT = 2;
     constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
     const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);

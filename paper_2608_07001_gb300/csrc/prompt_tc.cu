@@ -352,60 +352,85 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::mbar_wait(tc::smem_u32(&b.qfull), 0, kWaitNs);
             }
         } else if (warp == kWarpMma) {
-            // ---------------- MMA issue ----------------
-            if (lane == 0 && n > 0) {
+            // ---------------- MMA issue: the warp runs as one, one lane issues ----------------
+            if (n > 0) {
                 constexpr uint32_t idS = tc::idesc_bf16_f32(128, kN), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
-                const uint32_t qa = tc::smem_u32(Qs), ra = tc::smem_u32(ring);
-                int committed = 0;                           // commits to b.odone[0], b.odone[1] are the last ones
-                bool ok = wait(&b.qfull, 0, b, a.status);
-                auto qk = [&](int i, int j) {                // S_i = Q_i K_j^T
-                    const uint32_t ks = ra + (uint32_t)((2 * j) % C::NST) * C::TILE;
-    #pragma unroll
+                // descriptors: the start address (16-byte units) is the low word's low end, the rest is constant
+                const uint32_t qd = (tc::smem_u32(Qs) >> 4) | (1u << 16), kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
+                const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((128 * 128 >> 4) << 16);
+                const bool one = tc::elect_one();
+                int st = 0;
+                uint32_t ph = 0;                         // of the ring slot that comes next
+                bool issued = false;
+                bool ok = wait(&b.qfull, 0, b, a.status) && wait(&b.full[0], 0, b, a.status);
+                auto qk = [&](int i, int slot) {         // S_i = Q_i K^T, K in the slot
+                    const uint32_t qa = qd + i * (C::TILE >> 4), ka = kd + slot * (C::TILE >> 4);
+#pragma unroll
                     for (int c = 0; c < C::NB; c++)
-    #pragma unroll
+#pragma unroll
                         for (int x = 0; x < 4; x++)
-                            tc::mma_bf16(tb + i * kN, tc::sdesc_sw128(qa + i * C::TILE + c * 128 * 128 + 32 * x),
-                                         tc::sdesc_sw128(ks + c * 128 * 128 + 32 * x), idS, (c | x) != 0);
+                            tc::mma_bf16_lo(tb + i * kN, qa + c * (128 * 128 >> 4) + 2 * x, ka + c * (128 * 128 >> 4) + 2 * x,
+                                            idS, (c | x) != 0);
                     tc::mma_commit(tc::smem_u32(&b.sfull[i]));
                 };
-                if (ok) ok = wait(&b.full[0], 0, b, a.status);
+                ok = __all_sync(0xffffffffu, ok);
                 if (ok) {
                     tc::tc_fence_after();
-                    for (int i = 0; i < ntile; i++)
-                        if ((i ? nkv1 : nkv0) > 0) qk(i, 0);
-                    tc::mma_commit(tc::smem_u32(&b.empty[0]));
-                    committed = 1;
+                    if (one) {
+                        if (nkv0 > 0) qk(0, 0);
+                        if (nkv1 > 0) qk(1, 0);
+                        tc::mma_commit(tc::smem_u32(&b.empty[0]));
+                    }
+                    issued = true;
+                    st = 1;
                 }
                 for (int j = 0; ok && j < n; j++) {
-                    const int vi = 2 * j + 1, ki = 2 * j + 2;
-                    ok = wait(&b.full[vi % C::NST], (vi / C::NST) & 1, b, a.status);
-                    if (ok && fix && j == n - 1) ok = wait(&b.vfix, 0, b, a.status);
-                    if (ok && j + 1 < n) ok = wait(&b.full[ki % C::NST], (ki / C::NST) & 1, b, a.status);
-                    const uint32_t vs = ra + (uint32_t)(vi % C::NST) * C::TILE;
-                    for (int i = 0; ok && i < ntile; i++) {
+                    const int vs = st;
+                    const uint32_t vph = ph;
+                    if (++st == C::NST) { st = 0; ph ^= 1; }
+                    const int ks = st;
+                    const uint32_t kph = ph;
+                    const bool more = j + 1 < n;
+                    ok = wait(&b.full[vs], vph, b, a.status);
+                    if (fix && !more) ok = ok && wait(&b.vfix, 0, b, a.status);
+                    if (more) {
+                        ok = ok && wait(&b.full[ks], kph, b, a.status);
+                        if (++st == C::NST) { st = 0; ph ^= 1; }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
                         const int ni = i ? nkv1 : nkv0;
                         if (j >= ni) continue;
-                        ok = wait(&b.pfull[i], j & 1, b, a.status);
+                        ok = ok && wait(&b.pfull[i], j & 1, b, a.status);
+                        ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc::tc_fence_after();
-    #pragma unroll
-                        for (int x = 0; x < kN / 16; x++)
-                            tc::mma_bf16_ts(tb + 2 * kN + i * D, tb + i * kN + x * 8,
-                                            tc::sdesc_sw128_mn(vs + x * 16 * 128, 128 * 128), idO, (j | x) != 0);
-                        if (j == ni - 1) tc::mma_commit(tc::smem_u32(&b.odone[i]));
-                        else qk(i, j + 1);
+                        if (one) {
+                            const uint32_t va = vd + vs * (C::TILE >> 4);
+#pragma unroll
+                            for (int x = 0; x < kN / 16; x++)
+                                tc::mma_bf16_ts_lo(tb + 2 * kN + i * D, tb + i * kN + x * 8, va + x * (16 * 128 >> 4), idO,
+                                                   (j | x) != 0);
+                            if (j == ni - 1) tc::mma_commit(tc::smem_u32(&b.odone[i]));
+                            else qk(i, ks);
+                        }
+                        __syncwarp();
                     }
-                    if (!ok) break;
-                    tc::mma_commit(tc::smem_u32(&b.empty[vi % C::NST]));
-                    if (j + 1 < n) tc::mma_commit(tc::smem_u32(&b.empty[ki % C::NST]));
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (ok && one) {
+                        tc::mma_commit(tc::smem_u32(&b.empty[vs]));
+                        if (more) tc::mma_commit(tc::smem_u32(&b.empty[ks]));
+                    }
+                    __syncwarp();
                 }
-                if (!ok) {
+                if (!ok && lane == 0) {
                     atomicOr(a.status, kStTimeout);
                     atomicExch(&b.abort, 1);
                 }
                 // every operation issued is done before TMEM is freed: one more commit covers them
-                if (committed) {
-                    tc::mma_commit(tc::smem_u32(&b.fin));
+                if (issued) {
+                    if (one) tc::mma_commit(tc::smem_u32(&b.fin));
+                    __syncwarp();
                     tc::mbar_wait(tc::smem_u32(&b.fin), 0, kWaitNs);
                 }
             }

@@ -129,15 +129,9 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
 
 // B with its N index contiguous in shared memory ("MN-major"): rows of 64
 // elements (128 bytes, 128-byte swizzle) are K steps, 8-row groups 1024 bytes
-// apart, blocks of 64 N elements `lbo` bytes apart; the instruction descriptor
-// carries the transpose bit of B.
-__device__ __forceinline__ uint64_t sdesc_sw128_mn(uint32_t addr, uint32_t lbo) {
-    return (uint64_t)((addr >> 4) & 0x3FFFu)
-           | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16)
-           | ((uint64_t)(1024 >> 4) << 32)
-           | ((uint64_t)1 << 46)
-           | ((uint64_t)2 << 61);
-}
+// apart, blocks of 64 N elements the leading-dimension offset (bits 16..29 of
+// the low word, in 16 bytes) apart; the instruction descriptor carries the
+// transpose bit of B.
 constexpr uint32_t kIdescBmn = 1u << 16;
 
 // ---- MMA -------------------------------------------------------------------
@@ -151,15 +145,35 @@ __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t adesc, uint64
         "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// The same with A in TMEM: 128 lanes of packed bf16 pairs, 8 columns a K step.
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
+// The same for descriptors of which only the low word varies, and with A in
+// TMEM (128 lanes of packed bf16 pairs, 8 columns a K step): the high
+// word is that of a 128-byte-swizzled operand with 1024 bytes between its
+// 8-row groups (stride-dimension offset, version of the sm_100 family, swizzle).
+constexpr uint32_t kSdescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void mma_bf16_lo(uint32_t d_tmem, uint32_t alo, uint32_t blo, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 da, {%1, %4};\n\tmov.b64 db, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(alo), "r"(blo), "r"(idesc), "r"(kSdescHi), "r"(accumulate)
         : "memory");
+}
+__device__ __forceinline__ void mma_bf16_ts_lo(uint32_t d_tmem, uint32_t a_tmem, uint32_t blo, uint32_t idesc,
+                                               uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 db, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(blo), "r"(idesc), "r"(kSdescHi), "r"(accumulate)
+        : "memory");
+}
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 // Arrive once on `bar` when every tcgen05 operation this thread issued before
 // has completed.
