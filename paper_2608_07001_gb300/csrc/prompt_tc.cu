@@ -17,7 +17,8 @@
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread a row, its 128 scores
 // in registers), 8 TMA (Q once, then K and V tiles of 128 keys through a ring),
-// 9 MMA issue (10, 11 idle: registers are split by warpgroup).  TMEM: S0, S1 (128 columns each; P overlays the lower half of
+// 9 and 10 MMA issue of tile 0 and 1 (11 idle: registers are split by
+// warpgroup).  TMEM: S0, S1 (128 columns each; P overlays the lower half of
 // its S as packed bf16), O0, O1.  P is the A operand of its product from TMEM;
 // V is the B operand as it lies in memory (rows of channels, "MN-major").
 // tcgen05 operations of one thread complete in order, so the commit of S(j + 1)
@@ -46,7 +47,7 @@ constexpr int kThreads = 384;                  // three warpgroups: two of softm
 // Registers a thread after the split; 256 x 208 + 128 x 88 = 384 x 168, the launch's own.
 constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
 static_assert(256 * kRegsSoftmax + 128 * kRegsIssue <= kThreads * kRegs, "register split");
-constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr int kWarpTma = 8, kWarpMma = 9;      // MMA: warps 9 and 10, one a row tile
 constexpr float kLazy = 8.f;                   // log2 of the growth a reference lets pass
 constexpr uint64_t kWaitNs = 2000000000ull;
 
@@ -59,7 +60,7 @@ struct Cfg {
 };
 
 struct Bars {
-    uint64_t full[8], empty[8], qfull, sfull[2], pfull[2], odone[2], vfix, fin;
+    uint64_t full[8], empty[8], qfull, sfull[2], pfull[2][2], odone[2], vfix, fin;
     uint32_t tbase;
     int abort;
 };
@@ -89,6 +90,12 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars &b, in
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
 
@@ -129,14 +136,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::NST; i++) {
             tc::mbar_init(tc::smem_u32(&b.full[i]), 1);
-            tc::mbar_init(tc::smem_u32(&b.empty[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.empty[i]), 2);
         }
         tc::mbar_init(tc::smem_u32(&b.qfull), 1);
         tc::mbar_init(tc::smem_u32(&b.vfix), 1);
-        tc::mbar_init(tc::smem_u32(&b.fin), 1);
+        tc::mbar_init(tc::smem_u32(&b.fin), 2);
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(tc::smem_u32(&b.sfull[i]), 1);
-            tc::mbar_init(tc::smem_u32(&b.pfull[i]), 4);
+            for (int k = 0; k < 2; k++) tc::mbar_init(tc::smem_u32(&b.pfull[i][k]), 4);
             tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
         }
         b.abort = 0;
@@ -188,12 +195,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int e = 0; e < 32; e++)
                         if (k * 32 + e > rel) x[k][e] = 0xff800000u;       // -inf
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float mx[4];
 #pragma unroll
-            for (int k = 0; k < 4; k++)
+            for (int k = 0; k < 4; k++) {
+                mx[k] = fmaxf(__uint_as_float(x[k][0]), __uint_as_float(x[k][1]));
 #pragma unroll
-                for (int e = 0; e < 32; e += 2)
-                    mx[k] = fmaxf(mx[k], fmaxf(__uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1])));
+                for (int e = 2; e < 32; e += 2)
+                    mx[k] = max3(mx[k], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+            }
             const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
             if (m == -INFINITY) m = mn;                  // nothing accumulated yet
             else if (__builtin_expect(mn > m + kLazy, 0)) z = -z;          // asks for a rescale (z > 0 marks none)
@@ -229,12 +238,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     p[e] = pack2(w.x, w.y);
                 }
                 tc::tmem_st32(ts + 32 * k, p);
+                tc::tmem_wait_st();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][k]));
             }
             z += acc.x + acc.y;
-            tc::tmem_wait_st();
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i]));
         }
         if (ok && nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status));
         tc::tc_fence_after();
@@ -351,39 +360,37 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc::mbar_wait(tc::smem_u32(&b.full[i % C::NST]), (i / C::NST) & 1, kWaitNs);
                 tc::mbar_wait(tc::smem_u32(&b.qfull), 0, kWaitNs);
             }
-        } else if (warp == kWarpMma) {
-            // ---------------- MMA issue: the warp runs as one, one lane issues ----------------
+        } else if (warp <= kWarpMma + 1) {
+            // ---------------- MMA issue: one warp a row tile, one lane issues ----------------
             if (n > 0) {
                 constexpr uint32_t idS = tc::idesc_bf16_f32(128, kN), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
+                const int i = warp - kWarpMma, ni = i ? nkv1 : nkv0;
                 // descriptors: the start address (16-byte units) is the low word's low end, the rest is constant
-                const uint32_t qd = (tc::smem_u32(Qs) >> 4) | (1u << 16), kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
+                const uint32_t qd = ((tc::smem_u32(Qs) >> 4) | (1u << 16)) + i * (C::TILE >> 4);
+                const uint32_t kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
                 const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((128 * 128 >> 4) << 16);
+                const uint32_t ts = tb + i * kN, to = tb + 2 * kN + i * D;
                 const bool one = tc::elect_one();
-                int st = 0;
+                int st = 1;
                 uint32_t ph = 0;                         // of the ring slot that comes next
-                bool issued = false;
                 bool ok = wait(&b.qfull, 0, b, a.status) && wait(&b.full[0], 0, b, a.status);
-                auto qk = [&](int i, int slot) {         // S_i = Q_i K^T, K in the slot
-                    const uint32_t qa = qd + i * (C::TILE >> 4), ka = kd + slot * (C::TILE >> 4);
+                auto qk = [&](int slot) {                // S = Q K^T, K in the slot
+                    const uint32_t ka = kd + slot * (C::TILE >> 4);
 #pragma unroll
                     for (int c = 0; c < C::NB; c++)
 #pragma unroll
                         for (int x = 0; x < 4; x++)
-                            tc::mma_bf16_lo(tb + i * kN, qa + c * (128 * 128 >> 4) + 2 * x, ka + c * (128 * 128 >> 4) + 2 * x,
-                                            idS, (c | x) != 0);
+                            tc::mma_bf16_lo(ts, qd + c * (128 * 128 >> 4) + 2 * x, ka + c * (128 * 128 >> 4) + 2 * x, idS,
+                                            (c | x) != 0);
                     tc::mma_commit(tc::smem_u32(&b.sfull[i]));
                 };
-                ok = __all_sync(0xffffffffu, ok);
-                if (ok) {
-                    tc::tc_fence_after();
-                    if (one) {
-                        if (nkv0 > 0) qk(0, 0);
-                        if (nkv1 > 0) qk(1, 0);
-                        tc::mma_commit(tc::smem_u32(&b.empty[0]));
-                    }
-                    issued = true;
-                    st = 1;
+                tc::tc_fence_after();
+                if (ok && one) {
+                    if (ni > 0) qk(0);
+                    tc::mma_commit(tc::smem_u32(&b.empty[0]));
                 }
+                ok = __all_sync(0xffffffffu, ok);
+                // the row tiles may end at different key tiles: both warps release every slot, in order
                 for (int j = 0; ok && j < n; j++) {
                     const int vs = st;
                     const uint32_t vph = ph;
@@ -392,47 +399,43 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint32_t kph = ph;
                     const bool more = j + 1 < n;
                     ok = wait(&b.full[vs], vph, b, a.status);
-                    if (fix && !more) ok = ok && wait(&b.vfix, 0, b, a.status);
                     if (more) {
                         ok = ok && wait(&b.full[ks], kph, b, a.status);
                         if (++st == C::NST) { st = 0; ph ^= 1; }
+                    } else if (fix) {
+                        ok = ok && wait(&b.vfix, 0, b, a.status);
                     }
+                    if (j < ni) {
+                        const uint32_t va = vd + vs * (C::TILE >> 4);
 #pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const int ni = i ? nkv1 : nkv0;
-                        if (j >= ni) continue;
-                        ok = ok && wait(&b.pfull[i], j & 1, b, a.status);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (!ok) break;
-                        tc::tc_fence_after();
-                        if (one) {
-                            const uint32_t va = vd + vs * (C::TILE >> 4);
+                        for (int k = 0; k < 2; k++) {            // the weights come in two halves
+                            ok = ok && wait(&b.pfull[i][k], j & 1, b, a.status);
+                            tc::tc_fence_after();
+                            if (ok && one) {
 #pragma unroll
-                            for (int x = 0; x < kN / 16; x++)
-                                tc::mma_bf16_ts_lo(tb + 2 * kN + i * D, tb + i * kN + x * 8, va + x * (16 * 128 >> 4), idO,
-                                                   (j | x) != 0);
-                            if (j == ni - 1) tc::mma_commit(tc::smem_u32(&b.odone[i]));
-                            else qk(i, ks);
+                                for (int x = k * (kN / 32); x < (k + 1) * (kN / 32); x++)
+                                    tc::mma_bf16_ts_lo(to, ts + x * 8, va + x * (16 * 128 >> 4), idO, (j | x) != 0);
+                            }
                         }
-                        __syncwarp();
+                        if (ok && one) {
+                            if (j + 1 < ni) qk(ks);
+                            else tc::mma_commit(tc::smem_u32(&b.odone[i]));
+                        }
                     }
-                    ok = __all_sync(0xffffffffu, ok);
                     if (ok && one) {
                         tc::mma_commit(tc::smem_u32(&b.empty[vs]));
                         if (more) tc::mma_commit(tc::smem_u32(&b.empty[ks]));
                     }
-                    __syncwarp();
+                    ok = __all_sync(0xffffffffu, ok);
                 }
                 if (!ok && lane == 0) {
                     atomicOr(a.status, kStTimeout);
                     atomicExch(&b.abort, 1);
                 }
-                // every operation issued is done before TMEM is freed: one more commit covers them
-                if (issued) {
-                    if (one) tc::mma_commit(tc::smem_u32(&b.fin));
-                    __syncwarp();
-                    tc::mbar_wait(tc::smem_u32(&b.fin), 0, kWaitNs);
-                }
+                // every operation issued is done before TMEM is freed: one more commit of each covers them
+                if (one) tc::mma_commit(tc::smem_u32(&b.fin));
+                __syncwarp();
+                tc::mbar_wait(tc::smem_u32(&b.fin), 0, kWaitNs);
             }
         }
     }
