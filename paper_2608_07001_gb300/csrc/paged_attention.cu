@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                         }
                     }
                     const float r = Z > 0.f ? 1.f / Z : 0.f;
-                    put(out + i, v.x * r); put(out + i + 1, v.y * r); put(out + i + 2, v.z * r); put(out + i + 3, v.w * r);
+                    put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
                 }
                 if (tid == 0) a.cnt[c_lo] = 0;
             }

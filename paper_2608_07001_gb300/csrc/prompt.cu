@@ -20,15 +20,16 @@ namespace {
 
 using namespace serve;
 
-// One thread: four channels of a row, over the block's parts in order, eight
-// loads in flight.  TC: a warp takes 32 rows of one channel group, as the parts
-// lie; else neighbouring groups of a row.
+// Joins 32 rows of a split block, over its parts in order with eight loads in
+// flight.  A thread sums four channels: the tcgen05 kernel's parts are read
+// across rows as they lie and turned in shared memory, so that rows leave whole.
 template <typename T, int D, bool TC>
 __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
-    constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? kKeysTc : kKeysF32;
+    constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? kKeysTc : kKeysF32, LEAST = TC ? kLeastTc : kLeastF32;
+    constexpr int C4 = D / 4, LD = C4 + 1;
     constexpr size_t PF = part_floats(ROWS, D);
-    const int i = blockIdx.y * 256 + threadIdx.x;
-    const int r = TC ? i % ROWS : i / (D / 4), c = TC ? i / ROWS : i % (D / 4);
+    __shared__ float4 out_s[32 * LD];
+    __shared__ float m_s[32], z_s[32];
     const int gq = a.Hq / a.G, half = TC ? kRowsTc / 2 : kRowsF32, tpt = half / gq, tok = TC ? 2 * tpt : tpt;
     const int g = blockIdx.x % a.G;
     const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
@@ -38,53 +39,60 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
     const int64_t t0 = (slot - (q0 / tok + s)) * tok;
     if (t0 < 0 || t0 >= nq) return;
     const int last = (int)((nq < t0 + tok ? nq : t0 + tok) - 1 + nk - nq);
-    const int np = parts_of(last >= 0 ? last / KEYS + 1 : 0, a.split);
-    const int tk = r % half / gq;
-    const int64_t t = t0 + r / half * tpt + tk;
-    if (np == 1 || tk >= tpt || t >= nq) return;
+    const int np = parts_of(last >= 0 ? last / KEYS + 1 : 0, a.split, LEAST);
+    if (np == 1) return;
+    const int r0 = blockIdx.y * 32;
     const float *p0 = a.part + (size_t)blockIdx.x * a.split * PF;
-    const size_t at = TC ? (size_t)c * ROWS + r : (size_t)r * (D / 4) + c;
-    float M = -INFINITY, Z = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int b = 0; b < np; b += 8) {
-        float m[8], z[8], mx = M;
-        float4 x[8];
+#pragma unroll 1
+    for (int i = threadIdx.x; i < 32 * C4; i += 256) {
+        const int rr = TC ? i % 32 : i / C4, c = TC ? i / 32 : i % C4, r = r0 + rr;
+        const size_t at = TC ? (size_t)c * ROWS + r : (size_t)r * C4 + c;
+        if (r % half / gq >= tpt || t0 + r / half * tpt + r % half / gq >= nq) continue;
+        float M = -INFINITY, Z = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int b = 0; b < np; b += 8) {
+            float m[8], z[8], mx = M;
+            float4 x[8];
 #pragma unroll
-        for (int p = 0; p < 8; p++) {
-            const float *q = p0 + (size_t)(b + p) * PF;
-            const bool on = b + p < np;
-            m[p] = on ? q[ROWS * D + r] : -INFINITY;
-            z[p] = on ? q[ROWS * D + ROWS + r] : 0.f;
-            x[p] = on ? reinterpret_cast<const float4 *>(q)[at] : make_float4(0.f, 0.f, 0.f, 0.f);
-            mx = fmaxf(mx, m[p]);
-        }
-        const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
-        M = mx;
-        Z *= w;
-        v.x *= w; v.y *= w; v.z *= w; v.w *= w;
+            for (int p = 0; p < 8; p++) {
+                const float *q = p0 + (size_t)(b + p) * PF;
+                const bool on = b + p < np;
+                m[p] = on ? q[ROWS * D + r] : -INFINITY;
+                z[p] = on ? q[ROWS * D + ROWS + r] : 0.f;
+                x[p] = on ? reinterpret_cast<const float4 *>(q)[at] : make_float4(0.f, 0.f, 0.f, 0.f);
+                mx = fmaxf(mx, m[p]);
+            }
+            const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
+            M = mx;
+            Z *= w;
+            v.x *= w; v.y *= w; v.z *= w; v.w *= w;
 #pragma unroll
-        for (int p = 0; p < 8; p++) {
-            const float f = tc::ex2(m[p] - sh);
-            Z += f * z[p];
-            v.x += f * x[p].x; v.y += f * x[p].y; v.z += f * x[p].z; v.w += f * x[p].w;
+            for (int p = 0; p < 8; p++) {
+                const float f = tc::ex2(m[p] - sh);
+                Z += f * z[p];
+                v.x += f * x[p].x; v.y += f * x[p].y; v.z += f * x[p].z; v.w += f * x[p].w;
+            }
         }
+        const float inv = Z > 0.f ? 1.f / Z : Z;          // a row that sees no key: 0; a NaN stays
+        out_s[rr * LD + c] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        if (c == 0) { m_s[rr] = M; z_s[rr] = Z; }
     }
-    // a row that sees no key: 0; a NaN stays
-    const float inv = Z > 0.f ? 1.f / Z : Z;
-    const int h = g * gq + r % half % gq;
-    T *o = static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + c * 4;
-    put(o, v.x * inv);
-    put(o + 1, v.y * inv);
-    put(o + 2, v.z * inv);
-    put(o + 3, v.w * inv);
-    if (c == 0 && a.lse) a.lse[(q0 + t) * a.Hq + h] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.6931471805599453f;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * C4; i += 256) {
+        const int rr = i / C4, c = i % C4, r = r0 + rr, tk = r % half / gq, h = g * gq + r % half % gq;
+        const int64_t t = t0 + r / half * tpt + tk;
+        if (tk >= tpt || t >= nq) continue;
+        put4(static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + c * 4, out_s[rr * LD + c]);
+        if (c == 0 && a.lse)
+            a.lse[(q0 + t) * a.Hq + h] = z_s[rr] == 0.f ? -INFINITY : (m_s[rr] + log2f(z_s[rr])) * 0.6931471805599453f;
+    }
 }
 
 template <typename T, bool TC>
 cudaError_t join(const PromptArgs &a, int d, cudaStream_t s) {
     constexpr int ROWS = TC ? kRowsTc : kRowsF32;
     const int gq = a.Hq / a.G, tok = TC ? 2 * (kRowsTc / 2 / gq) : kRowsF32 / gq;
-    const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS * (d / 4) / 256);
+    const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS / 32);
     if (d == 128) prompt_join_kernel<T, 128, TC><<<grid, 256, 0, s>>>(a);
     else prompt_join_kernel<T, 64, TC><<<grid, 256, 0, s>>>(a);
     return cudaGetLastError();

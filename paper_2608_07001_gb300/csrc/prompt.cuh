@@ -59,8 +59,14 @@ __device__ __forceinline__ void check_bounds(const PromptArgs &a) {
     }
 }
 
+// Key tiles of a part at least: what joining costs (about 4 us) against a tile
+// (about 1 us on tcgen05, 6 us on CUDA cores).
+constexpr int kLeastTc = 4, kLeastF32 = 1;
 // Parts of a block of n key tiles when a launch splits blocks `split` ways.
-__host__ __device__ __forceinline__ int parts_of(int n, int split) { return n < 1 ? 1 : n < split ? n : split; }
+__host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
+    const int most = n / least;
+    return most < 1 ? 1 : most < split ? most : split;
+}
 // Floats of a part: 4-channel groups of the sums (by row or by group), then the
 // rows' maxima (base 2) and weight sums.
 __host__ __device__ constexpr size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64, off = nk - nq;
     const int last = min(nq, t0 + tok) - 1 + off;
     const int n = last >= 0 ? last / kK + 1 : 0;
-    const int np = parts_of(n, a.split);
+    const int np = parts_of(n, a.split, kLeastF32);
     if ((int)blockIdx.y >= np) return;
     const int j0 = (int)((int64_t)blockIdx.y * n / np), j1 = (int)((int64_t)(blockIdx.y + 1) * n / np);
 
@@ -212,12 +212,9 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         const float inv = z[i] > 0.f ? 1.f / z[i] : z[i];        // no key: 0; a NaN stays
         T *p = static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + tx * 4;
 #pragma unroll
-        for (int c = 0; c < D / 64; c++) {
-            put(p + c * 64, o[i][2 * c].x * inv);
-            put(p + c * 64 + 1, o[i][2 * c].y * inv);
-            put(p + c * 64 + 2, o[i][2 * c + 1].x * inv);
-            put(p + c * 64 + 3, o[i][2 * c + 1].y * inv);
-        }
+        for (int c = 0; c < D / 64; c++)
+            put4(p + c * 64, make_float4(o[i][2 * c].x * inv, o[i][2 * c].y * inv, o[i][2 * c + 1].x * inv,
+                                         o[i][2 * c + 1].y * inv));
         if (tx == 0 && a.lse)
             a.lse[(q0 + t) * a.Hq + h] = z[i] == 0.f ? -INFINITY : (m[i] + log2f(z[i])) * 0.6931471805599453f;
     }

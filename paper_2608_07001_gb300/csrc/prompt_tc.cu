@@ -62,7 +62,7 @@ struct Cfg {
 struct Bars {
     uint64_t full[8], empty[8], qfull, sfull[2], pfull[2][2], odone[2], vfix, fin;
     uint32_t tbase;
-    int abort;
+    int abort, turn;           // turn: key tiles whose products row tile 0 has issued
 };
 
 struct Tc {
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // them this part's: [j0, j0 + n)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
     const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
-    const int all = max(all0, all1), np = parts_of(all, a.split);
+    const int all = max(all0, all1), np = parts_of(all, a.split, kLeastTc);
     if ((int)blockIdx.y >= np) return;
     const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
     const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
@@ -147,6 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
         }
         b.abort = 0;
+        b.turn = 0;
         tc::fence_barrier_init();
     }
     if (warp == kWarpMma) {
@@ -405,6 +406,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else if (fix) {
                         ok = ok && wait(&b.vfix, 0, b, a.status);
                     }
+                    // d = 128: tile 1 goes after tile 0.  Products of the two issued at once would run
+                    // interleaved, end together and leave the tensor pipe idle while both tiles are in
+                    // their softmax (1250 us in turn, 1370 without, at 16K tokens).  At d = 64 the softmax
+                    // is the longer side and a turn only delays it (173 us in turn, 149 without).  An
+                    // order, not a dependence: the wait may run out.
+                    if (D == 128 && i == 1)
+                        for (int w = 0; w < 20000 && *(volatile int *)&b.turn <= j; w++) {}
                     if (j < ni) {
                         const uint32_t va = vd + vs * (C::TILE >> 4);
 #pragma unroll
@@ -422,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             else tc::mma_commit(tc::smem_u32(&b.odone[i]));
                         }
                     }
+                    if (i == 0 && one) *(volatile int *)&b.turn = j + 1;
                     if (ok && one) {
                         tc::mma_commit(tc::smem_u32(&b.empty[vs]));
                         if (more) tc::mma_commit(tc::smem_u32(&b.empty[ks]));
@@ -495,7 +504,7 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
         ready[dev].store(1, std::memory_order_relaxed);
     }
     // fewer blocks than SMs: their keys are split over the others
-    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + kN - 1) / kN));
+    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + kN - 1) / kN / kLeastTc));
     prompt_tc_kernel<D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
     e = cudaGetLastError();
     return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, GKV_BF16, true, s) : e;

@@ -56,5 +56,14 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ void put(float *p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16(x); }
 
+// Four neighbouring elements, on their own 4 x size boundary.
+__device__ __forceinline__ void put4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
+__device__ __forceinline__ void put4(__nv_bfloat16 *p, float4 x) {
+    uint2 u;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u.x) : "f"(x.y), "f"(x.x));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u.y) : "f"(x.w), "f"(x.z));
+    *reinterpret_cast<uint2 *>(p) = u;
+}
+
 }  // namespace serve
 }  // namespace gkv
