@@ -536,7 +536,7 @@ typedef struct {
     float *log_m;                     /* [n_pages][page_size]; NULL: every entry has log m = 0 */
     const int32_t *table;             /* [L][B][G][max_pages] */
     int32_t *lens;                    /* [L][B][G] entries */
-    double rope_base;                 /* of gracekv_paged_append (0: no rotation) */
+    double rope_base;                 /* of gracekv_paged_append (at least 1; 0: no rotation) */
 } gkv_paged_cache;
 
 /* Bytes of the device workspace of the calls below for this geometry (L, B,
@@ -563,24 +563,31 @@ gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K
  * layers' appends.  Errors: GKV_EINVAL, GKV_ECUDA. */
 gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream);
 
-/* The new tokens of layer l: keys rotated to their positions and stored, values
- * stored, log m = 0 (App. A.5: appended tokens have multiplicity 1), queries
- * rotated into q_out.  Token t belongs to request b with cu_new[b] <= t <
- * cu_new[b + 1] (device [B + 1]; NULL: n_tokens = B, token t is request t's)
- * and becomes entry lens[l][b][g] - (cu_new[b + 1] - t): the lengths count the
- * new tokens already (gracekv_paged_advance).  A negative index (an idle
- * request) stores nothing.  Rotation of a vector x to position p: the pair
- * (x[i], x[i + d/2]) turns by p * rope_base^(-2 i / d), computed in fp32 from an
- * angle that is exact to 2^-26 turns at every int32 position, rounded once.
- *   pos [n_tokens] int32; k, v [n_tokens][G][d], q and q_out [n_tokens][Hq][d],
- *   token and head strides in elements as in gkv_prompt; q (with q_out) may be
- *   NULL.  q_out may be q itself.
- * Errors: GKV_EINVAL (n_tokens < 0, n_tokens != B without cu_new, pointers,
- * strides), GKV_ECUDA. */
-gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, int32_t n_tokens, const int32_t *cu_new,
-                                const int32_t *pos, const void *k, int64_t k_ts, int64_t k_hs, const void *v,
-                                int64_t v_ts, int64_t v_hs, const void *q, int64_t q_ts, int64_t q_hs, void *q_out,
-                                int64_t qo_ts, int64_t qo_hs, void *workspace, void *stream);
+/* The new tokens of one layer (device pointers; strides in elements, of tokens
+ * and heads, as in gkv_prompt): pos [n_tokens]; k, v [n_tokens][G][d]; q and
+ * q_out [n_tokens][Hq][d], both NULL without queries; q_out may be q itself.
+ * cu_new [B + 1]: token t belongs to request b with cu_new[b] <= t <
+ * cu_new[b + 1]; NULL: n_tokens = B and token t is request t's. */
+typedef struct {
+    int32_t n_tokens;
+    const int32_t *cu_new, *pos;
+    const void *k, *v, *q;
+    void *q_out;
+    int64_t k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, qo_ts, qo_hs;
+} gkv_paged_tokens;
+
+/* Layer l takes its new tokens: keys rotated to their positions and stored,
+ * values stored, log m = 0 (App. A.5: appended tokens have multiplicity 1),
+ * queries rotated into q_out.  Token t of request b becomes entry
+ * lens[l][b][g] - (cu_new[b + 1] - t): the lengths count the new tokens already
+ * (gracekv_paged_advance).  A negative index (an idle request) stores nothing.
+ * Rotation of a vector x to position p: the pair (x[i], x[i + d/2]) turns by
+ * p * rope_base^(-2 i / d), computed in fp32 from an angle that is exact to
+ * 2^-26 turns at every int32 position, rounded once.  Errors: GKV_EINVAL
+ * (n_tokens < 0, n_tokens != B without cu_new, pointers, strides, a rope_base
+ * neither 0 nor a finite number of at least 1), GKV_ECUDA. */
+gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t, void *workspace,
+                                void *stream);
 
 /* Attention of one token per request over layer l: q [B][Hq][d] (rotated; its
  * own entry appended), out [B][Hq][d] of the cache's dtype:

@@ -9,10 +9,15 @@
 // a sin phi + b cos phi).  p can be large while only phi mod 2 pi counts, so
 // the angle is kept in turns as a 64-bit fraction: F_i = 2^64 theta_i / (2 pi)
 // (host, fp64), and p F_i mod 2^64 is the fraction of a turn -- one integer
-// product, exact up to p times F_i's rounding (below 2^-21 of 2^-11 turns for
-// any int32 p) -- whose upper 32 bits go to sincospi.  A thread holds 16 bytes
-// of each half of a row, so the rotation stays in its registers; its sines and
-// cosines serve every head it takes.
+// product whose error is |p| times that of F_i, a few 2^-56 turns -- and its
+// upper 32 bits go to sincospi.  A thread holds 16 bytes of each half of a row,
+// so the rotation stays in its registers; its sines and cosines serve every
+// row that it takes.
+//
+// Both move 2 es d bytes a row (in and out) and are bound by HBM, or by the
+// latency of a launch for a few tokens: 137 us for 32768 tokens of 32 + 2 x 8
+// rows of 128 bf16 (805 MB, 5.9 TB/s), 3 us for one token; load 167 us for 1M
+// entries of 2 x 128 bf16 (1082 MB, 6.5 TB/s).
 #include "paged.cuh"
 
 #include <math.h>
@@ -24,8 +29,14 @@ namespace {
 
 using namespace serve;
 
+// F_i = a[i / 8] m[i % 8], m in 0.64 fixed point (m[0] is 1): 128 bytes of a
+// launch's arguments instead of 512, one high product a pair.
 struct Turns {
-    unsigned long long f[64];      // 2^64 theta_i / (2 pi)
+    unsigned long long a[8], m[8];
+    __device__ __forceinline__ unsigned long long at(int i) const {
+        const unsigned long long f = a[i >> 3];
+        return (i & 7) ? __umul64hi(f, m[i & 7]) : f;
+    }
 };
 
 // The table of a base, kept per host thread for the calls of a step (d / 2 fp64
@@ -35,10 +46,11 @@ const Turns &turns_of(double base, int d) {
     thread_local int have_d = 0;
     thread_local Turns t{};
     if (base > 0.0 && (base != have || d != have_d)) {
-        for (int i = 0; i < d / 2; i++) {
-            // theta / (2 pi) of a turn; whole turns (bases below 1) drop out
-            const double f = pow(base, -2.0 * i / d) / 6.283185307179586476925287;
-            t.f[i] = (unsigned long long)ldexp(f - floor(f), 64);
+        // turns of the pair at position 1: theta / (2 pi), at most 1 / (2 pi) as bases are at least 1
+        for (int i = 0; i < 8; i++) {
+            const double f = pow(base, -16.0 * i / d) / 6.283185307179586476925287, m = pow(base, -2.0 * i / d);
+            t.a[i] = (unsigned long long)ldexp(f, 64);
+            t.m[i] = i == 0 ? 0 : m < 1.0 ? (unsigned long long)ldexp(m, 64) : ~0ull;
         }
         have = base;
         have_d = d;
@@ -102,7 +114,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
         const long long p = a.pos[t];
 #pragma unroll
         for (int j = 0; j < N; j++) {
-            const int hi = (int)(((unsigned long long)p * turns.f[ch * N + j]) >> 32);
+            const int hi = (int)(((unsigned long long)p * turns.at(ch * N + j)) >> 32);
             sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
         }
     }
@@ -278,25 +290,26 @@ extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int3
     return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
-extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, int32_t n_tokens,
-                                           const int32_t *cu_new, const int32_t *pos, const void *k, int64_t k_ts,
-                                           int64_t k_hs, const void *v, int64_t v_ts, int64_t v_hs, const void *q,
-                                           int64_t q_ts, int64_t q_hs, void *q_out, int64_t qo_ts, int64_t qo_hs,
+extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t,
                                            void *workspace, void *stream) {
     const gkv_status st = check_paged(c);
     if (st != GKV_OK) return st;
-    if (l < 0 || l >= c->L || n_tokens < 0 || (!cu_new && n_tokens != c->B) || !al(cu_new, 4)) return GKV_EINVAL;
+    if (!t || l < 0 || l >= c->L || t->n_tokens < 0 || (!t->cu_new && t->n_tokens != c->B) || !al(t->cu_new, 4))
+        return GKV_EINVAL;
     if (!workspace || !al(workspace, 256)) return GKV_EINVAL;
+    if (c->rope_base != 0.0 && !(c->rope_base >= 1.0 && c->rope_base < HUGE_VAL)) return GKV_EINVAL;
+    const int n_tokens = t->n_tokens;
     if (n_tokens == 0) return GKV_OK;
-    if (!pos || !al(pos, 4) || !rows_ok(k, k_ts, k_hs, c->dtype) || !rows_ok(v, v_ts, v_hs, c->dtype)) return GKV_EINVAL;
-    if ((q != nullptr) != (q_out != nullptr)) return GKV_EINVAL;
-    if (q && (!rows_ok(q, q_ts, q_hs, c->dtype) || !rows_ok(q_out, qo_ts, qo_hs, c->dtype))) return GKV_EINVAL;
-    if (!(c->rope_base >= 0.0) || isinf(c->rope_base)) return GKV_EINVAL;
+    if (!t->pos || !al(t->pos, 4) || !rows_ok(t->k, t->k_ts, t->k_hs, c->dtype) || !rows_ok(t->v, t->v_ts, t->v_hs, c->dtype))
+        return GKV_EINVAL;
+    const void *q = t->q;
+    if ((q != nullptr) != (t->q_out != nullptr)) return GKV_EINVAL;
+    if (q && (!rows_ok(q, t->q_ts, t->q_hs, c->dtype) || !rows_ok(t->q_out, t->qo_ts, t->qo_hs, c->dtype))) return GKV_EINVAL;
     const int es = elem_bytes(c->dtype);
-    AppendArgs a{paged_of(c), l, n_tokens, cu_new, pos, static_cast<const char *>(k), static_cast<const char *>(v),
-                 static_cast<const char *>(q), static_cast<char *>(q_out),
-                 k_ts * es, k_hs * es, v_ts * es, v_hs * es, q_ts * es, q_hs * es, qo_ts * es, qo_hs * es,
-                 c->rope_base > 0.0, static_cast<int *>(workspace)};
+    const AppendArgs a{paged_of(c), l, n_tokens, t->cu_new, t->pos, static_cast<const char *>(t->k),
+                       static_cast<const char *>(t->v), static_cast<const char *>(q), static_cast<char *>(t->q_out),
+                       t->k_ts * es, t->k_hs * es, t->v_ts * es, t->v_hs * es, t->q_ts * es, t->q_hs * es,
+                       t->qo_ts * es, t->qo_hs * es, c->rope_base > 0.0, static_cast<int *>(workspace)};
     const int64_t items = (int64_t)n_tokens * (2 * c->G + (q ? c->Hq : 0)) * (c->d * es / 32);
     if ((items + 255) / 256 >= (1LL << 31)) return GKV_EUNSUPPORTED;
     const Turns &turns = turns_of(c->rope_base, c->d);

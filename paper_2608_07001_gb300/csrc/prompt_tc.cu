@@ -406,12 +406,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else if (fix) {
                         ok = ok && wait(&b.vfix, 0, b, a.status);
                     }
-                    // d = 128: tile 1 goes after tile 0.  Products of the two issued at once would run
-                    // interleaved, end together and leave the tensor pipe idle while both tiles are in
-                    // their softmax (1250 us in turn, 1370 without, at 16K tokens).  At d = 64 the softmax
-                    // is the longer side and a turn only delays it (173 us in turn, 149 without).  An
-                    // order, not a dependence: the wait may run out.
-                    if (D == 128 && i == 1)
+                    // Tile 1 goes after tile 0.  Products of the two issued at once would run interleaved, end
+                    // together and leave the tensor pipe idle while both tiles are in their softmax (d = 128,
+                    // 16K tokens: 1250 us in turn, 1370 without; d = 64, where the softmax is the longer side,
+                    // the same either way).  An order, not a dependence: the wait may run out.
+                    if (i == 1)
                         for (int w = 0; w < 20000 && *(volatile int *)&b.turn <= j; w++) {}
                     if (j < ni) {
                         const uint32_t va = vd + vs * (C::TILE >> 4);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import dataclasses
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -69,6 +70,16 @@ class GkvPagedCache(C.Structure):
         ("K", C.c_void_p), ("V", C.c_void_p), ("log_m", C.c_void_p), ("table", C.c_void_p),
         ("lens", C.c_void_p), ("rope_base", C.c_double),
     ]
+
+
+class GkvPagedTokens(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32)] + [(n, C.c_void_p) for n in ("cu_new", "pos", "k", "v", "q", "q_out")] + [
+        (n, C.c_int64) for n in ("k_ts", "k_hs", "v_ts", "v_hs", "q_ts", "q_hs", "qo_ts", "qo_hs")]
+
+
+# the two structures that every call fills, packed in one go
+_PROMPT, _TOKENS = struct.Struct("@5i4x2q7P8q"), struct.Struct("@i4x6P8q")
+assert _PROMPT.size == C.sizeof(GkvPrompt) and _TOKENS.size == C.sizeof(GkvPagedTokens)
 
 
 class GraceKVError(RuntimeError):
@@ -139,7 +150,7 @@ def lib() -> C.CDLL:
     L.gracekv_paged_workspace_size.argtypes = [pcp, C.POINTER(C.c_size_t)]
     L.gracekv_paged_load.argtypes = [pcp, i32, vp, vp, vp, vp, i64, vp, vp]
     L.gracekv_paged_advance.argtypes = [pcp, vp, vp]
-    L.gracekv_paged_append.argtypes = [pcp, i32, i32, vp, vp] + [vp, i64, i64] * 4 + [vp, vp]
+    L.gracekv_paged_append.argtypes = [pcp, i32, C.POINTER(GkvPagedTokens), vp, vp]
     L.gracekv_paged_attention.argtypes = [pcp, i32, vp, vp, vp, vp]
     L.gracekv_paged_status.argtypes = [vp, vp]
     _lib = L
@@ -579,32 +590,39 @@ class PromptAttention:
     def __init__(self, *, G: int, Hq: int, d: int, dtype, device="cuda"):
         if dtype not in _DTYPES:
             raise _bad(f"dtype must be bf16 or fp32, not {dtype}")
-        self.G, self.Hq, self.d, self.dtype = G, Hq, d, dtype
-        self.desc = GkvPrompt(G, Hq, d, _DTYPES[dtype])
+        self.G, self.Hq, self.d, self.dtype, self._code = G, Hq, d, dtype, _DTYPES[dtype]
+        self._buf = bytearray(C.sizeof(GkvPrompt))
+        self.desc = GkvPrompt.from_buffer(self._buf)
+        _PROMPT.pack_into(self._buf, 0, G, Hq, d, self._code, *[0] * 18)
         n = C.c_size_t()
         _raise(lib().gracekv_prompt_workspace_size(C.byref(self.desc), C.byref(n)))
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=device)
         self._ref, self._device, self._ws = C.byref(self.desc), self.workspace.device, self.workspace.data_ptr()
+        self._call = lib().gracekv_prompt_attention
 
     def __call__(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, return_lse=False, stream=None):
         """out [N, Hq, d] of q's dtype (or (out, lse [N, Hq] fp32) with return_lse)."""
-        p, dev = self.desc, self._device
-        cu_k = cu_q if cu_k is None else cu_k
-        n_q, n_k = q.shape[0], k.shape[0]
+        dev, G, Hq, d, dt = self._device, self.G, self.Hq, self.d, self.dtype
+        n_q, n_k, n1 = q.shape[0], k.shape[0], cu_q.shape[0]
+        qp, q_ts, q_hs = _rows("q", q, n_q, Hq, d, dt, dev)
+        kp, k_ts, k_hs = _rows("k", k, n_k, G, d, dt, dev)
+        vp, v_ts, v_hs = _rows("v", v, n_k, G, d, dt, dev)
+        cq = _words("cu_q", cu_q, (n1,), torch.int32, dev)
+        ck = cq if cu_k is None else _words("cu_k", cu_k, (n1,), torch.int32, dev)
         if out is None:
-            out = _empty_like_on(stream, (n_q, self.Hq, self.d), self.dtype, dev)
-        if lse is None and return_lse:
-            lse = _empty_like_on(stream, (n_q, self.Hq), torch.float32, dev)
-        p.n_seqs, p.n_q, p.n_k = cu_q.numel() - 1, n_q, n_k
-        p.cu_q = _words("cu_q", cu_q, (p.n_seqs + 1,), torch.int32, dev)
-        p.cu_k = _words("cu_k", cu_k, (p.n_seqs + 1,), torch.int32, dev)
-        p.q, p.q_ts, p.q_hs = _rows("q", q, n_q, self.Hq, self.d, self.dtype, dev)
-        p.k, p.k_ts, p.k_hs = _rows("k", k, n_k, self.G, self.d, self.dtype, dev)
-        p.v, p.v_ts, p.v_hs = _rows("v", v, n_k, self.G, self.d, self.dtype, dev)
-        p.out, p.o_ts, p.o_hs = _rows("out", out, n_q, self.Hq, self.d, self.dtype, dev)
-        p.lse = None if lse is None else _words("lse", lse, (n_q, self.Hq), torch.float32, dev)
-        _raise(lib().gracekv_prompt_attention(self._ref, self._ws,
-                                              _on(stream, dev, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
+            out = _empty_like_on(stream, (n_q, Hq, d), dt, dev)
+            op, o_ts, o_hs = out.data_ptr(), Hq * d, d
+        else:
+            op, o_ts, o_hs = _rows("out", out, n_q, Hq, d, dt, dev)
+        lp = 0
+        if lse is not None:
+            lp = _words("lse", lse, (n_q, Hq), torch.float32, dev)
+        elif return_lse:
+            lse = _empty_like_on(stream, (n_q, Hq), torch.float32, dev)
+            lp = lse.data_ptr()
+        _PROMPT.pack_into(self._buf, 0, G, Hq, d, self._code, n1 - 1, n_q, n_k, cq, ck, qp, kp, vp, op, lp,
+                          q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs)
+        _raise(self._call(self._ref, self._ws, _on(stream, dev, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
         return (out, lse) if return_lse else out
 
     def status(self, stream=None):
@@ -642,6 +660,9 @@ class PagedCache:
         _raise(lib().gracekv_paged_workspace_size(C.byref(self.desc), C.byref(n)))
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)
         self._ref, self._device, self._ws = C.byref(self.desc), dev, self.workspace.data_ptr()
+        self._buf = bytearray(C.sizeof(GkvPagedTokens))
+        self._tokens = C.byref(GkvPagedTokens.from_buffer(self._buf))
+        self._append, self._attention = lib().gracekv_paged_append, lib().gracekv_paged_attention
         self._free = None
 
     @staticmethod
@@ -760,31 +781,39 @@ class PagedCache:
     def append(self, l: int, k, v, pos, q=None, cu_new=None, out=None, stream=None):
         """Layer l's new tokens: k, v [N, G, d] into the pages (k rotated to pos [N]
         int32); returns q [N, Hq, d] rotated (into `out`, which may be q), or None."""
-        dev, N = self._device, k.shape[0]
-        if q is not None and out is None:
-            out = _empty_like_on(stream, (N, self.Hq, self.d), self.dtype, dev)
-        none = (None, 0, 0)
-        _raise(lib().gracekv_paged_append(
-            self._ref, l, N,
-            None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
-            _words("pos", pos, (N,), torch.int32, dev), *_rows("k", k, N, self.G, self.d, self.dtype, dev),
-            *_rows("v", v, N, self.G, self.d, self.dtype, dev),
-            *(none if q is None else _rows("q", q, N, self.Hq, self.d, self.dtype, dev)),
-            *(none if q is None else _rows("out", out, N, self.Hq, self.d, self.dtype, dev)),
-            self._ws, _on(stream, dev, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
-                                           self.lens, self.workspace)))
+        dev, N, dt, d = self._device, k.shape[0], self.dtype, self.d
+        kp, k_ts, k_hs = _rows("k", k, N, self.G, d, dt, dev)
+        vp, v_ts, v_hs = _rows("v", v, N, self.G, d, dt, dev)
+        qp = op = q_ts = q_hs = o_ts = o_hs = 0
+        if q is not None:
+            qp, q_ts, q_hs = _rows("q", q, N, self.Hq, d, dt, dev)
+            if out is None:
+                out = _empty_like_on(stream, (N, self.Hq, d), dt, dev)
+                op, o_ts, o_hs = out.data_ptr(), self.Hq * d, d
+            else:
+                op, o_ts, o_hs = _rows("out", out, N, self.Hq, d, dt, dev)
+        _TOKENS.pack_into(self._buf, 0, N,
+                          0 if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
+                          _words("pos", pos, (N,), torch.int32, dev), kp, vp, qp, op,
+                          k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, o_ts, o_hs)
+        _raise(self._append(self._ref, l, self._tokens, self._ws,
+                            _on(stream, dev, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
+                                self.lens, self.workspace)))
         return out
 
     def attention(self, l: int, q, out=None, stream=None):
         """q [B, Hq, d], one rotated query per request slot -> out [B, Hq, d] of the
         cache's dtype over layer l (zeros for an idle slot)."""
         dev, shape = self._device, (self.B, self.Hq, self.d)
+        qp = _words("q", q, shape, self.dtype, dev)
         if out is None:
             out = _empty_like_on(stream, shape, self.dtype, dev)
-        _raise(lib().gracekv_paged_attention(
-            self._ref, l, _words("q", q, shape, self.dtype, dev), _words("out", out, shape, self.dtype, dev),
-            self._ws, _on(stream, dev, q, out, self.K, self.V, self.log_m, self.table, self.lens,
-                                           self.workspace)))
+            op = out.data_ptr()
+        else:
+            op = _words("out", out, shape, self.dtype, dev)
+        _raise(self._attention(self._ref, l, qp, op, self._ws,
+                               _on(stream, dev, q, out, self.K, self.V, self.log_m, self.table, self.lens,
+                                   self.workspace)))
         return out
 
     def status(self, stream=None):

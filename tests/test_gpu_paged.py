@@ -292,6 +292,7 @@ def test_append_positions(gk, dtype):
     pos = [0, 1, -1, 3, 131071, 1 << 20, (1 << 24) + 1, (1 << 31) - 1, -(1 << 31), 77777777]
     append_case(gk, [10], [[4]], 32, 2, 1, 128, dtype, 5e5, pos)
     append_case(gk, [10], [[4]], 32, 2, 1, 64, dtype, 1e4, pos)
+    append_case(gk, [10], [[4]], 32, 2, 1, 64, dtype, 1.0, pos)
 
 
 def test_append_a_long_prompt(gk):

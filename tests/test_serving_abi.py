@@ -59,7 +59,8 @@ def calls(gk, c):
     L = gk.lib()
     yield "load", lambda b=0, K=P, V=P, m=P, off=P, E=5, ws=P: L.gracekv_paged_load(c, b, K, V, m, off, E, ws, None)
     yield "append", lambda l=0, N=3, cu=P, pos=P, k=(P, 128, 64), v=(P, 128, 64), q=(P, 512, 64), o=(P, 512, 64), ws=P: \
-        L.gracekv_paged_append(c, l, N, cu, pos, *k, *v, *q, *o, ws, None)
+        L.gracekv_paged_append(c, l, C.byref(gk.GkvPagedTokens(N, cu, pos, k[0], v[0], q[0], o[0], *k[1:], *v[1:], *q[1:], *o[1:])),
+                               ws, None)
     yield "attention", lambda l=0, q=P, out=P, ws=P: L.gracekv_paged_attention(c, l, q, out, ws, None)
     yield "advance", lambda cu=P: L.gracekv_paged_advance(c, cu, None)
 
@@ -91,7 +92,9 @@ def test_paged_call_refusals(gk):
     assert c["advance"](cu=P + 1) == gk.GKV_EINVAL
     assert dict(calls(gk, paged(gk, log_m=None)))["load"]() == gk.GKV_EINVAL          # log m, and nowhere to keep it
     assert dict(calls(gk, paged(gk, page_size=24)))["attention"]() == gk.GKV_EUNSUPPORTED
-    assert dict(calls(gk, paged(gk, rope_base=-1.0)))["append"]() == gk.GKV_EINVAL
+    for base in (-1.0, 0.5, float("nan"), float("inf")):
+        assert dict(calls(gk, paged(gk, rope_base=base)))["append"]() == gk.GKV_EINVAL
+    assert gk.lib().gracekv_paged_append(paged(gk), 0, None, P, None) == gk.GKV_EINVAL
     assert c["append"](N=0) == gk.GKV_OK                                              # no token: nothing is launched
     n = C.c_size_t()
     assert gk.lib().gracekv_paged_workspace_size(paged(gk), C.byref(n)) == gk.GKV_OK and n.value >= 256
