@@ -27,12 +27,12 @@ namespace serve {
 namespace {
 
 constexpr int kR = kRowsF32, kK = kKeysF32, kThreads = 128;
-constexpr int kPs = kK + 4;                    // floats of a row of P
 
 template <int D>
 struct Cfg {
-    static constexpr int LD = D + 4;           // floats of a row of Q, K: 16-byte chunks of 8 rows in different banks
-    static constexpr int Q = kR * LD, K = kK * LD, V = kK * D, P = kR * kPs;
+    // Q, K, V, P without padding, so that two blocks fit a SM at d = 128 (2 x 112 KB); the 16-byte chunks of
+    // a key are permuted by key % 8 instead, as 8 lanes read one chunk of 8 keys
+    static constexpr int Q = kR * D, K = kK * D, V = kK * D, P = kR * kK;
     static constexpr size_t SMEM = (size_t)(Q + K + V + P) * sizeof(float);
 };
 
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     auto load_k = [&](int j) {
         for (int i = tid; i < kK * (D / 4); i += kThreads) {
             const int r = i / (D / 4), c = i % (D / 4), key = j * kK + r;
-            load4(Ks + r * C::LD + c * 4, K + (key < nk ? key : 0) * a.k_ts + c * 4, key < nk);
+            load4(Ks + r * D + (c ^ (r & 7)) * 4, K + (key < nk ? key : 0) * a.k_ts + c * 4, key < nk);
         }
         copy_commit();
     };
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         for (int i = tid; i < kR * (D / 4); i += kThreads) {
             const int r = i / (D / 4), c = i % (D / 4), t = t0 + r / gq;
             const bool on = r / gq < tok && t < nq;
-            load4(Qs + r * C::LD + c * 4,
+            load4(Qs + r * D + c * 4,
                   static_cast<const T *>(a.q) + (q0 + (on ? t : t0)) * a.q_ts + (g * gq + r % gq) * a.q_hs + c * 4, on);
         }
         load_k(j0);
@@ -128,10 +128,10 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         for (int e = 0; e < D; e += 4) {
             float4 kf[4];
 #pragma unroll
-            for (int c = 0; c < 4; c++) kf[c] = *reinterpret_cast<const float4 *>(Ks + (tx + 16 * c) * C::LD + e);
+            for (int c = 0; c < 4; c++) kf[c] = *reinterpret_cast<const float4 *>(Ks + (tx + 16 * c) * D + ((e >> 2) ^ (tx & 7)) * 4);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float4 qf = *reinterpret_cast<const float4 *>(Qs + (ty * 8 + i) * C::LD + e);
+                const float4 qf = *reinterpret_cast<const float4 *>(Qs + (ty * 8 + i) * D + e);
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
                     x[i][c] = __ffma2_rn(make_float2(qf.x, qf.y), make_float2(kf[c].x, kf[c].y), x[i][c]);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
             for (int c = 0; c < 4; c++) {
                 const float p = tc::ex2(y[c] - sh);
                 z[i] += p;
-                Ps[(ty * 8 + i) * kPs + tx + 16 * c] = p;
+                Ps[(ty * 8 + i) * kK + tx + 16 * c] = p;
             }
         }
         __syncthreads();                      // all of K is read, all of P written
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         for (int e = 0; e < kK; e += 4) {
             float4 p[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) p[i] = *reinterpret_cast<const float4 *>(Ps + (ty * 8 + i) * kPs + e);
+            for (int i = 0; i < 8; i++) p[i] = *reinterpret_cast<const float4 *>(Ps + (ty * 8 + i) * kK + e);
 #pragma unroll
             for (int f = 0; f < 4; f++) {
                 float4 v[D / 64];
