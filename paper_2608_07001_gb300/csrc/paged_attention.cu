@@ -617,11 +617,15 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                         float4 x[8];
 #pragma unroll
                         for (int p = 0; p < 8; p++) {
-                            const float *q = piece(p0 + p);
-                            const bool on = p0 + p < np;
-                            m[p] = on ? __ldcg(q + 8 * D + h) : -INFINITY;
-                            z[p] = on ? __ldcg(q + 8 * D + 8 + h) : 0.f;
-                            x[p] = on ? __ldcg(reinterpret_cast<const float4 *>(q + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            // past the last piece: the last one again, with no weight
+                            const float *q = piece(min(p0 + p, np - 1));
+                            m[p] = __ldcg(q + 8 * D + h);
+                            z[p] = __ldcg(q + 8 * D + 8 + h);
+                            x[p] = __ldcg(reinterpret_cast<const float4 *>(q + i));
+                        }
+#pragma unroll
+                        for (int p = 0; p < 8; p++) {
+                            if (p0 + p >= np) m[p] = -INFINITY;
                             mx = fmaxf(mx, m[p]);
                         }
                         const float sh = pa_shift(mx), f = tc::ex2(M - sh);

@@ -20,16 +20,19 @@ namespace {
 
 using namespace serve;
 
-// Joins 32 rows of a split block, over its parts in order with eight loads in
-// flight.  A thread sums four channels: the tcgen05 kernel's parts are read
-// across rows as they lie and turned in shared memory, so that rows leave whole.
+// Joins some rows of a split block (32 of the tcgen05 kernel's, 8 of the fp32
+// kernel's), four channels a thread, over the parts in order with eight loads in
+// flight: the latency of a read or two, whatever the number of parts.  The
+// tcgen05 kernel's parts are read across rows as they lie and turned in shared
+// memory, so that rows leave whole.
+constexpr int join_rows(bool tc) { return tc ? 32 : 8; }
 template <typename T, int D, bool TC>
-__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
+__global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(const PromptArgs a) {
     constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? kKeysTc : kKeysF32, LEAST = TC ? kLeastTc : kLeastF32;
-    constexpr int C4 = D / 4, LD = C4 + 1;
+    constexpr int C4 = D / 4, LD = C4 + 1, RB = join_rows(TC);
     constexpr size_t PF = part_floats(ROWS, D);
-    __shared__ float4 out_s[32 * LD];
-    __shared__ float m_s[32], z_s[32];
+    __shared__ float4 out_s[TC ? RB * LD : 1];
+    __shared__ float m_s[RB], z_s[RB];
     const int gq = a.Hq / a.G, half = TC ? kRowsTc / 2 : kRowsF32, tpt = half / gq, tok = TC ? 2 * tpt : tpt;
     const int g = blockIdx.x % a.G;
     const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
@@ -41,13 +44,20 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
     const int last = (int)((nq < t0 + tok ? nq : t0 + tok) - 1 + nk - nq);
     const int np = parts_of(last >= 0 ? last / KEYS + 1 : 0, a.split, LEAST);
     if (np == 1) return;
-    const int r0 = blockIdx.y * 32;
+    const int r0 = blockIdx.y * RB, i = threadIdx.x;
     const float *p0 = a.part + (size_t)blockIdx.x * a.split * PF;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < 32 * C4; i += 256) {
-        const int rr = TC ? i % 32 : i / C4, c = TC ? i / 32 : i % C4, r = r0 + rr;
-        const size_t at = TC ? (size_t)c * ROWS + r : (size_t)r * C4 + c;
-        if (r % half / gq >= tpt || t0 + r / half * tpt + r % half / gq >= nq) continue;
+    const int rr = TC ? i % RB : i / C4, c = TC ? i / RB : i % C4, r = r0 + rr;
+    const size_t at = TC ? (size_t)c * ROWS + r : (size_t)r * C4 + c;
+    auto token = [&](int row) { return row % half / gq < tpt ? t0 + row / half * tpt + row % half / gq : nq; };
+    auto write = [&](int row, int col, float4 v, float M, float Z) {
+        const int64_t t = token(row);
+        if (t >= nq) return;
+        const int h = g * gq + row % half % gq;
+        put4(static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + col * 4, v);
+        if (col == 0 && a.lse)
+            a.lse[(q0 + t) * a.Hq + h] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.6931471805599453f;
+    };
+    if (token(r) < nq) {
         float M = -INFINITY, Z = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int b = 0; b < np; b += 8) {
@@ -55,11 +65,15 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
             float4 x[8];
 #pragma unroll
             for (int p = 0; p < 8; p++) {
-                const float *q = p0 + (size_t)(b + p) * PF;
-                const bool on = b + p < np;
-                m[p] = on ? q[ROWS * D + r] : -INFINITY;
-                z[p] = on ? q[ROWS * D + ROWS + r] : 0.f;
-                x[p] = on ? reinterpret_cast<const float4 *>(q)[at] : make_float4(0.f, 0.f, 0.f, 0.f);
+                // past the last part: the last one again, with no weight
+                const float *q = p0 + (size_t)min(b + p, np - 1) * PF;
+                m[p] = q[ROWS * D + r];
+                z[p] = q[ROWS * D + ROWS + r];
+                x[p] = reinterpret_cast<const float4 *>(q)[at];
+            }
+#pragma unroll
+            for (int p = 0; p < 8; p++) {
+                if (b + p >= np) m[p] = -INFINITY;
                 mx = fmaxf(mx, m[p]);
             }
             const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
@@ -74,17 +88,17 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a) {
             }
         }
         const float inv = Z > 0.f ? 1.f / Z : Z;          // a row that sees no key: 0; a NaN stays
-        out_s[rr * LD + c] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-        if (c == 0) { m_s[rr] = M; z_s[rr] = Z; }
+        v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        if constexpr (TC) {
+            out_s[rr * LD + c] = v;
+            if (c == 0) { m_s[rr] = M; z_s[rr] = Z; }
+        } else {
+            write(r, c, v, M, Z);
+        }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * C4; i += 256) {
-        const int rr = i / C4, c = i % C4, r = r0 + rr, tk = r % half / gq, h = g * gq + r % half % gq;
-        const int64_t t = t0 + r / half * tpt + tk;
-        if (tk >= tpt || t >= nq) continue;
-        put4(static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + c * 4, out_s[rr * LD + c]);
-        if (c == 0 && a.lse)
-            a.lse[(q0 + t) * a.Hq + h] = z_s[rr] == 0.f ? -INFINITY : (m_s[rr] + log2f(z_s[rr])) * 0.6931471805599453f;
+    if constexpr (TC) {
+        __syncthreads();
+        write(r0 + i / C4, i % C4, out_s[i / C4 * LD + i % C4], m_s[i / C4], z_s[i / C4]);
     }
 }
 
@@ -92,9 +106,10 @@ template <typename T, bool TC>
 cudaError_t join(const PromptArgs &a, int d, cudaStream_t s) {
     constexpr int ROWS = TC ? kRowsTc : kRowsF32;
     const int gq = a.Hq / a.G, tok = TC ? 2 * (kRowsTc / 2 / gq) : kRowsF32 / gq;
-    const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS / 32);
-    if (d == 128) prompt_join_kernel<T, 128, TC><<<grid, 256, 0, s>>>(a);
-    else prompt_join_kernel<T, 64, TC><<<grid, 256, 0, s>>>(a);
+    constexpr int RB = join_rows(TC);
+    const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS / RB);
+    if (d == 128) prompt_join_kernel<T, 128, TC><<<grid, RB * 32, 0, s>>>(a);
+    else prompt_join_kernel<T, 64, TC><<<grid, RB * 16, 0, s>>>(a);
     return cudaGetLastError();
 }
 
