@@ -480,7 +480,7 @@ gkv_status gracekv_decode_status(void *workspace, void *stream);
  * backwards or past them is skipped and reported by gracekv_prompt_status.
  * d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED); pointers on 16
  * bytes, strides multiples of 16 bytes and not negative, lse on 4 bytes,
- * n_seqs >= 0, n_q and n_k below 2^31.  Values: bf16 products are exact, sums
+ * n_seqs >= 0, n_q and n_k at most 2^31 - 4096.  Values: bf16 products are exact, sums
  * fp32; the softmax weights of bf16 inputs are rounded to bf16 for the value
  * product and the output once to bf16; fp32 inputs stay fp32 throughout.
  * Keys and values of rows outside a sequence do not reach it whatever they

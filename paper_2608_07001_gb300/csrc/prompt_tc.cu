@@ -250,41 +250,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tc_fence_after();
         const int64_t row = q0 + token;
         const int hq = g * t.gq + h;
-        __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.out) + row * a.o_ts + hq * a.o_hs;
-        auto write8 = [&](int col, const float *v, float inv) {
-            uint4 u;
-            u.x = pack2(v[0] * inv, v[1] * inv);
-            u.y = pack2(v[2] * inv, v[3] * inv);
-            u.z = pack2(v[4] * inv, v[5] * inv);
-            u.w = pack2(v[6] * inv, v[7] * inv);
-            *reinterpret_cast<uint4 *>(o + col) = u;
-        };
-        auto write_lse = [&]() {
-            if (a.lse) a.lse[row * a.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
-        };
         if (np == 1) {
             if (ok && i < ntile) {
+                // A thread holds a row, and 32 rows a store are 32 memory sectors: the rows go through
+                // shared memory (this warp's rows of Q, which no product reads any more; 16-byte chunks
+                // permuted by row) and leave 512 bytes a store.
+                constexpr int CH = D / 8;                    // chunks of a row
                 const float inv = z > 0.f ? 1.f / z : z;     // no key: 0; a NaN stays
+                const int64_t at = live ? row * a.o_ts + hq * a.o_hs : -1;
+                unsigned char *stage = Qs + i * C::TILE + q * 32 * (D * 2);
 #pragma unroll
                 for (int k = 0; k < D / 32; k++) {
-                    float v[32];
+                    uint32_t u[32];
                     if (nj > 0) {
-                        uint32_t u[32];
                         tc::tmem_ld32_async(to + 32 * k, u);
                         tc::tmem_wait_ld(u);
-#pragma unroll
-                        for (int e = 0; e < 32; e++) v[e] = __uint_as_float(u[e]);
                     }
-                    if (nj == 0 || lim < 0) {
 #pragma unroll
-                        for (int e = 0; e < 32; e++) v[e] = 0.f;
-                    }
-                    if (live) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8) write8(k * 32 + e, v + e, inv);
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (lim >= 0) {
+                            v.x = pack2(__uint_as_float(u[e]) * inv, __uint_as_float(u[e + 1]) * inv);
+                            v.y = pack2(__uint_as_float(u[e + 2]) * inv, __uint_as_float(u[e + 3]) * inv);
+                            v.z = pack2(__uint_as_float(u[e + 4]) * inv, __uint_as_float(u[e + 5]) * inv);
+                            v.w = pack2(__uint_as_float(u[e + 6]) * inv, __uint_as_float(u[e + 7]) * inv);
+                        }
+                        const int ch = k * 4 + e / 8;
+                        if (nj > 0) *reinterpret_cast<uint4 *>(stage + lane * (D * 2) + ((ch ^ lane) & (CH - 1)) * 16) = v;
+                        else if (live) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at + ch * 8) = v;
                     }
                 }
-                if (live) write_lse();
+                if (nj > 0) {
+                    __syncwarp();
+#pragma unroll 4
+                    for (int x = 0; x < CH; x++) {
+                        const int rr = x * (32 / CH) + lane / CH, ch = lane % CH;
+                        const int64_t to_row = __shfl_sync(0xffffffffu, at, rr);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + rr * (D * 2) + ((ch ^ rr) & (CH - 1)) * 16);
+                        if (to_row >= 0) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + to_row + ch * 8) = v;
+                    }
+                }
+                if (live && a.lse) a.lse[row * a.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
             }
         } else {
             // a part: [D / 4][rows] sums of 4 channels, then [rows] references, [rows] sums of weights
