@@ -730,6 +730,12 @@ class PagedCache:
         counts = np.diff(off)
         if off[0] < 0 or counts.min() < 0 or off[-1] > n_entries or n_entries > cache.K.shape[0]:
             raise _bad("the cache's offsets do not fit its entries")
+        if not 0 <= b < self.B:
+            raise _bad(f"request {b} of {self.B}")
+        need = -(-counts // self.page_size)
+        held = int((self._host_table[:, b] >= 0).sum())
+        if need.max() > self.max_pages or need.sum() > self._n_free + held:
+            raise GraceKVError(GKV_ECAPACITY, f"{int(need.sum())} pages needed, {self._n_free + held} free")
         self.release(b, stream)
         new = self._host_lens.copy()
         new[:, b] = counts.reshape(self.L, self.G)
