@@ -97,6 +97,8 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
 template <typename T, int D, int R>
 __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
+    next_may_start();
+    after_previous();
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0), stride = (rows + R - 1) / R;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int ch = (int)(i % CH);
@@ -164,18 +166,19 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
 // of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread: 201 / 158 /
 // 137 / 144 us with two in flight, 5.9 TB/s at best).
 template <typename T, int D>
-void launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
+cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
     constexpr int CH = D * (int)sizeof(T) / 32;
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
     const int64_t one = (int64_t)a.n_tokens * rows * CH;
     const bool many = one >= kAppendMany;
     const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 3) / 4) * CH : one;
     const unsigned n = (unsigned)((threads + 255) / 256);
-    if (many) paged_append_kernel<T, D, 4><<<n, 256, 0, s>>>(a, turns);
-    else paged_append_kernel<T, D, 1><<<n, 256, 0, s>>>(a, turns);
+    return launch_overlapped(many ? paged_append_kernel<T, D, 4> : paged_append_kernel<T, D, 1>, n, 256, 0, s, a, turns);
 }
 
 __global__ void paged_advance_kernel(int32_t *lens, const int32_t *cu_new, int n, int B, int G) {
+    next_may_start();
+    after_previous();
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= n) return;
     const int b = i / G % B, len = lens[i];
@@ -200,6 +203,8 @@ template <int RB, int IT>
 __global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
     constexpr int CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
     constexpr int U = IT < 4 ? IT : 4;
+    next_may_start();
+    after_previous();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, cap = (int64_t)a.c.page_size * a.c.max_pages;
     const int heads = a.c.L * a.c.G, lane = threadIdx.x & 31;
     if (i < heads) {
@@ -250,12 +255,12 @@ __global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
 }
 
 template <int RB>
-void launch_load(const LoadArgs &a, cudaStream_t s) {
+cudaError_t launch_load(const LoadArgs &a, cudaStream_t s) {
     // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes (6.5 TB/s); one 187, four 200
     constexpr int IT = 2;
     constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
     const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);
-    paged_load_kernel<RB, IT><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a);
+    return launch_overlapped(paged_load_kernel<RB, IT>, (unsigned)((threads + 255) / 256), 256, 0, s, a);
 }
 
 }  // namespace
@@ -275,10 +280,8 @@ extern "C" gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, co
     const LoadArgs a{paged_of(c), b, static_cast<const char *>(K), static_cast<const char *>(V), log_m, offsets,
                      n_entries, static_cast<int *>(workspace)};
     const int rb = c->d * elem_bytes(c->dtype);
-    if (rb == 128) launch_load<128>(a, s);
-    else if (rb == 256) launch_load<256>(a, s);
-    else launch_load<512>(a, s);
-    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    const cudaError_t e = rb == 128 ? launch_load<128>(a, s) : rb == 256 ? launch_load<256>(a, s) : launch_load<512>(a, s);
+    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
 extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream) {
@@ -286,8 +289,9 @@ extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int3
     if (st != GKV_OK) return st;
     if (!al(cu_new, 4)) return GKV_EINVAL;
     const int n = c->L * c->B * c->G;
-    paged_advance_kernel<<<(n + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream)>>>(c->lens, cu_new, n, c->B, c->G);
-    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    const cudaError_t e = launch_overlapped(paged_advance_kernel, (n + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream),
+                                            c->lens, cu_new, n, c->B, c->G);
+    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
 extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t,
@@ -314,14 +318,10 @@ extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, 
     if ((items + 255) / 256 >= (1LL << 31)) return GKV_EUNSUPPORTED;
     const Turns &turns = turns_of(c->rope_base, c->d);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (c->dtype == GKV_BF16) {
-        if (c->d == 128) launch_append<__nv_bfloat16, 128>(a, turns, s);
-        else launch_append<__nv_bfloat16, 64>(a, turns, s);
-    } else {
-        if (c->d == 128) launch_append<float, 128>(a, turns, s);
-        else launch_append<float, 64>(a, turns, s);
-    }
-    return cudaGetLastError() == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    const cudaError_t e = c->dtype == GKV_BF16
+                              ? (c->d == 128 ? launch_append<__nv_bfloat16, 128>(a, turns, s) : launch_append<__nv_bfloat16, 64>(a, turns, s))
+                              : (c->d == 128 ? launch_append<float, 128>(a, turns, s) : launch_append<float, 64>(a, turns, s));
+    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
 extern "C" gkv_status gracekv_paged_status(void *workspace, void *stream) {

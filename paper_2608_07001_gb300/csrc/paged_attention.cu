@@ -413,6 +413,21 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int gq = a.c.Hq / a.c.G, S = a.S;
 
+    next_may_start();
+    if (tid == 0) {
+        for (int i = 0; i < C::NST; i++) {
+            tc::mbar_init(tc::smem_u32(&sm.full[i]), 1);
+            tc::mbar_init(tc::smem_u32(&sm.empty[i]), C::BF ? kPaWarps : 1);
+        }
+        sm.abort = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == kPaWarps && lane == 0) {
+        tc::tma_prefetch_desc(&mapK);
+        tc::tma_prefetch_desc(&mapV);
+    }
+    after_previous();
+
     // ---- the CTA's run: tiles of all sequences, and where its own begin
     const int seg = (S + kPaThreads - 1) / kPaThreads;
     long long mine = 0;
@@ -433,14 +448,6 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         if (lane >= o) incl += v;
     }
     if (lane == 31) sm.wsum[warp] = incl;
-    if (tid == 0) {
-        for (int i = 0; i < C::NST; i++) {
-            tc::mbar_init(tc::smem_u32(&sm.full[i]), 1);
-            tc::mbar_init(tc::smem_u32(&sm.empty[i]), C::BF ? kPaWarps : 1);
-        }
-        sm.abort = 0;
-        tc::fence_barrier_init();
-    }
     __syncthreads();
     long long before = incl - mine, total = 0;
 #pragma unroll
@@ -473,10 +480,6 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
 
     if (warp == kPaWarps) {
         // ---------------- producer ----------------
-        if (lane == 0) {
-            tc::tma_prefetch_desc(&mapK);
-            tc::tma_prefetch_desc(&mapV);
-        }
         const int per_tile = C::TE / min(a.box, C::TE), box = min(a.box, C::TE);
         uint32_t it = 0;
         bool ok = true;
@@ -691,8 +694,7 @@ cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
     const int64_t rows = a.c.n_pages * a.c.page_size;
     const int box = std::min(a.box, C::TE);
     if (!pa_map<T>(&mk, a.c.K, rows, D, box) || !pa_map<T>(&mv, a.c.V, rows, D, box)) return cudaErrorNotSupported;
-    kern<<<grid, kPaThreads, smem, s>>>(a, mk, mv);
-    return cudaGetLastError();
+    return launch_overlapped(kern, grid, kPaThreads, smem, s, a, mk, mv);
 }
 
 template <int D>

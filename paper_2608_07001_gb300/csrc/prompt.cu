@@ -33,6 +33,8 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
     constexpr size_t PF = part_floats(ROWS, D);
     __shared__ float4 out_s[TC ? RB * LD : 1];
     __shared__ float m_s[RB], z_s[RB];
+    next_may_start();
+    after_previous();
     const int gq = a.Hq / a.G, half = TC ? kRowsTc / 2 : kRowsF32, tpt = half / gq, tok = TC ? 2 * tpt : tpt;
     const int g = blockIdx.x % a.G;
     const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
@@ -108,9 +110,8 @@ cudaError_t join(const PromptArgs &a, int d, cudaStream_t s) {
     const int gq = a.Hq / a.G, tok = TC ? 2 * (kRowsTc / 2 / gq) : kRowsF32 / gq;
     constexpr int RB = join_rows(TC);
     const dim3 grid((unsigned)(prompt_slots(a.n_q, a.n_seqs, tok) * a.G), ROWS / RB);
-    if (d == 128) prompt_join_kernel<T, 128, TC><<<grid, RB * 32, 0, s>>>(a);
-    else prompt_join_kernel<T, 64, TC><<<grid, RB * 16, 0, s>>>(a);
-    return cudaGetLastError();
+    return d == 128 ? launch_overlapped(prompt_join_kernel<T, 128, TC>, grid, RB * 32, 0, s, a)
+                    : launch_overlapped(prompt_join_kernel<T, 64, TC>, grid, RB * 16, 0, s, a);
 }
 
 gkv_status check_geometry(const gkv_prompt *p) {

@@ -58,6 +58,8 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
     extern __shared__ __align__(16) float sm[];
     float *Qs = sm, *Ks = Qs + C::Q, *Vs = Ks + C::K, *Ps = Vs + C::V;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    next_may_start();
+    after_previous();
     if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
 
     // ---- the block: rows of one KV head, heavy blocks (late tokens) first
@@ -238,8 +240,7 @@ cudaError_t launch(PromptArgs a, int dtype, cudaStream_t s) {
     if (blocks >= (1LL << 31)) return cudaErrorInvalidConfiguration;
     // as many parts as fit beside one another, none smaller than a key tile
     a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsF32 / blocks, (a.n_k + kK - 1) / kK));
-    prompt_f32_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, smem, s>>>(a);
-    e = cudaGetLastError();
+    e = launch_overlapped(prompt_f32_kernel<T, D>, dim3((unsigned)blocks, (unsigned)a.split), kThreads, smem, s, a);
     return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, dtype, false, s) : e;
 }
 

@@ -111,28 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ Bars b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
-    // ---- the CTA's rows: heavy blocks (late tokens) first
-    const int g = blockIdx.x % a.G;
-    const int tok = 2 * t.tpt;
-    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
-    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
-    int64_t q0, nq64, k0, nk64;
-    if (!seq_bounds(a, s, q0, nq64, k0, nk64)) return;
-    const int64_t t0_64 = (slot - (q0 / tok + s)) * tok;
-    if (t0_64 < 0 || t0_64 >= nq64) return;
-    const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
-    const int off = nk - nq;                             // query i sees keys <= i + off
-    const int ntile = t0 + t.tpt < nq ? 2 : 1;
-    // key tiles of each row tile, up to the last key its last token sees; of
-    // them this part's: [j0, j0 + n)
-    const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
-    const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
-    const int all = max(all0, all1), np = parts_of(all, a.split, kLeastTc);
-    if ((int)blockIdx.y >= np) return;
-    const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
-    const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
-
+    next_may_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::NST; i++) {
             tc::mbar_init(tc::smem_u32(&b.full[i]), 1);
@@ -154,10 +133,41 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tmem_alloc(tc::smem_u32(&b.tbase), 512);
         tc::tmem_relinquish();
     }
+    if (warp == kWarpTma && lane == 0) {
+        tc::tma_prefetch_desc(&mapQ);
+        tc::tma_prefetch_desc(&mapK);
+        tc::tma_prefetch_desc(&mapV);
+    }
+    after_previous();
+    if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
+    // ---- the CTA's rows: heavy blocks (late tokens) first
+    const int g = blockIdx.x % a.G;
+    const int tok = 2 * t.tpt;
+    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
+    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    int64_t q0, nq64, k0, nk64;
+    const bool fits = seq_bounds(a, s, q0, nq64, k0, nk64);
+    const int64_t t0_64 = (slot - (q0 / tok + s)) * tok;
+    const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
+    const int off = nk - nq;                             // query i sees keys <= i + off
+    const int ntile = t0 + t.tpt < nq ? 2 : 1;
+    // key tiles of each row tile, up to the last key its last token sees; of
+    // them this part's: [j0, j0 + n)
+    const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
+    const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
+    const int all = max(all0, all1), np = parts_of(all, a.split, kLeastTc);
+    const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
+    const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
+
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tb = b.tbase;
+    // nothing to do: a sequence that does not fit, a slot past its tokens, a part beyond the block's
+    if (!fits || t0_64 < 0 || t0_64 >= nq64 || (int)blockIdx.y >= np) {
+        if (warp == kWarpMma) tc::tmem_dealloc(tb, 512);
+        return;
+    }
 
     // the sequence's last key tile is partial and other rows follow it: their V rows are zeroed
     const int keep = nk - (j1 - 1) * kN;                  // keys of the sequence in the part's last tile, from it on
@@ -323,9 +333,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             int issued = 0;
             bool ok = n > 0;
             if (lane == 0 && ok) {
-                tc::tma_prefetch_desc(&mapQ);
-                tc::tma_prefetch_desc(&mapK);
-                tc::tma_prefetch_desc(&mapV);
                 const uint32_t qb = tc::smem_u32(&b.qfull);
                 tc::mbar_expect_tx(qb, (uint32_t)(ntile * C::NB * t.tpt * t.gq * 128));
                 for (int i = 0; i < ntile; i++)
@@ -510,8 +517,8 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
     }
     // fewer blocks than SMs: their keys are split over the others
     a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + kN - 1) / kN / kLeastTc));
-    prompt_tc_kernel<D><<<dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s>>>(a, t, mq, mk, mv);
-    e = cudaGetLastError();
+    e = launch_overlapped(prompt_tc_kernel<D>, dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s, a, t, mq,
+                          mk, mv);
     return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, GKV_BF16, true, s) : e;
 }
 
