@@ -62,6 +62,7 @@ constexpr int kPaRing = 96 * 1024;                 // bytes of the ring
 constexpr int kPaPerSm = 2;                        // resident CTAs a SM
 constexpr int kPaMaxGrid = 512;
 constexpr int kPaSnap = 8;                         // tiles of the longest sequence up to which none is split
+constexpr int kPaPieces = 64;                      // pieces of a sequence that small launches aim at, at most
 constexpr uint64_t kPaWaitNs = 2000000000ull;
 
 template <typename T, int D>
@@ -71,7 +72,7 @@ struct PaCfg {
     static constexpr int NB = D * (int)sizeof(T) / 128;          // 128-byte column boxes of a row
     static constexpr int TB = NB * TE * 128;       // bytes of a tile's keys
     static constexpr int NST = kPaRing / (2 * TB); // stages
-    static constexpr int MIN = BF ? 4 : 3;         // tiles of a run at least
+    static constexpr int MIN = BF ? 2 : 1;         // tiles of a run at least
     static_assert(NST >= 3 && NST <= 12 && (BF || NST % kPaF32Warps == 0), "ring");
 };
 
@@ -457,7 +458,12 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         most = max(most, sm.wmax[w]);
     }
     const bool snap = most <= kPaSnap;
-    const long long nc = min((long long)gridDim.x, (total + C::MIN - 1) / C::MIN);
+    // A run holds MIN tiles at least, and as many as leave the longest sequence kPaPieces pieces: one CTA
+    // joins them, eight at a time.  (16000 entries of 2 sequences: 18.6 us with runs of 2 tiles, 15.7 of 4,
+    // 16.5 of 8; 2000 entries of 8: 11.2 of 2, 12.2 of 4, 14.7 of 8; fp32, 1000 entries of 10 in tiles of
+    // 32: 12.3 of 1, 13.9 of 2, 15.1 of 4.)
+    const long long least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
+    const long long nc = min((long long)gridDim.x, (total + least - 1) / least);
     const long long lo = (long long)blockIdx.x < nc ? blockIdx.x * total / nc : total;
     const long long hi = (long long)blockIdx.x < nc ? (blockIdx.x + 1) * total / nc : total;
     if (lo < hi && lo >= before && lo < before + mine) {
