@@ -15,9 +15,9 @@
 // row that it takes.
 //
 // Both move 2 es d bytes a row (in and out) and are bound by HBM, or by the
-// latency of a launch for a few tokens: 137 us for 32768 tokens of 32 + 2 x 8
-// rows of 128 bf16 (805 MB, 5.9 TB/s), 3 us for one token; load 167 us for 1M
-// entries of 2 x 128 bf16 (1082 MB, 6.5 TB/s).
+// latency of a launch for a few tokens: 128 us for 32768 tokens of 32 + 2 x 8
+// rows of 128 bf16 (805 MB, 6.3 TB/s), 2.5 us for one token; load 164 us for 1M
+// entries of 2 x 128 bf16 (1082 MB, 6.6 TB/s).
 #include "paged.cuh"
 
 #include <math.h>
@@ -94,8 +94,10 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
 // one 16-byte chunk of each half, and R of the rows, `stride` apart, so that
 // its sines and cosines serve R rows.  Neighbouring threads take neighbouring
 // chunks: a row's half is one 64- to 256-byte line.
+// Five blocks a SM (48 registers): 128 us at 32768 tokens of 48 rows; four 132 to
+// 146, six 139, eight (spills) 168.
 template <typename T, int D, int R>
-__global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
+__global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
     next_may_start();
     after_previous();
@@ -163,8 +165,8 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const AppendArgs a, c
 
 // R: rows of a thread.  Few tokens want every row on its own thread, the
 // latency of one row; many want a thread's sines to serve several (32768 tokens
-// of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread: 201 / 158 /
-// 137 / 144 us with two in flight, 5.9 TB/s at best).
+// of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread and two in
+// flight: 201 / 158 / 137 / 144 us, before five blocks a SM).
 template <typename T, int D>
 cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
     constexpr int CH = D * (int)sizeof(T) / 32;
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
 
 template <int RB>
 cudaError_t launch_load(const LoadArgs &a, cudaStream_t s) {
-    // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes (6.5 TB/s); one 187, four 200
+    // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes; one 187, four 200
     constexpr int IT = 2;
     constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
     const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);

@@ -11,6 +11,8 @@
 // a shared-memory read feeds 8 (S) and 10 (PV) FMAs; packed fp32x2 FMA halves
 // the issue slots, along the channels for S and across output columns for PV.
 // K of the next tile arrives (cp.async) under PV, V under S.  Two blocks a SM.
+// Measured: 50 TFLOP/s (32 / 8 heads of 128 at 4500 tokens; FMA pipe 67 % busy),
+// 25 us for 1024 tokens of 2 heads.  256 threads of 4 x 4 scores: 44 TFLOP/s.
 //
 // When a launch has fewer blocks than the GPU holds, a block's keys are split
 // into parts (prompt.cuh) that prompt.cu joins.
