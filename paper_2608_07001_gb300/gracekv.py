@@ -559,14 +559,29 @@ def _words(name: str, t: torch.Tensor, shape, dtype, device):
     return t.data_ptr()
 
 
-def _on(stream, device, *tensors):
-    """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return stream.cuda_stream
+class _Workspace:
+    """A zeroed workspace, usable on any one stream at a time: its zeros are there
+    before the constructor returns, and it stays alive for the streams it is used on."""
+
+    def _make_workspace(self, n: int, device):
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=device)
+        self._device, self._ws = self.workspace.device, self.workspace.data_ptr()
+        own = torch.cuda.current_stream(self._device)
+        own.synchronize()
+        self._own_stream = own.cuda_stream
+
+    def _on(self, stream, *tensors):
+        """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
+        if stream is None:
+            raw = torch._C._cuda_getCurrentRawStream(self._device.index)
+            if raw != self._own_stream:
+                self.workspace.record_stream(torch.cuda.current_stream(self._device))
+            return raw
+        self.workspace.record_stream(stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        return stream.cuda_stream
 
 
 def _empty_like_on(stream, shape, dtype, device):
@@ -576,7 +591,7 @@ def _empty_like_on(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-class PromptAttention:
+class PromptAttention(_Workspace):
     """Causal attention of packed prompts (gracekv_prompt_* of the C ABI).
 
     One object holds the workspace of one stream.  q [N, Hq, d], k and v
@@ -596,8 +611,8 @@ class PromptAttention:
         _PROMPT.pack_into(self._buf, 0, G, Hq, d, self._code, *[0] * 18)
         n = C.c_size_t()
         _raise(lib().gracekv_prompt_workspace_size(C.byref(self.desc), C.byref(n)))
-        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=device)
-        self._ref, self._device, self._ws = C.byref(self.desc), self.workspace.device, self.workspace.data_ptr()
+        self._make_workspace(n.value, device)
+        self._ref = C.byref(self.desc)
         self._call = lib().gracekv_prompt_attention
 
     def __call__(self, q, k, v, cu_q, cu_k=None, *, out=None, lse=None, return_lse=False, stream=None):
@@ -622,14 +637,14 @@ class PromptAttention:
             lp = lse.data_ptr()
         _PROMPT.pack_into(self._buf, 0, G, Hq, d, self._code, n1 - 1, n_q, n_k, cq, ck, qp, kp, vp, op, lp,
                           q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs)
-        _raise(self._call(self._ref, self._ws, _on(stream, dev, q, k, v, cu_q, cu_k, out, lse, self.workspace)))
+        _raise(self._call(self._ref, self._ws, self._on(stream, q, k, v, cu_q, cu_k, out, lse)))
         return (out, lse) if return_lse else out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_prompt_status(self.workspace.data_ptr(), _on(stream, self.workspace.device, self.workspace)))
+        _raise(lib().gracekv_prompt_status(self._ws, self._on(stream)))
 
 
-class PagedCache:
+class PagedCache(_Workspace):
     """A paged cache of many requests (gracekv_paged_* of the C ABI).
 
     K, V [n_pages, page_size, d], log_m [n_pages, page_size] fp32 (or None),
@@ -658,8 +673,8 @@ class PagedCache:
             float(rope_base))
         n = C.c_size_t()
         _raise(lib().gracekv_paged_workspace_size(C.byref(self.desc), C.byref(n)))
-        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)
-        self._ref, self._device, self._ws = C.byref(self.desc), dev, self.workspace.data_ptr()
+        self._make_workspace(n.value, dev)
+        self._ref = C.byref(self.desc)
         self._buf = bytearray(C.sizeof(GkvPagedTokens))
         self._tokens = C.byref(GkvPagedTokens.from_buffer(self._buf))
         self._append, self._attention = lib().gracekv_paged_append, lib().gracekv_paged_attention
@@ -717,7 +732,7 @@ class PagedCache:
             _words("V", V, (E, self.d), self.dtype, dev),
             None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
             _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self._ws,
-            _on(stream, dev, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens, self.workspace)))
+            self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens)))
 
     def load(self, b: int, cache: Cache, n_entries: int, stream=None):
         """A compressed cache (Compressor's output) as request b, replacing what the
@@ -765,7 +780,7 @@ class PagedCache:
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
         p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
-        _raise(lib().gracekv_paged_advance(self._ref, p, _on(stream, self.K.device, self.lens, cu_new)))
+        _raise(lib().gracekv_paged_advance(self._ref, p, self._on(stream, self.lens, cu_new)))
 
     def release(self, b: int, stream=None):
         """Request b's pages return to the pool; the slot is idle."""
@@ -803,8 +818,8 @@ class PagedCache:
                           _words("pos", pos, (N,), torch.int32, dev), kp, vp, qp, op,
                           k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, o_ts, o_hs)
         _raise(self._append(self._ref, l, self._tokens, self._ws,
-                            _on(stream, dev, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
-                                self.lens, self.workspace)))
+                            self._on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
+                                     self.lens)))
         return out
 
     def attention(self, l: int, q, out=None, stream=None):
@@ -818,9 +833,8 @@ class PagedCache:
         else:
             op = _words("out", out, shape, self.dtype, dev)
         _raise(self._attention(self._ref, l, qp, op, self._ws,
-                               _on(stream, dev, q, out, self.K, self.V, self.log_m, self.table, self.lens,
-                                   self.workspace)))
+                               self._on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens)))
         return out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_paged_status(self.workspace.data_ptr(), _on(stream, self.workspace.device, self.workspace)))
+        _raise(lib().gracekv_paged_status(self._ws, self._on(stream)))

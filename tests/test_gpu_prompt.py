@@ -196,6 +196,24 @@ def test_another_stream(gk):
     assert torch.equal(here, there)
 
 
+def test_made_here_and_used_on_another_stream(gk):
+    # the current stream is another one from the first call on; the object goes while its work is queued
+    q, k, v = (t.cuda() for t in inputs(17, 400, 400, 8, 2, 64, BF))
+    c = torch.tensor([0, 400], dtype=torch.int32, device="cuda")
+    want = gk.PromptAttention(G=2, Hq=8, d=64, dtype=BF)(q, k, v, c)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        op = gk.PromptAttention(G=2, Hq=8, d=64, dtype=BF)
+        first = op(q, k, v, c)
+    op2 = gk.PromptAttention(G=2, Hq=8, d=64, dtype=BF)
+    with torch.cuda.stream(s):
+        second = op2(q, k, v, c)
+    del op, op2
+    s.synchronize()
+    assert torch.equal(first, want) and torch.equal(second, want)
+
+
 def test_graph_capture(gk):
     q, k, v = (t.cuda() for t in inputs(13, 300, 300, 4, 2, 128, BF))
     c = torch.tensor([0, 120, 300], dtype=torch.int32, device="cuda")
