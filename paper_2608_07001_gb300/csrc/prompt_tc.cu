@@ -26,9 +26,9 @@
 //
 // Measured (32 / 8 heads): 16384 tokens of d = 128 1.24 to 1.36 ms by the power
 // limit, 1.62 to 1.78 PFLOP/s of 1.88 that a plain matrix product reaches, the
-// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.56 ms, 1.05
-// PFLOP/s: there the softmax warps bound it (special function units 43 %, issue
-// 48 % busy).  Tried for d = 64 and slower: key tiles of 64 with two or three
+// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.53 ms, 1.12
+// PFLOP/s (0.56 ms with the maximum taken in registers: 64 instructions a tile,
+// which tcgen05.ld.red, a load that also returns its largest value, saves).  Tried for d = 64 and slower: key tiles of 64 with two or three
 // score buffers a row tile, four row tiles a CTA, two threads a row.
 //
 // Few blocks (a short chunk over a long cache) leave SMs idle: then a block's
@@ -200,26 +200,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tc::tc_fence_after();
             uint32_t x[4][32];
+            float mx[4];
 #pragma unroll
-            for (int k = 0; k < 4; k++) tc::tmem_ld32_async(ts + 32 * k, x[k]);
+            for (int k = 0; k < 4; k++) tc::tmem_ld32_max_async(ts + 32 * k, x[k], mx[k]);
             tc::tmem_wait_ld(x[0]);
 #pragma unroll
             for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
+#pragma unroll
+            for (int k = 0; k < 4; k++) tc::tmem_loaded(mx[k]);
             if ((j0 + j) * kN + kN - 1 > clear) {
                 const int rel = lim - (j0 + j) * kN;
 #pragma unroll
-                for (int k = 0; k < 4; k++)
+                for (int k = 0; k < 4; k++) {
 #pragma unroll
                     for (int e = 0; e < 32; e++)
                         if (k * 32 + e > rel) x[k][e] = 0xff800000u;       // -inf
-            }
-            float mx[4];
+                    mx[k] = fmaxf(__uint_as_float(x[k][0]), __uint_as_float(x[k][1]));
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                mx[k] = fmaxf(__uint_as_float(x[k][0]), __uint_as_float(x[k][1]));
-#pragma unroll
-                for (int e = 2; e < 32; e += 2)
-                    mx[k] = max3(mx[k], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+                    for (int e = 2; e < 32; e += 2)
+                        mx[k] = max3(mx[k], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+                }
             }
             const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
             if (m == -INFINITY) m = mn;                  // nothing accumulated yet
