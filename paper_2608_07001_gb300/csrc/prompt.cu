@@ -28,7 +28,7 @@ using namespace serve;
 constexpr int join_rows(bool tc) { return tc ? 32 : 8; }
 template <typename T, int D, bool TC>
 __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(const PromptArgs a) {
-    constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? kKeysTc : kKeysF32, LEAST = TC ? kLeastTc : kLeastF32;
+    constexpr int ROWS = TC ? kRowsTc : kRowsF32, KEYS = TC ? keys_tc(D) : kKeysF32, LEAST = TC ? least_tc(D) : kLeastF32;
     constexpr int C4 = D / 4, LD = C4 + 1, RB = join_rows(TC);
     constexpr size_t PF = part_floats(ROWS, D);
     __shared__ float4 out_s[TC ? RB * LD : 1];

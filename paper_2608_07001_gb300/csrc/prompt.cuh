@@ -12,7 +12,8 @@ namespace serve {
 // whose parts are a quarter of the rows and two CTAs are resident).
 constexpr int kPartsTc = 152, kPartsF32 = 608;
 constexpr int kRowsTc = 256, kRowsF32 = 64;        // rows of a block
-constexpr int kKeysTc = 128, kKeysF32 = 64;        // keys of a tile
+constexpr int kKeysF32 = 64;                       // keys of a tile
+__host__ __device__ constexpr int keys_tc(int d) { return d == 64 ? 96 : 128; }
 
 struct PromptArgs {
     const void *q, *k, *v;
@@ -60,8 +61,9 @@ __device__ __forceinline__ void check_bounds(const PromptArgs &a) {
 }
 
 // Key tiles of a part at least: what joining costs (about 4 us) against a tile
-// (about 1 us on tcgen05, 6 us on CUDA cores).
-constexpr int kLeastTc = 4, kLeastF32 = 1;
+// (about 1 us for 128 keys on tcgen05, 6 us for 64 on CUDA cores).
+constexpr int kLeastF32 = 1;
+__host__ __device__ constexpr int least_tc(int d) { return 512 / keys_tc(d); }
 // Parts of a block of n key tiles when a launch splits blocks `split` ways.
 __host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
     const int most = n / least;

@@ -12,24 +12,35 @@
 //
 // What bounds it: at d = 128 a 128 x 128 tile costs 2 x 128^3 MACs in each of
 // the two products against 128^2 exponentials, so the tensor pipe; at d = 64
-// the exponentials weigh twice as much.  The two row tiles alternate: while the
-// tensor core works on one's S and PV, the other's warps take its softmax.
+// the exponentials weigh twice as much, and the softmax warps bound it.  The two
+// row tiles alternate: while the tensor core works on one's S and PV, the
+// other's warps take its softmax.
 //
-// Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread a row, its 128 scores
-// in registers), 8 TMA (Q once, then K and V tiles of 128 keys through a ring),
-// 9 and 10 MMA issue of tile 0 and 1 (11 idle: registers are split by
-// warpgroup).  TMEM: S0, S1 (128 columns each; P overlays the lower half of
-// its S as packed bf16), O0, O1.  P is the A operand of its product from TMEM;
-// V is the B operand as it lies in memory (rows of channels, "MN-major").
-// tcgen05 operations of one thread complete in order, so the commit of S(j + 1)
-// also tells that PV(j) is done: the rescaling needs no barrier of its own.
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1 (one thread a row, its scores of a
+// key tile in registers; the load from TMEM returns their maximum too), 8 TMA
+// (Q once, then K and V tiles through a ring), 9 and 10 MMA issue of tile 0 and
+// 1 (11 idle: registers are split by warpgroup).  P is the A operand of its
+// product from TMEM, packed bf16 over the first half of its S; V is the B
+// operand as it lies in memory (rows of channels, "MN-major").
+// TMEM, d = 128: S0, S1 of 128 keys, O0, O1.  tcgen05 operations of one thread
+// complete in order, so the commit of S(j + 1) also tells that PV(j) is done.
+// TMEM, d = 64: key tiles of 96, so that two S a row tile and O fill the 512
+// columns: S(j + 1) is made under the softmax of j, and the round trip P, PV,
+// QK, S (830 clocks and more) leaves the softmax warps' path.
+// The issuing warp is a chain of waits and commits, about 110 clocks each: at
+// d = 64 a ring slot holds V(j) and K(j + 2), one wait and one commit for both,
+// and P is handed over at once.
 //
-// Measured (32 / 8 heads): 16384 tokens of d = 128 1.24 to 1.36 ms by the power
-// limit, 1.62 to 1.78 PFLOP/s of 1.88 that a plain matrix product reaches, the
-// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.53 ms, 1.12
-// PFLOP/s (0.56 ms with the maximum taken in registers: 64 instructions a tile,
-// which tcgen05.ld.red, a load that also returns its largest value, saves).  Tried for d = 64 and slower: key tiles of 64 with two or three
-// score buffers a row tile, four row tiles a CTA, two threads a row.
+// Measured (32 / 8 heads): 16384 tokens of d = 128 1.20 to 1.36 ms by the power
+// limit, 1.62 to 1.83 PFLOP/s of 1.88 that a plain matrix product reaches, the
+// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.51 ms, 1.16
+// PFLOP/s.  d = 64 step by step: 128-key tiles, one S 560 us, the maximum with
+// the load 528, 96-key tiles and two S 532, one slot for V and K 511, P at once
+// 509.  A loop of the softmax alone takes 1000 clocks for 96 keys of two warps a
+// scheduler (770 of them exponentials), this kernel about 1430.  Tried for
+// d = 64 and slower: two threads a row, no maximum but a check of the weights'
+// sum, the next scores read under the last weights, P in columns of its own,
+// key tiles of 64 with two or three S, four row tiles a CTA.
 //
 // Few blocks (a short chunk over a long cache) leave SMs idle: then a block's
 // keys are split into parts (prompt.cuh) that prompt.cu joins.
@@ -49,7 +60,6 @@ namespace gkv {
 namespace serve {
 namespace {
 
-constexpr int kN = kKeysTc;
 constexpr int kThreads = 384;                  // three warpgroups: two of softmax, one of TMA and MMA issue
 // Registers a thread after the split; 256 x 208 + 128 x 88 = 384 x 168, the launch's own.
 constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
@@ -60,14 +70,23 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 
 template <int D>
 struct Cfg {
+    static constexpr int NK = keys_tc(D);                      // keys of a tile
+    static constexpr int SB = D == 128 ? 1 : 2;                // score buffers of a row tile
+    static constexpr int SW = SB * NK;                         // TMEM columns of a row tile's scores
+    static_assert(2 * (SW + D) <= 512 && NK % 32 == 0, "TMEM columns");
     static constexpr int NB = D / 64;                          // 64-channel blocks of a row
     static constexpr uint32_t TILE = NB * 128 * 128;           // bytes of a 128-row tile
-    static constexpr int NST = (D == 128 ? 5 : 8);             // ring slots (K and V tiles in turn)
-    static constexpr size_t SMEM = 1024 + (2 + NST) * (size_t)TILE;
+    static constexpr uint32_t KT = NB * NK * 128;              // bytes of a key or value tile
+    static constexpr bool PAIR = D == 64;                      // a ring slot holds V(j) and K(j + SB), or one of them
+    static constexpr uint32_t SLOT = PAIR ? 2 * KT : KT;
+    static constexpr int NST = D == 128 ? 5 : 8;               // ring slots
+    static constexpr int HV = D == 128 ? 2 : 1;                // pieces in which P is handed over
+    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + NST * (size_t)SLOT;
 };
 
 struct Bars {
-    uint64_t full[8], empty[8], qfull, sfull[2], pfull[2][2], odone[2], vfix, fin;
+    uint64_t full[8], empty[8], qfull, sfull[2][2], pfull[2][2][2], vfix, fin;
+    uint64_t odone[2], oprev[2];       // the last PV of a row tile is in O; the last but one (two score buffers)
     uint32_t tbase;
     int abort, turn;           // turn: key tiles whose products row tile 0 has issued
 };
@@ -77,21 +96,23 @@ struct Tc {
     int kh, vh;                // head coordinate step of k, v (0: one head for all)
 };
 
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars &b, int *status) {
-    const uint32_t addr = tc::smem_u32(bar);
-    if (tc::mbar_try_wait(addr, parity)) return true;
-    const uint64_t t0 = tc::globaltimer_ns();
-    for (uint32_t it = 0;; it++) {
-        if (tc::mbar_try_wait(addr, parity)) return true;
-        if ((it & 63u) == 63u) {
+__device__ __forceinline__ bool wait(uint32_t addr, uint32_t parity, Bars &b, int *status) {
+    uint64_t t0 = 0;
+    for (uint32_t it = 1; !tc::mbar_try_wait(addr, parity); it++)
+        if (!(it & 63u)) {
+            const uint64_t t = tc::globaltimer_ns();
+            if (t0 == 0) t0 = t;
             if (*(volatile int *)&b.abort) return false;
-            if (tc::globaltimer_ns() - t0 > kWaitNs) {
+            if (t - t0 > kWaitNs) {
                 atomicOr(status, kStTimeout);
                 atomicExch(&b.abort, 1);
                 return false;
             }
         }
-    }
+    return true;
+}
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Bars &b, int *status) {
+    return wait(tc::smem_u32(bar), parity, b, status);
 }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -111,6 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     prompt_tc_kernel(const PromptArgs a, const Tc t, const __grid_constant__ CUtensorMap mapQ,
                      const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
     using C = Cfg<D>;
+    constexpr int NK = C::NK, SB = C::SB;
     extern __shared__ __align__(1024) unsigned char raw[];
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) &
                                                             ~static_cast<uintptr_t>(1023));
@@ -128,9 +150,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::mbar_init(tc::smem_u32(&b.vfix), 1);
         tc::mbar_init(tc::smem_u32(&b.fin), 2);
         for (int i = 0; i < 2; i++) {
-            tc::mbar_init(tc::smem_u32(&b.sfull[i]), 1);
-            for (int k = 0; k < 2; k++) tc::mbar_init(tc::smem_u32(&b.pfull[i][k]), 4);
+            for (int k = 0; k < 2; k++) {
+                tc::mbar_init(tc::smem_u32(&b.sfull[i][k]), 1);
+                for (int x = 0; x < 2; x++) tc::mbar_init(tc::smem_u32(&b.pfull[i][k][x]), 4);
+            }
             tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.oprev[i]), 1);
         }
         b.abort = 0;
         b.turn = 0;
@@ -161,8 +186,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // key tiles of each row tile, up to the last key its last token sees; of
     // them this part's: [j0, j0 + n)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
-    const int all0 = last0 >= 0 ? last0 / kN + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / kN + 1 : 0;
-    const int all = max(all0, all1), np = parts_of(all, a.split, kLeastTc);
+    const int all0 = last0 >= 0 ? last0 / NK + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / NK + 1 : 0;
+    const int all = max(all0, all1), np = parts_of(all, a.split, least_tc(D));
     const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
     const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
 
@@ -177,8 +202,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 
     // the sequence's last key tile is partial and other rows follow it: their V rows are zeroed
-    const int keep = nk - (j1 - 1) * kN;                  // keys of the sequence in the part's last tile, from it on
-    const bool fix = n > 0 && keep < kN && k0 + nk < a.n_k;
+    const int keep = nk - (j1 - 1) * NK;                  // keys of the sequence in the part's last tile, from it on
+    const bool fix = n > 0 && keep < NK && k0 + nk < a.n_k;
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
@@ -189,29 +214,32 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool live = tk < t.tpt && token < nq;
         const int lim = live ? token + off : -1;         // last key the row sees
         const float c = a.scale * kLog2e;
-        const uint32_t ts = tb + ((uint32_t)(q * 32) << 16) + (uint32_t)(i * kN), to = tb + ((uint32_t)(q * 32) << 16) + 2 * kN + i * D;
+        const uint32_t lanes = tb + ((uint32_t)(q * 32) << 16);
+        const uint32_t ts0 = lanes + (uint32_t)(i * C::SW), to = lanes + 2 * C::SW + i * D;
         // the first token of the tile sees the fewest keys: below its limit no mask is needed
         const int clear = t0 + i * t.tpt + off;
         float m = -INFINITY, z = 0.f;                    // m: the reference times c
         const int nj = i ? nkv1 : nkv0;
         bool ok = true;
         for (int j = 0; j < nj; j++) {
-            ok = __all_sync(0xffffffffu, wait(&b.sfull[i], j & 1, b, a.status));
+            const int sb = j % SB;
+            const uint32_t ts = ts0 + (uint32_t)(sb * NK);
+            ok = __all_sync(0xffffffffu, wait(&b.sfull[i][sb], (j / SB) & 1, b, a.status));
             if (!ok) break;
             tc::tc_fence_after();
-            uint32_t x[4][32];
-            float mx[4];
+            uint32_t x[NK / 32][32];
+            float mx[NK / 32];
 #pragma unroll
-            for (int k = 0; k < 4; k++) tc::tmem_ld32_max_async(ts + 32 * k, x[k], mx[k]);
+            for (int k = 0; k < NK / 32; k++) tc::tmem_ld32_max_async(ts + 32 * k, x[k], mx[k]);
             tc::tmem_wait_ld(x[0]);
 #pragma unroll
-            for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
+            for (int k = 1; k < NK / 32; k++) tc::tmem_loaded(x[k]);
 #pragma unroll
-            for (int k = 0; k < 4; k++) tc::tmem_loaded(mx[k]);
-            if ((j0 + j) * kN + kN - 1 > clear) {
-                const int rel = lim - (j0 + j) * kN;
+            for (int k = 0; k < NK / 32; k++) tc::tmem_loaded(mx[k]);
+            if ((j0 + j) * NK + NK - 1 > clear) {
+                const int rel = lim - (j0 + j) * NK;
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
+                for (int k = 0; k < NK / 32; k++) {
 #pragma unroll
                     for (int e = 0; e < 32; e++)
                         if (k * 32 + e > rel) x[k][e] = 0xff800000u;       // -inf
@@ -221,10 +249,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                         mx[k] = max3(mx[k], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
                 }
             }
-            const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+#pragma unroll
+            for (int k = 1; k < NK / 32; k++) mx[0] = fmaxf(mx[0], mx[k]);
+            const float mn = mx[0] * c;
             if (m == -INFINITY) m = mn;                  // nothing accumulated yet
             else if (__builtin_expect(mn > m + kLazy, 0)) z = -z;          // asks for a rescale (z > 0 marks none)
             if (__any_sync(0xffffffffu, z < 0.f)) {
+                // O is rescaled once PV(j - 1) is in it: with one score buffer S(j) came after it; with two
+                // S(j + 1) does, and at the last tile a commit of its own tells
+                if constexpr (SB == 2) {
+                    ok = __all_sync(0xffffffffu, j + 1 < nj ? wait(&b.sfull[i][(j + 1) & 1], ((j + 1) / 2) & 1, b, a.status)
+                                                            : wait(&b.oprev[i], 0, b, a.status));
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                }
                 float w = 1.f;
                 if (z < 0.f) {
                     w = tc::ex2(m - mn);
@@ -238,29 +276,34 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc::tmem_wait_ld(o);
 #pragma unroll
                     for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
-                    tc::tmem_st32(to + 32 * k, o);
+                    tc::tmem_st(to + 32 * k, o);
                 }
             }
             const float sh = m == -INFINITY ? 0.f : -m;
             const float2 c2 = make_float2(c, c), s2 = make_float2(sh, sh);
             float2 acc = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                uint32_t p[32];
-#pragma unroll
-                for (int e = 0; e < 32; e++) {
-                    const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * k + e / 16][(2 * e) & 31]),
-                                                            __uint_as_float(x[2 * k + e / 16][((2 * e) & 31) + 1])), c2, s2);
-                    const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
-                    acc = __fadd2_rn(acc, w);
-                    p[e] = pack2(w.x, w.y);
-                }
-                tc::tmem_st32(ts + 32 * k, p);
+            auto weights = [&](uint32_t &p, int at) {
+                const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[at / 32][at & 31]),
+                                                        __uint_as_float(x[at / 32][(at & 31) + 1])), c2, s2);
+                const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
+                acc = __fadd2_rn(acc, w);
+                p = pack2(w.x, w.y);
+            };
+            auto hand = [&](int k) {
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][k]));
-            }
+                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][sb][k]));
+            };
+            uint32_t p0[32], p1[(NK - 64) / 2];
+#pragma unroll
+            for (int e = 0; e < 32; e++) weights(p0[e], 2 * e);
+            tc::tmem_st(ts, p0);
+            if (C::HV == 2) hand(0);
+#pragma unroll
+            for (int e = 0; e < (NK - 64) / 2; e++) weights(p1[e], 64 + 2 * e);
+            tc::tmem_st(ts + 32, p1);
+            hand(C::HV - 1);
             z += acc.x + acc.y;
         }
         if (ok && nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status));
@@ -343,31 +386,47 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint32_t qb = tc::smem_u32(&b.qfull);
                 tc::mbar_expect_tx(qb, (uint32_t)(ntile * C::NB * t.tpt * t.gq * 128));
                 for (int i = 0; i < ntile; i++)
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < C::NB; c++)
                         tc::tma_load_3d(tc::smem_u32(Qs + i * C::TILE + c * 128 * 128), &mapQ, c * 64, g * t.gq,
                                         (int)(q0 + t0 + i * t.tpt), qb);
-                for (int i = 0; i < 2 * n; i++) {
-                    const int st = i % C::NST;
-                    ok = !*(volatile int *)&b.abort && wait(&b.empty[st], ((i / C::NST) & 1) ^ 1, b, a.status);
-                    if (!ok) break;
-                    const uint32_t fb = tc::smem_u32(&b.full[st]);
-                    tc::mbar_expect_tx(fb, C::TILE);
-    #pragma unroll
+                // keys SB tiles ahead of their values, as the products take them
+                auto copy = [&](const CUtensorMap *map, int head, int j, uint32_t at, uint32_t fb) {
+#pragma unroll
                     for (int c = 0; c < C::NB; c++)
-                        tc::tma_load_3d(tc::smem_u32(ring + st * C::TILE + c * 128 * 128), (i & 1) ? &mapV : &mapK, c * 64,
-                                        g * ((i & 1) ? t.vh : t.kh), (int)(k0 + (j0 + (i >> 1)) * kN), fb);
+                        tc::tma_load_3d(tc::smem_u32(ring + at + c * NK * 128), map, c * 64, head, (int)(k0 + (j0 + j) * NK), fb);
+                };
+                // a slot with V(jv), K(jk) or both; with neither (fewer key tiles than score buffers) it arrives empty
+                auto fill = [&](int jv, int jk) {
+                    const int st = issued % C::NST;
+                    ok = !*(volatile int *)&b.abort && wait(&b.empty[st], ((issued / C::NST) & 1) ^ 1, b, a.status);
+                    if (!ok) return;
+                    const bool v = jv >= 0, k = jk >= 0 && jk < n;
+                    const uint32_t fb = tc::smem_u32(&b.full[st]);
+                    if (v || k) tc::mbar_expect_tx(fb, (v + k) * C::KT);
+                    else tc::mbar_arrive(fb);
+                    if (v) copy(&mapV, g * t.vh, jv, st * C::SLOT, fb);
+                    if (k) copy(&mapK, g * t.kh, jk, st * C::SLOT + (C::PAIR ? C::KT : 0), fb);
                     issued++;
+                };
+                for (int j = -SB; ok && j < n; j++) {
+                    if (C::PAIR) {
+                        fill(j, j + SB);
+                    } else {
+                        if (j >= 0) fill(j, -1);
+                        if (ok && j + SB < n) fill(-1, j + SB);
+                    }
                 }
             }
             issued = __shfl_sync(0xffffffffu, issued, 0);
-            ok = issued == 2 * n && n > 0;
+            const int slots = C::PAIR ? n + SB : 2 * n;
+            ok = issued == slots && n > 0;
             if (fix && ok) {
-                const int st = (2 * n - 1) % C::NST;
-                if (wait(&b.full[st], ((2 * n - 1) / C::NST) & 1, b, a.status)) {
-                    for (int i = lane; i < (kN - keep) * C::NB * 8; i += 32) {
+                const int st = (slots - 1) % C::NST;
+                if (wait(&b.full[st], ((slots - 1) / C::NST) & 1, b, a.status)) {
+                    for (int i = lane; i < (NK - keep) * C::NB * 8; i += 32) {
                         const int r = keep + i / (C::NB * 8), c = i % (C::NB * 8);
-                        *reinterpret_cast<uint4 *>(ring + st * C::TILE + (c >> 3) * (128 * 128) + r * 128 + (c & 7) * 16) =
+                        *reinterpret_cast<uint4 *>(ring + st * C::SLOT + (c >> 3) * (NK * 128) + r * 128 + (c & 7) * 16) =
                             make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -384,78 +443,91 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else if (warp <= kWarpMma + 1) {
             // ---------------- MMA issue: one warp a row tile, one lane issues ----------------
             if (n > 0) {
-                constexpr uint32_t idS = tc::idesc_bf16_f32(128, kN), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
+                constexpr uint32_t idS = tc::idesc_bf16_f32(128, NK), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
                 const int i = warp - kWarpMma, ni = i ? nkv1 : nkv0;
                 // descriptors: the start address (16-byte units) is the low word's low end, the rest is constant
                 const uint32_t qd = ((tc::smem_u32(Qs) >> 4) | (1u << 16)) + i * (C::TILE >> 4);
-                const uint32_t kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
-                const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((128 * 128 >> 4) << 16);
-                const uint32_t ts = tb + i * kN, to = tb + 2 * kN + i * D;
+                const uint32_t kd = ((tc::smem_u32(ring) + (C::PAIR ? C::KT : 0)) >> 4) | (1u << 16);
+                const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((NK * 128 >> 4) << 16);
+                const uint32_t ts = tb + i * C::SW, to = tb + 2 * C::SW + i * D;
                 const bool one = tc::elect_one();
-                int st = 1;
+                int st = 0;
                 uint32_t ph = 0;                         // of the ring slot that comes next
-                bool ok = wait(&b.qfull, 0, b, a.status) && wait(&b.full[0], 0, b, a.status);
-                auto qk = [&](int slot) {                // S = Q K^T, K in the slot
-                    const uint32_t ka = kd + slot * (C::TILE >> 4);
+                bool ok = wait(&b.qfull, 0, b, a.status);
+                auto qk = [&](int slot, int sb) {        // S = Q K^T into score buffer sb, K in the slot
+                    const uint32_t ka = kd + slot * (C::SLOT >> 4);
 #pragma unroll
                     for (int c = 0; c < C::NB; c++)
 #pragma unroll
                         for (int x = 0; x < 4; x++)
-                            tc::mma_bf16_lo(ts, qd + c * (128 * 128 >> 4) + 2 * x, ka + c * (128 * 128 >> 4) + 2 * x, idS,
-                                            (c | x) != 0);
-                    tc::mma_commit(tc::smem_u32(&b.sfull[i]));
+                            tc::mma_bf16_lo(ts + sb * NK, qd + c * (128 * 128 >> 4) + 2 * x, ka + c * (NK * 128 >> 4) + 2 * x,
+                                            idS, (c | x) != 0);
+                    tc::mma_commit(tc::smem_u32(&b.sfull[i][sb]));
                 };
-                tc::tc_fence_after();
-                if (ok && one) {
-                    if (ni > 0) qk(0);
-                    tc::mma_commit(tc::smem_u32(&b.empty[0]));
+#pragma unroll
+                for (int s0 = 0; s0 < SB; s0++) {
+                    if (!C::PAIR && s0 >= n) break;
+                    ok = wait(&b.full[st], ph, b, a.status) && ok;
+                    tc::tc_fence_after();
+                    if (ok && one) {
+                        if (s0 < ni) qk(st, s0);
+                        tc::mma_commit(tc::smem_u32(&b.empty[st]));
+                    }
+                    st++;
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 // the row tiles may end at different key tiles: both warps release every slot, in order
-                for (int j = 0; ok && j < n; j++) {
-                    const int vs = st;
-                    const uint32_t vph = ph;
-                    if (++st == C::NST) { st = 0; ph ^= 1; }
-                    const int ks = st;
-                    const uint32_t kph = ph;
-                    const bool more = j + 1 < n;
-                    ok = wait(&b.full[vs], vph, b, a.status);
-                    if (more) {
-                        ok = ok && wait(&b.full[ks], kph, b, a.status);
+                const uint32_t bfull = tc::smem_u32(&b.full[0]), bempty = tc::smem_u32(&b.empty[0]);
+                const uint32_t bp = tc::smem_u32(&b.pfull[i][0][0]);
+                uint32_t pp = 0;                         // phase of the weights
+                for (int jb = 0; ok && jb < n; jb += SB, pp ^= 1) {
+#pragma unroll
+                    for (int sb = 0; sb < SB; sb++) {
+                        const int j = jb + sb;
+                        if (SB > 1 && j >= n) break;
+                        const int vs = st;
+                        ok = wait(bfull + 8 * vs, ph, b, a.status) && ok;
                         if (++st == C::NST) { st = 0; ph ^= 1; }
-                    } else if (fix) {
-                        ok = ok && wait(&b.vfix, 0, b, a.status);
-                    }
-                    // Tile 1 goes after tile 0.  Products of the two issued at once would run interleaved, end
-                    // together and leave the tensor pipe idle while both tiles are in their softmax (d = 128,
-                    // 16K tokens: 1250 us in turn, 1370 without; d = 64, where the softmax is the longer side,
-                    // the same either way).  An order, not a dependence: the wait may run out.
-                    if (i == 1)
-                        for (int w = 0; w < 20000 && *(volatile int *)&b.turn <= j; w++) {}
-                    if (j < ni) {
-                        const uint32_t va = vd + vs * (C::TILE >> 4);
+                        int ks = vs;
+                        const bool more = !C::PAIR && j + SB < n;
+                        if (more) {
+                            ks = st;
+                            ok = wait(bfull + 8 * ks, ph, b, a.status) && ok;
+                            if (++st == C::NST) { st = 0; ph ^= 1; }
+                        }
+                        if (fix && j + 1 == n) ok = wait(&b.vfix, 0, b, a.status) && ok;
+                        // d = 128: tile 1 goes after tile 0.  Products of the two issued at once would run
+                        // interleaved, end together and leave the tensor pipe idle while both tiles are in
+                        // their softmax (16K tokens: 1250 us in turn, 1370 without).  At d = 64, where the
+                        // softmax is the longer side, a turn only delays.  An order, not a dependence: the
+                        // wait may run out.
+                        if (D == 128 && i == 1)
+                            for (int w = 0; w < 20000 && *(volatile int *)&b.turn <= j; w++) {}
+                        if (j < ni) {
+                            const uint32_t va = vd + vs * (C::SLOT >> 4);
 #pragma unroll
-                        for (int k = 0; k < 2; k++) {            // the weights come in two halves
-                            ok = ok && wait(&b.pfull[i][k], j & 1, b, a.status);
-                            tc::tc_fence_after();
-                            if (ok && one) {
+                            for (int k = 0; k < C::HV; k++) {        // the weights come in pieces
+                                ok = wait(bp + 8 * (2 * sb + k), pp, b, a.status) && ok;
+                                tc::tc_fence_after();
+                                if (one) {
 #pragma unroll
-                                for (int x = k * (kN / 32); x < (k + 1) * (kN / 32); x++)
-                                    tc::mma_bf16_ts_lo(to, ts + x * 8, va + x * (16 * 128 >> 4), idO, (j | x) != 0);
+                                    for (int x = k * 4; x < (k == C::HV - 1 ? NK / 16 : 4); x++)
+                                        tc::mma_bf16_ts_lo(to, ts + sb * NK + x * 8, va + x * (16 * 128 >> 4), idO, (j | x) != 0);
+                                    if (k == C::HV - 1) {
+                                        if (j + SB < ni) qk(ks, sb);
+                                        else tc::mma_commit(tc::smem_u32(j + 1 == ni ? &b.odone[i] : &b.oprev[i]));
+                                    }
+                                }
                             }
                         }
-                        if (ok && one) {
-                            if (j + 1 < ni) qk(ks);
-                            else tc::mma_commit(tc::smem_u32(&b.odone[i]));
+                        if (D == 128 && i == 0 && one) *(volatile int *)&b.turn = j + 1;
+                        if (one) {
+                            tc::mma_commit(bempty + 8 * vs);
+                            if (more) tc::mma_commit(bempty + 8 * ks);
                         }
                     }
-                    if (i == 0 && one) *(volatile int *)&b.turn = j + 1;
-                    if (ok && one) {
-                        tc::mma_commit(tc::smem_u32(&b.empty[vs]));
-                        if (more) tc::mma_commit(tc::smem_u32(&b.empty[ks]));
-                    }
-                    ok = __all_sync(0xffffffffu, ok);
                 }
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok && lane == 0) {
                     atomicOr(a.status, kStTimeout);
                     atomicExch(&b.abort, 1);
@@ -502,8 +574,8 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
     if (!make_map(&mq, a.q, a.n_q, a.Hq, D, a.q_ts, a.q_hs, t.gq, t.tpt)) return cudaErrorNotSupported;
     if (a.n_k == 0) {
         mk = mv = mq;
-    } else if (!make_map(&mk, a.k, a.n_k, t.kh ? a.G : 1, D, a.k_ts, a.k_hs, 1, kN) ||
-               !make_map(&mv, a.v, a.n_k, t.vh ? a.G : 1, D, a.v_ts, a.v_hs, 1, kN)) {
+    } else if (!make_map(&mk, a.k, a.n_k, t.kh ? a.G : 1, D, a.k_ts, a.k_hs, 1, Cfg<D>::NK) ||
+               !make_map(&mv, a.v, a.n_k, t.vh ? a.G : 1, D, a.v_ts, a.v_hs, 1, Cfg<D>::NK)) {
         return cudaErrorNotSupported;
     }
     const int64_t blocks = prompt_slots(a.n_q, a.n_seqs, 2 * t.tpt) * a.G;
@@ -523,7 +595,7 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
         ready[dev].store(1, std::memory_order_relaxed);
     }
     // fewer blocks than SMs: their keys are split over the others
-    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + kN - 1) / kN / kLeastTc));
+    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + Cfg<D>::NK - 1) / Cfg<D>::NK / least_tc(D)));
     e = launch_overlapped(prompt_tc_kernel<D>, dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s, a, t, mq,
                           mk, mv);
     return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, GKV_BF16, true, s) : e;

@@ -157,6 +157,20 @@ def test_large_logits(gk, dtype):
     check(gk, -q.abs(), k.abs(), v, cu([n]), cu([n]))     # all of them far below 0
 
 
+@pytest.mark.parametrize("fall", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [95, 96, 97, 128, 129, 192, 193, 288, 300, 577])
+def test_logits_that_rise_or_fall_along_the_keys(gk, n, d, fall):
+    """Every key tile raises the rows' maxima by far more than the one before
+    left (or none does after the first), the last tile of a row too."""
+    q, k, v = inputs(23, n, n, 8, 2, d, torch.float32, sharp=1.0)
+    u = torch.ones(d)
+    q, k = q * 0.1 + u, k * 0.1
+    t = torch.arange(n).flip(0) if fall else torch.arange(n)
+    k = k + (0.15 * t / math.sqrt(d))[:, None, None] * u            # 0.15 a key in the scaled product
+    check(gk, q.to(BF), k.to(BF), v.to(BF), cu([n]), cu([n]))
+
+
 def test_results_do_not_depend_on_timing(gk):
     lens = [513, 100, 1, 900]
     n = sum(lens)
