@@ -28,13 +28,17 @@ struct PromptArgs {
     int split;                     // most parts of a block's keys (set by the launchers)
 };
 
-// The rows of sequence s; false when its cu words do not fit.
-__device__ __forceinline__ bool seq_bounds(const PromptArgs &a, int s, int64_t &q0, int64_t &nq, int64_t &k0, int64_t &nk) {
-    q0 = a.cu_q[s];
-    nq = a.cu_q[s + 1] - q0;
-    k0 = a.cu_k[s];
-    nk = a.cu_k[s + 1] - k0;
+// The rows of a sequence from its cu words; false when they do not fit.
+__device__ __forceinline__ bool bounds_fit(const PromptArgs &a, int cq0, int cq1, int ck0, int ck1, int64_t &q0, int64_t &nq,
+                                           int64_t &k0, int64_t &nk) {
+    q0 = cq0;
+    nq = (int64_t)cq1 - q0;
+    k0 = ck0;
+    nk = (int64_t)ck1 - k0;
     return q0 >= 0 && nq >= 0 && q0 + nq <= a.n_q && k0 >= 0 && nk >= 0 && k0 + nk <= a.n_k;
+}
+__device__ __forceinline__ bool seq_bounds(const PromptArgs &a, int s, int64_t &q0, int64_t &nq, int64_t &k0, int64_t &nk) {
+    return bounds_fit(a, a.cu_q[s], a.cu_q[s + 1], a.cu_k[s], a.cu_k[s + 1], q0, nq, k0, nk);
 }
 
 // Work slots of `tok` queries: sequence s owns the slots from cu_q[s] / tok + s
@@ -68,6 +72,10 @@ __host__ __device__ constexpr int least_tc(int d) { return 512 / keys_tc(d); }
 __host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
     const int most = n / least;
     return most < 1 ? 1 : most < split ? most : split;
+}
+// The first key tile of part p of np: p <= np <= 152 (kPartsTc), and n < 2^31 / 96 key tiles: the product fits 32 bits.
+__device__ __forceinline__ int part_first(int n, int np, unsigned p) {
+    return (int)(np == 1 ? p * (unsigned)n : p * (unsigned)n / (unsigned)np);
 }
 // Floats of a part: 4-channel groups of the sums (by row or by group), then the
 // rows' maxima (base 2) and weight sums.

@@ -85,7 +85,7 @@ struct Cfg {
 };
 
 struct Bars {
-    uint64_t full[8], empty[8], qfull, sfull[2][2], pfull[2][2][2], vfix, fin;
+    uint64_t full[8], empty[8], qfull[2], sfull[2][2], pfull[2][2][2], vfix, fin;
     uint64_t odone[2], oprev[2];       // the last PV of a row tile is in O; the last but one (two score buffers)
     uint32_t tbase;
     int abort, turn;           // turn: key tiles whose products row tile 0 has issued
@@ -94,6 +94,7 @@ struct Bars {
 struct Tc {
     int gq, tpt;               // heads of a KV head, tokens of a row tile
     int kh, vh;                // head coordinate step of k, v (0: one head for all)
+    int slots;                 // of prompt_slots
 };
 
 __device__ __forceinline__ bool wait(uint32_t addr, uint32_t parity, Bars &b, int *status) {
@@ -141,15 +142,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     next_may_start();
-    if (threadIdx.x == 0) {
+    if (warp == kWarpTma && lane == 0) {                 // the thread that uses them first
         for (int i = 0; i < C::NST; i++) {
             tc::mbar_init(tc::smem_u32(&b.full[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.empty[i]), 2);
         }
-        tc::mbar_init(tc::smem_u32(&b.qfull), 1);
-        tc::mbar_init(tc::smem_u32(&b.vfix), 1);
-        tc::mbar_init(tc::smem_u32(&b.fin), 2);
         for (int i = 0; i < 2; i++) {
+            tc::mbar_init(tc::smem_u32(&b.qfull[i]), 1);
             for (int k = 0; k < 2; k++) {
                 tc::mbar_init(tc::smem_u32(&b.sfull[i][k]), 1);
                 for (int x = 0; x < 2; x++) tc::mbar_init(tc::smem_u32(&b.pfull[i][k][x]), 4);
@@ -157,29 +156,36 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.oprev[i]), 1);
         }
+        tc::mbar_init(tc::smem_u32(&b.vfix), 1);
+        tc::mbar_init(tc::smem_u32(&b.fin), 2);
         b.abort = 0;
         b.turn = 0;
         tc::fence_barrier_init();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == kWarpMma) {
         tc::tmem_alloc(tc::smem_u32(&b.tbase), 512);
         tc::tmem_relinquish();
-    }
-    if (warp == kWarpTma && lane == 0) {
-        tc::tma_prefetch_desc(&mapQ);
-        tc::tma_prefetch_desc(&mapK);
-        tc::tma_prefetch_desc(&mapV);
     }
     after_previous();
     if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
     // ---- the CTA's rows: heavy blocks (late tokens) first
     const int g = blockIdx.x % a.G;
     const int tok = 2 * t.tpt;
-    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
-    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    const int slot = t.slots - 1 - (int)(blockIdx.x / a.G);
     int64_t q0, nq64, k0, nk64;
-    const bool fits = seq_bounds(a, s, q0, nq64, k0, nk64);
-    const int64_t t0_64 = (slot - (q0 / tok + s)) * tok;
+    int s;
+    bool fits;
+    if (a.n_seqs < 32) {                                 // a lane a bound: one round of loads instead of a search
+        const int cq = lane <= a.n_seqs ? a.cu_q[lane] : 0, ck = lane <= a.n_seqs ? a.cu_k[lane] : 0;
+        s = max(0, __popc(__ballot_sync(0xffffffffu, lane < a.n_seqs && cq / tok + lane <= slot)) - 1);
+        fits = bounds_fit(a, __shfl_sync(0xffffffffu, cq, s), __shfl_sync(0xffffffffu, cq, s + 1),
+                          __shfl_sync(0xffffffffu, ck, s), __shfl_sync(0xffffffffu, ck, s + 1), q0, nq64, k0, nk64);
+    } else {
+        s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+        fits = seq_bounds(a, s, q0, nq64, k0, nk64);
+    }
+    const int64_t t0_64 = ((int64_t)slot - ((int)q0 / tok + s)) * tok;
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
     const int off = nk - nq;                             // query i sees keys <= i + off
     const int ntile = t0 + t.tpt < nq ? 2 : 1;
@@ -188,15 +194,45 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
     const int all0 = last0 >= 0 ? last0 / NK + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / NK + 1 : 0;
     const int all = max(all0, all1), np = parts_of(all, a.split, least_tc(D));
-    const int j0 = (int)((int64_t)blockIdx.y * all / np), j1 = (int)((int64_t)(blockIdx.y + 1) * all / np), n = j1 - j0;
+    const int j0 = part_first(all, np, blockIdx.y), j1 = part_first(all, np, blockIdx.y + 1), n = j1 - j0;
     const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
+
+    // nothing to do: a sequence that does not fit, a slot past its tokens, a part beyond the block's
+    const bool idle = !fits || t0_64 < 0 || t0_64 >= nq64 || (int)blockIdx.y >= np;
+
+    // ---- copies, by the producer's thread: the first ones leave before the block meets
+    auto copy = [&](const CUtensorMap *map, int head, int j, uint32_t at, uint32_t fb) {
+#pragma unroll
+        for (int c = 0; c < C::NB; c++)
+            tc::tma_load_3d(tc::smem_u32(ring + at + c * NK * 128), map, c * 64, head, (int)(k0 + (j0 + j) * NK), fb);
+    };
+    // a slot with V(jv), K(jk) or both; with neither (fewer key tiles than score buffers) it arrives empty
+    auto fill = [&](int st, int jv, int jk) {
+        const bool v = jv >= 0, k = jk >= 0 && jk < n;
+        const uint32_t fb = tc::smem_u32(&b.full[st]);
+        if (v || k) tc::mbar_expect_tx(fb, (v + k) * C::KT);
+        else tc::mbar_arrive(fb);
+        if (v) copy(&mapV, g * t.vh, jv, st * C::SLOT, fb);
+        if (k) copy(&mapK, g * t.kh, jk, st * C::SLOT + (C::PAIR ? C::KT : 0), fb);
+    };
+    if (warp == kWarpTma && lane == 0 && !idle && n > 0) {
+        for (int i = 0; i < ntile; i++) {
+            const uint32_t qb = tc::smem_u32(&b.qfull[i]);
+            tc::mbar_expect_tx(qb, (uint32_t)(C::NB * t.tpt * t.gq * 128));
+#pragma unroll
+            for (int c = 0; c < C::NB; c++)
+                tc::tma_load_3d(tc::smem_u32(Qs + i * C::TILE + c * 128 * 128), &mapQ, c * 64, g * t.gq,
+                                (int)(q0 + t0 + i * t.tpt), qb);
+            if (i == 0)
+                for (int k = 0; k < SB; k++) fill(k, -1, k);
+        }
+    }
 
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tb = b.tbase;
-    // nothing to do: a sequence that does not fit, a slot past its tokens, a part beyond the block's
-    if (!fits || t0_64 < 0 || t0_64 >= nq64 || (int)blockIdx.y >= np) {
+    if (idle) {
         if (warp == kWarpMma) tc::tmem_dealloc(tb, 512);
         return;
     }
@@ -318,37 +354,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                 constexpr int CH = D / 8;                    // chunks of a row
                 const float inv = z > 0.f ? 1.f / z : z;     // no key: 0; a NaN stays
                 const int64_t at = live ? row * a.o_ts + hq * a.o_hs : -1;
-                unsigned char *stage = Qs + i * C::TILE + q * 32 * (D * 2);
-#pragma unroll
-                for (int k = 0; k < D / 32; k++) {
-                    uint32_t u[32];
-                    if (nj > 0) {
-                        tc::tmem_ld32_async(to + 32 * k, u);
-                        tc::tmem_wait_ld(u);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (lim >= 0) {
-                            v.x = pack2(__uint_as_float(u[e]) * inv, __uint_as_float(u[e + 1]) * inv);
-                            v.y = pack2(__uint_as_float(u[e + 2]) * inv, __uint_as_float(u[e + 3]) * inv);
-                            v.z = pack2(__uint_as_float(u[e + 4]) * inv, __uint_as_float(u[e + 5]) * inv);
-                            v.w = pack2(__uint_as_float(u[e + 6]) * inv, __uint_as_float(u[e + 7]) * inv);
-                        }
-                        const int ch = k * 4 + e / 8;
-                        if (nj > 0) *reinterpret_cast<uint4 *>(stage + lane * (D * 2) + ((ch ^ lane) & (CH - 1)) * 16) = v;
-                        else if (live) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at + ch * 8) = v;
-                    }
-                }
+                uint4 v[CH];
                 if (nj > 0) {
+                    unsigned char *stage = Qs + i * C::TILE + q * 32 * (D * 2);
+                    uint32_t u[D / 32][32];
+#pragma unroll
+                    for (int k = 0; k < D / 32; k++) tc::tmem_ld32_async(to + 32 * k, u[k]);
+                    tc::tmem_wait_ld(u[0]);
+#pragma unroll
+                    for (int k = 1; k < D / 32; k++) tc::tmem_loaded(u[k]);
+#pragma unroll
+                    for (int ch = 0; ch < CH; ch++) {
+                        const uint32_t *w = &u[ch / 4][ch % 4 * 8];
+                        uint4 y = make_uint4(0, 0, 0, 0);
+                        if (lim >= 0) {
+                            y.x = pack2(__uint_as_float(w[0]) * inv, __uint_as_float(w[1]) * inv);
+                            y.y = pack2(__uint_as_float(w[2]) * inv, __uint_as_float(w[3]) * inv);
+                            y.z = pack2(__uint_as_float(w[4]) * inv, __uint_as_float(w[5]) * inv);
+                            y.w = pack2(__uint_as_float(w[6]) * inv, __uint_as_float(w[7]) * inv);
+                        }
+                        *reinterpret_cast<uint4 *>(stage + lane * (D * 2) + ((ch ^ lane) & (CH - 1)) * 16) = y;
+                    }
                     __syncwarp();
-#pragma unroll 4
+                    // all loads, then all stores: in turns every load would wait for the store before it
+#pragma unroll
                     for (int x = 0; x < CH; x++) {
                         const int rr = x * (32 / CH) + lane / CH, ch = lane % CH;
-                        const int64_t to_row = __shfl_sync(0xffffffffu, at, rr);
-                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + rr * (D * 2) + ((ch ^ rr) & (CH - 1)) * 16);
-                        if (to_row >= 0) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + to_row + ch * 8) = v;
+                        v[x] = *reinterpret_cast<const uint4 *>(stage + rr * (D * 2) + ((ch ^ rr) & (CH - 1)) * 16);
                     }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < CH; x++) v[x] = make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int x = 0; x < CH; x++) {
+                    const int64_t to_row = __shfl_sync(0xffffffffu, at, x * (32 / CH) + lane / CH);
+                    if (to_row >= 0) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + to_row + lane % CH * 8) = v[x];
                 }
                 if (live && a.lse) a.lse[row * a.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
             }
@@ -380,41 +421,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
         if (warp == kWarpTma) {
             // ---------------- producer ----------------
-            int issued = 0;
+            // keys SB tiles ahead of their values, as the products take them; the first SB key tiles are on their way
+            int issued = n > 0 ? (C::PAIR ? SB : min(SB, n)) : 0;
             bool ok = n > 0;
-            if (lane == 0 && ok) {
-                const uint32_t qb = tc::smem_u32(&b.qfull);
-                tc::mbar_expect_tx(qb, (uint32_t)(ntile * C::NB * t.tpt * t.gq * 128));
-                for (int i = 0; i < ntile; i++)
-#pragma unroll
-                    for (int c = 0; c < C::NB; c++)
-                        tc::tma_load_3d(tc::smem_u32(Qs + i * C::TILE + c * 128 * 128), &mapQ, c * 64, g * t.gq,
-                                        (int)(q0 + t0 + i * t.tpt), qb);
-                // keys SB tiles ahead of their values, as the products take them
-                auto copy = [&](const CUtensorMap *map, int head, int j, uint32_t at, uint32_t fb) {
-#pragma unroll
-                    for (int c = 0; c < C::NB; c++)
-                        tc::tma_load_3d(tc::smem_u32(ring + at + c * NK * 128), map, c * 64, head, (int)(k0 + (j0 + j) * NK), fb);
-                };
-                // a slot with V(jv), K(jk) or both; with neither (fewer key tiles than score buffers) it arrives empty
-                auto fill = [&](int jv, int jk) {
+            if (lane == 0) {
+                auto next = [&](int jv, int jk) {
                     const int st = issued % C::NST;
                     ok = !*(volatile int *)&b.abort && wait(&b.empty[st], ((issued / C::NST) & 1) ^ 1, b, a.status);
                     if (!ok) return;
-                    const bool v = jv >= 0, k = jk >= 0 && jk < n;
-                    const uint32_t fb = tc::smem_u32(&b.full[st]);
-                    if (v || k) tc::mbar_expect_tx(fb, (v + k) * C::KT);
-                    else tc::mbar_arrive(fb);
-                    if (v) copy(&mapV, g * t.vh, jv, st * C::SLOT, fb);
-                    if (k) copy(&mapK, g * t.kh, jk, st * C::SLOT + (C::PAIR ? C::KT : 0), fb);
+                    fill(st, jv, jk);
                     issued++;
                 };
-                for (int j = -SB; ok && j < n; j++) {
+                for (int j = 0; ok && j < n; j++) {
                     if (C::PAIR) {
-                        fill(j, j + SB);
+                        next(j, j + SB);
                     } else {
-                        if (j >= 0) fill(j, -1);
-                        if (ok && j + SB < n) fill(-1, j + SB);
+                        next(j, -1);
+                        if (ok && j + SB < n) next(-1, j + SB);
                     }
                 }
             }
@@ -438,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0 && n > 0) {
                 for (int i = max(0, issued - C::NST); i < issued; i++)
                     tc::mbar_wait(tc::smem_u32(&b.full[i % C::NST]), (i / C::NST) & 1, kWaitNs);
-                tc::mbar_wait(tc::smem_u32(&b.qfull), 0, kWaitNs);
+                for (int i = 0; i < ntile; i++) tc::mbar_wait(tc::smem_u32(&b.qfull[i]), 0, kWaitNs);
             }
         } else if (warp <= kWarpMma + 1) {
             // ---------------- MMA issue: one warp a row tile, one lane issues ----------------
@@ -453,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool one = tc::elect_one();
                 int st = 0;
                 uint32_t ph = 0;                         // of the ring slot that comes next
-                bool ok = wait(&b.qfull, 0, b, a.status);
+                bool ok = i >= ntile || wait(&b.qfull[i], 0, b, a.status);
                 auto qk = [&](int slot, int sb) {        // S = Q K^T into score buffer sb, K in the slot
                     const uint32_t ka = kd + slot * (C::SLOT >> 4);
 #pragma unroll
@@ -578,8 +601,9 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
                !make_map(&mv, a.v, a.n_k, t.vh ? a.G : 1, D, a.v_ts, a.v_hs, 1, Cfg<D>::NK)) {
         return cudaErrorNotSupported;
     }
-    const int64_t blocks = prompt_slots(a.n_q, a.n_seqs, 2 * t.tpt) * a.G;
+    const int64_t slots = prompt_slots(a.n_q, a.n_seqs, 2 * t.tpt), blocks = slots * a.G;
     if (blocks >= (1LL << 31)) return cudaErrorNotSupported;
+    t.slots = (int)slots;
     static std::atomic<int> ready[kMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
