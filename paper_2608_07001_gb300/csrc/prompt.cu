@@ -37,11 +37,11 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
     after_previous();
     const int gq = a.Hq / a.G, half = TC ? kRowsTc / 2 : kRowsF32, tpt = half / gq, tok = TC ? 2 * tpt : tpt;
     const int g = blockIdx.x % a.G;
-    const int64_t slot = prompt_slots(a.n_q, a.n_seqs, tok) - 1 - blockIdx.x / a.G;
-    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    const int slot = (int)prompt_slots(a.n_q, a.n_seqs, tok) - 1 - (int)(blockIdx.x / a.G);
+    int s;
     int64_t q0, nq, k0, nk;
-    if (!seq_bounds(a, s, q0, nq, k0, nk)) return;
-    const int64_t t0 = (slot - (q0 / tok + s)) * tok;
+    if (!slot_rows(a, slot, tok, s, q0, nq, k0, nk)) return;
+    const int64_t t0 = ((int64_t)slot - ((int)q0 / tok + s)) * tok;
     if (t0 < 0 || t0 >= nq) return;
     const int last = (int)((nq < t0 + tok ? nq : t0 + tok) - 1 + nk - nq);
     const int np = parts_of(last >= 0 ? last / KEYS + 1 : 0, a.split, LEAST);

@@ -46,14 +46,27 @@ __device__ __forceinline__ bool seq_bounds(const PromptArgs &a, int s, int64_t &
 // floors of two bounds nq apart differ by at least floor(nq / tok), and one
 // more slot a sequence is left), so n_q / tok + n_seqs slots cover every
 // packing without a pass over the lengths.
-__host__ __device__ __forceinline__ int64_t prompt_slots(int64_t n_q, int n_seqs, int tok) { return n_q / tok + n_seqs; }
-__device__ __forceinline__ int slot_seq(const int32_t *cu, int n, int64_t slot, int tok) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cu[mid] / tok + mid <= slot) lo = mid; else hi = mid;
+// 32-bit arithmetic: row counts are below 2^31, and the launchers keep the slots there too.
+__host__ __device__ __forceinline__ int64_t prompt_slots(int64_t n_q, int n_seqs, int tok) {
+    return (int64_t)((uint32_t)n_q / (uint32_t)tok) + n_seqs;
+}
+// The sequence of a slot and its rows; false when its cu words do not fit.  Whole warps call it.
+__device__ __forceinline__ bool slot_rows(const PromptArgs &a, int slot, int tok, int &s, int64_t &q0, int64_t &nq, int64_t &k0,
+                                          int64_t &nk) {
+    if (a.n_seqs < 32) {                                 // a lane a bound: one round of loads instead of a search
+        const int lane = threadIdx.x & 31;
+        const int cq = lane <= a.n_seqs ? a.cu_q[lane] : 0, ck = lane <= a.n_seqs ? a.cu_k[lane] : 0;
+        s = max(0, __popc(__ballot_sync(0xffffffffu, lane < a.n_seqs && cq / tok + lane <= slot)) - 1);
+        return bounds_fit(a, __shfl_sync(0xffffffffu, cq, s), __shfl_sync(0xffffffffu, cq, s + 1),
+                          __shfl_sync(0xffffffffu, ck, s), __shfl_sync(0xffffffffu, ck, s + 1), q0, nq, k0, nk);
     }
-    return lo;
+    int hi = a.n_seqs;
+    s = 0;
+    while (hi - s > 1) {
+        const int mid = (s + hi) >> 1;
+        if (a.cu_q[mid] / tok + mid <= slot) s = mid; else hi = mid;
+    }
+    return bounds_fit(a, a.cu_q[s], a.cu_q[s + 1], a.cu_k[s], a.cu_k[s + 1], q0, nq, k0, nk);
 }
 
 // Flags the sequences whose cu words do not fit (one block of a launch calls it).
@@ -73,10 +86,8 @@ __host__ __device__ __forceinline__ int parts_of(int n, int split, int least) {
     const int most = n / least;
     return most < 1 ? 1 : most < split ? most : split;
 }
-// The first key tile of part p of np: p <= np <= 152 (kPartsTc), and n < 2^31 / 96 key tiles: the product fits 32 bits.
-__device__ __forceinline__ int part_first(int n, int np, unsigned p) {
-    return (int)(np == 1 ? p * (unsigned)n : p * (unsigned)n / (unsigned)np);
-}
+// The first key tile of part p of np, floor(p n / np) in 32 bits (p <= np <= kPartsF32).
+__device__ __forceinline__ int part_first(int n, int np, int p) { return p * (n / np) + p * (n % np) / np; }
 // Floats of a part: 4-channel groups of the sums (by row or by group), then the
 // rows' maxima (base 2) and weight sums.
 __host__ __device__ constexpr size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }

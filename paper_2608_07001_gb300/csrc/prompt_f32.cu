@@ -66,18 +66,18 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
 
     // ---- the block: rows of one KV head, heavy blocks (late tokens) first
     const int gq = a.Hq / a.G, tok = kR / gq, g = blockIdx.x % a.G;
-    const int64_t slots = prompt_slots(a.n_q, a.n_seqs, tok), slot = slots - 1 - blockIdx.x / a.G;
-    const int s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
+    const int slot = (int)prompt_slots(a.n_q, a.n_seqs, tok) - 1 - (int)(blockIdx.x / a.G);
+    int s;
     int64_t q0, nq64, k0, nk64;
-    if (!seq_bounds(a, s, q0, nq64, k0, nk64)) return;
-    const int64_t t0_64 = (slot - (q0 / tok + s)) * tok;
+    if (!slot_rows(a, slot, tok, s, q0, nq64, k0, nk64)) return;
+    const int64_t t0_64 = ((int64_t)slot - ((int)q0 / tok + s)) * tok;
     if (t0_64 < 0 || t0_64 >= nq64) return;
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64, off = nk - nq;
     const int last = min(nq, t0 + tok) - 1 + off;
     const int n = last >= 0 ? last / kK + 1 : 0;
     const int np = parts_of(n, a.split, kLeastF32);
     if ((int)blockIdx.y >= np) return;
-    const int j0 = (int)((int64_t)blockIdx.y * n / np), j1 = (int)((int64_t)(blockIdx.y + 1) * n / np);
+    const int j0 = part_first(n, np, blockIdx.y), j1 = part_first(n, np, blockIdx.y + 1);
 
     const T *K = static_cast<const T *>(a.k) + k0 * a.k_ts + g * a.k_hs;
     const T *V = static_cast<const T *>(a.v) + k0 * a.v_ts + g * a.v_hs;

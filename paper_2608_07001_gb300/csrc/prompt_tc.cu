@@ -175,16 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int slot = t.slots - 1 - (int)(blockIdx.x / a.G);
     int64_t q0, nq64, k0, nk64;
     int s;
-    bool fits;
-    if (a.n_seqs < 32) {                                 // a lane a bound: one round of loads instead of a search
-        const int cq = lane <= a.n_seqs ? a.cu_q[lane] : 0, ck = lane <= a.n_seqs ? a.cu_k[lane] : 0;
-        s = max(0, __popc(__ballot_sync(0xffffffffu, lane < a.n_seqs && cq / tok + lane <= slot)) - 1);
-        fits = bounds_fit(a, __shfl_sync(0xffffffffu, cq, s), __shfl_sync(0xffffffffu, cq, s + 1),
-                          __shfl_sync(0xffffffffu, ck, s), __shfl_sync(0xffffffffu, ck, s + 1), q0, nq64, k0, nk64);
-    } else {
-        s = slot_seq(a.cu_q, a.n_seqs, slot, tok);
-        fits = seq_bounds(a, s, q0, nq64, k0, nk64);
-    }
+    const bool fits = slot_rows(a, slot, tok, s, q0, nq64, k0, nk64);
     const int64_t t0_64 = ((int64_t)slot - ((int)q0 / tok + s)) * tok;
     const int nq = (int)nq64, nk = (int)nk64, t0 = (int)t0_64;
     const int off = nk - nq;                             // query i sees keys <= i + off
