@@ -11,8 +11,10 @@
 // a shared-memory read feeds 8 (S) and 10 (PV) FMAs; packed fp32x2 FMA halves
 // the issue slots, along the channels for S and across output columns for PV.
 // K of the next tile arrives (cp.async) under PV, V under S.  Two blocks a SM.
-// Measured: 50 TFLOP/s (32 / 8 heads of 128 at 4500 tokens; FMA pipe 67 % busy),
-// 25 us for 1024 tokens of 2 heads.  256 threads of 4 x 4 scores: 44 TFLOP/s.
+// Measured: 52 TFLOP/s (32 / 8 heads of 128 at 4500 tokens; FMA pipe 67 % busy),
+// 48 at d = 64 (46 with the products unrolled by 2 instead of 8), 26 us for 1024
+// tokens of 2 heads: 13 us of a part's one tile, of which 3 issue its copies, 6
+// of the join, the rest launches.  256 threads of 4 x 4 scores: 44 TFLOP/s.
 //
 // When a launch has fewer blocks than the GPU holds, a block's keys are split
 // into parts (prompt.cuh) that prompt.cu joins.
@@ -96,13 +98,19 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         copy_commit();
     };
     if (n > 0) {
-        for (int i = tid; i < kR * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), c = i % (D / 4), t = t0 + r / gq;
-            const bool on = r / gq < tok && t < nq;
-            load4(Qs + r * D + c * 4,
-                  static_cast<const T *>(a.q) + (q0 + (on ? t : t0)) * a.q_ts + (g * gq + r % gq) * a.q_hs + c * 4, on);
-        }
         load_k(j0);
+        // a warp loads RW rows a step, N steps of STEP rows: each lane finds the offset of one of them
+        constexpr int RW = 32 / (D / 4), STEP = kThreads / (D / 4), N = kR / STEP;
+        const int lane = tid & 31, first = tid / 32 * RW, c = tid % (D / 4), rw = lane / (D / 4);
+        const int mine = first + lane / N + lane % N * STEP, tk = mine / gq;
+        const bool on = tk < tok && t0 + tk < nq;
+        const int64_t at = on ? (q0 + t0 + tk) * a.q_ts + (g * gq + mine - tk * gq) * a.q_hs : -1;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int64_t from = __shfl_sync(0xffffffffu, at, rw * N + i);
+            load4(Qs + (first + rw + i * STEP) * D + c * 4, static_cast<const T *>(a.q) + (from < 0 ? 0 : from) + c * 4, from >= 0);
+        }
+        copy_commit();
     }
 
     float2 o[8][D / 32];
@@ -128,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         for (int i = 0; i < 8; i++)
 #pragma unroll
             for (int c = 0; c < 4; c++) x[i][c] = make_float2(0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 8
         for (int e = 0; e < D; e += 4) {
             float4 kf[4];
 #pragma unroll
@@ -169,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_f32_kernel(const PromptArg
         if (j + 1 < j1) load_k(j + 1);
         if (j + 1 < j1) copy_wait<1>(); else copy_wait<0>();      // V of this tile
         __syncthreads();
-#pragma unroll 2
+#pragma unroll 8
         for (int e = 0; e < kK; e += 4) {
             float4 p[8];
 #pragma unroll
