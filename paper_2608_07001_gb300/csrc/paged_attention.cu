@@ -159,9 +159,16 @@ __device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity, SM &sm, i
 __device__ __forceinline__ int pa_len(const PaArgs &a, int s) {
     return max(0, min(a.lens[s], a.c.page_size * a.c.max_pages));
 }
-// CTA of tile i when `total` tiles are cut into nc runs [c total / nc, (c + 1) total / nc).
-__device__ __forceinline__ int pa_run_of(long long i, long long total, long long nc) {
-    return (int)(((i + 1) * nc + total - 1) / total - 1);
+// `total` tiles are cut into nc runs [c total / nc, (c + 1) total / nc): where run c begins, and the run of tile i.
+// Up to kPaNarrow tiles the products fit 32 bits (nc <= kPaMaxGrid); a 64-bit division costs about 0.1 us, and
+// five of them lie on the way of a call that reads little.
+constexpr long long kPaNarrow = 1 << 22;
+__device__ __forceinline__ long long pa_run_first(int c, long long total, int nc) {
+    return total <= kPaNarrow ? (uint32_t)c * (uint32_t)total / (uint32_t)nc : c * total / nc;
+}
+__device__ __forceinline__ int pa_run_of(long long i, long long total, int nc) {
+    return total <= kPaNarrow ? (int)((((uint32_t)i + 1) * (uint32_t)nc + (uint32_t)total - 1) / (uint32_t)total) - 1
+                              : (int)(((i + 1) * nc + total - 1) / total - 1);
 }
 
 // log m in base 2: finite values stay finite.
@@ -466,10 +473,11 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     // joins them, eight at a time.  (16000 entries of 2 sequences: 18.6 us with runs of 2 tiles, 15.7 of 4,
     // 16.5 of 8; 2000 entries of 8: 11.2 of 2, 12.2 of 4, 14.7 of 8; fp32, 1000 entries of 10 in tiles of
     // 32: 12.3 of 1, 13.9 of 2, 15.1 of 4.)
-    const long long least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
-    const long long nc = min((long long)gridDim.x, (total + least - 1) / least);
-    const long long lo = (long long)blockIdx.x < nc ? blockIdx.x * total / nc : total;
-    const long long hi = (long long)blockIdx.x < nc ? (blockIdx.x + 1) * total / nc : total;
+    const int least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
+    const int nc = total <= kPaNarrow ? min((int)gridDim.x, (int)(((uint32_t)total + least - 1) / (uint32_t)least))
+                                      : (int)min((long long)gridDim.x, (total + least - 1) / least);
+    const long long lo = (int)blockIdx.x < nc ? pa_run_first(blockIdx.x, total, nc) : total;
+    const long long hi = (int)blockIdx.x < nc ? pa_run_first(blockIdx.x + 1, total, nc) : total;
     if (lo < hi && lo >= before && lo < before + mine) {
         int s = tid * seg;
         for (;; s++) {
