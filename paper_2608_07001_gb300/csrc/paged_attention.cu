@@ -603,8 +603,10 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             sm.Z[tid] = Z;
         }
         pa_sync();
-        for (int i = 0; i < kPaWarps; i++) {
-            if (warp == i) w.add(sum, sm.M, gq, i == 0);
+        // fp32: only the warps that had one of the piece's tiles, from its first stage on
+        const int adds = C::BF ? kPaWarps : min(kPaF32Warps, t1 - t0), from = C::BF ? 0 : (int)((it - (t1 - t0)) % kPaF32Warps);
+        for (int i = 0; i < adds; i++) {
+            if (warp == (C::BF ? i : (from + i) % kPaF32Warps)) w.add(sum, sm.M, gq, i == 0);
             pa_sync();
         }
         T *out = static_cast<T *>(a.out) + (size_t)s * gq * D;
@@ -628,41 +630,46 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                 __threadfence();
                 const int np = c_hi - c_lo + 1;
                 auto piece = [&](int p) { return a.part + (size_t)(2 * (c_lo + p) + (p == 0)) * PF; };
-                // four channels a thread, over the pieces in order, eight loads in flight
-                for (int i = tid * 4; i < gq * D; i += kPaCons * 4) {
-                    const int h = i / D;
-                    float M = -INFINITY, Z = 0.f;
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int p0 = 0; p0 < np; p0 += 8) {
-                        float m[8], z[8], mx = M;
-                        float4 x[8];
+                // four channels a thread, over the pieces in order, N loads in flight: a batch is the latency of a
+                // read (0.8 us), so 16 where there are more than 8 pieces
+                auto join = [&](auto batch) {
+                    constexpr int N = decltype(batch)::value;
+                    for (int i = tid * 4; i < gq * D; i += kPaCons * 4) {
+                        const int h = i / D;
+                        float M = -INFINITY, Z = 0.f;
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int p0 = 0; p0 < np; p0 += N) {
+                            float m[N], z[N], mx = M;
+                            float4 x[N];
 #pragma unroll
-                        for (int p = 0; p < 8; p++) {
-                            // past the last piece: the last one again, with no weight
-                            const float *q = piece(min(p0 + p, np - 1));
-                            m[p] = __ldcg(q + 8 * D + h);
-                            z[p] = __ldcg(q + 8 * D + 8 + h);
-                            x[p] = __ldcg(reinterpret_cast<const float4 *>(q + i));
-                        }
+                            for (int p = 0; p < N; p++) {
+                                // past the last piece: the last one again, with no weight
+                                const float *q = piece(min(p0 + p, np - 1));
+                                m[p] = __ldcg(q + 8 * D + h);
+                                z[p] = __ldcg(q + 8 * D + 8 + h);
+                                x[p] = __ldcg(reinterpret_cast<const float4 *>(q + i));
+                            }
 #pragma unroll
-                        for (int p = 0; p < 8; p++) {
-                            if (p0 + p >= np) m[p] = -INFINITY;
-                            mx = fmaxf(mx, m[p]);
-                        }
-                        const float sh = pa_shift(mx), f = tc::ex2(M - sh);
-                        M = mx;
-                        Z *= f;
-                        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+                            for (int p = 0; p < N; p++) {
+                                if (p0 + p >= np) m[p] = -INFINITY;
+                                mx = fmaxf(mx, m[p]);
+                            }
+                            const float sh = pa_shift(mx), f = tc::ex2(M - sh);
+                            M = mx;
+                            Z *= f;
+                            v.x *= f; v.y *= f; v.z *= f; v.w *= f;
 #pragma unroll
-                        for (int p = 0; p < 8; p++) {
-                            const float g = tc::ex2(m[p] - sh);
-                            Z += g * z[p];
-                            v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
+                            for (int p = 0; p < N; p++) {
+                                const float g = tc::ex2(m[p] - sh);
+                                Z += g * z[p];
+                                v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
+                            }
                         }
+                        const float r = Z > 0.f ? 1.f / Z : 0.f;
+                        put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
                     }
-                    const float r = Z > 0.f ? 1.f / Z : 0.f;
-                    put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-                }
+                };
+                if (np > 8) join(std::integral_constant<int, 16>()); else join(std::integral_constant<int, 8>());
                 if (tid == 0) a.cnt[c_lo] = 0;
             }
         }
