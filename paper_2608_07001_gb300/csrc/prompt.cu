@@ -15,6 +15,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace gkv {
 namespace {
 
@@ -22,7 +24,7 @@ using namespace serve;
 
 // Joins some rows of a split block (32 of the tcgen05 kernel's, 8 of the fp32
 // kernel's), four channels a thread, over the parts in order with eight loads in
-// flight: the latency of a read or two, whatever the number of parts.  The
+// flight (16 for many fp32 parts): the latency of a read or two.  The
 // tcgen05 kernel's parts are read across rows as they lie and turned in shared
 // memory, so that rows leave whole.
 constexpr int join_rows(bool tc) { return tc ? 32 : 8; }
@@ -62,33 +64,37 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
     if (token(r) < nq) {
         float M = -INFINITY, Z = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int b = 0; b < np; b += 8) {
-            float m[8], z[8], mx = M;
-            float4 x[8];
+        auto join = [&](auto batch) {
+            constexpr int N = decltype(batch)::value;
+            for (int b = 0; b < np; b += N) {
+                float m[N], z[N], mx = M;
+                float4 x[N];
 #pragma unroll
-            for (int p = 0; p < 8; p++) {
-                // past the last part: the last one again, with no weight
-                const float *q = p0 + (size_t)min(b + p, np - 1) * PF;
-                m[p] = q[ROWS * D + r];
-                z[p] = q[ROWS * D + ROWS + r];
-                x[p] = reinterpret_cast<const float4 *>(q)[at];
-            }
+                for (int p = 0; p < N; p++) {
+                    // past the last part: the last one again, with no weight
+                    const float *q = p0 + (size_t)min(b + p, np - 1) * PF;
+                    m[p] = q[ROWS * D + r];
+                    z[p] = q[ROWS * D + ROWS + r];
+                    x[p] = reinterpret_cast<const float4 *>(q)[at];
+                }
 #pragma unroll
-            for (int p = 0; p < 8; p++) {
-                if (b + p >= np) m[p] = -INFINITY;
-                mx = fmaxf(mx, m[p]);
-            }
-            const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
-            M = mx;
-            Z *= w;
-            v.x *= w; v.y *= w; v.z *= w; v.w *= w;
+                for (int p = 0; p < N; p++) {
+                    if (b + p >= np) m[p] = -INFINITY;
+                    mx = fmaxf(mx, m[p]);
+                }
+                const float sh = mx == -INFINITY ? 0.f : mx, w = tc::ex2(M - sh);
+                M = mx;
+                Z *= w;
+                v.x *= w; v.y *= w; v.z *= w; v.w *= w;
 #pragma unroll
-            for (int p = 0; p < 8; p++) {
-                const float f = tc::ex2(m[p] - sh);
-                Z += f * z[p];
-                v.x += f * x[p].x; v.y += f * x[p].y; v.z += f * x[p].z; v.w += f * x[p].w;
+                for (int p = 0; p < N; p++) {
+                    const float f = tc::ex2(m[p] - sh);
+                    Z += f * z[p];
+                    v.x += f * x[p].x; v.y += f * x[p].y; v.z += f * x[p].z; v.w += f * x[p].w;
+                }
             }
-        }
+        };
+        if (!TC && np > 8) join(std::integral_constant<int, 16>()); else join(std::integral_constant<int, 8>());
         const float inv = Z > 0.f ? 1.f / Z : Z;          // a row that sees no key: 0; a NaN stays
         v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
         if constexpr (TC) {
