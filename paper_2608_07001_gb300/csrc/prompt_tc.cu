@@ -33,11 +33,12 @@
 //
 // Measured (32 / 8 heads): 16384 tokens of d = 128 1.20 to 1.36 ms by the power
 // limit, 1.62 to 1.83 PFLOP/s of 1.88 that a plain matrix product reaches, the
-// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.51 ms, 1.16
+// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.48 ms, 1.23
 // PFLOP/s.  d = 64 step by step: 128-key tiles, one S 560 us, the maximum with
 // the load 528, 96-key tiles and two S 532, one slot for V and K 511, P at once
-// 509.  A loop of the softmax alone takes 1000 clocks for 96 keys of two warps a
-// scheduler (770 of them exponentials), this kernel about 1430.  Tried for
+// 509, a faster start and end of a block 497, no vote at a wait and the loop by
+// two 480.  A loop of the softmax alone takes 1000 clocks for 96 keys of two
+// warps a scheduler (770 of them exponentials), this kernel about 1370.  Tried for
 // d = 64 and slower: two threads a row, no maximum but a check of the weights'
 // sum, the next scores read under the last weights, P in columns of its own,
 // key tiles of 64 with two or three S, four row tiles a CTA.
@@ -248,11 +249,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         float m = -INFINITY, z = 0.f;                    // m: the reference times c
         const int nj = i ? nkv1 : nkv0;
         bool ok = true;
+        // A wait that gave up leaves nothing to rely on, but the warp goes on together to the end: every later
+        // wait gives up at once, and nothing is written.
+        const uint32_t bs = tc::smem_u32(&b.sfull[i][0]), bp = tc::smem_u32(&b.pfull[i][0][0]);
+        uint32_t ph = 0;                                 // of the score buffers
+        // d = 64: by two, so that a score buffer's addresses are constants (12000 tokens 485 -> 480 us)
+#pragma unroll (SB)
         for (int j = 0; j < nj; j++) {
             const int sb = j % SB;
             const uint32_t ts = ts0 + (uint32_t)(sb * NK);
-            ok = __all_sync(0xffffffffu, wait(&b.sfull[i][sb], (j / SB) & 1, b, a.status));
-            if (!ok) break;
+            ok = wait(bs + 8 * sb, ph, b, a.status) && ok;
+            __syncwarp();
             tc::tc_fence_after();
             uint32_t x[NK / 32][32];
             float mx[NK / 32];
@@ -285,9 +292,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // O is rescaled once PV(j - 1) is in it: with one score buffer S(j) came after it; with two
                 // S(j + 1) does, and at the last tile a commit of its own tells
                 if constexpr (SB == 2) {
-                    ok = __all_sync(0xffffffffu, j + 1 < nj ? wait(&b.sfull[i][(j + 1) & 1], ((j + 1) / 2) & 1, b, a.status)
-                                                            : wait(&b.oprev[i], 0, b, a.status));
-                    if (!ok) break;
+                    ok = (j + 1 < nj ? wait(&b.sfull[i][(j + 1) & 1], ((j + 1) / 2) & 1, b, a.status)
+                                     : wait(&b.oprev[i], 0, b, a.status)) && ok;
+                    __syncwarp();
                     tc::tc_fence_after();
                 }
                 float w = 1.f;
@@ -320,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::tmem_wait_st();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][sb][k]));
+                if (lane == 0) tc::mbar_arrive(bp + 8 * (2 * sb + k));
             };
             uint32_t p0[32], p1[(NK - 64) / 2];
 #pragma unroll
@@ -332,8 +339,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tmem_st(ts + 32, p1);
             hand(C::HV - 1);
             z += acc.x + acc.y;
+            if (sb == SB - 1) ph ^= 1;
         }
-        if (ok && nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status));
+        if (nj > 0) ok = __all_sync(0xffffffffu, wait(&b.odone[i], 0, b, a.status) && ok);
         tc::tc_fence_after();
         const int64_t row = q0 + token;
         const int hq = g * t.gq + h;
