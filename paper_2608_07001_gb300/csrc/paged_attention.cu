@@ -37,9 +37,9 @@
 //     them in order.  Nothing waits for another CTA, and results do not depend
 //     on timing.
 //
-// Measured: 88 us for 1M entries of 2 x 128 bf16 and log m (32 requests x 8
+// Measured: 87.5 us for 1M entries of 2 x 128 bf16 and log m (32 requests x 8
 // heads, uneven; 6.1 TB/s, 0.90 of a plain copy's rate), the same for one
-// request of 131072 entries; 6.3 us for one request of 8 x 256 entries.
+// request of 131072 entries; 6.1 us for one request of 8 x 256 entries.
 //
 // log m joins in base 2 with log m log2(e) held at the lowest finite value, so
 // that entries of the lowest log m keep equal weights; -inf stays no weight.
@@ -470,9 +470,10 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     }
     const bool snap = most <= kPaSnap;
     // A run holds MIN tiles at least, and as many as leave the longest sequence kPaPieces pieces: one CTA
-    // joins them, eight at a time.  (16000 entries of 2 sequences: 18.6 us with runs of 2 tiles, 15.7 of 4,
-    // 16.5 of 8; 2000 entries of 8: 11.2 of 2, 12.2 of 4, 14.7 of 8; fp32, 1000 entries of 10 in tiles of
-    // 32: 12.3 of 1, 13.9 of 2, 15.1 of 4.)
+    // joins them, eight or sixteen at a time.  (16000 entries of 2 sequences: 14.9 us with runs of 2 or 4
+    // tiles, 16.4 of 8; 60000 entries of one head: 22.4 us in 64 pieces, 24.7 in 128; 2000 entries of 8
+    // sequences: 11.0 of 2 tiles, 11.8 of 4, 14.4 of 8; fp32, 1000 entries of 10 in tiles of 32: 11.5 of 1,
+    // 12.7 of 2, 14.0 of 4.)
     const int least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
     const int nc = total <= kPaNarrow ? min((int)gridDim.x, (int)(((uint32_t)total + least - 1) / (uint32_t)least))
                                       : (int)min((long long)gridDim.x, (total + least - 1) / least);
