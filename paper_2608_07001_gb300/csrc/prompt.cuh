@@ -8,9 +8,9 @@ namespace serve {
 
 // A launch with few blocks splits each block's keys into parts that run beside
 // one another and leave O, M and Z in the workspace; a second launch joins them
-// in order.  Most parts kept at once: one CTA a SM (tcgen05), four a SM (fp32,
-// whose parts are a quarter of the rows and two CTAs are resident).
-constexpr int kPartsTc = 152, kPartsF32 = 608;
+// in order.  Most parts kept at once: two a SM (tcgen05, one CTA resident), four
+// a SM (fp32, whose parts are a quarter of the rows and two CTAs are resident).
+constexpr int kSms = 152, kPartsTc = 2 * kSms, kPartsF32 = 4 * kSms;
 constexpr int kRowsTc = 256, kRowsF32 = 64;        // rows of a block
 constexpr int kKeysF32 = 64;                       // keys of a tile
 __host__ __device__ constexpr int keys_tc(int d) { return d == 64 ? 96 : 128; }

@@ -169,11 +169,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::tmem_relinquish();
     }
     after_previous();
-    if (blockIdx.x == 0 && blockIdx.y == 0) check_bounds(a);
+    if (blockIdx.x == 0) check_bounds(a);
     // ---- the CTA's rows: heavy blocks (late tokens) first
-    const int g = blockIdx.x % a.G;
+    const int part = blockIdx.x % a.split, block = blockIdx.x / a.split, g = block % a.G;
     const int tok = 2 * t.tpt;
-    const int slot = t.slots - 1 - (int)(blockIdx.x / a.G);
+    const int slot = t.slots - 1 - block / a.G;
     int64_t q0, nq64, k0, nk64;
     int s;
     const bool fits = slot_rows(a, slot, tok, s, q0, nq64, k0, nk64);
@@ -186,11 +186,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int last0 = min(nq, t0 + t.tpt) - 1 + off, last1 = min(nq, t0 + 2 * t.tpt) - 1 + off;
     const int all0 = last0 >= 0 ? last0 / NK + 1 : 0, all1 = ntile > 1 && last1 >= 0 ? last1 / NK + 1 : 0;
     const int all = max(all0, all1), np = parts_of(all, a.split, least_tc(D));
-    const int j0 = part_first(all, np, blockIdx.y), j1 = part_first(all, np, blockIdx.y + 1), n = j1 - j0;
+    const int j0 = part_first(all, np, part), j1 = part_first(all, np, part + 1), n = j1 - j0;
     const int nkv0 = max(0, min(all0, j1) - j0), nkv1 = max(0, min(all1, j1) - j0);
 
     // nothing to do: a sequence that does not fit, a slot past its tokens, a part beyond the block's
-    const bool idle = !fits || t0_64 < 0 || t0_64 >= nq64 || (int)blockIdx.y >= np;
+    const bool idle = !fits || t0_64 < 0 || t0_64 >= nq64 || part >= np;
 
     // ---- copies, by the producer's thread: the first ones leave before the block meets
     auto copy = [&](const CUtensorMap *map, int head, int j, uint32_t at, uint32_t fb) {
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else {
             // a part: [D / 4][rows] sums of 4 channels, then [rows] references, [rows] sums of weights
-            float *pp = a.part + ((size_t)blockIdx.x * a.split + blockIdx.y) * part_floats(kRowsTc, D);
+            float *pp = a.part + ((size_t)block * a.split + part) * part_floats(kRowsTc, D);
             const int pr = i * 128 + r;
             if (ok && i < ntile) {
 #pragma unroll
@@ -584,6 +584,27 @@ bool make_map(CUtensorMap *m, const void *p, int64_t tokens, int heads, int d, i
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Parts of a block.  Fewer blocks than SMs leave SMs idle, so their keys are split; parts and their join cost
+// about 5 us and 0.15 us a block (0.26 MB written and read a part), a wave's start and end 6 us.  Blocks see
+// `tiles` key tiles at most and, were the sequences' lengths within twice their mean, `some`.  Parts beyond one a
+// SM, which run in waves, are taken on the latter's account only.  (d = 128, us unsplit / split: 600 queries over
+// 30000 keys of 8 heads 354 / 230 in 3 parts, 2 waves; 120 over 30000 283 / 50 in 9, 71 in 19; 4000 of 2 heads
+// 48 / 26 in 4; not split: 2000 of 2 heads of 4 queries 25 / 30, 1024 of 8 17 / 32.)
+int split_of(int64_t blocks, int64_t tiles, int n_seqs, int d) {
+    const double tile = d == 64 ? 0.75 : 1.2;            // us
+    auto cost = [&](int64_t parts, int64_t n) {
+        return (double)((blocks * parts + kSms - 1) / kSms) * (6. + (double)((n + parts - 1) / parts) * tile) +
+               (parts > 1 ? 5. + 0.15 * (double)blocks : 0.);
+    };
+    const int64_t one = std::min<int64_t>(kSms / blocks, tiles / least_tc(d));
+    int64_t best = one > 1 && cost(one, tiles) < cost(1, tiles) ? one : 1;
+    const int64_t some = std::min<int64_t>(tiles, 2 * tiles / n_seqs);
+    const int64_t most = std::min<int64_t>(kPartsTc / blocks, some / least_tc(d));
+    for (int64_t p = best + 1; p <= most; p++)
+        if (cost(p, some) < cost(best, some)) best = p;
+    return (int)best;
+}
+
 template <int D>
 cudaError_t launch(PromptArgs a, cudaStream_t s) {
     Tc t;
@@ -617,9 +638,8 @@ cudaError_t launch(PromptArgs a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         ready[dev].store(1, std::memory_order_relaxed);
     }
-    // fewer blocks than SMs: their keys are split over the others
-    a.split = (int)std::max<int64_t>(1, std::min<int64_t>(kPartsTc / blocks, (a.n_k + Cfg<D>::NK - 1) / Cfg<D>::NK / least_tc(D)));
-    e = launch_overlapped(prompt_tc_kernel<D>, dim3((unsigned)blocks, (unsigned)a.split), kThreads, Cfg<D>::SMEM, s, a, t, mq,
+    a.split = split_of(blocks, (a.n_k + Cfg<D>::NK - 1) / Cfg<D>::NK, a.n_seqs, D);
+    e = launch_overlapped(prompt_tc_kernel<D>, dim3((unsigned)(blocks * a.split)), kThreads, Cfg<D>::SMEM, s, a, t, mq,
                           mk, mv);
     return e == cudaSuccess && a.split > 1 ? launch_prompt_join(a, D, GKV_BF16, true, s) : e;
 }

@@ -95,6 +95,11 @@ def test_few_queries_over_a_long_axis(gk, dtype, nq, nk):
     check(gk, *inputs(6, nq, nk, 4, 1, 64, dtype), cu([nq]), cu([nk]))
 
 
+@pytest.mark.parametrize("nq,nk,G", [(3, 12000, 80), (300, 6000, 20), (70, 9000, 1)])
+def test_parts_of_many_and_of_few_blocks(gk, nq, nk, G):
+    check(gk, *inputs(25, nq, nk, G, G, 64, BF), cu([nq]), cu([nk]))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("d", [64, 128])
 def test_rows_outside_the_sequences_do_not_matter(gk, dtype, d):
