@@ -10,8 +10,8 @@
 // rescaled a few times instead of once a key tile; P stays below 2^kLazy, and O
 // and Z share the reference, so the quotient is the same.
 //
-// What bounds it: at d = 128 a 128 x 128 tile costs 2 x 128^3 MACs in each of
-// the two products against 128^2 exponentials, so the tensor pipe; at d = 64
+// What bounds it: at d = 128 a 128 x 128 tile costs 128^3 MACs in each of the
+// two products against 128^2 exponentials, so the tensor pipe; at d = 64
 // the exponentials weigh twice as much, and the softmax warps bound it.  The two
 // row tiles alternate: while the tensor core works on one's S and PV, the
 // other's warps take its softmax.
@@ -33,7 +33,7 @@
 //
 // Measured (32 / 8 heads): 16384 tokens of d = 128 1.20 to 1.36 ms by the power
 // limit, 1.62 to 1.83 PFLOP/s of 1.88 that a plain matrix product reaches, the
-// tensor pipe 72 % busy at 8192 tokens; 12000 tokens of d = 64 0.48 ms, 1.23
+// tensor pipe 75 % busy at 8192 tokens; 12000 tokens of d = 64 0.48 ms, 1.23
 // PFLOP/s.  d = 64 step by step: 128-key tiles, one S 560 us, the maximum with
 // the load 528, 96-key tiles and two S 532, one slot for V and K 511, P at once
 // 509, a faster start and end of a block 497, no vote at a wait and the loop by
