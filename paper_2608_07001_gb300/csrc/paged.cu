@@ -71,7 +71,8 @@ struct AppendArgs {
     int *status;
 };
 
-__device__ __forceinline__ uint4 ld16(const char *p) { return __ldg(reinterpret_cast<const uint4 *>(p)); }
+// A plain load: the kernel before may have written it while this one had begun, and q_out may be q.
+__device__ __forceinline__ uint4 ld16(const char *p) { return *reinterpret_cast<const uint4 *>(p); }
 __device__ __forceinline__ void st16(char *p, uint4 x) { *reinterpret_cast<uint4 *>(p) = x; }
 
 template <typename T>

@@ -190,8 +190,8 @@ struct PaBf {
             static_cast<const __nv_bfloat16 *>(a.q) + ((size_t)s * gq + (hq < gq ? hq : 0)) * D);
 #pragma unroll
         for (int kk = 0; kk < D / 16; kk++) {
-            qa[kk][0] = hq < gq ? __ldg(q + kk * 8 + tq) : 0u;
-            qa[kk][1] = hq < gq ? __ldg(q + kk * 8 + 4 + tq) : 0u;
+            qa[kk][0] = hq < gq ? q[kk * 8 + tq] : 0u;
+            qa[kk][1] = hq < gq ? q[kk * 8 + 4 + tq] : 0u;
         }
 #pragma unroll
         for (int i = 0; i < D / 8; i++)

@@ -51,7 +51,7 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 __device__ __forceinline__ void load4(float *dst, const float *src, bool on) { copy16(dst, src, on); }
 __device__ __forceinline__ void load4(float *dst, const __nv_bfloat16 *src, bool on) {
     uint2 u = make_uint2(0, 0);
-    if (on) u = __ldg(reinterpret_cast<const uint2 *>(src));
+    if (on) u = *reinterpret_cast<const uint2 *>(src);
     *reinterpret_cast<float4 *>(dst) = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
                                                    __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
 }

@@ -55,7 +55,9 @@ inline gkv_status read_status(void *workspace, void *stream) {
 // start when all its own blocks run (next_may_start), and waits for the whole of
 // the one before, and for what it wrote, before it reads anything that a
 // kernel can have written (after_previous).  What comes before that wait --
-// barriers, TMEM, descriptors -- runs under the previous kernel's end.
+// barriers, TMEM, descriptors -- runs under the previous kernel's end.  Such
+// memory is read with plain loads (or through TMA), which stay behind the wait;
+// the read-only path is for data that nothing writes during a kernel's life.
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -1,0 +1,63 @@
+"""Serving operators where they can go wrong quietly: launches in a chain,
+non-finite values that a sequence holds, bounds that do not fit, sizes past 32
+bits, the branches that ordinary sizes do not take."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from . import serving_reference as R
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gk():
+    import __graft_entry__ as g
+    g.build()
+    assert torch.cuda.is_available()
+    from paper_2608_07001_gb300 import gracekv
+    return gracekv
+
+
+# ---------------------------------------------------------------------- chains
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,d", [(1, 64), (7, 128), (64, 128)])
+def test_in_place_rotation_and_attention_in_a_chain(gk, dtype, B, d):
+    # One buffer of queries, rotated in place and attended by layer after layer without a wait: every
+    # kernel starts under the end of the one that wrote what it reads.
+    L, G, Hq, ps, n = 6, 2, 8, 32, 150
+    g = torch.Generator(device="cuda").manual_seed(B)
+
+    def normal(*shape):
+        return torch.empty(*shape, dtype=dtype, device="cuda").normal_(generator=g)
+
+    mp = -(-n // ps)
+    table = torch.randperm(L * B * G * mp, device="cuda", generator=g).to(torch.int32).view(L, B, G, mp)
+    pool = [normal(L * B * G * mp, ps, d) for _ in range(2)]
+    k, v = (normal(L, B, G, d) for _ in range(2))
+    q0, pos = normal(B, Hq, d), torch.randint(0, 100000, (B,), device="cuda", generator=g).to(torch.int32)
+
+    def steps(wait):
+        c = gk.PagedCache(pool[0].clone(), pool[1].clone(), table, torch.full((L, B, G), n, **I32), Hq=Hq, rope_base=1e4)
+        q, seen = q0.clone(), []
+        outs = torch.zeros(4 * L, B, Hq, d, dtype=dtype, device="cuda")
+        torch.cuda.synchronize()
+        for i in range(4 * L):
+            l = i % L
+            c.append(l, k[l], v[l], pos, q=q, out=q)
+            if wait:
+                torch.cuda.synchronize()
+            c.attention(l, q, out=outs[i])
+            if wait:
+                torch.cuda.synchronize()
+        c.status()
+        return q, outs, c.K, c.V
+
+    want = steps(True)
+    for _ in range(3):
+        for a, b in zip(steps(False), want):
+            assert torch.equal(a, b)
