@@ -592,7 +592,9 @@ gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_p
 /* Attention of one token per request over layer l: q [B][Hq][d] (rotated; its
  * own entry appended), out [B][Hq][d] of the cache's dtype:
  *     x_e = q_h . k_e / sqrt(d) + log m_e,  out_h = sum_e softmax(x)_e v_e
- * over the lens[l][b][g] entries; a length of 0 gives 0.  page_size must be a
+ * over the lens[l][b][g] entries; a length of 0 gives 0, and so do entries of
+ * log m = -inf alone.  A head one of whose logits is NaN or +inf (a non-finite
+ * query, key or log m that the sequence holds) gives NaN.  page_size must be a
  * multiple of 16 here (GKV_EUNSUPPORTED).  Errors: GKV_EINVAL,
  * GKV_EUNSUPPORTED, GKV_ECUDA. */
 gkv_status gracekv_paged_attention(const gkv_paged_cache *c, int32_t l, const void *q, void *out, void *workspace,

@@ -41,8 +41,10 @@
 // heads, uneven; 6.1 TB/s, 0.90 of a plain copy's rate), the same for one
 // request of 131072 entries; 6.1 us for one request of 8 x 256 entries.
 //
-// log m joins in base 2 with log m log2(e) held at the lowest finite value, so
-// that entries of the lowest log m keep equal weights; -inf stays no weight.
+// log m joins in base 2 with log m log2(e) held between the finite values, so
+// that entries of the lowest or the largest log m keep equal weights; -inf stays
+// no weight.  A logit that is NaN or +inf makes its head's output NaN: the
+// quotient is 0 only where no weight at all was summed.
 #include "paged.cuh"
 #include "tc.cuh"
 
@@ -171,8 +173,10 @@ __device__ __forceinline__ int pa_run_of(long long i, long long total, int nc) {
                               : (int)(((i + 1) * nc + total - 1) / total - 1);
 }
 
-// log m in base 2: finite values stay finite.
-__device__ __forceinline__ float pa_lm2(float lm) { return lm == -INFINITY ? lm : fmaxf(lm * kLog2e, -FLT_MAX); }
+// log m in base 2: finite values stay finite, the others what they are.
+__device__ __forceinline__ float pa_lm2(float lm) {
+    return fabsf(lm) <= FLT_MAX ? fminf(fmaxf(lm * kLog2e, -FLT_MAX), FLT_MAX) : lm;
+}
 __device__ __forceinline__ float pa_shift(float m) { return m == -INFINITY ? 0.f : m; }
 
 // ---------------------------------------------------------------- consumers
@@ -615,7 +619,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         if (snap || c_lo == c_hi) {
             for (int i = tid; i < gq * D; i += kPaCons) {
                 const float Z = sm.Z[i / D];
-                put(out + i, Z > 0.f ? sum[i] / Z : 0.f);
+                put(out + i, Z == 0.f ? 0.f : sum[i] / Z);               // a NaN stays
             }
         } else {
             // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
@@ -666,7 +670,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                                 v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
                             }
                         }
-                        const float r = Z > 0.f ? 1.f / Z : 0.f;
+                        const float r = Z == 0.f ? 0.f : 1.f / Z;                // a NaN stays
                         put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
                     }
                 };
