@@ -477,7 +477,9 @@ gkv_status gracekv_decode_status(void *workspace, void *stream);
  * tensor's own strides in elements (so [N][Hq][d], [Hq][N][d] and a slice of a
  * fused projection all pass); k, v the same with G heads.  out may not overlap
  * the inputs.  n_q and n_k bound the rows: a sequence whose cu words run
- * backwards or past them is skipped and reported by gracekv_prompt_status.
+ * backwards or past them is skipped and reported by gracekv_prompt_status; so is
+ * one that, after such words, has query rows below the end of an earlier sequence.
+ * The others are computed.
  * d in {64, 128}, Hq / G in 1..8 (else GKV_EUNSUPPORTED); pointers on 16
  * bytes, strides multiples of 16 bytes and not negative, lse on 4 bytes,
  * n_seqs >= 0, n_q and n_k at most 2^31 - 4096.  Values: bf16 products are exact, sums

@@ -9,7 +9,7 @@
 //
 // bf16 runs on tcgen05 (prompt_tc.cu), fp32 on CUDA cores (prompt_f32.cu).
 // This file checks the arguments, lays out the workspace (the status word, the
-// parts of split blocks) and joins the parts.
+// word on the bounds' order, the parts of split blocks) and joins the parts.
 #include "prompt.cuh"
 #include "tc.cuh"
 
@@ -110,6 +110,17 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
     }
 }
 
+// One block: do the query bounds ascend?  Before launches of more than kScanSeqs sequences, whose blocks search the
+// bounds by halves instead of reading them all: a misplaced word would lead the search astray.
+__global__ void __launch_bounds__(1024) prompt_order_kernel(const PromptArgs a) {
+    next_may_start();
+    after_previous();
+    int bad = 0;
+    for (int s = threadIdx.x; s < a.n_seqs; s += 1024) bad |= !ascend(a.cu_q[s], a.cu_q[s + 1], a.n_q);
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *a.disorder = bad;
+}
+
 template <typename T, bool TC>
 cudaError_t join(const PromptArgs &a, int d, cudaStream_t s) {
     constexpr int ROWS = TC ? kRowsTc : kRowsF32;
@@ -170,8 +181,10 @@ extern "C" gkv_status gracekv_prompt_attention(const gkv_prompt *p, void *worksp
     const serve::PromptArgs a{p->q, p->k, p->v, p->out, p->lse, p->cu_q, p->cu_k, p->n_seqs, p->G, p->Hq, p->n_q, p->n_k,
                               p->q_ts, p->q_hs, p->k_ts, p->k_hs, p->v_ts, p->v_hs, p->o_ts, p->o_hs,
                               (float)(1.0 / sqrt((double)p->d)), reinterpret_cast<int *>(ws),
-                              reinterpret_cast<float *>(ws + serve::kWsHead), 1};
+                              reinterpret_cast<int *>(ws) + 1, reinterpret_cast<float *>(ws + serve::kWsHead), 1};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p->n_seqs > serve::kScanSeqs && launch_overlapped(prompt_order_kernel, 1, 1024, 0, s, a) != cudaSuccess)
+        return GKV_ECUDA;
     cudaError_t e = cudaErrorNotSupported;
     if (p->dtype == GKV_BF16) e = serve::launch_prompt_tc(a, p->d, s);
     if (e == cudaErrorNotSupported) e = serve::launch_prompt_f32(a, p->d, p->dtype, s);
