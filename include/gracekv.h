@@ -553,8 +553,8 @@ gkv_status gracekv_paged_workspace_size(const gkv_paged_cache *c, size_t *bytes)
  * lens[l][b][g] = offsets[l G + g + 1] - offsets[l G + g].  The table must hold
  * pages for them.  log_m may be NULL (written as 0); it must be NULL when the
  * cache has none.  Offsets past n_entries or running backwards give that head
- * length 0 and GKV_EINVAL from gracekv_paged_status; so do entries past
- * max_pages pages (the length is cut there).  Errors: GKV_EINVAL, GKV_ECUDA. */
+ * length 0, the others are loaded, and gracekv_paged_status reports GKV_EINVAL; so
+ * it does for entries past max_pages pages (the length is cut there).  Errors: GKV_EINVAL, GKV_ECUDA. */
 gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K, const void *V,
                               const float *log_m, const int64_t *offsets, int64_t n_entries, void *workspace,
                               void *stream);

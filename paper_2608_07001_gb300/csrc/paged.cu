@@ -204,24 +204,57 @@ struct LoadArgs {
     int *status;
 };
 
+__device__ __forceinline__ bool head_fits(const LoadArgs &a, int64_t lo, int64_t hi) {
+    return lo >= 0 && hi >= lo && hi <= a.n_entries;
+}
+
+// Offsets that run backwards or past the entries anywhere lead the search for an entry's head astray, so a block
+// then copies the heads [first, first + 256) that fit itself, one after another.  What the search finds is copied
+// too: the same entries to the same rows.  A call, so that it costs the caller no registers.
+template <int RB>
+__device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first) {
+    constexpr int CH = RB / 16;
+    const int heads = a.c.L * a.c.G;
+    const int64_t cap = (int64_t)a.c.page_size * a.c.max_pages;
+    for (int h = first; h < heads && h < first + 256; h++) {
+        const int64_t lo = a.off[h], hi = a.off[h + 1];
+        if (!head_fits(a, lo, hi)) continue;
+        const int64_t n = hi - lo < cap ? hi - lo : cap, s = ((int64_t)(h / a.c.G) * a.c.B + a.b) * a.c.G + h % a.c.G;
+        for (int64_t i = threadIdx.x; i < n * CH; i += 256) {
+            const int64_t e = i / CH, row = entry_row(a.c, s, (int)e, a.status);
+            const int ch = (int)(i % CH);
+            if (row < 0) continue;
+            st16(a.c.K + row * RB + ch * 16, ld16(a.K + (lo + e) * RB + ch * 16));
+            st16(a.c.V + row * RB + ch * 16, ld16(a.V + (lo + e) * RB + ch * 16));
+            if (ch == 0 && a.c.log_m) a.c.log_m[row] = a.log_m ? a.log_m[lo + e] : 0.f;
+        }
+    }
+}
+
 // The heads' lengths (offsets that do not fit give 0), one thread per (l, g);
 // then a warp copies a run of entries, 16 bytes of the key and of the value a
 // lane and IT times.  The head is searched for the run's first entry and
-// followed from there.
+// followed from there.  Eight blocks a SM: the registers that the call would take
+// otherwise leave room for six (1M entries of 2 x 256 bytes 163 us, 182 with 40).
 template <int RB, int IT>
-__global__ void __launch_bounds__(256) paged_load_kernel(const LoadArgs a) {
+__global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constant__ LoadArgs a) {
     constexpr int CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
     constexpr int U = IT < 4 ? IT : 4;
     next_may_start();
     after_previous();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, cap = (int64_t)a.c.page_size * a.c.max_pages;
     const int heads = a.c.L * a.c.G, lane = threadIdx.x & 31;
-    if (i < heads) {
-        const int64_t lo = a.off[i], hi = a.off[i + 1];
-        int64_t n = hi - lo;
-        if (lo < 0 || n < 0 || hi > a.n_entries) { atomicOr(a.status, kStRange); n = 0; }
-        if (n > cap) { atomicOr(a.status, kStRange); n = cap; }
-        a.c.lens[((int64_t)(i / a.c.G) * a.c.B + a.b) * a.c.G + i % a.c.G] = (int)n;
+    if ((int64_t)blockIdx.x * 256 < heads) {             // a block with a thread per head
+        if (i < heads) {
+            const int64_t lo = a.off[i], hi = a.off[i + 1];
+            int64_t n = hi - lo;
+            if (!head_fits(a, lo, hi)) { atomicOr(a.status, kStRange); n = 0; }
+            if (n > cap) { atomicOr(a.status, kStRange); n = cap; }
+            a.c.lens[((int64_t)(i / a.c.G) * a.c.B + a.b) * a.c.G + i % a.c.G] = (int)n;
+        }
+        int bad = 0;
+        for (int h = threadIdx.x; h < heads; h += 256) bad |= !head_fits(a, a.off[h], a.off[h + 1]);
+        if (__syncthreads_or(bad)) load_heads_disordered<RB>(a, (int)blockIdx.x * 256);
     }
     const int64_t e0 = (i >> 5) * (RW * IT) + lane / CH;
     if (e0 >= a.n_entries) return;
