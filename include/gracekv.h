@@ -485,6 +485,9 @@ gkv_status gracekv_decode_status(void *workspace, void *stream);
  * n_seqs >= 0, n_q and n_k at most 2^31 - 4096.  Values: bf16 products are exact, sums
  * fp32; the softmax weights of bf16 inputs are rounded to bf16 for the value
  * product and the output once to bf16; fp32 inputs stay fp32 throughout.
+ * Scores of bf16 inputs may reach 2^30 ln 2 = 7.4e8 in size; a row whose largest
+ * one is beyond that, on either side, gives NaN (scores of a row that lie further
+ * below its others weigh 0, as they should).
  * Keys and values of rows outside a sequence do not reach it whatever they
  * hold; a non-finite value inside a sequence may reach any of its queries.
  */

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
         const int h = g * gq + row % half % gq;
         put4(static_cast<T *>(a.out) + (q0 + t) * a.o_ts + h * a.o_hs + col * 4, v);
         if (col == 0 && a.lse)
-            a.lse[(q0 + t) * a.Hq + h] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * 0.6931471805599453f;
+            a.lse[(q0 + t) * a.Hq + h] = row_lse(M, Z);
     };
     if (token(r) < nq) {
         float M = -INFINITY, Z = 0.f;
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(join_rows(TC) * D / 4) prompt_join_kernel(cons
             }
         };
         if (!TC && np > 8) join(std::integral_constant<int, 16>()); else join(std::integral_constant<int, 8>());
-        const float inv = Z > 0.f ? 1.f / Z : Z;          // a row that sees no key: 0; a NaN stays
+        const float inv = row_scale(M, Z);
         v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
         if constexpr (TC) {
             out_s[rr * LD + c] = v;

@@ -3,6 +3,8 @@
 
 #include "serve.cuh"
 
+#include <math.h>
+
 namespace gkv {
 namespace serve {
 
@@ -158,6 +160,13 @@ __device__ __forceinline__ int part_first(int n, int np, int p) { return p * (n 
 // Floats of a part: 4-channel groups of the sums (by row or by group), then the
 // rows' maxima (base 2) and weight sums.
 __host__ __device__ constexpr size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
+
+// What a row's sums are multiplied by, and its lse, from its reference (base 2) and its weights' sum: 0 and -inf where it
+// saw no key, NaN where a weight was NaN or (tcgen05) none was in range.
+__device__ __forceinline__ float row_scale(float m, float z) { return z > 0.f ? 1.f / z : m == -INFINITY ? 0.f : NAN; }
+__device__ __forceinline__ float row_lse(float m, float z) {
+    return z == 0.f && m == -INFINITY ? m : z > 0.f ? (m + log2f(z)) * 0.6931471805599453f : NAN;
+}
 
 // Joins the parts of a split launch of the tcgen05 kernel (sums [d / 4][rows])
 // or of the fp32 kernel ([rows][d / 4]).

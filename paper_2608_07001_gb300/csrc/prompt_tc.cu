@@ -46,12 +46,20 @@
 // Few blocks (a short chunk over a long cache) leave SMs idle: then a block's
 // keys are split into parts (prompt.cuh) that prompt.cu joins.
 //
+// x c - m in one step keeps what rounding m left off, up to 2^-24 |m|, and so scales
+// a row's weights, O and Z alike, by up to 2^64 at |m| = 2^30.  References stop there
+// (kFar): a row of larger scores has infinite weights and gives NaN, one of nothing
+// but scores further below has none and gives NaN too; scores that far below the
+// others count 0.  Rounding x c as m was would lift the limit, but any look at m in
+// the loop that is not there now costs 4 to 8 % of every call at d = 128.
+//
 // Masks: only the tiles that reach past a row's last key compare columns; the
 // keys past a sequence's end get weight 0 that way, and their V rows, which
 // may hold anything, are zeroed in shared memory before the product.
 #include "prompt.cuh"
 #include "tc.cuh"
 
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -67,6 +75,7 @@ constexpr int kRegs = 168, kRegsSoftmax = 208, kRegsIssue = 88;
 static_assert(256 * kRegsSoftmax + 128 * kRegsIssue <= kThreads * kRegs, "register split");
 constexpr int kWarpTma = 8, kWarpMma = 9;      // MMA: warps 9 and 10, one a row tile
 constexpr float kLazy = 8.f;                   // log2 of the growth a reference lets pass
+constexpr float kFar = 1 << 30;                // size that a finite reference does not pass
 constexpr uint64_t kWaitNs = 2000000000ull;
 
 template <int D>
@@ -285,9 +294,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
 #pragma unroll
             for (int k = 1; k < NK / 32; k++) mx[0] = fmaxf(mx[0], mx[k]);
-            const float mn = mx[0] * c;
+            const float mn = mx[0] == -INFINITY ? -INFINITY : fminf(fmaxf(mx[0] * c, -kFar), kFar);
             if (m == -INFINITY) m = mn;                  // nothing accumulated yet
-            else if (__builtin_expect(mn > m + kLazy, 0)) z = -z;          // asks for a rescale (z > 0 marks none)
+            else if (__builtin_expect(mn > m + kLazy, 0)) z = -FLT_MIN - z;        // asks for a rescale, by a sum of 0 too
             if (__any_sync(0xffffffffu, z < 0.f)) {
                 // O is rescaled once PV(j - 1) is in it: with one score buffer S(j) came after it; with two
                 // S(j + 1) does, and at the last tile a commit of its own tells
@@ -351,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // shared memory (this warp's rows of Q, which no product reads any more; 16-byte chunks
                 // permuted by row) and leave 512 bytes a store.
                 constexpr int CH = D / 8;                    // chunks of a row
-                const float inv = z > 0.f ? 1.f / z : z;     // no key: 0; a NaN stays
+                const float inv = row_scale(m, z);
                 const int64_t at = live ? row * a.o_ts + hq * a.o_hs : -1;
                 uint4 v[CH];
                 if (nj > 0) {
@@ -390,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int64_t to_row = __shfl_sync(0xffffffffu, at, x * (32 / CH) + lane / CH);
                     if (to_row >= 0) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + to_row + lane % CH * 8) = v[x];
                 }
-                if (live && a.lse) a.lse[row * a.Hq + hq] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
+                if (live && a.lse) a.lse[row * a.Hq + hq] = row_lse(m, z);
             }
         } else {
             // a part: [D / 4][rows] sums of 4 channels, then [rows] references, [rows] sums of weights
