@@ -570,6 +570,14 @@ class _Workspace:
         own.synchronize()
         self._own_stream = own.cuda_stream
 
+    def _run(self, call, *args):
+        """A call of the library with the tensors' device current: it launches on the current one."""
+        if torch._C._cuda_getDevice() == self._device.index:
+            _raise(call(*args))
+        else:
+            with torch.cuda.device(self._device):
+                _raise(call(*args))
+
     def _on(self, stream, *tensors):
         """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
         if stream is None:
@@ -577,6 +585,8 @@ class _Workspace:
             if raw != self._own_stream:
                 self.workspace.record_stream(torch.cuda.current_stream(self._device))
             return raw
+        if stream.device != self._device:
+            raise _bad(f"the stream is on {stream.device}, the tensors are on {self._device}")
         self.workspace.record_stream(stream)
         for t in tensors:
             if t is not None:
@@ -637,11 +647,11 @@ class PromptAttention(_Workspace):
             lp = lse.data_ptr()
         _PROMPT.pack_into(self._buf, 0, G, Hq, d, self._code, n1 - 1, n_q, n_k, cq, ck, qp, kp, vp, op, lp,
                           q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs)
-        _raise(self._call(self._ref, self._ws, self._on(stream, q, k, v, cu_q, cu_k, out, lse)))
+        self._run(self._call, self._ref, self._ws, self._on(stream, q, k, v, cu_q, cu_k, out, lse))
         return (out, lse) if return_lse else out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_prompt_status(self._ws, self._on(stream)))
+        self._run(lib().gracekv_prompt_status, self._ws, self._on(stream))
 
 
 class PagedCache(_Workspace):
@@ -727,12 +737,12 @@ class PagedCache(_Workspace):
         """The packed cache K, V [E, d], log_m [E] or None, offsets [L G + 1] int64
         becomes request b's entries (the table already holds their pages)."""
         dev, E = self._device, K.shape[0]
-        _raise(lib().gracekv_paged_load(
-            self._ref, b, _words("K", K, (E, self.d), self.dtype, dev),
+        self._run(
+            lib().gracekv_paged_load, self._ref, b, _words("K", K, (E, self.d), self.dtype, dev),
             _words("V", V, (E, self.d), self.dtype, dev),
             None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
             _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self._ws,
-            self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens)))
+            self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens))
 
     def load(self, b: int, cache: Cache, n_entries: int, stream=None):
         """A compressed cache (Compressor's output) as request b, replacing what the
@@ -780,7 +790,7 @@ class PagedCache(_Workspace):
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
         p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
-        _raise(lib().gracekv_paged_advance(self._ref, p, self._on(stream, self.lens, cu_new)))
+        self._run(lib().gracekv_paged_advance, self._ref, p, self._on(stream, self.lens, cu_new))
 
     def release(self, b: int, stream=None):
         """Request b's pages return to the pool; the slot is idle."""
@@ -817,9 +827,8 @@ class PagedCache(_Workspace):
                           0 if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
                           _words("pos", pos, (N,), torch.int32, dev), kp, vp, qp, op,
                           k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, o_ts, o_hs)
-        _raise(self._append(self._ref, l, self._tokens, self._ws,
-                            self._on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table,
-                                     self.lens)))
+        self._run(self._append, self._ref, l, self._tokens, self._ws,
+                  self._on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table, self.lens))
         return out
 
     def attention(self, l: int, q, out=None, stream=None):
@@ -832,9 +841,9 @@ class PagedCache(_Workspace):
             op = out.data_ptr()
         else:
             op = _words("out", out, shape, self.dtype, dev)
-        _raise(self._attention(self._ref, l, qp, op, self._ws,
-                               self._on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens)))
+        self._run(self._attention, self._ref, l, qp, op, self._ws,
+                  self._on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens))
         return out
 
     def status(self, stream=None):
-        _raise(lib().gracekv_paged_status(self._ws, self._on(stream)))
+        self._run(lib().gracekv_paged_status, self._ws, self._on(stream))

@@ -1,0 +1,112 @@
+"""The host side of the serving objects without a GPU: tensors and the C library
+are stand-ins, so that what reaches a launch, and what does not, can be seen."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+from paper_2608_07001_gb300 import gracekv as gk
+
+BF = torch.bfloat16
+
+
+class Tensor:
+    """A CUDA tensor as the wrappers look at it."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=BF, device="cuda:1"):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device(device)
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        s = [1]
+        for n in reversed(self.shape[1:]):
+            s.insert(0, s[0] * n)
+        return tuple(s)
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def is_contiguous(self):
+        return True
+
+    def record_stream(self, stream):
+        pass
+
+
+class Lib:
+    """Every call succeeds and notes the device that was current."""
+
+    def __init__(self, now):
+        self.now, self.seen = now, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            if not name.endswith("workspace_size"):
+                self.seen.append((name, self.now["device"]))
+            return gk.GKV_OK
+        return call
+
+
+@pytest.fixture
+def on_device_1(monkeypatch):
+    """Objects whose tensors are on cuda:1 while cuda:0 is current: (their calls, the library)."""
+    now = {"device": 0}
+    lib = Lib(now)
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now["device"] = now["device"], torch.device(d).index
+        try:
+            yield
+        finally:
+            now["device"] = before
+
+    def make_workspace(self, n, dev):
+        self.workspace, self._device, self._ws, self._own_stream = Tensor(n, dtype=torch.uint8), torch.device("cuda", 1), 1 << 20, 0
+
+    monkeypatch.setattr(gk, "lib", lambda: lib)
+    monkeypatch.setattr(gk._Workspace, "_make_workspace", make_workspace)
+    monkeypatch.setattr(gk, "_empty_like_on", lambda stream, shape, dtype, dev: Tensor(*shape, dtype=dtype, device=dev))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now["device"], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 0, raising=False)
+    i32 = dict(dtype=torch.int32)
+    p = gk.PromptAttention(G=2, Hq=4, d=64, dtype=BF, device="cuda:1")
+    c = gk.PagedCache(Tensor(4, 16, 64), Tensor(4, 16, 64), Tensor(1, 3, 2, 2, **i32), Tensor(1, 3, 2, **i32), Hq=4)
+    q, k, cu = Tensor(3, 4, 64), Tensor(3, 2, 64), Tensor(4, **i32)
+    calls = {
+        "prompt_attention": lambda **kw: p(q, k, k, cu, **kw), "prompt_status": lambda **kw: p.status(**kw),
+        "paged_load": lambda **kw: c.load_packed(0, Tensor(5, 64), Tensor(5, 64), None, Tensor(3, dtype=torch.int64), **kw),
+        "paged_advance": lambda **kw: c.advance_by(cu, **kw), "paged_append": lambda **kw: c.append(0, k, k, Tensor(3, **i32), q=q, **kw),
+        "paged_attention": lambda **kw: c.attention(0, q, **kw), "paged_status": lambda **kw: c.status(**kw),
+    }
+    return calls, lib, now
+
+
+NAMES = ["prompt_attention", "prompt_status", "paged_load", "paged_advance", "paged_append", "paged_attention", "paged_status"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_calls_are_made_on_the_tensors_device(on_device_1, name):
+    # the library launches on the current device; the raw stream of another one's default is 0 there too
+    calls, lib, now = on_device_1
+    calls[name]()
+    assert lib.seen == [("gracekv_" + name, 1)] and now["device"] == 0
+    now["device"] = 1
+    calls[name]()
+    assert lib.seen[1:] == [("gracekv_" + name, 1)] and now["device"] == 1
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_stream_of_another_device_is_refused(on_device_1, name):
+    calls, lib, _ = on_device_1
+    stream = types.SimpleNamespace(device=torch.device("cuda", 0), cuda_stream=7)
+    with pytest.raises(gk.GraceKVError) as e:
+        calls[name](stream=stream)
+    assert e.value.status == gk.GKV_EINVAL and not lib.seen
+    calls[name](stream=types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=7))
+    assert lib.seen == [("gracekv_" + name, 1)]
