@@ -733,30 +733,42 @@ class PagedCache(_Workspace):
                                                 torch.from_numpy(pages).to(self.table.device))
         self._host_lens = new_lens
 
+    def _packed(self, b: int, K, V, log_m, offsets):
+        """The checked arguments of gracekv_paged_load from b to n_entries."""
+        dev, E = self._device, K.shape[0]
+        if not 0 <= b < self.B:
+            raise _bad(f"request {b} of {self.B}")
+        if log_m is not None and self.log_m is None:
+            raise _bad("log m, and this cache keeps none")
+        ptrs = (_words("K", K, (E, self.d), self.dtype, dev), _words("V", V, (E, self.d), self.dtype, dev),
+                None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
+                _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev))
+        if E >= 1 << 31 or (E and (ptrs[0] % 16 or ptrs[1] % 16)):
+            raise _bad("K and V are at most 2^31 - 1 entries, on 16 bytes")
+        return b, *ptrs, E
+
     def load_packed(self, b: int, K, V, log_m, offsets, stream=None):
         """The packed cache K, V [E, d], log_m [E] or None, offsets [L G + 1] int64
         becomes request b's entries (the table already holds their pages)."""
-        dev, E = self._device, K.shape[0]
-        self._run(
-            lib().gracekv_paged_load, self._ref, b, _words("K", K, (E, self.d), self.dtype, dev),
-            _words("V", V, (E, self.d), self.dtype, dev),
-            None if log_m is None else _words("log_m", log_m, (E,), torch.float32, dev),
-            _words("offsets", offsets, (self.L * self.G + 1,), torch.int64, dev), E, self._ws,
-            self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens))
+        self._run(lib().gracekv_paged_load, self._ref, *self._packed(b, K, V, log_m, offsets), self._ws,
+                  self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens))
 
     def load(self, b: int, cache: Cache, n_entries: int, stream=None):
         """A compressed cache (Compressor's output) as request b, replacing what the
-        slot held.  Reads the offsets back to the host once."""
+        slot held; refused, the slot keeps it.  Reads the offsets back to the host once."""
         import numpy as np
         self._own_pages()
+        if not 0 <= n_entries <= cache.K.shape[0]:
+            raise _bad(f"{n_entries} entries of {cache.K.shape[0]}")
+        args = (cache.K[:n_entries], cache.V[:n_entries], None if self.log_m is None else cache.log_m[:n_entries], cache.offsets)
+        self._packed(b, *args)
+        self._on(stream)
         s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
         with torch.cuda.stream(s):
             off = cache.offsets.cpu().numpy()
         counts = np.diff(off)
-        if off[0] < 0 or counts.min() < 0 or off[-1] > n_entries or n_entries > cache.K.shape[0]:
+        if off[0] < 0 or counts.min() < 0 or off[-1] > n_entries:
             raise _bad("the cache's offsets do not fit its entries")
-        if not 0 <= b < self.B:
-            raise _bad(f"request {b} of {self.B}")
         need = -(-counts // self.page_size)
         held = int((self._host_table[:, b] >= 0).sum())
         if need.max() > self.max_pages or need.sum() > self._n_free + held:
@@ -765,8 +777,7 @@ class PagedCache(_Workspace):
         new = self._host_lens.copy()
         new[:, b] = counts.reshape(self.L, self.G)
         self._grow(new, s)
-        self.load_packed(b, cache.K[:n_entries], cache.V[:n_entries],
-                         None if self.log_m is None else cache.log_m[:n_entries], cache.offsets, stream)
+        self.load_packed(b, *args, stream)
 
     def advance(self, counts=None, stream=None):
         """The next step's tokens: counts[b] of each request (default: one for every

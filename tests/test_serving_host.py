@@ -2,6 +2,7 @@
 are stand-ins, so that what reaches a launch, and what does not, can be seen."""
 import contextlib
 import types
+from ctypes import c_int32
 
 import pytest
 import torch
@@ -110,3 +111,92 @@ def test_a_stream_of_another_device_is_refused(on_device_1, name):
     assert e.value.status == gk.GKV_EINVAL and not lib.seen
     calls[name](stream=types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=7))
     assert lib.seen == [("gracekv_" + name, 1)]
+
+
+# ------------------------------------------------------- pages that the cache hands out
+L, B, G, HQ, D, PS = 2, 3, 2, 4, 64, 16
+
+
+class PageLib:
+    """gracekv_paged_advance on host memory; the other calls succeed without doing anything."""
+
+    def __init__(self):
+        self.cache = None
+
+    def gracekv_paged_advance(self, ref, cu, stream):
+        c = self.cache
+        n = torch.tensor((c_int32 * (c.B + 1)).from_address(cu)).diff() if cu else None
+        for b in range(c.B):
+            c.lens[:, b] += (c.lens[:, b] > 0).int() if n is None else int(n[b])
+        return gk.GKV_OK
+
+    def __getattr__(self, name):
+        return lambda *a: gk.GKV_OK
+
+
+@pytest.fixture
+def pages(monkeypatch):
+    """A function that makes caches of their own pages on the CPU."""
+    lib = PageLib()
+
+    def make_workspace(self, n, dev):
+        self.workspace, self._device, self._ws, self._own_stream = torch.zeros(256, dtype=torch.uint8), torch.device("cpu"), 0, 0
+
+    monkeypatch.setattr(gk, "lib", lambda: lib)
+    monkeypatch.setattr(gk._Workspace, "_make_workspace", make_workspace)
+    monkeypatch.setattr(gk._Workspace, "_on", lambda self, stream, *t: 0)
+    monkeypatch.setattr(gk._Workspace, "_run", lambda self, call, *a: gk._raise(call(*a)))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+
+    def make(**kw):
+        lib.cache = gk.PagedCache.allocate(**(dict(L=L, B=B, G=G, Hq=HQ, d=D, dtype=BF, n_pages=40, max_pages=5, page_size=PS,
+                                                   device="cpu") | kw))
+        return lib.cache
+    return make
+
+
+def packed(counts, d=D, dtype=BF, lg=None):
+    off = torch.tensor([0] + list(counts)).cumsum(0)
+    c = gk.Cache.empty(int(off[-1]), d, len(counts) if lg is None else lg, dtype, device="cpu")
+    c.log_m.zero_()
+    c.offsets.copy_(off) if lg is None else c.offsets.zero_()
+    return c, int(off[-1])
+
+
+def state(c):
+    return c.table.clone(), c.lens.clone(), c._host_lens.copy(), c._host_table.copy(), c._n_free, sorted(c._free[:c._n_free])
+
+
+def same(a, b):
+    return all(torch.equal(x, y) if isinstance(x, torch.Tensor) else (x == y) if isinstance(x, (int, list)) else (x == y).all()
+               for x, y in zip(a, b))
+
+
+def test_a_refused_load_changes_nothing(pages):
+    c = pages()
+    c.load(1, *packed([16, 17, 1, 3]))
+    before = state(c)
+    good, n = packed([20, 1, 1, 1])
+    bad = [
+        (1, packed([20, 1, 1, 1], dtype=torch.float32)[0], n),            # another type
+        (1, packed([20, 1, 1, 1], d=128)[0], n),                          # another head size
+        (1, packed([20, 1, 1, 1], lg=6)[0], n),                           # offsets of another L x G
+        (1, good, n + 1), (1, good, -1), (3, good, n), (-1, good, n),
+        (1, gk.Cache(*(getattr(good, f) if f != "V" else good.V[:5] for f in ("K", "V", "pos", "log_m", "src_lo", "src_hi", "offsets"))), n),
+        (1, gk.Cache(*(getattr(good, f) if f != "log_m" else good.log_m.double() for f in ("K", "V", "pos", "log_m", "src_lo", "src_hi", "offsets"))), n),
+        (1, packed([90, 1, 1, 1])[0], 93),                                # more pages than a sequence may have
+    ]
+    for b, cache, m in bad:
+        with pytest.raises((gk.GraceKVError, ValueError)):
+            c.load(b, cache, m)
+        assert same(state(c), before), (b, m)
+    with pytest.MonkeyPatch.context() as m:                               # a stream of another device
+        def refuse(self, stream, *t):
+            raise gk.GraceKVError(gk.GKV_EINVAL, "stream")
+        m.setattr(gk._Workspace, "_on", refuse)
+        with pytest.raises(gk.GraceKVError):
+            c.load(1, good, n, stream=object())
+        assert same(state(c), before)
+    c.load(1, good, n)
+    assert c._host_lens[:, 1].tolist() == [[20, 1], [1, 1]] and c._host_lens[:, [0, 2]].sum() == 0
