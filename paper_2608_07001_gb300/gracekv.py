@@ -780,23 +780,33 @@ class PagedCache(_Workspace):
         self.load_packed(b, *args, stream)
 
     def advance(self, counts=None, stream=None):
-        """The next step's tokens: counts[b] of each request (default: one for every
-        request with entries).  Lengths grow, pages are assigned; returns the
-        device cu_new of the appends (None with the default)."""
+        """The next step's tokens: counts[b] of each request.  Lengths grow, pages are
+        assigned; returns the device cu_new of the appends.  Default: one token for
+        every request with entries, in all its heads, and None.  (Where the pages are
+        the caller's, for every head with entries: gracekv_paged_advance without cu_new.)"""
         import numpy as np
+        self._on(stream)
         s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
-        cu = None
+        n = counts
         if counts is not None:
-            counts = np.asarray(counts, dtype=np.int64)
+            n = counts = np.asarray(counts, dtype=np.int64)
             if counts.shape != (self.B,) or counts.min() < 0:
                 raise _bad("counts is one token count per request")
-            with torch.cuda.stream(s):
-                cu = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(self.K.device)
         if self._free is not None:
-            add = (self._host_lens > 0) if counts is None else counts[None, :, None]
-            self._grow(self._host_lens + add, s)
+            if counts is None:
+                held = self._host_lens > 0
+                active = held.any(axis=(0, 2))
+                if not held[:, active].all():         # a head without entries: the library would leave it idle
+                    n = active
+                self._grow(self._host_lens + active[None, :, None], s)
+            else:
+                self._grow(self._host_lens + counts[None, :, None], s)
+        cu = None
+        if n is not None:
+            with torch.cuda.stream(s):
+                cu = torch.from_numpy(np.concatenate([[0], np.cumsum(n)]).astype(np.int32)).to(self.K.device)
         self.advance_by(cu, stream)
-        return cu
+        return None if counts is None else cu
 
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""

@@ -200,3 +200,20 @@ def test_a_refused_load_changes_nothing(pages):
         assert same(state(c), before)
     c.load(1, good, n)
     assert c._host_lens[:, 1].tolist() == [[20, 1], [1, 1]] and c._host_lens[:, [0, 2]].sum() == 0
+
+
+def test_a_request_that_takes_a_token_takes_it_in_every_head(pages):
+    # a head that holds nothing belongs to its request all the same; a request without entries is idle
+    c = pages()
+    c.load(1, *packed([16, 0, 0, 3]))
+    c.lens[:, 1] = torch.tensor([[16, 0], [0, 3]], dtype=torch.int32)         # as gracekv_paged_load writes them
+    for step in range(1, 4):
+        assert c.advance() is None
+        want = torch.zeros(L, B, G, dtype=torch.int32)
+        want[:, 1] = torch.tensor([[16, 0], [0, 3]]) + step
+        assert torch.equal(c.lens, want) and (c._host_lens == want.numpy()).all()
+        need = -(-want // PS)
+        assert torch.equal((c.table >= 0).sum(-1), need)                      # every entry has its page
+    c.release(1)
+    c.lens[:, 1] = 0
+    assert c.advance() is None and int(c.lens.sum()) == 0 and c._n_free == 40
