@@ -766,6 +766,8 @@ class PagedCache(_Workspace):
         s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
         with torch.cuda.stream(s):
             off = cache.offsets.cpu().numpy()
+            if self.log_m is None and bool((cache.log_m[:n_entries] != 0).any()):
+                raise _bad("entries of several tokens (log m above 0), and this cache keeps no log m")
         counts = np.diff(off)
         if off[0] < 0 or counts.min() < 0 or off[-1] > n_entries:
             raise _bad("the cache's offsets do not fit its entries")

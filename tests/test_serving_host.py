@@ -217,3 +217,21 @@ def test_a_request_that_takes_a_token_takes_it_in_every_head(pages):
     c.release(1)
     c.lens[:, 1] = 0
     assert c.advance() is None and int(c.lens.sum()) == 0 and c._n_free == 40
+
+
+def test_multiplicities_are_not_dropped(pages):
+    # a cache without log m takes a packed one whose entries are single tokens, and no other
+    c = pages(log_m=False)
+    cache, n = packed([16, 17, 1, 3])
+    c.load(1, cache, n)
+    before = state(c)
+    cache.log_m[20] = 0.7
+    with pytest.raises(gk.GraceKVError) as e:
+        c.load(1, cache, n)
+    assert e.value.status == gk.GKV_EINVAL and same(state(c), before)
+    cache.log_m[20] = 0.0
+    more = gk.Cache.empty(n + 5, D, L * G, BF, device="cpu")        # capacity past the entries holds anything
+    more.log_m.fill_(3.0)
+    more.log_m[:n] = 0
+    more.offsets.copy_(cache.offsets)
+    c.load(1, more, n)
