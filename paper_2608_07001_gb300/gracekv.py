@@ -831,6 +831,7 @@ class PagedCache(_Workspace):
         self._host_lens[:, b] = 0
         with torch.cuda.stream(s):
             self.lens[:, b] = 0
+            self.table[:, b] = -1           # the pages are another request's next: no word leads to them
 
     def append(self, l: int, k, v, pos, q=None, cu_new=None, out=None, stream=None):
         """Layer l's new tokens: k, v [N, G, d] into the pages (k rotated to pos [N]

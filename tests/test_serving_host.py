@@ -235,3 +235,16 @@ def test_multiplicities_are_not_dropped(pages):
     more.log_m[:n] = 0
     more.offsets.copy_(cache.offsets)
     c.load(1, more, n)
+
+
+def test_a_released_slot_leads_to_no_page(pages):
+    # words of a page that has gone back must not be followed: the page is another request's next
+    c = pages()
+    c.load(1, *packed([40, 17, 1, 3]))
+    c.load(2, *packed([5, 5, 5, 5]))
+    kept = c.table[:, 2].clone()
+    c.release(1)
+    assert (c.table[:, 1] == -1).all() and torch.equal(c.table[:, 2], kept)
+    c.load(1, *packed([1, 1, 1, 1]))
+    assert torch.equal((c.table >= 0).sum(-1)[:, 1], torch.ones(L, G, dtype=torch.int64))
+    assert (torch.from_numpy(c._host_table) == c.table).all()
