@@ -561,7 +561,8 @@ def _words(name: str, t: torch.Tensor, shape, dtype, device):
 
 class _Workspace:
     """A zeroed workspace, usable on any one stream at a time: its zeros are there
-    before the constructor returns, and it stays alive for the streams it is used on."""
+    before the constructor returns, and it and what else the object made stay alive
+    for the streams that they are used on."""
 
     def _make_workspace(self, n: int, device):
         self.workspace = torch.zeros(n, dtype=torch.uint8, device=device)
@@ -569,6 +570,7 @@ class _Workspace:
         own = torch.cuda.current_stream(self._device)
         own.synchronize()
         self._own_stream = own.cuda_stream
+        self._made, self._used_on = [self.workspace], set()
 
     def _run(self, call, *args):
         """A call of the library with the tensors' device current: it launches on the current one."""
@@ -582,8 +584,10 @@ class _Workspace:
         """The raw stream of a call; tensors used on an explicit stream stay alive for it."""
         if stream is None:
             raw = torch._C._cuda_getCurrentRawStream(self._device.index)
-            if raw != self._own_stream:
-                self.workspace.record_stream(torch.cuda.current_stream(self._device))
+            if raw != self._own_stream and raw not in self._used_on:
+                for t in self._made:
+                    t.record_stream(torch.cuda.current_stream(self._device))
+                self._used_on.add(raw)
             return raw
         if stream.device != self._device:
             raise _bad(f"the stream is on {stream.device}, the tensors are on {self._device}")
@@ -700,6 +704,7 @@ class PagedCache(_Workspace):
                        torch.full((L, B, G, max_pages), -1, dtype=torch.int32, device=device),
                        torch.zeros(L, B, G, dtype=torch.int32, device=device), Hq=Hq, rope_base=rope_base,
                        log_m=torch.empty(n_pages, page_size, device=device) if log_m else None)
+        c._made += [t for t in (c.K, c.V, c.log_m, c.table, c.lens) if t is not None]
         c._free = np.arange(n_pages - 1, -1, -1, dtype=np.int32)     # a stack: the last one goes next
         c._n_free = n_pages
         c._host_lens = np.zeros((L, B, G), np.int64)
@@ -813,7 +818,7 @@ class PagedCache(_Workspace):
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
         p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
-        self._run(lib().gracekv_paged_advance, self._ref, p, self._on(stream, self.lens, cu_new))
+        self._run(lib().gracekv_paged_advance, self._ref, p, self._on(stream, self.table, self.lens, cu_new))
 
     def release(self, b: int, stream=None):
         """Request b's pages return to the pool; the slot is idle."""
@@ -821,6 +826,7 @@ class PagedCache(_Workspace):
         self._own_pages()
         if not 0 <= b < self.B:
             raise _bad(f"request {b} of {self.B}")
+        self._on(stream, self.table, self.lens)
         s = stream if stream is not None else torch.cuda.current_stream(self.K.device)
         held = self._host_table[:, b]
         pages = held[held >= 0]

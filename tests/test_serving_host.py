@@ -68,6 +68,7 @@ def on_device_1(monkeypatch):
 
     def make_workspace(self, n, dev):
         self.workspace, self._device, self._ws, self._own_stream = Tensor(n, dtype=torch.uint8), torch.device("cuda", 1), 1 << 20, 0
+        self._made, self._used_on = [self.workspace], set()
 
     monkeypatch.setattr(gk, "lib", lambda: lib)
     monkeypatch.setattr(gk._Workspace, "_make_workspace", make_workspace)
@@ -141,6 +142,7 @@ def pages(monkeypatch):
 
     def make_workspace(self, n, dev):
         self.workspace, self._device, self._ws, self._own_stream = torch.zeros(256, dtype=torch.uint8), torch.device("cpu"), 0, 0
+        self._made, self._used_on = [self.workspace], set()
 
     monkeypatch.setattr(gk, "lib", lambda: lib)
     monkeypatch.setattr(gk._Workspace, "_make_workspace", make_workspace)
@@ -248,3 +250,27 @@ def test_a_released_slot_leads_to_no_page(pages):
     c.load(1, *packed([1, 1, 1, 1]))
     assert torch.equal((c.table >= 0).sum(-1)[:, 1], torch.ones(L, G, dtype=torch.int64))
     assert (torch.from_numpy(c._host_table) == c.table).all()
+
+
+def test_what_an_object_made_stays_for_the_streams_it_is_used_on(pages, monkeypatch):
+    # the workspace, and the pool, table and lengths of a cache of its own pages: none of them is reused while work of
+    # another current stream is queued
+    monkeypatch.undo()
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: types.SimpleNamespace(
+        synchronize=lambda: None, cuda_stream=0, device=torch.device("cpu")))
+    seen = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: seen.append(self.data_ptr()))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: now[0], raising=False)
+    now = [0]
+    c = gk.PagedCache.allocate(L=L, B=B, G=G, Hq=HQ, d=D, dtype=BF, n_pages=4, max_pages=2, page_size=PS, device="cpu")
+    own = {t.data_ptr() for t in (c.workspace, c.K, c.V, c.log_m, c.table, c.lens)}
+    assert len(own) == 6
+    c._on(None)
+    assert not seen                                          # the stream they were made on
+    now[0] = 5
+    c._on(None)
+    assert set(seen) == own
+    seen.clear()
+    theirs = gk.PagedCache(c.K, c.V, c.table, c.lens, log_m=c.log_m, Hq=HQ)
+    theirs._on(None)
+    assert seen == [theirs.workspace.data_ptr()]             # the caller's tensors are the caller's to keep
