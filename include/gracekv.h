@@ -476,7 +476,8 @@ gkv_status gracekv_decode_status(void *workspace, void *stream);
  * element (token, head, channel) at token * ts + head * hs + channel with the
  * tensor's own strides in elements (so [N][Hq][d], [Hq][N][d] and a slice of a
  * fused projection all pass); k, v the same with G heads.  out may not overlap
- * the inputs.  n_q and n_k bound the rows: a sequence whose cu words run
+ * the inputs, nor its rows each other (a stride below d is refused where its axis
+ * has several rows).  n_q and n_k bound the rows: a sequence whose cu words run
  * backwards or past them is skipped and reported by gracekv_prompt_status; so is
  * one that, after such words, has query rows below the end of an earlier sequence.
  * The others are computed.
@@ -570,7 +571,8 @@ gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new
 
 /* The new tokens of one layer (device pointers; strides in elements, of tokens
  * and heads, as in gkv_prompt): pos [n_tokens]; k, v [n_tokens][G][d]; q and
- * q_out [n_tokens][Hq][d], both NULL without queries; q_out may be q itself.
+ * q_out [n_tokens][Hq][d], both NULL without queries; q_out may be q itself, and
+ * its rows may not share memory.
  * cu_new [B + 1]: token t belongs to request b with cu_new[b] <= t <
  * cu_new[b + 1]; NULL: n_tokens = B and token t is request t's. */
 typedef struct {

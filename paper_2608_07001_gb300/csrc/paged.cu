@@ -350,7 +350,9 @@ extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, 
         return GKV_EINVAL;
     const void *q = t->q;
     if ((q != nullptr) != (t->q_out != nullptr)) return GKV_EINVAL;
-    if (q && (!rows_ok(q, t->q_ts, t->q_hs, c->dtype) || !rows_ok(t->q_out, t->qo_ts, t->qo_hs, c->dtype))) return GKV_EINVAL;
+    if (q && (!rows_ok(q, t->q_ts, t->q_hs, c->dtype) ||
+              !out_ok(t->q_out, t->qo_ts, t->qo_hs, c->dtype, n_tokens, c->Hq, c->d)))
+        return GKV_EINVAL;
     const int es = elem_bytes(c->dtype);
     const AppendArgs a{paged_of(c), l, n_tokens, t->cu_new, t->pos, static_cast<const char *>(t->k),
                        static_cast<const char *>(t->v), static_cast<const char *>(q), static_cast<char *>(t->q_out),

@@ -143,7 +143,8 @@ gkv_status check_prompt(const gkv_prompt *p) {
     if (st != GKV_OK) return st;
     if (p->n_seqs < 0 || p->n_q < 0 || p->n_k < 0 || p->n_q > (1LL << 31) - 4096 || p->n_k > (1LL << 31) - 4096) return GKV_EINVAL;
     if (!p->cu_q || !p->cu_k || !al(p->cu_q, 4) || !al(p->cu_k, 4) || !al(p->lse, 4)) return GKV_EINVAL;
-    if (p->n_q > 0 && (!rows_ok(p->q, p->q_ts, p->q_hs, p->dtype) || !rows_ok(p->out, p->o_ts, p->o_hs, p->dtype)))
+    if (p->n_q > 0 && (!rows_ok(p->q, p->q_ts, p->q_hs, p->dtype) ||
+                       !out_ok(p->out, p->o_ts, p->o_hs, p->dtype, p->n_q, p->Hq, p->d)))
         return GKV_EINVAL;
     if (p->n_k > 0 && (!rows_ok(p->k, p->k_ts, p->k_hs, p->dtype) || !rows_ok(p->v, p->v_ts, p->v_hs, p->dtype)))
         return GKV_EINVAL;

@@ -29,6 +29,11 @@ inline bool rows_ok(const void *p, int64_t ts, int64_t hs, int dtype) {
     return p && al(p, 16) && ts >= 0 && hs >= 0 && ts % q == 0 && hs % q == 0 && ts < (1LL << 40) && hs < (1LL << 40);
 }
 
+// The same for a tensor that is written: no two of its n x heads rows of d share an element by one stride alone.
+inline bool out_ok(const void *p, int64_t ts, int64_t hs, int dtype, int64_t n, int heads, int d) {
+    return rows_ok(p, ts, hs, dtype) && (n < 2 || ts >= d) && (heads < 2 || hs >= d);
+}
+
 // The sequence holding row i: the last s with cu[s] <= i.  cu is [n + 1],
 // n >= 1; any contents end the search inside [0, n).
 __device__ __forceinline__ int seq_of(const int32_t *cu, int n, int64_t i) {
