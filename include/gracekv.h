@@ -587,7 +587,9 @@ typedef struct {
  * values stored, log m = 0 (App. A.5: appended tokens have multiplicity 1),
  * queries rotated into q_out.  Token t of request b becomes entry
  * lens[l][b][g] - (cu_new[b + 1] - t): the lengths count the new tokens already
- * (gracekv_paged_advance).  A negative index (an idle request) stores nothing.
+ * (gracekv_paged_advance).  A negative index (an idle request) stores nothing, nor
+ * does a token of no request.  cu_new words that run backwards or past n_tokens
+ * are reported by gracekv_paged_status; which of their tokens are stored is open.
  * Rotation of a vector x to position p: the pair (x[i], x[i + d/2]) turns by
  * p * rope_base^(-2 i / d), computed in fp32 from an angle that is exact to
  * 2^-26 turns at every int32 position, rounded once.  Errors: GKV_EINVAL

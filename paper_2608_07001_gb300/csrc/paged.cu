@@ -108,6 +108,13 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
     next_may_start();
     after_previous();
+    if (a.cu_new && blockIdx.x == gridDim.x - 1) {       // a block for the bounds alone, out of the others' way
+        for (int b = threadIdx.x; b < a.c.B; b += 256) {
+            const int lo = a.cu_new[b], hi = a.cu_new[b + 1];
+            if (lo < 0 || hi < lo || hi > a.n_tokens) atomicOr(a.status, kStRange);
+        }
+        return;
+    }
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0), stride = (rows + R - 1) / R;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int ch = (int)(i % CH);
@@ -181,7 +188,7 @@ cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t 
     const int64_t one = (int64_t)a.n_tokens * rows * CH;
     const bool many = one >= kAppendMany;
     const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 3) / 4) * CH : one;
-    const unsigned n = (unsigned)((threads + 255) / 256);
+    const unsigned n = (unsigned)((threads + 255) / 256) + (a.cu_new ? 1 : 0);
     return launch_overlapped(many ? paged_append_kernel<T, D, 4> : paged_append_kernel<T, D, 1>, n, 256, 0, s, a, turns);
 }
 
@@ -359,7 +366,7 @@ extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, 
                        t->k_ts * es, t->k_hs * es, t->v_ts * es, t->v_hs * es, t->q_ts * es, t->q_hs * es,
                        t->qo_ts * es, t->qo_hs * es, c->rope_base > 0.0, static_cast<int *>(workspace)};
     const int64_t items = (int64_t)n_tokens * (2 * c->G + (q ? c->Hq : 0)) * (c->d * es / 32);
-    if ((items + 255) / 256 >= (1LL << 31)) return GKV_EUNSUPPORTED;
+    if ((items + 255) / 256 + 1 >= (1LL << 31)) return GKV_EUNSUPPORTED;
     const Turns &turns = turns_of(c->rope_base, c->d);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = c->dtype == GKV_BF16

@@ -61,3 +61,34 @@ def test_in_place_rotation_and_attention_in_a_chain(gk, dtype, B, d):
     for _ in range(3):
         for a, b in zip(steps(False), want):
             assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------- append's row bounds
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cu,bad", [([0, 2, 2, 5], False), ([0, 2, 2, 4], False), ([0, 5, 2, 5], True), ([0, 2, 9, 5], True),
+                                    ([0, 2, 2, 9], True), ([-1, 2, 2, 5], True), ([0, 0, 0, 0], False)])
+@pytest.mark.parametrize("tokens", [5, 3000])
+def test_append_reports_bounds_that_do_not_fit(gk, cu, bad, dtype, tokens):
+    # tokens past the last bound are of no request (a batch padded to a size): not stored, not reported
+    G, ps, d = 2, 16, 64
+    cu = [w * (tokens // 5) for w in cu]
+    pages = -(-tokens * 2 // ps)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    K, V = (torch.empty(3 * G * pages, ps, d, dtype=dtype, device="cuda").normal_(generator=g) for _ in range(2))
+    table = torch.arange(3 * G * pages, **I32).view(1, 3, G, pages)
+    lens = torch.full((1, 3, G), tokens * 2 - 3, **I32)
+    k, v = (torch.empty(tokens, G, d, dtype=dtype, device="cuda").normal_(generator=g) for _ in range(2))
+    c = gk.PagedCache(K, V, table, lens, Hq=G)
+    before = K.clone()
+    c.append(0, k, v, torch.zeros(tokens, **I32), cu_new=torch.tensor(cu, **I32))
+    if bad:
+        with pytest.raises(gk.GraceKVError) as e:
+            c.status()
+        assert e.value.status == gk.GKV_EINVAL
+        return
+    c.status()
+    want = before.view(3, G, pages * ps, d)
+    for b in range(3):
+        n = cu[b + 1] - cu[b]
+        want[b, :, tokens * 2 - 3 - n:tokens * 2 - 3] = k[cu[b]:cu[b + 1]].transpose(0, 1)
+    assert torch.equal(K.view(3, G, pages * ps, d), want)
