@@ -591,10 +591,11 @@ typedef struct {
  * does a token of no request.  cu_new words that run backwards or past n_tokens
  * are reported by gracekv_paged_status; which of their tokens are stored is open.
  * Rotation of a vector x to position p: the pair (x[i], x[i + d/2]) turns by
- * p * rope_base^(-2 i / d), computed in fp32 from an angle that is exact to
- * 2^-26 turns at every int32 position, rounded once.  Errors: GKV_EINVAL
- * (n_tokens < 0, n_tokens != B without cu_new, pointers, strides, a rope_base
- * neither 0 nor a finite number of at least 1), GKV_ECUDA. */
+ * p * rope_base^(-2 i / d), computed in fp32 from an angle that is off by at most
+ * 2^-25.9 + |p| 2^-53 turns (2^-25 up to positions of 2^27, 2^-21 at the ends of
+ * int32), rounded once.  Errors: GKV_EINVAL (n_tokens < 0, n_tokens != B without
+ * cu_new, pointers, strides, a rope_base neither 0 nor a finite number of at least
+ * 1), GKV_ECUDA. */
 gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t, void *workspace,
                                 void *stream);
 

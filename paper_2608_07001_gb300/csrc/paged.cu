@@ -9,15 +9,17 @@
 // a sin phi + b cos phi).  p can be large while only phi mod 2 pi counts, so
 // the angle is kept in turns as a 64-bit fraction: F_i = 2^64 theta_i / (2 pi)
 // (host, fp64), and p F_i mod 2^64 is the fraction of a turn -- one integer
-// product whose error is |p| times that of F_i, a few 2^-56 turns -- and its
-// upper 32 bits go to sincospi.  A thread holds 16 bytes of each half of a row,
-// so the rotation stays in its registers; its sines and cosines serve every
-// row that it takes.
+// product whose error is |p| times that of F_i, which two powers, a product and a
+// quotient in fp64 keep below 2^-53 turns (2^-55 found for bases from 1 to 1e7).
+// Its upper 32 bits, rounded to the 24 of a float (2^-26 turns), go to sincospi.  A
+// thread holds 16 bytes of each half of a row, so the rotation stays in its
+// registers; its sines and cosines serve every row that it takes.
 //
 // Both move 2 es d bytes a row (in and out) and are bound by HBM, or by the
-// latency of a launch for a few tokens: 128 us for 32768 tokens of 32 + 2 x 8
-// rows of 128 bf16 (805 MB, 6.3 TB/s), 2.5 us for one token; load 164 us for 1M
-// entries of 2 x 128 bf16 (1082 MB, 6.6 TB/s).
+// latency of a launch for a few tokens.  GPU time: 128 us for 32768 tokens of
+// 32 + 2 x 8 rows of 128 bf16 (805 MB, 6.3 TB/s; 16384 tokens of fp32 120 us,
+// 6.7 TB/s), 2.5 us for one token (a call from Python takes 10 to 12); load
+// 163 us for 1M entries of 2 x 128 bf16 (1082 MB, 6.6 TB/s).
 #include "paged.cuh"
 
 #include <math.h>

@@ -92,3 +92,32 @@ def test_append_reports_bounds_that_do_not_fit(gk, cu, bad, dtype, tokens):
         n = cu[b + 1] - cu[b]
         want[b, :, tokens * 2 - 3 - n:tokens * 2 - 3] = k[cu[b]:cu[b + 1]].transpose(0, 1)
     assert torch.equal(K.view(3, G, pages * ps, d), want)
+
+
+# --------------------------------------------------------------- the rotation's angle
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("base", [1.0, 1.0001, 2.0, 1e4, 5e5, 1e7])
+def test_angles_at_every_size_of_position(gk, base, d):
+    """Against exact turns.  The angle is off by 2^-26 turns (a fraction of 24 bits), 2^-32 (its upper word) and |p|
+    times the stored turn's error, below 2^-53 (two powers, a product and a quotient in fp64 of a turn of at most
+    1 / 2 pi); sine and cosine of it by 2^-23; a unit vector's rotation adds no rounding."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    two_pi = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534")
+    pos = [0, 1, -1, 7, 4095, 131071, (1 << 20) + 1, (1 << 24) + 1, (1 << 27) - 1, 123456789, -987654321, (1 << 30) + 12345,
+           (1 << 31) - 1, -(1 << 31)]
+    x = torch.zeros(len(pos), 1, d, device="cuda")
+    x[:, :, :d // 2] = 1.0
+    K = torch.zeros(1, 16, d, device="cuda")
+    c = gk.PagedCache(K, K.clone(), torch.zeros(1, 1, 1, 1, **I32), torch.tensor([[[len(pos)]]], **I32), Hq=1, rope_base=base)
+    q = c.append(0, x, x, torch.tensor(pos, **I32), q=x, cu_new=torch.tensor([0, len(pos)], **I32))
+    c.status()
+    assert torch.equal(q[:, 0], K[0, :len(pos)])
+    q = q[:, 0].double().cpu().numpy()
+    for i in range(d // 2):
+        turn = (Decimal(base).ln() * Decimal(-2 * i) / Decimal(d)).exp() / two_pi
+        for t, p in enumerate(pos):
+            a = 2 * math.pi * float((Decimal(p) * turn) % 1)
+            tol = 2 * math.pi * (2.0 ** -26 + 2.0 ** -32 + abs(p) * 2.0 ** -53) + 2.0 ** -22
+            assert abs(q[t, i] - math.cos(a)) <= tol and abs(q[t, i + d // 2] - math.sin(a)) <= tol, (i, p)
+
