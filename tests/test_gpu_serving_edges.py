@@ -8,6 +8,8 @@ import pytest
 import torch
 
 from . import serving_reference as R
+from .test_gpu_paged import append_case
+from .test_gpu_prompt import check, cu, inputs
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -121,3 +123,103 @@ def test_angles_at_every_size_of_position(gk, base, d):
             tol = 2 * math.pi * (2.0 ** -26 + 2.0 ** -32 + abs(p) * 2.0 ** -53) + 2.0 ** -22
             assert abs(q[t, i] - math.cos(a)) <= tol and abs(q[t, i + d // 2] - math.sin(a)) <= tol, (i, p)
 
+
+# ------------------------------------------------------- what ordinary sizes do not take
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [31, 32, 33, 64, 65, 300, 1100])
+def test_prompts_of_many_sequences(gk, n, d, dtype):
+    lens = [int(x) for x in np.random.default_rng(n).integers(0, 12, n)]
+    lens[n // 2] = 200
+    t = sum(lens)
+    check(gk, *inputs(n, t, t, 4, 2, d, dtype), cu(lens), cu(lens))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [20, 40, 70])
+def test_many_sequences_whose_keys_are_split(gk, n, dtype):
+    # one or two queries each over a few thousand keys, one sequence with none
+    rng = np.random.default_rng(n)
+    nq, nk = rng.integers(1, 3, n), rng.integers(1000, 2500, n)
+    nk[3] = 0
+    nq[5] = 0
+    check(gk, *inputs(n, int(nq.sum()), int(nk.sum()), 4, 1, 64, dtype), cu(nq.tolist()), cu(nk.tolist()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("which", ["query token", "query head", "key token", "value token"])
+@pytest.mark.parametrize("nq,nk", [(200, 200), (3, 4000), (70, 900)])
+def test_bf16_tensors_without_a_tensor_map(gk, nq, nk, which, d):
+    # an axis broadcast by a zero stride has no tensor map: these run on CUDA cores, whole and in parts
+    q, k, v = (t.cuda() for t in inputs(nq, nq, nk, 8, 2, d, BF))
+    if which == "query token":
+        q = q[:1].expand(nq, 8, d)
+    elif which == "query head":
+        q = q[:, :1].expand(nq, 8, d)
+    elif which == "key token":
+        k = k[:1].expand(nk, 2, d)
+    else:
+        v = v[:1].expand(nk, 2, d)
+    check(gk, q, k, v, cu([nq]), cu([nk]))
+    lens = [1, 0, nq - 1]
+    keys = [0, 5, nk - 5]
+    check(gk, q, k, v, cu(lens), cu(keys))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_rows_past_2_31_elements(gk, d, dtype):
+    # tokens 2^24 elements apart: the last rows begin past 2^31 elements (and 2^32 bytes)
+    n, Hq, G = 180, 4, 2
+    buf = torch.empty(n, 1 << 24, dtype=dtype, device="cuda")
+    q, k, v = inputs(n, n, n, Hq, G, d, dtype)
+    at, views = 1 << 23, []
+    for t in (q, k, v, q):
+        w = t.shape[1] * d
+        views.append(buf[:, at:at + w].view(n, t.shape[1], d))
+        at += w
+    for view, t in zip(views, (q, k, v)):
+        view.copy_(t)
+    c = torch.tensor([0, 100, n], **I32)
+    op = gk.PromptAttention(G=G, Hq=Hq, d=d, dtype=dtype)
+    op(*views[:3], c, out=views[3])
+    op.status()
+    assert torch.equal(views[3], op(q.cuda(), k.cuda(), v.cuda(), c))
+    for view, t in zip(views, (q, k, v)):
+        assert torch.equal(view.cpu(), t)                   # nothing was written beside the output
+    del buf, views
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,S", [(BF, 128), (F32, 64)])
+def test_attention_over_more_tiles_than_32_bits_hold_products_of(gk, dtype, S):
+    """4.3 million tiles, of a few pages that the tables name again and again.  All logits are 0 and all values 1, 0 or -1,
+    so that every sum is a whole number that fp32 holds exactly: one entry too many or too few shows."""
+    ps, d = 4096, 64
+    m = (540 if dtype == BF else 530) // 2 * 2              # pages of a sequence
+    K, V = torch.zeros(2, ps, d, dtype=dtype, device="cuda"), torch.ones(2, ps, d, dtype=dtype, device="cuda")
+    V[1, :, 0] = -1                                         # channel 0: pages cancel; 1: one page of two; others: 1
+    V[1, :, 1] = 0
+    table = (torch.arange(m, device="cuda") % 2).to(torch.int32).repeat(S, 1).view(1, S // 2, 2, m).contiguous()
+    lens = torch.full((1, S // 2, 2), m * ps, **I32)
+    lens[0, 5] = torch.tensor([0, 2 * ps], **I32)
+    lens[0, 7, 1] = m * ps - 2 * ps
+    tile = 64 if dtype == BF else 32
+    assert int(lens.long().sum()) // tile > 1 << 22
+    c = gk.PagedCache(K, V, table, lens, Hq=4)
+    q = torch.randn(S // 2, 4, d, device="cuda").to(dtype)
+    out = c.attention(0, q)
+    c.status()
+    want = torch.ones(S // 2, 4, d, dtype=dtype, device="cuda")
+    want[..., 0], want[..., 1] = 0, 0.5
+    want[5, :2] = 0
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_many_tokens_to_several_requests(gk, d, dtype):
+    # four rows a thread, rows that do not divide by four
+    counts = [1500, 0, 900, 1]
+    append_case(gk, counts, [[0, 3, 7]] * 4, 48, 9, 3, d, dtype, 5e5, np.arange(2401) * 7, strided=True)
+    append_case(gk, counts, [[0, 3, 7]] * 4, 48, 6, 3, d, dtype, 0.0, np.arange(2401), with_q=False)
