@@ -109,3 +109,55 @@ def test_paged_attention_of_the_largest_log_m(gk, shape, dtype):
     bits = R.BITS_BF16 if dtype == BF else R.BITS_F32
     weights = 2.0 ** -16 if dtype == BF else 2.0 ** -24
     assert ((got - want).abs() <= vmax * (2.0 ** -20 + weights + 2.0 ** -24 * (n + 64)) + 2.0 ** -bits * want.abs() * 1.01).all()
+
+
+# ------------------------------------------------------------------- the prompt's attention
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,nk", [(300, 300), (5, 4000)])
+def test_prompt_attention_keeps_what_is_not_a_number(gk, nq, nk, d, dtype):
+    g = torch.Generator().manual_seed(nq)
+    q0, k0, v0 = (torch.randn(n, h, d, generator=g).to(dtype) for n, h in ((nq, 8), (nk, 2), (nk, 2)))
+    q0 = q0.abs()                                            # an infinite key gives an infinite logit of its sign
+    op = gk.PromptAttention(G=2, Hq=8, d=d, dtype=dtype)
+    cq, ck = torch.tensor([0, nq], **I32), torch.tensor([0, nk], **I32)
+
+    def run(q=q0, k=k0, v=v0):
+        out, lse = op(q.cuda(), k.cuda(), v.cuda(), cq, ck, return_lse=True)
+        op.status()
+        return out.cpu(), lse.cpu()
+
+    clean, lclean = run()
+    assert torch.isfinite(clean.float()).all()
+    # a query: its own row and head alone
+    q = q0.clone()
+    q[3, 5, 7] = math.nan
+    out, lse = run(q=q)
+    assert torch.isnan(out[3, 5]).all() and torch.isnan(lse[3, 5])
+    out[3, 5], lse[3, 5] = clean[3, 5], lclean[3, 5]
+    assert torch.equal(out, clean) and torch.equal(lse, lclean)
+    for e in (0, nk - nq + 2, nk - 1, nk // 2):
+        first = max(0, e - (nk - nq))                        # the first query that sees key e
+        for value in (math.nan, math.inf):
+            k = k0.clone()
+            k[e, 1, 9] = value
+            out, lse = run(k=k)
+            assert torch.isnan(out[first:, 4:]).all() and not torch.isfinite(lse[first:, 4:]).any()
+            assert torch.equal(out[:, :4], clean[:, :4]) and torch.equal(out[:first], clean[:first])
+            assert torch.equal(lse[:, :4], lclean[:, :4]) and torch.equal(lse[:first], lclean[:first])
+        # a logit of -inf weighs nothing, as one that is merely far below the others
+        k, far = k0.clone(), k0.clone()
+        k[e, 1, 9], far[e, 1, 9] = -math.inf, -1e30
+        if e > 0:
+            a, b = run(k=k), run(k=far)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        # a value: its channel alone, in every query that sees it
+        v = v0.clone()
+        v[e, 0, 2] = math.nan
+        out, lse = run(v=v)
+        assert torch.isnan(out[first:, :4, 2]).all() and torch.equal(lse, lclean)
+        out[..., :4, 2] = clean[..., :4, 2]
+        assert torch.equal(out, clean)
+    # all logits -inf: no weight at all
+    out, lse = run(k=torch.full_like(k0, -math.inf))
+    assert (out == 0).all() and torch.isinf(lse).all() and (lse < 0).all()
