@@ -26,7 +26,9 @@
 //     products, fp32 sums): the heads are the 16 rows, and since gq <= 8 the
 //     upper 8 rows carry the same queries again -- the logits come out twice,
 //     and the value product's rows 0-7 take the weights' bf16 part and rows
-//     8-15 the remainder's, two parts (2^-16 of a weight) for one product.
+//     8-15 the remainder's, two parts (2^-16 of a weight) for one product.  That is
+//     2^-8 of what rounding the output to bf16 moves; a third part, as for one
+//     request's packed cache (decode.cu), would double the value product.
 //     tcgen05 would need 128 rows for the same 8 heads.
 //   * fp32: a warp takes whole tiles of 32 entries, the tiles of its own stages
 //     of the ring; lanes are entries for the logits (no reduction) and channels for the values; packed fp32x2 FMA.
@@ -37,9 +39,10 @@
 //     them in order.  Nothing waits for another CTA, and results do not depend
 //     on timing.
 //
-// Measured: 87.5 us for 1M entries of 2 x 128 bf16 and log m (32 requests x 8
-// heads, uneven; 6.1 TB/s, 0.90 of a plain copy's rate), the same for one
-// request of 131072 entries; 6.1 us for one request of 8 x 256 entries.
+// Measured, GPU time: 88 us for 1M entries of 2 x 128 bf16 and log m (32 requests x 8
+// heads, uneven; 6.1 TB/s, 0.90 of a plain copy's rate), the same for one request of
+// 131072 entries; 6.1 us for one request of 8 x 256 entries (a call from Python
+// takes 8 to 11).
 //
 // log m joins in base 2 with log m log2(e) held between the finite values, so
 // that entries of the lowest or the largest log m keep equal weights; -inf stays

@@ -12,7 +12,7 @@
 // the issue slots, along the channels for S and across output columns for PV.
 // K of the next tile arrives (cp.async) under PV, V under S.  Two blocks a SM.
 // Measured: 52 TFLOP/s (32 / 8 heads of 128 at 4500 tokens; FMA pipe 67 % busy),
-// 48 at d = 64 (46 with the products unrolled by 2 instead of 8), 24 us for 1024
+// 48 at d = 64 (46 with the products unrolled by 2 instead of 8), 25 us for 1024
 // tokens of 2 heads: 13 us of a part's one tile, of which 3 issue its copies, 4
 // of the join, the rest launches.  256 threads of 4 x 4 scores: 44 TFLOP/s.
 //

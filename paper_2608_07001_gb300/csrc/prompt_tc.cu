@@ -22,6 +22,10 @@
 // 1 (11 idle: registers are split by warpgroup).  P is the A operand of its
 // product from TMEM, packed bf16 over the first half of its S; V is the B
 // operand as it lies in memory (rows of channels, "MN-major").
+// P is rounded to bf16 once, because A and B of a product have one type; its sum Z is
+// not.  A weight moves by 2^-8 of itself at most, as each output does when it is
+// rounded: outputs are 2.0 to 2.2e-3 from 64 bits where weights of 32 bits give 1.65e-3.
+// A second bf16 part of P would take half as much tensor work again.
 // TMEM, d = 128: S0, S1 of 128 keys, O0, O1.  tcgen05 operations of one thread
 // complete in order, so the commit of S(j + 1) also tells that PV(j) is done.
 // TMEM, d = 64: key tiles of 96, so that two S a row tile and O fill the 512
@@ -31,9 +35,10 @@
 // d = 64 a ring slot holds V(j) and K(j + 2), one wait and one commit for both,
 // and P is handed over at once.
 //
-// Measured (32 / 8 heads): 16384 tokens of d = 128 1.20 to 1.36 ms by the power
-// limit, 1.62 to 1.83 PFLOP/s of 1.88 that a plain matrix product reaches, the
-// tensor pipe 75 % busy at 8192 tokens; 12000 tokens of d = 64 0.48 ms, 1.23
+// Measured (32 / 8 heads; GPU time): 16384 tokens of d = 128 1.17 to 1.38 ms by the
+// power limit, 1.60 to 1.88 PFLOP/s of 1.88 that a plain matrix product reaches, the
+// tensor pipe 75 % busy at 8192 tokens (316 us); 12000 tokens of d = 64 0.48 to 0.57
+// ms by the power limit, 1.21
 // PFLOP/s.  d = 64 step by step: 128-key tiles, one S 560 us, the maximum with
 // the load 528, 96-key tiles and two S 532, one slot for V and K 511, P at once
 // 509, a faster start and end of a block 497, no vote at a wait and the loop by
