@@ -610,6 +610,62 @@ gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_p
 gkv_status gracekv_paged_attention(const gkv_paged_cache *c, int32_t l, const void *q, void *out, void *workspace,
                                    void *stream);
 
+/*
+ * A quantised paged cache: the gkv_paged_cache above, its dtype that of k, v, q
+ * and out, whose pools K and V hold one byte an element (e4m3 codes,
+ * [n_pages][page_size][d], on 16 bytes) and whose rows have a scale each,
+ * [n_pages][page_size], on 16 bytes.  Element j of a row stands for
+ * code_j 2^(byte - 127).  What these calls write of a row x:
+ *     e = the smallest integer of [-120, 119] with max |x_j| <= 448 2^e over its
+ *     finite values,  code_j = x_j 2^-e to nearest even,  byte = e + 127 ;
+ * NaN and infinity become NaN codes, larger values than 448 2^119 become that.
+ * A value is off by at most 2^-4 of itself, or 2^-10 2^e where that is more, and
+ * exact in bf16 and fp32.  Bytes outside 7..246, which no call writes, make what
+ * is computed from their entries open.
+ */
+typedef struct {
+    uint8_t *k, *v;
+} gkv_paged_scales;
+
+/* gracekv_paged_load into quantised pages. */
+gkv_status gracekv_quant_load(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t b, const void *K,
+                              const void *V, const float *log_m, const int64_t *offsets, int64_t n_entries,
+                              void *workspace, void *stream);
+
+/* gracekv_paged_append into quantised pages: keys are rotated in fp32 and
+ * quantised from there, rounded once; queries as there. */
+gkv_status gracekv_quant_append(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l,
+                                const gkv_paged_tokens *t, void *workspace, void *stream);
+
+/* Rows that leave a paged cache (device pointers; strides in elements, of tokens
+ * and heads; rows may not share memory): k, v [n_tokens][G][d].  cu_new [B + 1] or
+ * NULL as in gkv_paged_tokens. */
+typedef struct {
+    int32_t n_tokens;
+    const int32_t *cu_new;
+    void *k, *v;
+    int64_t k_ts, k_hs, v_ts, v_hs;
+} gkv_paged_rows;
+
+/* The inverse of the append, of a cache with scales or (scales NULL) without:
+ * row t of request b is entry lens[l][b][g] - (cu_new[b + 1] - t) of every head
+ * g of layer l, so cu_new of the lengths themselves gives the whole sequences, as
+ * gracekv_prompt_attention takes them.  An entry of a negative index, or of a page that is not
+ * followed, gives a row of zeros; rows of no request are not written.  cu_new
+ * words that run backwards or past n_tokens are reported by gracekv_paged_status;
+ * which of their rows are written is open.  Errors: GKV_EINVAL, GKV_ECUDA. */
+gkv_status gracekv_paged_read(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l,
+                              const gkv_paged_rows *rows, void *workspace, void *stream);
+
+/* The inverse of the load: request b's entries of every layer as a packed cache
+ * K, V [n_entries][d] of the cache's dtype, log_m [n_entries] (NULL: not wanted;
+ * 0 for a cache without) and offsets [L G + 1] (all device, written here).  The
+ * pages stay as they are.  Entries past n_entries are not written, and
+ * gracekv_paged_status reports GKV_EINVAL; entries of pages that are not followed
+ * are zeros.  Errors: GKV_EINVAL, GKV_ECUDA. */
+gkv_status gracekv_paged_unload(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t b, void *K, void *V,
+                                float *log_m, int64_t *offsets, int64_t n_entries, void *workspace, void *stream);
+
 /* Synchronises `stream` and reports (then clears) the workspace's status word:
  * GKV_ETIMEOUT when a bounded device-side wait gave up, GKV_EINVAL when a
  * call met a page number, length or offset it did not follow, else GKV_OK. */

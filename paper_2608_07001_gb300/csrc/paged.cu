@@ -21,6 +21,7 @@
 // 6.7 TB/s), 2.5 us for one token (a call from Python takes 10 to 12); load
 // 163 us for 1M entries of 2 x 128 bf16 (1082 MB, 6.6 TB/s).
 #include "paged.cuh"
+#include "quant.cuh"
 
 #include <math.h>
 
@@ -71,6 +72,7 @@ struct AppendArgs {
     int64_t k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, qo_ts, qo_hs;     // bytes
     int rotate;
     int *status;
+    gkv_paged_scales scales;                   // of quantised pages
 };
 
 // Coherent: the kernel before may have written it while this one had begun, and q_out may be q.  As an instruction of
@@ -105,9 +107,10 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
 // chunks: a row's half is one 64- to 256-byte line.
 // Five blocks a SM (48 registers): 128 us at 32768 tokens of 48 rows; four 132 to
 // 146, six 139, eight (spills) 168.
-template <typename T, int D, int R>
-__global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
-    constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T);
+// QUANT: a row's lanes find its largest size together and store codes.
+template <typename T, int D, int R, bool QUANT>
+__global__ void __launch_bounds__(256, QUANT ? 4 : 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
+    constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T), PB = QUANT ? D : RB;      // bytes of a pool row
     next_may_start();
     after_previous();
     if (a.cu_new && blockIdx.x == gridDim.x - 1) {       // a block for the bounds alone, out of the others' way
@@ -143,6 +146,7 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
     for (int k0 = 0; k0 < R; k0 += U) {
         uint4 x[U], y[U];
         char *dst[U];
+        uint8_t *to_scale[U];
 #pragma unroll
         for (int k = 0; k < U; k++) {
             const int r = r0 + (k0 + k) * stride;
@@ -161,7 +165,8 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
                 const int idx = tail ? a.c.lens[s] - tail : -1;
                 const int64_t row = idx >= 0 ? entry_row(a.c, s, idx, a.status) : -1;
                 if (row >= 0) {
-                    dst[k] = (is_v ? a.c.V : a.c.K) + row * RB;
+                    dst[k] = (is_v ? a.c.V : a.c.K) + row * PB;
+                    if constexpr (QUANT) to_scale[k] = (is_v ? a.scales.v : a.scales.k) + row;
                     if (!is_v && ch == 0 && a.c.log_m) a.c.log_m[row] = 0.f;
                 }
             }
@@ -172,6 +177,26 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
         for (int k = 0; k < U; k++) {
             if (!dst[k]) continue;
             const int r = r0 + (k0 + k) * stride;
+            if constexpr (QUANT) {
+                if (r < 2 * a.c.G) {
+                    float u[N], w[N];
+                    unpack16(x[k], u);
+                    unpack16(y[k], w);
+                    if (a.rotate && r < a.c.G) {
+#pragma unroll
+                        for (int j = 0; j < N; j++) {
+                            const float p = u[j];
+                            u[j] = p * cs[j] - w[j] * sn[j];
+                            w[j] = p * sn[j] + w[j] * cs[j];
+                        }
+                    }
+                    const int byte = row_scale_byte(row_max<CH>(fmaxf(top_of(u), top_of(w))));
+                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + ch * N, u, inverse_of(byte));
+                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + D / 2 + ch * N, w, inverse_of(byte));
+                    if (ch == 0) *to_scale[k] = (uint8_t)byte;
+                    continue;
+                }
+            }
             if (a.rotate && (r < a.c.G || r >= 2 * a.c.G)) turn16<T>(x[k], y[k], cs, sn);
             st16(dst[k] + ch * 16, x[k]);
             st16(dst[k] + ch * 16 + RB / 2, y[k]);
@@ -183,7 +208,7 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
 // latency of one row; many want a thread's sines to serve several (32768 tokens
 // of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread and two in
 // flight: 201 / 158 / 137 / 144 us, before five blocks a SM).
-template <typename T, int D>
+template <typename T, int D, bool QUANT>
 cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
     constexpr int CH = D * (int)sizeof(T) / 32;
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
@@ -191,7 +216,7 @@ cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t 
     const bool many = one >= kAppendMany;
     const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 3) / 4) * CH : one;
     const unsigned n = (unsigned)((threads + 255) / 256) + (a.cu_new ? 1 : 0);
-    return launch_overlapped(many ? paged_append_kernel<T, D, 4> : paged_append_kernel<T, D, 1>, n, 256, 0, s, a, turns);
+    return launch_overlapped(many ? paged_append_kernel<T, D, 4, QUANT> : paged_append_kernel<T, D, 1, QUANT>, n, 256, 0, s, a, turns);
 }
 
 __global__ void paged_advance_kernel(int32_t *lens, const int32_t *cu_new, int n, int B, int G) {
@@ -211,6 +236,27 @@ struct LoadArgs {
     const int64_t *off;
     int64_t n_entries;
     int *status;
+    gkv_paged_scales scales;
+};
+
+// How 16 bytes of a packed row (chunk ch) become a pool row's: as they are, or as codes.  The row's lanes call it together.
+template <int BYTES>
+struct Plain {
+    static constexpr int RB = BYTES;
+    static __device__ __forceinline__ void put(char *pool, uint8_t *, int64_t row, int ch, uint4 x) {
+        st16(pool + row * RB + ch * 16, x);
+    }
+};
+template <typename T, int D>
+struct Quantised {
+    static constexpr int RB = D * sizeof(T), N = 16 / sizeof(T);
+    static __device__ __forceinline__ void put(char *pool, uint8_t *scales, int64_t row, int ch, uint4 x) {
+        float u[N];
+        unpack16(x, u);
+        const int byte = row_scale_byte(row_max<RB / 16>(top_of(u)));
+        put_codes(reinterpret_cast<uint8_t *>(pool) + row * D + ch * N, u, inverse_of(byte));
+        if (ch == 0) scales[row] = (uint8_t)byte;
+    }
 };
 
 __device__ __forceinline__ bool head_fits(const LoadArgs &a, int64_t lo, int64_t hi) {
@@ -220,9 +266,9 @@ __device__ __forceinline__ bool head_fits(const LoadArgs &a, int64_t lo, int64_t
 // Offsets that run backwards or past the entries anywhere lead the search for an entry's head astray, so a block
 // then copies the heads [first, first + 256) that fit itself, one after another.  What the search finds is copied
 // too: the same entries to the same rows.  A call, so that it costs the caller no registers.
-template <int RB>
+template <class W>
 __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first) {
-    constexpr int CH = RB / 16;
+    constexpr int RB = W::RB, CH = RB / 16;
     const int heads = a.c.L * a.c.G;
     const int64_t cap = (int64_t)a.c.page_size * a.c.max_pages;
     for (int h = first; h < heads && h < first + 256; h++) {
@@ -233,8 +279,8 @@ __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first)
             const int64_t e = i / CH, row = entry_row(a.c, s, (int)e, a.status);
             const int ch = (int)(i % CH);
             if (row < 0) continue;
-            st16(a.c.K + row * RB + ch * 16, ld16(a.K + (lo + e) * RB + ch * 16));
-            st16(a.c.V + row * RB + ch * 16, ld16(a.V + (lo + e) * RB + ch * 16));
+            W::put(a.c.K, a.scales.k, row, ch, ld16(a.K + (lo + e) * RB + ch * 16));
+            W::put(a.c.V, a.scales.v, row, ch, ld16(a.V + (lo + e) * RB + ch * 16));
             if (ch == 0 && a.c.log_m) a.c.log_m[row] = a.log_m ? a.log_m[lo + e] : 0.f;
         }
     }
@@ -245,9 +291,9 @@ __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first)
 // lane and IT times.  The head is searched for the run's first entry and
 // followed from there.  Eight blocks a SM: the registers that the call would take
 // otherwise leave room for six (1M entries of 2 x 256 bytes 163 us, 182 with 40).
-template <int RB, int IT>
+template <class W, int IT>
 __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constant__ LoadArgs a) {
-    constexpr int CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
+    constexpr int RB = W::RB, CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
     constexpr int U = IT < 4 ? IT : 4;
     next_may_start();
     after_previous();
@@ -263,7 +309,7 @@ __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constan
         }
         int bad = 0;
         for (int h = threadIdx.x; h < heads; h += 256) bad |= !head_fits(a, a.off[h], a.off[h + 1]);
-        if (__syncthreads_or(bad)) load_heads_disordered<RB>(a, (int)blockIdx.x * 256);
+        if (__syncthreads_or(bad)) load_heads_disordered<W>(a, (int)blockIdx.x * 256);
     }
     const int64_t e0 = (i >> 5) * (RW * IT) + lane / CH;
     if (e0 >= a.n_entries) return;
@@ -298,57 +344,46 @@ __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constan
 #pragma unroll
         for (int k = 0; k < U; k++) {
             if (row[k] < 0) continue;
-            st16(a.c.K + row[k] * RB + ch * 16, x[k]);
-            st16(a.c.V + row[k] * RB + ch * 16, y[k]);
+            W::put(a.c.K, a.scales.k, row[k], ch, x[k]);
+            W::put(a.c.V, a.scales.v, row[k], ch, y[k]);
             if (ch == 0 && a.c.log_m) a.c.log_m[row[k]] = a.log_m ? a.log_m[e0 + (int64_t)(k0 + k) * RW] : 0.f;
         }
     }
 }
 
-template <int RB>
+template <class W>
 cudaError_t launch_load(const LoadArgs &a, cudaStream_t s) {
+    constexpr int RB = W::RB;
     // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes; one 187, four 200
     constexpr int IT = 2;
     constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
     const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);
-    return launch_overlapped(paged_load_kernel<RB, IT>, (unsigned)((threads + 255) / 256), 256, 0, s, a);
+    return launch_overlapped(paged_load_kernel<W, IT>, (unsigned)((threads + 255) / 256), 256, 0, s, a);
 }
 
-}  // namespace
-}  // namespace gkv
-
-using namespace gkv;
-
-extern "C" gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K, const void *V,
-                                         const float *log_m, const int64_t *offsets, int64_t n_entries,
-                                         void *workspace, void *stream) {
-    const gkv_status st = check_paged(c);
-    if (st != GKV_OK) return st;
+// scales: of a quantised cache, else null.
+gkv_status load_call(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t b, const void *K, const void *V,
+                     const float *log_m, const int64_t *offsets, int64_t n_entries, void *workspace, void *stream) {
     if (b < 0 || b >= c->B || !offsets || !al(offsets, 8) || n_entries < 0 || n_entries >= (1LL << 31)) return GKV_EINVAL;
     if (n_entries > 0 && (!K || !V || !al(K, 16) || !al(V, 16))) return GKV_EINVAL;
     if (!al(log_m, 4) || (log_m && !c->log_m) || !workspace || !al(workspace, 256)) return GKV_EINVAL;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const LoadArgs a{paged_of(c), b, static_cast<const char *>(K), static_cast<const char *>(V), log_m, offsets,
-                     n_entries, static_cast<int *>(workspace)};
+                     n_entries, static_cast<int *>(workspace), scales ? *scales : gkv_paged_scales{}};
     const int rb = c->d * elem_bytes(c->dtype);
-    const cudaError_t e = rb == 128 ? launch_load<128>(a, s) : rb == 256 ? launch_load<256>(a, s) : launch_load<512>(a, s);
+    cudaError_t e;
+    if (!scales)
+        e = rb == 128 ? launch_load<Plain<128>>(a, s) : rb == 256 ? launch_load<Plain<256>>(a, s) : launch_load<Plain<512>>(a, s);
+    else if (c->dtype == GKV_BF16)
+        e = c->d == 128 ? launch_load<Quantised<__nv_bfloat16, 128>>(a, s) : launch_load<Quantised<__nv_bfloat16, 64>>(a, s);
+    else
+        e = c->d == 128 ? launch_load<Quantised<float, 128>>(a, s) : launch_load<Quantised<float, 64>>(a, s);
     return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }
 
-extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream) {
-    const gkv_status st = check_paged(c);
-    if (st != GKV_OK) return st;
-    if (!al(cu_new, 4)) return GKV_EINVAL;
-    const int n = c->L * c->B * c->G;
-    const cudaError_t e = launch_overlapped(paged_advance_kernel, (n + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream),
-                                            c->lens, cu_new, n, c->B, c->G);
-    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
-}
-
-extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t,
-                                           void *workspace, void *stream) {
-    const gkv_status st = check_paged(c);
-    if (st != GKV_OK) return st;
+template <bool QUANT>
+gkv_status append_call(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l, const gkv_paged_tokens *t,
+                       void *workspace, void *stream) {
     if (!t || l < 0 || l >= c->L || t->n_tokens < 0 || (!t->cu_new && t->n_tokens != c->B) || !al(t->cu_new, 4))
         return GKV_EINVAL;
     if (!workspace || !al(workspace, 256)) return GKV_EINVAL;
@@ -366,15 +401,58 @@ extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, 
     const AppendArgs a{paged_of(c), l, n_tokens, t->cu_new, t->pos, static_cast<const char *>(t->k),
                        static_cast<const char *>(t->v), static_cast<const char *>(q), static_cast<char *>(t->q_out),
                        t->k_ts * es, t->k_hs * es, t->v_ts * es, t->v_hs * es, t->q_ts * es, t->q_hs * es,
-                       t->qo_ts * es, t->qo_hs * es, c->rope_base > 0.0, static_cast<int *>(workspace)};
+                       t->qo_ts * es, t->qo_hs * es, c->rope_base > 0.0, static_cast<int *>(workspace),
+                       scales ? *scales : gkv_paged_scales{}};
     const int64_t items = (int64_t)n_tokens * (2 * c->G + (q ? c->Hq : 0)) * (c->d * es / 32);
     if ((items + 255) / 256 + 1 >= (1LL << 31)) return GKV_EUNSUPPORTED;
     const Turns &turns = turns_of(c->rope_base, c->d);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = c->dtype == GKV_BF16
-                              ? (c->d == 128 ? launch_append<__nv_bfloat16, 128>(a, turns, s) : launch_append<__nv_bfloat16, 64>(a, turns, s))
-                              : (c->d == 128 ? launch_append<float, 128>(a, turns, s) : launch_append<float, 64>(a, turns, s));
+    const cudaError_t e = c->dtype == GKV_BF16 ? (c->d == 128 ? launch_append<__nv_bfloat16, 128, QUANT>(a, turns, s)
+                                                              : launch_append<__nv_bfloat16, 64, QUANT>(a, turns, s))
+                                               : (c->d == 128 ? launch_append<float, 128, QUANT>(a, turns, s)
+                                                              : launch_append<float, 64, QUANT>(a, turns, s));
     return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+}  // namespace
+}  // namespace gkv
+
+using namespace gkv;
+
+extern "C" gkv_status gracekv_paged_load(const gkv_paged_cache *c, int32_t b, const void *K, const void *V,
+                                         const float *log_m, const int64_t *offsets, int64_t n_entries,
+                                         void *workspace, void *stream) {
+    const gkv_status st = check_paged(c);
+    return st != GKV_OK ? st : load_call(c, nullptr, b, K, V, log_m, offsets, n_entries, workspace, stream);
+}
+
+extern "C" gkv_status gracekv_quant_load(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t b, const void *K,
+                                         const void *V, const float *log_m, const int64_t *offsets, int64_t n_entries,
+                                         void *workspace, void *stream) {
+    const gkv_status st = check_quant(c, scales);
+    return st != GKV_OK ? st : load_call(c, scales, b, K, V, log_m, offsets, n_entries, workspace, stream);
+}
+
+extern "C" gkv_status gracekv_paged_advance(const gkv_paged_cache *c, const int32_t *cu_new, void *stream) {
+    const gkv_status st = check_paged(c);
+    if (st != GKV_OK) return st;
+    if (!al(cu_new, 4)) return GKV_EINVAL;
+    const int n = c->L * c->B * c->G;
+    const cudaError_t e = launch_overlapped(paged_advance_kernel, (n + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream),
+                                            c->lens, cu_new, n, c->B, c->G);
+    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+extern "C" gkv_status gracekv_paged_append(const gkv_paged_cache *c, int32_t l, const gkv_paged_tokens *t,
+                                           void *workspace, void *stream) {
+    const gkv_status st = check_paged(c);
+    return st != GKV_OK ? st : append_call<false>(c, nullptr, l, t, workspace, stream);
+}
+
+extern "C" gkv_status gracekv_quant_append(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l,
+                                           const gkv_paged_tokens *t, void *workspace, void *stream) {
+    const gkv_status st = check_quant(c, scales);
+    return st != GKV_OK ? st : append_call<true>(c, scales, l, t, workspace, stream);
 }
 
 extern "C" gkv_status gracekv_paged_status(void *workspace, void *stream) {

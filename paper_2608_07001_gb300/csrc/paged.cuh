@@ -38,6 +38,13 @@ inline gkv_status check_paged(const gkv_paged_cache *c) {
     return GKV_OK;
 }
 
+// The same for a quantised cache.
+inline gkv_status check_quant(const gkv_paged_cache *c, const gkv_paged_scales *scales) {
+    const gkv_status st = check_paged(c);
+    if (st != GKV_OK) return st;
+    return scales && scales->k && scales->v && al(scales->k, 16) && al(scales->v, 16) ? GKV_OK : GKV_EINVAL;
+}
+
 // Pool row of entry idx of sequence s = (l B + b) G + g; -1 (and the status
 // bit) when the table does not lead into the pool.
 __device__ __forceinline__ int64_t entry_row(const Paged &c, int64_t s, int idx, int *status) {

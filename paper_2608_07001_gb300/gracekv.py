@@ -77,9 +77,18 @@ class GkvPagedTokens(C.Structure):
         (n, C.c_int64) for n in ("k_ts", "k_hs", "v_ts", "v_hs", "q_ts", "q_hs", "qo_ts", "qo_hs")]
 
 
-# the two structures that every call fills, packed in one go
-_PROMPT, _TOKENS = struct.Struct("@5i4x2q7P8q"), struct.Struct("@i4x6P8q")
-assert _PROMPT.size == C.sizeof(GkvPrompt) and _TOKENS.size == C.sizeof(GkvPagedTokens)
+class GkvPagedScales(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class GkvPagedRows(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32)] + [(n, C.c_void_p) for n in ("cu_new", "k", "v")] + [
+        (n, C.c_int64) for n in ("k_ts", "k_hs", "v_ts", "v_hs")]
+
+
+# the structures that every call fills, packed in one go
+_PROMPT, _TOKENS, _ROWS = struct.Struct("@5i4x2q7P8q"), struct.Struct("@i4x6P8q"), struct.Struct("@i4x3P4q")
+assert _PROMPT.size == C.sizeof(GkvPrompt) and _TOKENS.size == C.sizeof(GkvPagedTokens) and _ROWS.size == C.sizeof(GkvPagedRows)
 
 
 class GraceKVError(RuntimeError):
@@ -100,7 +109,8 @@ EXPORTED = ["gracekv_default_params", "gracekv_budget_for_ratio", "gracekv_graph
             "gracekv_decode_attention", "gracekv_decode_status",
             "gracekv_prompt_workspace_size", "gracekv_prompt_attention", "gracekv_prompt_status",
             "gracekv_paged_workspace_size", "gracekv_paged_load", "gracekv_paged_advance",
-            "gracekv_paged_append", "gracekv_paged_attention", "gracekv_paged_status"]
+            "gracekv_paged_append", "gracekv_paged_attention", "gracekv_paged_status",
+            "gracekv_quant_load", "gracekv_quant_append", "gracekv_paged_read", "gracekv_paged_unload"]
 
 
 def lib() -> C.CDLL:
@@ -153,6 +163,11 @@ def lib() -> C.CDLL:
     L.gracekv_paged_append.argtypes = [pcp, i32, C.POINTER(GkvPagedTokens), vp, vp]
     L.gracekv_paged_attention.argtypes = [pcp, i32, vp, vp, vp, vp]
     L.gracekv_paged_status.argtypes = [vp, vp]
+    scp = C.POINTER(GkvPagedScales)
+    L.gracekv_quant_load.argtypes = [pcp, scp, i32, vp, vp, vp, vp, i64, vp, vp]
+    L.gracekv_quant_append.argtypes = [pcp, scp, i32, C.POINTER(GkvPagedTokens), vp, vp]
+    L.gracekv_paged_read.argtypes = [pcp, scp, i32, C.POINTER(GkvPagedRows), vp, vp]
+    L.gracekv_paged_unload.argtypes = [pcp, scp, i32, vp, vp, vp, vp, i64, vp, vp]
     _lib = L
     return L
 
@@ -666,45 +681,71 @@ class PagedCache(_Workspace):
     device tensors; `PagedCache.allocate` makes them and then also hands out
     the pages (`load`, `advance`, `release`).  A dense [L, G, T, d] cache is one
     too: L G pages of T entries.  One object holds the workspace of one stream.
+
+    Pages of torch.float8_e4m3fn with k_scale, v_scale [n_pages, page_size] uint8
+    are quantised (gracekv_quant_* of the C ABI): a row stands for its codes times
+    2^(byte - 127).  Every call takes and gives rows of `dtype` (bf16 or fp32)
+    then too, and the writing ones quantise.
     """
 
-    def __init__(self, K, V, table, lens, *, Hq: int, log_m=None, rope_base: float = 0.0):
-        if K.dtype not in _DTYPES:
-            raise _bad(f"K must be bf16 or fp32, not {K.dtype}")
+    def __init__(self, K, V, table, lens, *, Hq: int, log_m=None, rope_base: float = 0.0, k_scale=None, v_scale=None, dtype=None):
+        quant = K.dtype is torch.float8_e4m3fn
+        if dtype is None:
+            dtype = torch.bfloat16 if quant else K.dtype
+        if dtype not in _DTYPES or not (quant or dtype is K.dtype):
+            raise _bad(f"K must be bf16, fp32 or e4m3 with rows of either, not {K.dtype} with rows of {dtype}")
+        if (k_scale is not None) != quant or (v_scale is not None) != quant:
+            raise _bad("quantised pages, and no others, have scales of their keys and of their values")
         if K.dim() != 3 or table.dim() != 4:
             raise _bad("K is [n_pages, page_size, d] and table [L, B, G, max_pages]")
         dev = K.device
         n_pages, ps, d = K.shape
         L, B, G, mp = table.shape
         self.K, self.V, self.log_m, self.table, self.lens = K, V, log_m, table, lens
-        self.L, self.B, self.G, self.Hq, self.d, self.dtype = L, B, G, Hq, d, K.dtype
+        self.L, self.B, self.G, self.Hq, self.d, self.dtype = L, B, G, Hq, d, dtype
         self.page_size, self.max_pages, self.n_pages = ps, mp, n_pages
+        self.k_scale, self.v_scale, self.quantised = k_scale, v_scale, quant
+        self._pool = (K, V, log_m, table, lens, k_scale, v_scale)
         self.desc = GkvPagedCache(
-            L, B, G, Hq, d, _DTYPES[K.dtype], ps, mp, n_pages, _words("K", K, K.shape, K.dtype, dev),
+            L, B, G, Hq, d, _DTYPES[dtype], ps, mp, n_pages, _words("K", K, K.shape, K.dtype, dev),
             _words("V", V, K.shape, K.dtype, dev),
             None if log_m is None else _words("log_m", log_m, (n_pages, ps), torch.float32, dev),
             _words("table", table, table.shape, torch.int32, dev), _words("lens", lens, (L, B, G), torch.int32, dev),
             float(rope_base))
+        self._scales = None
+        if quant:
+            self._scales = GkvPagedScales(*(_words(x, t, (n_pages, ps), torch.uint8, dev)
+                                            for x, t in (("k_scale", k_scale), ("v_scale", v_scale))))
         n = C.c_size_t()
         _raise(lib().gracekv_paged_workspace_size(C.byref(self.desc), C.byref(n)))
         self._make_workspace(n.value, dev)
-        self._ref = C.byref(self.desc)
-        self._buf = bytearray(C.sizeof(GkvPagedTokens))
+        self._buf, self._row_buf = bytearray(C.sizeof(GkvPagedTokens)), bytearray(C.sizeof(GkvPagedRows))
         self._tokens = C.byref(GkvPagedTokens.from_buffer(self._buf))
-        self._append, self._attention = lib().gracekv_paged_append, lib().gracekv_paged_attention
+        self._rows = C.byref(GkvPagedRows.from_buffer(self._row_buf))
+        # the cache's own arguments of a call that takes both kinds, and of one of its kind
+        self._both = (C.byref(self.desc), None if self._scales is None else C.byref(self._scales))
+        self._ref = self._both if quant else self._both[:1]
+        L_, kind = lib(), "gracekv_quant_" if quant else "gracekv_paged_"
+        self._load, self._append = getattr(L_, kind + "load"), getattr(L_, kind + "append")
+        self._attention = L_.gracekv_paged_attention
         self._free = None
 
     @staticmethod
     def allocate(*, L: int, B: int, G: int, Hq: int, d: int, dtype, n_pages: int, max_pages: int,
-                 page_size: int = 64, log_m: bool = True, rope_base: float = 0.0, device="cuda") -> "PagedCache":
+                 page_size: int = 64, log_m: bool = True, rope_base: float = 0.0, device="cuda",
+                 quantised: bool = False) -> "PagedCache":
         """An empty cache that hands out its own pages."""
         import numpy as np
-        c = PagedCache(torch.empty(n_pages, page_size, d, dtype=dtype, device=device),
-                       torch.empty(n_pages, page_size, d, dtype=dtype, device=device),
+        kind = torch.float8_e4m3fn if quantised else dtype
+        scale = dict(dtype=torch.uint8, device=device)
+        c = PagedCache(torch.empty(n_pages, page_size, d, dtype=kind, device=device),
+                       torch.empty(n_pages, page_size, d, dtype=kind, device=device),
                        torch.full((L, B, G, max_pages), -1, dtype=torch.int32, device=device),
-                       torch.zeros(L, B, G, dtype=torch.int32, device=device), Hq=Hq, rope_base=rope_base,
+                       torch.zeros(L, B, G, dtype=torch.int32, device=device), Hq=Hq, rope_base=rope_base, dtype=dtype,
+                       k_scale=torch.empty(n_pages, page_size, **scale) if quantised else None,
+                       v_scale=torch.empty(n_pages, page_size, **scale) if quantised else None,
                        log_m=torch.empty(n_pages, page_size, device=device) if log_m else None)
-        c._made += [t for t in (c.K, c.V, c.log_m, c.table, c.lens) if t is not None]
+        c._made += [t for t in c._pool if t is not None]
         c._free = np.arange(n_pages - 1, -1, -1, dtype=np.int32)     # a stack: the last one goes next
         c._n_free = n_pages
         c._host_lens = np.zeros((L, B, G), np.int64)
@@ -755,8 +796,37 @@ class PagedCache(_Workspace):
     def load_packed(self, b: int, K, V, log_m, offsets, stream=None):
         """The packed cache K, V [E, d], log_m [E] or None, offsets [L G + 1] int64
         becomes request b's entries (the table already holds their pages)."""
-        self._run(lib().gracekv_paged_load, self._ref, *self._packed(b, K, V, log_m, offsets), self._ws,
-                  self._on(stream, K, V, log_m, offsets, self.K, self.V, self.log_m, self.table, self.lens))
+        self._run(self._load, *self._ref, *self._packed(b, K, V, log_m, offsets), self._ws,
+                  self._on(stream, K, V, log_m, offsets, *self._pool))
+
+    def unload_packed(self, b: int, n_entries: int, out=None, stream=None):
+        """Request b's entries, at most n_entries, as a packed cache: (K, V [n_entries, d]
+        of `dtype`, log_m [n_entries], offsets [L G + 1] int64), new or the four tensors
+        `out`.  What load_packed takes; the pages stay as they are."""
+        dev, E, n1 = self._device, n_entries, self.L * self.G + 1
+        if not 0 <= b < self.B or not 0 <= E < 1 << 31:
+            raise _bad(f"request {b} of {self.B}, {E} entries")
+        if out is None:
+            out = (_empty_like_on(stream, (E, self.d), self.dtype, dev), _empty_like_on(stream, (E, self.d), self.dtype, dev),
+                   _empty_like_on(stream, (E,), torch.float32, dev), _empty_like_on(stream, (n1,), torch.int64, dev))
+        K, V, log_m, offsets = out
+        kp, vp = _words("K", K, (E, self.d), self.dtype, dev), _words("V", V, (E, self.d), self.dtype, dev)
+        mp, op = _words("log_m", log_m, (E,), torch.float32, dev), _words("offsets", offsets, (n1,), torch.int64, dev)
+        if E and (kp % 16 or vp % 16):
+            raise _bad("K and V are on 16 bytes")
+        self._run(lib().gracekv_paged_unload, *self._both, b, kp, vp, mp, op, E, self._ws,
+                  self._on(stream, K, V, log_m, offsets, *self._pool))
+        return out
+
+    def unload(self, b: int, stream=None) -> Cache:
+        """Request b's entries as a packed cache, to be loaded again (here, into another
+        cache, of another kind of pages) after its pages went back (`release`).  Its
+        positions and source intervals are not kept in pages: None."""
+        self._own_pages()
+        if not 0 <= b < self.B:
+            raise _bad(f"request {b} of {self.B}")
+        K, V, log_m, offsets = self.unload_packed(b, int(self._host_lens[:, b].sum()), None, stream)
+        return Cache(K, V, None, log_m, None, None, offsets)
 
     def load(self, b: int, cache: Cache, n_entries: int, stream=None):
         """A compressed cache (Compressor's output) as request b, replacing what the
@@ -818,7 +888,7 @@ class PagedCache(_Workspace):
     def advance_by(self, cu_new=None, stream=None):
         """Lengths alone, from a device cu_new [B + 1] (gracekv_paged_advance)."""
         p = None if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, self.K.device)
-        self._run(lib().gracekv_paged_advance, self._ref, p, self._on(stream, self.table, self.lens, cu_new))
+        self._run(lib().gracekv_paged_advance, self._both[0], p, self._on(stream, self.table, self.lens, cu_new))
 
     def release(self, b: int, stream=None):
         """Request b's pages return to the pool; the slot is idle."""
@@ -857,9 +927,26 @@ class PagedCache(_Workspace):
                           0 if cu_new is None else _words("cu_new", cu_new, (self.B + 1,), torch.int32, dev),
                           _words("pos", pos, (N,), torch.int32, dev), kp, vp, qp, op,
                           k_ts, k_hs, v_ts, v_hs, q_ts, q_hs, o_ts, o_hs)
-        self._run(self._append, self._ref, l, self._tokens, self._ws,
-                  self._on(stream, k, v, pos, q, cu_new, out, self.K, self.V, self.log_m, self.table, self.lens))
+        self._run(self._append, *self._ref, l, self._tokens, self._ws,
+                  self._on(stream, k, v, pos, q, cu_new, out, *self._pool))
         return out
+
+    def read(self, l: int, n: int, cu=None, k=None, v=None, stream=None):
+        """Layer l's last entries as n rows of tokens (k, v [n, G, d] of `dtype`, new or
+        the tensors given, with strides as append's): the last cu[b + 1] - cu[b] of
+        every head of request b, as rows cu[b]...; without cu one of each request.
+        Zeros where a head has fewer; rows of no request are not written."""
+        dev, dt, shape = self._device, self.dtype, (n, self.G, self.d)
+        if n < 0:
+            raise _bad(f"{n} rows")
+        k = _empty_like_on(stream, shape, dt, dev) if k is None else k
+        v = _empty_like_on(stream, shape, dt, dev) if v is None else v
+        kp, k_ts, k_hs = _rows("k", k, *shape, dt, dev)
+        vp, v_ts, v_hs = _rows("v", v, *shape, dt, dev)
+        _ROWS.pack_into(self._row_buf, 0, n, 0 if cu is None else _words("cu", cu, (self.B + 1,), torch.int32, dev), kp, vp,
+                        k_ts, k_hs, v_ts, v_hs)
+        self._run(lib().gracekv_paged_read, *self._both, l, self._rows, self._ws, self._on(stream, k, v, cu, *self._pool))
+        return k, v
 
     def attention(self, l: int, q, out=None, stream=None):
         """q [B, Hq, d], one rotated query per request slot -> out [B, Hq, d] of the
@@ -871,8 +958,7 @@ class PagedCache(_Workspace):
             op = out.data_ptr()
         else:
             op = _words("out", out, shape, self.dtype, dev)
-        self._run(self._attention, self._ref, l, qp, op, self._ws,
-                  self._on(stream, q, out, self.K, self.V, self.log_m, self.table, self.lens))
+        self._run(self._attention, *self._ref, l, qp, op, self._ws, self._on(stream, q, out, *self._pool))
         return out
 
     def status(self, stream=None):
