@@ -637,6 +637,12 @@ gkv_status gracekv_quant_load(const gkv_paged_cache *c, const gkv_paged_scales *
 gkv_status gracekv_quant_append(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l,
                                 const gkv_paged_tokens *t, void *workspace, void *stream);
 
+/* gracekv_paged_attention over quantised pages: of the values that the rows
+ * stand for, products and sums in fp32.  Logits of fp32 queries above 2^100 in
+ * size are open. */
+gkv_status gracekv_quant_attention(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l, const void *q,
+                                   void *out, void *workspace, void *stream);
+
 /* Rows that leave a paged cache (device pointers; strides in elements, of tokens
  * and heads; rows may not share memory): k, v [n_tokens][G][d].  cu_new [B + 1] or
  * NULL as in gkv_paged_tokens. */

@@ -49,6 +49,8 @@
 // no weight.  A logit that is NaN or +inf makes its head's output NaN: the
 // quotient is 0 only where no weight at all was summed.
 #include "paged.cuh"
+#include "quant.cuh"
+#include "shared.cuh"
 #include "tc.cuh"
 
 #include <float.h>
@@ -74,13 +76,20 @@ constexpr int kPaSnap = 8;                         // tiles of the longest seque
 constexpr int kPaPieces = 64;                      // pieces of a sequence that small launches aim at, at most
 constexpr uint64_t kPaWaitNs = 2000000000ull;
 
-template <typename T, int D>
+// T: rows of q and out; S: rows of the pools.
+template <typename T, typename S, int D>
 struct PaCfg {
-    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr bool BF = sizeof(T) == 2, QUANT = sizeof(S) == 1;
     static constexpr int TE = BF ? 64 : 32;        // entries of a tile
-    static constexpr int NB = D * (int)sizeof(T) / 128;          // 128-byte column boxes of a row
-    static constexpr int TB = NB * TE * 128;       // bytes of a tile's keys
-    static constexpr int NST = kPaRing / (2 * TB); // stages
+    static constexpr int RB = D * (int)sizeof(S), BW = RB < 128 ? RB : 128;      // bytes of a row, of a column box's row
+    static constexpr int NB = RB / BW;             // column boxes of a row
+    static constexpr int TB = TE * RB;             // bytes of a tile's keys
+    static constexpr int NST = kPaRing / (2 * TB) < 12 ? kPaRing / (2 * TB) : 12;      // stages
+    // Offset of the 16-byte chunk `ch` of row r of a tile, swizzled over 128 or 64 bytes.
+    static __device__ __forceinline__ uint32_t at(int r, int ch) {
+        return BW == 128 ? (uint32_t)((ch >> 3) * (TE * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4))
+                         : (uint32_t)(r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
+    }
     static constexpr int MIN = BF ? 2 : 1;         // tiles of a run at least
     static_assert(NST >= 3 && NST <= 12 && (BF || NST % kPaF32Warps == 0), "ring");
 };
@@ -96,12 +105,16 @@ struct PaArgs {
     int *status;
     int box;                    // rows of a box
     float scale;                // log2(e) / sqrt(d)
+    gkv_paged_scales scales;    // of quantised pools
+    SharedPlan plan;            // of a shared prefix
+    int tok;
 };
 
-template <int NST, int TE>
+template <int NST, int TE, bool QUANT>
 struct PaSmem {
     uint64_t full[NST], empty[NST];
     alignas(16) float lm[NST][TE];
+    alignas(16) uint8_t ks[QUANT ? NST : 1][TE], vs[QUANT ? NST : 1][TE];
     int count[NST];             // valid entries of the stage's tile
     unsigned units[NST];        // its boxes that were read
     long long first, total;     // the CTA's first sequence: prefix of tiles before it; all tiles
@@ -186,7 +199,7 @@ __device__ __forceinline__ float pa_shift(float m) { return m == -INFINITY ? 0.f
 // bf16: this warp's 16 entries of every tile of [t0, t1).
 template <int D>
 struct PaBf {
-    using C = PaCfg<__nv_bfloat16, D>;
+    using C = PaCfg<__nv_bfloat16, __nv_bfloat16, D>;
     uint32_t qa[D / 16][2];     // the queries as 16 x 16 row operands: rows 0-7 (8-15 the same)
     float acc[D / 8][4];        // rows hq: weights' first part, rows hq + 8: second part; columns of 8 channels
     float m, z;                 // of head hq; z: this lane's share
@@ -208,13 +221,8 @@ struct PaBf {
         z = 0.f;
     }
 
-    // Offset of the 16-byte chunk `ch` of row r of a tile.
-    static __device__ __forceinline__ uint32_t at(int r, int ch) {
-        return (uint32_t)((ch >> 3) * (C::TE * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
-    }
-
-    __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const float *lm, int count, unsigned units, int box,
-                                         float scale, bool has_lm) {
+    __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const uint8_t *, const uint8_t *, const float *lm,
+                                         int count, unsigned units, int box, float scale, bool has_lm) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tq = lane & 3;
         const int r0 = warp * 16;
         const int nv = min(16, count - r0);                       // valid entries of the slice
@@ -229,7 +237,7 @@ struct PaBf {
 #pragma unroll
         for (int kk = 0; kk < D / 16; kk++) {
             uint32_t b[4];
-            pa_ldsm4(kst + at(r0 + ri + (mi >> 1) * 8, kk * 2 + (mi & 1)), b);
+            pa_ldsm4(kst + C::at(r0 + ri + (mi >> 1) * 8, kk * 2 + (mi & 1)), b);
             pa_mma(x[0], qa[kk][0], qa[kk][0], qa[kk][1], qa[kk][1], b[0], b[1]);
             pa_mma(x[1], qa[kk][0], qa[kk][0], qa[kk][1], qa[kk][1], b[2], b[3]);
         }
@@ -274,7 +282,7 @@ struct PaBf {
 #pragma unroll
         for (int i = 0; i < D / 16; i++) {
             uint32_t b[4];      // entries 0-7, 8-15 of channels 16 i .. + 7, then of + 8 .. + 15
-            pa_ldsm4t(vst + at(r0 + ri + (mi & 1) * 8, i * 2 + (mi >> 1)), b);
+            pa_ldsm4t(vst + C::at(r0 + ri + (mi & 1) * 8, i * 2 + (mi >> 1)), b);
             pa_mma(acc[2 * i], hi[0], lo[0], hi[1], lo[1], b[0] & keep0, b[1] & keep1);
             pa_mma(acc[2 * i + 1], hi[0], lo[0], hi[1], lo[1], b[2] & keep0, b[3] & keep1);
         }
@@ -303,10 +311,180 @@ struct PaBf {
     }
 };
 
-// fp32: whole tiles of 32 entries, one warp each.
-template <int D, int GQ>
+// The same over quantised pools.  The codes are exact in f16, and so are a head's
+// queries times a power of two that brings its largest to 2^14 (down to 2^-38 of
+// that), so the logits' products are those of the codes and both scales' exponents come after.  A
+// thread's 4 bytes of an ldmatrix row are 4 neighbouring channels: they serve as
+// channels 2 t, 2 t + 1 and + 8 of the product's step, which sums over them all, and
+// the queries are laid out to match.  Values become bf16, code and scale, exactly, so
+// that the weights keep the range of bf16; a transposed 16-bit word holds two
+// channels, the even ones and the odd ones of 16 to a product.
+template <int D>
+struct PaE4 {
+    using C = PaCfg<__nv_bfloat16, E4m3, D>;
+    uint32_t qa[D / 16][2];     // queries in f16, channels 16 i + 4 t .. + 3
+    float acc[D / 8][4];        // as PaBf's, columns: the even, then the odd channels of 16
+    float m, z;
+    int qe;                     // the power of two taken from head hq's queries
+
+    __device__ __forceinline__ void begin(const PaArgs &a, int s, int gq) {
+        const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
+        const uint2 *q = reinterpret_cast<const uint2 *>(
+            static_cast<const __nv_bfloat16 *>(a.q) + ((size_t)s * gq + (hq < gq ? hq : 0)) * D);
+        float top = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 16; c++) {
+            const uint2 u = hq < gq ? q[c * 4 + tq] : make_uint2(0, 0);
+            qa[c][0] = u.x;
+            qa[c][1] = u.y;
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+                top = fmaxf(top, fmaxf(finite_size(__uint_as_float(qa[c][i] << 16)), finite_size(__uint_as_float(qa[c][i] & 0xffff0000u))));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        qe = max((int)(__float_as_uint(top) >> 23) - 127 - 14, -100);
+        const float f = __uint_as_float((uint32_t)(127 - qe) << 23);
+#pragma unroll
+        for (int c = 0; c < D / 16; c++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(qa[c][i] << 16) * f, __uint_as_float(qa[c][i] & 0xffff0000u) * f);
+                qa[c][i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+#pragma unroll
+        for (int i = 0; i < D / 8; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[i][j] = 0.f;
+        m = -INFINITY;
+        z = 0.f;
+    }
+
+    // Two codes as f16, exact.
+    static __device__ __forceinline__ uint32_t half2(uint32_t c) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+        return h;
+    }
+    static __device__ __forceinline__ void mma_f16(float c[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+            "{%0, %1, %2, %3}, {%4, %4, %5, %5}, {%6, %7}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a2), "r"(b0), "r"(b1));
+    }
+    // Two codes of neighbouring entries times their scales.
+    static __device__ __forceinline__ uint32_t value2(uint32_t c, float s0, float s1) {
+        const float2 v = values2(c);
+        return bf16x2_of(v.x * s0, v.y * s1);
+    }
+
+    __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const uint8_t *ks, const uint8_t *vs, const float *lm,
+                                         int count, unsigned units, int box, float scale, bool has_lm) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tq = lane & 3;
+        const int r0 = warp * 16;
+        const int nv = min(16, count - r0);
+        if (nv <= 0 || !((units >> (r0 / box)) & 1u)) return;
+        float x[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[n][j] = 0.f;
+        const int mi = lane >> 3, ri = lane & 7;
+#pragma unroll
+        for (int c = 0; c < D / 16; c += 2) {
+            uint32_t b[4];      // entries 0-7 of chunks c, c + 1, then entries 8-15
+            pa_ldsm4(kst + C::at(r0 + ri + (mi >> 1) * 8, c + (mi & 1)), b);
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+                    mma_f16(x[n], qa[c + i][0], qa[c + i][1], half2(b[2 * n + i] & 0xffffu), half2(b[2 * n + i] >> 16));
+        }
+        float y[2][2], mx = -INFINITY, vsc[2][2];
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int e = n * 8 + 2 * tq + j;
+                // both powers of two in two steps, so that only a logit out of range leaves it
+                const int t = qe + (int)ks[r0 + e] - 127;
+                float v = x[n][j] * scale * __uint_as_float((uint32_t)(127 + (t >> 1)) << 23) *
+                          __uint_as_float((uint32_t)(127 + t - (t >> 1)) << 23);
+                if (has_lm) v += pa_lm2(lm[r0 + e]);
+                y[n][j] = e < nv ? v : -INFINITY;
+                vsc[n][j] = e < nv ? scale_of(vs[r0 + e]) : 0.f;
+                mx = fmaxf(mx, y[n][j]);
+            }
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        if (__any_sync(0xffffffffu, mx > m)) {
+            const float mn = fmaxf(m, mx), w = tc::ex2(m - pa_shift(mn));
+            m = mn;
+            z *= w;
+#pragma unroll
+            for (int i = 0; i < D / 8; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[i][j] *= w;
+        }
+        const float sh = pa_shift(m);
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int n = 0; n < 2; n++) {
+            const float p0 = tc::ex2(y[n][0] - sh), p1 = tc::ex2(y[n][1] - sh);
+            z += p0 + p1;
+            hi[n] = pa_bf16x2(p0, p1);
+            lo[n] = pa_bf16x2(p0 - __uint_as_float(hi[n] << 16), p1 - __uint_as_float(hi[n] & 0xffff0000u));
+        }
+        uint32_t keep0 = ~0u, keep1 = ~0u;
+        if (nv < 16) {
+            keep0 = (2 * tq < nv ? 0xffffu : 0u) | (2 * tq + 1 < nv ? 0xffff0000u : 0u);
+            keep1 = (2 * tq + 8 < nv ? 0xffffu : 0u) | (2 * tq + 9 < nv ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 2) {
+            uint32_t b[4];      // entries 0-7, 8-15 of chunk i, then of i + 1
+            pa_ldsm4t(vst + C::at(r0 + ri + (mi & 1) * 8, i + (mi >> 1)), b);
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                // bytes (entry 0, channels 0 1), (entry 1, channels 0 1) -> channel 0 of both, channel 1 of both
+                const uint32_t c0 = __byte_perm(b[2 * k] & keep0, 0, 0x3120), c1 = __byte_perm(b[2 * k + 1] & keep1, 0, 0x3120);
+                pa_mma(acc[2 * (i + k)], hi[0], lo[0], hi[1], lo[1], value2(c0 & 0xffffu, vsc[0][0], vsc[0][1]),
+                       value2(c1 & 0xffffu, vsc[1][0], vsc[1][1]));
+                pa_mma(acc[2 * (i + k) + 1], hi[0], lo[0], hi[1], lo[1], value2(c0 >> 16, vsc[0][0], vsc[0][1]),
+                       value2(c1 >> 16, vsc[1][0], vsc[1][1]));
+            }
+        }
+    }
+
+    __device__ __forceinline__ void stats(float *ms, float *zs) {
+        const int lane = threadIdx.x & 31;
+        z += __shfl_xor_sync(0xffffffffu, z, 1);
+        z += __shfl_xor_sync(0xffffffffu, z, 2);
+        if ((lane & 3) == 0) { ms[lane >> 2] = m; zs[lane >> 2] = z; }
+    }
+    __device__ __forceinline__ void add(float *sum, const float *M, int gq, bool first) {
+        const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
+        if (hq >= gq) return;
+        const float w = tc::ex2(m - pa_shift(M[hq]));
+#pragma unroll
+        for (int c = 0; c < D / 16; c++) {
+            float4 *p = reinterpret_cast<float4 *>(sum + hq * D + c * 16 + 4 * tq);
+            float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *p;
+            v.x += w * (acc[2 * c][0] + acc[2 * c][2]);
+            v.y += w * (acc[2 * c + 1][0] + acc[2 * c + 1][2]);
+            v.z += w * (acc[2 * c][1] + acc[2 * c][3]);
+            v.w += w * (acc[2 * c + 1][1] + acc[2 * c + 1][3]);
+            *p = v;
+        }
+    }
+};
+
+// fp32: whole tiles of 32 entries, one warp each.  Over quantised pools the key's scale
+// multiplies the logit and the value's the weight.
+template <typename S, int D, int GQ>
 struct PaF32 {
-    using C = PaCfg<float, D>;
+    using C = PaCfg<float, S, D>;
     static constexpr int E = D / 32;           // channels of a lane
     float2 acc[GQ][E / 2];
     float m[GQ], z[GQ];                        // z: this lane's share
@@ -322,28 +500,43 @@ struct PaF32 {
         }
     }
 
-    __device__ __forceinline__ void tile(const unsigned char *kst, const unsigned char *vst, const float *lm, int count,
-                                         unsigned units, int box, bool has_lm) {
+    __device__ __forceinline__ void tile(const unsigned char *kst, const unsigned char *vst, const uint8_t *ks,
+                                         const uint8_t *vs, const float *lm, int count, unsigned units, int box, bool has_lm) {
         const int lane = threadIdx.x & 31;
         const bool in = lane < count && ((units >> (lane / box)) & 1u);
         float2 x[GQ];
 #pragma unroll
         for (int h = 0; h < GQ; h++) x[h] = make_float2(0.f, 0.f);
-#pragma unroll 8
-        for (int ch = 0; ch < D / 4; ch++) {
-            const float4 k = *reinterpret_cast<const float4 *>(kst + (ch >> 3) * (C::TE * 128) + lane * 128 +
-                                                               (((ch & 7) ^ (lane & 7)) << 4));
+        auto product = [&](int c4, float4 k) {
 #pragma unroll
             for (int h = 0; h < GQ; h++) {
-                const float4 q = *reinterpret_cast<const float4 *>(qs + h * D + ch * 4);
+                const float4 q = *reinterpret_cast<const float4 *>(qs + h * D + c4 * 4);
                 x[h] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k.x, k.y), x[h]);
                 x[h] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k.z, k.w), x[h]);
             }
+        };
+        float kscale = 1.f, vscale = 1.f;
+        if constexpr (C::QUANT) {
+            kscale = in ? scale_of(ks[lane]) : 0.f;
+            vscale = in ? scale_of(vs[lane]) : 0.f;
+#pragma unroll 2
+            for (int ch = 0; ch < D / 16; ch++) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(kst + C::at(lane, ch));
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 k0 = values2(w[i] & 0xffffu), k1 = values2(w[i] >> 16);
+                    product(ch * 4 + i, make_float4(k0.x, k0.y, k1.x, k1.y));
+                }
+            }
+        } else {
+#pragma unroll 8
+            for (int ch = 0; ch < D / 4; ch++) product(ch, *reinterpret_cast<const float4 *>(kst + C::at(lane, ch)));
         }
         const float l2 = has_lm ? pa_lm2(lm[lane]) : 0.f;
 #pragma unroll
         for (int h = 0; h < GQ; h++) {
-            const float y = in ? x[h].x + x[h].y + l2 : -INFINITY;
+            const float y = in ? (C::QUANT ? (x[h].x + x[h].y) * kscale : x[h].x + x[h].y) + l2 : -INFINITY;
             float mx = y;
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -356,13 +549,12 @@ struct PaF32 {
             }
             const float p = tc::ex2(y - pa_shift(m[h]));
             z[h] += p;
-            ps[h * 32 + lane] = p;
+            ps[h * 32 + lane] = C::QUANT ? p * vscale : p;
         }
         __syncwarp();
         const unsigned ok = __ballot_sync(0xffffffffu, in);
         // lane's channels: E consecutive ones
-        const int ch = lane * E / 4;
-        const int off = (ch >> 3) * (C::TE * 128) + (E == 2 ? (lane & 1) * 8 : 0);
+        const int ch = lane * E / (16 / (int)sizeof(S)), in_chunk = lane * E * (int)sizeof(S) & 15;
 #pragma unroll 2
         for (int e0 = 0; e0 < 32; e0 += 4) {
             if (!((ok >> e0) & 15u)) continue;
@@ -373,9 +565,14 @@ struct PaF32 {
             for (int j = 0; j < 4; j++) {
                 const int e = e0 + j;
                 float2 v[E / 2];
-                const unsigned char *r = vst + off + e * 128 + (((ch & 7) ^ (e & 7)) << 4);
+                const unsigned char *r = vst + C::at(e, ch) + in_chunk;
+                if constexpr (C::QUANT) {
 #pragma unroll
-                for (int i = 0; i < E / 2; i++) v[i] = *reinterpret_cast<const float2 *>(r + i * 8);
+                    for (int i = 0; i < E / 2; i++) v[i] = values2(*reinterpret_cast<const uint16_t *>(r + i * 2));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < E / 2; i++) v[i] = *reinterpret_cast<const float2 *>(r + i * 8);
+                }
                 if (!((ok >> e) & 1u)) {
 #pragma unroll
                     for (int i = 0; i < E / 2; i++) v[i] = make_float2(0.f, 0.f);
@@ -418,12 +615,69 @@ struct PaF32 {
     }
 };
 
+// ------------------------------------------------------------ a shared prefix
+// Four channels (c4) of head h: the prefix's parts, in order, join (M, Z, v).  A part
+// without an entry has reference -inf and sum 0, and its sums may be anything.
+template <bool BF, int D>
+__device__ __forceinline__ void pa_add_prefix(const PrefixParts &pre, int h, int c4, float &M, float &Z, float4 &v) {
+    constexpr int R = BF ? kShRowsTc : kShRowsF32, N = 8;
+    const int row = pre.row + h;
+    for (int p0 = 0; p0 < pre.count; p0 += N) {
+        float m[N], z[N], mx = M;
+        float4 x[N];
+#pragma unroll
+        for (int p = 0; p < N; p++) {
+            const float *q = pre.at + (int64_t)min(p0 + p, pre.count - 1) * pre.step;
+            m[p] = __ldcg(q + R * D + row);
+            z[p] = __ldcg(q + R * (D + 1) + row);
+            x[p] = __ldcg(reinterpret_cast<const float4 *>(q) + (BF ? c4 * R + row : row * (D / 4) + c4));
+        }
+#pragma unroll
+        for (int p = 0; p < N; p++) {
+            const bool none = p0 + p >= pre.count || (m[p] == -INFINITY && z[p] == 0.f);
+            if (none) {
+                m[p] = -INFINITY;
+                z[p] = 0.f;
+                x[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            mx = fmaxf(mx, m[p]);
+        }
+        const float sh = pa_shift(mx), f = tc::ex2(M - sh);
+        M = mx;
+        Z *= f;
+        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll
+        for (int p = 0; p < N; p++) {
+            // a part of NaN weights alone has reference -inf and a NaN sum, which stays
+            const float g = m[p] == -INFINITY && z[p] != 0.f ? 1.f : tc::ex2(m[p] - sh);
+            Z += g * z[p];
+            v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
+        }
+    }
+}
+// Sequence s from its own sums (shared memory; null: none) and its prefix's parts.
+template <typename T, int D>
+__device__ __forceinline__ void pa_join_prefix(const PaArgs &a, int s, int gq, int tid, int threads, const float *sum, const float *M_,
+                                               const float *Z_) {
+    constexpr bool BF = sizeof(T) == 2;
+    const PrefixParts pre = prefix_parts<BF, D>(a.plan, a.tok, s / a.c.G, s % a.c.G, a.c.G, gq);
+    for (int i = tid * 4; i < gq * D; i += threads * 4) {
+        const int h = i / D;
+        float M = sum ? M_[h] : -INFINITY, Z = sum ? Z_[h] : 0.f;
+        float4 v = sum ? *reinterpret_cast<const float4 *>(sum + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+        pa_add_prefix<BF, D>(pre, h, i % D / 4, M, Z, v);
+        const float r = Z == 0.f ? 0.f : 1.f / Z;                                // a NaN stays
+        put4(static_cast<T *>(a.out) + (size_t)s * gq * D + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+    }
+}
+
 // ------------------------------------------------------------------ kernel
-template <typename T, int D, int GQ>
+// SHARED: the parts of a shared prefix join each sequence's.
+template <typename T, typename S_, int D, int GQ, bool SHARED>
 __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     paged_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
-    using C = PaCfg<T, D>;
-    using SM = PaSmem<C::NST, C::TE>;
+    using C = PaCfg<T, S_, D>;
+    using SM = PaSmem<C::NST, C::TE, C::QUANT>;
     extern __shared__ __align__(1024) unsigned char dsm[];
     unsigned char *ring = dsm;                                   // [NST][keys, values]
     float *sum = reinterpret_cast<float *>(dsm + C::NST * 2 * C::TB);        // [8][D]
@@ -499,8 +753,12 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     }
     // sequences without an entry
     for (int s = blockIdx.x; s < S; s += gridDim.x)
-        if (a.lens[s] <= 0)
-            for (int i = tid; i < gq * D; i += kPaThreads) put(static_cast<T *>(a.out) + (size_t)s * gq * D + i, 0.f);
+        if (a.lens[s] <= 0) {
+            if constexpr (SHARED)
+                pa_join_prefix<T, D>(a, s, gq, tid, kPaThreads, nullptr, nullptr, nullptr);
+            else
+                for (int i = tid; i < gq * D; i += kPaThreads) put(static_cast<T *>(a.out) + (size_t)s * gq * D + i, 0.f);
+        }
     __syncthreads();
     if (lo >= hi) return;
 
@@ -539,7 +797,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                 const bool have = u < per_tile && r >= 0;
                 const unsigned units = __ballot_sync(0xffffffffu, have);
                 const uint32_t fb = tc::smem_u32(&sm.full[st]);
-                const uint32_t bytes = (uint32_t)(2 * C::NB * box * 128 + (a.c.log_m ? box * 4 : 0));
+                const uint32_t bytes = (uint32_t)(2 * C::NB * box * C::BW + (a.c.log_m ? box * 4 : 0) + (C::QUANT ? 2 * box : 0));
                 if (lane == 0) {
                     sm.count[st] = min(C::TE, n - t * C::TE);
                     sm.units[st] = units;
@@ -548,11 +806,15 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                 }
                 __syncwarp();
                 if (have) {
-                    const uint32_t kb = tc::smem_u32(ring + st * 2 * C::TB) + (uint32_t)(u * box * 128);
+                    const uint32_t kb = tc::smem_u32(ring + st * 2 * C::TB) + (uint32_t)(u * box * C::BW);
 #pragma unroll
                     for (int b = 0; b < C::NB; b++) {
-                        tc::tma_load_2d(kb + (uint32_t)(b * C::TE * 128), &mapK, b * (128 / (int)sizeof(T)), r, fb);
-                        tc::tma_load_2d(kb + (uint32_t)(C::TB + b * C::TE * 128), &mapV, b * (128 / (int)sizeof(T)), r, fb);
+                        tc::tma_load_2d(kb + (uint32_t)(b * C::TE * C::BW), &mapK, b * (C::BW / (int)sizeof(S_)), r, fb);
+                        tc::tma_load_2d(kb + (uint32_t)(C::TB + b * C::TE * C::BW), &mapV, b * (C::BW / (int)sizeof(S_)), r, fb);
+                    }
+                    if constexpr (C::QUANT) {
+                        pa_bulk(tc::smem_u32(&sm.ks[st][u * box]), a.scales.k + r, (uint32_t)box, fb);
+                        pa_bulk(tc::smem_u32(&sm.vs[st][u * box]), a.scales.v + r, (uint32_t)box, fb);
                     }
                     if (a.c.log_m) pa_bulk(tc::smem_u32(&sm.lm[st][u * box]), a.c.log_m + r, (uint32_t)(box * 4), fb);
                 }
@@ -566,7 +828,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     }
 
     // ---------------- consumers ----------------
-    typename std::conditional<C::BF, PaBf<D>, PaF32<D, GQ>>::type w;
+    typename std::conditional<C::BF, typename std::conditional<C::QUANT, PaE4<D>, PaBf<D>>::type, PaF32<S_, D, GQ>>::type w;
     if constexpr (!C::BF) {
         w.qs = qs;
         w.ps = qs + GQ * D + warp * GQ * 32;
@@ -592,11 +854,12 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             if (!pa_wait(tc::smem_u32(&sm.full[st]), (it / C::NST) & 1, sm, a.status)) continue;
             unsigned char *base = ring + st * 2 * C::TB;
             const int box = min(a.box, C::TE);
+            const uint8_t *ks = sm.ks[C::QUANT ? st : 0], *vsc = sm.vs[C::QUANT ? st : 0];
             if constexpr (C::BF)
-                w.tile(tc::smem_u32(base), tc::smem_u32(base + C::TB), sm.lm[st], sm.count[st], sm.units[st], box, a.scale,
-                       a.c.log_m != nullptr);
+                w.tile(tc::smem_u32(base), tc::smem_u32(base + C::TB), ks, vsc, sm.lm[st], sm.count[st], sm.units[st], box,
+                       a.scale, a.c.log_m != nullptr);
             else
-                w.tile(base, base + C::TB, sm.lm[st], sm.count[st], sm.units[st], box, a.c.log_m != nullptr);
+                w.tile(base, base + C::TB, ks, vsc, sm.lm[st], sm.count[st], sm.units[st], box, a.c.log_m != nullptr);
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sm.empty[st]));
         }
@@ -620,9 +883,13 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         T *out = static_cast<T *>(a.out) + (size_t)s * gq * D;
         const int c_lo = pa_run_of(vs, total, nc), c_hi = pa_run_of(ve - 1, total, nc);
         if (snap || c_lo == c_hi) {
-            for (int i = tid; i < gq * D; i += kPaCons) {
-                const float Z = sm.Z[i / D];
-                put(out + i, Z == 0.f ? 0.f : sum[i] / Z);               // a NaN stays
+            if constexpr (SHARED) {
+                pa_join_prefix<T, D>(a, s, gq, tid, kPaCons, sum, sm.M, sm.Z);
+            } else {
+                for (int i = tid; i < gq * D; i += kPaCons) {
+                    const float Z = sm.Z[i / D];
+                    put(out + i, Z == 0.f ? 0.f : sum[i] / Z);               // a NaN stays
+                }
             }
         } else {
             // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
@@ -637,6 +904,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             if (sm.last) {
                 __threadfence();
                 const int np = c_hi - c_lo + 1;
+                PrefixParts pre{};
+                if constexpr (SHARED) pre = prefix_parts<C::BF, D>(a.plan, a.tok, s / a.c.G, s % a.c.G, a.c.G, gq);
                 auto piece = [&](int p) { return a.part + (size_t)(2 * (c_lo + p) + (p == 0)) * PF; };
                 // four channels a thread, over the pieces in order, N loads in flight: a batch is the latency of a
                 // read (0.8 us), so 16 where there are more than 8 pieces
@@ -673,6 +942,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                                 v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
                             }
                         }
+                        if constexpr (SHARED) pa_add_prefix<C::BF, D>(pre, h, i % D / 4, M, Z, v);
                         const float r = Z == 0.f ? 0.f : 1.f / Z;                // a NaN stays
                         put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
                     }
@@ -686,26 +956,26 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     }
 }
 
-// [rows][D] rows, boxes of [box][128 bytes], 128-byte swizzle.
-template <typename T>
+// [rows][D] rows, boxes of [box][128 or 64 bytes] with a swizzle as wide.
+template <typename C, typename S>
 bool pa_map(CUtensorMap *m, const void *p, int64_t rows, int d, int box) {
     auto enc = tc::tensor_map_encoder();
     if (!enc) return false;
     cuuint64_t gdim[2] = {(cuuint64_t)d, (cuuint64_t)rows};
-    cuuint64_t gstr[1] = {(cuuint64_t)d * sizeof(T)};
-    cuuint32_t bx[2] = {128 / (cuuint32_t)sizeof(T), (cuuint32_t)box};
+    cuuint64_t gstr[1] = {(cuuint64_t)d * sizeof(S)};
+    cuuint32_t bx[2] = {C::BW / (cuuint32_t)sizeof(S), (cuuint32_t)box};
     cuuint32_t es[2] = {1, 1};
-    return enc(m, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
-               const_cast<void *>(p), gdim, gstr, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return enc(m, C::QUANT ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : C::BF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+               2, const_cast<void *>(p), gdim, gstr, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               C::BW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-
-template <typename T, int D, int GQ>
+template <typename T, typename S, int D, int GQ, bool SHARED>
 cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
-    using C = PaCfg<T, D>;
+    using C = PaCfg<T, S, D>;
     static std::atomic<int> grid_of[kMaxDevices];
-    const auto kern = paged_attention_kernel<T, D, GQ>;
+    const auto kern = paged_attention_kernel<T, S, D, GQ, SHARED>;
     const size_t smem = (size_t)C::NST * 2 * C::TB + 8 * D * sizeof(float) +
                         (C::BF ? 0 : (size_t)(GQ * D + kPaWarps * GQ * 32) * sizeof(float));
     int dev = 0;
@@ -726,19 +996,64 @@ cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
     CUtensorMap mk, mv;
     const int64_t rows = a.c.n_pages * a.c.page_size;
     const int box = std::min(a.box, C::TE);
-    if (!pa_map<T>(&mk, a.c.K, rows, D, box) || !pa_map<T>(&mv, a.c.V, rows, D, box)) return cudaErrorNotSupported;
+    if (!pa_map<C, S>(&mk, a.c.K, rows, D, box) || !pa_map<C, S>(&mv, a.c.V, rows, D, box)) return cudaErrorNotSupported;
     return launch_overlapped(kern, grid, kPaThreads, smem, s, a, mk, mv);
 }
 
-template <int D>
+template <typename S, int D, bool SHARED>
 cudaError_t pa_launch_f32(const PaArgs &a, int gq, cudaStream_t s) {
-    return gq == 1 ? pa_launch<float, D, 1>(a, s) : gq == 2 ? pa_launch<float, D, 2>(a, s)
-           : gq <= 4 ? pa_launch<float, D, 4>(a, s) : pa_launch<float, D, 8>(a, s);
+    return gq == 1 ? pa_launch<float, S, D, 1, SHARED>(a, s) : gq == 2 ? pa_launch<float, S, D, 2, SHARED>(a, s)
+           : gq <= 4 ? pa_launch<float, S, D, 4, SHARED>(a, s) : pa_launch<float, S, D, 8, SHARED>(a, s);
+}
+
+template <bool SHARED>
+cudaError_t pa_launch_any(const PaArgs &a, const gkv_paged_cache *c, bool quant, cudaStream_t s) {
+    const int gq = c->Hq / c->G;
+    if (c->dtype == GKV_BF16) {
+        if (quant)
+            return c->d == 128 ? pa_launch<__nv_bfloat16, E4m3, 128, 8, SHARED>(a, s) : pa_launch<__nv_bfloat16, E4m3, 64, 8, SHARED>(a, s);
+        return c->d == 128 ? pa_launch<__nv_bfloat16, __nv_bfloat16, 128, 8, SHARED>(a, s)
+                           : pa_launch<__nv_bfloat16, __nv_bfloat16, 64, 8, SHARED>(a, s);
+    }
+    if (quant) return c->d == 128 ? pa_launch_f32<E4m3, 128, SHARED>(a, gq, s) : pa_launch_f32<E4m3, 64, SHARED>(a, gq, s);
+    return c->d == 128 ? pa_launch_f32<float, 128, SHARED>(a, gq, s) : pa_launch_f32<float, 64, SHARED>(a, gq, s);
 }
 
 constexpr size_t kPaCntBytes = kPaMaxGrid * sizeof(int);
 
 }  // namespace
+
+namespace serve {
+
+size_t paged_scratch_bytes(int d) { return kPaCntBytes + (size_t)2 * kPaMaxGrid * pa_part_floats(d) * sizeof(float); }
+
+gkv_status paged_attention_call(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l, const void *q, void *out,
+                                int *status, void *scratch, const SharedArgs *shared, cudaStream_t s) {
+    if (l < 0 || l >= c->L || !q || !out || !al(q, 16) || !al(out, 16)) return GKV_EINVAL;
+    if (c->page_size % 16) return GKV_EUNSUPPORTED;
+    unsigned char *ws = static_cast<unsigned char *>(scratch);
+    PaArgs a{};
+    a.c = paged_of(c);
+    a.S = c->B * c->G;
+    a.lens = c->lens + (int64_t)l * a.S;
+    a.table = c->table + (int64_t)l * a.S * c->max_pages;
+    a.q = q;
+    a.out = out;
+    a.status = status;
+    a.cnt = reinterpret_cast<int *>(ws);
+    a.part = reinterpret_cast<float *>(ws + kPaCntBytes);
+    a.box = c->page_size % 64 == 0 ? 64 : c->page_size % 32 == 0 ? 32 : 16;
+    a.scale = (float)(1.4426950408889634 / sqrt((double)c->d));
+    if (scales) a.scales = *scales;
+    if (shared) {
+        a.plan = shared->plan;
+        a.tok = shared->tok;
+    }
+    const cudaError_t e = shared ? pa_launch_any<true>(a, c, scales, s) : pa_launch_any<false>(a, c, scales, s);
+    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
+}
+
+}  // namespace serve
 }  // namespace gkv
 
 using namespace gkv;
@@ -747,7 +1062,7 @@ extern "C" gkv_status gracekv_paged_workspace_size(const gkv_paged_cache *c, siz
     const gkv_status st = serve::check_paged_geometry(c);
     if (st != GKV_OK) return st;
     if (!bytes) return GKV_EINVAL;
-    *bytes = serve::kWsHead + kPaCntBytes + (size_t)2 * kPaMaxGrid * pa_part_floats(c->d) * sizeof(float);
+    *bytes = serve::kWsHead + serve::paged_scratch_bytes(c->d);
     return GKV_OK;
 }
 
@@ -755,28 +1070,18 @@ extern "C" gkv_status gracekv_paged_attention(const gkv_paged_cache *c, int32_t 
                                               void *workspace, void *stream) {
     const gkv_status st = serve::check_paged(c);
     if (st != GKV_OK) return st;
-    if (l < 0 || l >= c->L || !q || !out || !workspace) return GKV_EINVAL;
-    if (!serve::al(q, 16) || !serve::al(out, 16) || !serve::al(workspace, 256)) return GKV_EINVAL;
-    if (c->page_size % 16) return GKV_EUNSUPPORTED;
-    unsigned char *ws = static_cast<unsigned char *>(workspace);
-    PaArgs a;
-    a.c = serve::paged_of(c);
-    a.S = c->B * c->G;
-    a.lens = c->lens + (int64_t)l * a.S;
-    a.table = c->table + (int64_t)l * a.S * c->max_pages;
-    a.q = q;
-    a.out = out;
-    a.status = reinterpret_cast<int *>(ws);
-    a.cnt = reinterpret_cast<int *>(ws + serve::kWsHead);
-    a.part = reinterpret_cast<float *>(ws + serve::kWsHead + kPaCntBytes);
-    a.box = c->page_size % 64 == 0 ? 64 : c->page_size % 32 == 0 ? 32 : 16;
-    a.scale = (float)(1.4426950408889634 / sqrt((double)c->d));
-    const int gq = c->Hq / c->G;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (c->dtype == GKV_BF16)
-        e = c->d == 128 ? pa_launch<__nv_bfloat16, 128, 8>(a, s) : pa_launch<__nv_bfloat16, 64, 8>(a, s);
-    else
-        e = c->d == 128 ? pa_launch_f32<128>(a, gq, s) : pa_launch_f32<64>(a, gq, s);
-    return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
+    if (!workspace || !serve::al(workspace, 256)) return GKV_EINVAL;
+    return serve::paged_attention_call(c, nullptr, l, q, out, static_cast<int *>(workspace),
+                                       static_cast<unsigned char *>(workspace) + serve::kWsHead, nullptr,
+                                       static_cast<cudaStream_t>(stream));
+}
+
+extern "C" gkv_status gracekv_quant_attention(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l, const void *q,
+                                              void *out, void *workspace, void *stream) {
+    const gkv_status st = serve::check_quant(c, scales);
+    if (st != GKV_OK) return st;
+    if (!workspace || !serve::al(workspace, 256)) return GKV_EINVAL;
+    return serve::paged_attention_call(c, scales, l, q, out, static_cast<int *>(workspace),
+                                       static_cast<unsigned char *>(workspace) + serve::kWsHead, nullptr,
+                                       static_cast<cudaStream_t>(stream));
 }

@@ -110,7 +110,7 @@ EXPORTED = ["gracekv_default_params", "gracekv_budget_for_ratio", "gracekv_graph
             "gracekv_prompt_workspace_size", "gracekv_prompt_attention", "gracekv_prompt_status",
             "gracekv_paged_workspace_size", "gracekv_paged_load", "gracekv_paged_advance",
             "gracekv_paged_append", "gracekv_paged_attention", "gracekv_paged_status",
-            "gracekv_quant_load", "gracekv_quant_append", "gracekv_paged_read", "gracekv_paged_unload"]
+            "gracekv_quant_load", "gracekv_quant_append", "gracekv_quant_attention", "gracekv_paged_read", "gracekv_paged_unload"]
 
 
 def lib() -> C.CDLL:
@@ -166,6 +166,7 @@ def lib() -> C.CDLL:
     scp = C.POINTER(GkvPagedScales)
     L.gracekv_quant_load.argtypes = [pcp, scp, i32, vp, vp, vp, vp, i64, vp, vp]
     L.gracekv_quant_append.argtypes = [pcp, scp, i32, C.POINTER(GkvPagedTokens), vp, vp]
+    L.gracekv_quant_attention.argtypes = [pcp, scp, i32, vp, vp, vp, vp]
     L.gracekv_paged_read.argtypes = [pcp, scp, i32, C.POINTER(GkvPagedRows), vp, vp]
     L.gracekv_paged_unload.argtypes = [pcp, scp, i32, vp, vp, vp, vp, i64, vp, vp]
     _lib = L
@@ -726,8 +727,7 @@ class PagedCache(_Workspace):
         self._both = (C.byref(self.desc), None if self._scales is None else C.byref(self._scales))
         self._ref = self._both if quant else self._both[:1]
         L_, kind = lib(), "gracekv_quant_" if quant else "gracekv_paged_"
-        self._load, self._append = getattr(L_, kind + "load"), getattr(L_, kind + "append")
-        self._attention = L_.gracekv_paged_attention
+        self._load, self._append, self._attention = (getattr(L_, kind + x) for x in ("load", "append", "attention"))
         self._free = None
 
     @staticmethod

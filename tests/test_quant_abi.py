@@ -93,3 +93,13 @@ def test_the_reference_rounds_as_torch_does():
     codes = (x.double() / 2.0 ** torch.from_numpy(e).double()).float().to(torch.float8_e4m3fn)
     assert np.array_equal(codes.double().numpy() * 2.0 ** e, v)
     assert (np.abs(x.double().numpy()).max(-1) <= 448 * 2.0 ** e[:, 0]).all() and (np.abs(x.double().numpy()).max(-1) > 224 * 2.0 ** e[:, 0]).all()
+
+
+def test_attention_refusals(gk):  # noqa: F811
+    L = gk.lib()
+    sc = C.byref(gk.GkvPagedScales(P, P))
+    call = lambda c, l=0, q=P, out=P, ws=P, s=sc: L.gracekv_quant_attention(c, s, l, q, out, ws, None)  # noqa: E731
+    for kw in (dict(l=2), dict(l=-1), dict(q=None), dict(q=P + 8), dict(out=None), dict(out=P + 8), dict(ws=None), dict(ws=P + 1),
+               dict(s=None), dict(s=C.byref(gk.GkvPagedScales(P, P + 1)))):
+        assert call(paged(gk), **kw) == gk.GKV_EINVAL, kw
+    assert call(paged(gk, page_size=24)) == gk.GKV_EUNSUPPORTED and call(None) == gk.GKV_EINVAL
