@@ -677,6 +677,43 @@ gkv_status gracekv_paged_unload(const gkv_paged_cache *c, const gkv_paged_scales
  * call met a page number, length or offset it did not follow, else GKV_OK. */
 gkv_status gracekv_paged_status(void *workspace, void *stream);
 
+/*
+ * Attention of one token per request where requests share long prefixes (one
+ * compressed context, many questions on it): a prefix is kept once, in a slot of a
+ * paged cache of its own, and attended once for all its requests.  Requests
+ * [cu_prefix[p], cu_prefix[p + 1]) share slot p (device [P + 1], P = prefix->B;
+ * NULL with one slot: all of them do); a request of no slot has no prefix.  For
+ * query head h of request b over layer l, with the entries e of (l, p, g) in the
+ * prefix cache and then those of (l, b, g) in c, g = h / (Hq / G):
+ *     x_e = q_h . k_e / sqrt(d) + log m_e,  out_h = sum_e softmax(x)_e v_e ;
+ * without an entry, or with entries of log m = -inf alone, 0; NaN as in
+ * gracekv_paged_attention.  q, out [B][Hq][d] of the caches' dtype.
+ *
+ * L, G, Hq, d and dtype of both caches are the same; B, pages and their sizes are
+ * each one's own, and each one has scales (quantised pages) or NULL.  rope_base and
+ * c's workspace are not used.  Slots whose cu words run backwards or past B, or that begin
+ * below the end of an earlier one whose own words fit, are left out (their requests have no prefix)
+ * and gracekv_shared_status reports GKV_EINVAL, as it does for pages and lengths
+ * that are not followed; the others are computed.
+ * Values: as gracekv_paged_attention, but for bf16 rows the weights of the
+ * prefix's entries are rounded to bf16 for the value product (their sum is not).
+ */
+
+/* Bytes of the device workspace: a function of both caches' L, B, G, Hq, d and
+ * dtype alone.  The caller allocates it 256-byte aligned and zeroes it once.  One
+ * workspace serves one stream at a time. */
+gkv_status gracekv_shared_workspace_size(const gkv_paged_cache *c, const gkv_paged_cache *prefix, size_t *bytes);
+
+/* Enqueues the attention on `stream`.  page_size must be a multiple of 16 in both
+ * caches (GKV_EUNSUPPORTED).  Errors: GKV_EINVAL, GKV_EUNSUPPORTED, GKV_ECUDA. */
+gkv_status gracekv_shared_attention(const gkv_paged_cache *c, const gkv_paged_scales *scales, const gkv_paged_cache *prefix,
+                                    const gkv_paged_scales *prefix_scales, int32_t l, const int32_t *cu_prefix,
+                                    const void *q, void *out, void *workspace, void *stream);
+
+/* Synchronises `stream` and reports (then clears) the workspace's status word, as
+ * gracekv_paged_status. */
+gkv_status gracekv_shared_status(void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,8 +23,12 @@ constexpr int kShKeysTc = 128, kShKeysF32 = 64;        // keys of a tile
 __host__ __device__ constexpr int shared_tok(bool bf16, int gq) { return bf16 ? 2 * (kShRowsTc / gq) : kShRowsF32 / gq; }
 // Blocks of rows of one KV head at most: sum over slots of ceil(n_p / tok).
 __host__ __device__ inline int64_t shared_row_blocks(int B, int P, int tok) { return (int64_t)B / tok + P; }
-// Pieces at most (plan kernel).
-__host__ __device__ inline int64_t shared_pieces(int64_t blocks) { return blocks + 2 * kShSms; }
+// Pieces at most: one a SM where the blocks are few enough to share the SMs among them, else (a block's last
+// piece is a partial one) as many as fill the SMs twice and one more a block.
+constexpr int kShFewBlocks = kShSms / 2;
+__host__ __device__ inline int64_t shared_pieces(int64_t blocks) {
+    return blocks <= kShFewBlocks ? kShSms : blocks + 2 * kShSms;
+}
 // Floats of a part: sums by 4 channels, the rows' references (base 2), their weights' sums.
 __host__ __device__ constexpr size_t shared_part_floats(bool bf16, int d) {
     return (size_t)(bf16 ? kShRowsTc : kShRowsF32) * (d + 2);
@@ -35,6 +39,7 @@ __host__ __device__ constexpr int shared_halves(bool bf16) { return bf16 ? 2 : 1
 // The plan, in the workspace.
 struct SharedPlan {
     int *pieces;            // their number
+    int4 *piece;            // [pieces][2] (slot, first request, requests, entries), (head, first key tile, end, 0)
     int2 *req;              // [B] (block of rows, place in it) of a request, (-1, 0) for none
     int4 *blk;              // [blocks] (slot, first request, requests, entries); block = block of rows * G + head
     int *first;             // [blocks + 1] first piece

@@ -110,7 +110,8 @@ EXPORTED = ["gracekv_default_params", "gracekv_budget_for_ratio", "gracekv_graph
             "gracekv_prompt_workspace_size", "gracekv_prompt_attention", "gracekv_prompt_status",
             "gracekv_paged_workspace_size", "gracekv_paged_load", "gracekv_paged_advance",
             "gracekv_paged_append", "gracekv_paged_attention", "gracekv_paged_status",
-            "gracekv_quant_load", "gracekv_quant_append", "gracekv_quant_attention", "gracekv_paged_read", "gracekv_paged_unload"]
+            "gracekv_quant_load", "gracekv_quant_append", "gracekv_quant_attention", "gracekv_paged_read", "gracekv_paged_unload",
+            "gracekv_shared_workspace_size", "gracekv_shared_attention", "gracekv_shared_status"]
 
 
 def lib() -> C.CDLL:
@@ -169,6 +170,9 @@ def lib() -> C.CDLL:
     L.gracekv_quant_attention.argtypes = [pcp, scp, i32, vp, vp, vp, vp]
     L.gracekv_paged_read.argtypes = [pcp, scp, i32, C.POINTER(GkvPagedRows), vp, vp]
     L.gracekv_paged_unload.argtypes = [pcp, scp, i32, vp, vp, vp, vp, i64, vp, vp]
+    L.gracekv_shared_workspace_size.argtypes = [pcp, pcp, C.POINTER(C.c_size_t)]
+    L.gracekv_shared_attention.argtypes = [pcp, scp, pcp, scp, i32, vp, vp, vp, vp, vp]
+    L.gracekv_shared_status.argtypes = [vp, vp]
     _lib = L
     return L
 
@@ -963,3 +967,46 @@ class PagedCache(_Workspace):
 
     def status(self, stream=None):
         self._run(lib().gracekv_paged_status, self._ws, self._on(stream))
+
+
+class SharedAttention(_Workspace):
+    """Decoding attention of requests that share prefixes (gracekv_shared_* of the C ABI).
+
+    cache holds the requests' own entries, prefix (a PagedCache of the same L, G, Hq,
+    d and dtype; either may be quantised) one prefix a slot, read once for all the
+    requests that share it.  One object holds the workspace of one stream.
+    """
+
+    def __init__(self, cache: PagedCache, prefix: PagedCache):
+        if prefix._device != cache._device:
+            raise _bad(f"the prefix is on {prefix._device}, the cache on {cache._device}")
+        self.cache, self.prefix = cache, prefix
+        n = C.c_size_t()
+        _raise(lib().gracekv_shared_workspace_size(cache._both[0], prefix._both[0], C.byref(n)))
+        self._make_workspace(n.value, cache._device)
+        self._call = lib().gracekv_shared_attention
+
+    def __call__(self, l: int, q, cu_prefix=None, out=None, stream=None):
+        """q [B, Hq, d], one rotated query per request slot -> out [B, Hq, d] over layer l:
+        requests cu_prefix[p]... cu_prefix[p + 1] (int32 [prefix.B + 1]; None with one
+        prefix slot: all) attend prefix slot p's entries and then their own."""
+        c, x, dev = self.cache, self.prefix, self._device
+        shape = (c.B, c.Hq, c.d)
+        qp = _words("q", q, shape, c.dtype, dev)
+        cp = None
+        if cu_prefix is not None:
+            cp = _words("cu_prefix", cu_prefix, (x.B + 1,), torch.int32, dev)
+        elif x.B != 1:
+            raise _bad(f"{x.B} prefix slots and no cu_prefix")
+        if out is None:
+            out = _empty_like_on(stream, shape, c.dtype, dev)
+            op = out.data_ptr()
+        else:
+            op = _words("out", out, shape, c.dtype, dev)
+        c._on(stream, *c._pool)
+        x._on(stream, *x._pool)
+        self._run(self._call, *c._both, *x._both, l, cp, qp, op, self._ws, self._on(stream, q, cu_prefix, out))
+        return out
+
+    def status(self, stream=None):
+        self._run(lib().gracekv_shared_status, self._ws, self._on(stream))

@@ -103,3 +103,28 @@ def test_attention_refusals(gk):  # noqa: F811
                dict(s=None), dict(s=C.byref(gk.GkvPagedScales(P, P + 1)))):
         assert call(paged(gk), **kw) == gk.GKV_EINVAL, kw
     assert call(paged(gk, page_size=24)) == gk.GKV_EUNSUPPORTED and call(None) == gk.GKV_EINVAL
+
+
+def shared(gk, c=None, p=None, sc=None, psc=None, l=0, cu=P, q=P, out=P, ws=P):
+    c, p = paged(gk) if c is None else c, paged(gk) if p is None else p
+    return gk.lib().gracekv_shared_attention(c, sc, p, psc, l, cu, q, out, ws, None)
+
+
+def test_shared_refusals(gk):  # noqa: F811
+    for kw in (dict(l=2), dict(l=-1), dict(cu=P + 2), dict(cu=None), dict(q=None), dict(q=P + 8), dict(out=None), dict(out=P + 4),
+               dict(ws=None), dict(ws=P + 128), dict(sc=C.byref(gk.GkvPagedScales(P, None))),
+               dict(psc=C.byref(gk.GkvPagedScales(P + 2, P)))):
+        assert shared(gk, **kw) == gk.GKV_EINVAL, kw
+    for kw in (dict(L=1), dict(G=1), dict(Hq=4), dict(d=128), dict(dtype=gk.GKV_F32)):       # caches of different models
+        assert shared(gk, p=paged(gk, **kw)) == gk.GKV_EINVAL, kw
+        assert shared(gk, c=paged(gk, **kw)) == gk.GKV_EINVAL, kw
+    for kw in (dict(B=0), dict(K=None), dict(lens=P + 1), dict(n_pages=0)):
+        assert shared(gk, p=paged(gk, **kw)) == gk.GKV_EINVAL and shared(gk, c=paged(gk, **kw)) == gk.GKV_EINVAL, kw
+    assert shared(gk, p=paged(gk, page_size=24)) == gk.GKV_EUNSUPPORTED and shared(gk, c=paged(gk, page_size=8)) == gk.GKV_EUNSUPPORTED
+    n, L = C.c_size_t(), gk.lib()
+    assert L.gracekv_shared_workspace_size(paged(gk), paged(gk, B=1), C.byref(n)) == gk.GKV_OK and n.value > 256
+    assert L.gracekv_shared_workspace_size(paged(gk), paged(gk), None) == gk.GKV_EINVAL
+    assert L.gracekv_shared_workspace_size(None, paged(gk), C.byref(n)) == gk.GKV_EINVAL
+    assert L.gracekv_shared_workspace_size(paged(gk), None, C.byref(n)) == gk.GKV_EINVAL
+    assert L.gracekv_shared_workspace_size(paged(gk, d=96), paged(gk, d=96), C.byref(n)) == gk.GKV_EUNSUPPORTED
+    assert L.gracekv_shared_status(None, None) == gk.GKV_EINVAL
