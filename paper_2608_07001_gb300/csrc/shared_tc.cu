@@ -18,10 +18,10 @@
 //
 // Warps: 0-3 and 4-7 softmax (a thread a row), 8 looks pages up and issues TMA
 // (boxes of up to 64 entries that do not cross a page; K and V tiles through a ring,
-// log m through a ring of its own), 9 and 10 issue the MMAs of row tile 0 and 1, 11
-// turns log m into base 2, masks what no page or length covers, and zeroes V rows
-// that such entries would take from stale memory (0 P V is NaN for what is not
-// finite).  Quantised pages: codes come through a ring of their own, and a
+// log m through a ring of its own) and zeroes V rows of entries that are not there,
+// which are stale memory (0 times what is not finite is NaN), 9 and 10 issue the MMAs
+// of row tile 0 and 1, 11 turns log m into base 2 and masks what no page or length
+// covers.  Quantised pages: codes come through a ring of their own, and a
 // warpgroup more (12-15) writes the tiles as bf16, code times scale, exactly: from
 // there on nothing differs.
 // P is rounded to bf16 once, as A and B of a product have one type; Z is not.
@@ -61,7 +61,7 @@ struct Cfg {
 template <int NST, int NR>
 struct Bars {
     uint64_t full[NST], empty[NST], rfull[NR], rempty[NR], qfull[2], sfull[2], pfull[2][2], odone[2];
-    uint64_t lfull[NBIAS], bfull[NBIAS], bempty[NBIAS], fin;
+    uint64_t lfull[NBIAS], bfull[NBIAS], bempty[NBIAS], vfix[NBIAS], fin;
     alignas(16) float bias[NBIAS][NK];
     alignas(16) uint8_t rscale[NR][NR > 1 ? NK : 16];
     unsigned units[NBIAS];             // boxes of the tile that were read
@@ -105,10 +105,6 @@ __device__ __forceinline__ float log2_m(float lm) {
     return fabsf(lm) <= FLT_MAX ? fminf(fmaxf(lm * kLog2e, -FLT_MAX), FLT_MAX) : lm;
 }
 
-// The order of a piece's tiles in the ring: L key tiles, then V(j) and K(j + L) in turn.
-__device__ __forceinline__ int k_seq(int j, int L) { return j < L ? j : 2 * j - L + 1; }
-__device__ __forceinline__ int v_seq(int j, int L, int n) { return j + min(n, L + j); }
-
 template <int D, bool QUANT>
 __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     shared_tc_kernel(const SharedArgs a, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -150,7 +146,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     if (warp == kWarpTma && lane == 0) {                 // the thread that uses them first
         for (int i = 0; i < NST; i++) {
             tc::mbar_init(tc::smem_u32(&b.full[i]), QUANT ? 4 : 1);
-            tc::mbar_init(tc::smem_u32(&b.empty[i]), two ? 2 : 1);
+            tc::mbar_init(tc::smem_u32(&b.empty[i]), 2);
         }
         for (int i = 0; i < NR; i++) {
             tc::mbar_init(tc::smem_u32(&b.rfull[i]), 1);
@@ -165,6 +161,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         for (int i = 0; i < NBIAS; i++) {
             tc::mbar_init(tc::smem_u32(&b.lfull[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.bfull[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.vfix[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.bempty[i]), two ? 8 : 4);
         }
         tc::mbar_init(tc::smem_u32(&b.fin), 2);
@@ -396,6 +393,25 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             for (int j = 0; ok && j < min(L, n); j++) key(j);
             for (int j = 0; ok && j < n; j++) {
                 next(mapV, win[1], j, a.scales.v);
+                if (ok && !QUANT) {
+                    // V rows of entries that are not there: 0, once the tile has landed (which this warp, having waited
+                    // for the slot's last use, is the one to see without mistaking the phase)
+                    const int count = min(NK, len - (j0 + j) * NK), row = rows_of(win[1], j), st = (issued - 1) % NST;
+                    const unsigned units = __ballot_sync(0xffffffffu, lane < per_tile && row >= 0);
+                    if (count < NK || units != (1u << per_tile) - 1) {
+                        ok = __all_sync(0xffffffffu, wait(&b.full[st], ((issued - 1) / NST) & 1, b, a.status));
+                        if (!ok) break;
+                        for (int i = lane; i < NK * C::NB * 8; i += 32) {
+                            const int r = i / (C::NB * 8), cb = i % (C::NB * 8);
+                            if (r < count && ((units >> (r / box)) & 1u)) continue;
+                            *reinterpret_cast<uint4 *>(ring + st * C::TILE + (cb >> 3) * (NK * 128) + r * 128 + (cb & 7) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.vfix[j % NBIAS]));
+                }
                 if (ok && j + L < n) key(j + L);
             }
             // the copies still in flight land before the block exits
@@ -427,17 +443,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 *reinterpret_cast<float4 *>(&b.bias[sl][k0]) = v;
                 const bool special = __any_sync(0xffffffffu, !there || k0 + 3 >= count);
                 if (lane == 0) b.special[sl] = special;
-                if (special && !QUANT) {
-                    const int sq = v_seq(j, L, n), st = sq % NST;
-                    if (!__all_sync(0xffffffffu, wait(&b.full[st], (sq / NST) & 1, b, a.status))) break;
-                    for (int i = lane; i < NK * C::NB * 8; i += 32) {
-                        const int r = i / (C::NB * 8), cb = i % (C::NB * 8);
-                        if (r < count && ((units >> (r / box)) & 1u)) continue;
-                        *reinterpret_cast<uint4 *>(ring + st * C::TILE + (cb >> 3) * (NK * 128) + r * 128 + (cb & 7) * 16) =
-                            make_uint4(0, 0, 0, 0);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
+                // before the weights, and so before the product that they enter
+                if (special && !QUANT && !__all_sync(0xffffffffu, wait(&b.vfix[sl], (j / NBIAS) & 1, b, a.status))) break;
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bfull[sl]));
             }
@@ -451,43 +458,58 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             const uint32_t ts = tb + i * NK, to = tb + 2 * NK + i * D;
             const bool one = tc::elect_one();
             bool ok = start >= n || wait(&b.qfull[qi], 0, b, a.status);
-            // S = Q K(j)^T, and K(j)'s slot is free
-            auto scores = [&](int j) {
-                const int sq = k_seq(j, L), st = sq % NST;
-                ok = wait(&b.full[st], (sq / NST) & 1, b, a.status) && ok;
+            // Both warps walk the ring in its order and release every slot, whoever uses it: a warp that passed over a
+            // slot's phase could take the one after it for landed.
+            int st = 0;
+            uint32_t ph = 0, pp = 0;                     // of the slot that comes next; of the weights
+            auto arrived = [&] {
+                ok = wait(&b.full[st], ph, b, a.status) && ok;
                 tc::tc_fence_after();
-                if (ok && one) {
-                    const uint32_t ka = kd + st * (C::TILE >> 4);
+                const int at = st;
+                if (++st == NST) { st = 0; ph ^= 1; }
+                return at;
+            };
+            auto mine = [&](int j) { return two || (j & 1) == i; };
+            auto key = [&](int j) {
+                const int at = arrived();
+                if (!ok || !one) return;
+                if (mine(j)) {
+                    const uint32_t ka = kd + at * (C::TILE >> 4);
 #pragma unroll
                     for (int cb = 0; cb < C::NB; cb++)
 #pragma unroll
                         for (int x = 0; x < 4; x++)
                             tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
                     tc::mma_commit(tc::smem_u32(&b.sfull[i]));
-                    tc::mma_commit(tc::smem_u32(&b.empty[st]));
+                    tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                } else {
+                    tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
                 }
             };
-            if (start < n) scores(start);
-            uint32_t ph = 0;
-            for (int j = start; ok && j < n; j += step, ph ^= 1) {
-                const int sq = v_seq(j, L, n), st = sq % NST;
-                ok = wait(&b.full[st], (sq / NST) & 1, b, a.status) && ok;
-                const uint32_t va = vd + st * (C::TILE >> 4);
+            for (int j = 0; j < min(L, n); j++) key(j);
+            for (int j = 0; ok && j < n; j++) {
+                const int at = arrived();
+                if (mine(j)) {
+                    const uint32_t va = vd + at * (C::TILE >> 4);
 #pragma unroll
-                for (int k = 0; k < 2; k++) {            // the weights come in halves
-                    ok = wait(&b.pfull[i][k], ph, b, a.status) && ok;
-                    tc::tc_fence_after();
-                    if (ok && one) {
+                    for (int k = 0; k < 2; k++) {        // the weights come in halves
+                        ok = wait(&b.pfull[i][k], pp, b, a.status) && ok;
+                        tc::tc_fence_after();
+                        if (ok && one) {
 #pragma unroll
-                        for (int x = k * 4; x < k * 4 + 4; x++)
-                            tc::mma_bf16_ts_lo(to, ts + x * 8, va + x * (16 * 128 >> 4), idO, j != start || x != 0);
+                            for (int x = k * 4; x < k * 4 + 4; x++)
+                                tc::mma_bf16_ts_lo(to, ts + x * 8, va + x * (16 * 128 >> 4), idO, j != start || x != 0);
+                        }
                     }
+                    pp ^= 1;
+                    if (ok && one) {
+                        tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                        if (j + step >= n) tc::mma_commit(tc::smem_u32(&b.odone[i]));
+                    }
+                } else if (ok && one) {
+                    tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
                 }
-                if (ok && one) {
-                    tc::mma_commit(tc::smem_u32(&b.empty[st]));
-                    if (j + step >= n) tc::mma_commit(tc::smem_u32(&b.odone[i]));
-                }
-                if (j + step < n) scores(j + step);
+                if (ok && j + L < n) key(j + L);
             }
             ok = __all_sync(0xffffffffu, ok);
             if (!ok && lane == 0) {

@@ -338,3 +338,50 @@ def test_a_prefix_in_the_requests_own_pool(gk):
             return R.entries(K.cpu(), t, n).double(), R.entries(V.cpu(), t, n).double(), torch.zeros(n).double()
     want, tol = expected(q, S(own), S(pre), [0, 3])
     assert ((out.double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [5, 40])
+def test_long_runs_of_tiles(gk, quant, d, B):
+    """Pieces of fifty key tiles and more, read from memory rather than L2: rings turn many times, tiles land out of order.
+
+    The values are independent of the weights, so an output is a sum of terms w v of random signs, and rounding every
+    w by at most 2^-8 of itself moves it by a sum of such terms 2^-8 as large: 2^-8 of the outputs in norm, and as much
+    again for rounding them."""
+    G, gq, n, ps = 8, 4, 131072, 64
+    g = torch.Generator(device="cuda").manual_seed(B)
+    pool = []
+    for _ in range(2):
+        x = torch.empty(G * n // ps, ps, d, dtype=BF, device="cuda").normal_(generator=g)
+        pool.append(x)
+    real_kv = [x.float() for x in pool]
+    sc = {}
+    if quant:
+        for i, name in enumerate(("k_scale", "v_scale")):
+            e = torch.randint(117, 121, pool[i].shape[:2], generator=g, device="cuda", dtype=torch.int32)
+            s = (e << 23).view(torch.float32).unsqueeze(-1)
+            pool[i] = (real_kv[i] / s).clamp(-448, 448).to(torch.float8_e4m3fn)
+            real_kv[i] = pool[i].float() * s
+            sc[name] = e.to(torch.uint8)
+        sc["dtype"] = BF
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = torch.randperm(G * n // ps, generator=g, device="cuda").to(torch.int32).view(1, 1, G, -1)
+    prefix = gk.PagedCache(*pool, table, torch.full((1, 1, G), n - 37, **i32), Hq=G * gq, **sc)
+    own = gk.PagedCache(torch.zeros(1, 16, d, dtype=BF, device="cuda"), torch.zeros(1, 16, d, dtype=BF, device="cuda"),
+                        torch.full((1, B, G, 1), -1, **i32), torch.zeros(1, B, G, **i32), Hq=G * gq)
+    q = torch.empty(B, G * gq, d, dtype=BF, device="cuda").normal_(generator=g)
+    f = gk.SharedAttention(own, prefix)
+    flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    outs = []
+    for _ in range(3):
+        flush.zero_()
+        outs.append(f(0, q))
+    f.status()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    for h in range(G):
+        k, v = (x[table[0, 0, h].long()].view(n, d)[:n - 37].double() for x in real_kv)
+        x = q[:, h * gq:(h + 1) * gq].reshape(-1, d).double() @ k.T / math.sqrt(d)
+        want = (torch.softmax(x, dim=1) @ v).view(B, gq, d)
+        got = outs[0][:, h * gq:(h + 1) * gq].double()
+        assert float((got - want).norm() / want.norm()) < 2.0 ** -7
