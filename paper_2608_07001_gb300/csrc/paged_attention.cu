@@ -50,7 +50,7 @@
 // quotient is 0 only where no weight at all was summed.
 #include "paged.cuh"
 #include "quant.cuh"
-#include "shared.cuh"
+#include "shared_plan.cuh"
 #include "tc.cuh"
 
 #include <float.h>
@@ -106,9 +106,12 @@ struct PaArgs {
     int box;                    // rows of a box
     float scale;                // log2(e) / sqrt(d)
     gkv_paged_scales scales;    // of quantised pools
-    SharedPlan plan;            // of a shared prefix
-    int tok;
 };
+struct PaSharedArgs : PaArgs {
+    SharedArgs shared;
+};
+template <bool SHARED>
+using PaArgsOf = typename std::conditional<SHARED, PaSharedArgs, PaArgs>::type;
 
 template <int NST, int TE, bool QUANT>
 struct PaSmem {
@@ -615,67 +618,11 @@ struct PaF32 {
     }
 };
 
-// ------------------------------------------------------------ a shared prefix
-// Four channels (c4) of head h: the prefix's parts, in order, join (M, Z, v).  A part
-// without an entry has reference -inf and sum 0, and its sums may be anything.
-template <bool BF, int D>
-__device__ __forceinline__ void pa_add_prefix(const PrefixParts &pre, int h, int c4, float &M, float &Z, float4 &v) {
-    constexpr int R = BF ? kShRowsTc : kShRowsF32, N = 8;
-    const int row = pre.row + h;
-    for (int p0 = 0; p0 < pre.count; p0 += N) {
-        float m[N], z[N], mx = M;
-        float4 x[N];
-#pragma unroll
-        for (int p = 0; p < N; p++) {
-            const float *q = pre.at + (int64_t)min(p0 + p, pre.count - 1) * pre.step;
-            m[p] = __ldcg(q + R * D + row);
-            z[p] = __ldcg(q + R * (D + 1) + row);
-            x[p] = __ldcg(reinterpret_cast<const float4 *>(q) + (BF ? c4 * R + row : row * (D / 4) + c4));
-        }
-#pragma unroll
-        for (int p = 0; p < N; p++) {
-            const bool none = p0 + p >= pre.count || (m[p] == -INFINITY && z[p] == 0.f);
-            if (none) {
-                m[p] = -INFINITY;
-                z[p] = 0.f;
-                x[p] = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            mx = fmaxf(mx, m[p]);
-        }
-        const float sh = pa_shift(mx), f = tc::ex2(M - sh);
-        M = mx;
-        Z *= f;
-        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-#pragma unroll
-        for (int p = 0; p < N; p++) {
-            // a part of NaN weights alone has reference -inf and a NaN sum, which stays
-            const float g = m[p] == -INFINITY && z[p] != 0.f ? 1.f : tc::ex2(m[p] - sh);
-            Z += g * z[p];
-            v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
-        }
-    }
-}
-// Sequence s from its own sums (shared memory; null: none) and its prefix's parts.
-template <typename T, int D>
-__device__ __forceinline__ void pa_join_prefix(const PaArgs &a, int s, int gq, int tid, int threads, const float *sum, const float *M_,
-                                               const float *Z_) {
-    constexpr bool BF = sizeof(T) == 2;
-    const PrefixParts pre = prefix_parts<BF, D>(a.plan, a.tok, s / a.c.G, s % a.c.G, a.c.G, gq);
-    for (int i = tid * 4; i < gq * D; i += threads * 4) {
-        const int h = i / D;
-        float M = sum ? M_[h] : -INFINITY, Z = sum ? Z_[h] : 0.f;
-        float4 v = sum ? *reinterpret_cast<const float4 *>(sum + i) : make_float4(0.f, 0.f, 0.f, 0.f);
-        pa_add_prefix<BF, D>(pre, h, i % D / 4, M, Z, v);
-        const float r = Z == 0.f ? 0.f : 1.f / Z;                                // a NaN stays
-        put4(static_cast<T *>(a.out) + (size_t)s * gq * D + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-    }
-}
-
 // ------------------------------------------------------------------ kernel
-// SHARED: the parts of a shared prefix join each sequence's.
+// SHARED: the plan of a shared prefix is made by the first block, and sequences leave parts to be joined with it.
 template <typename T, typename S_, int D, int GQ, bool SHARED>
 __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
-    paged_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
+    paged_attention_kernel(const PaArgsOf<SHARED> a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
     using C = PaCfg<T, S_, D>;
     using SM = PaSmem<C::NST, C::TE, C::QUANT>;
     extern __shared__ __align__(1024) unsigned char dsm[];
@@ -700,6 +647,14 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         tc::tma_prefetch_desc(&mapV);
     }
     after_previous();
+    const int nblocks = (int)gridDim.x - SHARED, block = (int)blockIdx.x - SHARED;
+    if constexpr (SHARED) {
+        static_assert(sizeof(PlanSmem<kPaThreads>) <= kPaRing / 2, "plan");
+        if (block < 0) {
+            make_plan<kPaThreads>(a.shared, *reinterpret_cast<PlanSmem<kPaThreads> *>(dsm));
+            return;
+        }
+    }
 
     // ---- the CTA's run: tiles of all sequences, and where its own begin
     const int seg = (S + kPaThreads - 1) / kPaThreads;
@@ -736,10 +691,10 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     // sequences: 11.0 of 2 tiles, 11.8 of 4, 14.4 of 8; fp32, 1000 entries of 10 in tiles of 32: 11.5 of 1,
     // 12.7 of 2, 14.0 of 4.)
     const int least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
-    const int nc = total <= kPaNarrow ? min((int)gridDim.x, (int)(((uint32_t)total + least - 1) / (uint32_t)least))
-                                      : (int)min((long long)gridDim.x, (total + least - 1) / least);
-    const long long lo = (int)blockIdx.x < nc ? pa_run_first(blockIdx.x, total, nc) : total;
-    const long long hi = (int)blockIdx.x < nc ? pa_run_first(blockIdx.x + 1, total, nc) : total;
+    const int nc = total <= kPaNarrow ? min(nblocks, (int)(((uint32_t)total + least - 1) / (uint32_t)least))
+                                      : (int)min((long long)nblocks, (total + least - 1) / least);
+    const long long lo = block < nc ? pa_run_first(block, total, nc) : total;
+    const long long hi = block < nc ? pa_run_first(block + 1, total, nc) : total;
     if (lo < hi && lo >= before && lo < before + mine) {
         int s = tid * seg;
         for (;; s++) {
@@ -752,12 +707,13 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         sm.first = before;
     }
     // sequences without an entry
-    for (int s = blockIdx.x; s < S; s += gridDim.x)
+    for (int s = block; s < S; s += nblocks)
         if (a.lens[s] <= 0) {
-            if constexpr (SHARED)
-                pa_join_prefix<T, D>(a, s, gq, tid, kPaThreads, nullptr, nullptr, nullptr);
-            else
+            if constexpr (SHARED) {
+                if (tid < gq) a.shared.plan.own_mz[(size_t)s * gq + tid] = make_float2(-INFINITY, 0.f);
+            } else {
                 for (int i = tid; i < gq * D; i += kPaThreads) put(static_cast<T *>(a.out) + (size_t)s * gq * D + i, 0.f);
+            }
         }
     __syncthreads();
     if (lo >= hi) return;
@@ -884,7 +840,9 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         const int c_lo = pa_run_of(vs, total, nc), c_hi = pa_run_of(ve - 1, total, nc);
         if (snap || c_lo == c_hi) {
             if constexpr (SHARED) {
-                pa_join_prefix<T, D>(a, s, gq, tid, kPaCons, sum, sm.M, sm.Z);
+                for (int i = tid * 4; i < gq * D; i += kPaCons * 4)
+                    *reinterpret_cast<float4 *>(a.shared.plan.own + (size_t)s * gq * D + i) = *reinterpret_cast<const float4 *>(sum + i);
+                if (tid < gq) a.shared.plan.own_mz[(size_t)s * gq + tid] = make_float2(sm.M[tid], sm.Z[tid]);
             } else {
                 for (int i = tid; i < gq * D; i += kPaCons) {
                     const float Z = sm.Z[i / D];
@@ -894,7 +852,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         } else {
             // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
             constexpr int PF = pa_part_floats(D);
-            float *pp = a.part + (size_t)(2 * blockIdx.x + ((int)blockIdx.x == c_lo)) * PF;
+            float *pp = a.part + (size_t)(2 * block + (block == c_lo)) * PF;
             for (int i = tid; i < gq * D; i += kPaCons) pp[i] = sum[i];
             if (tid < gq) { pp[8 * D + tid] = sm.M[tid]; pp[8 * D + 8 + tid] = sm.Z[tid]; }
             __threadfence();
@@ -904,8 +862,6 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             if (sm.last) {
                 __threadfence();
                 const int np = c_hi - c_lo + 1;
-                PrefixParts pre{};
-                if constexpr (SHARED) pre = prefix_parts<C::BF, D>(a.plan, a.tok, s / a.c.G, s % a.c.G, a.c.G, gq);
                 auto piece = [&](int p) { return a.part + (size_t)(2 * (c_lo + p) + (p == 0)) * PF; };
                 // four channels a thread, over the pieces in order, N loads in flight: a batch is the latency of a
                 // read (0.8 us), so 16 where there are more than 8 pieces
@@ -942,9 +898,13 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
                                 v.x += g * x[p].x; v.y += g * x[p].y; v.z += g * x[p].z; v.w += g * x[p].w;
                             }
                         }
-                        if constexpr (SHARED) pa_add_prefix<C::BF, D>(pre, h, i % D / 4, M, Z, v);
-                        const float r = Z == 0.f ? 0.f : 1.f / Z;                // a NaN stays
-                        put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+                        if constexpr (SHARED) {
+                            *reinterpret_cast<float4 *>(a.shared.plan.own + (size_t)s * gq * D + i) = v;
+                            if (i % D == 0) a.shared.plan.own_mz[(size_t)s * gq + h] = make_float2(M, Z);
+                        } else {
+                            const float r = Z == 0.f ? 0.f : 1.f / Z;            // a NaN stays
+                            put4(out + i, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+                        }
                     }
                 };
                 if (np > 8) join(std::integral_constant<int, 16>()); else join(std::integral_constant<int, 8>());
@@ -972,7 +932,7 @@ bool pa_map(CUtensorMap *m, const void *p, int64_t rows, int d, int box) {
 }
 
 template <typename T, typename S, int D, int GQ, bool SHARED>
-cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
+cudaError_t pa_launch(const PaArgsOf<SHARED> &a, cudaStream_t s) {
     using C = PaCfg<T, S, D>;
     static std::atomic<int> grid_of[kMaxDevices];
     const auto kern = paged_attention_kernel<T, S, D, GQ, SHARED>;
@@ -1001,13 +961,13 @@ cudaError_t pa_launch(PaArgs a, cudaStream_t s) {
 }
 
 template <typename S, int D, bool SHARED>
-cudaError_t pa_launch_f32(const PaArgs &a, int gq, cudaStream_t s) {
+cudaError_t pa_launch_f32(const PaArgsOf<SHARED> &a, int gq, cudaStream_t s) {
     return gq == 1 ? pa_launch<float, S, D, 1, SHARED>(a, s) : gq == 2 ? pa_launch<float, S, D, 2, SHARED>(a, s)
            : gq <= 4 ? pa_launch<float, S, D, 4, SHARED>(a, s) : pa_launch<float, S, D, 8, SHARED>(a, s);
 }
 
 template <bool SHARED>
-cudaError_t pa_launch_any(const PaArgs &a, const gkv_paged_cache *c, bool quant, cudaStream_t s) {
+cudaError_t pa_launch_any(const PaArgsOf<SHARED> &a, const gkv_paged_cache *c, bool quant, cudaStream_t s) {
     const int gq = c->Hq / c->G;
     if (c->dtype == GKV_BF16) {
         if (quant)
@@ -1032,7 +992,7 @@ gkv_status paged_attention_call(const gkv_paged_cache *c, const gkv_paged_scales
     if (l < 0 || l >= c->L || !q || !out || !al(q, 16) || !al(out, 16)) return GKV_EINVAL;
     if (c->page_size % 16) return GKV_EUNSUPPORTED;
     unsigned char *ws = static_cast<unsigned char *>(scratch);
-    PaArgs a{};
+    PaSharedArgs a{};
     a.c = paged_of(c);
     a.S = c->B * c->G;
     a.lens = c->lens + (int64_t)l * a.S;
@@ -1045,10 +1005,7 @@ gkv_status paged_attention_call(const gkv_paged_cache *c, const gkv_paged_scales
     a.box = c->page_size % 64 == 0 ? 64 : c->page_size % 32 == 0 ? 32 : 16;
     a.scale = (float)(1.4426950408889634 / sqrt((double)c->d));
     if (scales) a.scales = *scales;
-    if (shared) {
-        a.plan = shared->plan;
-        a.tok = shared->tok;
-    }
+    if (shared) a.shared = *shared;
     const cudaError_t e = shared ? pa_launch_any<true>(a, c, scales, s) : pa_launch_any<false>(a, c, scales, s);
     return e == cudaSuccess ? GKV_OK : GKV_ECUDA;
 }

@@ -1,10 +1,10 @@
 // shared.cuh -- the attention over a shared prefix as its kernels see it.
 //
-// Requests [cu[p], cu[p + 1]) of a batch share slot p of a prefix cache.  A
-// launch of one block makes the plan, a second one attends the slots' entries
-// for all their requests at once (shared_tc.cu, shared_f32.cu) and leaves parts,
-// a third one attends the requests' own entries and joins everything
-// (paged_attention.cu).
+// Requests [cu[p], cu[p + 1]) of a batch share slot p of a prefix cache.  Three
+// launches: the requests' own entries (paged_attention.cu), whose first block makes
+// the plan meanwhile (shared_plan.cuh); the slots' entries, for all their requests at
+// once (shared_tc.cu, shared_f32.cu); and the join of the parts that both leave
+// (shared_attention.cu).
 //
 // The rows of (slot, KV head) are its requests' gq query heads, `tok` requests
 // to a block of rows; a block's key tiles are cut into pieces, one CTA each.
@@ -44,6 +44,8 @@ struct SharedPlan {
     int4 *blk;              // [blocks] (slot, first request, requests, entries); block = block of rows * G + head
     int *first;             // [blocks + 1] first piece
     float *part;            // [pieces][halves][part floats]
+    float *own;             // [B][Hq][D] sums over the requests' own entries
+    float2 *own_mz;         // [B][Hq] their references and sums of weights
 };
 
 struct SharedArgs {
@@ -51,6 +53,7 @@ struct SharedArgs {
     gkv_paged_scales scales;
     SharedPlan plan;
     int B, P, tok, blocks;  // requests, slots, requests of a block of rows, blocks at most
+    int keys, pieces;       // keys of a tile, pieces at most
     const int32_t *lens, *table;                       // of the layer
     const int32_t *cu;      // [P + 1]; null: one slot for all
     const void *q;          // [B][Hq][d]
@@ -92,8 +95,8 @@ __device__ __forceinline__ PrefixParts prefix_parts(const SharedPlan &p, int tok
 cudaError_t launch_shared_tc(const SharedArgs &a, int d, bool quant, cudaStream_t s);
 cudaError_t launch_shared_f32(const SharedArgs &a, int d, bool quant, cudaStream_t s);
 
-// Attention of a request's own entries (paged_attention.cu); with shared, joined with its prefix's parts.  Its own
-// scratch: ws of paged_scratch_bytes(d), zeroed once.
+// Attention of a request's own entries (paged_attention.cu): out; or, with shared, the plan of the prefix and the own
+// parts.  Its scratch: paged_scratch_bytes(d), zeroed once.
 size_t paged_scratch_bytes(int d);
 gkv_status paged_attention_call(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l, const void *q, void *out,
                                 int *status, void *scratch, const SharedArgs *shared, cudaStream_t s);

@@ -1,5 +1,5 @@
 // shared_attention.cu -- attention of one token per request where requests
-// share long prefixes (gracekv_shared_*): its plan, its arguments.
+// share long prefixes (gracekv_shared_*): its arguments, the join of its parts.
 //
 // For request b of slot p and a query head of KV head g, over the entries of the
 // prefix (l, p, g) and then of the request's own (l, b, g):
@@ -11,12 +11,14 @@
 // rows of a matrix product) and only (M, Z, O) is kept of it per row.
 // Reading the prefix once bounds it for few requests, the products for many.
 //
-// The plan: the blocks of rows of all slots, and how many pieces each one's keys
-// are cut into, so that the pieces fill the SMs at a time that is the least of 32
-// candidates' (one a warp).
+//
+// The join: a thread holds four channels of a row, over the parts in order with
+// eight loads of each in flight.  The bf16 kernel's parts lie by channel, so a warp's
+// lanes are rows; the fp32 kernel's by row.
+#include "quant.cuh"
 #include "shared.cuh"
+#include "tc.cuh"
 
-#include <limits.h>
 #include <math.h>
 
 namespace gkv {
@@ -24,164 +26,90 @@ namespace {
 
 using namespace serve;
 
-constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
-constexpr int kPieceStart = 5;             // what a piece costs beside its tiles, in tiles
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinC4 = 8;         // rows and groups of 4 channels of a block
 
-__device__ __forceinline__ int warp_scan_max(int v) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
-        if ((threadIdx.x & 31) >= o) v = max(v, u);
-    }
-    return v;
-}
-__device__ __forceinline__ int warp_scan_sum(int v) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
-        if ((threadIdx.x & 31) >= o) v += u;
-    }
-    return v;
-}
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
-// keys: of a tile.
-__global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a, int keys, int most) {
-    __shared__ int w_max[kPlanWarps], w_sum[kPlanWarps], lo_s[kPlanThreads], n_s[kPlanThreads], rb_s[kPlanThreads];
-    __shared__ long long w_cost[kPlanWarps];
-    __shared__ int w_run[kPlanWarps];
-    __shared__ unsigned long long total_s;
-    __shared__ int blocks_s, most_s;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.c.G;
+template <typename T, int D>
+__global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedArgs a, T *out) {
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int R = BF ? kShRowsTc : kShRowsF32, N = 8;
+    __shared__ float4 v_s[kJoinRows][kJoinC4 + 1];
+    __shared__ float m_s[kJoinRows], z_s[kJoinRows];
     next_may_start();
-    if (tid == 0) {
-        total_s = 0;
-        blocks_s = 0;
-        most_s = 0;
-    }
     after_previous();
-    for (int b = tid; b < a.B; b += kPlanThreads) a.plan.req[b] = make_int2(-1, 0);
-    __syncthreads();
-
-    // ---- the slots' requests.  A slot is left out when its words do not ascend within the batch, or when it
-    // begins below the end of an earlier one whose own do; the others have their requests to themselves.
-    int end = 0, base = 0;                               // largest end, blocks of rows so far
-    for (int p0 = 0; p0 < a.P; p0 += kPlanThreads) {
-        const int p = p0 + tid;
-        int lo = 0, hi = 0;
-        if (p < a.P) {
-            lo = a.cu ? a.cu[p] : 0;
-            hi = a.cu ? a.cu[p + 1] : a.B;
-        }
-        const bool fits = lo >= 0 && lo <= hi && hi <= a.B;
-        const int upto = warp_scan_max(fits ? hi : 0);
-        if (lane == 31) w_max[warp] = upto;
-        __syncthreads();
-        int before = __shfl_up_sync(0xffffffffu, upto, 1);
-        if (lane == 0) before = 0;
-        before = max(before, end);
-        for (int w = 0; w < kPlanWarps; w++) {
-            if (w < warp) before = max(before, w_max[w]);
-            end = max(end, w_max[w]);
-        }
-        const bool owned = p < a.P && fits && (lo >= before || lo == hi);
-        if (p < a.P && !owned) atomicOr(a.status, kStRange);
-        const int n = owned ? hi - lo : 0, rb = (n + a.tok - 1) / a.tok;
-        const int incl = warp_scan_sum(rb);
-        if (lane == 31) w_sum[warp] = incl;
-        __syncthreads();
-        int first = base + incl - rb;
-        for (int w = 0; w < kPlanWarps; w++) {
-            if (w < warp) first += w_sum[w];
-            base += w_sum[w];
-        }
-        lo_s[tid] = lo;
-        n_s[tid] = n;
-        rb_s[tid] = first;
-        __syncthreads();
-        for (int s = warp; s < min(kPlanThreads, a.P - p0); s += kPlanWarps) {
-            const int l0 = lo_s[s], ns = n_s[s], r0 = rb_s[s];
-            for (int i = lane; i < ns; i += 32) a.plan.req[l0 + i] = make_int2(r0 + i / a.tok, i % a.tok);
-            const int nb = (ns + a.tok - 1) / a.tok * G;
-            for (int i = lane; i < nb; i += 32) {
-                const int rb_i = i / G, g = i % G, len = a.lens[(int64_t)(p0 + s) * G + g];
-                const int cap = a.c.page_size * a.c.max_pages, k = max(0, min(len, cap));
-                if (len > cap) atomicOr(a.status, kStRange);
-                a.plan.blk[(r0 + rb_i) * G + g] = make_int4(p0 + s, l0 + rb_i * a.tok, min(a.tok, ns - rb_i * a.tok), k);
-                const int t = (k + keys - 1) / keys;
-                atomicAdd(&total_s, (unsigned long long)t);
-                if (t > 0) atomicAdd(&blocks_s, 1);
-                atomicMax(&most_s, t);
-            }
-        }
-        __syncthreads();
-    }
-    const int blocks = base * G, used = blocks_s, longest = most_s;
-    const long long total = (long long)total_s;
-    auto tiles = [&](int i) { return (a.plan.blk[i].w + keys - 1) / keys; };
-
-    // ---- tiles of a piece: the candidates lie between an even share of all tiles and what is sure to give no more
-    // pieces than there is room for (sum of ceil(t / run) <= total / run + used)
-    const int room = most - used;                        // at least half of the SMs, or twice the SMs
-    const int share = (int)min((total + most - 1) / most, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
-    {
-        const long long widest = max((long long)sure, min((long long)longest, 4ll * sure));
-        const int run = max(1, (int)(share + (widest - share) * warp / (kPlanWarps - 1)));
-        long long n = 0;
-        for (int i = lane; i < blocks; i += 32) n += (tiles(i) + run - 1) / run;
+    const int gq = a.c.Hq / a.c.G, reqs = kJoinRows / gq, tid = threadIdx.x;
+    const int g = blockIdx.x % a.c.G, b0 = blockIdx.x / a.c.G * reqs, c0 = blockIdx.y * kJoinC4;
+    const int rr = BF ? tid % kJoinRows : tid / kJoinC4, cc = BF ? tid / kJoinRows : tid % kJoinC4;
+    const int b = b0 + rr / gq, h = rr % gq;
+    float M = -INFINITY, Z = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (rr / gq < reqs && b < a.B) {
+        const PrefixParts pre = prefix_parts<BF, D>(a.plan, a.tok, b, g, a.c.G, gq);
+        const int row = pre.row + h, c4 = c0 + cc;
+        for (int p0 = 0; p0 < pre.count; p0 += N) {
+            float m[N], z[N], mx = M;
+            float4 x[N];
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        if (lane == 0) {
-            w_run[warp] = run;
-            w_cost[warp] = n > most ? LLONG_MAX : (n + kShSms - 1) / kShSms * (run + kPieceStart);
-        }
-    }
-    __syncthreads();
-    long long best = LLONG_MAX;
-    int run = max(1, sure);
-    for (int w = 0; w < kPlanWarps; w++)
-        if (w_cost[w] < best) {
-            best = w_cost[w];
-            run = w_run[w];
-        }
-
-    // ---- the pieces
-    int pieces = 0;
-    for (int i0 = 0; i0 < blocks; i0 += kPlanThreads) {
-        const int i = i0 + tid;
-        const int4 k = i < blocks ? a.plan.blk[i] : make_int4(0, 0, 0, 0);
-        const int t = (k.w + keys - 1) / keys, np = (t + run - 1) / run;
-        const int incl = warp_scan_sum(np);
-        if (lane == 31) w_sum[warp] = incl;
-        __syncthreads();
-        int first = pieces + incl - np;
-        for (int w = 0; w < kPlanWarps; w++) {
-            if (w < warp) first += w_sum[w];
-            pieces += w_sum[w];
-        }
-        if (i < blocks) a.plan.first[i] = first;
-        // a warp writes the pieces of its 32 blocks, a block at a time
-        for (int s = 0; s < 32; s++) {
-            const int n = __shfl_sync(0xffffffffu, np, s), f = __shfl_sync(0xffffffffu, first, s), ts = __shfl_sync(0xffffffffu, t, s);
-            const int4 ks = make_int4(__shfl_sync(0xffffffffu, k.x, s), __shfl_sync(0xffffffffu, k.y, s),
-                                      __shfl_sync(0xffffffffu, k.z, s), __shfl_sync(0xffffffffu, k.w, s));
-            const int g = (i0 + warp * 32 + s) % G;
-            for (int j = lane; j < n; j += 32) {
-                a.plan.piece[2 * (f + j)] = ks;
-                a.plan.piece[2 * (f + j) + 1] = make_int4(g, (int)((long long)j * ts / n), (int)((j + 1ll) * ts / n), 0);
+            for (int p = 0; p < N; p++) {
+                const float *q = pre.at + (int64_t)min(p0 + p, pre.count - 1) * pre.step;
+                m[p] = __ldcg(q + R * D + row);
+                z[p] = __ldcg(q + R * (D + 1) + row);
+                x[p] = __ldcg(reinterpret_cast<const float4 *>(q) + (BF ? c4 * R + row : row * (D / 4) + c4));
+            }
+#pragma unroll
+            for (int p = 0; p < N; p++) {
+                // past the last part, or one without an entry, whose sums may be anything
+                if (p0 + p >= pre.count || (m[p] == -INFINITY && z[p] == 0.f)) {
+                    m[p] = -INFINITY;
+                    z[p] = 0.f;
+                    x[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                mx = fmaxf(mx, m[p]);
+            }
+            const float sh = shift_of(mx), f = tc::ex2(M - sh);
+            M = mx;
+            Z *= f;
+            v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll
+            for (int p = 0; p < N; p++) {
+                // a part of NaN weights alone has reference -inf and a NaN sum, which stays
+                const float w = m[p] == -INFINITY && z[p] != 0.f ? 1.f : tc::ex2(m[p] - sh);
+                Z += w * z[p];
+                v.x += w * x[p].x; v.y += w * x[p].y; v.z += w * x[p].z; v.w += w * x[p].w;
             }
         }
-        __syncthreads();
     }
-    if (tid == 0) {
-        a.plan.first[blocks] = pieces;
-        *a.plan.pieces = pieces;
-    }
+    v_s[rr][cc] = v;
+    if (cc == 0) { m_s[rr] = M; z_s[rr] = Z; }
+    __syncthreads();
+    // the own part, and out: by row
+    const int r2 = tid / kJoinC4, k2 = tid % kJoinC4, b2 = b0 + r2 / gq;
+    if (r2 / gq >= reqs || b2 >= a.B) return;
+    const int64_t at = (int64_t)b2 * a.c.Hq + g * gq + r2 % gq;
+    const float2 own = __ldcg(a.plan.own_mz + at);
+    const bool none = own.x == -INFINITY && own.y == 0.f;
+    const float m1 = m_s[r2], z1 = z_s[r2], mx = fmaxf(m1, none ? -INFINITY : own.x), sh = shift_of(mx);
+    float4 x = v_s[r2][k2], y = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!none) y = __ldcg(reinterpret_cast<const float4 *>(a.plan.own + at * D) + c0 + k2);
+    const float w1 = m1 == -INFINITY && z1 != 0.f ? 1.f : tc::ex2(m1 - sh);
+    const float w2 = none ? 0.f : own.x == -INFINITY ? 1.f : tc::ex2(own.x - sh);
+    const float Zs = w1 * z1 + w2 * own.y, r = Zs == 0.f ? 0.f : 1.f / Zs;                 // a NaN stays
+    put4(out + at * D + (c0 + k2) * 4, make_float4((w1 * x.x + w2 * y.x) * r, (w1 * x.y + w2 * y.y) * r,
+                                                   (w1 * x.z + w2 * y.z) * r, (w1 * x.w + w2 * y.w) * r));
+}
+
+template <typename T, int D>
+cudaError_t launch_join(const SharedArgs &a, void *out, cudaStream_t s) {
+    const int reqs = kJoinRows / (a.c.Hq / a.c.G);
+    const dim3 grid((unsigned)(((a.B + reqs - 1) / reqs) * a.c.G), D / 4 / kJoinC4);
+    return launch_overlapped(shared_join_kernel<T, D>, grid, kJoinThreads, 0, s, a, static_cast<T *>(out));
 }
 
 struct Layout {
     int tok;
     int64_t blocks, pieces;
-    size_t scratch, counts, req, blk, first, piece, part, bytes;
+    size_t scratch, counts, req, blk, first, piece, part, own, own_mz, bytes;
 };
 
 gkv_status layout_of(const gkv_paged_cache *c, const gkv_paged_cache *prefix, Layout &y) {
@@ -202,7 +130,9 @@ gkv_status layout_of(const gkv_paged_cache *c, const gkv_paged_cache *prefix, La
     y.first = up(y.blk + (size_t)y.blocks * sizeof(int4));
     y.piece = up(y.first + (size_t)(y.blocks + 1) * sizeof(int));
     y.part = up(y.piece + (size_t)y.pieces * 2 * sizeof(int4));
-    y.bytes = y.part + (size_t)y.pieces * shared_halves(bf16) * shared_part_floats(bf16, c->d) * sizeof(float);
+    y.own = up(y.part + (size_t)y.pieces * shared_halves(bf16) * shared_part_floats(bf16, c->d) * sizeof(float));
+    y.own_mz = up(y.own + (size_t)c->B * c->Hq * c->d * sizeof(float));
+    y.bytes = y.own_mz + (size_t)c->B * c->Hq * sizeof(float2);
     return GKV_OK;
 }
 
@@ -241,11 +171,14 @@ extern "C" gkv_status gracekv_shared_attention(const gkv_paged_cache *c, const g
     a.c = serve::paged_of(prefix);
     if (prefix_scales) a.scales = *prefix_scales;
     a.plan = {reinterpret_cast<int *>(ws + y.counts), reinterpret_cast<int4 *>(ws + y.piece), reinterpret_cast<int2 *>(ws + y.req),
-              reinterpret_cast<int4 *>(ws + y.blk), reinterpret_cast<int *>(ws + y.first), reinterpret_cast<float *>(ws + y.part)};
+              reinterpret_cast<int4 *>(ws + y.blk), reinterpret_cast<int *>(ws + y.first), reinterpret_cast<float *>(ws + y.part),
+              reinterpret_cast<float *>(ws + y.own), reinterpret_cast<float2 *>(ws + y.own_mz)};
     a.B = c->B;
     a.P = prefix->B;
     a.tok = y.tok;
     a.blocks = (int)y.blocks;
+    a.keys = bf16 ? serve::kShKeysTc : serve::kShKeysF32;
+    a.pieces = (int)y.pieces;
     a.lens = prefix->lens + (int64_t)l * S;
     a.table = prefix->table + (int64_t)l * S * prefix->max_pages;
     a.cu = cu_prefix;
@@ -253,11 +186,12 @@ extern "C" gkv_status gracekv_shared_attention(const gkv_paged_cache *c, const g
     a.status = reinterpret_cast<int *>(ws);
     a.box = prefix->page_size % 64 == 0 ? 64 : prefix->page_size % 32 == 0 ? 32 : 16;
     a.scale = (float)(1.4426950408889634 / sqrt((double)c->d));
-    cudaError_t e = serve::launch_overlapped(shared_plan_kernel, 1, kPlanThreads, 0, s, a,
-                                             bf16 ? serve::kShKeysTc : serve::kShKeysF32, (int)y.pieces);
-    if (e == cudaSuccess) e = bf16 ? serve::launch_shared_tc(a, c->d, prefix_scales, s) : serve::launch_shared_f32(a, c->d, prefix_scales, s);
-    if (e != cudaSuccess) return e == cudaErrorInvalidConfiguration ? GKV_EUNSUPPORTED : GKV_ECUDA;
-    return serve::paged_attention_call(c, scales, l, q, out, a.status, ws + y.scratch, &a, s);
+    if ((st = serve::paged_attention_call(c, scales, l, q, out, a.status, ws + y.scratch, &a, s)) != GKV_OK) return st;
+    cudaError_t e = bf16 ? serve::launch_shared_tc(a, c->d, prefix_scales, s) : serve::launch_shared_f32(a, c->d, prefix_scales, s);
+    if (e == cudaSuccess)
+        e = bf16 ? (c->d == 128 ? launch_join<__nv_bfloat16, 128>(a, out, s) : launch_join<__nv_bfloat16, 64>(a, out, s))
+                 : (c->d == 128 ? launch_join<float, 128>(a, out, s) : launch_join<float, 64>(a, out, s));
+    return e == cudaSuccess ? GKV_OK : e == cudaErrorInvalidConfiguration ? GKV_EUNSUPPORTED : GKV_ECUDA;
 }
 
 extern "C" gkv_status gracekv_shared_status(void *workspace, void *stream) {

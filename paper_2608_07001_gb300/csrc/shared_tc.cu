@@ -42,7 +42,7 @@ constexpr int kWarpTma = 8, kWarpMma = 9, kWarpBias = 11, kWarpConv = 12;
 constexpr float kLazy = 8.f;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int NK = kShKeysTc;                              // keys of a tile
-constexpr int NBIAS = 2;                                   // slots of log m
+constexpr int NBIAS = 4;                                   // slots of log m
 
 template <int D, bool QUANT>
 struct Cfg {
@@ -51,7 +51,7 @@ struct Cfg {
     static constexpr uint32_t RAW = 128 * D;               // bytes of a tile of codes
     static constexpr int NST = QUANT ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);       // ring slots, bf16
     static constexpr int NR = QUANT ? (D == 128 ? 3 : 6) : 1;                          // ring slots, codes
-    static constexpr size_t SMEM = 1024 + 2 * (size_t)TILE + NST * (size_t)TILE + (QUANT ? NR * (size_t)RAW : 0);
+    static constexpr size_t SMEM = 2 * (size_t)TILE + NST * (size_t)TILE + (QUANT ? NR * (size_t)RAW : 0);
     static constexpr int THREADS = QUANT ? 512 : 384;
     // Registers a thread at launch, then of the softmax, issue and conversion warps; the sums agree.
     static constexpr int REGS = QUANT ? 128 : 168, RSOFT = QUANT ? 184 : 208, RISSUE = QUANT ? 64 : 88, RCONV = 80;
@@ -111,10 +111,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                      const __grid_constant__ CUtensorMap mapV) {
     using C = Cfg<D, QUANT>;
     constexpr int NST = C::NST, NR = C::NR;
-    extern __shared__ __align__(1024) unsigned char raw_smem[];
-    unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) &
-                                                            ~static_cast<uintptr_t>(1023));
-    unsigned char *Qs = base, *ring = base + 2 * C::TILE, *codes = ring + NST * C::TILE;
+    extern __shared__ __align__(1024) unsigned char Qs[];
+    unsigned char *ring = Qs + 2 * C::TILE, *codes = ring + NST * C::TILE;
     __shared__ Bars<NST, NR> b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
