@@ -696,7 +696,10 @@ gkv_status gracekv_paged_status(void *workspace, void *stream);
  * and gracekv_shared_status reports GKV_EINVAL, as it does for pages and lengths
  * that are not followed; the others are computed.
  * Values: as gracekv_paged_attention, but for bf16 rows the weights of the
- * prefix's entries are rounded to bf16 for the value product (their sum is not).
+ * prefix's entries are rounded once for the value product (their sum is not): to bf16,
+ * over quantised pages to f16, where values of less than 2^-33 of the largest one
+ * that has a weight count 0, and queries of less than 2^-24 lose bits.  A
+ * log m of more than 2^40 ln 2 in size counts as that.
  */
 
 /* Bytes of the device workspace: a function of both caches' L, B, G, Hq, d and

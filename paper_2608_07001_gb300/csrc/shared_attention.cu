@@ -28,6 +28,10 @@ using namespace serve;
 
 constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinC4 = 8;         // rows and groups of 4 channels of a block
 
+// A part's reference, held within kShMost.
+__device__ __forceinline__ float held(float m) {
+    return fabsf(m) >= kShMost * 0.999f && fabsf(m) <= FLT_MAX ? copysignf(kShMost, m) : m;
+}
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <typename T, int D>
@@ -53,7 +57,7 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedA
 #pragma unroll
             for (int p = 0; p < N; p++) {
                 const float *q = pre.at + (int64_t)min(p0 + p, pre.count - 1) * pre.step;
-                m[p] = __ldcg(q + R * D + row);
+                m[p] = held(__ldcg(q + R * D + row));
                 z[p] = __ldcg(q + R * (D + 1) + row);
                 x[p] = __ldcg(reinterpret_cast<const float4 *>(q) + (BF ? c4 * R + row : row * (D / 4) + c4));
             }
@@ -73,8 +77,8 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedA
             v.x *= f; v.y *= f; v.z *= f; v.w *= f;
 #pragma unroll
             for (int p = 0; p < N; p++) {
-                // a part of NaN weights alone has reference -inf and a NaN sum, which stays
-                const float w = m[p] == -INFINITY && z[p] != 0.f ? 1.f : tc::ex2(m[p] - sh);
+                // (a part of NaN weights alone has reference -inf and a NaN sum, which stays)
+                const float w = tc::ex2(m[p] - sh);
                 Z += w * z[p];
                 v.x += w * x[p].x; v.y += w * x[p].y; v.z += w * x[p].z; v.w += w * x[p].w;
             }
@@ -87,14 +91,14 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedA
     const int r2 = tid / kJoinC4, k2 = tid % kJoinC4, b2 = b0 + r2 / gq;
     if (r2 / gq >= reqs || b2 >= a.B) return;
     const int64_t at = (int64_t)b2 * a.c.Hq + g * gq + r2 % gq;
-    const float2 own = __ldcg(a.plan.own_mz + at);
+    float2 own = __ldcg(a.plan.own_mz + at);
+    own.x = held(own.x);
     const bool none = own.x == -INFINITY && own.y == 0.f;
     const float m1 = m_s[r2], z1 = z_s[r2], mx = fmaxf(m1, none ? -INFINITY : own.x), sh = shift_of(mx);
     float4 x = v_s[r2][k2], y = make_float4(0.f, 0.f, 0.f, 0.f);
     if (!none) y = __ldcg(reinterpret_cast<const float4 *>(a.plan.own + at * D) + c0 + k2);
-    const float w1 = m1 == -INFINITY && z1 != 0.f ? 1.f : tc::ex2(m1 - sh);
-    const float w2 = none ? 0.f : own.x == -INFINITY ? 1.f : tc::ex2(own.x - sh);
-    const float Zs = w1 * z1 + w2 * own.y, r = Zs == 0.f ? 0.f : 1.f / Zs;                 // a NaN stays
+    const float w1 = tc::ex2(m1 - sh), w2 = none ? 0.f : tc::ex2(own.x - sh);
+    const float Zs = w1 * z1 + (none ? 0.f : w2 * own.y), r = Zs == 0.f ? 0.f : 1.f / Zs;                // a NaN stays
     put4(out + at * D + (c0 + k2) * 4, make_float4((w1 * x.x + w2 * y.x) * r, (w1 * x.y + w2 * y.y) * r,
                                                    (w1 * x.z + w2 * y.z) * r, (w1 * x.w + w2 * y.w) * r));
 }

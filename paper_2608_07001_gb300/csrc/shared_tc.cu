@@ -4,11 +4,16 @@
 // A CTA takes a piece: the gq query heads of up to `tok` requests (two row tiles
 // of 128) over a run of key tiles of 128 entries of one (slot, KV head).  For a row
 // tile
-//   S = Q K^T (fp32 in TMEM), y = S c + log m log2(e), c = log2(e) / sqrt(d),
+//   S = Q K^T + sqrt(d) log m (fp32 in TMEM), y = S c, c = log2(e) / sqrt(d),
 //   P = 2^(y - M), Z += sum P, O += P V,
 // with M a reference that follows the running maximum only when that has grown by
 // more than 2^kLazy, so that O is rescaled in TMEM a few times instead of once a
 // tile; (M, Z, O) of every row leave as the piece's parts.
+// log m joins as one more K step of the product, 1 1 1 against its three bf16 parts
+// (24 bits), and so does -inf for what no length or page covers: the softmax of a
+// thread, which has a row, would otherwise read 128 words of shared memory a tile
+// and find the maximum by hand (1650 clocks of 3400), where the load from TMEM
+// returns it.
 // Two row tiles take every key tile, each with its own softmax warps.  Where the
 // requests fill one row tile at most, both warpgroups work on it, each with every
 // other key tile and sums of its own, which are two parts.
@@ -17,14 +22,23 @@
 // products of 128^3; many: by the tensor pipe and the 128^2 exponentials a tile.
 //
 // Warps: 0-3 and 4-7 softmax (a thread a row), 8 looks pages up and issues TMA
-// (boxes of up to 64 entries that do not cross a page; K and V tiles through a ring,
-// log m through a ring of its own) and zeroes V rows of entries that are not there,
-// which are stale memory (0 times what is not finite is NaN), 9 and 10 issue the MMAs
-// of row tile 0 and 1, 11 turns log m into base 2 and masks what no page or length
-// covers.  Quantised pages: codes come through a ring of their own, and a
-// warpgroup more (12-15) writes the tiles as bf16, code times scale, exactly: from
-// there on nothing differs.
-// P is rounded to bf16 once, as A and B of a product have one type; Z is not.
+// (boxes of up to 64 entries that do not cross a page; K and V tiles through a ring)
+// and zeroes rows of entries that are not there, which are stale memory (0 times
+// what is not finite is NaN), 9 and 10 issue the MMAs of row tile 0 and 1, 11 makes
+// the K step of log m.
+// P is rounded once, as A and B of a product have one type; Z is not.  The scaling
+// goes into the exponent's own FMA, whose result is exact but for one rounding as
+// long as references stay below 2^20 (kFar); beyond, it is a step of its own.
+//
+// Quantised pages: codes come through a ring of their own, and a warpgroup more
+// (12-15) writes the tiles as f16, 3 clocks for two codes (as bf16 with their scale 8,
+// which bounded a tile: 2700 of 5100 clocks).  With k_e, v_e the scales' exponents,
+//   K' = code 2^(k_e - k),  V' = code 2^(v_e - E),  y = S 2^q 2^k c,  O 2^E in the end,
+// k the largest k_e of the tile, E the largest v_e so far, of entries that have a
+// weight at all (no -inf), q the power of two that brings a row's queries into f16 (its
+// largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
+// largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M) has 11 bits,
+// at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.
 #include "quant.cuh"
 #include "shared.cuh"
 #include "tc.cuh"
@@ -39,35 +53,42 @@ namespace serve {
 namespace {
 
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpBias = 11, kWarpConv = 12;
-constexpr float kLazy = 8.f;
+constexpr float kLazy = 8.f;                               // log2 of the growth a reference lets pass
+constexpr float kHead = 7.f;                               // f16: log2 of where the weights start
+constexpr float kFar = 1 << 20;
+constexpr int kNoScale = -120;                             // E before any entry
+constexpr int kLeastQ = -30, kLeastK = -40;                // least q and k, so that kShMost 2^-q 2^-k is a number
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int NK = kShKeysTc;                              // keys of a tile
-constexpr int NBIAS = 4;                                   // slots of log m
+constexpr int NBIAS = 4;                                   // slots of the K step of log m
+constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
+constexpr int NFIX = 8;                                    // tiles that the ring holds, at most (10 slots), and more
+constexpr int kBiased = 1, kSpecial = 2;                   // of a tile: log m; entries that are not there
 
 template <int D, bool QUANT>
 struct Cfg {
-    static constexpr int NB = D / 64;                      // 64-channel blocks of a bf16 row
-    static constexpr uint32_t TILE = NB * 128 * 128;       // bytes of a 128-row bf16 tile
+    static constexpr int NB = D / 64;                      // 64-channel blocks of a 16-bit row
+    static constexpr uint32_t TILE = NB * 128 * 128;       // bytes of a 128-row 16-bit tile
     static constexpr uint32_t RAW = 128 * D;               // bytes of a tile of codes
-    static constexpr int NST = QUANT ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);       // ring slots, bf16
-    static constexpr int NR = QUANT ? (D == 128 ? 3 : 6) : 1;                          // ring slots, codes
-    static constexpr size_t SMEM = 2 * (size_t)TILE + NST * (size_t)TILE + (QUANT ? NR * (size_t)RAW : 0);
+    static constexpr int NST = QUANT ? (D == 128 ? 3 : 6) : (D == 128 ? 4 : 10);       // ring slots, 16-bit
+    // ring slots of codes beside two row tiles of queries; one row tile leaves room for two more
+    static constexpr int NR = QUANT ? (D == 128 ? 2 : 6) : 0;
+    static constexpr int NQA = QUANT ? 2 : 1;              // left sides of the K step: by row, or the same for all
+    static constexpr size_t SMEM = 2 * (size_t)TILE + NST * (size_t)TILE + (NBIAS + NQA) * (size_t)AUG + NR * (size_t)RAW;
     static constexpr int THREADS = QUANT ? 512 : 384;
     // Registers a thread at launch, then of the softmax, issue and conversion warps; the sums agree.
     static constexpr int REGS = QUANT ? 128 : 168, RSOFT = QUANT ? 184 : 208, RISSUE = QUANT ? 64 : 88, RCONV = 80;
     static_assert(256 * RSOFT + 128 * RISSUE + (QUANT ? 128 * RCONV : 0) <= THREADS * REGS, "register split");
+    static_assert(NST <= 2 * NFIX - 2, "fixed tiles");
 };
 
-template <int NST, int NR>
+template <int NST, int NR, bool QUANT>
 struct Bars {
-    uint64_t full[NST], empty[NST], rfull[NR], rempty[NR], qfull[2], sfull[2], pfull[2][2], odone[2];
-    uint64_t lfull[NBIAS], bfull[NBIAS], bempty[NBIAS], vfix[NBIAS], fin;
-    alignas(16) float bias[NBIAS][NK];
-    alignas(16) uint8_t rscale[NR][NR > 1 ? NK : 16];
-    unsigned units[NBIAS];             // boxes of the tile that were read
-    int special[NBIAS];                // some key of the tile is not there
-    unsigned runits[NR];
-    int rcount[NR];                    // entries of the stage's tile up to the sequence's end
+    uint64_t full[NST], empty[NST], rfull[NR + 2], rempty[NR + 2], qfull[2], qready[2], sfull[2], pfull[2][2], odone[2];
+    uint64_t bfull[NBIAS], bempty[NBIAS], kfix[NFIX], vfix[NFIX], fin;
+    alignas(16) __half kmul[QUANT ? NBIAS : 1][QUANT ? NK : 8], vmul[QUANT ? NBIAS : 1][QUANT ? NK : 8];   // 2^(k_e - k), 2^(v_e - E)
+    float qscale[2][QUANT ? 128 : 1];  // 2^q
+    int kind[NBIAS], ktop[NBIAS], vtop[NBIAS];             // k, E
     uint32_t tbase;
     int abort;
 };
@@ -95,14 +116,39 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
-__device__ __forceinline__ void bulk(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
-                 : "memory");
+__device__ __forceinline__ uint32_t f16x2_of(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
-// log m in base 2: finite values stay finite, the others what they are.
-__device__ __forceinline__ float log2_m(float lm) {
-    return fabsf(lm) <= FLT_MAX ? fminf(fmaxf(lm * kLog2e, -FLT_MAX), FLT_MAX) : lm;
+// Two codes as f16 times a scale.
+__device__ __forceinline__ uint32_t half2_of(uint32_t c, __half2 s) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+    const __half2 x = __hmul2(*reinterpret_cast<const __half2 *>(&h), s);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+// 2^e in f16, e <= 0; 0 below its smallest.
+__device__ __forceinline__ __half half_pow2(int e) {
+    return __ushort_as_half((unsigned short)(e >= -14 ? (e + 15) << 10 : e >= -24 ? 1 << (e + 24) : 0));
+}
+// Three bf16 parts of x, packed: x = lo(a) + hi(a) + lo(b), to 24 bits; what is not finite in the first.
+__device__ __forceinline__ uint2 three_parts(float x) {
+    const uint32_t a = bf16x2_of(x, 0.f);
+    if (!(fabsf(x) <= FLT_MAX)) return make_uint2(a, 0u);
+    const float r = x - __uint_as_float(a << 16);
+    const uint32_t b = bf16x2_of(r, 0.f);
+    return make_uint2(a | (b << 16), bf16x2_of(r - __uint_as_float(b << 16), 0.f));
+}
+// Shared-memory descriptors of the K step's operands: rows of 32 bytes, 32-byte swizzle (bit 4 of an address by bit 7).
+__device__ __forceinline__ uint64_t aug_desc(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)6 << 61);
+}
+// Row r of such an operand: three elements, the others 0.
+__device__ __forceinline__ void put_aug(unsigned char *base, int r, uint2 v) {
+    const int flip = (r >> 2) & 1;
+    *reinterpret_cast<uint4 *>(base + r * 32 + flip * 16) = make_uint4(v.x, v.y, 0u, 0u);
+    *reinterpret_cast<uint4 *>(base + r * 32 + (flip ^ 1) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 template <int D, bool QUANT>
@@ -110,10 +156,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     shared_tc_kernel(const SharedArgs a, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                      const __grid_constant__ CUtensorMap mapV) {
     using C = Cfg<D, QUANT>;
-    constexpr int NST = C::NST, NR = C::NR;
+    constexpr int NST = C::NST;
+    // first row tile of queries, ring, K steps, second row tile, codes (where there is no second row tile, from its place on)
     extern __shared__ __align__(1024) unsigned char Qs[];
-    unsigned char *ring = Qs + 2 * C::TILE, *codes = ring + NST * C::TILE;
-    __shared__ Bars<NST, NR> b;
+    unsigned char *ring = Qs + C::TILE, *aug = ring + NST * C::TILE, *qaug = aug + NBIAS * AUG, *Qs1 = qaug + C::NQA * AUG;
+    __shared__ Bars<NST, C::NR, QUANT> b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     next_may_start();
@@ -126,6 +173,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         tc::tma_prefetch_desc(&mapK);
         tc::tma_prefetch_desc(&mapV);
     }
+    if (!QUANT && warp == kWarpBias) {                   // 1 1 1 in every row
+        for (int r = lane; r < 128; r += 32) put_aug(qaug, r, make_uint2(0x3f803f80u, 0x3f80u));
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     after_previous();
     // ---- the piece
     const bool idle = (int)blockIdx.x >= *a.plan.pieces;
@@ -135,32 +186,38 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         w0 = a.plan.piece[2 * blockIdx.x];
         w1 = a.plan.piece[2 * blockIdx.x + 1];
     }
-    const int p = w0.x, b0 = w0.y, nb = w0.z, len = w0.w, g = w1.x, j0 = w1.y, n = w1.z - w1.y;
+    const int b0 = w0.y, nb = w0.z, len = w0.w, g = w1.x, j0 = w1.y, n = w1.z - w1.y;
     const bool two = nb > tpt;                           // two row tiles
     const int step = two ? 1 : 2, L = step;              // key tiles of a warpgroup; keys ahead of their values
-    const int64_t seq = (int64_t)p * a.c.G + g;
+    const int64_t seq = (int64_t)w0.x * a.c.G + g;
     const int box = a.box, per_tile = NK / box;
+    const int nr = C::NR + (two ? 0 : 2);                // slots of codes
+    unsigned char *codes = two ? Qs1 + C::TILE : Qs1;
 
     if (warp == kWarpTma && lane == 0) {                 // the thread that uses them first
         for (int i = 0; i < NST; i++) {
             tc::mbar_init(tc::smem_u32(&b.full[i]), QUANT ? 4 : 1);
             tc::mbar_init(tc::smem_u32(&b.empty[i]), 2);
         }
-        for (int i = 0; i < NR; i++) {
+        for (int i = 0; i < C::NR + 2; i++) {
             tc::mbar_init(tc::smem_u32(&b.rfull[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.rempty[i]), 4);
         }
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(tc::smem_u32(&b.qfull[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.qready[i]), 4);
             tc::mbar_init(tc::smem_u32(&b.sfull[i]), 1);
             for (int k = 0; k < 2; k++) tc::mbar_init(tc::smem_u32(&b.pfull[i][k]), 4);
             tc::mbar_init(tc::smem_u32(&b.odone[i]), 1);
         }
         for (int i = 0; i < NBIAS; i++) {
-            tc::mbar_init(tc::smem_u32(&b.lfull[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.bfull[i]), 1);
+            // read by the products, and of quantised tiles by the conversion and the softmax warps
+            tc::mbar_init(tc::smem_u32(&b.bempty[i]), 2 + (QUANT ? 4 + (two ? 8 : 4) : 0));
+        }
+        for (int i = 0; i < NFIX; i++) {
+            tc::mbar_init(tc::smem_u32(&b.kfix[i]), 1);
             tc::mbar_init(tc::smem_u32(&b.vfix[i]), 1);
-            tc::mbar_init(tc::smem_u32(&b.bempty[i]), two ? 8 : 4);
         }
         tc::mbar_init(tc::smem_u32(&b.fin), 2);
         b.abort = 0;
@@ -183,9 +240,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         const int tk = r / gq, first = two ? i * tpt : 0;
         const bool live = tk < tpt && first + tk < nb;
         const bool work = __any_sync(0xffffffffu, live);
-        const float c = a.scale;
         const uint32_t ts = tb + ((uint32_t)(q * 32) << 16) + i * NK, to = tb + ((uint32_t)(q * 32) << 16) + 2 * NK + i * D;
         const int start = two ? 0 : i;
+        float c = a.scale;
+        int ve = kNoScale;                               // E
         float m = -INFINITY, z = 0.f;                    // the reference and the sum of the weights
         bool ok = true, any = false;
         // A wait that gave up leaves nothing to rely on, but the warp goes on together to the end: every later
@@ -194,8 +252,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         for (int j = start; j < n; j += step, ph ^= 1) {
             const int sl = j % NBIAS;
             ok = wait(&b.sfull[i], ph, b, a.status) && ok;
-            ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
+            float cs = c;                                // what a score is to be scaled by
+            int ve_new = kNoScale;
+            if (QUANT) {
+                ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
+                if (j == start) c *= b.qscale[two ? i : 0][QUANT ? r : 0];
+                cs = c * __uint_as_float((uint32_t)(127 + b.ktop[sl]) << 23);
+                ve_new = b.vtop[sl];
+            }
             __syncwarp();
+            if (QUANT && lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
             tc::tc_fence_after();
             auto hand = [&](int k) {
                 tc::tmem_wait_st();
@@ -205,48 +271,26 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             };
             if (work) {
                 uint32_t x[4][32];
+                float mx[4];
 #pragma unroll
-                for (int k = 0; k < 4; k++) tc::tmem_ld32_async(ts + 32 * k, x[k]);
+                for (int k = 0; k < 4; k++) tc::tmem_ld32_max_async(ts + 32 * k, x[k], mx[k]);
                 tc::tmem_wait_ld(x[0]);
 #pragma unroll
                 for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
-                const float4 *bias = reinterpret_cast<const float4 *>(b.bias[sl]);
-                float mx = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const float2 c2 = make_float2(c, c);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 u = bias[k * 8 + e / 4];
-                        const float2 y0 = __ffma2_rn(make_float2(__uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1])), c2, make_float2(u.x, u.y));
-                        const float2 y1 = __ffma2_rn(make_float2(__uint_as_float(x[k][e + 2]), __uint_as_float(x[k][e + 3])), c2, make_float2(u.z, u.w));
-                        x[k][e] = __float_as_uint(y0.x);
-                        x[k][e + 1] = __float_as_uint(y0.y);
-                        x[k][e + 2] = __float_as_uint(y1.x);
-                        x[k][e + 3] = __float_as_uint(y1.y);
-                        if (e & 8) asm volatile("" ::: "memory");        // no more of log m in registers at once
-                    }
-                }
-                if (b.special[sl]) {                     // keys that are not there: whatever their scores
-#pragma unroll
-                    for (int k = 0; k < 4; k++)
-#pragma unroll
-                        for (int e = 0; e < 32; e++) {
-                            if (b.bias[sl][k * 32 + e] == -INFINITY) x[k][e] = 0xff800000u;
-                            if ((e & 7) == 7) asm volatile("" ::: "memory");
-                        }
-                }
-#pragma unroll
-                for (int k = 0; k < 4; k++)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
-                const bool grow = m != -INFINITY && mx > m + kLazy;
-                if (m == -INFINITY) m = mx;              // no weight so far
-                if (__any_sync(0xffffffffu, grow)) {
+                for (int k = 0; k < 4; k++) tc::tmem_loaded(mx[k]);
+                const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * cs - (QUANT ? kHead : 0.f);
+                const bool grow = m != -INFINITY && top > m + kLazy, far = fabsf(top) > kFar && top != -INFINITY;
+                if (m == -INFINITY) m = top;             // no weight so far
+                if (__any_sync(0xffffffffu, grow || far) || (QUANT && ve_new != ve)) {
                     // S(j) was issued after the last product into O, so that one is done
-                    const float w = grow ? tc::ex2(m - mx) : 1.f;
+                    float w = grow ? tc::ex2(m - top) : 1.f;
                     z *= w;
-                    if (grow) m = mx;
+                    if (grow) m = top;
+                    if (QUANT) {
+                        w *= __uint_as_float((uint32_t)max(0, 127 + ve - ve_new) << 23);
+                        ve = ve_new;
+                    }
                     if (any) {
 #pragma unroll
                         for (int k = 0; k < D / 32; k++) {
@@ -258,9 +302,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                             tc::tmem_st(to + 32 * k, o);
                         }
                     }
+                    if (__any_sync(0xffffffffu, far)) {  // the scaling rounded on its own
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+#pragma unroll
+                            for (int e = 0; e < 32; e++) x[k][e] = __float_as_uint(__uint_as_float(x[k][e]) * cs);
+                        cs = 1.f;
+                    }
                 }
                 const float sh = m == -INFINITY ? 0.f : -m;
-                const float2 s2 = make_float2(sh, sh);
+                const float2 s2 = make_float2(sh, sh), cs2 = make_float2(cs, cs);
                 float2 acc = make_float2(0.f, 0.f);
                 uint32_t pk[32];
 #pragma unroll
@@ -268,10 +319,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
 #pragma unroll
                     for (int e = 0; e < 32; e++) {
                         const int at = h * 64 + 2 * e;
-                        const float2 y = __fadd2_rn(make_float2(__uint_as_float(x[at / 32][at & 31]), __uint_as_float(x[at / 32][(at & 31) + 1])), s2);
+                        const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[at / 32][at & 31]), __uint_as_float(x[at / 32][(at & 31) + 1])),
+                                                    cs2, s2);
                         const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
                         acc = __fadd2_rn(acc, w);
-                        pk[e] = bf16x2_of(w.x, w.y);
+                        pk[e] = QUANT ? f16x2_of(w.x, w.y) : bf16x2_of(w.x, w.y);
                     }
                     tc::tmem_st(ts + 32 * h, pk);
                     hand(h);
@@ -281,7 +333,6 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 hand(0);
                 hand(1);
             }
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
             any = true;
         }
         if (any) ok = wait(&b.odone[i], 0, b, a.status) && ok;
@@ -296,6 +347,12 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     uint32_t u[32];
                     tc::tmem_ld32_async(to + 32 * k, u);
                     tc::tmem_wait_ld(u);
+                    if constexpr (QUANT) {               // O 2^E, in two steps that stay in range
+                        const int h = ve >> 1;
+                        const float f0 = __uint_as_float((uint32_t)(127 + h) << 23), f1 = __uint_as_float((uint32_t)(127 + ve - h) << 23);
+#pragma unroll
+                        for (int e = 0; e < 32; e++) u[e] = __float_as_uint(__uint_as_float(u[e]) * f0 * f1);
+                    }
                     if (live) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
@@ -319,87 +376,60 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     tc::mbar_expect_tx(qb, (uint32_t)(C::NB * tpt * gq * 128));
 #pragma unroll
                     for (int cb = 0; cb < C::NB; cb++)
-                        tc::tma_load_3d(tc::smem_u32(Qs + i * C::TILE + cb * 128 * 128), &mapQ, cb * 64, g * gq, b0 + i * tpt, qb);
+                        tc::tma_load_3d(tc::smem_u32((i ? Qs1 : Qs) + cb * 128 * 128), &mapQ, cb * 64, g * gq, b0 + i * tpt, qb);
                 }
             }
-            struct Window { int held0 = 0, held = 0, row = -1; } win[2];          // boxes looked up, one a lane: of keys, of values
+            // boxes of a tile and their pool rows: a window of 32 boxes, one a lane, the next one on its way
+            const bool one = tc::elect_one();
             const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
-            // pool rows of tile j's boxes, in lanes 0 .. per_tile - 1
-            auto rows_of = [&](Window &w, int j) {
-                const int u0 = (j0 + j) * per_tile;
-                if (u0 < w.held0 || u0 + per_tile > w.held0 + w.held) {
-                    w.held0 = u0;
-                    w.held = 32;
-                    const int64_t e = (int64_t)(u0 + lane) * box;
-                    w.row = e < len && u0 + lane < (j0 + n) * per_tile ? (int)entry_row(look, seq, (int)e, a.status) : -1;
-                }
-                return __shfl_sync(0xffffffffu, w.row, (u0 - w.held0 + lane) & 31);
+            const int tiles_w = 32 / per_tile;                                     // tiles of a window
+            auto rows_of = [&](int w) {                                            // window w's rows
+                const int u = w * 32 + lane;
+                const int64_t e = (int64_t)j0 * NK + (int64_t)u * box;
+                return u < n * per_tile && e < len ? (int)entry_row(look, seq, (int)e, a.status) : -1;
             };
-            int issued = 0;
+            int before = -1, now = rows_of(0), after = rows_of(1), w_now = 0;
+            const int N = QUANT ? nr : NST;
+            int st = 0, issued = 0;
+            uint32_t ph = 1;
             bool ok = true;
-            auto next = [&](const CUtensorMap &map, Window &w, int j, const uint8_t *scales) {
-                const int row = rows_of(w, j);
-                const bool have = lane < per_tile && row >= 0;
-                const unsigned units = __ballot_sync(0xffffffffu, have);
-                const int st = issued % (QUANT ? NR : NST);
-                const uint32_t par = ((issued / (QUANT ? NR : NST)) & 1) ^ 1;
-                ok = __all_sync(0xffffffffu, !*(volatile int *)&b.abort && wait(QUANT ? &b.rempty[st] : &b.empty[st], par, b, a.status));
-                if (!ok) return;
-                const uint32_t fb = tc::smem_u32(QUANT ? &b.rfull[st] : &b.full[st]);
-                const uint32_t bytes = QUANT ? (uint32_t)(box * (D + 1)) : (uint32_t)(C::NB * box * 128);
-                if (lane == 0) {
-                    if (QUANT) {
-                        b.runits[st] = units;
-                        b.rcount[st] = min(NK, len - (j0 + j) * NK);
-                    }
-                    if (units) tc::mbar_expect_tx(fb, bytes * __popc(units));
-                    else tc::mbar_arrive(fb);
+            // tile j into the next slot; rows of entries that are not there become 0 once the tile has landed (which this
+            // warp, having waited for the slot's last use, is the one to see without mistaking the phase)
+            auto next = [&](const CUtensorMap &map, int j, uint64_t *fix) {
+                const int w = j / tiles_w, u0 = (j - w * tiles_w) * per_tile;
+                if (w > w_now) {                                                   // a key tile, the first of its window
+                    before = now;
+                    now = after;
+                    after = rows_of(++w_now + 1);
                 }
-                __syncwarp();
-                if (have) {
-                    if (QUANT) {
-                        tc::tma_load_2d(tc::smem_u32(codes + st * C::RAW + lane * box * D), &map, 0, row, fb);
-                        bulk(tc::smem_u32(&b.rscale[st][lane * box]), scales + row, (uint32_t)box, fb);
-                    } else {
+                const int rows = w == w_now ? now : before;
+                const unsigned units = (__ballot_sync(0xffffffffu, rows >= 0) >> u0) & ((1u << per_tile) - 1);
+                ok = __all_sync(0xffffffffu, wait(QUANT ? &b.rempty[st] : &b.empty[st], ph, b, a.status));
+                if (!ok) return;
+                uint64_t *fb = QUANT ? &b.rfull[st] : &b.full[st];
+                if (one) {
+                    if (units) tc::mbar_expect_tx(tc::smem_u32(fb), (uint32_t)(box * D * (QUANT ? 1 : 2) * __popc(units)));
+                    else tc::mbar_arrive(tc::smem_u32(fb));
+                }
+                for (int u = 0; u < per_tile; u++) {
+                    const int row = __shfl_sync(0xffffffffu, rows, u0 + u);
+                    if (row < 0) continue;
+                    if (one) {
+                        if (QUANT) {
+                            tc::tma_load_2d(tc::smem_u32(codes + st * C::RAW + u * box * D), &map, 0, row, tc::smem_u32(fb));
+                        } else {
 #pragma unroll
-                        for (int cb = 0; cb < C::NB; cb++)
-                            tc::tma_load_2d(tc::smem_u32(ring + st * C::TILE + cb * 128 * 128 + lane * box * 128), &map, cb * 64, row, fb);
+                            for (int cb = 0; cb < C::NB; cb++)
+                                tc::tma_load_2d(tc::smem_u32(ring + st * C::TILE + cb * 128 * 128 + u * box * 128), &map, cb * 64, row,
+                                                tc::smem_u32(fb));
+                        }
                     }
                 }
-                issued++;
-            };
-            int biased = 0;
-            auto key = [&](int j) {
-                next(mapK, win[0], j, a.scales.k);
-                if (!ok) return;
-                // the tile's log m, and which of its keys are there
-                const int row = rows_of(win[0], j), sl = j % NBIAS;
-                const bool have = lane < per_tile && row >= 0;
-                const unsigned units = __ballot_sync(0xffffffffu, have);
-                ok = __all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status));
-                if (!ok) return;
-                const uint32_t lb = tc::smem_u32(&b.lfull[sl]);
-                if (lane == 0) {
-                    b.units[sl] = units;
-                    if (units && a.c.log_m) tc::mbar_expect_tx(lb, (uint32_t)(box * 4 * __popc(units)));
-                    else tc::mbar_arrive(lb);
-                }
-                __syncwarp();
-                if (have && a.c.log_m) bulk(tc::smem_u32(&b.bias[sl][lane * box]), a.c.log_m + row, (uint32_t)(box * 4), lb);
-                biased++;
-            };
-            for (int j = 0; ok && j < min(L, n); j++) key(j);
-            for (int j = 0; ok && j < n; j++) {
-                next(mapV, win[1], j, a.scales.v);
-                if (ok && !QUANT) {
-                    // V rows of entries that are not there: 0, once the tile has landed (which this warp, having waited
-                    // for the slot's last use, is the one to see without mistaking the phase)
-                    const int count = min(NK, len - (j0 + j) * NK), row = rows_of(win[1], j), st = (issued - 1) % NST;
-                    const unsigned units = __ballot_sync(0xffffffffu, lane < per_tile && row >= 0);
+                if (!QUANT) {
+                    const int count = min(NK, len - (j0 + j) * NK);
                     if (count < NK || units != (1u << per_tile) - 1) {
-                        ok = __all_sync(0xffffffffu, wait(&b.full[st], ((issued - 1) / NST) & 1, b, a.status));
-                        if (!ok) break;
-                        for (int i = lane; i < NK * C::NB * 8; i += 32) {
+                        ok = __all_sync(0xffffffffu, wait(fb, ph ^ 1, b, a.status));
+                        for (int i = lane; ok && i < NK * C::NB * 8; i += 32) {
                             const int r = i / (C::NB * 8), cb = i % (C::NB * 8);
                             if (r < count && ((units >> (r / box)) & 1u)) continue;
                             *reinterpret_cast<uint4 *>(ring + st * C::TILE + (cb >> 3) * (NK * 128) + r * 128 + (cb & 7) * 16) =
@@ -408,58 +438,118 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.vfix[j % NBIAS]));
+                    if (one) tc::mbar_arrive(tc::smem_u32(fix + j % NFIX));
                 }
-                if (ok && j + L < n) key(j + L);
+                issued++;
+                if (++st == N) { st = 0; ph ^= 1; }
+            };
+            for (int j = 0; ok && j < min(L, n); j++) next(mapK, j, b.kfix);
+            for (int j = 0; ok && j < n; j++) {
+                next(mapV, j, b.vfix);
+                if (ok && j + L < n) next(mapK, j + L, b.kfix);
             }
             // the copies still in flight land before the block exits
             if (lane == 0) {
-                constexpr int N = QUANT ? NR : NST;
                 for (int i = max(0, issued - N); i < issued; i++)
                     tc::mbar_wait(tc::smem_u32(QUANT ? &b.rfull[i % N] : &b.full[i % N]), (i / N) & 1, kWaitNs);
-                for (int i = max(0, biased - NBIAS); i < biased; i++)
-                    tc::mbar_wait(tc::smem_u32(&b.lfull[i % NBIAS]), (i / NBIAS) & 1, kWaitNs);
                 for (int i = 0; i < (two ? 2 : 1); i++) tc::mbar_wait(tc::smem_u32(&b.qfull[i]), 0, kWaitNs);
             }
         } else if (warp == kWarpBias) {
-            // ---------------- log m, masks, stale values ----------------
+            // ---------------- log m, masks, scales: four keys a lane ----------------
+            const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
+            struct Four { int row; float4 lm; uint32_t ks, vs; };
+            auto row_of = [&](int j) {                   // of the first of the lane's keys; the four share a page
+                const int64_t e = (int64_t)(j0 + j) * NK + lane * 4;
+                return j < n && e < len ? (int)entry_row(look, seq, (int)e, a.status) : -1;
+            };
+            auto load = [&](int row) {
+                Four f{row, make_float4(0.f, 0.f, 0.f, 0.f), 0x7f7f7f7fu, 0x7f7f7f7fu};
+                if (row >= 0) {
+                    if (a.c.log_m) f.lm = *reinterpret_cast<const float4 *>(a.c.log_m + row);
+                    if (QUANT) {
+                        f.ks = *reinterpret_cast<const uint32_t *>(a.scales.k + row);
+                        f.vs = *reinterpret_cast<const uint32_t *>(a.scales.v + row);
+                    }
+                }
+                return f;
+            };
+            const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
+            int top_ve = kNoScale;
+            Four cur = load(row_of(0));
+            int row1 = row_of(1);
             for (int j = 0; j < n; j++) {
                 const int sl = j % NBIAS;
-                if (!__all_sync(0xffffffffu, wait(&b.lfull[sl], (j / NBIAS) & 1, b, a.status))) break;
-                const unsigned units = b.units[sl];
-                const int count = min(NK, len - (j0 + j) * NK), k0 = lane * 4;
-                const bool there = (units >> (k0 / box)) & 1u;                     // a box holds whole fours
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (a.c.log_m && there) {
-                    v = *reinterpret_cast<const float4 *>(&b.bias[sl][k0]);
-                    v = make_float4(log2_m(v.x), log2_m(v.y), log2_m(v.z), log2_m(v.w));
+                const Four f = cur;
+                cur = load(row1);                        // on their way: the next tile's words, the one after's pages
+                row1 = row_of(j + 2);
+                if (!__all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status))) break;
+                const int count = f.row < 0 ? 0 : min(4, len - ((j0 + j) * NK + lane * 4));       // keys that are there
+                const float lm[4] = {f.lm.x, f.lm.y, f.lm.z, f.lm.w};
+                float v[4];
+                float down = 1.f;                        // 2^-k
+                bool in[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    in[i] = i < count && lm[i] != -INFINITY;
+                    v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
                 }
-                if (!there || k0 >= count) v.x = -INFINITY;
-                if (!there || k0 + 1 >= count) v.y = -INFINITY;
-                if (!there || k0 + 2 >= count) v.z = -INFINITY;
-                if (!there || k0 + 3 >= count) v.w = -INFINITY;
-                *reinterpret_cast<float4 *>(&b.bias[sl][k0]) = v;
-                const bool special = __any_sync(0xffffffffu, !there || k0 + 3 >= count);
-                if (lane == 0) b.special[sl] = special;
-                // before the weights, and so before the product that they enter
-                if (special && !QUANT && !__all_sync(0xffffffffu, wait(&b.vfix[sl], (j / NBIAS) & 1, b, a.status))) break;
+                if constexpr (QUANT) {
+                    int ke[4], we[4], kt = kLeastK, vt = kNoScale;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        ke[i] = min((int)((f.ks >> (8 * i)) & 255) - 127, 119);
+                        we[i] = min((int)((f.vs >> (8 * i)) & 255) - 127, 119);
+                        if (in[i]) { kt = max(kt, ke[i]); vt = max(vt, we[i]); }
+                    }
+                    kt = __reduce_max_sync(0xffffffffu, kt);
+                    top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
+                    down = __uint_as_float((uint32_t)(127 - kt) << 23);
+                    __half km[4], vm[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        km[i] = in[i] ? half_pow2(ke[i] - kt) : __ushort_as_half(0);
+                        vm[i] = in[i] ? half_pow2(we[i] - top_ve) : __ushort_as_half(0);
+                    }
+                    *reinterpret_cast<uint2 *>(&b.kmul[sl][lane * 4]) = *reinterpret_cast<const uint2 *>(km);
+                    *reinterpret_cast<uint2 *>(&b.vmul[sl][lane * 4]) = *reinterpret_cast<const uint2 *>(vm);
+                    if (lane == 0) {
+                        b.ktop[sl] = kt;
+                        b.vtop[sl] = top_ve;
+                    }
+                }
+                const bool special = __any_sync(0xffffffffu, count < 4);
+                if (a.c.log_m || special) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        put_aug(aug + sl * AUG, lane * 4 + i, three_parts(QUANT ? v[i] * down : v[i]));
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                if (lane == 0) b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
+                // the key rows that are not there are 0 before the product
+                if (special && !QUANT && !__all_sync(0xffffffffu, wait(&b.kfix[j % NFIX], (j / NFIX) & 1, b, a.status))) break;
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bfull[sl]));
             }
         } else {
             // ---------------- MMA issue: one warp a row tile, one lane issues ----------------
-            constexpr uint32_t idS = tc::idesc_bf16_f32(128, NK), idO = tc::idesc_bf16_f32(128, D) | tc::kIdescBmn;
+            // f16 operands where bf16's have a one: their type's field is 0
+            constexpr uint32_t kTypes = tc::idesc_bf16_f32(0, 0) & ~(1u << 4), idA = tc::idesc_bf16_f32(128, NK);
+            constexpr uint32_t idS = idA & (QUANT ? ~kTypes : ~0u);
+            constexpr uint32_t idO = (tc::idesc_bf16_f32(128, D) & (QUANT ? ~kTypes : ~0u)) | tc::kIdescBmn;
             const int i = warp - kWarpMma, start = two ? 0 : i, qi = two ? i : 0;
-            const uint32_t qd = ((tc::smem_u32(Qs) >> 4) | (1u << 16)) + qi * (C::TILE >> 4);
+            const uint32_t qd = (tc::smem_u32(qi ? Qs1 : Qs) >> 4) | (1u << 16);
             const uint32_t kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
             const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((NK * 128 >> 4) << 16);
+            const uint64_t ad = aug_desc(tc::smem_u32(aug)), qad = aug_desc(tc::smem_u32(qaug + (QUANT ? qi : 0) * AUG));
             const uint32_t ts = tb + i * NK, to = tb + 2 * NK + i * D;
             const bool one = tc::elect_one();
-            bool ok = start >= n || wait(&b.qfull[qi], 0, b, a.status);
+            bool ok = start >= n || wait(QUANT ? &b.qready[qi] : &b.qfull[qi], 0, b, a.status);
             // Both warps walk the ring in its order and release every slot, whoever uses it: a warp that passed over a
             // slot's phase could take the one after it for landed.
             int st = 0;
             uint32_t ph = 0, pp = 0;                     // of the slot that comes next; of the weights
+            unsigned fixed = 0;                          // bit j % 32: tile j has rows that are not there
             auto arrived = [&] {
                 ok = wait(&b.full[st], ph, b, a.status) && ok;
                 tc::tc_fence_after();
@@ -469,7 +559,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             };
             auto mine = [&](int j) { return two || (j & 1) == i; };
             auto key = [&](int j) {
-                const int at = arrived();
+                const int at = arrived(), sl = j % NBIAS;
+                ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
+                tc::tc_fence_after();
+                const int kind = b.kind[sl];
+                fixed = (fixed & ~(1u << (j & 31))) | (kind & kSpecial ? 1u << (j & 31) : 0u);
                 if (!ok || !one) return;
                 if (mine(j)) {
                     const uint32_t ka = kd + at * (C::TILE >> 4);
@@ -478,10 +572,13 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
 #pragma unroll
                         for (int x = 0; x < 4; x++)
                             tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
+                    if (kind) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
                     tc::mma_commit(tc::smem_u32(&b.sfull[i]));
                     tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                    tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
                 } else {
                     tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
+                    tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
                 }
             };
             for (int j = 0; j < min(L, n); j++) key(j);
@@ -489,6 +586,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 const int at = arrived();
                 if (mine(j)) {
                     const uint32_t va = vd + at * (C::TILE >> 4);
+                    if (!QUANT && (fixed >> (j & 31)) & 1u) ok = wait(&b.vfix[j % NFIX], (j / NFIX) & 1, b, a.status) && ok;
 #pragma unroll
                     for (int k = 0; k < 2; k++) {        // the weights come in halves
                         ok = wait(&b.pfull[i][k], pp, b, a.status) && ok;
@@ -521,15 +619,47 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         }
     } else if constexpr (QUANT) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::RCONV));
-        // ---------------- codes to bf16: one thread a row ----------------
+        // ---------------- queries and codes to f16: one thread a row ----------------
         const int r = (warp - kWarpConv) * 32 + lane;
-        for (int s = 0; s < 2 * n; s++) {
-            const int rs = s % NR, st = s % NST;
-            bool ok = wait(&b.rfull[rs], (s / NR) & 1, b, a.status);
-            ok = wait(&b.empty[st], ((s / NST) & 1) ^ 1, b, a.status) && ok;
-            if (!__all_sync(0xffffffffu, ok)) break;
-            const bool there = r < b.rcount[rs] && ((b.runits[rs] >> (r / box)) & 1u);
-            const float sc = there ? scale_of(b.rscale[rs][r]) : 0.f;
+        for (int i = 0; i < (two ? 2 : 1); i++) {
+            if (!__all_sync(0xffffffffu, wait(&b.qfull[i], 0, b, a.status))) break;
+            unsigned char *row = (i ? Qs1 : Qs) + r * 128;
+            auto chunk = [&](int ch) { return reinterpret_cast<uint4 *>(row + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (r & 7)) << 4)); };
+            float top = 0.f;
+#pragma unroll
+            for (int ch = 0; ch < D / 8; ch++) {
+                float x[8];
+                unpack16(*chunk(ch), x);
+                top = fmaxf(top, top_of(x));
+            }
+            const int qe = max((int)(__float_as_uint(top) >> 23) - 127 - 14, kLeastQ);
+            const float f = __uint_as_float((uint32_t)(127 - qe) << 23);
+#pragma unroll
+            for (int ch = 0; ch < D / 8; ch++) {
+                float x[8];
+                unpack16(*chunk(ch), x);
+                *chunk(ch) = make_uint4(f16x2_of(x[0] * f, x[1] * f), f16x2_of(x[2] * f, x[3] * f), f16x2_of(x[4] * f, x[5] * f),
+                                        f16x2_of(x[6] * f, x[7] * f));
+            }
+            b.qscale[i][r] = __uint_as_float((uint32_t)(127 + qe) << 23);
+            const uint32_t ff = bf16x2_of(f, f);         // log m is scaled up with the row's scores
+            put_aug(qaug + i * AUG, r, make_uint2(ff, ff & 0xffffu));
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.qready[i]));
+        }
+        int rs = 0, st = 0;
+        uint32_t rph = 0, ph = 1;
+        bool ok = true;
+        auto convert = [&](int j, const __half *mul, bool last) {
+            const int sl = j % NBIAS;
+            ok = wait(&b.rfull[rs], rph, b, a.status) && ok;
+            ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
+            ok = __all_sync(0xffffffffu, wait(&b.empty[st], ph, b, a.status) && ok);
+            if (!ok) return;
+            const __half2 s = __half2half2(mul[(QUANT ? sl * NK : 0) + r]);
+            // entries that are not there have a scale of 0 and, as their codes may be NaN, none of those
+            const bool there = (j0 + j) * NK + r < len && (!(b.kind[sl] & kSpecial) || __half_as_ushort(__low2half(s)) != 0);
             const unsigned char *src = codes + rs * C::RAW + r * D;
             unsigned char *dst = ring + st * C::TILE + r * 128;
 #pragma unroll
@@ -537,23 +667,27 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 const int from = D == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3);
                 uint4 u = *reinterpret_cast<const uint4 *>(src + from * 16);
                 if (!there) u = make_uint4(0, 0, 0, 0);
-                auto two_of = [&](uint32_t c) {
-                    const float2 v = values2(c);
-                    return bf16x2_of(v.x * sc, v.y * sc);
-                };
-                const uint4 lo = make_uint4(two_of(u.x & 0xffffu), two_of(u.x >> 16), two_of(u.y & 0xffffu), two_of(u.y >> 16));
-                const uint4 hi = make_uint4(two_of(u.z & 0xffffu), two_of(u.z >> 16), two_of(u.w & 0xffffu), two_of(u.w >> 16));
                 unsigned char *d = dst + (ch >> 2) * (128 * 128);
                 const int at = (ch & 3) * 2;
-                *reinterpret_cast<uint4 *>(d + ((at ^ (r & 7)) << 4)) = lo;
-                *reinterpret_cast<uint4 *>(d + (((at + 1) ^ (r & 7)) << 4)) = hi;
+                *reinterpret_cast<uint4 *>(d + ((at ^ (r & 7)) << 4)) =
+                    make_uint4(half2_of(u.x & 0xffffu, s), half2_of(u.x >> 16, s), half2_of(u.y & 0xffffu, s), half2_of(u.y >> 16, s));
+                *reinterpret_cast<uint4 *>(d + (((at + 1) ^ (r & 7)) << 4)) =
+                    make_uint4(half2_of(u.z & 0xffffu, s), half2_of(u.z >> 16, s), half2_of(u.w & 0xffffu, s), half2_of(u.w >> 16, s));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 tc::mbar_arrive(tc::smem_u32(&b.full[st]));
                 tc::mbar_arrive(tc::smem_u32(&b.rempty[rs]));
+                if (last) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
             }
+            if (++rs == nr) { rs = 0; rph ^= 1; }
+            if (++st == NST) { st = 0; ph ^= 1; }
+        };
+        for (int j = 0; ok && j < min(L, n); j++) convert(j, b.kmul[0], false);
+        for (int j = 0; ok && j < n; j++) {
+            convert(j, b.vmul[0], true);
+            if (ok && j + L < n) convert(j + L, b.kmul[0], false);
         }
     }
     tc::tc_fence_before();
