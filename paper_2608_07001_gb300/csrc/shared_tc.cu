@@ -76,8 +76,10 @@ struct Cfg {
     static constexpr int NQA = QUANT ? 2 : 1;              // left sides of the K step: by row, or the same for all
     static constexpr size_t SMEM = 2 * (size_t)TILE + NST * (size_t)TILE + (NBIAS + NQA) * (size_t)AUG + NR * (size_t)RAW;
     static constexpr int THREADS = QUANT ? 512 : 384;
-    // Registers a thread at launch, then of the softmax, issue and conversion warps; the sums agree.
-    static constexpr int REGS = QUANT ? 128 : 168, RSOFT = QUANT ? 184 : 208, RISSUE = QUANT ? 64 : 88, RCONV = 80;
+    // Registers a thread at launch, then of the softmax, issue and conversion warps; the sums agree.  With 208 a thread
+    // keeps a row's 128 scores; beside a fourth warpgroup it reads them from TMEM twice, for their maximum and, in
+    // halves, for the weights (184 for all at once: 95 in local memory, 3000 clocks a tile instead of 1200).
+    static constexpr int REGS = QUANT ? 128 : 168, RSOFT = QUANT ? 160 : 208, RISSUE = QUANT ? 96 : 88, RCONV = 96;
     static_assert(256 * RSOFT + 128 * RISSUE + (QUANT ? 128 * RCONV : 0) <= THREADS * REGS, "register split");
     static_assert(NST <= 2 * NFIX - 2, "fixed tiles");
 };
@@ -140,6 +142,8 @@ __device__ __forceinline__ uint2 three_parts(float x) {
     const uint32_t b = bf16x2_of(r, 0.f);
     return make_uint2(a | (b << 16), bf16x2_of(r - __uint_as_float(b << 16), 0.f));
 }
+// The order of a piece's tiles in the ring: L key tiles, then V(j) and K(j + L) in turn; keys and values so far.
+__device__ __forceinline__ bool next_is_key(int keys, int values, int L, int n) { return keys < n && keys < values + L; }
 // Shared-memory descriptors of the K step's operands: rows of 32 bytes, 32-byte swizzle (bit 4 of an address by bit 7).
 __device__ __forceinline__ uint64_t aug_desc(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)6 << 61);
@@ -270,18 +274,26 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][k]));
             };
             if (work) {
-                uint32_t x[4][32];
-                float mx[4];
+                constexpr int XK = QUANT ? 2 : 4;        // groups of 32 scores in registers
+                uint32_t x[XK][32];
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int k0 = 0; k0 < 4; k0 += XK) {
+                    float mx[XK];
 #pragma unroll
-                for (int k = 0; k < 4; k++) tc::tmem_ld32_max_async(ts + 32 * k, x[k], mx[k]);
-                tc::tmem_wait_ld(x[0]);
+                    for (int k = 0; k < XK; k++) tc::tmem_ld32_max_async(ts + 32 * (k0 + k), x[k], mx[k]);
+                    tc::tmem_wait_ld(x[0]);
 #pragma unroll
-                for (int k = 1; k < 4; k++) tc::tmem_loaded(x[k]);
+                    for (int k = 1; k < XK; k++) tc::tmem_loaded(x[k]);
 #pragma unroll
-                for (int k = 0; k < 4; k++) tc::tmem_loaded(mx[k]);
-                const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * cs - (QUANT ? kHead : 0.f);
+                    for (int k = 0; k < XK; k++) tc::tmem_loaded(mx[k]);
+#pragma unroll
+                    for (int k = 0; k < XK; k += 2) top = max3(top, mx[k], mx[k + 1]);
+                }
+                top = top * cs - (QUANT ? kHead : 0.f);
                 const bool grow = m != -INFINITY && top > m + kLazy, far = fabsf(top) > kFar && top != -INFINITY;
                 if (m == -INFINITY) m = top;             // no weight so far
+                bool apart = false;                      // the scaling rounded on its own
                 if (__any_sync(0xffffffffu, grow || far) || (QUANT && ve_new != ve)) {
                     // S(j) was issued after the last product into O, so that one is done
                     float w = grow ? tc::ex2(m - top) : 1.f;
@@ -292,7 +304,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         ve = ve_new;
                     }
                     if (any) {
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < D / 32; k++) {
                             uint32_t o[32];
                             tc::tmem_ld32_async(to + 32 * k, o);
@@ -302,23 +314,31 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                             tc::tmem_st(to + 32 * k, o);
                         }
                     }
-                    if (__any_sync(0xffffffffu, far)) {  // the scaling rounded on its own
-#pragma unroll
-                        for (int k = 0; k < 4; k++)
-#pragma unroll
-                            for (int e = 0; e < 32; e++) x[k][e] = __float_as_uint(__uint_as_float(x[k][e]) * cs);
-                        cs = 1.f;
-                    }
+                    apart = __any_sync(0xffffffffu, far);
                 }
                 const float sh = m == -INFINITY ? 0.f : -m;
-                const float2 s2 = make_float2(sh, sh), cs2 = make_float2(cs, cs);
+                const float2 s2 = make_float2(sh, sh), cs2 = apart ? make_float2(1.f, 1.f) : make_float2(cs, cs);
                 float2 acc = make_float2(0.f, 0.f);
                 uint32_t pk[32];
-#pragma unroll
+#pragma unroll (QUANT ? 1 : 2)
                 for (int h = 0; h < 2; h++) {
+                    constexpr int K0 = QUANT ? 0 : 1;
+                    if constexpr (QUANT) {
+                        tc::tmem_ld32_async(ts + 64 * h, x[0]);
+                        tc::tmem_ld32_async(ts + 64 * h + 32, x[1]);
+                        tc::tmem_wait_ld(x[0]);
+                        tc::tmem_loaded(x[1]);
+                    }
+                    if (apart) {
+#pragma unroll
+                        for (int e = 0; e < 64; e++) {
+                            uint32_t &v = x[K0 * 2 * h + e / 32][e & 31];
+                            v = __float_as_uint(__uint_as_float(v) * cs);
+                        }
+                    }
 #pragma unroll
                     for (int e = 0; e < 32; e++) {
-                        const int at = h * 64 + 2 * e;
+                        const int at = K0 * h * 64 + 2 * e;
                         const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[at / 32][at & 31]), __uint_as_float(x[at / 32][(at & 31) + 1])),
                                                     cs2, s2);
                         const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
@@ -342,7 +362,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         float *pp = a.plan.part + (2 * (size_t)blockIdx.x + i) * shared_part_floats(true, D);
         if (ok && work) {
             if (any) {
-#pragma unroll
+#pragma unroll 1
                 for (int k = 0; k < D / 32; k++) {
                     uint32_t u[32];
                     tc::tmem_ld32_async(to + 32 * k, u);
@@ -393,9 +413,12 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int st = 0, issued = 0;
             uint32_t ph = 1;
             bool ok = true;
-            // tile j into the next slot; rows of entries that are not there become 0 once the tile has landed (which this
+            // tiles in the ring's order; rows of entries that are not there become 0 once the tile has landed (which this
             // warp, having waited for the slot's last use, is the one to see without mistaking the phase)
-            auto next = [&](const CUtensorMap &map, int j, uint64_t *fix) {
+            for (int jk = 0, jv = 0; jv < n;) {
+                const bool is_key = next_is_key(jk, jv, L, n);
+                const int j = is_key ? jk++ : jv++;
+                const CUtensorMap *map = is_key ? &mapK : &mapV;
                 const int w = j / tiles_w, u0 = (j - w * tiles_w) * per_tile;
                 if (w > w_now) {                                                   // a key tile, the first of its window
                     before = now;
@@ -405,7 +428,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 const int rows = w == w_now ? now : before;
                 const unsigned units = (__ballot_sync(0xffffffffu, rows >= 0) >> u0) & ((1u << per_tile) - 1);
                 ok = __all_sync(0xffffffffu, wait(QUANT ? &b.rempty[st] : &b.empty[st], ph, b, a.status));
-                if (!ok) return;
+                if (!ok) break;
                 uint64_t *fb = QUANT ? &b.rfull[st] : &b.full[st];
                 if (one) {
                     if (units) tc::mbar_expect_tx(tc::smem_u32(fb), (uint32_t)(box * D * (QUANT ? 1 : 2) * __popc(units)));
@@ -416,11 +439,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     if (row < 0) continue;
                     if (one) {
                         if (QUANT) {
-                            tc::tma_load_2d(tc::smem_u32(codes + st * C::RAW + u * box * D), &map, 0, row, tc::smem_u32(fb));
+                            tc::tma_load_2d(tc::smem_u32(codes + st * C::RAW + u * box * D), map, 0, row, tc::smem_u32(fb));
                         } else {
 #pragma unroll
                             for (int cb = 0; cb < C::NB; cb++)
-                                tc::tma_load_2d(tc::smem_u32(ring + st * C::TILE + cb * 128 * 128 + u * box * 128), &map, cb * 64, row,
+                                tc::tma_load_2d(tc::smem_u32(ring + st * C::TILE + cb * 128 * 128 + u * box * 128), map, cb * 64, row,
                                                 tc::smem_u32(fb));
                         }
                     }
@@ -438,15 +461,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    if (one) tc::mbar_arrive(tc::smem_u32(fix + j % NFIX));
+                    if (one) tc::mbar_arrive(tc::smem_u32((is_key ? b.kfix : b.vfix) + j % NFIX));
                 }
                 issued++;
                 if (++st == N) { st = 0; ph ^= 1; }
-            };
-            for (int j = 0; ok && j < min(L, n); j++) next(mapK, j, b.kfix);
-            for (int j = 0; ok && j < n; j++) {
-                next(mapV, j, b.vfix);
-                if (ok && j + L < n) next(mapK, j + L, b.kfix);
             }
             // the copies still in flight land before the block exits
             if (lane == 0) {
@@ -550,41 +568,35 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int st = 0;
             uint32_t ph = 0, pp = 0;                     // of the slot that comes next; of the weights
             unsigned fixed = 0;                          // bit j % 32: tile j has rows that are not there
-            auto arrived = [&] {
-                ok = wait(&b.full[st], ph, b, a.status) && ok;
-                tc::tc_fence_after();
-                const int at = st;
-                if (++st == NST) { st = 0; ph ^= 1; }
-                return at;
-            };
             auto mine = [&](int j) { return two || (j & 1) == i; };
-            auto key = [&](int j) {
-                const int at = arrived(), sl = j % NBIAS;
-                ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
-                tc::tc_fence_after();
-                const int kind = b.kind[sl];
-                fixed = (fixed & ~(1u << (j & 31))) | (kind & kSpecial ? 1u << (j & 31) : 0u);
-                if (!ok || !one) return;
-                if (mine(j)) {
-                    const uint32_t ka = kd + at * (C::TILE >> 4);
+            for (int jk = 0, jv = 0; ok && jv < n;) {
+                const bool is_key = next_is_key(jk, jv, L, n);
+                const int j = is_key ? jk++ : jv++, at = st;
+                ok = wait(&b.full[st], ph, b, a.status) && ok;
+                if (++st == NST) { st = 0; ph ^= 1; }
+                if (is_key) {
+                    const int sl = j % NBIAS;
+                    ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
+                    tc::tc_fence_after();
+                    const int kind = b.kind[sl];
+                    fixed = (fixed & ~(1u << (j & 31))) | (kind & kSpecial ? 1u << (j & 31) : 0u);
+                    if (!ok || !one) continue;
+                    if (mine(j)) {
+                        const uint32_t ka = kd + at * (C::TILE >> 4);
 #pragma unroll
-                    for (int cb = 0; cb < C::NB; cb++)
+                        for (int cb = 0; cb < C::NB; cb++)
 #pragma unroll
-                        for (int x = 0; x < 4; x++)
-                            tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
-                    if (kind) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
-                    tc::mma_commit(tc::smem_u32(&b.sfull[i]));
-                    tc::mma_commit(tc::smem_u32(&b.empty[at]));
-                    tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
-                } else {
-                    tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
-                    tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
-                }
-            };
-            for (int j = 0; j < min(L, n); j++) key(j);
-            for (int j = 0; ok && j < n; j++) {
-                const int at = arrived();
-                if (mine(j)) {
+                            for (int x = 0; x < 4; x++)
+                                tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
+                        if (kind) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
+                        tc::mma_commit(tc::smem_u32(&b.sfull[i]));
+                        tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                        tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
+                    } else {
+                        tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
+                        tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
+                    }
+                } else if (mine(j)) {
                     const uint32_t va = vd + at * (C::TILE >> 4);
                     if (!QUANT && (fixed >> (j & 31)) & 1u) ok = wait(&b.vfix[j % NFIX], (j / NFIX) & 1, b, a.status) && ok;
 #pragma unroll
@@ -605,7 +617,6 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 } else if (ok && one) {
                     tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
                 }
-                if (ok && j + L < n) key(j + L);
             }
             ok = __all_sync(0xffffffffu, ok);
             if (!ok && lane == 0) {
@@ -651,13 +662,14 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         int rs = 0, st = 0;
         uint32_t rph = 0, ph = 1;
         bool ok = true;
-        auto convert = [&](int j, const __half *mul, bool last) {
-            const int sl = j % NBIAS;
+        for (int jk = 0, jv = 0; jv < n;) {
+            const bool is_key = next_is_key(jk, jv, L, n);
+            const int j = is_key ? jk++ : jv++, sl = j % NBIAS;
             ok = wait(&b.rfull[rs], rph, b, a.status) && ok;
             ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
             ok = __all_sync(0xffffffffu, wait(&b.empty[st], ph, b, a.status) && ok);
-            if (!ok) return;
-            const __half2 s = __half2half2(mul[(QUANT ? sl * NK : 0) + r]);
+            if (!ok) break;
+            const __half2 s = __half2half2((is_key ? b.kmul : b.vmul)[QUANT ? sl : 0][QUANT ? r : 0]);
             // entries that are not there have a scale of 0 and, as their codes may be NaN, none of those
             const bool there = (j0 + j) * NK + r < len && (!(b.kind[sl] & kSpecial) || __half_as_ushort(__low2half(s)) != 0);
             const unsigned char *src = codes + rs * C::RAW + r * D;
@@ -679,15 +691,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             if (lane == 0) {
                 tc::mbar_arrive(tc::smem_u32(&b.full[st]));
                 tc::mbar_arrive(tc::smem_u32(&b.rempty[rs]));
-                if (last) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
+                if (!is_key) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
             }
             if (++rs == nr) { rs = 0; rph ^= 1; }
             if (++st == NST) { st = 0; ph ^= 1; }
-        };
-        for (int j = 0; ok && j < min(L, n); j++) convert(j, b.kmul[0], false);
-        for (int j = 0; ok && j < n; j++) {
-            convert(j, b.vmul[0], true);
-            if (ok && j + L < n) convert(j + L, b.kmul[0], false);
         }
     }
     tc::tc_fence_before();
