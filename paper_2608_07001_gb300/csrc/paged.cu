@@ -107,9 +107,10 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
 // chunks: a row's half is one 64- to 256-byte line.
 // Five blocks a SM (48 registers): 128 us at 32768 tokens of 48 rows; four 132 to
 // 146, six 139, eight (spills) 168.
-// QUANT: a row's lanes find its largest size together and store codes.
+// QUANT: a row's lanes find its largest size together and store codes; one row in flight, for the same five blocks (186 us
+// of 4 rows with two in flight and four blocks, 178 this way).
 template <typename T, int D, int R, bool QUANT>
-__global__ void __launch_bounds__(256, QUANT ? 4 : 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
+__global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T), PB = QUANT ? D : RB;      // bytes of a pool row
     next_may_start();
     after_previous();
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(256, QUANT ? 4 : 5) paged_append_kernel(const 
             sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
         }
     }
-    constexpr int U = R < 2 ? R : 2;          // rows in flight
+    constexpr int U = R < 2 || QUANT ? 1 : 2;       // rows in flight
 #pragma unroll 1
     for (int k0 = 0; k0 < R; k0 += U) {
         uint4 x[U], y[U];
@@ -179,20 +180,20 @@ __global__ void __launch_bounds__(256, QUANT ? 4 : 5) paged_append_kernel(const 
             const int r = r0 + (k0 + k) * stride;
             if constexpr (QUANT) {
                 if (r < 2 * a.c.G) {
-                    float u[N], w[N];
-                    unpack16(x[k], u);
-                    unpack16(y[k], w);
+                    float u[2 * N];
+                    unpack16(x[k], reinterpret_cast<float(&)[N]>(u[0]));
+                    unpack16(y[k], reinterpret_cast<float(&)[N]>(u[N]));
                     if (a.rotate && r < a.c.G) {
 #pragma unroll
                         for (int j = 0; j < N; j++) {
-                            const float p = u[j];
-                            u[j] = p * cs[j] - w[j] * sn[j];
-                            w[j] = p * sn[j] + w[j] * cs[j];
+                            const float p = u[j], w = u[N + j];
+                            u[j] = p * cs[j] - w * sn[j];
+                            u[N + j] = p * sn[j] + w * cs[j];
                         }
                     }
-                    const int byte = row_scale_byte(row_max<CH>(fmaxf(top_of(u), top_of(w))));
-                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + ch * N, u, inverse_of(byte));
-                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + D / 2 + ch * N, w, inverse_of(byte));
+                    const int byte = row_scale<CH>(u);
+                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + ch * N, u, inverse_of(byte), std::integral_constant<int, N>());
+                    put_codes(reinterpret_cast<uint8_t *>(dst[k]) + D / 2 + ch * N, u + N, inverse_of(byte), std::integral_constant<int, N>());
                     if (ch == 0) *to_scale[k] = (uint8_t)byte;
                     continue;
                 }
@@ -207,16 +208,18 @@ __global__ void __launch_bounds__(256, QUANT ? 4 : 5) paged_append_kernel(const 
 // R: rows of a thread.  Few tokens want every row on its own thread, the
 // latency of one row; many want a thread's sines to serve several (32768 tokens
 // of 48 rows of 128 bf16, the time with 1 / 2 / 4 / 8 rows a thread and two in
-// flight: 201 / 158 / 137 / 144 us, before five blocks a SM).
+// flight: 201 / 158 / 137 / 144 us, before five blocks a SM; quantised, one in flight, with the rows read back, 2 / 3 / 4
+// / 6 / 8 rows a thread: 204 / 183 / 177 / 170 / 175 us).
 template <typename T, int D, bool QUANT>
 cudaError_t launch_append(const AppendArgs &a, const Turns &turns, cudaStream_t s) {
     constexpr int CH = D * (int)sizeof(T) / 32;
     const int rows = 2 * a.c.G + (a.q ? a.c.Hq : 0);
     const int64_t one = (int64_t)a.n_tokens * rows * CH;
+    constexpr int R = QUANT ? 6 : 4;
     const bool many = one >= kAppendMany;
-    const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + 3) / 4) * CH : one;
+    const int64_t threads = many ? (int64_t)a.n_tokens * ((rows + R - 1) / R) * CH : one;
     const unsigned n = (unsigned)((threads + 255) / 256) + (a.cu_new ? 1 : 0);
-    return launch_overlapped(many ? paged_append_kernel<T, D, 4, QUANT> : paged_append_kernel<T, D, 1, QUANT>, n, 256, 0, s, a, turns);
+    return launch_overlapped(many ? paged_append_kernel<T, D, R, QUANT> : paged_append_kernel<T, D, 1, QUANT>, n, 256, 0, s, a, turns);
 }
 
 __global__ void paged_advance_kernel(int32_t *lens, const int32_t *cu_new, int n, int B, int G) {
@@ -239,25 +242,34 @@ struct LoadArgs {
     gkv_paged_scales scales;
 };
 
-// How 16 bytes of a packed row (chunk ch) become a pool row's: as they are, or as codes.  The row's lanes call it together.
+// How a lane's P pieces of 16 bytes of a packed row (ch, and ch plus the row's lanes) become a pool row's: as they are, or
+// as codes.  The row's lanes call it together.  Codes: two pieces a lane, as what a lane does for an entry bounds it.
 template <int BYTES>
 struct Plain {
-    static constexpr int RB = BYTES;
-    static __device__ __forceinline__ void put(char *pool, uint8_t *, int64_t row, int ch, uint4 x) {
-        st16(pool + row * RB + ch * 16, x);
+    static constexpr int RB = BYTES, P = 1, CH = RB / 16, BLOCKS = 8;
+    static __device__ __forceinline__ void put(char *pool, uint8_t *, int64_t row, int ch, const uint4 (&x)[P]) {
+        st16(pool + row * RB + ch * 16, x[0]);
     }
 };
 template <typename T, int D>
 struct Quantised {
-    static constexpr int RB = D * sizeof(T), N = 16 / sizeof(T);
-    static __device__ __forceinline__ void put(char *pool, uint8_t *scales, int64_t row, int ch, uint4 x) {
-        float u[N];
-        unpack16(x, u);
-        const int byte = row_scale_byte(row_max<RB / 16>(top_of(u)));
-        put_codes(reinterpret_cast<uint8_t *>(pool) + row * D + ch * N, u, inverse_of(byte));
+    static constexpr int RB = D * sizeof(T), N = 16 / sizeof(T), P = 2, CH = RB / 32, BLOCKS = 8;
+    static __device__ __forceinline__ void put(char *pool, uint8_t *scales, int64_t row, int ch, const uint4 (&x)[P]) {
+        float u[2 * N];
+        unpack16(x[0], reinterpret_cast<float(&)[N]>(u[0]));
+        unpack16(x[1], reinterpret_cast<float(&)[N]>(u[N]));
+        const int byte = row_scale<CH>(u);
+        uint8_t *p = reinterpret_cast<uint8_t *>(pool) + row * D + ch * N;
+        put_codes(p, u, inverse_of(byte), std::integral_constant<int, N>());
+        put_codes(p + D / 2, u + N, inverse_of(byte), std::integral_constant<int, N>());
         if (ch == 0) scales[row] = (uint8_t)byte;
     }
 };
+template <class W>
+__device__ __forceinline__ void take(uint4 (&x)[W::P], const char *row, int ch) {
+#pragma unroll
+    for (int p = 0; p < W::P; p++) x[p] = ld16(row + (ch + p * W::CH) * 16);
+}
 
 __device__ __forceinline__ bool head_fits(const LoadArgs &a, int64_t lo, int64_t hi) {
     return lo >= 0 && hi >= lo && hi <= a.n_entries;
@@ -268,7 +280,7 @@ __device__ __forceinline__ bool head_fits(const LoadArgs &a, int64_t lo, int64_t
 // too: the same entries to the same rows.  A call, so that it costs the caller no registers.
 template <class W>
 __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first) {
-    constexpr int RB = W::RB, CH = RB / 16;
+    constexpr int RB = W::RB, CH = W::CH;
     const int heads = a.c.L * a.c.G;
     const int64_t cap = (int64_t)a.c.page_size * a.c.max_pages;
     for (int h = first; h < heads && h < first + 256; h++) {
@@ -279,8 +291,11 @@ __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first)
             const int64_t e = i / CH, row = entry_row(a.c, s, (int)e, a.status);
             const int ch = (int)(i % CH);
             if (row < 0) continue;
-            W::put(a.c.K, a.scales.k, row, ch, ld16(a.K + (lo + e) * RB + ch * 16));
-            W::put(a.c.V, a.scales.v, row, ch, ld16(a.V + (lo + e) * RB + ch * 16));
+            uint4 x[W::P], y[W::P];
+            take<W>(x, a.K + (lo + e) * RB, ch);
+            take<W>(y, a.V + (lo + e) * RB, ch);
+            W::put(a.c.K, a.scales.k, row, ch, x);
+            W::put(a.c.V, a.scales.v, row, ch, y);
             if (ch == 0 && a.c.log_m) a.c.log_m[row] = a.log_m ? a.log_m[lo + e] : 0.f;
         }
     }
@@ -292,8 +307,8 @@ __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first)
 // followed from there.  Eight blocks a SM: the registers that the call would take
 // otherwise leave room for six (1M entries of 2 x 256 bytes 163 us, 182 with 40).
 template <class W, int IT>
-__global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constant__ LoadArgs a) {
-    constexpr int RB = W::RB, CH = RB / 16, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
+__global__ void __launch_bounds__(256, W::BLOCKS) paged_load_kernel(const __grid_constant__ LoadArgs a) {
+    constexpr int RB = W::RB, CH = W::CH, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
     constexpr int U = IT < 4 ? IT : 4;
     next_may_start();
     after_previous();
@@ -322,7 +337,7 @@ __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constan
     const int ch = lane % CH;
 #pragma unroll 1
     for (int k0 = 0; k0 < IT; k0 += U) {
-        uint4 x[U], y[U];
+        uint4 x[U][W::P], y[U][W::P];
         int64_t row[U];
 #pragma unroll
         for (int k = 0; k < U; k++) {
@@ -338,8 +353,8 @@ __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constan
             if (o0 < 0 || e < o0 || e >= o1 || o1 > a.n_entries || e - o0 >= cap) continue;
             const int64_t s = ((int64_t)(h / a.c.G) * a.c.B + a.b) * a.c.G + h % a.c.G;
             row[k] = entry_row(a.c, s, (int)(e - o0), a.status);
-            x[k] = ld16(a.K + e * RB + ch * 16);
-            y[k] = ld16(a.V + e * RB + ch * 16);
+            take<W>(x[k], a.K + e * RB, ch);
+            take<W>(y[k], a.V + e * RB, ch);
         }
 #pragma unroll
         for (int k = 0; k < U; k++) {
@@ -353,10 +368,9 @@ __global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constan
 
 template <class W>
 cudaError_t launch_load(const LoadArgs &a, cudaStream_t s) {
-    constexpr int RB = W::RB;
     // two entries in flight a lane: 167 us for 1M entries of 2 x 256 bytes; one 187, four 200
-    constexpr int IT = 2;
-    constexpr int64_t run = (RB < 512 ? 512 / RB : 1) * IT;         // entries of a warp
+    constexpr int IT = W::P == 1 ? 2 : 1;
+    constexpr int64_t run = (W::CH < 32 ? 32 / W::CH : 1) * IT;     // entries of a warp
     const int64_t threads = std::max<int64_t>((int64_t)a.c.L * a.c.G, (a.n_entries + run - 1) / run * 32);
     return launch_overlapped(paged_load_kernel<W, IT>, (unsigned)((threads + 255) / 256), 256, 0, s, a);
 }

@@ -80,7 +80,8 @@ constexpr uint64_t kPaWaitNs = 2000000000ull;
 template <typename T, typename S, int D>
 struct PaCfg {
     static constexpr bool BF = sizeof(T) == 2, QUANT = sizeof(S) == 1;
-    static constexpr int TE = BF ? 64 : 32;        // entries of a tile
+    static constexpr int TE = BF ? (QUANT ? 128 : 64) : 32;      // entries of a tile
+    static constexpr int SNAP = kPaSnap * 64 / (BF ? TE : 64);   // kPaSnap in them (fp32: as it is)
     static constexpr int RB = D * (int)sizeof(S), BW = RB < 128 ? RB : 128;      // bytes of a row, of a column box's row
     static constexpr int NB = RB / BW;             // column boxes of a row
     static constexpr int TB = TE * RB;             // bytes of a tile's keys
@@ -90,7 +91,7 @@ struct PaCfg {
         return BW == 128 ? (uint32_t)((ch >> 3) * (TE * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4))
                          : (uint32_t)(r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
     }
-    static constexpr int MIN = BF ? 2 : 1;         // tiles of a run at least
+    static constexpr int MIN = BF && !QUANT ? 2 : 1;             // tiles of a run at least
     static_assert(NST >= 3 && NST <= 12 && (BF || NST % kPaF32Warps == 0), "ring");
 };
 
@@ -319,16 +320,20 @@ struct PaBf {
 // that), so the logits' products are those of the codes and both scales' exponents come after.  A
 // thread's 4 bytes of an ldmatrix row are 4 neighbouring channels: they serve as
 // channels 2 t, 2 t + 1 and + 8 of the product's step, which sums over them all, and
-// the queries are laid out to match.  Values become bf16, code and scale, exactly, so
-// that the weights keep the range of bf16; a transposed 16-bit word holds two
-// channels, the even ones and the odd ones of 16 to a product.
+// the queries are laid out to match.  A transposed 16-bit word holds two channels, the
+// even ones and the odd ones of 16 to a product.
+// The values' scales 2^v_e go into the weights, P = p 2^(v_e - E + 14), E the largest
+// v_e so far of entries that have a weight at all (log m above -inf); P as f16 and the
+// remainder's 2^11 as f16, so to 2^-22 of a weight, or 2^-50 of the largest value.
+// (Values as bf16 with their scales took 8 clocks for two codes instead of 2, and the
+// kernel 73 us for 1M entries of d = 128.)
 template <int D>
 struct PaE4 {
     using C = PaCfg<__nv_bfloat16, E4m3, D>;
     uint32_t qa[D / 16][2];     // queries in f16, channels 16 i + 4 t .. + 3
     float acc[D / 8][4];        // as PaBf's, columns: the even, then the odd channels of 16
     float m, z;
-    int qe;                     // the power of two taken from head hq's queries
+    int qe, ve;                 // the power of two taken from head hq's queries; E
 
     __device__ __forceinline__ void begin(const PaArgs &a, int s, int gq) {
         const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
@@ -355,6 +360,7 @@ struct PaE4 {
                 const __half2 h = __floats2half2_rn(__uint_as_float(qa[c][i] << 16) * f, __uint_as_float(qa[c][i] & 0xffff0000u) * f);
                 qa[c][i] = *reinterpret_cast<const uint32_t *>(&h);
             }
+        ve = -120;
 #pragma unroll
         for (int i = 0; i < D / 8; i++)
 #pragma unroll
@@ -369,93 +375,127 @@ struct PaE4 {
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
         return h;
     }
-    static __device__ __forceinline__ void mma_f16(float c[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
+    static __device__ __forceinline__ void mma_f16(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                                   uint32_t b1) {
         asm volatile(
             "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
-            "{%0, %1, %2, %3}, {%4, %4, %5, %5}, {%6, %7}, {%0, %1, %2, %3};"
+            "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-            : "r"(a0), "r"(a2), "r"(b0), "r"(b1));
-    }
-    // Two codes of neighbouring entries times their scales.
-    static __device__ __forceinline__ uint32_t value2(uint32_t c, float s0, float s1) {
-        const float2 v = values2(c);
-        return bf16x2_of(v.x * s0, v.y * s1);
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
 
+    // This warp's NG groups of 16 entries: their chains of products, exponentials and conversions run beside one another.
+    static constexpr int NG = C::TE / 64;
     __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const uint8_t *ks, const uint8_t *vs, const float *lm,
                                          int count, unsigned units, int box, float scale, bool has_lm) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tq = lane & 3;
-        const int r0 = warp * 16;
-        const int nv = min(16, count - r0);
-        if (nv <= 0 || !((units >> (r0 / box)) & 1u)) return;
-        float x[2][4];
-#pragma unroll
-        for (int n = 0; n < 2; n++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) x[n][j] = 0.f;
         const int mi = lane >> 3, ri = lane & 7;
+        int nv[NG], some = 0;            // valid entries of a group
 #pragma unroll
-        for (int c = 0; c < D / 16; c += 2) {
-            uint32_t b[4];      // entries 0-7 of chunks c, c + 1, then entries 8-15
-            pa_ldsm4(kst + C::at(r0 + ri + (mi >> 1) * 8, c + (mi & 1)), b);
+        for (int g = 0; g < NG; g++) {
+            const int r0 = (warp * NG + g) * 16;
+            nv[g] = (units >> (r0 / box)) & 1u ? max(0, min(16, count - r0)) : 0;
+            some |= nv[g];
+        }
+        if (!some) return;
+        float x[NG][2][4];
+#pragma unroll
+        for (int g = 0; g < NG; g++)
 #pragma unroll
             for (int n = 0; n < 2; n++)
 #pragma unroll
-                for (int i = 0; i < 2; i++)
-                    mma_f16(x[n], qa[c + i][0], qa[c + i][1], half2(b[2 * n + i] & 0xffffu), half2(b[2 * n + i] >> 16));
+                for (int j = 0; j < 4; j++) x[g][n][j] = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 16; c += 2) {
+#pragma unroll
+            for (int g = 0; g < NG; g++) {
+                uint32_t b[4];      // entries 0-7 of chunks c, c + 1, then entries 8-15
+                pa_ldsm4(kst + C::at((warp * NG + g) * 16 + ri + (mi >> 1) * 8, c + (mi & 1)), b);
+#pragma unroll
+                for (int n = 0; n < 2; n++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++)
+                        mma_f16(x[g][n], qa[c + i][0], qa[c + i][0], qa[c + i][1], qa[c + i][1], half2(b[2 * n + i] & 0xffffu),
+                                half2(b[2 * n + i] >> 16));
+            }
         }
-        float y[2][2], mx = -INFINITY, vsc[2][2];
+        float y[NG][2][2], mx = -INFINITY;
+        int we[NG][2][2], top = ve;      // the values' scales; kOut: without a weight
+        constexpr int kOut = -1000;
 #pragma unroll
-        for (int n = 0; n < 2; n++)
+        for (int g = 0; g < NG; g++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const int e = n * 8 + 2 * tq + j;
-                // both powers of two in two steps, so that only a logit out of range leaves it
-                const int t = qe + (int)ks[r0 + e] - 127;
-                float v = x[n][j] * scale * __uint_as_float((uint32_t)(127 + (t >> 1)) << 23) *
-                          __uint_as_float((uint32_t)(127 + t - (t >> 1)) << 23);
-                if (has_lm) v += pa_lm2(lm[r0 + e]);
-                y[n][j] = e < nv ? v : -INFINITY;
-                vsc[n][j] = e < nv ? scale_of(vs[r0 + e]) : 0.f;
-                mx = fmaxf(mx, y[n][j]);
+            for (int n = 0; n < 2; n++) {
+                const int e0 = n * 8 + 2 * tq, at = (warp * NG + g) * 16 + e0;
+                const uint32_t k2 = *reinterpret_cast<const uint16_t *>(ks + at), v2 = *reinterpret_cast<const uint16_t *>(vs + at);
+                const float2 l2 = has_lm ? *reinterpret_cast<const float2 *>(lm + at) : make_float2(0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const bool in = e0 + j < nv[g];
+                    // both powers of two in two steps, so that only a logit out of range leaves it
+                    const int t = qe + (int)((k2 >> (8 * j)) & 255) - 127;
+                    float v = x[g][n][j] * scale * __uint_as_float((uint32_t)(127 + (t >> 1)) << 23) *
+                              __uint_as_float((uint32_t)(127 + t - (t >> 1)) << 23);
+                    we[g][n][j] = in ? (int)((v2 >> (8 * j)) & 255) - 127 : kOut;
+                    if (has_lm) {
+                        const float l = j ? l2.y : l2.x;
+                        v += pa_lm2(l);
+                        if (l == -INFINITY) we[g][n][j] = kOut;
+                    }
+                    y[g][n][j] = in ? v : -INFINITY;
+                    top = max(top, we[g][n][j]);
+                    mx = fmaxf(mx, y[g][n][j]);
+                }
             }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        if (__any_sync(0xffffffffu, mx > m)) {
-            const float mn = fmaxf(m, mx), w = tc::ex2(m - pa_shift(mn));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        if (__any_sync(0xffffffffu, mx > m || top != ve)) {
+            const float mn = fmaxf(m, mx);
+            float w = tc::ex2(m - pa_shift(mn));
             m = mn;
             z *= w;
+            w *= __uint_as_float((uint32_t)max(0, 127 + ve - top) << 23);
+            ve = top;
 #pragma unroll
             for (int i = 0; i < D / 8; i++)
 #pragma unroll
                 for (int j = 0; j < 4; j++) acc[i][j] *= w;
         }
         const float sh = pa_shift(m);
-        uint32_t hi[2], lo[2];
+        uint32_t hi[NG][2], lo[NG][2], keep[NG][2];
 #pragma unroll
-        for (int n = 0; n < 2; n++) {
-            const float p0 = tc::ex2(y[n][0] - sh), p1 = tc::ex2(y[n][1] - sh);
-            z += p0 + p1;
-            hi[n] = pa_bf16x2(p0, p1);
-            lo[n] = pa_bf16x2(p0 - __uint_as_float(hi[n] << 16), p1 - __uint_as_float(hi[n] & 0xffff0000u));
-        }
-        uint32_t keep0 = ~0u, keep1 = ~0u;
-        if (nv < 16) {
-            keep0 = (2 * tq < nv ? 0xffffu : 0u) | (2 * tq + 1 < nv ? 0xffff0000u : 0u);
-            keep1 = (2 * tq + 8 < nv ? 0xffffu : 0u) | (2 * tq + 9 < nv ? 0xffff0000u : 0u);
+        for (int g = 0; g < NG; g++) {
+#pragma unroll
+            for (int n = 0; n < 2; n++) {
+                const float p0 = tc::ex2(y[g][n][0] - sh), p1 = tc::ex2(y[g][n][1] - sh);
+                z += p0 + p1;
+                const float v0 = p0 * __uint_as_float((uint32_t)max(0, 127 + 14 + we[g][n][0] - ve) << 23);
+                const float v1 = p1 * __uint_as_float((uint32_t)max(0, 127 + 14 + we[g][n][1] - ve) << 23);
+                const __half2 h = __floats2half2_rn(v0, v1);
+                const float2 f = __half22float2(h);
+                const __half2 r = __floats2half2_rn((v0 - f.x) * 2048.f, (v1 - f.y) * 2048.f);
+                hi[g][n] = *reinterpret_cast<const uint32_t *>(&h);
+                lo[g][n] = *reinterpret_cast<const uint32_t *>(&r);
+                // value rows past the length hold anything: 0
+                const int e0 = n * 8 + 2 * tq;
+                keep[g][n] = (e0 < nv[g] ? 0xffffu : 0u) | (e0 + 1 < nv[g] ? 0xffff0000u : 0u);
+            }
         }
 #pragma unroll
         for (int i = 0; i < D / 16; i += 2) {
-            uint32_t b[4];      // entries 0-7, 8-15 of chunk i, then of i + 1
-            pa_ldsm4t(vst + C::at(r0 + ri + (mi & 1) * 8, i + (mi >> 1)), b);
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                // bytes (entry 0, channels 0 1), (entry 1, channels 0 1) -> channel 0 of both, channel 1 of both
-                const uint32_t c0 = __byte_perm(b[2 * k] & keep0, 0, 0x3120), c1 = __byte_perm(b[2 * k + 1] & keep1, 0, 0x3120);
-                pa_mma(acc[2 * (i + k)], hi[0], lo[0], hi[1], lo[1], value2(c0 & 0xffffu, vsc[0][0], vsc[0][1]),
-                       value2(c1 & 0xffffu, vsc[1][0], vsc[1][1]));
-                pa_mma(acc[2 * (i + k) + 1], hi[0], lo[0], hi[1], lo[1], value2(c0 >> 16, vsc[0][0], vsc[0][1]),
-                       value2(c1 >> 16, vsc[1][0], vsc[1][1]));
+            for (int g = 0; g < NG; g++) {
+                uint32_t b[4];      // entries 0-7, 8-15 of chunk i, then of i + 1
+                pa_ldsm4t(vst + C::at((warp * NG + g) * 16 + ri + (mi & 1) * 8, i + (mi >> 1)), b);
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    // bytes (entry 0, channels 0 1), (entry 1, channels 0 1) -> channel 0 of both, channel 1 of both
+                    const uint32_t c0 = __byte_perm(b[2 * k] & keep[g][0], 0, 0x3120), c1 = __byte_perm(b[2 * k + 1] & keep[g][1], 0, 0x3120);
+                    mma_f16(acc[2 * (i + k)], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 & 0xffffu), half2(c1 & 0xffffu));
+                    mma_f16(acc[2 * (i + k) + 1], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 >> 16), half2(c1 >> 16));
+                }
             }
         }
     }
@@ -469,15 +509,17 @@ struct PaE4 {
     __device__ __forceinline__ void add(float *sum, const float *M, int gq, bool first) {
         const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
         if (hq >= gq) return;
-        const float w = tc::ex2(m - pa_shift(M[hq]));
+        // times 2^(E - 14), in two steps that stay in range
+        const float w = tc::ex2(m - pa_shift(M[hq])) * __uint_as_float((uint32_t)(127 + ((ve - 14) >> 1)) << 23);
+        const float w2 = __uint_as_float((uint32_t)(127 + ve - 14 - ((ve - 14) >> 1)) << 23);
 #pragma unroll
         for (int c = 0; c < D / 16; c++) {
             float4 *p = reinterpret_cast<float4 *>(sum + hq * D + c * 16 + 4 * tq);
             float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *p;
-            v.x += w * (acc[2 * c][0] + acc[2 * c][2]);
-            v.y += w * (acc[2 * c + 1][0] + acc[2 * c + 1][2]);
-            v.z += w * (acc[2 * c][1] + acc[2 * c][3]);
-            v.w += w * (acc[2 * c + 1][1] + acc[2 * c + 1][3]);
+            v.x += w * (acc[2 * c][0] + acc[2 * c][2] * 0x1p-11f) * w2;
+            v.y += w * (acc[2 * c + 1][0] + acc[2 * c + 1][2] * 0x1p-11f) * w2;
+            v.z += w * (acc[2 * c][1] + acc[2 * c][3] * 0x1p-11f) * w2;
+            v.w += w * (acc[2 * c + 1][1] + acc[2 * c + 1][3] * 0x1p-11f) * w2;
             *p = v;
         }
     }
@@ -684,7 +726,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         total += sm.wsum[w];
         most = max(most, sm.wmax[w]);
     }
-    const bool snap = most <= kPaSnap;
+    const bool snap = most <= C::SNAP;
     // A run holds MIN tiles at least, and as many as leave the longest sequence kPaPieces pieces: one CTA
     // joins them, eight or sixteen at a time.  (16000 entries of 2 sequences: 14.9 us with runs of 2 or 4
     // tiles, 16.4 of 8; 60000 entries of one head: 22.4 us in 64 pieces, 24.7 in 128; 2000 entries of 8

@@ -18,32 +18,37 @@ namespace {
 
 using namespace serve;
 
-// 16 bytes of the row in T (chunk ch), from a pool of S.
+// A lane's two pieces of 16 bytes of a row in T (ch, and ch plus the row's lanes), from a pool of S.
 template <typename T, typename S, int D>
 struct Row {
-    static constexpr int N = 16 / sizeof(T), CH = D / N, PB = D * sizeof(S);
-    struct Raw { uint4 u; int byte; };
+    static constexpr int N = 16 / sizeof(T), CH = D / N / 2, PB = D * sizeof(S);
+    struct Raw { uint4 u[2]; int byte; };
     // Plain loads: the launch before may still be writing when this kernel begins.
     static __device__ __forceinline__ Raw load(const char *pool, const uint8_t *scales, int64_t row, int ch) {
         Raw r;
         r.byte = 0;
         const char *p = pool + row * PB;
         if constexpr (sizeof(S) == sizeof(T)) {
-            r.u = *reinterpret_cast<const uint4 *>(p + ch * 16);
+#pragma unroll
+            for (int i = 0; i < 2; i++) r.u[i] = *reinterpret_cast<const uint4 *>(p + (ch + i * CH) * 16);
         } else {
             r.byte = scales[row];
-            if constexpr (N == 8) {
-                const uint2 c = *reinterpret_cast<const uint2 *>(p + ch * 8);
-                r.u = make_uint4(c.x, c.y, 0, 0);
-            } else {
-                r.u = make_uint4(*reinterpret_cast<const uint32_t *>(p + ch * 4), 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                if constexpr (N == 8) {
+                    const uint2 c = *reinterpret_cast<const uint2 *>(p + (ch + i * CH) * 8);
+                    r.u[i] = make_uint4(c.x, c.y, 0, 0);
+                } else {
+                    r.u[i] = make_uint4(*reinterpret_cast<const uint32_t *>(p + (ch + i * CH) * 4), 0, 0, 0);
+                }
             }
         }
         return r;
     }
-    static __device__ __forceinline__ uint4 value(Raw r) {
+    static __device__ __forceinline__ uint4 value(const Raw &r, int i) {
+        const uint4 u = r.u[i];
         if constexpr (sizeof(S) == sizeof(T)) {
-            return r.u;
+            return u;
         } else {
             const float s = scale_of(r.byte);
             if constexpr (N == 8) {
@@ -51,13 +56,19 @@ struct Row {
                     const float2 v = values2(c);
                     return bf16x2_of(v.x * s, v.y * s);
                 };
-                return make_uint4(two(r.u.x & 0xffffu), two(r.u.x >> 16), two(r.u.y & 0xffffu), two(r.u.y >> 16));
+                return make_uint4(two(u.x & 0xffffu), two(u.x >> 16), two(u.y & 0xffffu), two(u.y >> 16));
             } else {
-                const float2 a = values2(r.u.x & 0xffffu), b = values2(r.u.x >> 16);
+                const float2 a = values2(u.x & 0xffffu), b = values2(u.x >> 16);
                 return make_uint4(__float_as_uint(a.x * s), __float_as_uint(a.y * s), __float_as_uint(b.x * s),
                                   __float_as_uint(b.y * s));
             }
         }
+    }
+    // The row at p, or zeros.
+    static __device__ __forceinline__ void put(char *p, int ch, const Raw &r, bool there) {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            *reinterpret_cast<uint4 *>(p + (ch + i * CH) * 16) = there ? value(r, i) : make_uint4(0, 0, 0, 0);
     }
 };
 
@@ -71,7 +82,7 @@ struct ReadArgs {
     int *status;
 };
 
-// A thread: 16 bytes of the key's row and of the value's row of one entry.
+// A thread: two pieces of 16 bytes of the key's row and of the value's row of one entry.
 template <typename T, typename S, int D>
 __global__ void __launch_bounds__(256) paged_read_kernel(const ReadArgs a) {
     using X = Row<T, S, D>;
@@ -97,14 +108,13 @@ __global__ void __launch_bounds__(256) paged_read_kernel(const ReadArgs a) {
     const int64_t s = ((int64_t)a.l * a.c.B + b) * a.c.G + h;
     const int idx = a.c.lens[s] - tail;
     const int64_t row = idx >= 0 ? entry_row(a.c, s, idx, a.status) : -1;
-    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+    typename X::Raw x, y;
     if (row >= 0) {
-        const typename X::Raw p = X::load(a.c.K, a.scales.k, row, ch), q = X::load(a.c.V, a.scales.v, row, ch);
-        x = X::value(p);
-        y = X::value(q);
+        x = X::load(a.c.K, a.scales.k, row, ch);
+        y = X::load(a.c.V, a.scales.v, row, ch);
     }
-    *reinterpret_cast<uint4 *>(a.k + t * a.k_ts + h * a.k_hs + ch * 16) = x;
-    *reinterpret_cast<uint4 *>(a.v + t * a.v_ts + h * a.v_hs + ch * 16) = y;
+    X::put(a.k + t * a.k_ts + h * a.k_hs, ch, x, row >= 0);
+    X::put(a.v + t * a.v_ts + h * a.v_hs, ch, y, row >= 0);
 }
 
 struct UnloadArgs {
@@ -159,7 +169,7 @@ __global__ void __launch_bounds__(1024) paged_offsets_kernel(const UnloadArgs a)
     if (bad) atomicOr(a.status, kStRange);
 }
 
-// A thread: 16 bytes of the key's row and of the value's row of IT entries.
+// A thread: two pieces of 16 bytes of the key's row and of the value's row of IT entries.
 template <typename T, typename S, int D, int IT>
 __global__ void __launch_bounds__(256) paged_unload_kernel(const UnloadArgs a) {
     using X = Row<T, S, D>;
@@ -198,9 +208,8 @@ __global__ void __launch_bounds__(256) paged_unload_kernel(const UnloadArgs a) {
     for (int k = 0; k < IT; k++) {
         if (!in[k]) continue;
         const int64_t e = e0 + (int64_t)k * RW;
-        const uint4 none = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4 *>(a.K + e * RB + ch * 16) = row[k] < 0 ? none : X::value(x[k]);
-        *reinterpret_cast<uint4 *>(a.V + e * RB + ch * 16) = row[k] < 0 ? none : X::value(y[k]);
+        X::put(a.K + e * RB, ch, x[k], row[k] >= 0);
+        X::put(a.V + e * RB, ch, y[k], row[k] >= 0);
         if (ch == 0 && a.log_m) a.log_m[e] = row[k] >= 0 && a.c.log_m ? a.c.log_m[row[k]] : 0.f;
     }
 }
@@ -215,7 +224,7 @@ template <typename T, typename S, int D>
 cudaError_t launch_unload(const UnloadArgs &a, cudaStream_t s) {
     cudaError_t e = launch_overlapped(paged_offsets_kernel, 1, 1024, 0, s, a);
     if (e != cudaSuccess || a.n_entries == 0) return e;
-    constexpr int IT = 2;
+    constexpr int IT = 1;
     constexpr int64_t run = 32 / Row<T, S, D>::CH * IT;                  // entries of a warp
     return launch_overlapped(paged_unload_kernel<T, S, D, IT>, (unsigned)(((a.n_entries + run - 1) / run * 32 + 255) / 256), 256,
                              0, s, a);

@@ -15,6 +15,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 namespace gkv {
 namespace serve {
 
@@ -25,19 +27,17 @@ __device__ __forceinline__ float finite_size(float x) {
     return a <= FLT_MAX ? a : 0.f;
 }
 
-// e + 127 from the largest finite size: its exponent p with 1.m <= 1.75, one more above (the sum carries), less 8.
-__device__ __forceinline__ int row_scale_byte(float top) {
-    return min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8, 7), 246);
+// e + 127 from the bits of the largest finite size: its exponent p with 1.m <= 1.75, one more above (the sum carries), less 8.
+__device__ __forceinline__ int row_scale_byte(uint32_t top) {
+    return min(max((int)((top + 0x1fffffu) >> 23) - 8, 7), 246);
 }
 __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 __device__ __forceinline__ float inverse_of(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 
 // Codes of two values times inv, the first in the low byte.
 __device__ __forceinline__ uint32_t codes2(float x, float y, float inv) {
-    x = fabsf(x) <= FLT_MAX ? x * inv : NAN;
-    y = fabsf(y) <= FLT_MAX ? y * inv : NAN;
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y * inv), "f"(x * inv));
     return r;
 }
 __device__ __forceinline__ uint32_t codes4(const float *x, float inv) {
@@ -57,16 +57,6 @@ __device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
     return r;
 }
 
-// The largest of `n` lanes (a power of two, all of one row), in each of them.  The other lanes of the warp may be elsewhere.
-template <int N>
-__device__ __forceinline__ float row_max(float x) {
-    const int lane = threadIdx.x & 31;
-    const unsigned mask = N == 32 ? 0xffffffffu : ((1u << (N & 31)) - 1) << (lane & ~(N - 1));
-#pragma unroll
-    for (int o = N / 2; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor_sync(mask, x, o));
-    return x;
-}
-
 // 16 bytes of a row: 4 or 8 numbers.
 __device__ __forceinline__ void unpack16(uint4 u, float (&x)[4]) {
     x[0] = __uint_as_float(u.x);
@@ -82,20 +72,52 @@ __device__ __forceinline__ void unpack16(uint4 u, float (&x)[8]) {
         x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
+// The size of a number as its bits without the sign: ordered as the sizes are, infinity and NaN above all others.
+constexpr uint32_t kInfBits = 0x7f800000u;
 template <int N>
-__device__ __forceinline__ float top_of(const float (&x)[N]) {
-    float m = finite_size(x[0]);
+__device__ __forceinline__ uint32_t top_bits(const float (&x)[N]) {
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 1; i < N; i++) m = fmaxf(m, finite_size(x[i]));
+    for (int i = 0; i < N; i++) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
     return m;
 }
+template <int N>
+__device__ __forceinline__ uint32_t top_finite_bits(const float (&x)[N]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) m = max(m, __float_as_uint(finite_size(x[i])));
+    return m;
+}
+// The largest of N lanes (a power of two, all of one row), in each of them.  The other lanes of the warp may be elsewhere.
+template <int N>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+    const int lane = threadIdx.x & 31;
+    const unsigned mask = N == 32 ? 0xffffffffu : ((1u << (N & 31)) - 1) << (lane & ~(N - 1));
+#pragma unroll
+    for (int o = N / 2; o >= 1; o >>= 1) x = max(x, __shfl_xor_sync(mask, x, o));
+    return x;
+}
+// The scale byte of a row of which LANES lanes hold N numbers each; those that are not finite become NaN.
+template <int LANES, int N>
+__device__ __forceinline__ int row_scale(float (&x)[N]) {
+    uint32_t top = row_max<LANES>(top_bits(x));
+    if (top >= kInfBits) {                     // the row's lanes together
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (!(fabsf(x[i]) <= FLT_MAX)) x[i] = NAN;
+        top = row_max<LANES>(top_finite_bits(x));
+    }
+    return row_scale_byte(top);
+}
 // Their codes, at 4 or 8 bytes.
-__device__ __forceinline__ void put_codes(uint8_t *p, const float (&x)[4], float inv) {
+__device__ __forceinline__ void put_codes(uint8_t *p, const float *x, float inv, std::integral_constant<int, 4>) {
     *reinterpret_cast<uint32_t *>(p) = codes4(x, inv);
 }
-__device__ __forceinline__ void put_codes(uint8_t *p, const float (&x)[8], float inv) {
+__device__ __forceinline__ void put_codes(uint8_t *p, const float *x, float inv, std::integral_constant<int, 8>) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(codes4(x, inv), codes4(x + 4, inv));
 }
+template <int N>
+__device__ __forceinline__ float top_of(const float (&x)[N]) { return __uint_as_float(top_finite_bits(x)); }
 
 }  // namespace serve
 }  // namespace gkv

@@ -11,18 +11,15 @@ namespace gkv {
 namespace serve {
 
 constexpr int kPieceStart = 5;             // what a piece costs beside its tiles, in tiles
-constexpr int kPlanBlocks = 2048;          // blocks whose tiles are kept in shared memory
-constexpr int kPlanSearch = 128;           // blocks up to which candidates are compared
+constexpr int kPlanBlocks = 512;           // blocks that are kept in shared memory too
+constexpr int kPlanSearch = 64;            // blocks up to which candidates are compared
 
 template <int T>
 struct PlanSmem {
     int w_max[T / 32], w_sum[T / 32], lo[T], n[T], rb[T], np[T], first[T];
-    int4 blk[T];
-    long long cost[32];
-    int run[32];
-    unsigned long long total;
-    int used, longest;
-    int tiles[kPlanBlocks];
+    int used[T / 32], longest[T / 32], run;
+    long long total[T / 32];
+    int4 blk[kPlanBlocks];
 };
 
 template <typename Op>
@@ -42,17 +39,14 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.c.G, keys = a.keys, most = a.pieces;
     auto larger = [](int x, int y) { return max(x, y); };
     auto sum = [](int x, int y) { return x + y; };
-    if (tid == 0) {
-        sm.total = 0;
-        sm.used = 0;
-        sm.longest = 0;
-    }
     for (int b = tid; b < a.B; b += T) a.plan.req[b] = make_int2(-1, 0);
     __syncthreads();
 
     // ---- the slots' requests.  A slot is left out when its words do not ascend within the batch, or when it
     // begins below the end of an earlier one whose own do; the others have their requests to themselves.
     int end = 0, base = 0;                               // largest end, blocks of rows so far
+    long long total = 0;                                 // tiles; blocks that have any; the most of a block
+    int used = 0, longest = 0;
     for (int p0 = 0; p0 < a.P; p0 += T) {
         const int p = p0 + tid;
         int lo = 0, hi = 0;
@@ -94,19 +88,38 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
                 const int rb_i = i / G, g = i % G, len = a.lens[(int64_t)(p0 + s) * G + g];
                 const int cap = a.c.page_size * a.c.max_pages, k = max(0, min(len, cap)), at = (r0 + rb_i) * G + g;
                 if (len > cap) atomicOr(a.status, kStRange);
-                a.plan.blk[at] = make_int4(p0 + s, l0 + rb_i * a.tok, min(a.tok, ns - rb_i * a.tok), k);
+                const int4 w = make_int4(p0 + s, l0 + rb_i * a.tok, min(a.tok, ns - rb_i * a.tok), k);
+                a.plan.blk[at] = w;
+                if (at < kPlanBlocks) sm.blk[at] = w;
                 const int t = (k + keys - 1) / keys;
-                if (at < kPlanBlocks) sm.tiles[at] = t;
-                atomicAdd(&sm.total, (unsigned long long)t);
-                if (t > 0) atomicAdd(&sm.used, 1);
-                atomicMax(&sm.longest, t);
+                total += t;
+                used += t > 0;
+                longest = max(longest, t);
             }
         }
         __syncthreads();
     }
-    const int blocks = base * G, used = sm.used, longest = sm.longest;
-    const long long total = (long long)sm.total;
-    auto tiles = [&](int i) { return i < kPlanBlocks ? sm.tiles[i] : (a.plan.blk[i].w + keys - 1) / keys; };
+    const int blocks = base * G;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+        used += __shfl_xor_sync(0xffffffffu, used, o);
+        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+    }
+    if (lane == 0) {
+        sm.total[warp] = total;
+        sm.used[warp] = used;
+        sm.longest[warp] = longest;
+    }
+    __syncthreads();
+    total = used = longest = 0;
+    for (int w = 0; w < W; w++) {
+        total += sm.total[w];
+        used += sm.used[w];
+        longest = max(longest, sm.longest[w]);
+    }
+    auto block = [&](int i) { return i < kPlanBlocks ? sm.blk[i] : a.plan.blk[i]; };
+    auto tiles = [&](int i) { return (block(i).w + keys - 1) / keys; };
 
     // ---- tiles of a piece: the candidates lie between an even share of all tiles and what is sure to give no more
     // pieces than there is room for (sum of ceil(t / run) <= total / run + used)
@@ -114,21 +127,20 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
     const int share = (int)min((total + most - 1) / most, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
     int run = max(1, sure);
     if (blocks <= kPlanSearch) {
-        if (tid < 32) {
+        if (warp == 0) {
             const long long widest = max((long long)sure, min((long long)longest, 4ll * sure));
-            const int r = max(1, (int)(share + (widest - share) * tid / 31));
-            long long n = 0;
-            for (int i = 0; i < blocks; i++) n += (sm.tiles[i] + r - 1) / r;
-            sm.run[tid] = r;
-            sm.cost[tid] = n > most ? LLONG_MAX : (n + kShSms - 1) / kShSms * (r + kPieceStart);
+            const int r = max(1, (int)(share + (widest - share) * lane / 31));
+            int n = 0;                                   // pieces, above `most` too many anyway
+            for (int i = 0; i < blocks; i++) n = min(n + (tiles(i) + r - 1) / r, most + 1);
+            // the cost and the candidate in one word, the least of all lanes
+            long long cost = n > most ? LLONG_MAX : (long long)((n + kShSms - 1) / kShSms) * (r + kPieceStart) * 32 + lane;
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) cost = min(cost, __shfl_xor_sync(0xffffffffu, cost, o));
+            const int best = __shfl_sync(0xffffffffu, r, (int)(cost & 31));
+            if (lane == 0) sm.run = cost == LLONG_MAX ? run : best;
         }
         __syncthreads();
-        long long best = LLONG_MAX;
-        for (int w = 0; w < 32; w++)
-            if (sm.cost[w] < best) {
-                best = sm.cost[w];
-                run = sm.run[w];
-            }
+        run = sm.run;
     }
 
     // ---- the pieces
@@ -144,16 +156,13 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
             if (w < warp) first += sm.w_sum[w];
             pieces += sm.w_sum[w];
         }
-        if (i < blocks) {
-            a.plan.first[i] = first;
-            sm.blk[tid] = a.plan.blk[i];
-        }
+        if (i < blocks) a.plan.first[i] = first;
         sm.np[tid] = np;
         sm.first[tid] = first;
         __syncthreads();
         for (int s = warp; s < min(T, blocks - i0); s += W) {
             const int n = sm.np[s], f = sm.first[s];
-            const int4 k = sm.blk[s];
+            const int4 k = block(i0 + s);
             const int t = (k.w + keys - 1) / keys, g = (i0 + s) % G;
             for (int j = lane; j < n; j += 32) {
                 a.plan.piece[2 * (f + j)] = k;
