@@ -147,6 +147,9 @@ __device__ __forceinline__ void pa_mma(float c[4], uint32_t a0, uint32_t a1, uin
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void pa_zero16(uint32_t addr) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0) : "memory");
+}
 __device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -398,6 +401,17 @@ struct PaE4 {
             some |= nv[g];
         }
         if (!some) return;
+        if (count < C::TE || units != (1u << (C::TE / box)) - 1) {
+            // value rows that are not there hold anything: 0
+#pragma unroll
+            for (int g = 0; g < NG; g++)
+                for (int i = lane; i < 16 * (D / 16); i += 32) {
+                    const int r = (warp * NG + g) * 16 + i / (D / 16);
+                    if (i / (D / 16) >= nv[g]) pa_zero16(vst + C::at(r, i % (D / 16)));
+                }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // before the next copy into the stage
+            __syncwarp();
+        }
         float x[NG][2][4];
 #pragma unroll
         for (int g = 0; g < NG; g++)
@@ -432,10 +446,9 @@ struct PaE4 {
 #pragma unroll
                 for (int j = 0; j < 2; j++) {
                     const bool in = e0 + j < nv[g];
-                    // both powers of two in two steps, so that only a logit out of range leaves it
-                    const int t = qe + (int)((k2 >> (8 * j)) & 255) - 127;
-                    float v = x[g][n][j] * scale * __uint_as_float((uint32_t)(127 + (t >> 1)) << 23) *
-                              __uint_as_float((uint32_t)(127 + t - (t >> 1)) << 23);
+                    // 2^(q + k_e), where it is a number: the logit is next to nothing below, out of range above
+                    const int t = min(max(qe + (int)((k2 >> (8 * j)) & 255), 1), 254);
+                    float v = x[g][n][j] * scale * __uint_as_float((uint32_t)t << 23);
                     we[g][n][j] = in ? (int)((v2 >> (8 * j)) & 255) - 127 : kOut;
                     if (has_lm) {
                         const float l = j ? l2.y : l2.x;
@@ -464,7 +477,7 @@ struct PaE4 {
                 for (int j = 0; j < 4; j++) acc[i][j] *= w;
         }
         const float sh = pa_shift(m);
-        uint32_t hi[NG][2], lo[NG][2], keep[NG][2];
+        uint32_t hi[NG][2], lo[NG][2];
 #pragma unroll
         for (int g = 0; g < NG; g++) {
 #pragma unroll
@@ -478,9 +491,6 @@ struct PaE4 {
                 const __half2 r = __floats2half2_rn((v0 - f.x) * 2048.f, (v1 - f.y) * 2048.f);
                 hi[g][n] = *reinterpret_cast<const uint32_t *>(&h);
                 lo[g][n] = *reinterpret_cast<const uint32_t *>(&r);
-                // value rows past the length hold anything: 0
-                const int e0 = n * 8 + 2 * tq;
-                keep[g][n] = (e0 < nv[g] ? 0xffffu : 0u) | (e0 + 1 < nv[g] ? 0xffff0000u : 0u);
             }
         }
 #pragma unroll
@@ -492,7 +502,7 @@ struct PaE4 {
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
                     // bytes (entry 0, channels 0 1), (entry 1, channels 0 1) -> channel 0 of both, channel 1 of both
-                    const uint32_t c0 = __byte_perm(b[2 * k] & keep[g][0], 0, 0x3120), c1 = __byte_perm(b[2 * k + 1] & keep[g][1], 0, 0x3120);
+                    const uint32_t c0 = __byte_perm(b[2 * k], 0, 0x3120), c1 = __byte_perm(b[2 * k + 1], 0, 0x3120);
                     mma_f16(acc[2 * (i + k)], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 & 0xffffu), half2(c1 & 0xffffu));
                     mma_f16(acc[2 * (i + k) + 1], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 >> 16), half2(c1 >> 16));
                 }
