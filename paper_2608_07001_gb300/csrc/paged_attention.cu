@@ -745,9 +745,16 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     const int least = max(C::MIN, (most + kPaPieces - 1) / kPaPieces);
     const int nc = total <= kPaNarrow ? min(nblocks, (int)(((uint32_t)total + least - 1) / (uint32_t)least))
                                       : (int)min((long long)nblocks, (total + least - 1) / least);
-    const long long lo = block < nc ? pa_run_first(block, total, nc) : total;
-    const long long hi = block < nc ? pa_run_first(block + 1, total, nc) : total;
-    if (lo < hi && lo >= before && lo < before + mine) {
+    // short sequences and a CTA for each: no CTA gets two (32 x 8 sequences of 200 entries: 13 us with two in some, 9 so)
+    const bool each = (SHARED || C::QUANT) && snap && S <= nblocks, one = each && block < S && pa_len(a, block) > 0;
+    const long long lo = each ? (one ? 0 : total) : block < nc ? pa_run_first(block, total, nc) : total;
+    const long long hi = each ? (one ? 1 : total) : block < nc ? pa_run_first(block + 1, total, nc) : total;
+    if (each) {
+        if (tid == 0) {
+            sm.s_first = block;
+            sm.first = 0;
+        }
+    } else if (lo < hi && lo >= before && lo < before + mine) {
         int s = tid * seg;
         for (;; s++) {
             const int n = (pa_len(a, s) + C::TE - 1) / C::TE;

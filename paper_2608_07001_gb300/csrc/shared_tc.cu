@@ -26,12 +26,10 @@
 // and zeroes rows of entries that are not there, which are stale memory (0 times
 // what is not finite is NaN), 9 and 10 issue the MMAs of row tile 0 and 1, 11 makes
 // the K step of log m.
-// P is rounded once, as A and B of a product have one type; Z is not.  The scaling
-// goes into the exponent's own FMA, whose result is exact but for one rounding as
-// long as references stay below 2^20 (kFar); beyond, it is a step of its own.
+// P is rounded once, as A and B of a product have one type; Z is not.
 //
-// Quantised pages: codes come through a ring of their own, and a warpgroup more
-// (12-15) writes the tiles as f16, 3 clocks for two codes (as bf16 with their scale 8,
+// Quantised pages: codes come through a ring of their own, and two warpgroups more
+// (12-15 keys, 16-19 values) write the tiles as f16, 3 clocks for two codes (as bf16 with their scale 8,
 // which bounded a tile: 2700 of 5100 clocks).  With k_e, v_e the scales' exponents,
 //   K' = code 2^(k_e - k),  V' = code 2^(v_e - E),  y = S 2^q 2^k c,  O 2^E in the end,
 // k the largest k_e of the tile, E the largest v_e so far, of entries that have a
@@ -55,14 +53,14 @@ namespace {
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpBias = 11, kWarpConv = 12;
 constexpr float kLazy = 8.f;                               // log2 of the growth a reference lets pass
 constexpr float kHead = 7.f;                               // f16: log2 of where the weights start
-constexpr float kFar = 1 << 20;
 constexpr int kNoScale = -120;                             // E before any entry
 constexpr int kLeastQ = -30, kLeastK = -40;                // least q and k, so that kShMost 2^-q 2^-k is a number
 constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr uint32_t kNapNs = 20000;                         // a look at a barrier may last that long
 constexpr int NK = kShKeysTc;                              // keys of a tile
 constexpr int NBIAS = 4;                                   // slots of the K step of log m
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
-constexpr int NFIX = 8;                                    // tiles that the ring holds, at most (10 slots), and more
+constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
 constexpr int kBiased = 1, kSpecial = 2;                   // of a tile: log m; entries that are not there
 
 template <int D, bool QUANT>
@@ -70,47 +68,62 @@ struct Cfg {
     static constexpr int NB = D / 64;                      // 64-channel blocks of a 16-bit row
     static constexpr uint32_t TILE = NB * 128 * 128;       // bytes of a 128-row 16-bit tile
     static constexpr uint32_t RAW = 128 * D;               // bytes of a tile of codes
-    static constexpr int NST = QUANT ? (D == 128 ? 3 : 6) : (D == 128 ? 4 : 10);       // ring slots, 16-bit
-    // ring slots of codes beside two row tiles of queries; one row tile leaves room for two more
-    static constexpr int NR = QUANT ? (D == 128 ? 2 : 6) : 0;
+    // ring slots, 16-bit, of key and of value tiles
+    static constexpr int KS = QUANT ? (D == 128 ? 1 : 3) : (D == 128 ? 2 : 5), VS = QUANT && D == 128 ? 2 : KS;
+    // ring slots of codes, of either kind, beside two row tiles of queries; one row tile leaves room for one more of each
+    static constexpr int NR = QUANT ? (D == 128 ? 1 : 3) : 0;
     static constexpr int NQA = QUANT ? 2 : 1;              // left sides of the K step: by row, or the same for all
-    static constexpr size_t SMEM = 2 * (size_t)TILE + NST * (size_t)TILE + (NBIAS + NQA) * (size_t)AUG + NR * (size_t)RAW;
-    static constexpr int THREADS = QUANT ? 512 : 384;
-    // Registers a thread at launch, then of the softmax, issue and conversion warps; the sums agree.  With 208 a thread
-    // keeps a row's 128 scores; beside a fourth warpgroup it reads them from TMEM twice, for their maximum and, in
-    // halves, for the weights (184 for all at once: 95 in local memory, 3000 clocks a tile instead of 1200).
-    static constexpr int REGS = QUANT ? 128 : 168, RSOFT = QUANT ? 160 : 208, RISSUE = QUANT ? 96 : 88, RCONV = 96;
-    static_assert(256 * RSOFT + 128 * RISSUE + (QUANT ? 128 * RCONV : 0) <= THREADS * REGS, "register split");
-    static_assert(NST <= 2 * NFIX - 2, "fixed tiles");
+    static constexpr size_t SMEM = (2 + KS + VS) * (size_t)TILE + (NBIAS + NQA) * (size_t)AUG + 2 * NR * (size_t)RAW;
+    static constexpr int THREADS = QUANT ? 640 : 384;
+    static_assert(KS < NFIX && VS < NFIX && KS + 4 < 2 * NFIX, "fixed tiles");
 };
 
-template <int NST, int NR, bool QUANT>
+template <int KS, int VS, int NR, bool QUANT>
 struct Bars {
-    uint64_t full[NST], empty[NST], rfull[NR + 2], rempty[NR + 2], qfull[2], qready[2], sfull[2], pfull[2][2], odone[2];
+    uint64_t kfull[KS], kempty[KS], vfull[VS], vempty[VS], krfull[NR + 1], krempty[NR + 1], vrfull[NR + 1], vrempty[NR + 1], qfull[2], qready[2], sfull[2], pfull[2][2], odone[2];
     uint64_t bfull[NBIAS], bempty[NBIAS], kfix[NFIX], vfix[NFIX], fin;
-    alignas(16) __half kmul[QUANT ? NBIAS : 1][QUANT ? NK : 8], vmul[QUANT ? NBIAS : 1][QUANT ? NK : 8];   // 2^(k_e - k), 2^(v_e - E)
+    alignas(16) float lm[QUANT ? NBIAS : 1][QUANT ? NK : 4];             // sqrt(d) log m, -inf for what is not there
+    alignas(16) uint8_t ke[QUANT ? NBIAS : 1][QUANT ? NK : 16], ve[QUANT ? NBIAS : 1][QUANT ? NK : 16];       // scale bytes
     float qscale[2][QUANT ? 128 : 1];  // 2^q
     int kind[NBIAS], ktop[NBIAS], vtop[NBIAS];             // k, E
     uint32_t tbase;
     int abort;
 };
 
-template <class B>
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, B &b, int *status) {
-    const uint32_t addr = tc::smem_u32(bar);
-    uint64_t t0 = 0;
-    for (uint32_t it = 1; !tc::mbar_try_wait(addr, parity); it++)
-        if (!(it & 63u)) {
-            const uint64_t t = tc::globaltimer_ns();
-            if (t0 == 0) t0 = t;
-            if (*(volatile int *)&b.abort) return false;
-            if (t - t0 > kWaitNs) {
+// Bounded.  What a wait does beyond its first look is a call: inlined, two dozen of them were half of the kernel's code,
+// and its roles, which run beside one another, spent most of their time on fetching theirs.
+__device__ __forceinline__ bool try_wait_for(uint32_t bar, uint32_t parity, uint32_t ns) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(ns)
+        : "memory");
+    return ok != 0;
+}
+__device__ __noinline__ bool wait_long(uint32_t addr, uint32_t parity, int *abort, int *status) {
+    const uint64_t t0 = tc::globaltimer_ns();
+    for (uint32_t it = 1; !try_wait_for(addr, parity, kNapNs); it++)
+        if (!(it & 3u)) {
+            if (*(volatile int *)abort) return false;
+            if (tc::globaltimer_ns() - t0 > kWaitNs) {
                 atomicOr(status, kStTimeout);
-                atomicExch(&b.abort, 1);
+                atomicExch(abort, 1);
                 return false;
             }
         }
     return true;
+}
+template <class B>
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, B &b, int *status) {
+    const uint32_t addr = tc::smem_u32(bar);
+    return tc::mbar_try_wait(addr, parity) || wait_long(addr, parity, &b.abort, status);
+}
+__device__ __noinline__ int pool_row(const SharedArgs &a, int64_t seq, int64_t e) {
+    const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
+    return (int)entry_row(look, seq, (int)e, a.status);
 }
 
 __device__ __forceinline__ float max3(float x, float y, float z) {
@@ -142,8 +155,17 @@ __device__ __forceinline__ uint2 three_parts(float x) {
     const uint32_t b = bf16x2_of(r, 0.f);
     return make_uint2(a | (b << 16), bf16x2_of(r - __uint_as_float(b << 16), 0.f));
 }
-// The order of a piece's tiles in the ring: L key tiles, then V(j) and K(j + L) in turn; keys and values so far.
+// The order in which a piece's tiles are taken: L key tiles, then V(j) and K(j + L) in turn; keys and values so far.
 __device__ __forceinline__ bool next_is_key(int keys, int values, int L, int n) { return keys < n && keys < values + L; }
+// A ring's slot that comes next and its phase.
+struct Turn {
+    int at = 0;
+    uint32_t ph;
+    __device__ __forceinline__ explicit Turn(uint32_t first) : ph(first) {}
+    __device__ __forceinline__ void step(int slots) {
+        if (++at == slots) { at = 0; ph ^= 1; }
+    }
+};
 // Shared-memory descriptors of the K step's operands: rows of 32 bytes, 32-byte swizzle (bit 4 of an address by bit 7).
 __device__ __forceinline__ uint64_t aug_desc(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)6 << 61);
@@ -160,11 +182,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     shared_tc_kernel(const SharedArgs a, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                      const __grid_constant__ CUtensorMap mapV) {
     using C = Cfg<D, QUANT>;
-    constexpr int NST = C::NST;
-    // first row tile of queries, ring, K steps, second row tile, codes (where there is no second row tile, from its place on)
+    // first row tile of queries, key slots, value slots, K steps, second row tile, codes (where there is no second row tile, from its place on)
     extern __shared__ __align__(1024) unsigned char Qs[];
-    unsigned char *ring = Qs + C::TILE, *aug = ring + NST * C::TILE, *qaug = aug + NBIAS * AUG, *Qs1 = qaug + C::NQA * AUG;
-    __shared__ Bars<NST, C::NR, QUANT> b;
+    unsigned char *kring = Qs + C::TILE, *vring = kring + C::KS * C::TILE, *aug = vring + C::VS * C::TILE, *qaug = aug + NBIAS * AUG, *Qs1 = qaug + C::NQA * AUG;
+    __shared__ Bars<C::KS, C::VS, C::NR, QUANT> b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     next_may_start();
@@ -195,17 +216,23 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     const int step = two ? 1 : 2, L = step;              // key tiles of a warpgroup; keys ahead of their values
     const int64_t seq = (int64_t)w0.x * a.c.G + g;
     const int box = a.box, per_tile = NK / box;
-    const int nr = C::NR + (two ? 0 : 2);                // slots of codes
+    const int nr = C::NR + (two ? 0 : 1);                // slots of codes, of either kind
     unsigned char *codes = two ? Qs1 + C::TILE : Qs1;
 
     if (warp == kWarpTma && lane == 0) {                 // the thread that uses them first
-        for (int i = 0; i < NST; i++) {
-            tc::mbar_init(tc::smem_u32(&b.full[i]), QUANT ? 4 : 1);
-            tc::mbar_init(tc::smem_u32(&b.empty[i]), 2);
+        for (int i = 0; i < C::KS; i++) {
+            tc::mbar_init(tc::smem_u32(&b.kfull[i]), QUANT ? 4 : 1);
+            tc::mbar_init(tc::smem_u32(&b.kempty[i]), 2);
         }
-        for (int i = 0; i < C::NR + 2; i++) {
-            tc::mbar_init(tc::smem_u32(&b.rfull[i]), 1);
-            tc::mbar_init(tc::smem_u32(&b.rempty[i]), 4);
+        for (int i = 0; i < C::VS; i++) {
+            tc::mbar_init(tc::smem_u32(&b.vfull[i]), QUANT ? 4 : 1);
+            tc::mbar_init(tc::smem_u32(&b.vempty[i]), 2);
+        }
+        for (int i = 0; i < C::NR + 1; i++) {
+            tc::mbar_init(tc::smem_u32(&b.krfull[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.krempty[i]), 4);
+            tc::mbar_init(tc::smem_u32(&b.vrfull[i]), 1);
+            tc::mbar_init(tc::smem_u32(&b.vrempty[i]), 4);
         }
         for (int i = 0; i < 2; i++) {
             tc::mbar_init(tc::smem_u32(&b.qfull[i]), 1);
@@ -228,6 +255,26 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         tc::fence_barrier_init();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    // pages are looked up before the block meets: boxes of tiles, in windows of 32, one a lane, the next window on its
+    // way; for log m, the first of a lane's four keys of a tile, which share a page
+    auto box_rows = [&](int w) {
+        const int u = w * 32 + lane;
+        const int64_t e = (int64_t)j0 * NK + (int64_t)u * box;
+        return u < n * per_tile && e < len ? pool_row(a, seq, e) : -1;
+    };
+    auto key_row = [&](int j) {
+        const int64_t e = (int64_t)(j0 + j) * NK + lane * 4;
+        return j < n && e < len ? pool_row(a, seq, e) : -1;
+    };
+    int now = -1, after = -1, row0 = -1, row1 = -1;
+    if (warp == kWarpTma) {
+        now = box_rows(0);
+        after = box_rows(1);
+    }
+    if (warp == kWarpBias) {
+        row0 = key_row(0);
+        row1 = key_row(1);
+    }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -238,7 +285,6 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     }
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::RSOFT));
         // ---------------- softmax: one thread a row ----------------
         const int i = warp >> 2, q = warp & 3, r = q * 32 + lane;
         const int tk = r / gq, first = two ? i * tpt : 0;
@@ -274,27 +320,24 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.pfull[i][k]));
             };
             if (work) {
-                constexpr int XK = QUANT ? 2 : 4;        // groups of 32 scores in registers
-                uint32_t x[XK][32];
+                // Scores are read twice: for their maximum, which the load returns, and, in halves, for the weights.
+                uint32_t x[2][32];
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int k0 = 0; k0 < 4; k0 += XK) {
-                    float mx[XK];
-#pragma unroll
-                    for (int k = 0; k < XK; k++) tc::tmem_ld32_max_async(ts + 32 * (k0 + k), x[k], mx[k]);
+                for (int h = 0; h < 2; h++) {
+                    float mx[2];
+                    tc::tmem_ld32_max_async(ts + 64 * h, x[0], mx[0]);
+                    tc::tmem_ld32_max_async(ts + 64 * h + 32, x[1], mx[1]);
                     tc::tmem_wait_ld(x[0]);
-#pragma unroll
-                    for (int k = 1; k < XK; k++) tc::tmem_loaded(x[k]);
-#pragma unroll
-                    for (int k = 0; k < XK; k++) tc::tmem_loaded(mx[k]);
-#pragma unroll
-                    for (int k = 0; k < XK; k += 2) top = max3(top, mx[k], mx[k + 1]);
+                    tc::tmem_loaded(x[1]);
+                    tc::tmem_loaded(mx[0]);
+                    tc::tmem_loaded(mx[1]);
+                    top = max3(top, mx[0], mx[1]);
                 }
-                top = top * cs - (QUANT ? kHead : 0.f);
-                const bool grow = m != -INFINITY && top > m + kLazy, far = fabsf(top) > kFar && top != -INFINITY;
+                top = __fadd_rn(__fmul_rn(top, cs), QUANT ? -kHead : 0.f);
+                const bool grow = m != -INFINITY && top > m + kLazy;
                 if (m == -INFINITY) m = top;             // no weight so far
-                bool apart = false;                      // the scaling rounded on its own
-                if (__any_sync(0xffffffffu, grow || far) || (QUANT && ve_new != ve)) {
+                if (__any_sync(0xffffffffu, grow) || (QUANT && ve_new != ve)) {
                     // S(j) was issued after the last product into O, so that one is done
                     float w = grow ? tc::ex2(m - top) : 1.f;
                     z *= w;
@@ -306,41 +349,29 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     if (any) {
 #pragma unroll 1
                         for (int k = 0; k < D / 32; k++) {
-                            uint32_t o[32];
-                            tc::tmem_ld32_async(to + 32 * k, o);
-                            tc::tmem_wait_ld(o);
+                            tc::tmem_ld32_async(to + 32 * k, x[0]);
+                            tc::tmem_wait_ld(x[0]);
 #pragma unroll
-                            for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
-                            tc::tmem_st(to + 32 * k, o);
+                            for (int e = 0; e < 32; e++) x[0][e] = __float_as_uint(__uint_as_float(x[0][e]) * w);
+                            tc::tmem_st(to + 32 * k, x[0]);
                         }
                     }
-                    apart = __any_sync(0xffffffffu, far);
                 }
                 const float sh = m == -INFINITY ? 0.f : -m;
-                const float2 s2 = make_float2(sh, sh), cs2 = apart ? make_float2(1.f, 1.f) : make_float2(cs, cs);
                 float2 acc = make_float2(0.f, 0.f);
                 uint32_t pk[32];
-#pragma unroll (QUANT ? 1 : 2)
+#pragma unroll 1
                 for (int h = 0; h < 2; h++) {
-                    constexpr int K0 = QUANT ? 0 : 1;
-                    if constexpr (QUANT) {
-                        tc::tmem_ld32_async(ts + 64 * h, x[0]);
-                        tc::tmem_ld32_async(ts + 64 * h + 32, x[1]);
-                        tc::tmem_wait_ld(x[0]);
-                        tc::tmem_loaded(x[1]);
-                    }
-                    if (apart) {
-#pragma unroll
-                        for (int e = 0; e < 64; e++) {
-                            uint32_t &v = x[K0 * 2 * h + e / 32][e & 31];
-                            v = __float_as_uint(__uint_as_float(v) * cs);
-                        }
-                    }
+                    tc::tmem_ld32_async(ts + 64 * h, x[0]);
+                    tc::tmem_ld32_async(ts + 64 * h + 32, x[1]);
+                    tc::tmem_wait_ld(x[0]);
+                    tc::tmem_loaded(x[1]);
 #pragma unroll
                     for (int e = 0; e < 32; e++) {
-                        const int at = K0 * h * 64 + 2 * e;
-                        const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[at / 32][at & 31]), __uint_as_float(x[at / 32][(at & 31) + 1])),
-                                                    cs2, s2);
+                        // scaled and shifted in two roundings, as the reference was: of scores of any size the largest gives 1
+                        // (products and sums of pairs would be fused whatever they are called)
+                        const float2 y = make_float2(__fadd_rn(__fmul_rn(__uint_as_float(x[e / 16][2 * e & 31]), cs), sh),
+                                                     __fadd_rn(__fmul_rn(__uint_as_float(x[e / 16][(2 * e & 31) + 1]), cs), sh));
                         const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
                         acc = __fadd2_rn(acc, w);
                         pk[e] = QUANT ? f16x2_of(w.x, w.y) : bf16x2_of(w.x, w.y);
@@ -387,9 +418,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             }
         }
     } else if (warp < kWarpConv) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::RISSUE));
+        const bool one = tc::elect_one();
+        bool ok = true;
         if (warp == kWarpTma) {
-            // ---------------- producer ----------------
+            // ---------------- copies of key and value tiles ----------------
             if (lane == 0) {
                 for (int i = 0; i < (two ? 2 : 1); i++) {
                     const uint32_t qb = tc::smem_u32(&b.qfull[i]);
@@ -399,87 +431,82 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         tc::tma_load_3d(tc::smem_u32((i ? Qs1 : Qs) + cb * 128 * 128), &mapQ, cb * 64, g * gq, b0 + i * tpt, qb);
                 }
             }
-            // boxes of a tile and their pool rows: a window of 32 boxes, one a lane, the next one on its way
-            const bool one = tc::elect_one();
-            const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
-            const int tiles_w = 32 / per_tile;                                     // tiles of a window
-            auto rows_of = [&](int w) {                                            // window w's rows
-                const int u = w * 32 + lane;
-                const int64_t e = (int64_t)j0 * NK + (int64_t)u * box;
-                return u < n * per_tile && e < len ? (int)entry_row(look, seq, (int)e, a.status) : -1;
-            };
-            int before = -1, now = rows_of(0), after = rows_of(1), w_now = 0;
-            const int N = QUANT ? nr : NST;
-            int st = 0, issued = 0;
-            uint32_t ph = 1;
-            bool ok = true;
-            // tiles in the ring's order; rows of entries that are not there become 0 once the tile has landed (which this
-            // warp, having waited for the slot's last use, is the one to see without mistaking the phase)
-            for (int jk = 0, jv = 0; jv < n;) {
+            __syncwarp();
+            const int lp = 31 - __clz(per_tile), ks = QUANT ? nr : C::KS, vs = QUANT ? nr : C::VS;       // per_tile = 2^lp
+            const unsigned whole = (1u << per_tile) - 1;
+            const uint32_t bytes = (uint32_t)(box * D * (QUANT ? 1 : 2)), stepb = (uint32_t)(box * (QUANT ? D : 128));
+            const uint32_t slot = QUANT ? C::RAW : C::TILE, kbase = tc::smem_u32(QUANT ? codes : kring),
+                           vbase = tc::smem_u32(QUANT ? codes + nr * C::RAW : vring);
+            uint64_t *const kf = QUANT ? b.krfull : b.kfull, *const vf = QUANT ? b.vrfull : b.vfull;
+            uint64_t *const ke = QUANT ? b.krempty : b.kempty, *const ve = QUANT ? b.vrempty : b.vempty;
+            // rows of this window, the one before it and the one after it, and which of them are there
+            int before = -1, window = 0, jk = 0, jv = 0;
+            unsigned v_before = 0, v_now = __ballot_sync(0xffffffffu, now >= 0);
+            Turn kt(1), vt(1);
+            // Rows of entries that are not there become 0 once the tile has landed (which this warp, having waited for
+            // the slot's last use, is the one to see without mistaking the phase).
+            while (jv < n) {
                 const bool is_key = next_is_key(jk, jv, L, n);
-                const int j = is_key ? jk++ : jv++;
-                const CUtensorMap *map = is_key ? &mapK : &mapV;
-                const int w = j / tiles_w, u0 = (j - w * tiles_w) * per_tile;
-                if (w > w_now) {                                                   // a key tile, the first of its window
+                const int j = is_key ? jk : jv, w = j >> (5 - lp), u0 = (j << lp) & 31, at = is_key ? kt.at : vt.at;
+                const uint32_t ph = is_key ? kt.ph : vt.ph;
+                if (w > window) {                        // a key tile, the first of its window
                     before = now;
+                    v_before = v_now;
                     now = after;
-                    after = rows_of(++w_now + 1);
+                    v_now = __ballot_sync(0xffffffffu, now >= 0);
+                    after = box_rows(++window + 1);
                 }
-                const int rows = w == w_now ? now : before;
-                const unsigned units = (__ballot_sync(0xffffffffu, rows >= 0) >> u0) & ((1u << per_tile) - 1);
-                ok = __all_sync(0xffffffffu, wait(QUANT ? &b.rempty[st] : &b.empty[st], ph, b, a.status));
+                const int rows = w == window ? now : before;
+                const unsigned units = ((w == window ? v_now : v_before) >> u0) & whole;
+                ok = __all_sync(0xffffffffu, wait((is_key ? ke : ve) + at, ph, b, a.status));
                 if (!ok) break;
-                uint64_t *fb = QUANT ? &b.rfull[st] : &b.full[st];
+                const uint32_t fb = tc::smem_u32((is_key ? kf : vf) + at);
+                uint32_t to = (is_key ? kbase : vbase) + at * slot;
                 if (one) {
-                    if (units) tc::mbar_expect_tx(tc::smem_u32(fb), (uint32_t)(box * D * (QUANT ? 1 : 2) * __popc(units)));
-                    else tc::mbar_arrive(tc::smem_u32(fb));
+                    if (units) tc::mbar_expect_tx(fb, bytes * __popc(units));
+                    else tc::mbar_arrive(fb);
                 }
-                for (int u = 0; u < per_tile; u++) {
+                for (int u = 0; u < per_tile; u++, to += stepb) {
                     const int row = __shfl_sync(0xffffffffu, rows, u0 + u);
-                    if (row < 0) continue;
-                    if (one) {
-                        if (QUANT) {
-                            tc::tma_load_2d(tc::smem_u32(codes + st * C::RAW + u * box * D), map, 0, row, tc::smem_u32(fb));
-                        } else {
+                    if (one && row >= 0) {
 #pragma unroll
-                            for (int cb = 0; cb < C::NB; cb++)
-                                tc::tma_load_2d(tc::smem_u32(ring + st * C::TILE + cb * 128 * 128 + u * box * 128), map, cb * 64, row,
-                                                tc::smem_u32(fb));
+                        for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) {
+                            if (is_key) tc::tma_load_2d(to + cb * 128 * 128, &mapK, cb * 64, row, fb);
+                            else tc::tma_load_2d(to + cb * 128 * 128, &mapV, cb * 64, row, fb);
                         }
                     }
                 }
                 if (!QUANT) {
-                    const int count = min(NK, len - (j0 + j) * NK);
-                    if (count < NK || units != (1u << per_tile) - 1) {
-                        ok = __all_sync(0xffffffffu, wait(fb, ph ^ 1, b, a.status));
+                    const int count = len - (j0 + j) * NK;
+                    if (count < NK || units != whole) {
+                        ok = __all_sync(0xffffffffu, wait((is_key ? kf : vf) + at, ph ^ 1, b, a.status));
+                        unsigned char *tile = (is_key ? kring : vring) + at * C::TILE;
                         for (int i = lane; ok && i < NK * C::NB * 8; i += 32) {
                             const int r = i / (C::NB * 8), cb = i % (C::NB * 8);
                             if (r < count && ((units >> (r / box)) & 1u)) continue;
-                            *reinterpret_cast<uint4 *>(ring + st * C::TILE + (cb >> 3) * (NK * 128) + r * 128 + (cb & 7) * 16) =
-                                make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4 *>(tile + (cb >> 3) * (NK * 128) + r * 128 + (cb & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
                     if (one) tc::mbar_arrive(tc::smem_u32((is_key ? b.kfix : b.vfix) + j % NFIX));
                 }
-                issued++;
-                if (++st == N) { st = 0; ph ^= 1; }
+                if (is_key) {
+                    jk++;
+                    kt.step(ks);
+                } else {
+                    jv++;
+                    vt.step(vs);
+                }
             }
-            // the copies still in flight land before the block exits
-            if (lane == 0) {
-                for (int i = max(0, issued - N); i < issued; i++)
-                    tc::mbar_wait(tc::smem_u32(QUANT ? &b.rfull[i % N] : &b.full[i % N]), (i / N) & 1, kWaitNs);
+            if (lane == 0) {                             // the copies still in flight land before the block exits
+                for (int i = max(0, jk - ks); i < jk; i++) tc::mbar_wait(tc::smem_u32(kf + i % ks), (i / ks) & 1, kWaitNs);
+                for (int i = max(0, jv - vs); i < jv; i++) tc::mbar_wait(tc::smem_u32(vf + i % vs), (i / vs) & 1, kWaitNs);
                 for (int i = 0; i < (two ? 2 : 1); i++) tc::mbar_wait(tc::smem_u32(&b.qfull[i]), 0, kWaitNs);
             }
         } else if (warp == kWarpBias) {
             // ---------------- log m, masks, scales: four keys a lane ----------------
-            const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
             struct Four { int row; float4 lm; uint32_t ks, vs; };
-            auto row_of = [&](int j) {                   // of the first of the lane's keys; the four share a page
-                const int64_t e = (int64_t)(j0 + j) * NK + lane * 4;
-                return j < n && e < len ? (int)entry_row(look, seq, (int)e, a.status) : -1;
-            };
             auto load = [&](int row) {
                 Four f{row, make_float4(0.f, 0.f, 0.f, 0.f), 0x7f7f7f7fu, 0x7f7f7f7fu};
                 if (row >= 0) {
@@ -493,61 +520,51 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             };
             const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
             int top_ve = kNoScale;
-            Four cur = load(row_of(0));
-            int row1 = row_of(1);
-            for (int j = 0; j < n; j++) {
+            Four cur = load(row0);
+            for (int j = 0; ok && j < n; j++) {
                 const int sl = j % NBIAS;
                 const Four f = cur;
                 cur = load(row1);                        // on their way: the next tile's words, the one after's pages
-                row1 = row_of(j + 2);
-                if (!__all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status))) break;
+                row1 = key_row(j + 2);
+                ok = __all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status));
+                if (!ok) break;
                 const int count = f.row < 0 ? 0 : min(4, len - ((j0 + j) * NK + lane * 4));       // keys that are there
                 const float lm[4] = {f.lm.x, f.lm.y, f.lm.z, f.lm.w};
                 float v[4];
-                float down = 1.f;                        // 2^-k
                 bool in[4];
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     in[i] = i < count && lm[i] != -INFINITY;
                     v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
                 }
-                if constexpr (QUANT) {
-                    int ke[4], we[4], kt = kLeastK, vt = kNoScale;
+                const bool special = __any_sync(0xffffffffu, count < 4);
+                if constexpr (QUANT) {                   // the rows' threads make the rest of it
+                    int kt = kLeastK, vt = kNoScale;
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        ke[i] = min((int)((f.ks >> (8 * i)) & 255) - 127, 119);
-                        we[i] = min((int)((f.vs >> (8 * i)) & 255) - 127, 119);
-                        if (in[i]) { kt = max(kt, ke[i]); vt = max(vt, we[i]); }
-                    }
+                    for (int i = 0; i < 4; i++)
+                        if (in[i]) {
+                            kt = max(kt, min((int)((f.ks >> (8 * i)) & 255) - 127, 119));
+                            vt = max(vt, min((int)((f.vs >> (8 * i)) & 255) - 127, 119));
+                        }
                     kt = __reduce_max_sync(0xffffffffu, kt);
                     top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
-                    down = __uint_as_float((uint32_t)(127 - kt) << 23);
-                    __half km[4], vm[4];
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        km[i] = in[i] ? half_pow2(ke[i] - kt) : __ushort_as_half(0);
-                        vm[i] = in[i] ? half_pow2(we[i] - top_ve) : __ushort_as_half(0);
-                    }
-                    *reinterpret_cast<uint2 *>(&b.kmul[sl][lane * 4]) = *reinterpret_cast<const uint2 *>(km);
-                    *reinterpret_cast<uint2 *>(&b.vmul[sl][lane * 4]) = *reinterpret_cast<const uint2 *>(vm);
+                    *reinterpret_cast<float4 *>(&b.lm[sl][lane * 4]) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks;
+                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = f.vs;
                     if (lane == 0) {
                         b.ktop[sl] = kt;
                         b.vtop[sl] = top_ve;
                     }
-                }
-                const bool special = __any_sync(0xffffffffu, count < 4);
-                if (a.c.log_m || special) {
+                } else if (a.c.log_m || special) {
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        put_aug(aug + sl * AUG, lane * 4 + i, three_parts(QUANT ? v[i] * down : v[i]));
-                    }
+                    for (int i = 0; i < 4; i++) put_aug(aug + sl * AUG, lane * 4 + i, three_parts(v[i]));
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 if (lane == 0) b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
                 // the key rows that are not there are 0 before the product
-                if (special && !QUANT && !__all_sync(0xffffffffu, wait(&b.kfix[j % NFIX], (j / NFIX) & 1, b, a.status))) break;
+                if (special && !QUANT) ok = __all_sync(0xffffffffu, wait(&b.kfix[j % NFIX], (j / NFIX) & 1, b, a.status));
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bfull[sl]));
+                if (ok && lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bfull[sl]));
             }
         } else {
             // ---------------- MMA issue: one warp a row tile, one lane issues ----------------
@@ -557,25 +574,24 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             constexpr uint32_t idO = (tc::idesc_bf16_f32(128, D) & (QUANT ? ~kTypes : ~0u)) | tc::kIdescBmn;
             const int i = warp - kWarpMma, start = two ? 0 : i, qi = two ? i : 0;
             const uint32_t qd = (tc::smem_u32(qi ? Qs1 : Qs) >> 4) | (1u << 16);
-            const uint32_t kd = (tc::smem_u32(ring) >> 4) | (1u << 16);
-            const uint32_t vd = (tc::smem_u32(ring) >> 4) | ((NK * 128 >> 4) << 16);
+            const uint32_t kd = (tc::smem_u32(kring) >> 4) | (1u << 16);
+            const uint32_t vd = (tc::smem_u32(vring) >> 4) | ((NK * 128 >> 4) << 16);
             const uint64_t ad = aug_desc(tc::smem_u32(aug)), qad = aug_desc(tc::smem_u32(qaug + (QUANT ? qi : 0) * AUG));
             const uint32_t ts = tb + i * NK, to = tb + 2 * NK + i * D;
-            const bool one = tc::elect_one();
-            bool ok = start >= n || wait(QUANT ? &b.qready[qi] : &b.qfull[qi], 0, b, a.status);
-            // Both warps walk the ring in its order and release every slot, whoever uses it: a warp that passed over a
+            ok = start >= n || wait(QUANT ? &b.qready[qi] : &b.qfull[qi], 0, b, a.status);
+            // Both warps walk both rings in their order and release every slot, whoever uses it: a warp that passed over a
             // slot's phase could take the one after it for landed.
-            int st = 0;
-            uint32_t ph = 0, pp = 0;                     // of the slot that comes next; of the weights
+            Turn kt(0), vt(0);
+            uint32_t pp = 0;                             // phase of the weights
             unsigned fixed = 0;                          // bit j % 32: tile j has rows that are not there
             auto mine = [&](int j) { return two || (j & 1) == i; };
             for (int jk = 0, jv = 0; ok && jv < n;) {
                 const bool is_key = next_is_key(jk, jv, L, n);
-                const int j = is_key ? jk++ : jv++, at = st;
-                ok = wait(&b.full[st], ph, b, a.status) && ok;
-                if (++st == NST) { st = 0; ph ^= 1; }
+                const int j = is_key ? jk++ : jv++, at = is_key ? kt.at : vt.at;
+                ok = wait(is_key ? &b.kfull[at] : &b.vfull[at], is_key ? kt.ph : vt.ph, b, a.status) && ok;
                 if (is_key) {
                     const int sl = j % NBIAS;
+                    kt.step(C::KS);
                     ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
                     tc::tc_fence_after();
                     const int kind = b.kind[sl];
@@ -590,13 +606,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                                 tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
                         if (kind) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
                         tc::mma_commit(tc::smem_u32(&b.sfull[i]));
-                        tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                        tc::mma_commit(tc::smem_u32(&b.kempty[at]));
                         tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
                     } else {
-                        tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
+                        tc::mbar_arrive(tc::smem_u32(&b.kempty[at]));
                         tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
                     }
-                } else if (mine(j)) {
+                    continue;
+                }
+                vt.step(C::VS);
+                if (mine(j)) {
                     const uint32_t va = vd + at * (C::TILE >> 4);
                     if (!QUANT && (fixed >> (j & 31)) & 1u) ok = wait(&b.vfix[j % NFIX], (j / NFIX) & 1, b, a.status) && ok;
 #pragma unroll
@@ -611,11 +630,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     }
                     pp ^= 1;
                     if (ok && one) {
-                        tc::mma_commit(tc::smem_u32(&b.empty[at]));
+                        tc::mma_commit(tc::smem_u32(&b.vempty[at]));
                         if (j + step >= n) tc::mma_commit(tc::smem_u32(&b.odone[i]));
                     }
                 } else if (ok && one) {
-                    tc::mbar_arrive(tc::smem_u32(&b.empty[at]));
+                    tc::mbar_arrive(tc::smem_u32(&b.vempty[at]));
                 }
             }
             ok = __all_sync(0xffffffffu, ok);
@@ -629,15 +648,15 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             tc::mbar_wait(tc::smem_u32(&b.fin), 0, kWaitNs);
         }
     } else if constexpr (QUANT) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::RCONV));
         // ---------------- queries and codes to f16: one thread a row ----------------
-        const int r = (warp - kWarpConv) * 32 + lane;
-        for (int i = 0; i < (two ? 2 : 1); i++) {
+        // the first warpgroup takes the first row tile of queries and the keys, the second one the second and the values
+        const int r = (warp & 3) * 32 + lane, wg = (warp - kWarpConv) >> 2;
+        for (int i = wg; i < (two ? 2 : 1); i += 2) {
             if (!__all_sync(0xffffffffu, wait(&b.qfull[i], 0, b, a.status))) break;
             unsigned char *row = (i ? Qs1 : Qs) + r * 128;
             auto chunk = [&](int ch) { return reinterpret_cast<uint4 *>(row + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (r & 7)) << 4)); };
             float top = 0.f;
-#pragma unroll
+#pragma unroll 1
             for (int ch = 0; ch < D / 8; ch++) {
                 float x[8];
                 unpack16(*chunk(ch), x);
@@ -645,7 +664,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             }
             const int qe = max((int)(__float_as_uint(top) >> 23) - 127 - 14, kLeastQ);
             const float f = __uint_as_float((uint32_t)(127 - qe) << 23);
-#pragma unroll
+#pragma unroll 1
             for (int ch = 0; ch < D / 8; ch++) {
                 float x[8];
                 unpack16(*chunk(ch), x);
@@ -659,42 +678,47 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&b.qready[i]));
         }
-        int rs = 0, st = 0;
-        uint32_t rph = 0, ph = 1;
+        Turn from(0), into(1);
+        const bool keys = wg == 0;
+        const int slots = keys ? C::KS : C::VS;
+        unsigned char *const ring = keys ? kring : vring, *const raw = codes + (keys ? 0 : nr * C::RAW);
         bool ok = true;
-        for (int jk = 0, jv = 0; jv < n;) {
-            const bool is_key = next_is_key(jk, jv, L, n);
-            const int j = is_key ? jk++ : jv++, sl = j % NBIAS;
-            ok = wait(&b.rfull[rs], rph, b, a.status) && ok;
+        for (int j = 0; j < n; j++) {
+            const int sl = j % NBIAS, at = from.at, to = into.at;
+            ok = wait(keys ? &b.krfull[at] : &b.vrfull[at], from.ph, b, a.status) && ok;
             ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
-            ok = __all_sync(0xffffffffu, wait(&b.empty[st], ph, b, a.status) && ok);
+            ok = __all_sync(0xffffffffu, wait(keys ? &b.kempty[to] : &b.vempty[to], into.ph, b, a.status) && ok);
             if (!ok) break;
-            const __half2 s = __half2half2((is_key ? b.kmul : b.vmul)[QUANT ? sl : 0][QUANT ? r : 0]);
-            // entries that are not there have a scale of 0 and, as their codes may be NaN, none of those
-            const bool there = (j0 + j) * NK + r < len && (!(b.kind[sl] & kSpecial) || __half_as_ushort(__low2half(s)) != 0);
-            const unsigned char *src = codes + rs * C::RAW + r * D;
-            unsigned char *dst = ring + st * C::TILE + r * 128;
+            from.step(nr);
+            into.step(slots);
+            // codes of entries that are not there may be anything, NaN too; those without a weight have a scale of 0
+            const float lm = b.lm[QUANT ? sl : 0][QUANT ? r : 0];
+            const int top = keys ? b.ktop[sl] : b.vtop[sl], kind = b.kind[sl];
+            const int e = min((int)(keys ? b.ke : b.ve)[QUANT ? sl : 0][QUANT ? r : 0] - 127, 119) - top;
+            const __half2 s = __half2half2(lm != -INFINITY ? half_pow2(e) : __ushort_as_half(0));
+            const bool there = lm != -INFINITY || !(kind & kSpecial);
+            if (keys && kind) put_aug(aug + sl * AUG, r, three_parts(lm * __uint_as_float((uint32_t)(127 - top) << 23)));
+            const unsigned char *src = raw + at * C::RAW + r * D;
+            unsigned char *dst = ring + to * C::TILE + r * 128;
 #pragma unroll
             for (int ch = 0; ch < D / 16; ch++) {
-                const int from = D == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3);
-                uint4 u = *reinterpret_cast<const uint4 *>(src + from * 16);
+                const int c16 = D == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3);
+                uint4 u = *reinterpret_cast<const uint4 *>(src + c16 * 16);
                 if (!there) u = make_uint4(0, 0, 0, 0);
                 unsigned char *d = dst + (ch >> 2) * (128 * 128);
-                const int at = (ch & 3) * 2;
-                *reinterpret_cast<uint4 *>(d + ((at ^ (r & 7)) << 4)) =
+                const int c8 = (ch & 3) * 2;
+                *reinterpret_cast<uint4 *>(d + ((c8 ^ (r & 7)) << 4)) =
                     make_uint4(half2_of(u.x & 0xffffu, s), half2_of(u.x >> 16, s), half2_of(u.y & 0xffffu, s), half2_of(u.y >> 16, s));
-                *reinterpret_cast<uint4 *>(d + (((at + 1) ^ (r & 7)) << 4)) =
+                *reinterpret_cast<uint4 *>(d + (((c8 + 1) ^ (r & 7)) << 4)) =
                     make_uint4(half2_of(u.z & 0xffffu, s), half2_of(u.z >> 16, s), half2_of(u.w & 0xffffu, s), half2_of(u.w >> 16, s));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                tc::mbar_arrive(tc::smem_u32(&b.full[st]));
-                tc::mbar_arrive(tc::smem_u32(&b.rempty[rs]));
-                if (!is_key) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
+                tc::mbar_arrive(tc::smem_u32(keys ? &b.kfull[to] : &b.vfull[to]));
+                tc::mbar_arrive(tc::smem_u32(keys ? &b.krempty[at] : &b.vrempty[at]));
+                if (!keys) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
             }
-            if (++rs == nr) { rs = 0; rph ^= 1; }
-            if (++st == NST) { st = 0; ph ^= 1; }
         }
     }
     tc::tc_fence_before();
@@ -745,10 +769,6 @@ cudaError_t launch(const SharedArgs &a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
     if (!ready[dev].load(std::memory_order_relaxed)) {
-        cudaFuncAttributes at;
-        e = cudaFuncGetAttributes(&at, kern);
-        if (e != cudaSuccess) return e;
-        if (at.numRegs != C::REGS) return cudaErrorInvalidConfiguration;       // the register split would not add up
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
         if (e != cudaSuccess) return e;
         ready[dev].store(1, std::memory_order_relaxed);
