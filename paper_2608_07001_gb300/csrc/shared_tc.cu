@@ -443,44 +443,56 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int before = -1, window = 0, jk = 0, jv = 0;
             unsigned v_before = 0, v_now = __ballot_sync(0xffffffffu, now >= 0);
             Turn kt(1), vt(1);
-            // Rows of entries that are not there become 0 once the tile has landed (which this warp, having waited for
-            // the slot's last use, is the one to see without mistaking the phase).
-            while (jv < n) {
+            // d = 64: a round takes V(j) and K(j + L), lane 0 sees to the key tile's barriers, lane 1 to the value tile's, as
+            // it is the steps of this one warp that bound a piece of few rows (a tile at a time 2100 clocks a key tile, so
+            // 1500 to 1800).  At d = 128 a tile a round: with rings of two each, waiting for both slots at once loses more
+            // (16 requests on 131072 entries 132 us instead of 114).
+            constexpr bool PAIR = D == 64;
+            while (ok && jv < n) {
                 const bool is_key = next_is_key(jk, jv, L, n);
-                const int j = is_key ? jk : jv, w = j >> (5 - lp), u0 = (j << lp) & 31, at = is_key ? kt.at : vt.at;
-                const uint32_t ph = is_key ? kt.ph : vt.ph;
-                if (w > window) {                        // a key tile, the first of its window
+                const bool has_k = PAIR ? jk < n : is_key, has_v = PAIR ? jk >= L || jk == n : !is_key;
+                const int wk = jk >> (5 - lp), uk = (jk << lp) & 31, uv = (jv << lp) & 31;
+                if (has_k && wk > window) {              // the first key tile of its window
                     before = now;
                     v_before = v_now;
                     now = after;
                     v_now = __ballot_sync(0xffffffffu, now >= 0);
                     after = box_rows(++window + 1);
                 }
-                const int rows = w == window ? now : before;
-                const unsigned units = ((w == window ? v_now : v_before) >> u0) & whole;
-                ok = __all_sync(0xffffffffu, wait((is_key ? ke : ve) + at, ph, b, a.status));
+                const bool v_old = (jv >> (5 - lp)) < window;
+                const int rows = v_old ? before : now;   // of the value tile
+                const unsigned k_units = has_k ? (v_now >> uk) & whole : 0u, v_units = has_v ? ((v_old ? v_before : v_now) >> uv) & whole : 0u;
+                const bool mine_v = lane & 1, has = mine_v ? has_v : has_k;
+                ok = __all_sync(0xffffffffu, !has || wait(mine_v ? ve + vt.at : ke + kt.at, mine_v ? vt.ph : kt.ph, b, a.status));
                 if (!ok) break;
-                const uint32_t fb = tc::smem_u32((is_key ? kf : vf) + at);
-                uint32_t to = (is_key ? kbase : vbase) + at * slot;
-                if (one) {
-                    if (units) tc::mbar_expect_tx(fb, bytes * __popc(units));
-                    else tc::mbar_arrive(fb);
+                const uint32_t kb = tc::smem_u32(kf + kt.at), vb = tc::smem_u32(vf + vt.at);
+                if (lane < 2 && has) {
+                    const unsigned units = mine_v ? v_units : k_units;
+                    if (units) tc::mbar_expect_tx(mine_v ? vb : kb, bytes * __popc(units));
+                    else tc::mbar_arrive(mine_v ? vb : kb);
                 }
-                for (int u = 0; u < per_tile; u++, to += stepb) {
-                    const int row = __shfl_sync(0xffffffffu, rows, u0 + u);
-                    if (one && row >= 0) {
+                __syncwarp();
+                uint32_t k_to = kbase + kt.at * slot, v_to = vbase + vt.at * slot;
+                for (int u = 0; u < per_tile; u++, k_to += stepb, v_to += stepb) {
+                    const int k_row = __shfl_sync(0xffffffffu, now, uk + u), v_row = __shfl_sync(0xffffffffu, rows, uv + u);
+                    if (one) {
+                        if ((k_units >> u) & 1u) {
 #pragma unroll
-                        for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) {
-                            if (is_key) tc::tma_load_2d(to + cb * 128 * 128, &mapK, cb * 64, row, fb);
-                            else tc::tma_load_2d(to + cb * 128 * 128, &mapV, cb * 64, row, fb);
+                            for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) tc::tma_load_2d(k_to + cb * 128 * 128, &mapK, cb * 64, k_row, kb);
+                        }
+                        if ((v_units >> u) & 1u) {
+#pragma unroll
+                            for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) tc::tma_load_2d(v_to + cb * 128 * 128, &mapV, cb * 64, v_row, vb);
                         }
                     }
                 }
                 if (!QUANT) {
-                    const int count = len - (j0 + j) * NK;
-                    if (count < NK || units != whole) {
-                        ok = __all_sync(0xffffffffu, wait((is_key ? kf : vf) + at, ph ^ 1, b, a.status));
-                        unsigned char *tile = (is_key ? kring : vring) + at * C::TILE;
+                    // Rows of entries that are not there become 0 once the tile has landed (which this warp, having waited
+                    // for the slot's last use, is the one to see without mistaking the phase).
+                    auto fixed = [&](int j, unsigned units, uint64_t *full, uint32_t parity, unsigned char *tile) {
+                        const int count = len - (j0 + j) * NK;
+                        if (count >= NK && units == whole) return;
+                        ok = __all_sync(0xffffffffu, wait(full, parity, b, a.status)) && ok;
                         for (int i = lane; ok && i < NK * C::NB * 8; i += 32) {
                             const int r = i / (C::NB * 8), cb = i % (C::NB * 8);
                             if (r < count && ((units >> (r / box)) & 1u)) continue;
@@ -488,13 +500,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
-                    }
-                    if (one) tc::mbar_arrive(tc::smem_u32((is_key ? b.kfix : b.vfix) + j % NFIX));
+                    };
+                    if (has_v) fixed(jv, v_units, vf + vt.at, vt.ph ^ 1, vring + vt.at * C::TILE);
+                    if (has_k) fixed(jk, k_units, kf + kt.at, kt.ph ^ 1, kring + kt.at * C::TILE);
+                    if (lane < 2 && has) tc::mbar_arrive(tc::smem_u32(mine_v ? b.vfix + jv % NFIX : b.kfix + jk % NFIX));
                 }
-                if (is_key) {
+                if (has_k) {
                     jk++;
                     kt.step(ks);
-                } else {
+                }
+                if (has_v) {
                     jv++;
                     vt.step(vs);
                 }
