@@ -732,6 +732,7 @@ class PagedCache(_Workspace):
         self._ref = self._both if quant else self._both[:1]
         L_, kind = lib(), "gracekv_quant_" if quant else "gracekv_paged_"
         self._load, self._append, self._attention = (getattr(L_, kind + x) for x in ("load", "append", "attention"))
+        self._read, self._unload = L_.gracekv_paged_read, L_.gracekv_paged_unload
         self._free = None
 
     @staticmethod
@@ -811,14 +812,17 @@ class PagedCache(_Workspace):
         if not 0 <= b < self.B or not 0 <= E < 1 << 31:
             raise _bad(f"request {b} of {self.B}, {E} entries")
         if out is None:
-            out = (_empty_like_on(stream, (E, self.d), self.dtype, dev), _empty_like_on(stream, (E, self.d), self.dtype, dev),
-                   _empty_like_on(stream, (E,), torch.float32, dev), _empty_like_on(stream, (n1,), torch.int64, dev))
-        K, V, log_m, offsets = out
-        kp, vp = _words("K", K, (E, self.d), self.dtype, dev), _words("V", V, (E, self.d), self.dtype, dev)
-        mp, op = _words("log_m", log_m, (E,), torch.float32, dev), _words("offsets", offsets, (n1,), torch.int64, dev)
-        if E and (kp % 16 or vp % 16):
-            raise _bad("K and V are on 16 bytes")
-        self._run(lib().gracekv_paged_unload, *self._both, b, kp, vp, mp, op, E, self._ws,
+            out = K, V, log_m, offsets = (
+                _empty_like_on(stream, (E, self.d), self.dtype, dev), _empty_like_on(stream, (E, self.d), self.dtype, dev),
+                _empty_like_on(stream, (E,), torch.float32, dev), _empty_like_on(stream, (n1,), torch.int64, dev))
+            kp, vp, mp, op = K.data_ptr(), V.data_ptr(), log_m.data_ptr(), offsets.data_ptr()
+        else:
+            K, V, log_m, offsets = out
+            kp, vp = _words("K", K, (E, self.d), self.dtype, dev), _words("V", V, (E, self.d), self.dtype, dev)
+            mp, op = _words("log_m", log_m, (E,), torch.float32, dev), _words("offsets", offsets, (n1,), torch.int64, dev)
+            if E and (kp % 16 or vp % 16):
+                raise _bad("K and V are on 16 bytes")
+        self._run(self._unload, *self._both, b, kp, vp, mp, op, E, self._ws,
                   self._on(stream, K, V, log_m, offsets, *self._pool))
         return out
 
@@ -943,13 +947,20 @@ class PagedCache(_Workspace):
         dev, dt, shape = self._device, self.dtype, (n, self.G, self.d)
         if n < 0:
             raise _bad(f"{n} rows")
-        k = _empty_like_on(stream, shape, dt, dev) if k is None else k
-        v = _empty_like_on(stream, shape, dt, dev) if v is None else v
-        kp, k_ts, k_hs = _rows("k", k, *shape, dt, dev)
-        vp, v_ts, v_hs = _rows("v", v, *shape, dt, dev)
+        whole = self.G * self.d
+        if k is None:
+            k = _empty_like_on(stream, shape, dt, dev)
+            kp, k_ts, k_hs = k.data_ptr(), whole, self.d
+        else:
+            kp, k_ts, k_hs = _rows("k", k, *shape, dt, dev)
+        if v is None:
+            v = _empty_like_on(stream, shape, dt, dev)
+            vp, v_ts, v_hs = v.data_ptr(), whole, self.d
+        else:
+            vp, v_ts, v_hs = _rows("v", v, *shape, dt, dev)
         _ROWS.pack_into(self._row_buf, 0, n, 0 if cu is None else _words("cu", cu, (self.B + 1,), torch.int32, dev), kp, vp,
                         k_ts, k_hs, v_ts, v_hs)
-        self._run(lib().gracekv_paged_read, *self._both, l, self._rows, self._ws, self._on(stream, k, v, cu, *self._pool))
+        self._run(self._read, *self._both, l, self._rows, self._ws, self._on(stream, k, v, cu, *self._pool))
         return k, v
 
     def attention(self, l: int, q, out=None, stream=None):
