@@ -57,6 +57,7 @@ struct SharedArgs {
     SharedPlan plan;
     int B, P, tok, blocks;  // requests, slots, requests of a block of rows, blocks at most
     int keys, pieces;       // keys of a tile, pieces at most
+    int two;                // what a key tile costs with more than half of a block's requests (shared_plan.cuh)
     const int32_t *lens, *table;                       // of the layer
     const int32_t *cu;      // [P + 1]; null: one slot for all
     const void *q;          // [B][Hq][d]

@@ -16,7 +16,7 @@
 // eight loads of each in flight.  The bf16 kernel's parts lie by channel, so a warp's
 // lanes are rows; the fp32 kernel's by row.
 #include "quant.cuh"
-#include "shared.cuh"
+#include "shared_plan.cuh"
 #include "tc.cuh"
 
 #include <math.h>
@@ -183,6 +183,7 @@ extern "C" gkv_status gracekv_shared_attention(const gkv_paged_cache *c, const g
     a.blocks = (int)y.blocks;
     a.keys = bf16 ? serve::kShKeysTc : serve::kShKeysF32;
     a.pieces = (int)y.pieces;
+    a.two = !bf16 ? serve::kPlanOne : prefix_scales ? serve::kPlanTwoQuant : serve::kPlanTwo;
     a.lens = prefix->lens + (int64_t)l * S;
     a.table = prefix->table + (int64_t)l * S * prefix->max_pages;
     a.cu = cu_prefix;

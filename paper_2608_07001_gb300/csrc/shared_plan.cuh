@@ -1,6 +1,6 @@
 // shared_plan.cuh -- the plan of the attention over a shared prefix: the blocks of
-// rows of all slots, and how many pieces each one's keys are cut into, so that
-// the pieces fill the SMs at a time that is the least of 32 candidates'.
+// rows of all slots, and how many pieces each one's keys are cut into, so that the
+// pieces fill the SMs and the longest one is short.
 #pragma once
 
 #include "shared.cuh"
@@ -10,14 +10,16 @@
 namespace gkv {
 namespace serve {
 
-constexpr int kPieceStart = 5;             // what a piece costs beside its tiles, in tiles
 constexpr int kPlanBlocks = 512;           // blocks that are kept in shared memory too
-constexpr int kPlanSearch = 64;            // blocks up to which candidates are compared
+// What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured, us a key tile, pages of 64: bf16 d = 64
+// 0.98 and 1.68, d = 128 1.26 and 1.89; quantised 0.93 and 1.87, 1.43 and 2.44.
+constexpr int kPlanOne = 2, kPlanTwo = 3, kPlanTwoQuant = 4;
+constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared: there is a piece a SM then (shared_pieces)
 
 template <int T>
 struct PlanSmem {
     int w_max[T / 32], w_sum[T / 32], lo[T], n[T], rb[T], np[T], first[T];
-    int used[T / 32], longest[T / 32], run;
+    int used[T / 32];
     long long total[T / 32];
     int4 blk[kPlanBlocks];
 };
@@ -45,8 +47,9 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
     // ---- the slots' requests.  A slot is left out when its words do not ascend within the batch, or when it
     // begins below the end of an earlier one whose own do; the others have their requests to themselves.
     int end = 0, base = 0;                               // largest end, blocks of rows so far
-    long long total = 0;                                 // tiles; blocks that have any; the most of a block
-    int used = 0, longest = 0;
+    long long total = 0;                                 // what all tiles cost; blocks that have any
+    int used = 0;
+    auto cost = [&](int4 k) { return (k.z > a.tok / 2 ? a.two : kPlanOne) * ((k.w + keys - 1) / keys); };
     for (int p0 = 0; p0 < a.P; p0 += T) {
         const int p = p0 + tid;
         int lo = 0, hi = 0;
@@ -91,10 +94,9 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
                 const int4 w = make_int4(p0 + s, l0 + rb_i * a.tok, min(a.tok, ns - rb_i * a.tok), k);
                 a.plan.blk[at] = w;
                 if (at < kPlanBlocks) sm.blk[at] = w;
-                const int t = (k + keys - 1) / keys;
+                const int t = cost(w);
                 total += t;
                 used += t > 0;
-                longest = max(longest, t);
             }
         }
         __syncthreads();
@@ -104,50 +106,40 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
     for (int o = 16; o >= 1; o >>= 1) {
         total += __shfl_xor_sync(0xffffffffu, total, o);
         used += __shfl_xor_sync(0xffffffffu, used, o);
-        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
     }
     if (lane == 0) {
         sm.total[warp] = total;
         sm.used[warp] = used;
-        sm.longest[warp] = longest;
     }
     __syncthreads();
-    total = used = longest = 0;
+    total = used = 0;
     for (int w = 0; w < W; w++) {
         total += sm.total[w];
         used += sm.used[w];
-        longest = max(longest, sm.longest[w]);
     }
     auto block = [&](int i) { return i < kPlanBlocks ? sm.blk[i] : a.plan.blk[i]; };
-    auto tiles = [&](int i) { return (block(i).w + keys - 1) / keys; };
 
-    // ---- tiles of a piece: the candidates lie between an even share of all tiles and what is sure to give no more
-    // pieces than there is room for (sum of ceil(t / run) <= total / run + used)
+    // ---- the cost of a piece, the least that gives no more pieces than there is room for.  It lies between an even
+    // share of all and what is sure to (sum of ceil(t / run) <= total / run + used); a candidate a thread.
     const int room = most - used;                        // at least half of the SMs, or twice the SMs
     const int share = (int)min((total + most - 1) / most, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
     int run = max(1, sure);
     if (blocks <= kPlanSearch) {
-        if (warp == 0) {
-            const long long widest = max((long long)sure, min((long long)longest, 4ll * sure));
-            const int r = max(1, (int)(share + (widest - share) * lane / 31));
-            int n = 0;                                   // pieces, above `most` too many anyway
-            for (int i = 0; i < blocks; i++) n = min(n + (tiles(i) + r - 1) / r, most + 1);
-            // the cost and the candidate in one word, the least of all lanes
-            long long cost = n > most ? LLONG_MAX : (long long)((n + kShSms - 1) / kShSms) * (r + kPieceStart) * 32 + lane;
-#pragma unroll
-            for (int o = 16; o >= 1; o >>= 1) cost = min(cost, __shfl_xor_sync(0xffffffffu, cost, o));
-            const int best = __shfl_sync(0xffffffffu, r, (int)(cost & 31));
-            if (lane == 0) sm.run = cost == LLONG_MAX ? run : best;
-        }
+        const int r = max(1, (int)(share + (long long)(sure - share) * tid / (T - 1)));
+        int n = 0;
+        for (int i = 0; i < blocks; i++) n = min(n + (int)(((unsigned)cost(block(i)) + r - 1) / (unsigned)r), most + 1);
+        const int least = __reduce_min_sync(0xffffffffu, n > most ? run : r);
+        if (lane == 0) sm.w_max[warp] = least;
         __syncthreads();
-        run = sm.run;
+        for (int w = 0; w < W; w++) run = min(run, sm.w_max[w]);
     }
 
     // ---- the pieces
     int pieces = 0;
     for (int i0 = 0; i0 < blocks; i0 += T) {
         const int i = i0 + tid;
-        const int np = i < blocks ? (tiles(i) + run - 1) / run : 0;
+        const int4 at = i < blocks ? block(i) : make_int4(0, 0, 0, 0);
+        const int np = min((at.w + keys - 1) / keys, (int)(((unsigned)cost(at) + run - 1) / (unsigned)run));
         const int incl = plan_scan(np, sum);
         if (lane == 31) sm.w_sum[warp] = incl;
         __syncthreads();

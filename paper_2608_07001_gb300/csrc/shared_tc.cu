@@ -58,6 +58,7 @@ constexpr int kLeastQ = -30, kLeastK = -40;                // least q and k, so 
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint32_t kNapNs = 20000;                         // a look at a barrier may last that long
 constexpr int NK = kShKeysTc;                              // keys of a tile
+constexpr int kAhead = 4;                                  // tiles that the words beside the rows are fetched ahead: a window at most
 constexpr int NBIAS = 4;                                   // slots of the K step of log m
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
 constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
@@ -126,6 +127,7 @@ __device__ __noinline__ int pool_row(const SharedArgs &a, int64_t seq, int64_t e
     return (int)entry_row(look, seq, (int)e, a.status);
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
@@ -256,24 +258,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     // pages are looked up before the block meets: boxes of tiles, in windows of 32, one a lane, the next window on its
-    // way; for log m, the first of a lane's four keys of a tile, which share a page
+    // way
     auto box_rows = [&](int w) {
         const int u = w * 32 + lane;
         const int64_t e = (int64_t)j0 * NK + (int64_t)u * box;
         return u < n * per_tile && e < len ? pool_row(a, seq, e) : -1;
     };
-    auto key_row = [&](int j) {
-        const int64_t e = (int64_t)(j0 + j) * NK + lane * 4;
-        return j < n && e < len ? pool_row(a, seq, e) : -1;
-    };
-    int now = -1, after = -1, row0 = -1, row1 = -1;
-    if (warp == kWarpTma) {
+    int now = -1, after = -1;
+    if (warp == kWarpTma || warp == kWarpBias) {
         now = box_rows(0);
         after = box_rows(1);
-    }
-    if (warp == kWarpBias) {
-        row0 = key_row(0);
-        row1 = key_row(1);
     }
     tc::tc_fence_before();
     __syncthreads();
@@ -533,14 +527,38 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 }
                 return f;
             };
+            // The first of this lane's keys of tile j, which share a box: of this window or of the one after it.
+            const int lp = 31 - __clz(per_tile), in_box = (lane * 4) & (box - 1);
+            int window = 0;
+            auto key_row = [&](int j) {
+                const int src = (j << lp) >> 5 == window ? now : after;
+                const int r = __shfl_sync(0xffffffffu, src, ((j << lp) + lane * 4 / box) & 31);
+                return r < 0 ? -1 : r + in_box;
+            };
+            // Into L2 a few tiles ahead: from HBM these words take longer than a tile (d = 64, quantised, one row tile,
+            // pages not in L2: 1.45 us a key tile without).
+            auto fetch = [&](int row) {
+                if (row < 0) return;
+                if (a.c.log_m) prefetch_l2(a.c.log_m + row);
+                if (QUANT) {
+                    prefetch_l2(a.scales.k + row);
+                    prefetch_l2(a.scales.v + row);
+                }
+            };
             const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
             int top_ve = kNoScale;
-            Four cur = load(row0);
+            Four cur = load(key_row(0));
+#pragma unroll 1
+            for (int i = 1; i < kAhead; i++) fetch(key_row(i));
             for (int j = 0; ok && j < n; j++) {
                 const int sl = j % NBIAS;
                 const Four f = cur;
-                cur = load(row1);                        // on their way: the next tile's words, the one after's pages
-                row1 = key_row(j + 2);
+                if (((j + 1) << lp) >> 5 > window) {
+                    now = after;
+                    after = box_rows(++window + 1);
+                }
+                cur = load(key_row(j + 1));              // on its way: the next tile's words, a later one's into L2
+                fetch(key_row(j + kAhead));
                 ok = __all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status));
                 if (!ok) break;
                 const int count = f.row < 0 ? 0 : min(4, len - ((j0 + j) * NK + lane * 4));       // keys that are there
