@@ -68,6 +68,7 @@ using namespace serve;
 constexpr int kPaWarps = 4;                        // consumer warps
 constexpr int kPaCons = kPaWarps * 32;
 constexpr int kPaThreads = kPaCons + 32;           // + the producer warp
+constexpr int kPaHeads = 4;                        // heads whose sums the warps leave at once
 constexpr int kPaF32Warps = 3;                     // of them take tiles in the fp32 kernel: one a stage, in turn
 constexpr int kPaRing = 96 * 1024;                 // bytes of the ring
 constexpr int kPaPerSm = 2;                        // resident CTAs a SM
@@ -126,7 +127,7 @@ struct PaSmem {
     int abort, last;
     long long wsum[kPaThreads / 32];
     int wmax[kPaThreads / 32];
-    float m[kPaWarps][8], z[kPaWarps][8], M[8], Z[8];
+    float m[kPaWarps][8], z[kPaWarps][8], f[QUANT ? kPaWarps : 1][8], M[8], Z[8];
 };
 
 constexpr int pa_part_floats(int D) { return 8 * D + 16; }
@@ -296,25 +297,19 @@ struct PaBf {
     }
 
     // Maximum and sum of every head of this warp into shared memory.
-    __device__ __forceinline__ void stats(float *ms, float *zs) {
+    __device__ __forceinline__ void stats(float *ms, float *zs, float *) {
         const int lane = threadIdx.x & 31;
         z += __shfl_xor_sync(0xffffffffu, z, 1);
         z += __shfl_xor_sync(0xffffffffu, z, 2);
         if ((lane & 3) == 0) { ms[lane >> 2] = m; zs[lane >> 2] = z; }
     }
-    // Adds this warp's sums, scaled to the maxima M, into [8][D].
-    __device__ __forceinline__ void add(float *sum, const float *M, int gq, bool first) {
+    // This warp's sums of heads h0 ... h0 + 3 into [4][D].
+    __device__ __forceinline__ void leave(float *sum, int h0, int gq) {
         const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
-        if (hq >= gq) return;
-        const float w = tc::ex2(m - pa_shift(M[hq]));
+        if (hq < h0 || hq >= min(gq, h0 + kPaHeads)) return;
 #pragma unroll
-        for (int i = 0; i < D / 8; i++) {
-            float2 *p = reinterpret_cast<float2 *>(sum + hq * D + i * 8 + 2 * tq);
-            float2 v = first ? make_float2(0.f, 0.f) : *p;
-            v.x += w * (acc[i][0] + acc[i][2]);
-            v.y += w * (acc[i][1] + acc[i][3]);
-            *p = v;
-        }
+        for (int i = 0; i < D / 8; i++)
+            *reinterpret_cast<float2 *>(sum + (hq - h0) * D + i * 8 + 2 * tq) = make_float2(acc[i][0] + acc[i][2], acc[i][1] + acc[i][3]);
     }
 };
 
@@ -510,28 +505,26 @@ struct PaE4 {
         }
     }
 
-    __device__ __forceinline__ void stats(float *ms, float *zs) {
+    // What the sums are to be multiplied by in the end, 2^(E - 14), goes in two steps that stay in range.
+    __device__ __forceinline__ void stats(float *ms, float *zs, float *fs) {
         const int lane = threadIdx.x & 31;
         z += __shfl_xor_sync(0xffffffffu, z, 1);
         z += __shfl_xor_sync(0xffffffffu, z, 2);
-        if ((lane & 3) == 0) { ms[lane >> 2] = m; zs[lane >> 2] = z; }
-    }
-    __device__ __forceinline__ void add(float *sum, const float *M, int gq, bool first) {
-        const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
-        if (hq >= gq) return;
-        // times 2^(E - 14), in two steps that stay in range
-        const float w = tc::ex2(m - pa_shift(M[hq])) * __uint_as_float((uint32_t)(127 + ((ve - 14) >> 1)) << 23);
-        const float w2 = __uint_as_float((uint32_t)(127 + ve - 14 - ((ve - 14) >> 1)) << 23);
-#pragma unroll
-        for (int c = 0; c < D / 16; c++) {
-            float4 *p = reinterpret_cast<float4 *>(sum + hq * D + c * 16 + 4 * tq);
-            float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *p;
-            v.x += w * (acc[2 * c][0] + acc[2 * c][2] * 0x1p-11f) * w2;
-            v.y += w * (acc[2 * c + 1][0] + acc[2 * c + 1][2] * 0x1p-11f) * w2;
-            v.z += w * (acc[2 * c][1] + acc[2 * c][3] * 0x1p-11f) * w2;
-            v.w += w * (acc[2 * c + 1][1] + acc[2 * c + 1][3] * 0x1p-11f) * w2;
-            *p = v;
+        if ((lane & 3) == 0) {
+            ms[lane >> 2] = m;
+            zs[lane >> 2] = z;
+            fs[lane >> 2] = __uint_as_float((uint32_t)(127 + ve - 14 - ((ve - 14) >> 1)) << 23);
         }
+    }
+    __device__ __forceinline__ void leave(float *sum, int h0, int gq) {
+        const int lane = threadIdx.x & 31, hq = lane >> 2, tq = lane & 3;
+        if (hq < h0 || hq >= min(gq, h0 + kPaHeads)) return;
+        const float f = __uint_as_float((uint32_t)(127 + ((ve - 14) >> 1)) << 23);
+#pragma unroll
+        for (int c = 0; c < D / 16; c++)
+            *reinterpret_cast<float4 *>(sum + (hq - h0) * D + c * 16 + 4 * tq) =
+                make_float4((acc[2 * c][0] + acc[2 * c][2] * 0x1p-11f) * f, (acc[2 * c + 1][0] + acc[2 * c + 1][2] * 0x1p-11f) * f,
+                            (acc[2 * c][1] + acc[2 * c][3] * 0x1p-11f) * f, (acc[2 * c + 1][1] + acc[2 * c + 1][3] * 0x1p-11f) * f);
     }
 };
 
@@ -679,7 +672,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     using SM = PaSmem<C::NST, C::TE, C::QUANT>;
     extern __shared__ __align__(1024) unsigned char dsm[];
     unsigned char *ring = dsm;                                   // [NST][keys, values]
-    float *sum = reinterpret_cast<float *>(dsm + C::NST * 2 * C::TB);        // [8][D]
+    float *sum = reinterpret_cast<float *>(dsm + C::NST * 2 * C::TB);        // bf16: [warps][kPaHeads][D]; fp32: [8][D]
     float *qs = sum + 8 * D;                                     // fp32: [GQ][D] queries, then [4][GQ][32] weights
     __shared__ SM sm;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -879,41 +872,75 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sm.empty[st]));
         }
         // ---- the piece: the warps' maxima, then their sums in order
-        w.stats(sm.m[warp], sm.z[warp]);
-        pa_sync();
-        if (tid < gq) {
-            float M = -INFINITY, Z = 0.f;
-            for (int i = 0; i < kPaWarps; i++) M = fmaxf(M, sm.m[i][tid]);
-            for (int i = 0; i < kPaWarps; i++) Z += sm.z[i][tid] * tc::ex2(sm.m[i][tid] - pa_shift(M));
-            sm.M[tid] = M;
-            sm.Z[tid] = Z;
-        }
-        pa_sync();
-        // fp32: only the warps that had one of the piece's tiles, from its first stage on
-        const int adds = C::BF ? kPaWarps : min(kPaF32Warps, t1 - t0), from = C::BF ? 0 : (int)((it - (t1 - t0)) % kPaF32Warps);
-        for (int i = 0; i < adds; i++) {
-            if (warp == (C::BF ? i : (from + i) % kPaF32Warps)) w.add(sum, sm.M, gq, i == 0);
-            pa_sync();
-        }
         T *out = static_cast<T *>(a.out) + (size_t)s * gq * D;
-        const int c_lo = pa_run_of(vs, total, nc), c_hi = pa_run_of(ve - 1, total, nc);
-        if (snap || c_lo == c_hi) {
-            if constexpr (SHARED) {
-                for (int i = tid * 4; i < gq * D; i += kPaCons * 4)
-                    *reinterpret_cast<float4 *>(a.shared.plan.own + (size_t)s * gq * D + i) = *reinterpret_cast<const float4 *>(sum + i);
-                if (tid < gq) a.shared.plan.own_mz[(size_t)s * gq + tid] = make_float2(sm.M[tid], sm.Z[tid]);
+        const int c_lo = snap ? 0 : pa_run_of(vs, total, nc), c_hi = snap ? 0 : pa_run_of(ve - 1, total, nc);
+        // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
+        constexpr int PF = pa_part_floats(D);
+        float *pp = a.part + (size_t)(2 * block + (block == c_lo)) * PF;
+        // four channels of head h, of all heads' from i on
+        auto finish = [&](int i, int h, float M, float Z, float4 v) {
+            if (c_lo != c_hi) {
+                *reinterpret_cast<float4 *>(pp + i) = v;
+                if (i % D == 0) { pp[8 * D + h] = M; pp[8 * D + 8 + h] = Z; }
+            } else if constexpr (SHARED) {
+                *reinterpret_cast<float4 *>(a.shared.plan.own + (size_t)s * gq * D + i) = v;
+                if (i % D == 0) a.shared.plan.own_mz[(size_t)s * gq + h] = make_float2(M, Z);
+            } else if (Z == 0.f) {                                           // a NaN stays
+                put4(out + i, make_float4(0.f, 0.f, 0.f, 0.f));
             } else {
-                for (int i = tid; i < gq * D; i += kPaCons) {
-                    const float Z = sm.Z[i / D];
-                    put(out + i, Z == 0.f ? 0.f : sum[i] / Z);               // a NaN stays
+                put4(out + i, make_float4(v.x / Z, v.y / Z, v.z / Z, v.w / Z));
+            }
+        };
+        if constexpr (C::BF) {
+            // Every warp leaves its sums, four heads at a time, and every thread joins four channels of them: two meetings
+            // a piece.  (Each warp adding to one sum in turn is six, and 1500 of the 5000 clocks that a sequence of 64
+            // entries took; 256 requests of about 100 entries in 8 heads, own entries: 45 us so.)
+            w.stats(sm.m[warp], sm.z[warp], sm.f[C::QUANT ? warp : 0]);
+            for (int h0 = 0; h0 < gq; h0 += kPaHeads) {
+                if (h0) pa_sync();
+                w.leave(sum + warp * kPaHeads * D, h0, gq);
+                pa_sync();
+                const int i = tid * 4, h = h0 + i / D;
+                if (h < min(gq, h0 + kPaHeads)) {
+                    float M = -INFINITY, Z = 0.f;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int k = 0; k < kPaWarps; k++) M = fmaxf(M, sm.m[k][h]);
+#pragma unroll
+                    for (int k = 0; k < kPaWarps; k++) {
+                        const float g = tc::ex2(sm.m[k][h] - pa_shift(M)), f = C::QUANT ? sm.f[C::QUANT ? k : 0][h] : 1.f;
+                        const float4 x = *reinterpret_cast<const float4 *>(sum + k * kPaHeads * D + i);
+                        Z += sm.z[k][h] * g;
+                        if (C::QUANT) {
+                            v.x += g * x.x * f; v.y += g * x.y * f; v.z += g * x.z * f; v.w += g * x.w * f;
+                        } else {
+                            v.x += g * x.x; v.y += g * x.y; v.z += g * x.z; v.w += g * x.w;
+                        }
+                    }
+                    finish(h0 * D + i, h, M, Z, v);
                 }
             }
         } else {
-            // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
-            constexpr int PF = pa_part_floats(D);
-            float *pp = a.part + (size_t)(2 * block + (block == c_lo)) * PF;
-            for (int i = tid; i < gq * D; i += kPaCons) pp[i] = sum[i];
-            if (tid < gq) { pp[8 * D + tid] = sm.M[tid]; pp[8 * D + 8 + tid] = sm.Z[tid]; }
+            w.stats(sm.m[warp], sm.z[warp]);
+            pa_sync();
+            if (tid < gq) {
+                float M = -INFINITY, Z = 0.f;
+                for (int i = 0; i < kPaWarps; i++) M = fmaxf(M, sm.m[i][tid]);
+                for (int i = 0; i < kPaWarps; i++) Z += sm.z[i][tid] * tc::ex2(sm.m[i][tid] - pa_shift(M));
+                sm.M[tid] = M;
+                sm.Z[tid] = Z;
+            }
+            pa_sync();
+            // only the warps that had one of the piece's tiles, from its first stage on
+            const int adds = min(kPaF32Warps, t1 - t0), from = (int)((it - (t1 - t0)) % kPaF32Warps);
+            for (int i = 0; i < adds; i++) {
+                if (warp == (from + i) % kPaF32Warps) w.add(sum, sm.M, gq, i == 0);
+                pa_sync();
+            }
+            for (int i = tid * 4; i < gq * D; i += kPaCons * 4)
+                finish(i, i / D, sm.M[i / D], sm.Z[i / D], *reinterpret_cast<const float4 *>(sum + i));
+        }
+        if (c_lo != c_hi) {
             __threadfence();
             pa_sync();
             if (tid == 0) sm.last = atomicAdd(a.cnt + c_lo, 1) == c_hi - c_lo;
@@ -995,7 +1022,7 @@ cudaError_t pa_launch(const PaArgsOf<SHARED> &a, cudaStream_t s) {
     using C = PaCfg<T, S, D>;
     static std::atomic<int> grid_of[kMaxDevices];
     const auto kern = paged_attention_kernel<T, S, D, GQ, SHARED>;
-    const size_t smem = (size_t)C::NST * 2 * C::TB + 8 * D * sizeof(float) +
+    const size_t smem = (size_t)C::NST * 2 * C::TB + (C::BF ? kPaWarps * kPaHeads : 8) * D * sizeof(float) +
                         (C::BF ? 0 : (size_t)(GQ * D + kPaWarps * GQ * 32) * sizeof(float));
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
