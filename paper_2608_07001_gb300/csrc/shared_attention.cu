@@ -183,7 +183,7 @@ extern "C" gkv_status gracekv_shared_attention(const gkv_paged_cache *c, const g
     a.blocks = (int)y.blocks;
     a.keys = bf16 ? serve::kShKeysTc : serve::kShKeysF32;
     a.pieces = (int)y.pieces;
-    a.two = !bf16 ? serve::kPlanOne : prefix_scales ? serve::kPlanTwoQuant : serve::kPlanTwo;
+    a.two = !bf16 ? serve::kPlanOne : c->d == 128 && !prefix_scales ? serve::kPlanTwoWide : serve::kPlanTwo;
     a.lens = prefix->lens + (int64_t)l * S;
     a.table = prefix->table + (int64_t)l * S * prefix->max_pages;
     a.cu = cu_prefix;

@@ -12,8 +12,9 @@ namespace serve {
 
 constexpr int kPlanBlocks = 512;           // blocks that are kept in shared memory too
 // What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured, us a key tile, pages of 64: bf16 d = 64
-// 0.98 and 1.68, d = 128 1.26 and 1.89; quantised 0.93 and 1.87, 1.43 and 2.44.
-constexpr int kPlanOne = 2, kPlanTwo = 3, kPlanTwoQuant = 4;
+// 0.79 and 1.44, d = 128 1.27 and 1.53; quantised 0.95 and 1.69, 1.44 and 2.41.
+// From HBM one row tile waits for its pages: bf16 d = 128 1.65 and 1.92, the others 1.08 to 1.64 and 1.7 to 2.9.
+constexpr int kPlanOne = 4, kPlanTwoWide = 5, kPlanTwo = 7;
 constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared: there is a piece a SM then (shared_pieces)
 
 template <int T>
