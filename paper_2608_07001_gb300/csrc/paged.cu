@@ -11,7 +11,9 @@
 // (host, fp64), and p F_i mod 2^64 is the fraction of a turn -- one integer
 // product whose error is |p| times that of F_i, which two powers, a product and a
 // quotient in fp64 keep below 2^-53 turns (2^-55 found for bases from 1 to 1e7).
-// Its upper 32 bits, rounded to the 24 of a float (2^-26 turns), go to sincospi.  A
+// Its upper 32 bits, rounded to the 24 of a float (2^-26 turns), go to sincospi; of
+// quantised pages 24 of them, and the 8 left turn the result, as an angle that is off
+// moves a key over the middle between two codes, which is 2^-4 of it.  A
 // thread holds 16 bytes of each half of a row, so the rotation stays in its
 // registers; its sines and cosines serve every row that it takes.
 //
@@ -139,7 +141,15 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
 #pragma unroll
         for (int j = 0; j < N; j++) {
             const int hi = (int)(((unsigned long long)p * turns.at(ch * N + j)) >> 32);
-            sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
+            if constexpr (QUANT) {
+                float s0, c0;
+                sincospif((float)(hi & ~255) * 0x1p-31f, &s0, &c0);
+                const float lo = (__uint_as_float(0x4b000000u | (unsigned)(hi & 255)) - 0x1p23f) * 0x1.921fb6p-30f;     // radians
+                sn[j] = fmaf(lo, c0, s0);
+                cs[j] = fmaf(-lo, s0, c0);
+            } else {
+                sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
+            }
         }
     }
     constexpr int U = R < 2 || QUANT ? 1 : 2;       // rows in flight
