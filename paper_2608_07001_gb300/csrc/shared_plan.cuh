@@ -15,7 +15,7 @@ constexpr int kPlanBlocks = 512;           // blocks that are kept in shared mem
 // 0.79 and 1.44, d = 128 1.27 and 1.53; quantised 0.95 and 1.69, 1.44 and 2.41.
 // From HBM one row tile waits for its pages: bf16 d = 128 1.65 and 1.92, the others 1.08 to 1.64 and 1.7 to 2.9.
 constexpr int kPlanOne = 4, kPlanTwoWide = 5, kPlanTwo = 7;
-constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared: there is a piece a SM then (shared_pieces)
+constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared, for a piece a SM
 
 template <int T>
 struct PlanSmem {
@@ -122,14 +122,17 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
 
     // ---- the cost of a piece, the least that gives no more pieces than there is room for.  It lies between an even
     // share of all and what is sure to (sum of ceil(t / run) <= total / run + used); a candidate a thread.
-    const int room = most - used;                        // at least half of the SMs, or twice the SMs
-    const int share = (int)min((total + most - 1) / most, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
+    // (Room for more pieces than SMs, as slots without requests leave, is of no use to few blocks: a piece has its own
+    // start of some ten tiles.)
+    const int target = blocks <= kPlanSearch ? min(most, kShSms) : most;
+    const int room = target - used;                      // at least half of the SMs, or twice the SMs
+    const int share = (int)min((total + target - 1) / target, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
     int run = max(1, sure);
     if (blocks <= kPlanSearch) {
         const int r = max(1, (int)(share + (long long)(sure - share) * tid / (T - 1)));
         int n = 0;
-        for (int i = 0; i < blocks; i++) n = min(n + (int)(((unsigned)cost(block(i)) + r - 1) / (unsigned)r), most + 1);
-        const int least = __reduce_min_sync(0xffffffffu, n > most ? run : r);
+        for (int i = 0; i < blocks; i++) n = min(n + (int)(((unsigned)cost(block(i)) + r - 1) / (unsigned)r), target + 1);
+        const int least = __reduce_min_sync(0xffffffffu, n > target ? run : r);
         if (lane == 0) sm.w_max[warp] = least;
         __syncthreads();
         for (int w = 0; w < W; w++) run = min(run, sm.w_max[w]);
