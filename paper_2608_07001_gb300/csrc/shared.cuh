@@ -26,11 +26,12 @@ constexpr int kShKeysTc = 128, kShKeysF32 = 64;        // keys of a tile
 __host__ __device__ constexpr int shared_tok(bool bf16, int gq) { return bf16 ? 2 * (kShRowsTc / gq) : kShRowsF32 / gq; }
 // Blocks of rows of one KV head at most: sum over slots of ceil(n_p / tok).
 __host__ __device__ inline int64_t shared_row_blocks(int B, int P, int tok) { return (int64_t)B / tok + P; }
-// Pieces at most: one a SM where the blocks are few enough to share the SMs among them, else (a block's last
-// piece is a partial one) as many as fill the SMs twice and one more a block.
-constexpr int kShFewBlocks = kShSms / 2;
-__host__ __device__ inline int64_t shared_pieces(int64_t blocks) {
-    return blocks <= kShFewBlocks ? kShSms : blocks + 2 * kShSms;
+// Pieces that run at once: one a SM (bf16), two (fp32: 64 rows of 4 warps; one a SM 24 TFLOP/s at d = 128, two 48).
+__host__ __device__ constexpr int shared_at_once(bool bf16) { return bf16 ? kShSms : 2 * kShSms; }
+// Pieces at most: as many where the blocks are few enough to share the SMs among them, else (a block's last
+// piece is a partial one) twice as many and one more a block.
+__host__ __device__ inline int64_t shared_pieces(bool bf16, int64_t blocks) {
+    return blocks <= shared_at_once(bf16) / 2 ? shared_at_once(bf16) : blocks + 2 * shared_at_once(bf16);
 }
 // Floats of a part: sums by 4 channels, the rows' references (base 2), their weights' sums.
 __host__ __device__ constexpr size_t shared_part_floats(bool bf16, int d) {

@@ -124,7 +124,7 @@ gkv_status layout_of(const gkv_paged_cache *c, const gkv_paged_cache *prefix, La
     const bool bf16 = c->dtype == GKV_BF16;
     y.tok = shared_tok(bf16, c->Hq / c->G);
     y.blocks = shared_row_blocks(c->B, prefix->B, y.tok) * c->G;
-    y.pieces = shared_pieces(y.blocks);
+    y.pieces = shared_pieces(bf16, y.blocks);
     if (y.pieces * 2 >= (1LL << 31)) return GKV_EUNSUPPORTED;
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     y.scratch = kWsHead;

@@ -225,7 +225,7 @@ cudaError_t launch(const SharedArgs &a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         ready[dev].store(1, std::memory_order_relaxed);
     }
-    return launch_overlapped(kern, dim3((unsigned)shared_pieces(a.blocks)), kThreads, Cfg<D>::SMEM, s, a);
+    return launch_overlapped(kern, dim3((unsigned)shared_pieces(false, a.blocks)), kThreads, Cfg<D>::SMEM, s, a);
 }
 
 }  // namespace

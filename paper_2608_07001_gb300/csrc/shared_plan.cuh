@@ -15,7 +15,7 @@ constexpr int kPlanBlocks = 512;           // blocks that are kept in shared mem
 // 0.79 and 1.44, d = 128 1.27 and 1.53; quantised 0.95 and 1.69, 1.44 and 2.41.
 // From HBM one row tile waits for its pages: bf16 d = 128 1.65 and 1.92, the others 1.08 to 1.64 and 1.7 to 2.9.
 constexpr int kPlanOne = 4, kPlanTwoWide = 5, kPlanTwo = 7;
-constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared, for a piece a SM
+constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared, for as many pieces as run at once
 
 template <int T>
 struct PlanSmem {
@@ -124,7 +124,7 @@ __device__ __noinline__ void make_plan(const SharedArgs &a, PlanSmem<T> &sm) {
     // share of all and what is sure to (sum of ceil(t / run) <= total / run + used); a candidate a thread.
     // (Room for more pieces than SMs, as slots without requests leave, is of no use to few blocks: a piece has its own
     // start of some ten tiles.)
-    const int target = blocks <= kPlanSearch ? min(most, kShSms) : most;
+    const int target = blocks <= kPlanSearch ? min(most, shared_at_once(keys == kShKeysTc)) : most;
     const int room = target - used;                      // at least half of the SMs, or twice the SMs
     const int share = (int)min((total + target - 1) / target, (long long)INT_MAX), sure = (int)min((total + room - 1) / room, (long long)INT_MAX);
     int run = max(1, sure);

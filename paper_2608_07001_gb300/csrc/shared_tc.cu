@@ -827,7 +827,7 @@ cudaError_t launch(const SharedArgs &a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         ready[dev].store(1, std::memory_order_relaxed);
     }
-    return launch_overlapped(kern, dim3((unsigned)shared_pieces(a.blocks)), C::THREADS, C::SMEM, s, a, mq, mk, mv);
+    return launch_overlapped(kern, dim3((unsigned)shared_pieces(true, a.blocks)), C::THREADS, C::SMEM, s, a, mq, mk, mv);
 }
 
 }  // namespace
