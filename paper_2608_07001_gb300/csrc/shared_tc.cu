@@ -19,7 +19,16 @@
 // other key tile and sums of its own, which are two parts.
 //
 // Few requests: bound by reading the prefix, 64 KB a key tile of d = 128 against two
-// products of 128^3; many: by the tensor pipe and the 128^2 exponentials a tile.
+// products of 128^3; many: by the chain product, exponentials, product of a row tile, of
+// which TMEM holds two.  us a key tile and SM, pages of 64 entries, log m; in L2 / from HBM:
+//                      one row tile     two row tiles
+//   bf16       d = 64  0.79 / 1.08      1.44 / 1.55
+//              d = 128 1.27 / 1.65      1.53 / 1.67       (64 KB in 1.65 us: 6.0 TB/s of all SMs)
+//   quantised  d = 64  0.95 / 1.08      1.69 / 1.80
+//              d = 128 1.44 / 1.64      2.41 / 2.9
+// Pages of 16 entries: 1.4 to 2.5, as every box of a page is a copy of its own (shapes of one
+// copy that leave out the second 64 channels are not to be had with rows of 128 bytes).
+// A piece takes about 10 us beside its tiles.
 //
 // Warps: 0-3 and 4-7 softmax (a thread a row), 8 looks pages up and issues TMA
 // (boxes of up to 64 entries that do not cross a page; K and V tiles through a ring)
@@ -467,18 +476,17 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     else tc::mbar_arrive(mine_v ? vb : kb);
                 }
                 __syncwarp();
-                uint32_t k_to = kbase + kt.at * slot, v_to = vbase + vt.at * slot;
-                for (int u = 0; u < per_tile; u++, k_to += stepb, v_to += stepb) {
-                    const int k_row = __shfl_sync(0xffffffffu, now, uk + u), v_row = __shfl_sync(0xffffffffu, rows, uv + u);
-                    if (one) {
-                        if ((k_units >> u) & 1u) {
+                // a box a lane: 0-7 of the key tile, 8-15 of the value tile (one lane with a loop over the boxes: pages of 16, quantised
+                // d = 128 2.2 us a key tile instead of 1.5, bf16 2.3 instead of 2.0; pages of 64, bf16 1.27 instead of 1.19)
+                {
+                    const int u = lane & 7;
+                    const bool v_lane = lane & 8;
+                    const int k_row = __shfl_sync(0xffffffffu, now, (uk + u) & 31), v_row = __shfl_sync(0xffffffffu, rows, (uv + u) & 31);
+                    if (lane < 16 && ((v_lane ? v_units : k_units) >> u) & 1u) {
+                        const uint32_t to = (v_lane ? vbase + vt.at * slot : kbase + kt.at * slot) + u * stepb;
+                        const CUtensorMap *map = v_lane ? &mapV : &mapK;
 #pragma unroll
-                            for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) tc::tma_load_2d(k_to + cb * 128 * 128, &mapK, cb * 64, k_row, kb);
-                        }
-                        if ((v_units >> u) & 1u) {
-#pragma unroll
-                            for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) tc::tma_load_2d(v_to + cb * 128 * 128, &mapV, cb * 64, v_row, vb);
-                        }
+                        for (int cb = 0; cb < (QUANT ? 1 : C::NB); cb++) tc::tma_load_2d(to + cb * 128 * 128, map, cb * 64, v_lane ? v_row : k_row, v_lane ? vb : kb);
                     }
                 }
                 if (!QUANT) {
