@@ -25,8 +25,8 @@
 //
 // Quantised pages (quant.cuh): a row's threads find its largest size with shuffles and
 // store 1 byte for 2 or 4, so HBM asks for half as much and what bounds both is the
-// instructions of a row: the same tokens 138 us (642 MB, 4.7 TB/s), load 150 us (818 MB,
-// 5.5 TB/s).
+// instructions of a row: the same tokens 138 us (738 MB, 5.3 TB/s), load 150 us (816 MB,
+// 5.4 TB/s).
 #include "paged.cuh"
 #include "quant.cuh"
 

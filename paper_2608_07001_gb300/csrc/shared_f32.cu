@@ -47,8 +47,8 @@ __global__ void __launch_bounds__(kThreads, 2) shared_f32_kernel(const SharedArg
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     next_may_start();
     after_previous();
-    if ((int)blockIdx.x >= *a.plan.pieces) return;
     const int4 w0 = a.plan.piece[2 * blockIdx.x], w1 = a.plan.piece[2 * blockIdx.x + 1];
+    if ((int)blockIdx.x >= *a.plan.pieces) return;
     const int b0 = w0.y, nb = w0.z, len = w0.w, g = w1.x, j0 = w1.y, j1 = w1.z, gq = a.c.Hq / a.c.G;
     const int64_t seq = (int64_t)w0.x * a.c.G + g;
 

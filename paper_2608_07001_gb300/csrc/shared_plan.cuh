@@ -11,9 +11,8 @@ namespace gkv {
 namespace serve {
 
 constexpr int kPlanBlocks = 512;           // blocks that are kept in shared memory too
-// What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured, us a key tile, pages of 64: bf16 d = 64
-// 0.79 and 1.44, d = 128 1.27 and 1.53; quantised 0.95 and 1.69, 1.44 and 2.41.
-// From HBM one row tile waits for its pages: bf16 d = 128 1.65 and 1.92, the others 1.08 to 1.64 and 1.7 to 2.9.
+// What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured (shared_tc.cu) 1.3 and 1.15 times as much
+// for bf16 of d = 128, in L2 and from HBM, 1.4 to 1.8 for the others.
 constexpr int kPlanOne = 4, kPlanTwoWide = 5, kPlanTwo = 7;
 constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared, for as many pieces as run at once
 

@@ -22,12 +22,11 @@
 // products of 128^3; many: by the chain product, exponentials, product of a row tile, of
 // which TMEM holds two.  us a key tile and SM, pages of 64 entries, log m; in L2 / from HBM:
 //                      one row tile     two row tiles
-//   bf16       d = 64  0.79 / 1.08      1.44 / 1.55
-//              d = 128 1.27 / 1.65      1.53 / 1.67       (64 KB in 1.65 us: 6.0 TB/s of all SMs)
-//   quantised  d = 64  0.95 / 1.08      1.69 / 1.80
-//              d = 128 1.44 / 1.64      2.41 / 2.9
-// Pages of 16 entries: 1.4 to 2.5, as every box of a page is a copy of its own (shapes of one
-// copy that leave out the second 64 channels are not to be had with rows of 128 bytes).
+//   bf16       d = 64  0.79 / 1.03      1.44 / 1.45
+//              d = 128 1.19 / 1.59      1.54 / 1.82       (64 KB in 1.59 us: 6.3 TB/s of all SMs)
+//   quantised  d = 64  0.95 / 1.05      1.68 / 1.71
+//              d = 128 1.43 / 1.51      2.20 / 2.52
+// Pages of 16 entries, each box of which is a copy of its own: 1.1 to 1.3, 2.0 to 2.2 (bf16, d = 128) and as above.
 // A piece takes about 10 us beside its tiles.
 //
 // Warps: 0-3 and 4-7 softmax (a thread a row), 8 looks pages up and issues TMA
@@ -215,13 +214,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     }
     after_previous();
     // ---- the piece
+    int4 w0 = a.plan.piece[2 * blockIdx.x], w1 = a.plan.piece[2 * blockIdx.x + 1];        // (of a block without one: anything)
     const bool idle = (int)blockIdx.x >= *a.plan.pieces;
     const int gq = a.c.Hq / a.c.G, tpt = a.tok / 2;
-    int4 w0 = make_int4(0, 0, 0, 0), w1 = w0;
-    if (!idle) {
-        w0 = a.plan.piece[2 * blockIdx.x];
-        w1 = a.plan.piece[2 * blockIdx.x + 1];
-    }
+    if (idle) w0 = w1 = make_int4(0, 0, 0, 0);
     const int b0 = w0.y, nb = w0.z, len = w0.w, g = w1.x, j0 = w1.y, n = w1.z - w1.y;
     const bool two = nb > tpt;                           // two row tiles
     const int step = two ? 1 : 2, L = step;              // key tiles of a warpgroup; keys ahead of their values

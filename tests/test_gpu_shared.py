@@ -188,6 +188,36 @@ def test_many_slots_and_layers(gk):
 
 
 @pytest.mark.parametrize("dtype,quant", KINDS)
+def test_few_of_many_slots(gk, dtype, quant):
+    # the workspace has room for more pieces than run at once; blocks of one and of two row tiles share them
+    own = np.random.default_rng(9).integers(0, 30, (1, 50, 2))
+    pre = np.full((1, 60, 2), 3)
+    pre[0, 7], pre[0, 31] = (3000, 5000), (2500, 40)
+    cu = [0] * 8 + [41] * 24 + [50] * 29
+    attend(gk, own, pre, cu=cu, d=64, dtype=dtype, quant=(quant, quant), seed=9)
+
+
+@pytest.mark.parametrize("dtype,quant", KINDS)
+@pytest.mark.parametrize("Hq", [2, 10, 14, 16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_short_own_sequences(gk, dtype, quant, Hq, d):
+    # several sequences a CTA, whole and cut, of up to eight heads
+    rng = np.random.default_rng(Hq)
+    own = rng.integers(1, 150, (1, 400, 2))
+    if Hq == 14:
+        own[0, 5] = 3000
+    attend(gk, own, [[[70, 0]]], Hq=Hq, d=d, dtype=dtype, quant=(quant, False), seed=Hq)
+
+
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [3, 40])
+def test_long_prefix_of_small_pages(gk, quant, d, B):
+    # windows of looked-up boxes turn many times beside tiles of log m
+    attend(gk, np.full((1, B, 1), 2), [[[50011]]], ps=(16, 16), Hq=4, d=d, quant=(quant, quant), seed=B)
+
+
+@pytest.mark.parametrize("dtype,quant", KINDS)
 def test_log_m_extremes(gk, dtype, quant):
     low = torch.finfo(torch.float32).min
 
