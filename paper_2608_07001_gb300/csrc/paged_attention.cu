@@ -706,14 +706,18 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         }
     }
 
-    // ---- the CTA's run: tiles of all sequences, and where its own begin
+    // ---- the CTA's run: tiles of all sequences, and where its own begin.  On the line that is cut a sequence has LEAD
+    // places in front of its tiles: it begins and ends in the time of about 128 entries.  (256 requests of about 100
+    // entries in 8 heads: the last CTA done after 51 us, of 12 sequences, the first after 26, of one, without.)
+    constexpr int LEAD = SHARED || C::QUANT ? 128 / C::TE : 0;
+    auto places = [&](int n) { return n > 0 ? (n + C::TE - 1) / C::TE + LEAD : 0; };
     const int seg = (S + kPaThreads - 1) / kPaThreads;
     long long mine = 0;
     int most = 0;
     for (int s = tid * seg; s < min(S, (tid + 1) * seg); s++) {
         const int n = pa_len(a, s);
         if (n < a.lens[s]) atomicOr(a.status, kStRange);
-        mine += (n + C::TE - 1) / C::TE;
+        mine += places(n);
         most = max(most, (n + C::TE - 1) / C::TE);
     }
 #pragma unroll
@@ -755,11 +759,11 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     } else if (lo < hi && lo >= before && lo < before + mine) {
         int s = tid * seg;
         for (;; s++) {
-            const int n = (pa_len(a, s) + C::TE - 1) / C::TE;
+            const int n = places(pa_len(a, s));
             if (lo < before + n) break;
             before += n;
         }
-        if (snap && lo > before) before += (pa_len(a, s++) + C::TE - 1) / C::TE;
+        if (snap && lo > before) before += places(pa_len(a, s++));
         sm.s_first = s;
         sm.first = before;
     }
@@ -783,8 +787,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         long long vs = sm.first;
         for (int s = sm.s_first; ok && s < S && vs < hi; s++) {
             const int n = pa_len(a, s), nt = (n + C::TE - 1) / C::TE;
-            const int t0 = snap ? 0 : (int)(max(lo, vs) - vs), t1 = snap ? nt : (int)(min(hi, vs + nt) - vs);
-            vs += nt;
+            const int t0 = snap ? 0 : (int)max(lo - vs - LEAD, 0ll), t1 = snap ? nt : (int)min(hi - vs - LEAD, (long long)nt);
+            vs += places(n);
             int held0 = 0, held = 0;                 // boxes [held0, held0 + held) looked up, one a lane
             int row = -1;
             for (int t = t0; ok && t < t1; t++, it++) {
@@ -851,8 +855,9 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
     for (int s = sm.s_first; s < S && vs < hi; s++) {
         const int n = pa_len(a, s), nt = (n + C::TE - 1) / C::TE;
         if (nt == 0) continue;
-        const long long ve = vs + nt;
-        const int t0 = snap ? 0 : (int)(max(lo, vs) - vs), t1 = snap ? nt : (int)(min(hi, ve) - vs);
+        const long long ve = vs + nt + LEAD;
+        const int t0 = snap ? 0 : (int)max(lo - vs - LEAD, 0ll), t1 = snap ? nt : (int)min(hi - vs - LEAD, (long long)nt);
+        if (t0 >= t1) { vs = ve; continue; }             // its tiles begin in the next run
         if constexpr (C::BF) {
             w.begin(a, s, gq);
         } else {
@@ -878,7 +883,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         }
         // ---- the piece: the warps' maxima, then their sums in order
         T *out = static_cast<T *>(a.out) + (size_t)s * gq * D;
-        const int c_lo = snap ? 0 : pa_run_of(vs, total, nc), c_hi = snap ? 0 : pa_run_of(ve - 1, total, nc);
+        const int c_lo = snap ? 0 : pa_run_of(vs + LEAD, total, nc), c_hi = snap ? 0 : pa_run_of(ve - 1, total, nc);
         // slot 2 c: the sequence the CTA continues, 2 c + 1: the one it begins and leaves
         constexpr int PF = pa_part_floats(D);
         float *pp = a.part + (size_t)(2 * block + (block == c_lo)) * PF;
