@@ -394,21 +394,26 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         if (ok && work) {
             if (any) {
 #pragma unroll 1
-                for (int k = 0; k < D / 32; k++) {
-                    uint32_t u[32];
-                    tc::tmem_ld32_async(to + 32 * k, u);
-                    tc::tmem_wait_ld(u);
-                    if constexpr (QUANT) {               // O 2^E, in two steps that stay in range
-                        const int h = ve >> 1;
-                        const float f0 = __uint_as_float((uint32_t)(127 + h) << 23), f1 = __uint_as_float((uint32_t)(127 + ve - h) << 23);
+                for (int k = 0; k < D / 32; k += 2) {
+                    uint32_t u[2][32];
+                    tc::tmem_ld32_async(to + 32 * k, u[0]);
+                    tc::tmem_ld32_async(to + 32 * k + 32, u[1]);
+                    tc::tmem_wait_ld(u[0]);
+                    tc::tmem_loaded(u[1]);
 #pragma unroll
-                        for (int e = 0; e < 32; e++) u[e] = __float_as_uint(__uint_as_float(u[e]) * f0 * f1);
-                    }
-                    if (live) {
+                    for (int x = 0; x < 2; x++) {
+                        if constexpr (QUANT) {           // O 2^E, in two steps that stay in range
+                            const int h = ve >> 1;
+                            const float f0 = __uint_as_float((uint32_t)(127 + h) << 23), f1 = __uint_as_float((uint32_t)(127 + ve - h) << 23);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4 *>(pp + ((size_t)(k * 8 + e / 4) * kShRowsTc + r) * 4) =
-                                make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                            for (int e = 0; e < 32; e++) u[x][e] = __float_as_uint(__uint_as_float(u[x][e]) * f0 * f1);
+                        }
+                        if (live) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<uint4 *>(pp + ((size_t)((k + x) * 8 + e / 4) * kShRowsTc + r) * 4) =
+                                    make_uint4(u[x][e], u[x][e + 1], u[x][e + 2], u[x][e + 3]);
+                        }
                     }
                 }
             }
@@ -707,14 +712,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         }
     } else if constexpr (QUANT) {
         // ---------------- queries and codes to f16: one thread a row ----------------
-        // the first warpgroup takes the first row tile of queries and the keys, the second one the second and the values
+        // the first warpgroup takes the keys, the second one the values and, as the first product waits for keys and queries,
+        // the first row tile of queries
         const int r = (warp & 3) * 32 + lane, wg = (warp - kWarpConv) >> 2;
-        for (int i = wg; i < (two ? 2 : 1); i += 2) {
+        for (int i = wg ^ 1; i < (two ? 2 : 1); i += 2) {
             if (!__all_sync(0xffffffffu, wait(&b.qfull[i], 0, b, a.status))) break;
             unsigned char *row = (i ? Qs1 : Qs) + r * 128;
             auto chunk = [&](int ch) { return reinterpret_cast<uint4 *>(row + (ch >> 3) * (128 * 128) + (((ch & 7) ^ (r & 7)) << 4)); };
             float top = 0.f;
-#pragma unroll 1
+            // (3650 clocks of the 19000 of a piece of one tile; 4400 with a chunk at a time)
+#pragma unroll 4
             for (int ch = 0; ch < D / 8; ch++) {
                 float x[8];
                 unpack16(*chunk(ch), x);
@@ -722,7 +729,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             }
             const int qe = max((int)(__float_as_uint(top) >> 23) - 127 - 14, kLeastQ);
             const float f = __uint_as_float((uint32_t)(127 - qe) << 23);
-#pragma unroll 1
+#pragma unroll 4
             for (int ch = 0; ch < D / 8; ch++) {
                 float x[8];
                 unpack16(*chunk(ch), x);
