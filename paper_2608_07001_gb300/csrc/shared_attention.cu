@@ -15,11 +15,12 @@
 // the plan (paged_attention.cu, shared_plan.cuh); the prefix (shared_tc.cu, shared_f32.cu); the
 // join.  (A last piece that joins, found with a counter, would save the third, but its reads
 // are one block's: slower from a few pieces on.)  Of short calls they are all there is: 32
-// requests with 200 entries of 8 heads on 4096 quantised ones 32 us, of which 8, 13 and 5
-// and the way from one to the next.
+// requests with 200 entries of 8 heads on 4096 quantised ones 30 us: own entries and plan
+// 12, the prefix 11 from 1 later on, the join what is left.
 //
 // The join: a thread holds four channels of a row, over the parts in order with
-// eight loads of each in flight.  The bf16 kernel's parts lie by channel, so a warp's
+// eight loads of each in flight, or sixteen (32 requests on 4096 quantised entries, 33 parts
+// a row: 31.5 -> 30.2 us).  The bf16 kernel's parts lie by channel, so a warp's
 // lanes are rows; the fp32 kernel's by row.
 #include "quant.cuh"
 #include "shared_plan.cuh"
@@ -40,10 +41,11 @@ __device__ __forceinline__ float held(float m) {
 }
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <typename T, int D>
+// N: parts in flight, 8 or, where a row has more, 16: a batch is the latency of a read.
+template <typename T, int D, int N>
 __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedArgs a, T *out) {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int R = BF ? kShRowsTc : kShRowsF32, N = 8;
+    constexpr int R = BF ? kShRowsTc : kShRowsF32;
     __shared__ float4 v_s[kJoinRows][kJoinC4 + 1];
     __shared__ float m_s[kJoinRows], z_s[kJoinRows];
     next_may_start();
@@ -113,7 +115,9 @@ template <typename T, int D>
 cudaError_t launch_join(const SharedArgs &a, void *out, cudaStream_t s) {
     const int reqs = kJoinRows / (a.c.Hq / a.c.G);
     const dim3 grid((unsigned)(((a.B + reqs - 1) / reqs) * a.c.G), D / 4 / kJoinC4);
-    return launch_overlapped(shared_join_kernel<T, D>, grid, kJoinThreads, 0, s, a, static_cast<T *>(out));
+    const bool many = (int64_t)a.pieces * shared_halves(sizeof(T) == 2) > 8 * (int64_t)a.blocks;       // parts of a row
+    return launch_overlapped(many ? shared_join_kernel<T, D, 16> : shared_join_kernel<T, D, 8>, grid, kJoinThreads, 0, s, a,
+                             static_cast<T *>(out));
 }
 
 struct Layout {
