@@ -12,8 +12,8 @@
 // product whose error is |p| times that of F_i, which two powers, a product and a
 // quotient in fp64 keep below 2^-53 turns (2^-55 found for bases from 1 to 1e7).
 // Its upper 32 bits, rounded to the 24 of a float (2^-26 turns), go to sincospi; of
-// quantised pages 24 of them, and the 8 left turn the result, as an angle that is off
-// moves a key over the middle between two codes, which is 2^-4 of it.  A
+// quantised pages all 32 count (turn_of), as an angle that is off moves a key over the
+// middle between two codes, which is 2^-4 of it.  A
 // thread holds 16 bytes of each half of a row, so the rotation stays in its
 // registers; its sines and cosines serve every row that it takes.
 //
@@ -48,6 +48,21 @@ struct Turns {
         return (i & 7) ? __umul64hi(f, m[i & 7]) : f;
     }
 };
+
+// Sine and cosine of u 2^-32 turns, within 1.4 of a float's last bit, on average 0.27 (rounding alone: 0.25): the quadrant nearest, what is left of it as an angle
+// y = yh + yl of at most pi / 4 in two floats, and the Taylor series of both there (next terms below 2^-29).
+__device__ __forceinline__ void turn_of(unsigned u, float &sn, float &cs) {
+    constexpr float kHi = 0x1.921fb60000000p-30f, kLo = -0x1.777a5c0000000p-55f;          // pi 2^-31
+    const unsigned q = (u + (1u << 29)) >> 30;
+    const int r = (int)(u - (q << 30));
+    const float f = (float)(r & ~63), g = __uint_as_float(0x4b000000u | (unsigned)(r & 63)) - 0x1p23f;       // exact
+    const float yh = f * kHi, yl = fmaf(g, kHi, fmaf(f, kLo, fmaf(f, kHi, -yh))), z = yh * yh;
+    const float ps = z * fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
+    const float pc = z * fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f);
+    const float s = yh + fmaf(yh, ps, yl), c = 1.f + fmaf(-yh, yl, pc);
+    sn = __uint_as_float(__float_as_uint(q & 1 ? c : s) ^ (q & 2) << 30);
+    cs = __uint_as_float(__float_as_uint(q & 1 ? s : c) ^ ((q + 1) & 2) << 30);
+}
 
 // The table of a base, kept per host thread for the calls of a step (d / 2 fp64
 // powers take longer than a launch).
@@ -147,11 +162,7 @@ __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a
         for (int j = 0; j < N; j++) {
             const int hi = (int)(((unsigned long long)p * turns.at(ch * N + j)) >> 32);
             if constexpr (QUANT) {
-                float s0, c0;
-                sincospif((float)(hi & ~255) * 0x1p-31f, &s0, &c0);
-                const float lo = (__uint_as_float(0x4b000000u | (unsigned)(hi & 255)) - 0x1p23f) * 0x1.921fb6p-30f;     // radians
-                sn[j] = fmaf(lo, c0, s0);
-                cs[j] = fmaf(-lo, s0, c0);
+                turn_of((unsigned)hi, sn[j], cs[j]);
             } else {
                 sincospif((float)hi * 0x1p-31f, &sn[j], &cs[j]);
             }
