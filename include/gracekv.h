@@ -633,7 +633,8 @@ gkv_status gracekv_quant_load(const gkv_paged_cache *c, const gkv_paged_scales *
                               void *workspace, void *stream);
 
 /* gracekv_paged_append into quantised pages: keys are rotated in fp32 and
- * quantised from there, rounded once; queries as there. */
+ * quantised from there, rounded once; queries as there, but for the last bit of
+ * their sines, which are the keys'. */
 gkv_status gracekv_quant_append(const gkv_paged_cache *c, const gkv_paged_scales *scales, int32_t l,
                                 const gkv_paged_tokens *t, void *workspace, void *stream);
 
