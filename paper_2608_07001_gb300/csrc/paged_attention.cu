@@ -202,9 +202,9 @@ __device__ __forceinline__ int pa_run_of(long long i, long long total, int nc) {
                               : (int)(((i + 1) * nc + total - 1) / total - 1);
 }
 
-// log m in base 2: finite values stay finite, the others what they are.
-__device__ __forceinline__ float pa_lm2(float lm) {
-    return fabsf(lm) <= FLT_MAX ? fminf(fmaxf(lm * kLog2e, -FLT_MAX), FLT_MAX) : lm;
+// log m in base 2, held within `most` (finite values stay finite), the others what they are.
+__device__ __forceinline__ float pa_lm2(float lm, float most) {
+    return fabsf(lm) <= FLT_MAX ? fminf(fmaxf(lm * kLog2e, -most), most) : lm;
 }
 __device__ __forceinline__ float pa_shift(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -235,7 +235,7 @@ struct PaBf {
     }
 
     __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const uint8_t *, const uint8_t *, const float *lm,
-                                         int count, unsigned units, int box, float scale, bool has_lm) {
+                                         int count, unsigned units, int box, float scale, bool has_lm, float most) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tq = lane & 3;
         const int r0 = warp * 16;
         const int nv = min(16, count - r0);                       // valid entries of the slice
@@ -262,7 +262,7 @@ struct PaBf {
             for (int j = 0; j < 2; j++) {
                 const int e = n * 8 + 2 * tq + j;
                 float v = x[n][j] * scale;
-                if (has_lm) v += pa_lm2(lm[r0 + e]);
+                if (has_lm) v += pa_lm2(lm[r0 + e], most);
                 y[n][j] = e < nv ? v : -INFINITY;
                 mx = fmaxf(mx, y[n][j]);
             }
@@ -390,7 +390,7 @@ struct PaE4 {
     // This warp's NG groups of 16 entries: their chains of products, exponentials and conversions run beside one another.
     static constexpr int NG = C::TE / 64;
     __device__ __forceinline__ void tile(uint32_t kst, uint32_t vst, const uint8_t *ks, const uint8_t *vs, const float *lm,
-                                         int count, unsigned units, int box, float scale, bool has_lm) {
+                                         int count, unsigned units, int box, float scale, bool has_lm, float most) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tq = lane & 3;
         const int mi = lane >> 3, ri = lane & 7;
         int nv[NG], some = 0;            // valid entries of a group
@@ -452,7 +452,7 @@ struct PaE4 {
                     we[g][n][j] = in ? (int)((v2 >> (8 * j)) & 255) - 127 : kOut;
                     if (has_lm) {
                         const float l = j ? l2.y : l2.x;
-                        v += pa_lm2(l);
+                        v += pa_lm2(l, most);
                         if (l == -INFINITY) we[g][n][j] = kOut;
                     }
                     y[g][n][j] = in ? v : -INFINITY;
@@ -554,7 +554,8 @@ struct PaF32 {
     }
 
     __device__ __forceinline__ void tile(const unsigned char *kst, const unsigned char *vst, const uint8_t *ks,
-                                         const uint8_t *vs, const float *lm, int count, unsigned units, int box, bool has_lm) {
+                                         const uint8_t *vs, const float *lm, int count, unsigned units, int box, bool has_lm,
+                                         float most) {
         const int lane = threadIdx.x & 31;
         const bool in = lane < count && ((units >> (lane / box)) & 1u);
         float2 x[GQ];
@@ -586,7 +587,7 @@ struct PaF32 {
 #pragma unroll 8
             for (int ch = 0; ch < D / 4; ch++) product(ch, *reinterpret_cast<const float4 *>(kst + C::at(lane, ch)));
         }
-        const float l2 = has_lm ? pa_lm2(lm[lane]) : 0.f;
+        const float l2 = has_lm ? pa_lm2(lm[lane], most) : 0.f;
 #pragma unroll
         for (int h = 0; h < GQ; h++) {
             const float y = in ? (C::QUANT ? (x[h].x + x[h].y) * kscale : x[h].x + x[h].y) + l2 : -INFINITY;
@@ -851,6 +852,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
         w.qs = qs;
         w.ps = qs + GQ * D + warp * GQ * 32;
     }
+    constexpr float kMost = SHARED ? kShMost : FLT_MAX;      // masks meet those of a shared prefix
     uint32_t it = 0;
     long long vs = sm.first;
     for (int s = sm.s_first; s < S && vs < hi; s++) {
@@ -876,9 +878,9 @@ __global__ void __launch_bounds__(kPaThreads, kPaPerSm)
             const uint8_t *ks = sm.ks[C::QUANT ? st : 0], *vsc = sm.vs[C::QUANT ? st : 0];
             if constexpr (C::BF)
                 w.tile(tc::smem_u32(base), tc::smem_u32(base + C::TB), ks, vsc, sm.lm[st], sm.count[st], sm.units[st], box,
-                       a.scale, a.c.log_m != nullptr);
+                       a.scale, a.c.log_m != nullptr, kMost);
             else
-                w.tile(base, base + C::TB, ks, vsc, sm.lm[st], sm.count[st], sm.units[st], box, a.c.log_m != nullptr);
+                w.tile(base, base + C::TB, ks, vsc, sm.lm[st], sm.count[st], sm.units[st], box, a.c.log_m != nullptr, kMost);
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sm.empty[st]));
         }

@@ -16,8 +16,8 @@ namespace gkv {
 namespace serve {
 
 constexpr int kShSms = 152;
-// log m (base 2) counts up to this size, so that it stays a number beside every scale; masks of the type's lowest
-// value, of which the prefix's and the own parts keep their own roundings, meet there (shared_attention.cu).
+// log m (base 2) counts up to this size, in the prefix and in the own entries, so that it stays a number beside every
+// scale and masks of the type's lowest value meet there.
 constexpr float kShMost = 0x1p40f;
 constexpr int kShRowsTc = 128, kShRowsF32 = 64;        // rows of a part
 constexpr int kShKeysTc = 128, kShKeysF32 = 64;        // keys of a tile

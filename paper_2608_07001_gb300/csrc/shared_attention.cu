@@ -35,10 +35,6 @@ using namespace serve;
 
 constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinC4 = 8;         // rows and groups of 4 channels of a block
 
-// A part's reference, held within kShMost.
-__device__ __forceinline__ float held(float m) {
-    return fabsf(m) >= kShMost * 0.999f && fabsf(m) <= FLT_MAX ? copysignf(kShMost, m) : m;
-}
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // N: parts in flight, 8 or, where a row has more, 16: a batch is the latency of a read.
@@ -65,7 +61,7 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedA
 #pragma unroll
             for (int p = 0; p < N; p++) {
                 const float *q = pre.at + (int64_t)min(p0 + p, pre.count - 1) * pre.step;
-                m[p] = held(__ldcg(q + R * D + row));
+                m[p] = __ldcg(q + R * D + row);
                 z[p] = __ldcg(q + R * (D + 1) + row);
                 x[p] = __ldcg(reinterpret_cast<const float4 *>(q) + (BF ? c4 * R + row : row * (D / 4) + c4));
             }
@@ -99,8 +95,7 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const SharedA
     const int r2 = tid / kJoinC4, k2 = tid % kJoinC4, b2 = b0 + r2 / gq;
     if (r2 / gq >= reqs || b2 >= a.B) return;
     const int64_t at = (int64_t)b2 * a.c.Hq + g * gq + r2 % gq;
-    float2 own = __ldcg(a.plan.own_mz + at);
-    own.x = held(own.x);
+    const float2 own = __ldcg(a.plan.own_mz + at);
     const bool none = own.x == -INFINITY && own.y == 0.f;
     const float m1 = m_s[r2], z1 = z_s[r2], mx = fmaxf(m1, none ? -INFINITY : own.x), sh = shift_of(mx);
     float4 x = v_s[r2][k2], y = make_float4(0.f, 0.f, 0.f, 0.f);

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kThreads, 2) shared_f32_kernel(const SharedArg
             const Paged look{nullptr, nullptr, nullptr, a.table, nullptr, 0, 0, 0, 0, a.c.page_size, a.c.max_pages, a.c.n_pages};
             const int row = e < len ? (int)entry_row(look, seq, e, a.status) : -1;
             float lm = row >= 0 && a.c.log_m ? a.c.log_m[row] : 0.f;
-            if (fabsf(lm) <= FLT_MAX) lm = fminf(fmaxf(lm * kLog2e, -FLT_MAX), FLT_MAX);
+            if (fabsf(lm) <= FLT_MAX) lm = fminf(fmaxf(lm * kLog2e, -kShMost), kShMost);
             row_s[j & 1][tid] = row;
             bias_s[j & 1][tid] = lm;
         }

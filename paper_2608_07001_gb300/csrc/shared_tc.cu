@@ -71,6 +71,7 @@ constexpr int NBIAS = 4;                                   // slots of the K ste
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
 constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
 constexpr int kBiased = 1, kSpecial = 2;                   // of a tile: log m; entries that are not there
+constexpr int kLowest = 1, kLargest = 2;                   // of a part: every log m at -kShMost; some at kShMost
 
 template <int D, bool QUANT>
 struct Cfg {
@@ -95,6 +96,7 @@ struct Bars {
     alignas(16) uint8_t ke[QUANT ? NBIAS : 1][QUANT ? NK : 16], ve[QUANT ? NBIAS : 1][QUANT ? NK : 16];       // scale bytes
     float qscale[2][QUANT ? 128 : 1];  // 2^q
     int kind[NBIAS], ktop[NBIAS], vtop[NBIAS];             // k, E
+    int limit[2];                      // of the part that a row tile or, of one row tile, a warpgroup leaves (kLowest, kLargest in the low bits)
     uint32_t tbase;
     int abort;
 };
@@ -418,6 +420,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 }
             }
             if (live) {
+                // log m at the limit has come through the product, its scale and back: off by a few last bits, which are
+                // 2^17 there.  The reference becomes what the own entries and the other parts have; of other logits, of
+                // any size, it stays as it is.
+                const int limit = b.limit[two ? 0 : i];
+                if ((limit & (m < 0.f ? kLowest : kLargest)) && fabsf(fabsf(m) - kShMost) <= kShMost * 0x1p-20f) m = copysignf(kShMost, m);
                 pp[(size_t)kShRowsTc * D + r] = m;
                 pp[(size_t)kShRowsTc * (D + 1) + r] = z;
             }
@@ -556,7 +563,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 }
             };
             const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
-            int top_ve = kNoScale;
+            int top_ve = kNoScale, limits = kLowest | kLowest << 2;
             Four cur = load(key_row(0));
 #pragma unroll 1
             for (int i = 1; i < kAhead; i++) fetch(key_row(i));
@@ -581,6 +588,15 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
                 }
                 const bool special = __any_sync(0xffffffffu, count < 4);
+                bool lowest = true, largest = false;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    lowest = lowest && (!in[i] || v[i] <= -most);
+                    largest = largest || (in[i] && v[i] >= most);
+                }
+                const int part = two ? 0 : j & 1;
+                if (!__all_sync(0xffffffffu, lowest)) limits &= ~(kLowest << 2 * part);
+                if (__any_sync(0xffffffffu, largest)) limits |= kLargest << 2 * part;
                 if constexpr (QUANT) {                   // the rows' threads make the rest of it
                     int kt = kLeastK, vt = kNoScale;
 #pragma unroll
@@ -603,7 +619,10 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     for (int i = 0; i < 4; i++) put_aug(aug + sl * AUG, lane * 4 + i, three_parts(v[i]));
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                if (lane == 0) b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
+                if (lane == 0) {
+                    b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
+                    b.limit[part] = limits >> 2 * part;
+                }
                 // the key rows that are not there are 0 before the product
                 if (special && !QUANT) ok = __all_sync(0xffffffffu, wait(&b.kfix[j % NFIX], (j / NFIX) & 1, b, a.status));
                 __syncwarp();
