@@ -699,8 +699,9 @@ gkv_status gracekv_paged_status(void *workspace, void *stream);
  * Values: as gracekv_paged_attention, but for bf16 rows the weights of the
  * prefix's entries are rounded once for the value product (their sum is not): to bf16,
  * over quantised pages to f16, where values of less than 2^-33 of the largest one
- * that has a weight count 0, and queries of less than 2^-24 lose bits.  A
- * log m of more than 2^40 ln 2 in size counts as that.
+ * that has a weight count 0.  Keys count whatever their scales, and over quantised
+ * pages logits of fp32 queries above 2^100 in size are open.  A log m of more than
+ * 2^40 ln 2 in size counts as that.
  */
 
 /* Bytes of the device workspace: a function of both caches' L, B, G, Hq, d and

@@ -45,6 +45,9 @@
 // largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
 // largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M) has 11 bits,
 // at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.
+// Where that would cost keys their bits (k_e that lie further apart in a tile) or log m beside
+// q and k is no number (they are beyond 2^30 and 2^40), K' = code and the softmax warps make
+// y = S 2^q 2^(k_e) c + log m from the scores themselves, with 128 reads of shared memory.
 #include "quant.cuh"
 #include "shared.cuh"
 #include "tc.cuh"
@@ -62,7 +65,11 @@ constexpr int kWarpTma = 8, kWarpMma = 9, kWarpBias = 11, kWarpConv = 12;
 constexpr float kLazy = 8.f;                               // log2 of the growth a reference lets pass
 constexpr float kHead = 7.f;                               // f16: log2 of where the weights start
 constexpr int kNoScale = -120;                             // E before any entry
-constexpr int kLeastQ = -30, kLeastK = -40;                // least q and k, so that kShMost 2^-q 2^-k is a number
+constexpr int kLeastQ = -100;                              // least q
+// How large q and k may be for log m to join in the product: kShMost 2^-q 2^-k is a number and its last bits are too.
+// kSpread: how far a key's scale may be below the tile's largest, its code exact in f16 (a key of zeros has the least
+// scale there is, and its tile goes the longer way).
+constexpr int kMostQ = 30, kMostK = 40, kSpread = 15;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint32_t kNapNs = 20000;                         // a look at a barrier may last that long
 constexpr int NK = kShKeysTc;                              // keys of a tile
@@ -70,7 +77,7 @@ constexpr int kAhead = 4;                                  // tiles that the wor
 constexpr int NBIAS = 4;                                   // slots of the K step of log m
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
 constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
-constexpr int kBiased = 1, kSpecial = 2;                   // of a tile: log m; entries that are not there
+constexpr int kBiased = 1, kSpecial = 2, kFar = 4;         // of a tile: log m; entries that are not there; keys by their own scales
 constexpr int kLowest = 1, kLargest = 2;                   // of a part: every log m at -kShMost; some at kShMost
 
 template <int D, bool QUANT>
@@ -96,6 +103,7 @@ struct Bars {
     alignas(16) uint8_t ke[QUANT ? NBIAS : 1][QUANT ? NK : 16], ve[QUANT ? NBIAS : 1][QUANT ? NK : 16];       // scale bytes
     float qscale[2][QUANT ? 128 : 1];  // 2^q
     int kind[NBIAS], ktop[NBIAS], vtop[NBIAS];             // k, E
+    int far[2];                        // of a row tile: q of some row is beyond kMostQ
     int limit[2];                      // of the part that a row tile or, of one row tile, a warpgroup leaves (kLowest, kLargest in the low bits)
     uint32_t tbase;
     int abort;
@@ -189,6 +197,25 @@ __device__ __forceinline__ void put_aug(unsigned char *base, int r, uint2 v) {
     *reinterpret_cast<uint4 *>(base + r * 32 + (flip ^ 1) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// The scores of a row (TMEM, 128 columns) become base-2 logits in place: those of which log m could not be a part of the
+// product, with each key's own scale (own) or the tile's, byte.  As the attention over quantised pages makes them: 2^(q + k_e)
+// where it is a number.
+__device__ __noinline__ void far_logits(uint32_t ts, const float *lm, const uint8_t *ke, bool own, int byte, int qe, float c) {
+#pragma unroll 1
+    for (int h = 0; h < NK / 32; h++) {
+        uint32_t x[32];
+        tc::tmem_ld32_async(ts + 32 * h, x);
+        tc::tmem_wait_ld(x);
+#pragma unroll
+        for (int e = 0; e < 32; e++) {
+            const int t = min(max(qe + (own ? (int)ke[32 * h + e] : byte), 1), 254);
+            x[e] = __float_as_uint(__uint_as_float(x[e]) * c * __uint_as_float((uint32_t)t << 23) + lm[32 * h + e] * c);
+        }
+        tc::tmem_st(ts + 32 * h, x);
+    }
+    tc::tmem_wait_st();
+}
+
 template <int D, bool QUANT>
 __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
     shared_tc_kernel(const SharedArgs a, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -261,7 +288,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         }
         for (int i = 0; i < 2; i++) tc::mbar_init(tc::smem_u32(&b.turn[i]), 1);
         tc::mbar_init(tc::smem_u32(&b.fin), 2);
-        b.abort = 0;
+        b.abort = b.far[0] = b.far[1] = 0;
         tc::fence_barrier_init();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -294,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         const bool work = __any_sync(0xffffffffu, live);
         const uint32_t ts = tb + ((uint32_t)(q * 32) << 16) + i * NK, to = tb + ((uint32_t)(q * 32) << 16) + 2 * NK + i * D;
         const int start = two ? 0 : i;
-        float c = a.scale;
+        const float c = a.scale;
         int ve = kNoScale;                               // E
         float m = -INFINITY, z = 0.f;                    // the reference and the sum of the weights
         bool ok = true, any = false;
@@ -308,9 +335,14 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int ve_new = kNoScale;
             if (QUANT) {
                 ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
-                if (j == start) c *= b.qscale[two ? i : 0][QUANT ? r : 0];
-                cs = c * __uint_as_float((uint32_t)(127 + b.ktop[sl]) << 23);
+                const float qs = b.qscale[two ? i : 0][QUANT ? r : 0];
+                cs = c * qs * __uint_as_float((uint32_t)(127 + b.ktop[sl]) << 23);
                 ve_new = b.vtop[sl];
+                if (work && ((b.kind[sl] & kFar) || b.far[two ? i : 0])) {
+                    tc::tc_fence_after();
+                    far_logits(ts, b.lm[sl], b.ke[sl], b.kind[sl] & kFar, b.ktop[sl] + 127, (int)(__float_as_uint(qs) >> 23) - 127, c);
+                    cs = 1.f;
+                }
             }
             __syncwarp();
             if (QUANT && lane == 0) tc::mbar_arrive(tc::smem_u32(&b.bempty[sl]));
@@ -597,15 +629,21 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 const int part = two ? 0 : j & 1;
                 if (!__all_sync(0xffffffffu, lowest)) limits &= ~(kLowest << 2 * part);
                 if (__any_sync(0xffffffffu, largest)) limits |= kLargest << 2 * part;
+                bool far = false;
                 if constexpr (QUANT) {                   // the rows' threads make the rest of it
-                    int kt = kLeastK, vt = kNoScale;
+                    int kt = kNoScale, kb = kNoScale + 255, vt = kNoScale;
 #pragma unroll
                     for (int i = 0; i < 4; i++)
                         if (in[i]) {
-                            kt = max(kt, min((int)((f.ks >> (8 * i)) & 255) - 127, 119));
+                            const int k = min((int)((f.ks >> (8 * i)) & 255) - 127, 119);
+                            kt = max(kt, k);
+                            kb = min(kb, k);
                             vt = max(vt, min((int)((f.vs >> (8 * i)) & 255) - 127, 119));
                         }
                     kt = __reduce_max_sync(0xffffffffu, kt);
+                    kb = __reduce_min_sync(0xffffffffu, kb);
+                    if (kb > kt) kt = 0;                 // no key that has a weight
+                    else far = kt > kMostK || kt < -kMostK || kb < kt - kSpread;
                     top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
                     *reinterpret_cast<float4 *>(&b.lm[sl][lane * 4]) = make_float4(v[0], v[1], v[2], v[3]);
                     *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks;
@@ -620,7 +658,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 if (lane == 0) {
-                    b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
+                    b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0) | (far ? kFar : 0);
                     b.limit[part] = limits >> 2 * part;
                 }
                 // the key rows that are not there are 0 before the product
@@ -681,7 +719,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
 #pragma unroll
                             for (int x = 0; x < 4; x++)
                                 tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
-                        if (kind) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
+                        if (kind && !(QUANT && ((kind & kFar) || b.far[qi]))) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
                         tc::mma_commit(tc::smem_u32(&b.sfull[i]));
                         tc::mma_commit(tc::smem_u32(&b.kempty[at]));
                         tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
@@ -746,7 +784,9 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 unpack16(*chunk(ch), x);
                 top = fmaxf(top, top_of(x));
             }
-            const int qe = max((int)(__float_as_uint(top) >> 23) - 127 - 14, kLeastQ);
+            const int qe = top > 0.f ? max((int)(__float_as_uint(top) >> 23) - 127 - 14, kLeastQ) : 0;
+            const bool far = r / gq < tpt && (i * tpt + r / gq) < nb && abs(qe) > kMostQ;          // (the other rows may be anything)
+            if (far) b.far[i] = 1;
             const float f = __uint_as_float((uint32_t)(127 - qe) << 23);
 #pragma unroll 4
             for (int ch = 0; ch < D / 8; ch++) {
@@ -778,10 +818,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             // codes of entries that are not there may be anything, NaN too; those without a weight have a scale of 0
             const float lm = b.lm[QUANT ? sl : 0][QUANT ? r : 0];
             const int top = keys ? b.ktop[sl] : b.vtop[sl], kind = b.kind[sl];
-            const int e = min((int)(keys ? b.ke : b.ve)[QUANT ? sl : 0][QUANT ? r : 0] - 127, 119) - top;
+            const bool far = keys && (kind & kFar);      // codes as they are
+            const int e = far ? 0 : min((int)(keys ? b.ke : b.ve)[QUANT ? sl : 0][QUANT ? r : 0] - 127, 119) - top;
             const __half2 s = __half2half2(lm != -INFINITY ? half_pow2(e) : __ushort_as_half(0));
             const bool there = lm != -INFINITY || !(kind & kSpecial);
-            if (keys && kind) put_aug(aug + sl * AUG, r, three_parts(lm * __uint_as_float((uint32_t)(127 - top) << 23)));
+            if (keys && kind && !far) put_aug(aug + sl * AUG, r, three_parts(lm * __uint_as_float((uint32_t)(127 - top) << 23)));
             const unsigned char *src = raw + at * C::RAW + r * D;
             unsigned char *dst = ring + to * C::TILE + r * 128;
 #pragma unroll
