@@ -78,6 +78,7 @@ constexpr int NBIAS = 4;                                   // slots of the K ste
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
 constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
 constexpr int kBiased = 1, kSpecial = 2, kFar = 4;         // of a tile: log m; entries that are not there; keys by their own scales
+constexpr int kGone = 255;                                 // scale byte of an entry that is not there: one that no row has
 constexpr int kLowest = 1, kLargest = 2;                   // of a part: every log m at -kShMost; some at kShMost
 
 template <int D, bool QUANT>
@@ -646,8 +647,9 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     else far = kt > kMostK || kt < -kMostK || kb < kt - kSpread;
                     top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
                     *reinterpret_cast<float4 *>(&b.lm[sl][lane * 4]) = make_float4(v[0], v[1], v[2], v[3]);
-                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks;
-                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = f.vs;
+                    const uint32_t gone = count >= 4 ? 0u : ~0u << 8 * max(count, 0);         // bytes of kGone
+                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks | gone;
+                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = f.vs | gone;
                     if (lane == 0) {
                         b.ktop[sl] = kt;
                         b.vtop[sl] = top_ve;
@@ -815,13 +817,14 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             if (!ok) break;
             from.step(nr);
             into.step(slots);
-            // codes of entries that are not there may be anything, NaN too; those without a weight have a scale of 0
+            // codes of entries that are not there may be anything, NaN too; those without a weight have a scale of 0, and a
+            // NaN of theirs stays
             const float lm = b.lm[QUANT ? sl : 0][QUANT ? r : 0];
             const int top = keys ? b.ktop[sl] : b.vtop[sl], kind = b.kind[sl];
             const bool far = keys && (kind & kFar);      // codes as they are
-            const int e = far ? 0 : min((int)(keys ? b.ke : b.ve)[QUANT ? sl : 0][QUANT ? r : 0] - 127, 119) - top;
+            const int byte = (keys ? b.ke : b.ve)[QUANT ? sl : 0][QUANT ? r : 0], e = far ? 0 : min(byte - 127, 119) - top;
             const __half2 s = __half2half2(lm != -INFINITY ? half_pow2(e) : __ushort_as_half(0));
-            const bool there = lm != -INFINITY || !(kind & kSpecial);
+            const bool there = byte != kGone;
             if (keys && kind && !far) put_aug(aug + sl * AUG, r, three_parts(lm * __uint_as_float((uint32_t)(127 - top) << 23)));
             const unsigned char *src = raw + at * C::RAW + r * D;
             unsigned char *dst = ring + to * C::TILE + r * 128;
