@@ -70,6 +70,7 @@ constexpr int kLeastQ = -100;                              // least q
 // kSpread: how far a key's scale may be below the tile's largest, its code exact in f16 (a key of zeros has the least
 // scale there is, and its tile goes the longer way).
 constexpr int kMostQ = 30, kMostK = 40, kSpread = 15;
+constexpr int kOwn = -127;                                 // k of a tile whose keys keep their own scales (a number's exponent, of 0)
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint32_t kNapNs = 20000;                         // a look at a barrier may last that long
 constexpr int NK = kShKeysTc;                              // keys of a tile
@@ -77,9 +78,9 @@ constexpr int kAhead = 4;                                  // tiles that the wor
 constexpr int NBIAS = 4;                                   // slots of the K step of log m
 constexpr uint32_t AUG = NK * 32;                          // its bytes: 16 elements a key
 constexpr int NFIX = 8;                                    // more than the tiles that a ring holds
-constexpr int kBiased = 1, kSpecial = 2, kFar = 4;         // of a tile: log m; entries that are not there; keys by their own scales
+constexpr int kBiased = 1, kSpecial = 2, kFar = 4;         // of a tile: log m; entries that are not there; k = kOwn
 constexpr int kGone = 255;                                 // scale byte of an entry that is not there: one that no row has
-constexpr int kLowest = 1, kLargest = 2;                   // of a part: every log m at -kShMost; some at kShMost
+constexpr int kLowest = 1, kLargest = 2;                   // of a piece: every log m at -kShMost; some at kShMost
 
 template <int D, bool QUANT>
 struct Cfg {
@@ -105,7 +106,7 @@ struct Bars {
     float qscale[2][QUANT ? 128 : 1];  // 2^q
     int kind[NBIAS], ktop[NBIAS], vtop[NBIAS];             // k, E
     int far[2];                        // of a row tile: q of some row is beyond kMostQ
-    int limit[2];                      // of the part that a row tile or, of one row tile, a warpgroup leaves (kLowest, kLargest in the low bits)
+    int limit;                         // of the piece
     uint32_t tbase;
     int abort;
 };
@@ -199,9 +200,10 @@ __device__ __forceinline__ void put_aug(unsigned char *base, int r, uint2 v) {
 }
 
 // The scores of a row (TMEM, 128 columns) become base-2 logits in place: those of which log m could not be a part of the
-// product, with each key's own scale (own) or the tile's, byte.  As the attention over quantised pages makes them: 2^(q + k_e)
+// product, with each key's own scale (kOwn) or the tile's.  As the attention over quantised pages makes them: 2^(q + k_e)
 // where it is a number.
-__device__ __noinline__ void far_logits(uint32_t ts, const float *lm, const uint8_t *ke, bool own, int byte, int qe, float c) {
+__device__ __noinline__ void far_logits(uint32_t ts, const float *lm, const uint8_t *ke, int kt, float two_q, float c) {
+    const int qe = (int)(__float_as_uint(two_q) >> 23) - 127;
 #pragma unroll 1
     for (int h = 0; h < NK / 32; h++) {
         uint32_t x[32];
@@ -209,7 +211,7 @@ __device__ __noinline__ void far_logits(uint32_t ts, const float *lm, const uint
         tc::tmem_wait_ld(x);
 #pragma unroll
         for (int e = 0; e < 32; e++) {
-            const int t = min(max(qe + (own ? (int)ke[32 * h + e] : byte), 1), 254);
+            const int t = min(max(qe + (kt == kOwn ? (int)ke[32 * h + e] : kt + 127), 1), 254);
             x[e] = __float_as_uint(__uint_as_float(x[e]) * c * __uint_as_float((uint32_t)t << 23) + lm[32 * h + e] * c);
         }
         tc::tmem_st(ts + 32 * h, x);
@@ -322,7 +324,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
         const bool work = __any_sync(0xffffffffu, live);
         const uint32_t ts = tb + ((uint32_t)(q * 32) << 16) + i * NK, to = tb + ((uint32_t)(q * 32) << 16) + 2 * NK + i * D;
         const int start = two ? 0 : i;
-        const float c = a.scale;
+        float c = a.scale;
+        bool far = false;
         int ve = kNoScale;                               // E
         float m = -INFINITY, z = 0.f;                    // the reference and the sum of the weights
         bool ok = true, any = false;
@@ -336,12 +339,16 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int ve_new = kNoScale;
             if (QUANT) {
                 ok = wait(&b.bfull[sl], (j / NBIAS) & 1, b, a.status) && ok;
-                const float qs = b.qscale[two ? i : 0][QUANT ? r : 0];
-                cs = c * qs * __uint_as_float((uint32_t)(127 + b.ktop[sl]) << 23);
+                if (j == start) {
+                    c *= b.qscale[two ? i : 0][QUANT ? r : 0];
+                    far = b.far[two ? i : 0];
+                }
+                const int kt = b.ktop[sl];
+                cs = c * __uint_as_float((uint32_t)(127 + kt) << 23);
                 ve_new = b.vtop[sl];
-                if (work && ((b.kind[sl] & kFar) || b.far[two ? i : 0])) {
+                if (work && (far || kt == kOwn)) {
                     tc::tc_fence_after();
-                    far_logits(ts, b.lm[sl], b.ke[sl], b.kind[sl] & kFar, b.ktop[sl] + 127, (int)(__float_as_uint(qs) >> 23) - 127, c);
+                    far_logits(ts, b.lm[sl], b.ke[sl], kt, b.qscale[two ? i : 0][QUANT ? r : 0], a.scale);
                     cs = 1.f;
                 }
             }
@@ -456,8 +463,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 // log m at the limit has come through the product, its scale and back: off by a few last bits, which are
                 // 2^17 there.  The reference becomes what the own entries and the other parts have; of other logits, of
                 // any size, it stays as it is.
-                const int limit = b.limit[two ? 0 : i];
-                if ((limit & (m < 0.f ? kLowest : kLargest)) && fabsf(fabsf(m) - kShMost) <= kShMost * 0x1p-20f) m = copysignf(kShMost, m);
+                if ((b.limit & (m < 0.f ? kLowest : kLargest)) && fabsf(fabsf(m) - kShMost) <= kShMost * 0x1p-20f) m = copysignf(kShMost, m);
                 pp[(size_t)kShRowsTc * D + r] = m;
                 pp[(size_t)kShRowsTc * (D + 1) + r] = z;
             }
@@ -596,7 +602,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 }
             };
             const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
-            int top_ve = kNoScale, limits = kLowest | kLowest << 2;
+            int top_ve = kNoScale;
+            float piece_top = -INFINITY;
             Four cur = load(key_row(0));
 #pragma unroll 1
             for (int i = 1; i < kAhead; i++) fetch(key_row(i));
@@ -621,15 +628,11 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
                 }
                 const bool special = __any_sync(0xffffffffu, count < 4);
-                bool lowest = true, largest = false;
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    lowest = lowest && (!in[i] || v[i] <= -most);
-                    largest = largest || (in[i] && v[i] >= most);
-                }
-                const int part = two ? 0 : j & 1;
-                if (!__all_sync(0xffffffffu, lowest)) limits &= ~(kLowest << 2 * part);
-                if (__any_sync(0xffffffffu, largest)) limits |= kLargest << 2 * part;
+                // the piece's largest log m so far, by lane (of the softmax warps' two parts of one row tile together: an
+                // entry above the lowest in one of them has all of the weight beside the other's lowest)
+                piece_top = fmaxf(max3(piece_top, v[0], v[1]), fmaxf(v[2], v[3]));
+                if (j == n - 1)
+                    b.limit = (__any_sync(0xffffffffu, piece_top > -most) ? 0 : kLowest) | (__any_sync(0xffffffffu, piece_top >= most) ? kLargest : 0);
                 bool far = false;
                 if constexpr (QUANT) {                   // the rows' threads make the rest of it
                     int kt = kNoScale, kb = kNoScale + 255, vt = kNoScale;
@@ -642,16 +645,18 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                             vt = max(vt, min((int)((f.vs >> (8 * i)) & 255) - 127, 119));
                         }
                     kt = __reduce_max_sync(0xffffffffu, kt);
-                    kb = __reduce_min_sync(0xffffffffu, kb);
-                    if (kb > kt) kt = 0;                 // no key that has a weight
-                    else far = kt > kMostK || kt < -kMostK || kb < kt - kSpread;
+                    far = __any_sync(0xffffffffu, kb < kt - kSpread) || abs(kt) > kMostK;
                     top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
                     *reinterpret_cast<float4 *>(&b.lm[sl][lane * 4]) = make_float4(v[0], v[1], v[2], v[3]);
-                    const uint32_t gone = count >= 4 ? 0u : ~0u << 8 * max(count, 0);         // bytes of kGone
-                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks | gone;
-                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = f.vs | gone;
+                    uint32_t ks = f.ks, vs = f.vs;
+                    if (count < 4) {                     // bytes of kGone
+                        ks |= ~0u << 8 * max(count, 0);
+                        vs |= ~0u << 8 * max(count, 0);
+                    }
+                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = ks;
+                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = vs;
                     if (lane == 0) {
-                        b.ktop[sl] = kt;
+                        b.ktop[sl] = far ? kOwn : kt;
                         b.vtop[sl] = top_ve;
                     }
                 } else if (a.c.log_m || special) {
@@ -659,10 +664,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     for (int i = 0; i < 4; i++) put_aug(aug + sl * AUG, lane * 4 + i, three_parts(v[i]));
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                if (lane == 0) {
-                    b.kind[sl] = (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0) | (far ? kFar : 0);
-                    b.limit[part] = limits >> 2 * part;
-                }
+                // (of keys with their own scales the rows' threads make that, too)
+                if (lane == 0) b.kind[sl] = far ? kFar : (a.c.log_m ? kBiased : 0) | (special ? kSpecial : 0);
                 // the key rows that are not there are 0 before the product
                 if (special && !QUANT) ok = __all_sync(0xffffffffu, wait(&b.kfix[j % NFIX], (j / NFIX) & 1, b, a.status));
                 __syncwarp();
@@ -681,6 +684,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             const uint64_t ad = aug_desc(tc::smem_u32(aug)), qad = aug_desc(tc::smem_u32(qaug + (QUANT ? qi : 0) * AUG));
             const uint32_t ts = tb + i * NK, to = tb + 2 * NK + i * D;
             ok = start >= n || wait(QUANT ? &b.qready[qi] : &b.qfull[qi], 0, b, a.status);
+            const int joins = QUANT && b.far[qi] ? 0 : kBiased | kSpecial;       // kinds of tiles whose log m joins in the product
             // Both warps walk both rings in their order and release every slot, whoever uses it: a warp that passed over a
             // slot's phase could take the one after it for landed.
             Turn kt(0), vt(0);
@@ -721,7 +725,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
 #pragma unroll
                             for (int x = 0; x < 4; x++)
                                 tc::mma_bf16_lo(ts, qd + cb * (128 * 128 >> 4) + 2 * x, ka + cb * (NK * 128 >> 4) + 2 * x, idS, (cb | x) != 0);
-                        if (kind && !(QUANT && ((kind & kFar) || b.far[qi]))) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
+                        if (kind & joins) tc::mma_bf16(ts, qad, ad + sl * (AUG >> 4), idA, 1);
                         tc::mma_commit(tc::smem_u32(&b.sfull[i]));
                         tc::mma_commit(tc::smem_u32(&b.kempty[at]));
                         tc::mma_commit(tc::smem_u32(&b.bempty[sl]));
