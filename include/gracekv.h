@@ -696,10 +696,10 @@ gkv_status gracekv_paged_status(void *workspace, void *stream);
  * below the end of an earlier one whose own words fit, are left out (their requests have no prefix)
  * and gracekv_shared_status reports GKV_EINVAL, as it does for pages and lengths
  * that are not followed; the others are computed.
- * Values: as gracekv_paged_attention, but for bf16 rows the weights of the
- * prefix's entries are rounded once for the value product (their sum is not): to bf16,
- * over quantised pages to f16, where values of less than 2^-33 of the largest one
- * that has a weight count 0.  Keys count whatever their scales, and over quantised
+ * Values: as gracekv_paged_attention, but for bf16 rows over a quantised prefix
+ * its entries' weights are rounded to f16 for the value product (their sum is
+ * not), and values of less than 2^-33 of the largest one that has a weight count 0.
+ * Keys count whatever their scales, and over quantised
  * pages logits of fp32 queries above 2^100 in size are open.  A log m of more than
  * 2^40 ln 2 in size counts as that.
  */

@@ -22,11 +22,11 @@
 // products of 128^3; many: by the chain product, exponentials, product of a row tile, of
 // which TMEM holds two.  us a key tile and SM, pages of 64 entries, log m; in L2 / from HBM:
 //                      one row tile     two row tiles
-//   bf16       d = 64  0.79 / 1.03      1.44 / 1.45
-//              d = 128 1.19 / 1.59      1.54 / 1.82       (64 KB in 1.59 us: 6.3 TB/s of all SMs)
-//   quantised  d = 64  0.95 / 1.05      1.68 / 1.71
-//              d = 128 1.43 / 1.51      2.20 / 2.52
-// Pages of 16 entries, each box of which is a copy of its own: 1.1 to 1.3, 2.0 to 2.2 (bf16, d = 128) and as above.
+//   bf16       d = 64  0.97 / 1.10      1.72 / 1.76
+//              d = 128 1.33 / 1.61      2.18 / 2.28       (64 KB in 1.61 us: 6.2 TB/s of all SMs)
+//   quantised  d = 64  1.02 / 1.12      1.74 / 1.78
+//              d = 128 1.39 / 1.56      2.22 / 2.54
+// Pages of 16 entries, each box of which is a copy of its own: 1.3 to 1.4, 2.1 to 2.4 (bf16, d = 128) and as above.
 // A piece takes about 10 us beside its tiles.
 //
 // Warps: 0-3 and 4-7 softmax (a thread a row), 8 looks pages up and issues TMA
@@ -34,7 +34,12 @@
 // and zeroes rows of entries that are not there, which are stale memory (0 times
 // what is not finite is NaN), 9 and 10 issue the MMAs of row tile 0 and 1, 11 makes
 // the K step of log m.
-// P is rounded once, as A and B of a product have one type; Z is not.
+// A and B of a product have one type, so P goes as its bf16 part and the remainder's, two
+// parts (2^-16 of a weight, as the own entries'), each half of them in the columns of its own
+// scores.  Rounded once, a key tile of two row tiles took 1.54 us instead of 2.18 (d = 128) and
+// 1.44 instead of 1.72 (d = 64), of one 1.19 instead of 1.33 and 0.79 instead of 0.97, 1.59
+// instead of 1.61 from HBM; but outputs were 2.2 to 2.4e-3 from 64 bits, where rounding them
+// makes 1.65e-3.
 //
 // Quantised pages: codes come through a ring of their own, and two warpgroups more
 // (12-15 keys, 16-19 values) write the tiles as f16, 3 clocks for two codes (as bf16 with their scale 8,
@@ -43,7 +48,7 @@
 // k the largest k_e of the tile, E the largest v_e so far, of entries that have a
 // weight at all (no -inf), q the power of two that brings a row's queries into f16 (its
 // largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
-// largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M) has 11 bits,
+// largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M), rounded once, has 11 bits,
 // at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.
 // Where that would cost keys their bits (k_e that lie further apart in a tile) or log m beside
 // q and k is no number (they are beyond 2^30 and 2^40), K' = code and the softmax warps make
@@ -91,6 +96,7 @@ struct Cfg {
     static constexpr int KS = QUANT ? (D == 128 ? 1 : 3) : (D == 128 ? 2 : 5), VS = QUANT && D == 128 ? 2 : KS;
     // ring slots of codes, of either kind, beside two row tiles of queries; one row tile leaves room for one more of each
     static constexpr int NR = QUANT ? (D == 128 ? 1 : 3) : 0;
+    static constexpr int PW = QUANT ? 32 : 64;             // TMEM columns of 64 keys' weights: one part or two
     static constexpr int NQA = QUANT ? 2 : 1;              // left sides of the K step: by row, or the same for all
     static constexpr size_t SMEM = (2 + KS + VS) * (size_t)TILE + (NBIAS + NQA) * (size_t)AUG + 2 * NR * (size_t)RAW;
     static constexpr int THREADS = QUANT ? 640 : 384;
@@ -401,7 +407,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                 }
                 const float sh = m == -INFINITY ? 0.f : -m;
                 float2 acc = make_float2(0.f, 0.f);
-                uint32_t pk[32];
+                uint32_t pk[32], rest[QUANT ? 1 : 32];
 #pragma unroll 1
                 for (int h = 0; h < 2; h++) {
                     tc::tmem_ld32_async(ts + 64 * h, x[0]);
@@ -416,9 +422,17 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                                                      __fadd_rn(__fmul_rn(__uint_as_float(x[e / 16][(2 * e & 31) + 1]), cs), sh));
                         const float2 w = make_float2(tc::ex2(y.x), tc::ex2(y.y));
                         acc = __fadd2_rn(acc, w);
-                        pk[e] = QUANT ? f16x2_of(w.x, w.y) : bf16x2_of(w.x, w.y);
+                        if constexpr (QUANT) {
+                            pk[e] = f16x2_of(w.x, w.y);
+                        } else {
+                            pk[e] = bf16x2_of(w.x, w.y);
+                            const float2 r = __ffma2_rn(make_float2(__uint_as_float(pk[e] << 16), __uint_as_float(pk[e] & 0xffff0000u)),
+                                                        make_float2(-1.f, -1.f), w);
+                            rest[e] = bf16x2_of(r.x, r.y);
+                        }
                     }
-                    tc::tmem_st(ts + 32 * h, pk);
+                    tc::tmem_st(ts + C::PW * h, pk);
+                    if constexpr (!QUANT) tc::tmem_st(ts + C::PW * h + 32, rest);
                     hand(h);
                 }
                 z += acc.x + acc.y;
@@ -692,8 +706,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             unsigned fixed = 0;                          // bit j % 32: tile j has rows that are not there
             auto mine = [&](int j) { return two || (j & 1) == i; };
             // Two row tiles: the warps issue O(j), S(j + 1) in turn, so that one row tile's exponentials run beside the
-            // other's products.  Issued as they come, both wait for both: bf16 1.87 us a key tile of d = 128 instead of
-            // 1.53, 1.63 of d = 64 instead of 1.44; quantised d = 64 1.80, 1.69.  Quantised d = 128 waits for its keys,
+            // other's products.  Issued as they come, both wait for both: bf16 2.40 us a key tile of d = 128 instead of
+            // 2.20, 1.95 of d = 64 instead of 1.72; quantised d = 64 1.88, 1.74.  Quantised d = 128 waits for its keys,
             // which have one slot: 2.41, in turn 2.50.
             uint32_t tp = i ^ 1;
             const bool turns = two && !(QUANT && D == 128);
@@ -747,8 +761,8 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                         tc::tc_fence_after();
                         if (ok && one) {
 #pragma unroll
-                            for (int x = k * 4; x < k * 4 + 4; x++)
-                                tc::mma_bf16_ts_lo(to, ts + x * 8, va + x * (16 * 128 >> 4), idO, j != start || x != 0);
+                            for (int x = 0; x < C::PW / 8; x++)
+                                tc::mma_bf16_ts_lo(to, ts + k * C::PW + x * 8, va + (k * 4 + x % 4) * (16 * 128 >> 4), idO, j != start || k + x != 0);
                         }
                     }
                     pp ^= 1;
