@@ -325,9 +325,10 @@ struct PaBf {
 // channels 2 t, 2 t + 1 and + 8 of the product's step, which sums over them all, and
 // the queries are laid out to match.  A transposed 16-bit word holds two channels, the
 // even ones and the odd ones of 16 to a product.
-// The values' scales 2^v_e go into the weights, P = p 2^(v_e - E + 14), E the largest
-// v_e so far of entries that have a weight at all (log m above -inf); P as f16 and the
-// remainder's 2^11 as f16, so to 2^-22 of a weight, or 2^-50 of the largest value.
+// The values' scales 2^v_e go into the weights, P = p 2^(v_e - E + 14), E the power of two
+// at or above the largest p 2^(v_e) so far, so that a value counts by its weight too; P
+// as f16 and the remainder's 2^11 as f16, so to 2^-22 of a weight, or 2^-50 of the largest
+// p 2^(v_e).  2^E follows U, the largest log2 of p 2^(v_e) beside no reference.
 // (Values as bf16 with their scales took 8 clocks for two codes instead of 2, and the
 // kernel 73 us for 1M entries of d = 128.)
 template <int D>
@@ -335,7 +336,7 @@ struct PaE4 {
     using C = PaCfg<__nv_bfloat16, E4m3, D>;
     uint32_t qa[D / 16][2];     // queries in f16, channels 16 i + 4 t .. + 3
     float acc[D / 8][4];        // as PaBf's, columns: the even, then the odd channels of 16
-    float m, z;
+    float m, z, u;              // u: U
     int qe, ve;                 // the power of two taken from head hq's queries; E
 
     __device__ __forceinline__ void begin(const PaArgs &a, int s, int gq) {
@@ -368,7 +369,7 @@ struct PaE4 {
         for (int i = 0; i < D / 8; i++)
 #pragma unroll
             for (int j = 0; j < 4; j++) acc[i][j] = 0.f;
-        m = -INFINITY;
+        m = u = -INFINITY;
         z = 0.f;
     }
 
@@ -434,8 +435,8 @@ struct PaE4 {
             }
         }
         float y[NG][2][2], mx = -INFINITY;
-        int we[NG][2][2], top = ve;      // the values' scales; kOut: without a weight
-        constexpr int kOut = -1000;
+        float us = -INFINITY;
+        int we[NG][2][2];                // the values' scales
 #pragma unroll
         for (int g = 0; g < NG; g++)
 #pragma unroll
@@ -449,27 +450,24 @@ struct PaE4 {
                     // 2^(q + k_e), where it is a number: the logit is next to nothing below, out of range above
                     const int t = min(max(qe + (int)((k2 >> (8 * j)) & 255), 1), 254);
                     float v = x[g][n][j] * scale * __uint_as_float((uint32_t)t << 23);
-                    we[g][n][j] = in ? (int)((v2 >> (8 * j)) & 255) - 127 : kOut;
-                    if (has_lm) {
-                        const float l = j ? l2.y : l2.x;
-                        v += pa_lm2(l, most);
-                        if (l == -INFINITY) we[g][n][j] = kOut;
-                    }
+                    we[g][n][j] = (int)((v2 >> (8 * j)) & 255) - 127;
+                    if (has_lm) v += pa_lm2(j ? l2.y : l2.x, most);
                     y[g][n][j] = in ? v : -INFINITY;
-                    top = max(top, we[g][n][j]);
+                    us = fmaxf(us, y[g][n][j] + (float)we[g][n][j]);
                     mx = fmaxf(mx, y[g][n][j]);
                 }
             }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        if (__any_sync(0xffffffffu, mx > m || top != ve)) {
-            const float mn = fmaxf(m, mx);
-            float w = tc::ex2(m - pa_shift(mn));
+        us = fmaxf(us, __shfl_xor_sync(0xffffffffu, us, 1));
+        us = fmaxf(us, __shfl_xor_sync(0xffffffffu, us, 2));
+        if (__any_sync(0xffffffffu, mx > m || us > u)) {
+            const float mn = fmaxf(m, mx), by = m - pa_shift(mn);
             m = mn;
-            z *= w;
-            w *= __uint_as_float((uint32_t)max(0, 127 + ve - top) << 23);
+            u = fmaxf(u, us);
+            const int top = u == -INFINITY ? ve : min(max(__float2int_ru(u - pa_shift(mn)), -120), 119);
+            z *= tc::ex2(by);
+            const float w = tc::ex2(by + (float)(ve - top));
             ve = top;
 #pragma unroll
             for (int i = 0; i < D / 8; i++)
@@ -484,8 +482,9 @@ struct PaE4 {
             for (int n = 0; n < 2; n++) {
                 const float p0 = tc::ex2(y[g][n][0] - sh), p1 = tc::ex2(y[g][n][1] - sh);
                 z += p0 + p1;
-                const float v0 = p0 * __uint_as_float((uint32_t)max(0, 127 + 14 + we[g][n][0] - ve) << 23);
-                const float v1 = p1 * __uint_as_float((uint32_t)max(0, 127 + 14 + we[g][n][1] - ve) << 23);
+                // (2^(v_e - E) is a number where p is not 0)
+                const float v0 = p0 * 0x1p14f * __uint_as_float((uint32_t)min(max(0, 127 + we[g][n][0] - ve), 254) << 23);
+                const float v1 = p1 * 0x1p14f * __uint_as_float((uint32_t)min(max(0, 127 + we[g][n][1] - ve), 254) << 23);
                 const __half2 h = __floats2half2_rn(v0, v1);
                 const float2 f = __half22float2(h);
                 const __half2 r = __floats2half2_rn((v0 - f.x) * 2048.f, (v1 - f.y) * 2048.f);
