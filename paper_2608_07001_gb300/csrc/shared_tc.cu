@@ -46,7 +46,7 @@
 // which bounded a tile: 2700 of 5100 clocks).  With k_e, v_e the scales' exponents,
 //   K' = code 2^(k_e - k),  V' = code 2^(v_e - E),  y = S 2^q 2^k c,  O 2^E in the end,
 // k the largest k_e of the tile, E the largest v_e so far, of entries that have a
-// weight at all (no -inf), q the power of two that brings a row's queries into f16 (its
+// weight at all (no -inf, nor the lowest log m where there is another), q the power of two that brings a row's queries into f16 (its
 // largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
 // largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M), rounded once, has 11 bits,
 // at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     z *= w;
                     if (grow) m = top;
                     if (QUANT) {
-                        w *= __uint_as_float((uint32_t)max(0, 127 + ve - ve_new) << 23);
+                        w *= __uint_as_float((uint32_t)min(max(0, 127 + ve - ve_new), 254) << 23);       // (E falls beside w = 0 alone)
                         ve = ve_new;
                     }
                     if (any) {
@@ -618,6 +618,7 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             const float unscale = kLog2e / a.scale, most = kShMost / a.scale;       // sqrt(d)
             int top_ve = kNoScale;
             float piece_top = -INFINITY;
+            bool seen = false;
             Four cur = load(key_row(0));
 #pragma unroll 1
             for (int i = 1; i < kAhead; i++) fetch(key_row(i));
@@ -641,10 +642,25 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     in[i] = i < count && lm[i] != -INFINITY;
                     v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
                 }
+                const float top = fmaxf(max3(v[0], v[1], v[2]), v[3]);
+                if (QUANT) {
+                    // Beside an entry above the lowest log m those of it have no weight, nor a say in the scales; until there is one
+                    // they are what there is.
+                    if (!seen && __any_sync(0xffffffffu, top > -most)) {
+                        seen = true;
+                        top_ve = kNoScale;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (seen && v[i] <= -most) {
+                            v[i] = -INFINITY;
+                            in[i] = false;
+                        }
+                }
                 const bool special = __any_sync(0xffffffffu, count < 4);
                 // the piece's largest log m so far, by lane (of the softmax warps' two parts of one row tile together: an
                 // entry above the lowest in one of them has all of the weight beside the other's lowest)
-                piece_top = fmaxf(max3(piece_top, v[0], v[1]), fmaxf(v[2], v[3]));
+                piece_top = fmaxf(piece_top, top);
                 if (j == n - 1)
                     b.limit = (__any_sync(0xffffffffu, piece_top > -most) ? 0 : kLowest) | (__any_sync(0xffffffffu, piece_top >= most) ? kLargest : 0);
                 bool far = false;

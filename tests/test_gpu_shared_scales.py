@@ -192,3 +192,39 @@ def test_a_length_past_the_table(gk, dtype):
     assert e.value.status == gk.GKV_EINVAL
     want, tol = expected(q, a, p, [0, 2])
     assert ((out - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [3, 40])
+@pytest.mark.parametrize("way", ["some", "first", "last"])
+def test_large_rows_under_masks(gk, dtype, d, B, way):
+    # keys and values of any size under the lowest log m are as if they were not there: scattered, before all others of a
+    # sequence, behind them
+    low = torch.finfo(torch.float32).min
+    lens = np.array([[[900, 895]]])
+    table, n = R.scattered_table(np.random.default_rng(20), lens, 32)
+    out = torch.zeros(n * 32, dtype=torch.bool)
+    for h in range(2):
+        e = torch.arange(int(lens[0, 0, h]))
+        at = table[0, 0, h, e // 32].long() * 32 + e % 32
+        out[at[{"some": e % 7 == 3, "first": e < 300, "last": e >= 300}[way]]] = True
+
+    def edit(K, ks, V, vs, lm):
+        if lm.numel() != out.numel():
+            return None
+        vs.view(-1)[out] = 230
+        ks.view(-1)[out] += 3
+        lm.view(-1)[out] = low
+        return out
+
+    own = Side(gk, np.random.default_rng(21).integers(0, 40, (1, B, 2)), 16, 8, d, dtype, 22, lambda *a: None)
+    pre = Side(gk, lens, 32, 8, d, dtype, 20, edit)
+    assert torch.equal(pre.table, table)
+    q = queries(B, 8, d, dtype, 23)
+    f = gk.SharedAttention(own.cache, pre.cache)
+    got = f(0, q.cuda()).double().cpu()
+    f.status()
+    want, tol = expected(q, own, pre, [0, B])
+    assert torch.isfinite(got).all()
+    assert ((got - want).abs() <= tol).all(), f"{float(((got - want).abs() - tol).max()):.3e} over its bound"
