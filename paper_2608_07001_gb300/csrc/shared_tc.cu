@@ -619,9 +619,13 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
             int top_ve = kNoScale;
             float piece_top = -INFINITY;
             bool seen = false;
+            // This warp alone sees to every tile's words, one after another, and where requests fill one row tile of d = 64
+            // its steps are what bounds a tile: so rows are looked up once, and tiles all of whose entries count (ordinary)
+            // pass by what the others need.
             Four cur = load(key_row(0));
-#pragma unroll 1
-            for (int i = 1; i < kAhead; i++) fetch(key_row(i));
+            int next[kAhead - 1];                        // rows of the tiles from the next one on
+#pragma unroll
+            for (int i = 1; i < kAhead; i++) fetch(next[i - 1] = key_row(i));
             for (int j = 0; ok && j < n; j++) {
                 const int sl = j % NBIAS;
                 const Four f = cur;
@@ -629,62 +633,59 @@ __global__ void __launch_bounds__(Cfg<D, QUANT>::THREADS, 1)
                     now = after;
                     after = box_rows(++window + 1);
                 }
-                cur = load(key_row(j + 1));              // on its way: the next tile's words, a later one's into L2
-                fetch(key_row(j + kAhead));
+                cur = load(next[0]);                     // on its way: the next tile's words, a later one's into L2
+#pragma unroll
+                for (int i = 0; i < kAhead - 2; i++) next[i] = next[i + 1];
+                fetch(next[kAhead - 2] = key_row(j + kAhead));
                 ok = __all_sync(0xffffffffu, wait(&b.bempty[sl], ((j / NBIAS) & 1) ^ 1, b, a.status));
                 if (!ok) break;
                 const int count = f.row < 0 ? 0 : min(4, len - ((j0 + j) * NK + lane * 4));       // keys that are there
                 const float lm[4] = {f.lm.x, f.lm.y, f.lm.z, f.lm.w};
-                float v[4];
-                bool in[4];
+                float v[4] = {f.lm.x * unscale, f.lm.y * unscale, f.lm.z * unscale, f.lm.w * unscale};
+                const float low = fminf(fminf(v[0], v[1]), fminf(v[2], v[3]));
+                float top = fmaxf(max3(v[0], v[1], v[2]), v[3]);
+                const float any_nan = v[0] + v[1] + v[2] + v[3];
+                const bool ordinary = __all_sync(0xffffffffu, count >= 4 && low > -most && top < most && any_nan == any_nan);
+                bool special = false, far = false;
+                uint32_t counts = ~0u, gone = 0;         // bytes: of entries that count, of those that are not there
+                if (!ordinary) {
+                    special = __any_sync(0xffffffffu, count < 4);
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    in[i] = i < count && lm[i] != -INFINITY;
-                    v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(lm[i] * unscale, -most), most) : lm[i];
-                }
-                const float top = fmaxf(max3(v[0], v[1], v[2]), v[3]);
-                if (QUANT) {
-                    // Beside an entry above the lowest log m those of it have no weight, nor a say in the scales; until there is one
-                    // they are what there is.
-                    if (!seen && __any_sync(0xffffffffu, top > -most)) {
-                        seen = true;
-                        top_ve = kNoScale;
-                    }
+                    for (int i = 0; i < 4; i++) v[i] = i >= count ? -INFINITY : fabsf(lm[i]) <= FLT_MAX ? fminf(fmaxf(v[i], -most), most) : lm[i];
+                    top = fmaxf(max3(v[0], v[1], v[2]), v[3]);
+                    if (QUANT) {
+                        // Beside an entry above the lowest log m those of it have no weight, nor a say in the scales; until
+                        // there is one they are what there is.
+                        const bool beside = seen || __any_sync(0xffffffffu, top > -most);
+                        if (beside && !seen) top_ve = kNoScale;
+                        seen = beside;
+                        if (count < 4) gone = ~0u << 8 * max(count, 0);
 #pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (seen && v[i] <= -most) {
-                            v[i] = -INFINITY;
-                            in[i] = false;
+                        for (int i = 0; i < 4; i++) {
+                            if (seen && v[i] <= -most) v[i] = -INFINITY;
+                            if (v[i] == -INFINITY) counts &= ~(255u << 8 * i);
                         }
+                    }
+                } else if (QUANT && !seen) {
+                    seen = true;
+                    top_ve = kNoScale;
                 }
-                const bool special = __any_sync(0xffffffffu, count < 4);
                 // the piece's largest log m so far, by lane (of the softmax warps' two parts of one row tile together: an
                 // entry above the lowest in one of them has all of the weight beside the other's lowest)
                 piece_top = fmaxf(piece_top, top);
                 if (j == n - 1)
                     b.limit = (__any_sync(0xffffffffu, piece_top > -most) ? 0 : kLowest) | (__any_sync(0xffffffffu, piece_top >= most) ? kLargest : 0);
-                bool far = false;
                 if constexpr (QUANT) {                   // the rows' threads make the rest of it
-                    int kt = kNoScale, kb = kNoScale + 255, vt = kNoScale;
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        if (in[i]) {
-                            const int k = min((int)((f.ks >> (8 * i)) & 255) - 127, 119);
-                            kt = max(kt, k);
-                            kb = min(kb, k);
-                            vt = max(vt, min((int)((f.vs >> (8 * i)) & 255) - 127, 119));
-                        }
-                    kt = __reduce_max_sync(0xffffffffu, kt);
-                    far = __any_sync(0xffffffffu, kb < kt - kSpread) || abs(kt) > kMostK;
-                    top_ve = max(top_ve, __reduce_max_sync(0xffffffffu, vt));
+                    auto byte = [](uint32_t w, int i) { return (int)(w >> 8 * i & 255u); };
+                    auto largest = [&](uint32_t w) { return max(max(byte(w, 0), byte(w, 1)), max(byte(w, 2), byte(w, 3))); };
+                    const uint32_t kw = f.ks | ~counts;
+                    const int least = min(min(byte(kw, 0), byte(kw, 1)), min(byte(kw, 2), byte(kw, 3)));
+                    const int kb = (int)__reduce_max_sync(0xffffffffu, largest(f.ks & counts)), kt = min(kb, 246) - 127;
+                    top_ve = max(top_ve, min((int)__reduce_max_sync(0xffffffffu, largest(f.vs & counts)), 246) - 127);
+                    far = __any_sync(0xffffffffu, least < kb - kSpread) || abs(kt) > kMostK;
                     *reinterpret_cast<float4 *>(&b.lm[sl][lane * 4]) = make_float4(v[0], v[1], v[2], v[3]);
-                    uint32_t ks = f.ks, vs = f.vs;
-                    if (count < 4) {                     // bytes of kGone
-                        ks |= ~0u << 8 * max(count, 0);
-                        vs |= ~0u << 8 * max(count, 0);
-                    }
-                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = ks;
-                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = vs;
+                    *reinterpret_cast<uint32_t *>(&b.ke[sl][lane * 4]) = f.ks | gone;
+                    *reinterpret_cast<uint32_t *>(&b.ve[sl][lane * 4]) = f.vs | gone;
                     if (lane == 0) {
                         b.ktop[sl] = far ? kOwn : kt;
                         b.vtop[sl] = top_ve;
