@@ -42,8 +42,8 @@
 // Measured, GPU time: 88 us for 1M entries of 2 x 128 bf16 and log m (32 requests x 8
 // heads, uneven; 6.1 TB/s, 0.90 of a plain copy's rate), the same for one request of
 // 131072 entries; 6.1 us for one request of 8 x 256 entries (a call from Python
-// takes 8 to 11).  Quantised, half of the bytes: 58 us for those 1M entries (4.7 TB/s), 52 us
-// for one request's, bound by the latency of the consumers' chain of a tile (2450 clocks
+// takes 8 to 11).  Quantised, half of the bytes: 59 us for those 1M entries (4.6 TB/s), 54 us
+// for one request's, bound by the latency of the consumers' chain of a tile (about 2500 clocks
 // for 128 entries, two CTAs of four such warps a SM) and not by HBM.
 //
 // Of a shared prefix's requests (SHARED) the same kernel leaves (maximum, sum, weighted
@@ -328,7 +328,8 @@ struct PaBf {
 // The values' scales 2^v_e go into the weights, P = p 2^(v_e - E + 14), E the power of two
 // at or above the largest p 2^(v_e) so far, so that a value counts by its weight too; P
 // as f16 and the remainder's 2^11 as f16, so to 2^-22 of a weight, or 2^-50 of the largest
-// p 2^(v_e).  2^E follows U, the largest log2 of p 2^(v_e) beside no reference.
+// p 2^(v_e).  U is the largest log2 of that, E its integer above; both go by differences
+// from the maximum, as beside logits of any size a scale's exponent would be lost.
 // (Values as bf16 with their scales took 8 clocks for two codes instead of 2, and the
 // kernel 73 us for 1M entries of d = 128.)
 template <int D>
@@ -435,7 +436,6 @@ struct PaE4 {
             }
         }
         float y[NG][2][2], mx = -INFINITY;
-        float us = -INFINITY;
         int we[NG][2][2];                // the values' scales
 #pragma unroll
         for (int g = 0; g < NG; g++)
@@ -453,19 +453,29 @@ struct PaE4 {
                     we[g][n][j] = (int)((v2 >> (8 * j)) & 255) - 127;
                     if (has_lm) v += pa_lm2(j ? l2.y : l2.x, most);
                     y[g][n][j] = in ? v : -INFINITY;
-                    us = fmaxf(us, y[g][n][j] + (float)we[g][n][j]);
                     mx = fmaxf(mx, y[g][n][j]);
                 }
             }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float mn = fmaxf(m, mx), sh = pa_shift(mn);
+        float us = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < NG; g++)
+#pragma unroll
+            for (int n = 0; n < 2; n++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    y[g][n][j] -= sh;
+                    us = fmaxf(us, y[g][n][j] + (float)we[g][n][j]);
+                }
         us = fmaxf(us, __shfl_xor_sync(0xffffffffu, us, 1));
         us = fmaxf(us, __shfl_xor_sync(0xffffffffu, us, 2));
-        if (__any_sync(0xffffffffu, mx > m || us > u)) {
-            const float mn = fmaxf(m, mx), by = m - pa_shift(mn);
+        if (__any_sync(0xffffffffu, mn > m || us > u)) {
+            const float by = m - sh;
             m = mn;
-            u = fmaxf(u, us);
-            const int top = u == -INFINITY ? ve : min(max(__float2int_ru(u - pa_shift(mn)), -120), 119);
+            u = fmaxf(u + by, us);
+            const int top = u == -INFINITY ? ve : min(max(__float2int_ru(u), -120), 119);
             z *= tc::ex2(by);
             const float w = tc::ex2(by + (float)(ve - top));
             ve = top;
@@ -474,13 +484,12 @@ struct PaE4 {
 #pragma unroll
                 for (int j = 0; j < 4; j++) acc[i][j] *= w;
         }
-        const float sh = pa_shift(m);
         uint32_t hi[NG][2], lo[NG][2];
 #pragma unroll
         for (int g = 0; g < NG; g++) {
 #pragma unroll
             for (int n = 0; n < 2; n++) {
-                const float p0 = tc::ex2(y[g][n][0] - sh), p1 = tc::ex2(y[g][n][1] - sh);
+                const float p0 = tc::ex2(y[g][n][0]), p1 = tc::ex2(y[g][n][1]);
                 z += p0 + p1;
                 // (2^(v_e - E) is a number where p is not 0)
                 const float v0 = p0 * 0x1p14f * __uint_as_float((uint32_t)min(max(0, 127 + we[g][n][0] - ve), 254) << 23);

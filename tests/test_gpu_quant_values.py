@@ -53,3 +53,27 @@ def test_large_values_of_little_weight(gk, dtype, d, lm, by, every):
         got = out[b, g * 4:g * 4 + 4]
         assert torch.isfinite(got).all()
         assert ((got - want).abs() <= tol).all(), f"{float(((got - want).abs() / tol).max()):.3e} of its bound"
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lm", [torch.finfo(torch.float32).min, -1e30, -1e9, 3e6, 1e9])
+@pytest.mark.parametrize("by", [-90, -30, 30, 100])
+def test_values_beside_large_log_m(gk, dtype, lm, by):
+    # every entry as large a log m: equal weights, whatever the values' scales
+    lens = np.array([[[700, 130]]])
+    table, n = R.scattered_table(np.random.default_rng(4), lens, 16)
+    ((K, ks), (V, vs)), m = pages(5, n, 16, 64, spread=4.0)
+    K.view(torch.uint8).fill_(0)
+    vs.copy_((vs.int() + by).clamp(7, 246).to(torch.uint8))
+    m.fill_(lm)
+    q = torch.randn(1, 8, 64, generator=torch.Generator().manual_seed(6)).to(dtype)
+    c = gk.PagedCache(K.cuda(), V.cuda(), table.cuda(), torch.from_numpy(lens.astype(np.int32)).cuda(), log_m=m.cuda(), Hq=8,
+                      k_scale=ks.cuda(), v_scale=vs.cuda(), dtype=dtype)
+    out = c.attention(0, q.cuda()).double().cpu()
+    c.status()
+    for g in range(2):
+        v = R.entries(real(V, vs), table[0, 0, g], int(lens[0, 0, g])).double()
+        want, sure = v.mean(0), v.abs().mean(0)
+        tol = sure * (2.0 ** -16 + 2.0 ** -24 * (len(v) + 64)) + 2.0 ** -(8 if dtype == BF else 24) * want.abs() * 1.01
+        got = out[0, g * 4:g * 4 + 4]
+        assert torch.isfinite(got).all() and ((got - want).abs() <= tol).all()
