@@ -130,7 +130,8 @@ __device__ __forceinline__ void turn16(uint4 &a, uint4 &b, const float *cs, cons
 // Five blocks a SM (48 registers): 128 us at 32768 tokens of 48 rows; four 132 to
 // 146, six 139, eight (spills) 168.
 // QUANT: a row's lanes find its largest size together and store codes; one row in flight, for the same five blocks (186 us
-// of 4 rows with two in flight and four blocks, 178 this way).
+// of 4 rows with two in flight and four blocks, 178 this way; of 6 rows, read back, 171.8 though 21 registers are spilled,
+// 173.5 with four blocks, which spill none).
 template <typename T, int D, int R, bool QUANT>
 __global__ void __launch_bounds__(256, 5) paged_append_kernel(const AppendArgs a, const __grid_constant__ Turns turns) {
     constexpr int N = 16 / sizeof(T), CH = D / 2 / N, RB = D * sizeof(T), PB = QUANT ? D : RB;      // bytes of a pool row
@@ -272,14 +273,14 @@ struct LoadArgs {
 // as codes.  The row's lanes call it together.  Codes: two pieces a lane, as what a lane does for an entry bounds it.
 template <int BYTES>
 struct Plain {
-    static constexpr int RB = BYTES, P = 1, CH = RB / 16, BLOCKS = 8;
+    static constexpr int RB = BYTES, P = 1, CH = RB / 16;
     static __device__ __forceinline__ void put(char *pool, uint8_t *, int64_t row, int ch, const uint4 (&x)[P]) {
         st16(pool + row * RB + ch * 16, x[0]);
     }
 };
 template <typename T, int D>
 struct Quantised {
-    static constexpr int RB = D * sizeof(T), N = 16 / sizeof(T), P = 2, CH = RB / 32, BLOCKS = 8;
+    static constexpr int RB = D * sizeof(T), N = 16 / sizeof(T), P = 2, CH = RB / 32;
     static __device__ __forceinline__ void put(char *pool, uint8_t *scales, int64_t row, int ch, const uint4 (&x)[P]) {
         float u[2 * N];
         unpack16(x[0], reinterpret_cast<float(&)[N]>(u[0]));
@@ -331,9 +332,10 @@ __device__ __noinline__ void load_heads_disordered(const LoadArgs &a, int first)
 // then a warp copies a run of entries, 16 bytes of the key and of the value a
 // lane and IT times.  The head is searched for the run's first entry and
 // followed from there.  Eight blocks a SM: the registers that the call would take
-// otherwise leave room for six (1M entries of 2 x 256 bytes 163 us, 182 with 40).
+// otherwise leave room for six (1M entries of 2 x 256 bytes 163 us, 182 with 40; quantised,
+// with 25 of them spilled, and unloaded again 282.7 us, 287 with six).
 template <class W, int IT>
-__global__ void __launch_bounds__(256, W::BLOCKS) paged_load_kernel(const __grid_constant__ LoadArgs a) {
+__global__ void __launch_bounds__(256, 8) paged_load_kernel(const __grid_constant__ LoadArgs a) {
     constexpr int RB = W::RB, CH = W::CH, RW = CH < 32 ? 32 / CH : 1;         // entries a warp copies at once
     constexpr int U = IT < 4 ? IT : 4;
     next_may_start();

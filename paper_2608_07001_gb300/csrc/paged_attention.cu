@@ -156,11 +156,6 @@ __device__ __forceinline__ void pa_mma(float c[4], uint32_t a0, uint32_t a1, uin
 __device__ __forceinline__ void pa_zero16(uint32_t addr) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0) : "memory");
 }
-__device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 __device__ __forceinline__ void pa_bulk(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
@@ -283,8 +278,8 @@ struct PaBf {
         for (int n = 0; n < 2; n++) {
             const float p0 = tc::ex2(y[n][0] - sh), p1 = tc::ex2(y[n][1] - sh);
             z += p0 + p1;
-            hi[n] = pa_bf16x2(p0, p1);
-            lo[n] = pa_bf16x2(p0 - __uint_as_float(hi[n] << 16), p1 - __uint_as_float(hi[n] & 0xffff0000u));
+            hi[n] = bf16x2_of(p0, p1);
+            lo[n] = bf16x2_of(p0 - __uint_as_float(hi[n] << 16), p1 - __uint_as_float(hi[n] & 0xffff0000u));
         }
         // value rows past the length hold anything: 0 in the operand (words of entries 2 tq, 2 tq + 1 and + 8)
         uint32_t keep0 = ~0u, keep1 = ~0u;
@@ -374,12 +369,6 @@ struct PaE4 {
         z = 0.f;
     }
 
-    // Two codes as f16, exact.
-    static __device__ __forceinline__ uint32_t half2(uint32_t c) {
-        uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
-        return h;
-    }
     static __device__ __forceinline__ void mma_f16(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                                    uint32_t b1) {
         asm volatile(
@@ -431,8 +420,8 @@ struct PaE4 {
                 for (int n = 0; n < 2; n++)
 #pragma unroll
                     for (int i = 0; i < 2; i++)
-                        mma_f16(x[g][n], qa[c + i][0], qa[c + i][0], qa[c + i][1], qa[c + i][1], half2(b[2 * n + i] & 0xffffu),
-                                half2(b[2 * n + i] >> 16));
+                        mma_f16(x[g][n], qa[c + i][0], qa[c + i][0], qa[c + i][1], qa[c + i][1], f16x2_codes(b[2 * n + i] & 0xffffu),
+                                f16x2_codes(b[2 * n + i] >> 16));
             }
         }
         float y[NG][2][2], mx = -INFINITY;
@@ -511,8 +500,8 @@ struct PaE4 {
                 for (int k = 0; k < 2; k++) {
                     // bytes (entry 0, channels 0 1), (entry 1, channels 0 1) -> channel 0 of both, channel 1 of both
                     const uint32_t c0 = __byte_perm(b[2 * k], 0, 0x3120), c1 = __byte_perm(b[2 * k + 1], 0, 0x3120);
-                    mma_f16(acc[2 * (i + k)], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 & 0xffffu), half2(c1 & 0xffffu));
-                    mma_f16(acc[2 * (i + k) + 1], hi[g][0], lo[g][0], hi[g][1], lo[g][1], half2(c0 >> 16), half2(c1 >> 16));
+                    mma_f16(acc[2 * (i + k)], hi[g][0], lo[g][0], hi[g][1], lo[g][1], f16x2_codes(c0 & 0xffffu), f16x2_codes(c1 & 0xffffu));
+                    mma_f16(acc[2 * (i + k) + 1], hi[g][0], lo[g][0], hi[g][1], lo[g][1], f16x2_codes(c0 >> 16), f16x2_codes(c1 >> 16));
                 }
             }
         }

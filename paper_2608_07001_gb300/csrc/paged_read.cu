@@ -170,49 +170,32 @@ __global__ void __launch_bounds__(1024) paged_offsets_kernel(const UnloadArgs a)
     if (bad) atomicOr(a.status, kStRange);
 }
 
-// A thread: two pieces of 16 bytes of the key's row and of the value's row of IT entries.
-template <typename T, typename S, int D, int IT>
+// A thread: two pieces of 16 bytes of the key's row and of the value's row of one entry.
+template <typename T, typename S, int D>
 __global__ void __launch_bounds__(256) paged_unload_kernel(const UnloadArgs a) {
     using X = Row<T, S, D>;
-    constexpr int CH = X::CH, RB = D * sizeof(T), RW = 32 / CH;          // entries a warp takes at once
+    constexpr int CH = X::CH, RB = D * sizeof(T);
     next_may_start();
     after_previous();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int heads = a.c.L * a.c.G, lane = threadIdx.x & 31, ch = lane % CH;
-    const int64_t e0 = (i >> 5) * (RW * IT) + lane / CH;
+    const int heads = a.c.L * a.c.G, ch = (int)(i % CH);
+    const int64_t e = i / CH;
+    if (e >= a.n_entries) return;
     int h = 0, hi = heads;
     while (hi - h > 1) {
         const int mid = (h + hi) >> 1;
-        if (a.off[mid] <= e0) h = mid; else hi = mid;
+        if (a.off[mid] <= e) h = mid; else hi = mid;
     }
-    int64_t o0 = a.off[h], o1 = a.off[h + 1];
-    typename X::Raw x[IT], y[IT];
-    int64_t row[IT];
-    bool in[IT];
-#pragma unroll
-    for (int k = 0; k < IT; k++) {
-        const int64_t e = e0 + (int64_t)k * RW;
-        row[k] = -1;
-        while (e >= o1 && h + 1 < heads) {
-            h++;
-            o0 = a.off[h];
-            o1 = a.off[h + 1];
-        }
-        in[k] = e < a.n_entries && e >= o0 && e < o1;
-        if (!in[k]) continue;
-        row[k] = entry_row(a.c, ((int64_t)(h / a.c.G) * a.c.B + a.b) * a.c.G + h % a.c.G, (int)(e - o0), a.status);
-        if (row[k] < 0) continue;
-        x[k] = X::load(a.c.K, a.scales.k, row[k], ch);
-        y[k] = X::load(a.c.V, a.scales.v, row[k], ch);
+    if (e >= a.off[h + 1]) return;                       // past the request's last one
+    const int64_t row = entry_row(a.c, ((int64_t)(h / a.c.G) * a.c.B + a.b) * a.c.G + h % a.c.G, (int)(e - a.off[h]), a.status);
+    typename X::Raw x, y;
+    if (row >= 0) {
+        x = X::load(a.c.K, a.scales.k, row, ch);
+        y = X::load(a.c.V, a.scales.v, row, ch);
     }
-#pragma unroll
-    for (int k = 0; k < IT; k++) {
-        if (!in[k]) continue;
-        const int64_t e = e0 + (int64_t)k * RW;
-        X::put(a.K + e * RB, ch, x[k], row[k] >= 0);
-        X::put(a.V + e * RB, ch, y[k], row[k] >= 0);
-        if (ch == 0 && a.log_m) a.log_m[e] = row[k] >= 0 && a.c.log_m ? a.c.log_m[row[k]] : 0.f;
-    }
+    X::put(a.K + e * RB, ch, x, row >= 0);
+    X::put(a.V + e * RB, ch, y, row >= 0);
+    if (ch == 0 && a.log_m) a.log_m[e] = row >= 0 && a.c.log_m ? a.c.log_m[row] : 0.f;
 }
 
 template <typename T, typename S, int D>
@@ -225,10 +208,7 @@ template <typename T, typename S, int D>
 cudaError_t launch_unload(const UnloadArgs &a, cudaStream_t s) {
     cudaError_t e = launch_overlapped(paged_offsets_kernel, 1, 1024, 0, s, a);
     if (e != cudaSuccess || a.n_entries == 0) return e;
-    constexpr int IT = 1;
-    constexpr int64_t run = 32 / Row<T, S, D>::CH * IT;                  // entries of a warp
-    return launch_overlapped(paged_unload_kernel<T, S, D, IT>, (unsigned)(((a.n_entries + run - 1) / run * 32 + 255) / 256), 256,
-                             0, s, a);
+    return launch_overlapped(paged_unload_kernel<T, S, D>, (unsigned)((a.n_entries * Row<T, S, D>::CH + 255) / 256), 256, 0, s, a);
 }
 
 // f(rows' type, pools' type, channels) of a cache.

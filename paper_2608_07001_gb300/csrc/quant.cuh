@@ -44,10 +44,14 @@ __device__ __forceinline__ uint32_t codes4(const float *x, float inv) {
     return codes2(x[0], x[1], inv) | codes2(x[2], x[3], inv) << 16;
 }
 
-// The two codes in the low half of c as numbers.
-__device__ __forceinline__ float2 values2(uint32_t c) {
+// The two codes in the low half of c, as f16 (exact) and as numbers.
+__device__ __forceinline__ uint32_t f16x2_codes(uint32_t c) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+    return h;
+}
+__device__ __forceinline__ float2 values2(uint32_t c) {
+    const uint32_t h = f16x2_codes(c);
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 

@@ -166,8 +166,7 @@ __device__ __forceinline__ uint32_t f16x2_of(float lo, float hi) {
 }
 // Two codes as f16 times a scale.
 __device__ __forceinline__ uint32_t half2_of(uint32_t c, __half2 s) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+    const uint32_t h = f16x2_codes(c);
     const __half2 x = __hmul2(*reinterpret_cast<const __half2 *>(&h), s);
     return *reinterpret_cast<const uint32_t *>(&x);
 }
