@@ -6,9 +6,9 @@ import pytest
 import torch
 
 from . import serving_reference as R
-from .test_gpu_quant_attention import junk, pages
-from .test_gpu_shared import BF, F32, queries
-from .test_gpu_shared_scales import Side
+from .test_gpu_quant_attention import junk, pages, real
+from .test_gpu_shared import BF, F32, KINDS, queries
+from .test_gpu_shared_scales import Side, no_zeros
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,35 @@ def test_nan_in_quantised_prefixes(gk, dtype):
     assert torch.isnan(out[2:, 2:, 11]).all() and torch.isnan(out[3, 3]).all()
     keep = torch.arange(64) != 11
     assert torch.isfinite(out[2, 2:, keep]).all() and torch.isfinite(out[3, 2, keep]).all()
+
+
+@pytest.mark.parametrize("dtype,quant,wide", [(*k, False) for k in KINDS] + [(BF, True, True), (F32, True, True)])
+@pytest.mark.parametrize("B", [3, 40])
+@pytest.mark.parametrize("lm", [math.nan, math.inf])
+def test_log_m_that_is_no_number(gk, dtype, quant, wide, B, lm):
+    # in a prefix it makes its head NaN for all requests, in a request's own entries for that one; with keys of scales close
+    # together and far apart, and whatever its page neighbours hold
+    lens = np.array([[[300, 300]]])
+    table, count = R.scattered_table(np.random.default_rng(12), lens, 16)
+    ((K, ks), (V, vs)), m = pages(13, count, 16, 64)
+    no_zeros(K, ks, V, vs, m)
+    if wide:
+        ks.view(-1)[::50] = 80
+    for at in (299, 20):
+        g = torch.Generator().manual_seed(at)
+        own_m = torch.rand(B * 2, 16, generator=g)
+        own_m[2 * (B - 1) + 1, 3] = lm
+        pre_m = m.clone()
+        pre_m[table[0, 0, 0, at // 16], at % 16] = lm
+        sc = dict(k_scale=ks.cuda(), v_scale=vs.cuda(), dtype=dtype) if quant else {}
+        Kp, Vp = (K, V) if quant else (real(K, ks).to(dtype), real(V, vs).to(dtype))
+        i32 = dict(dtype=torch.int32, device="cuda")
+        prefix = gk.PagedCache(Kp.cuda(), Vp.cuda(), table.cuda(), torch.from_numpy(lens.astype(np.int32)).cuda(), Hq=4,
+                               log_m=pre_m.cuda(), **sc)
+        x = torch.randn(2, B * 2, 16, 64, generator=g).to(dtype).cuda()
+        own = gk.PagedCache(x[0], x[1], torch.arange(B * 2, **i32).view(1, B, 2, 1), torch.full((1, B, 2), 9, **i32), Hq=4,
+                            log_m=own_m.cuda())
+        f = gk.SharedAttention(own, prefix)
+        out = f(0, queries(B, 4, 64, dtype, 14).cuda()).cpu()
+        f.status()
+        assert torch.isnan(out[:, :2]).all() and torch.isfinite(out[:B - 1, 2:]).all() and torch.isnan(out[B - 1, 2:]).all()
