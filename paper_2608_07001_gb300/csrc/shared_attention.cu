@@ -110,7 +110,8 @@ template <typename T, int D>
 cudaError_t launch_join(const SharedArgs &a, void *out, cudaStream_t s) {
     const int reqs = kJoinRows / (a.c.Hq / a.c.G);
     const dim3 grid((unsigned)(((a.B + reqs - 1) / reqs) * a.c.G), D / 4 / kJoinC4);
-    const bool many = (int64_t)a.pieces * shared_halves(sizeof(T) == 2) > 8 * (int64_t)a.blocks;       // parts of a row
+    // whether a row can have more than eight parts: by the room for them, as the plan's own number is on the device
+    const bool many = (int64_t)a.pieces * shared_halves(sizeof(T) == 2) > 8 * (int64_t)a.blocks;
     return launch_overlapped(many ? shared_join_kernel<T, D, 16> : shared_join_kernel<T, D, 8>, grid, kJoinThreads, 0, s, a,
                              static_cast<T *>(out));
 }

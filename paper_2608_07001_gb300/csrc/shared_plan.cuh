@@ -11,8 +11,8 @@ namespace gkv {
 namespace serve {
 
 constexpr int kPlanBlocks = 512;           // blocks that are kept in shared memory too
-// What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured (shared_tc.cu) 1.64 and 1.42 times as much
-// for bf16 of d = 128, in L2 and from HBM, 1.6 to 1.8 for the others.
+// What a key tile costs: of one row tile, and (SharedArgs::two) of two.  Measured (shared_tc.cu) 1.68 and 1.43 times as much
+// for bf16 of d = 128, in L2 and from HBM, 1.55 to 1.8 for the others.
 constexpr int kPlanOne = 4, kPlanTwoWide = 6, kPlanTwo = 7;
 constexpr int kPlanSearch = 64;            // blocks up to which lengths are compared, for as many pieces as run at once
 

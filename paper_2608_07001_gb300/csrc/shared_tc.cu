@@ -22,10 +22,10 @@
 // products of 128^3; many: by the chain product, exponentials, product of a row tile, of
 // which TMEM holds two.  us a key tile and SM, pages of 64 entries, log m; in L2 / from HBM:
 //                      one row tile     two row tiles
-//   bf16       d = 64  0.97 / 1.10      1.72 / 1.76
-//              d = 128 1.33 / 1.61      2.18 / 2.28       (64 KB in 1.61 us: 6.2 TB/s of all SMs)
-//   quantised  d = 64  1.02 / 1.12      1.74 / 1.78
-//              d = 128 1.39 / 1.56      2.22 / 2.54
+//   bf16       d = 64  0.96 / 1.07      1.73 / 1.76
+//              d = 128 1.32 / 1.60      2.22 / 2.28       (64 KB in 1.60 us: 6.2 TB/s of all SMs)
+//   quantised  d = 64  0.99 / 1.10      1.77 / 1.81
+//              d = 128 1.40 / 1.55      2.17 / 2.52
 // Pages of 16 entries, each box of which is a copy of its own: 1.3 to 1.4, 2.1 to 2.4 (bf16, d = 128) and as above.
 // A piece takes about 10 us beside its tiles.
 //
@@ -36,9 +36,9 @@
 // the K step of log m.
 // A and B of a product have one type, so P goes as its bf16 part and the remainder's, two
 // parts (2^-16 of a weight, as the own entries'), each half of them in the columns of its own
-// scores.  Rounded once, a key tile of two row tiles took 1.54 us instead of 2.18 (d = 128) and
-// 1.44 instead of 1.72 (d = 64), of one 1.19 instead of 1.33 and 0.79 instead of 0.97, 1.59
-// instead of 1.61 from HBM; but outputs were 2.2 to 2.4e-3 from 64 bits, where rounding them
+// scores.  Rounded once, a key tile of two row tiles took 1.54 us instead of 2.2 (d = 128) and
+// 1.44 instead of 1.7 (d = 64), of one 1.19 instead of 1.32 and 0.79 instead of 0.96, from HBM
+// 1.59 as it does; but outputs were 2.2 to 2.4e-3 from 64 bits, where rounding them
 // makes 1.65e-3.
 //
 // Quantised pages: codes come through a ring of their own, and two warpgroups more
@@ -49,7 +49,9 @@
 // weight at all (no -inf, nor the lowest log m where there is another), q the power of two that brings a row's queries into f16 (its
 // largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
 // largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M), rounded once, has 11 bits,
-// at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.
+// at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.  (A remainder's part beside
+// it, as of bf16: 75 requests of five contexts 135.6 us instead of 111.3, for a rounding an
+// eighth of the output's.)
 // Where that would cost keys their bits (k_e that lie further apart in a tile) or log m beside
 // q and k is no number (they are beyond 2^30 and 2^40), K' = code and the softmax warps make
 // y = S 2^q 2^(k_e) c + log m from the scores themselves, with 128 reads of shared memory.

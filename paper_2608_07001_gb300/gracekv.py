@@ -807,7 +807,8 @@ class PagedCache(_Workspace):
     def unload_packed(self, b: int, n_entries: int, out=None, stream=None):
         """Request b's entries, at most n_entries, as a packed cache: (K, V [n_entries, d]
         of `dtype`, log_m [n_entries], offsets [L G + 1] int64), new or the four tensors
-        `out`.  What load_packed takes; the pages stay as they are."""
+        `out`.  What load_packed takes, but that a cache without log m gives zeros for it
+        and loads with None.  The pages stay as they are."""
         dev, E, n1 = self._device, n_entries, self.L * self.G + 1
         if not 0 <= b < self.B or not 0 <= E < 1 << 31:
             raise _bad(f"request {b} of {self.B}, {E} entries")
@@ -986,6 +987,11 @@ class SharedAttention(_Workspace):
     cache holds the requests' own entries, prefix (a PagedCache of the same L, G, Hq,
     d and dtype; either may be quantised) one prefix a slot, read once for all the
     requests that share it.  One object holds the workspace of one stream.
+
+    Three launches: for bf16 rows worth it from about 50000 requests x prefix entries
+    of a KV head on (32 heads, 8 of KV), for fp32 from 32 requests on 1024 entries, 16
+    on 4096, 8 on longer ones.  Below, PagedCache.attention over tables that begin with
+    the prefix's pages is faster.
     """
 
     def __init__(self, cache: PagedCache, prefix: PagedCache):
