@@ -706,10 +706,10 @@ gkv_status gracekv_paged_status(void *workspace, void *stream);
  * that are not followed; the others are computed.
  * Values: as gracekv_paged_attention, but for bf16 rows over a quantised prefix
  * its entries' weights are rounded to f16 for the value product (their sum is
- * not), and values of less than 2^-33 of the largest one that has a weight count 0.
- * Keys count whatever their scales, and over quantised
- * pages logits of fp32 queries above 2^100 in size are open.  A log m of more than
- * 2^40 ln 2 in size counts as that.
+ * not), and values of less than 2^-33 of the largest one count 0 (of entries of log
+ * m above -inf, and above the lowest where there is one).  Keys count whatever their
+ * scales, and logits compare whatever their size; over quantised pages those of fp32
+ * queries above 2^100 are open.  A log m of more than 2^40 ln 2 in size counts as that.
  */
 
 /* Bytes of the device workspace: a function of both caches' L, B, G, Hq, d and

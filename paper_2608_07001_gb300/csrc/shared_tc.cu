@@ -46,12 +46,13 @@
 // which bounded a tile: 2700 of 5100 clocks).  With k_e, v_e the scales' exponents,
 //   K' = code 2^(k_e - k),  V' = code 2^(v_e - E),  y = S 2^q 2^k c,  O 2^E in the end,
 // k the largest k_e of the tile, E the largest v_e so far, of entries that have a
-// weight at all (no -inf, nor the lowest log m where there is another), q the power of two that brings a row's queries into f16 (its
-// largest to 2^14, exact down to 2^-38 of that).  Codes stay exact down to 2^-15 of the
-// largest scale and go to 0 at 2^-33 of the largest value.  P = 2^(y - M), rounded once, has 11 bits,
-// at most 2^15 and exact to 2^-29 of that, its last bit 2^-39 of it.  (A remainder's part beside
-// it, as of bf16: 75 requests of five contexts 135.6 us instead of 111.3, for a rounding an
-// eighth of the output's.)
+// weight at all (no -inf, nor the lowest log m where there is another), q the power of
+// two that brings a row's queries into f16 (its largest to 2^14, exact down to 2^-38 of
+// that).  Codes stay exact down to 2^-15 of the largest scale and go to 0 at 2^-33 of the
+// largest value.  P = 2^(y - M), rounded once, has 11 bits, at most 2^15 and exact to
+// 2^-29 of that, its last bit 2^-39 of it.  (A remainder's part beside it, as of bf16: 75
+// requests of five contexts 135.6 us instead of 111.3, for a rounding an eighth of the
+// output's.)
 // Where that would cost keys their bits (k_e that lie further apart in a tile) or log m beside
 // q and k is no number (they are beyond 2^30 and 2^40), K' = code and the softmax warps make
 // y = S 2^q 2^(k_e) c + log m from the scores themselves, with 128 reads of shared memory.
